@@ -399,6 +399,141 @@ size_t fa_noalloc_scratch_bytes(void);   /* FA_NOALLOC_SCRATCH_BYTES as built in
  * detail is not NULL) and clears the word.  Allocates nothing.  The word is shared by all calls, like the array. */
 fa_status fa_noalloc_last_status(uint32_t* detail);
 
+/*
+ * Paged key/value cache.  (The paper has no counterpart: serving keeps the keys and values of many growing sequences
+ * in pages of a pool instead of one contiguous tensor per sequence.)
+ *
+ * Key j of sequence b lives in slot j % page_size of page block_table[b][j / page_size].  The pool is two tensors, logically
+ *     k [num_pages, Hkv, page_size, dqk]      v [num_pages, Hkv, page_size, dv]
+ * with any order of the first three dimensions in memory: element (p, h, s, c) sits at p*strides[0] + h*strides[1] +
+ * s*strides[2] + c (strides in elements, 64-bit).  A page may appear in several sequences (a shared prefix).
+ *   type     FA_CACHE_BF16, or FA_CACHE_E4M3: one-byte values with one fp32 scale per K/V head,
+ *            K = k_scale[h] * code, V = v_scale[h] * code (DEVICE arrays of Hkv positive numbers; NULL = 1).
+ *   k, v     DEVICE pointers, 16-byte aligned; every stride a positive multiple of 16 bytes, strides[2] >= the head size.
+ *   page_size  a multiple of 16, at most 65536.
+ *   (dqk, dv)  as for fa_forward.
+ * Set struct_size = sizeof(fa_paged_cache).
+ */
+#define FA_CACHE_BF16 0
+#define FA_CACHE_E4M3 1
+typedef struct fa_paged_cache {
+    uint32_t struct_size;
+    int32_t type;
+    void* k;
+    void* v;
+    int32_t num_pages, page_size, Hkv, dqk, dv;
+    int32_t reserved;             /* 0 */
+    int64_t k_strides[3];         /* page, head, slot */
+    int64_t v_strides[3];
+    const float* k_scale;
+    const float* v_scale;
+} fa_paged_cache;
+
+/*
+ * The sequences of a call: block_table is a DEVICE array of int32 [B, max_pages] with rows table_stride elements apart
+ * (entries that no key of a sequence needs are never read), seq_lens a DEVICE array of B int32: the number of keys of each
+ * sequence, the tokens of this step INCLUDED.  The host never reads them, so a captured call can be replayed with new
+ * contents.  What the host cannot check the kernels do: a length that is negative or needs more than max_pages pages, a
+ * page number outside the pool and a position past the rotation table make fa_last_status return FA_ERR_INVALID_ARG; nothing
+ * out of range is read or written, and the outputs of the sequences concerned are unspecified.
+ */
+typedef struct fa_paged_seqs {
+    uint32_t struct_size;         /* sizeof(fa_paged_seqs) */
+    int32_t B;
+    const int32_t* block_table;
+    int64_t table_stride;         /* >= max_pages */
+    const int32_t* seq_lens;
+    int32_t max_pages;
+    int32_t reserved;             /* 0 */
+} fa_paged_seqs;
+
+/*
+ * Rotation by position: of every `span` dimensions of a head (span divides dqk; a head of two maps of 64 has span 64) the
+ * dimensions [offset, offset + dim) are turned in pairs (x1, x2) -> (x1 cos - x2 sin, x2 cos + x1 sin); pair i is
+ * (offset + i, offset + i + dim/2), or with interleaved != 0 (offset + 2i, offset + 2i + 1).  cos_sin is a DEVICE array
+ * [max_pos, dim] of fp32: row p holds the dim/2 cosines, then the dim/2 sines of position p.  dim and span are multiples of
+ * 16, offset a multiple of 8.
+ */
+typedef struct fa_rope {
+    uint32_t struct_size;         /* sizeof(fa_rope) */
+    int32_t max_pos;
+    const float* cos_sin;         /* 16-byte aligned */
+    int32_t dim, offset, span, interleaved;
+} fa_rope;
+
+/*
+ * Appends the keys and values of new tokens to a paged cache, rotating the keys (and, where Q is given, the queries of the
+ * same tokens) by their positions on the way.  The tokens of the sequences are packed: sequence b owns rows
+ * [cu_seqlens[b], cu_seqlens[b+1]) of K [total, Hkv, dqk], V [total, Hkv, dv], Q and Q_out [total, Hq, dqk] (bf16 DEVICE
+ * tensors, 16-byte aligned, {token, head} strides in elements, multiples of 8, so that slices of one projection's output
+ * can be passed as they are).  cu_seqlens is a DEVICE array of B+1 int32, non-decreasing from 0, or NULL: every sequence has
+ * total / B rows (B divides total).  Token i of the n new ones of sequence b has position seq_lens[b] - n + i, which
+ * picks the row of the rotation table and the slot.  Tokens whose position would be negative (the padding of a batch: length
+ * 0) and rows behind cu_seqlens[B] are skipped: nothing is stored for them, their rows of Q_out stay as they were.
+ *   rope    NULL = no rotation (Q is then copied).      Q, Q_out   both or neither NULL; Q_out may be Q itself.
+ * Arithmetic is fp32 with one rounding to bf16, or of value / scale to e4m3 (saturating at +-448).  A slot that two tokens of
+ * a call name (sequences sharing a page that is written to) ends with either's values.  Asynchronous on `stream`.
+ */
+fa_status fa_append_paged(fa_handle* h, const fa_paged_cache* cache, const fa_paged_seqs* seqs,
+                          const int32_t* cu_seqlens, int total,
+                          const void* K, const void* V, const void* Q, void* Q_out, int Hq,
+                          const int64_t* k_strides, const int64_t* v_strides,
+                          const int64_t* q_strides, const int64_t* qo_strides,
+                          const fa_rope* rope, void* stream);
+
+/*
+ * Attention of the last Sq tokens of every sequence (1 <= Sq <= FA_PAGED_MAX_SQ; one in ordinary decoding) over a paged
+ * cache that holds their keys and values already.  Q [B*Sq, Hq, dqk] and O [B*Sq, Hq, dv] are bf16 DEVICE tensors,
+ * 16-byte aligned, with {token, head} strides in elements, multiples of 8; lse is fp32 [Hq, B*Sq] or NULL.  Token i of
+ * sequence b sees the keys j <= seq_lens[b] - Sq + i.  A token that sees no key (length 0, or less than its place among the new
+ * tokens) gets O = 0 and lse = -inf.  Slots past a sequence's length take no part, whatever they hold.  Scores, softmax state
+ * and both accumulators are fp32; the probabilities enter the second product as bf16, and over an e4m3 cache as the sum of three
+ * 8-bit terms (at least 9 significant bits), the queries as such a sum too (exact for entries within 2^-22 of the head's
+ * largest).  scale as for fa_forward.
+ * One launch: the K/V tiles of all sequences are dealt out evenly over the SMs on the device and the pieces of a
+ * sequence are joined by the SM that finishes last, in a fixed order, so equal calls give equal bits.  The partial results use the
+ * handle's scratch buffer, under the rule of fa_forward: launches through one handle must not overlap on the device.  Scratch
+ * smaller than two partials per SM: FA_ERR_UNSUPPORTED.
+ */
+#define FA_PAGED_MAX_SQ 16
+fa_status fa_forward_paged(fa_handle* h, const fa_paged_cache* cache, const fa_paged_seqs* seqs,
+                           const void* Q, void* O, float* lse, int Hq, int Sq, float scale,
+                           const int64_t* q_strides, const int64_t* o_strides, void* stream);
+
+/*
+ * Differential attention: a head's queries and keys are two halves of dqk/2 = 64 dimensions, q = [q1 | q2], k = [k1 | k2],
+ * and its result is the difference of two softmax maps over the same values (dv = 128),
+ *     Y = ( softmax(scale q1 k1^T) - lambda[hq] softmax(scale q2 k2^T) ) V
+ *     O = out_scale * weight (*) Y / sqrt(mean_c(Y_c^2) + eps)       (weight NULL: O = out_scale * Y)
+ * with the normalisation over the dv values of a head.  lambda: DEVICE fp32 [Hq]; weight: DEVICE fp32 [dv], 16-byte aligned; eps > 0;
+ * a scale of 0 selects 1/sqrt(64).  Set struct_size = sizeof(fa_diff).
+ */
+typedef struct fa_diff {
+    uint32_t struct_size;
+    float eps;
+    const float* lambda;
+    const float* weight;
+    float out_scale;
+    float reserved;               /* 0 */
+} fa_diff;
+
+/* Differential attention over whole prompts: tensors, strides, mask and errors as for fa_forward_strided with
+ * dqk = dv = 128.  A row that sees no key gets O = 0. */
+fa_status fa_forward_diff(fa_handle* h, const void* Q, const void* K, const void* V, void* O,
+                          int B, int Hq, int Hkv, int Sq, int Sk, int dqk, int dv, int causal, float scale,
+                          const fa_diff* diff,
+                          const int64_t* q_strides, const int64_t* k_strides,
+                          const int64_t* v_strides, const int64_t* o_strides, void* stream);
+
+/* Differential attention of the last Sq tokens of every sequence over a paged cache; everything else as for fa_forward_paged
+ * with dqk = dv = 128. */
+fa_status fa_forward_paged_diff(fa_handle* h, const fa_paged_cache* cache, const fa_paged_seqs* seqs,
+                                const void* Q, void* O, int Hq, int Sq, float scale, const fa_diff* diff,
+                                const int64_t* q_strides, const int64_t* o_strides, void* stream);
+
+/* CUDA device ordinal that the handle is bound to (-1 for NULL). */
+int fa_device(const fa_handle* h);
+
 #ifdef __cplusplus
 }
 #endif

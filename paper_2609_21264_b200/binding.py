@@ -34,7 +34,11 @@ FA_FLAG_QUAD_KERNEL = 1024
 
 EXPORTS = ("fa_create", "fa_forward", "fa_forward_strided", "fa_forward_varlen", "fa_forward_fp8", "fa_forward_mxfp8", "fa_plan", "fa_forward_host", "fa_last_status", "fa_destroy",
            "fa_strerror", "fa_launch_count", "fa_last_kernel_name", "fa_last_kv_splits",
-           "fa_forward_split_noalloc", "fa_noalloc_scratch_bytes", "fa_noalloc_last_status", "fa_debug_set_drop_v_load")
+           "fa_forward_split_noalloc", "fa_noalloc_scratch_bytes", "fa_noalloc_last_status", "fa_debug_set_drop_v_load",
+           "fa_append_paged", "fa_forward_paged", "fa_forward_paged_diff", "fa_forward_diff", "fa_device")
+FA_CACHE_BF16 = 0
+FA_CACHE_E4M3 = 1
+FA_PAGED_MAX_SQ = 16
 
 
 class FaError(RuntimeError):
@@ -49,6 +53,31 @@ class fa_config(ctypes.Structure):
                 ("kv_splits", ctypes.c_uint32), ("scratch_bytes", ctypes.c_uint64)]
 
 
+class fa_paged_cache(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("type", ctypes.c_int32), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("dqk", ctypes.c_int32),
+                ("dv", ctypes.c_int32), ("reserved", ctypes.c_int32), ("k_strides", ctypes.c_int64 * 3),
+                ("v_strides", ctypes.c_int64 * 3), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class fa_paged_seqs(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("B", ctypes.c_int32), ("block_table", ctypes.c_void_p),
+                ("table_stride", ctypes.c_int64), ("seq_lens", ctypes.c_void_p), ("max_pages", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+class fa_rope(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("max_pos", ctypes.c_int32), ("cos_sin", ctypes.c_void_p),
+                ("dim", ctypes.c_int32), ("offset", ctypes.c_int32), ("span", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+
+
+class fa_diff(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("eps", ctypes.c_float), ("lambda_", ctypes.c_void_p),
+                ("weight", ctypes.c_void_p), ("out_scale", ctypes.c_float), ("reserved", ctypes.c_float)]
+
+
+_I64x2 = ctypes.c_int64 * 2
+_I64x3 = ctypes.c_int64 * 3
 _lib = None
 
 
@@ -107,6 +136,16 @@ def load():
     lib.fa_noalloc_scratch_bytes.argtypes = []
     lib.fa_debug_set_drop_v_load.restype = i32
     lib.fa_debug_set_drop_v_load.argtypes = [vp, i32]
+    lib.fa_append_paged.restype = i32
+    lib.fa_append_paged.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp]
+    lib.fa_forward_paged.restype = i32
+    lib.fa_forward_paged.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, f32, vp, vp, vp]
+    lib.fa_forward_paged_diff.restype = i32
+    lib.fa_forward_paged_diff.argtypes = [vp, vp, vp, vp, vp, i32, i32, f32, vp, vp, vp, vp]
+    lib.fa_forward_diff.restype = i32
+    lib.fa_forward_diff.argtypes = [vp] * 5 + [i32] * 8 + [f32] + [vp] * 6
+    lib.fa_device.restype = i32
+    lib.fa_device.argtypes = [vp]
     lib.fa_noalloc_last_status.restype = i32
     lib.fa_noalloc_last_status.argtypes = [ctypes.POINTER(ctypes.c_uint32)]
     _lib = lib
@@ -341,3 +380,247 @@ def forward_mxfp8(h, q8, k8, v8, q_sf, k_sf, v_sf, *, causal: bool, scale: float
     if st != FA_OK:
         raise FaError(st, "fa_forward_mxfp8")
     return out, lse
+
+
+def fa_device(h) -> int:
+    """CUDA device ordinal of the handle (-1 for None)."""
+    return int(load().fa_device(h))
+
+
+def fa_append_paged(h, cache, seqs, cu_seqlens, total, K, V, Q, Q_out, Hq, k_strides, v_strides, q_strides, qo_strides, rope,
+                    stream=0) -> int:
+    """Raw call: `cache`, `seqs` and `rope` are the structures above (rope may be None), pointers integers, strides
+    (token, head) pairs in elements; returns the status code."""
+    arr = [None if x is None else _I64x2(*[int(i) for i in x]) for x in (k_strides, v_strides, q_strides, qo_strides)]
+    ref = lambda x: None if x is None else ctypes.addressof(x)
+    return load().fa_append_paged(h, ref(cache), ref(seqs), cu_seqlens, total, K, V, Q, Q_out, Hq, *arr, ref(rope), stream)
+
+
+def fa_forward_paged(h, cache, seqs, Q, O, lse, Hq, Sq, scale, q_strides, o_strides, stream=0) -> int:
+    """Raw call on a paged cache (structures above, pointers as integers, (token, head) strides); returns the status code."""
+    arr = [None if x is None else _I64x2(*[int(i) for i in x]) for x in (q_strides, o_strides)]
+    ref = lambda x: None if x is None else ctypes.addressof(x)
+    return load().fa_forward_paged(h, ref(cache), ref(seqs), Q, O, lse, Hq, Sq, float(scale), *arr, stream)
+
+
+def fa_forward_paged_diff(h, cache, seqs, Q, O, Hq, Sq, scale, diff, q_strides, o_strides, stream=0) -> int:
+    """Raw call of differential attention on a paged cache; returns the status code."""
+    arr = [None if x is None else _I64x2(*[int(i) for i in x]) for x in (q_strides, o_strides)]
+    ref = lambda x: None if x is None else ctypes.addressof(x)
+    return load().fa_forward_paged_diff(h, ref(cache), ref(seqs), Q, O, Hq, Sq, float(scale), ref(diff), *arr, stream)
+
+
+def fa_forward_diff(h, Q, K, V, O, B, Hq, Hkv, Sq, Sk, dqk, dv, causal, scale, diff, q_strides, k_strides, v_strides, o_strides,
+                    stream=0) -> int:
+    """Raw call of differential attention on dense tensors with (batch, head, row) strides; returns the status code."""
+    arr = [None if x is None else _I64x3(*[int(i) for i in x]) for x in (q_strides, k_strides, v_strides, o_strides)]
+    return load().fa_forward_diff(h, Q, K, V, O, B, Hq, Hkv, Sq, Sk, dqk, dv, int(bool(causal)), float(scale),
+                                  None if diff is None else ctypes.addressof(diff), *arr, stream)
+
+
+class PagedCache:
+    """A paged key/value cache for the paged entry points.
+
+    k [num_pages, Hkv, page_size, dqk] and v [num_pages, Hkv, page_size, dv]: CUDA tensors of that logical shape in any order of
+    the first three dimensions in memory (a [pages, page_size, Hkv, d] pool is passed permuted), bf16, or e4m3
+    (torch.float8_e4m3fn or uint8 codes) with one fp32 scale per K/V head.  Make it once per cache; it keeps the tensors alive.
+    """
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        import torch
+        if k.dim() != 4 or v.dim() != 4 or k.shape[:3] != v.shape[:3] or k.dtype != v.dtype:
+            raise ValueError("k and v must be 4-D tensors of one dtype with the same pages, heads and page size")
+        if k.dtype not in (torch.bfloat16, torch.float8_e4m3fn, torch.uint8):
+            raise ValueError("the cache must be bf16 or e4m3")
+        if not k.is_cuda or v.device != k.device or k.stride(3) != 1 or v.stride(3) != 1:
+            raise ValueError("k and v must be on one CUDA device, their last dimension contiguous")
+        for t in (k_scale, v_scale):
+            if t is not None and (t.dtype != torch.float32 or t.device != k.device or not t.is_contiguous() or
+                                  tuple(t.shape) != (k.shape[1],) or k.dtype == torch.bfloat16):
+                raise ValueError("scales are contiguous fp32 tensors of Hkv values on the cache's device, for e4m3 caches only")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.device, self.dqk, self.dv = k.device, k.shape[3], v.shape[3]
+        self.c = fa_paged_cache(ctypes.sizeof(fa_paged_cache), FA_CACHE_BF16 if k.dtype == torch.bfloat16 else FA_CACHE_E4M3,
+                                k.data_ptr(), v.data_ptr(), k.shape[0], k.shape[2], k.shape[1], k.shape[3], v.shape[3], 0,
+                                _I64x3(*k.stride()[:3]), _I64x3(*v.stride()[:3]),
+                                None if k_scale is None else k_scale.data_ptr(), None if v_scale is None else v_scale.data_ptr())
+        self.address = ctypes.addressof(self.c)
+
+
+class Rope:
+    """Rotation by position for `append_paged`: cos_sin is a contiguous fp32 CUDA tensor [max_pos, dim] (dim/2 cosines, then
+    dim/2 sines per position); of every `span` dimensions of a head (0: the whole head) those from `offset` on are turned, as
+    halves or in interleaved pairs."""
+
+    def __init__(self, cos_sin, *, offset: int = 0, span: int = 0, interleaved: bool = False):
+        import torch
+        if cos_sin.dtype != torch.float32 or not cos_sin.is_cuda or not cos_sin.is_contiguous() or cos_sin.dim() != 2:
+            raise ValueError("cos_sin must be a contiguous 2-D fp32 CUDA tensor")
+        self.cos_sin, self.device, self.span = cos_sin, cos_sin.device, int(span)
+        self.c = fa_rope(ctypes.sizeof(fa_rope), cos_sin.shape[0], cos_sin.data_ptr(), cos_sin.shape[1], int(offset), int(span),
+                         int(bool(interleaved)))
+        self.address = ctypes.addressof(self.c)
+
+    def struct_for(self, dqk: int) -> int:
+        """Address of the C structure for heads of dqk dimensions."""
+        if self.span:
+            return self.address
+        self.c.span = dqk
+        return self.address
+
+
+def _seqs(h, cache, block_table, seq_lens):
+    """The fa_paged_seqs of a call, after the checks that all paged calls share."""
+    import torch
+    if block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.stride(1) != 1 or block_table.device != cache.device:
+        raise ValueError("block_table must be a 2-D int32 tensor with contiguous rows on the cache's device")
+    B, max_pages = block_table.shape
+    if seq_lens.dtype != torch.int32 or seq_lens.device != cache.device or seq_lens.shape != (B,) or not seq_lens.is_contiguous():
+        raise ValueError("seq_lens must be a contiguous int32 tensor of one length per row of block_table")
+    if load().fa_device(h) != cache.device.index:
+        raise ValueError("the handle belongs to another device than the cache")
+    stride = block_table.stride(0)
+    return fa_paged_seqs(ctypes.sizeof(fa_paged_seqs), B, block_table.data_ptr(), stride if stride > max_pages else max_pages,
+                         seq_lens.data_ptr(), max_pages, 0)
+
+
+def _rows(t, cache, d, what):
+    """(token, head) strides of a [tokens, heads, d] bf16 tensor on the cache's device."""
+    import torch
+    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.device != cache.device or t.shape[2] != d:
+        raise ValueError("%s must be a 3-D bf16 tensor [tokens, heads, %d] on the cache's device" % (what, d))
+    st, sh, sd = t.stride()
+    if sd != 1:
+        raise ValueError("the last dimension of %s must be contiguous" % what)
+    # (the stride of a dimension of one row is whatever the view left; the library wants it to be valid)
+    return _I64x2(st if t.shape[0] > 1 else max(d, (st + 7) // 8 * 8), sh if t.shape[1] > 1 else max(d, (sh + 7) // 8 * 8))
+
+
+def append_paged(h, k, v, cache: PagedCache, block_table, seq_lens, *, cu_seqlens=None, q=None, q_out=None, rope: Rope = None):
+    """New keys and values [T, Hkv, d] of packed tokens into `cache`, rotated by their positions; returns q_out.
+
+    seq_lens [B] int32 counts the new tokens in; cu_seqlens [B+1] int32 gives each sequence's rows (None: T / B each).  With q
+    [T, Hq, dqk] the queries are rotated too, into q_out (allocated when not given; may be q itself).
+    """
+    import torch
+    seqs = _seqs(h, cache, block_table, seq_lens)
+    ks, vs = _rows(k, cache, cache.dqk, "k"), _rows(v, cache, cache.dv, "v")
+    total = k.shape[0]
+    if v.shape[0] != total or k.shape[1] != cache.c.Hkv or v.shape[1] != cache.c.Hkv:
+        raise ValueError("k and v must have the same tokens and the cache's heads")
+    if cu_seqlens is not None and (cu_seqlens.dtype != torch.int32 or cu_seqlens.device != cache.device or
+                                   cu_seqlens.shape != (seqs.B + 1,) or not cu_seqlens.is_contiguous()):
+        raise ValueError("cu_seqlens must be a contiguous int32 tensor of B + 1 offsets on the cache's device")
+    if rope is not None and rope.device != cache.device:
+        raise ValueError("the rotation table must be on the cache's device")
+    q_ptr = qo_ptr = qs = qos = None
+    Hq = 0
+    if q is not None:
+        qs, Hq = _rows(q, cache, cache.dqk, "q"), q.shape[1]
+        if q.shape[0] != total:
+            raise ValueError("q must have the tokens of k")
+        if q_out is None:
+            q_out = torch.empty((total, Hq, cache.dqk), dtype=torch.bfloat16, device=q.device)
+        elif q_out.shape != q.shape:
+            raise ValueError("q_out must have q's shape")
+        qos = _rows(q_out, cache, cache.dqk, "q_out")
+        q_ptr, qo_ptr = q.data_ptr(), q_out.data_ptr()
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    st = load().fa_append_paged(h, cache.address, ctypes.addressof(seqs), None if cu_seqlens is None else cu_seqlens.data_ptr(), total,
+                                k.data_ptr(), v.data_ptr(), q_ptr, qo_ptr, Hq, ks, vs, qs, qos,
+                                None if rope is None else rope.struct_for(cache.dqk),
+                                torch.cuda.current_stream(cache.device).cuda_stream)
+    if st != FA_OK:
+        raise FaError(st, "fa_append_paged")
+    return q_out
+
+
+def _paged_out(q, cache, seqs, out):
+    import torch
+    T, Hq = q.shape[0], q.shape[1]
+    if seqs.B == 0 or T == 0 or T % seqs.B:
+        raise ValueError("q must hold the same number of tokens for every sequence")
+    if out is None:
+        return torch.empty((T, Hq, cache.dv), dtype=torch.bfloat16, device=q.device)
+    if tuple(out.shape) != (T, Hq, cache.dv):
+        raise ValueError("out must have shape %s" % ((T, Hq, cache.dv),))
+    return out
+
+
+def forward_paged(h, q, cache: PagedCache, block_table, seq_lens, *, scale: float = 0.0, out=None, want_lse=True):
+    """Attention of the last tokens of every sequence over a paged cache: q [B*Sq, Hq, dqk] bf16; returns (O [B*Sq, Hq, dv],
+    lse [Hq, B*Sq] fp32 or None)."""
+    import torch
+    seqs = _seqs(h, cache, block_table, seq_lens)
+    qs = _rows(q, cache, cache.dqk, "q")
+    out = _paged_out(q, cache, seqs, out)
+    os_ = _rows(out, cache, cache.dv, "out")
+    T, Hq = q.shape[0], q.shape[1]
+    lse = torch.empty((Hq, T), dtype=torch.float32, device=q.device) if want_lse else None
+    st = load().fa_forward_paged(h, cache.address, ctypes.addressof(seqs), q.data_ptr(), out.data_ptr(),
+                                 None if lse is None else lse.data_ptr(), Hq, T // seqs.B, scale, qs, os_,
+                                 torch.cuda.current_stream(cache.device).cuda_stream)
+    if st != FA_OK:
+        raise FaError(st, "fa_forward_paged")
+    return out, lse
+
+
+def _diff(lam, norm_weight, eps, out_scale, Hq, device):
+    import torch
+    if lam.dtype != torch.float32 or lam.device != device or tuple(lam.shape) != (Hq,) or not lam.is_contiguous():
+        raise ValueError("lam must be a contiguous fp32 tensor of one value per query head")
+    if norm_weight is not None and (norm_weight.dtype != torch.float32 or norm_weight.device != device or
+                                    tuple(norm_weight.shape) != (128,) or not norm_weight.is_contiguous()):
+        raise ValueError("norm_weight must be a contiguous fp32 tensor of 128 values")
+    return fa_diff(ctypes.sizeof(fa_diff), eps, lam.data_ptr(), None if norm_weight is None else norm_weight.data_ptr(), out_scale, 0.0)
+
+
+def forward_paged_diff(h, q, cache: PagedCache, block_table, seq_lens, lam, *, norm_weight=None, eps: float = 1e-5,
+                       out_scale: float = 1.0, scale: float = 0.0, out=None):
+    """Differential attention of the last tokens over a paged cache whose heads are two maps of 64 and values of 128; returns O."""
+    import torch
+    seqs = _seqs(h, cache, block_table, seq_lens)
+    qs = _rows(q, cache, cache.dqk, "q")
+    out = _paged_out(q, cache, seqs, out)
+    os_ = _rows(out, cache, cache.dv, "out")
+    T, Hq = q.shape[0], q.shape[1]
+    diff = _diff(lam, norm_weight, eps, out_scale, Hq, cache.device)
+    st = load().fa_forward_paged_diff(h, cache.address, ctypes.addressof(seqs), q.data_ptr(), out.data_ptr(), Hq, T // seqs.B, scale,
+                                      ctypes.addressof(diff), qs, os_, torch.cuda.current_stream(cache.device).cuda_stream)
+    if st != FA_OK:
+        raise FaError(st, "fa_forward_paged_diff")
+    return out
+
+
+def forward_diff(h, q, k, v, lam, *, causal: bool, norm_weight=None, eps: float = 1e-5, out_scale: float = 1.0, scale: float = 0.0,
+                 out=None):
+    """Differential attention on torch CUDA tensors (bf16, logical shape [B, H, S, 128], any batch/head/row strides; the two
+    halves of a query and key are its two maps); returns O, in q's memory layout when `out` is not given."""
+    import torch
+    for t in (q, k, v):
+        if t.dtype != torch.bfloat16 or not t.is_cuda or t.dim() != 4 or t.device != q.device:
+            raise ValueError("q, k, v must be 4-D bf16 tensors on one CUDA device")
+    B, Hq, Sq, dqk = q.shape
+    _, Hkv, Sk, dv = v.shape
+    if tuple(k.shape) != (B, Hkv, Sk, dqk) or v.shape[0] != B:
+        raise ValueError("k and v must have q's batch, the same heads and rows, and k q's head size")
+    if load().fa_device(h) != q.device.index:
+        raise ValueError("the handle belongs to another device than the tensors")
+    if out is None:
+        order = sorted(range(3), key=lambda i: -q.stride(i)) + [3]
+        shape = (B, Hq, Sq, dv)
+        buf = torch.empty([shape[i] for i in order], dtype=torch.bfloat16, device=q.device)
+        out = buf.permute([order.index(i) for i in range(4)])
+    elif tuple(out.shape) != (B, Hq, Sq, dv) or out.dtype != torch.bfloat16 or out.device != q.device:
+        raise ValueError("out must be a bf16 tensor of shape %s on q's device" % ((B, Hq, Sq, dv),))
+    for t in (q, k, v, out):
+        if t.stride(3) != 1:
+            raise ValueError("the last dimension must be contiguous")
+    diff = _diff(lam, norm_weight, eps, out_scale, Hq, q.device)
+    st = load().fa_forward_diff(h, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), B, Hq, Hkv, Sq, Sk, dqk, dv,
+                                int(bool(causal)), scale, ctypes.addressof(diff), _I64x3(*q.stride()[:3]), _I64x3(*k.stride()[:3]),
+                                _I64x3(*v.stride()[:3]), _I64x3(*out.stride()[:3]), torch.cuda.current_stream(q.device).cuda_stream)
+    if st != FA_OK:
+        raise FaError(st, "fa_forward_diff")
+    return out

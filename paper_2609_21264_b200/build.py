@@ -8,9 +8,9 @@ import subprocess
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libfa_b200.so")
-SOURCES = ("fa_api.cu", "fa_noalloc.cu")
+SOURCES = ("fa_api.cu", "fa_noalloc.cu", "fa_paged.cu")
 NVCC_FLAGS = ("-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-shared", "-Xcompiler", "-fPIC", "-Xptxas", "-v")
+              "-shared", "-Xcompiler", "-fPIC", "-Xptxas", "-v", "--threads", "0")
 
 
 def _nvcc() -> str:

@@ -1,0 +1,259 @@
+// Host side of the paged-cache and differential-attention entry points declared in include/fa.h: argument checks,
+// tensor maps, kernel selection and launch.
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+#include <string.h>
+
+#include "../../include/fa.h"
+#include "fa_append_paged.cuh"
+#include "fa_common.cuh"
+#include "fa_handle.h"
+#include "fa_paged_common.cuh"
+#include "fa_paged_simple.cuh"
+
+namespace {
+
+using namespace fa_host;
+
+bool head_sizes_ok(int dqk, int dv) {
+    return (dqk == 64 && dv == 64) || (dqk == 128 && dv == 128) || (dqk == 192 && dv == 128);
+}
+
+fa_status check_cache(const fa_paged_cache* c) {
+    if (!c || c->struct_size != sizeof(fa_paged_cache) || c->reserved != 0) return FA_ERR_INVALID_ARG;
+    if (c->type != FA_CACHE_BF16 && c->type != FA_CACHE_E4M3) return FA_ERR_INVALID_ARG;
+    if (!c->k || !c->v || misaligned(c->k, 16) || misaligned(c->v, 16)) return FA_ERR_INVALID_ARG;
+    if (c->num_pages <= 0 || c->page_size <= 0 || c->Hkv <= 0 || c->dqk <= 0 || c->dv <= 0) return FA_ERR_INVALID_ARG;
+    if (!head_sizes_ok(c->dqk, c->dv)) return FA_ERR_UNSUPPORTED;
+    if (c->page_size % 16 != 0 || c->page_size > 65536) return FA_ERR_UNSUPPORTED;
+    const int64_t unit = c->type == FA_CACHE_E4M3 ? 16 : 8;      // 16 bytes
+    for (int i = 0; i < 3; ++i)
+        if (c->k_strides[i] <= 0 || c->v_strides[i] <= 0 || c->k_strides[i] % unit != 0 || c->v_strides[i] % unit != 0)
+            return FA_ERR_INVALID_ARG;
+    if (c->k_strides[2] < c->dqk || c->v_strides[2] < c->dv) return FA_ERR_INVALID_ARG;
+    if (c->type == FA_CACHE_BF16 && (c->k_scale || c->v_scale)) return FA_ERR_INVALID_ARG;
+    if ((c->k_scale && misaligned(c->k_scale, 4)) || (c->v_scale && misaligned(c->v_scale, 4))) return FA_ERR_INVALID_ARG;
+    return FA_OK;
+}
+
+fa_status check_seqs(const fa_paged_seqs* s, const fa_paged_cache* c) {
+    if (!s || s->struct_size != sizeof(fa_paged_seqs) || s->reserved != 0) return FA_ERR_INVALID_ARG;
+    if (s->B < 0 || s->max_pages <= 0 || s->table_stride < s->max_pages) return FA_ERR_INVALID_ARG;
+    if (!s->block_table || !s->seq_lens || misaligned(s->block_table, 4) || misaligned(s->seq_lens, 4)) return FA_ERR_INVALID_ARG;
+    // positions are 32-bit
+    if (static_cast<int64_t>(s->max_pages) * c->page_size > 0x7fffff00LL) return FA_ERR_UNSUPPORTED;
+    return FA_OK;
+}
+
+// {token, head} strides of a row-major [tokens, heads, d] tensor
+bool row_strides_ok(const int64_t* s, int d) { return s && s[0] > 0 && s[1] >= d && ((s[0] | s[1]) & 7) == 0; }
+
+fa_status check_diff(const fa_diff* d) {
+    if (!d || d->struct_size != sizeof(fa_diff) || d->reserved != 0.f) return FA_ERR_INVALID_ARG;
+    if (!d->lambda || misaligned(d->lambda, 4)) return FA_ERR_INVALID_ARG;
+    if (d->weight && (misaligned(d->weight, 16) || !isfinite(d->eps) || d->eps <= 0.f)) return FA_ERR_INVALID_ARG;
+    if (!isfinite(d->out_scale)) return FA_ERR_INVALID_ARG;
+    return FA_OK;
+}
+
+// Launch with programmatic stream serialisation (see FA_FLAG_NO_DEPENDENT_LAUNCH).
+template <typename... Params, typename... Args>
+fa_status launch(fa_handle* h, void (*kernel)(Params...), long long blocks, int threads, int smem, cudaStream_t st, const Args&... args) {
+    if (blocks <= 0 || blocks > 0x7fffffffLL) return FA_ERR_UNSUPPORTED;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(blocks), 1, 1);
+    cfg.blockDim = dim3(threads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = (h->flags & FA_FLAG_NO_DEPENDENT_LAUNCH) ? 0 : 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, args...) != cudaSuccess) {
+        cudaGetLastError();
+        return FA_ERR_CUDA;
+    }
+    h->launches += 1;
+    return FA_OK;
+}
+
+template <bool kE4m3, bool kDiff>
+fa_status launch_simple(fa_handle* h, int dqk, const fa::PagedParams& p, cudaStream_t st) {
+    const long long blocks = static_cast<long long>(p.B) * p.Sq * p.Hq;
+    h->last_kernel = "fa_paged_simple";
+    h->last_splits = 1;
+    if constexpr (!kDiff) {
+        if (dqk == 64) return launch(h, fa::fa_paged_simple_kernel<64, 64, kE4m3, kDiff>, blocks, 128, 0, st, p);
+        if (dqk == 192) return launch(h, fa::fa_paged_simple_kernel<192, 128, kE4m3, kDiff>, blocks, 128, 0, st, p);
+    }
+    return launch(h, fa::fa_paged_simple_kernel<128, 128, kE4m3, kDiff>, blocks, 128, 0, st, p);
+}
+
+fa_status forward_paged(fa_handle* h, const fa_paged_cache* cache, const fa_paged_seqs* seqs, const void* Q, void* O, float* lse,
+                        int Hq, int Sq, float scale, const fa_diff* diff, const int64_t* q_strides, const int64_t* o_strides,
+                        void* stream) {
+    fa_status s = check_cache(cache);
+    if (s != FA_OK) return s;
+    if ((s = check_seqs(seqs, cache)) != FA_OK) return s;
+    if (!Q || !O || misaligned(Q, 16) || misaligned(O, 16) || (lse && misaligned(lse, 4))) return FA_ERR_INVALID_ARG;
+    if (Hq <= 0 || Sq <= 0 || Hq % cache->Hkv != 0 || !isfinite(scale) || scale < 0.f) return FA_ERR_INVALID_ARG;
+    if (!row_strides_ok(q_strides, cache->dqk) || !row_strides_ok(o_strides, cache->dv)) return FA_ERR_INVALID_ARG;
+    if (Sq > FA_PAGED_MAX_SQ || Hq > 65535 || seqs->B > 65535) return FA_ERR_UNSUPPORTED;
+    if (diff && (cache->dqk != 128 || cache->dv != 128)) return FA_ERR_UNSUPPORTED;
+    if (seqs->B == 0) return FA_OK;
+    DeviceGuard guard(h->device);
+    if (!guard.ok()) return FA_ERR_CUDA;
+    if (scale == 0.f) scale = 1.f / sqrtf(static_cast<float>(diff ? 64 : cache->dqk));
+
+    fa::PagedParams p;
+    memset(&p, 0, sizeof p);
+    p.Q = static_cast<const __nv_bfloat16*>(Q);
+    p.O = static_cast<__nv_bfloat16*>(O);
+    p.lse = lse;
+    p.q_st = q_strides[0]; p.q_sh = q_strides[1]; p.q_sb = Sq * q_strides[0];
+    p.o_st = o_strides[0]; p.o_sh = o_strides[1]; p.o_sb = Sq * o_strides[0];
+    p.k = cache->k; p.v = cache->v;
+    for (int i = 0; i < 3; ++i) { p.k_stride[i] = cache->k_strides[i]; p.v_stride[i] = cache->v_strides[i]; }
+    p.k_scale = cache->k_scale; p.v_scale = cache->v_scale;
+    p.block_table = seqs->block_table; p.table_stride = seqs->table_stride; p.seq_lens = seqs->seq_lens;
+    p.B = seqs->B; p.max_pages = seqs->max_pages; p.num_pages = cache->num_pages; p.page_size = cache->page_size;
+    p.Hq = Hq; p.Hkv = cache->Hkv; p.Sq = Sq;
+    p.causal = 1;
+    p.scale_log2 = scale * 1.4426950408889634f;
+    if (diff) { p.lambda = diff->lambda; p.weight = diff->weight; p.eps = diff->eps; p.out_scale = diff->out_scale; }
+    p.status = h->status_dev;
+    p.wait_limit_ns = h->wait_limit_ns;
+    p.debug_drop_v_load = (h->flags & FA_FLAG_DEBUG_DROP_V_LOAD) ? 1 : 0;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const bool e4m3 = cache->type == FA_CACHE_E4M3;
+    if (e4m3) return diff ? launch_simple<true, true>(h, cache->dqk, p, st) : launch_simple<true, false>(h, cache->dqk, p, st);
+    return diff ? launch_simple<false, true>(h, cache->dqk, p, st) : launch_simple<false, false>(h, cache->dqk, p, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+fa_status fa_append_paged(fa_handle* h, const fa_paged_cache* cache, const fa_paged_seqs* seqs, const int32_t* cu_seqlens, int total,
+                          const void* K, const void* V, const void* Q, void* Q_out, int Hq, const int64_t* k_strides,
+                          const int64_t* v_strides, const int64_t* q_strides, const int64_t* qo_strides, const fa_rope* rope,
+                          void* stream) {
+    if (!h) return FA_ERR_INVALID_ARG;
+    fa_status s = check_cache(cache);
+    if (s != FA_OK) return s;
+    if ((s = check_seqs(seqs, cache)) != FA_OK) return s;
+    if (total < 0 || (cu_seqlens && misaligned(cu_seqlens, 4))) return FA_ERR_INVALID_ARG;
+    if (total == 0 || seqs->B == 0) return FA_OK;
+    if (!cu_seqlens && total % seqs->B != 0) return FA_ERR_INVALID_ARG;
+    if (!K || !V || misaligned(K, 16) || misaligned(V, 16)) return FA_ERR_INVALID_ARG;
+    if (!row_strides_ok(k_strides, cache->dqk) || !row_strides_ok(v_strides, cache->dv)) return FA_ERR_INVALID_ARG;
+    if (!Q != !Q_out) return FA_ERR_INVALID_ARG;
+    if (Q) {
+        if (misaligned(Q, 16) || misaligned(Q_out, 16) || Hq <= 0 || Hq > 65535) return FA_ERR_INVALID_ARG;
+        if (!row_strides_ok(q_strides, cache->dqk) || !row_strides_ok(qo_strides, cache->dqk)) return FA_ERR_INVALID_ARG;
+    }
+    if (rope) {
+        if (rope->struct_size != sizeof(fa_rope) || !rope->cos_sin || misaligned(rope->cos_sin, 16)) return FA_ERR_INVALID_ARG;
+        if (rope->max_pos <= 0 || rope->dim <= 0 || rope->offset < 0 || rope->span <= 0) return FA_ERR_INVALID_ARG;
+        if (rope->dim % 16 != 0 || rope->span % 16 != 0 || rope->offset % 8 != 0) return FA_ERR_UNSUPPORTED;
+        if (cache->dqk % rope->span != 0 || rope->dim > rope->span || rope->offset > rope->span - rope->dim) return FA_ERR_INVALID_ARG;
+    }
+    DeviceGuard guard(h->device);
+    if (!guard.ok()) return FA_ERR_CUDA;
+    fa::AppendParams p;
+    memset(&p, 0, sizeof p);
+    p.K = static_cast<const __nv_bfloat16*>(K);
+    p.V = static_cast<const __nv_bfloat16*>(V);
+    p.k_st = k_strides[0]; p.k_sh = k_strides[1];
+    p.v_st = v_strides[0]; p.v_sh = v_strides[1];
+    if (Q) {
+        p.Q = static_cast<const __nv_bfloat16*>(Q);
+        p.Q_out = static_cast<__nv_bfloat16*>(Q_out);
+        p.q_st = q_strides[0]; p.q_sh = q_strides[1];
+        p.qo_st = qo_strides[0]; p.qo_sh = qo_strides[1];
+        p.Hq = Hq;
+    }
+    p.k_cache = cache->k; p.v_cache = cache->v;
+    for (int i = 0; i < 3; ++i) { p.k_stride[i] = cache->k_strides[i]; p.v_stride[i] = cache->v_strides[i]; }
+    p.k_scale = cache->k_scale; p.v_scale = cache->v_scale;
+    p.block_table = seqs->block_table; p.table_stride = seqs->table_stride; p.seq_lens = seqs->seq_lens;
+    p.cu_seqlens = cu_seqlens;
+    p.B = seqs->B; p.max_pages = seqs->max_pages; p.num_pages = cache->num_pages; p.page_size = cache->page_size;
+    p.total = total;
+    p.per_seq = cu_seqlens ? 0 : total / seqs->B;
+    p.Hkv = cache->Hkv; p.dqk = cache->dqk; p.dv = cache->dv;
+    p.span = cache->dqk;
+    if (rope) {
+        p.cos_sin = rope->cos_sin;
+        p.max_pos = rope->max_pos; p.rot_dim = rope->dim; p.rot_offset = rope->offset; p.span = rope->span;
+        p.interleaved = rope->interleaved ? 1 : 0;
+    }
+    p.span_units = p.span / 8 - ((rope && !p.interleaved) ? p.rot_dim / 16 : 0);
+    p.head_units = p.span_units * (p.dqk / p.span);
+    p.k_units = p.Hkv * p.head_units;
+    p.v_units = p.Hkv * (p.dv / 8);
+    p.q_units = p.Hq * p.head_units;
+    p.status = h->status_dev;
+    h->last_kernel = "fa_append_paged";
+    h->last_splits = 1;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (cache->type == FA_CACHE_E4M3) return launch(h, fa::fa_append_paged_kernel<true>, total, 256, 0, st, p);
+    return launch(h, fa::fa_append_paged_kernel<false>, total, 256, 0, st, p);
+}
+
+fa_status fa_forward_paged(fa_handle* h, const fa_paged_cache* cache, const fa_paged_seqs* seqs, const void* Q, void* O, float* lse,
+                           int Hq, int Sq, float scale, const int64_t* q_strides, const int64_t* o_strides, void* stream) {
+    if (!h) return FA_ERR_INVALID_ARG;
+    return forward_paged(h, cache, seqs, Q, O, lse, Hq, Sq, scale, nullptr, q_strides, o_strides, stream);
+}
+
+fa_status fa_forward_paged_diff(fa_handle* h, const fa_paged_cache* cache, const fa_paged_seqs* seqs, const void* Q, void* O, int Hq,
+                                int Sq, float scale, const fa_diff* diff, const int64_t* q_strides, const int64_t* o_strides,
+                                void* stream) {
+    if (!h) return FA_ERR_INVALID_ARG;
+    const fa_status s = check_diff(diff);
+    if (s != FA_OK) return s;
+    return forward_paged(h, cache, seqs, Q, O, nullptr, Hq, Sq, scale, diff, q_strides, o_strides, stream);
+}
+
+fa_status fa_forward_diff(fa_handle* h, const void* Q, const void* K, const void* V, void* O, int B, int Hq, int Hkv, int Sq, int Sk,
+                          int dqk, int dv, int causal, float scale, const fa_diff* diff, const int64_t* q_strides,
+                          const int64_t* k_strides, const int64_t* v_strides, const int64_t* o_strides, void* stream) {
+    if (!h) return FA_ERR_INVALID_ARG;
+    fa_status s = check_diff(diff);
+    if (s != FA_OK) return s;
+    if (!Q || !K || !V || !O || misaligned(Q, 16) || misaligned(K, 16) || misaligned(V, 16) || misaligned(O, 16)) return FA_ERR_INVALID_ARG;
+    if (B <= 0 || Hq <= 0 || Hkv <= 0 || Sq <= 0 || Sk <= 0 || Hq % Hkv != 0 || !isfinite(scale) || scale < 0.f) return FA_ERR_INVALID_ARG;
+    if (dqk != 128 || dv != 128) return dqk > 0 && dv > 0 ? FA_ERR_UNSUPPORTED : FA_ERR_INVALID_ARG;
+    if (!q_strides || !k_strides || !v_strides || !o_strides) return FA_ERR_INVALID_ARG;
+    for (int i = 0; i < 3; ++i) {
+        if (q_strides[i] <= 0 || k_strides[i] <= 0 || v_strides[i] <= 0 || o_strides[i] <= 0) return FA_ERR_INVALID_ARG;
+        if ((q_strides[i] | k_strides[i] | v_strides[i] | o_strides[i]) & 7) return FA_ERR_INVALID_ARG;
+    }
+    if (q_strides[2] < dqk || k_strides[2] < dqk || v_strides[2] < dv || o_strides[2] < dv) return FA_ERR_INVALID_ARG;
+    if (Hq > 65535 || B > 65535 || static_cast<int64_t>(B) * Hq > 0x7fffffffLL || Sq > 0x7fffff00 || Sk > 0x7fffff00) return FA_ERR_UNSUPPORTED;
+    DeviceGuard guard(h->device);
+    if (!guard.ok()) return FA_ERR_CUDA;
+    if (scale == 0.f) scale = 0.125f;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    fa::PagedParams p;
+    memset(&p, 0, sizeof p);
+    p.Q = static_cast<const __nv_bfloat16*>(Q);
+    p.O = static_cast<__nv_bfloat16*>(O);
+    p.q_sb = q_strides[0]; p.q_sh = q_strides[1]; p.q_st = q_strides[2];
+    p.o_sb = o_strides[0]; p.o_sh = o_strides[1]; p.o_st = o_strides[2];
+    p.k = K; p.v = V;
+    for (int i = 0; i < 3; ++i) { p.k_stride[i] = k_strides[i]; p.v_stride[i] = v_strides[i]; }
+    p.B = B; p.num_pages = B; p.page_size = Sk; p.fixed_len = Sk;
+    p.Hq = Hq; p.Hkv = Hkv; p.Sq = Sq;
+    p.causal = causal ? 1 : 0;
+    p.scale_log2 = scale * 1.4426950408889634f;
+    p.lambda = diff->lambda; p.weight = diff->weight; p.eps = diff->eps; p.out_scale = diff->out_scale;
+    p.status = h->status_dev;
+    return launch_simple<false, true>(h, 128, p, st);
+}
+
+}  // extern "C"
