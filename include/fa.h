@@ -501,6 +501,28 @@ fa_status fa_forward_paged(fa_handle* h, const fa_paged_cache* cache, const fa_p
                            const int64_t* q_strides, const int64_t* o_strides, void* stream);
 
 /*
+ * How fa_forward_paged would deal out a batch, the counterpart of fa_plan: a pure host function that runs the kernel's own walk
+ * over the list of work units (one unit = 128 keys of one sequence, K/V head and block of query rows).  seqs->seq_lens is a HOST array
+ * here, block_table and the cache's pointers and strides are not looked at.  `pieces` receives up to max_pieces entries, in
+ * the order of the CTAs; out->pieces is their number in any case.
+ */
+typedef struct fa_paged_plan_info {
+    int32_t rows_per_block;       /* query rows that share a pass over the keys (16, 32 or 64)   */
+    int32_t row_blocks;           /* blocks that a K/V head's (Hq / Hkv) * Sq rows are cut into   */
+    int32_t ctas;                 /* grid size                                                    */
+    int32_t reserved;
+    int64_t units, units_per_cta, pieces;
+} fa_paged_plan_info;
+typedef struct fa_paged_piece {
+    int32_t cta, sequence, kv_head, row_block;
+    int32_t first_tile, end_tile; /* tiles of 128 keys [first_tile, end_tile)                     */
+    int32_t slot;                 /* partial-result slot, -1: the piece is whole                  */
+    int32_t pieces, first_cta;    /* of the same sequence, head and block                         */
+} fa_paged_piece;
+fa_status fa_plan_paged(int num_sms, const fa_config* cfg, const fa_paged_cache* cache, const fa_paged_seqs* seqs,
+                        int Hq, int Sq, int diff, fa_paged_plan_info* out, fa_paged_piece* pieces, int max_pieces);
+
+/*
  * Differential attention: a head's queries and keys are two halves of dqk/2 = 64 dimensions, q = [q1 | q2], k = [k1 | k2],
  * and its result is the difference of two softmax maps over the same values (dv = 128),
  *     Y = ( softmax(scale q1 k1^T) - lambda[hq] softmax(scale q2 k2^T) ) V

@@ -35,7 +35,8 @@ FA_FLAG_QUAD_KERNEL = 1024
 EXPORTS = ("fa_create", "fa_forward", "fa_forward_strided", "fa_forward_varlen", "fa_forward_fp8", "fa_forward_mxfp8", "fa_plan", "fa_forward_host", "fa_last_status", "fa_destroy",
            "fa_strerror", "fa_launch_count", "fa_last_kernel_name", "fa_last_kv_splits",
            "fa_forward_split_noalloc", "fa_noalloc_scratch_bytes", "fa_noalloc_last_status", "fa_debug_set_drop_v_load",
-           "fa_append_paged", "fa_forward_paged", "fa_forward_paged_diff", "fa_forward_diff", "fa_device")
+           "fa_append_paged", "fa_forward_paged", "fa_forward_paged_diff", "fa_forward_diff", "fa_device",
+           "fa_plan_paged")
 FA_CACHE_BF16 = 0
 FA_CACHE_E4M3 = 1
 FA_PAGED_MAX_SQ = 16
@@ -74,6 +75,16 @@ class fa_rope(ctypes.Structure):
 class fa_diff(ctypes.Structure):
     _fields_ = [("struct_size", ctypes.c_uint32), ("eps", ctypes.c_float), ("lambda_", ctypes.c_void_p),
                 ("weight", ctypes.c_void_p), ("out_scale", ctypes.c_float), ("reserved", ctypes.c_float)]
+
+
+class fa_paged_plan_info(ctypes.Structure):
+    _fields_ = [("rows_per_block", ctypes.c_int32), ("row_blocks", ctypes.c_int32), ("ctas", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("units", ctypes.c_int64), ("units_per_cta", ctypes.c_int64), ("pieces", ctypes.c_int64)]
+
+
+class fa_paged_piece(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("cta", "sequence", "kv_head", "row_block", "first_tile", "end_tile", "slot", "pieces",
+                                              "first_cta")]
 
 
 _I64x2 = ctypes.c_int64 * 2
@@ -144,6 +155,8 @@ def load():
     lib.fa_forward_paged_diff.argtypes = [vp, vp, vp, vp, vp, i32, i32, f32, vp, vp, vp, vp]
     lib.fa_forward_diff.restype = i32
     lib.fa_forward_diff.argtypes = [vp] * 5 + [i32] * 8 + [f32] + [vp] * 6
+    lib.fa_plan_paged.restype = i32
+    lib.fa_plan_paged.argtypes = [i32, vp, vp, vp, i32, i32, i32, vp, vp, i32]
     lib.fa_device.restype = i32
     lib.fa_device.argtypes = [vp]
     lib.fa_noalloc_last_status.restype = i32
@@ -385,6 +398,26 @@ def forward_mxfp8(h, q8, k8, v8, q_sf, k_sf, v_sf, *, causal: bool, scale: float
 def fa_device(h) -> int:
     """CUDA device ordinal of the handle (-1 for None)."""
     return int(load().fa_device(h))
+
+
+def fa_plan_paged(num_sms, seq_lens, Hq, Hkv, Sq, dqk, dv, *, page_size=16, max_pages=0, e4m3=False, diff=False, scratch_bytes=0):
+    """How fa_forward_paged deals out a batch with these lengths on a device with `num_sms` SMs (no GPU needed):
+    (info dict, list of piece dicts)."""
+    lens = (ctypes.c_int32 * len(seq_lens))(*[int(n) for n in seq_lens])
+    most = max_pages or max(1, -(-max(seq_lens) // page_size))
+    cfg = fa_config(ctypes.sizeof(fa_config), -1, 0, 0, 0, scratch_bytes)
+    cache = fa_paged_cache(ctypes.sizeof(fa_paged_cache), FA_CACHE_E4M3 if e4m3 else FA_CACHE_BF16, None, None, 1, page_size, Hkv, dqk, dv)
+    seqs = fa_paged_seqs(ctypes.sizeof(fa_paged_seqs), len(seq_lens), None, most, ctypes.addressof(lens), most, 0)
+    out, pieces = fa_paged_plan_info(), None
+    for n in (0, None):          # how many, then which
+        count = int(out.pieces) if n is None else 0
+        pieces = (fa_paged_piece * max(1, count))()
+        st = load().fa_plan_paged(num_sms, ctypes.addressof(cfg), ctypes.addressof(cache), ctypes.addressof(seqs), Hq, Sq, int(bool(diff)),
+                                  ctypes.addressof(out), ctypes.addressof(pieces), count)
+        if st != FA_OK:
+            raise FaError(st, "fa_plan_paged")
+    as_dict = lambda x: {f: getattr(x, f) for f, _ in x._fields_ if f != "reserved"}
+    return as_dict(out), [as_dict(x) for x in pieces[:out.pieces]]
 
 
 def fa_append_paged(h, cache, seqs, cu_seqlens, total, K, V, Q, Q_out, Hq, k_strides, v_strides, q_strides, qo_strides, rope,

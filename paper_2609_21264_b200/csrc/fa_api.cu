@@ -750,8 +750,9 @@ fa_status fa_create(fa_handle** out, const fa_config* cfg) {
         return FA_ERR_OOM;
     }
     h->scratch_bytes = scratch_bytes;
-    if (cudaMalloc(reinterpret_cast<void**>(&h->sched_counter), 256) != cudaSuccess ||
-        cudaMemset(h->sched_counter, 0, 256) != cudaSuccess) {
+    const size_t counter_bytes = 256 + static_cast<size_t>(num_sms) * sizeof(unsigned int);
+    if (cudaMalloc(reinterpret_cast<void**>(&h->sched_counter), counter_bytes) != cudaSuccess ||
+        cudaMemset(h->sched_counter, 0, counter_bytes) != cudaSuccess) {
         cudaGetLastError();
         if (h->sched_counter) cudaFree(h->sched_counter);
         cudaFree(h->scratch);
@@ -759,6 +760,7 @@ fa_status fa_create(fa_handle** out, const fa_config* cfg) {
         delete h;
         return FA_ERR_OOM;
     }
+    h->arrivals = h->sched_counter + 64;
     *out = h;
     return FA_OK;
 }
@@ -796,7 +798,7 @@ fa_status fa_last_status(fa_handle* h, uint32_t* detail) {
         // middle of its item list.  (The caller synchronised before asking, so no launch is using the counter.)
         if (h->sched_counter) {
             DeviceGuard guard(h->device);
-            if (guard.ok()) cudaMemset(h->sched_counter, 0, sizeof(unsigned int));
+            if (guard.ok()) cudaMemset(h->sched_counter, 0, 256 + static_cast<size_t>(h->num_sms) * sizeof(unsigned int));
         }
     }
     if (code == FA_OK || code == FA_ERR_DEVICE_TIMEOUT || code == FA_ERR_INVALID_ARG) return static_cast<fa_status>(code);

@@ -39,6 +39,7 @@ struct fa_handle {
     uint32_t kv_splits_cfg = 0;              // 0 auto, 1 never, n force
     void* scratch = nullptr;                 // split-KV partials
     unsigned int* sched_counter = nullptr;   // work-item ticket counter of the persistent kernel
+    unsigned int* arrivals = nullptr;        // paged kernel: finished pieces of a shared row block, one counter per SM (zero between launches)
     size_t scratch_bytes = 0;
     int last_splits = 1;
     unsigned long long wait_limit_ns = 2000ull * 1000000ull;

@@ -10,12 +10,15 @@
 #include "fa_append_paged.cuh"
 #include "fa_common.cuh"
 #include "fa_handle.h"
+#include "fa_paged.cuh"
 #include "fa_paged_common.cuh"
 #include "fa_paged_simple.cuh"
 
 namespace {
 
 using namespace fa_host;
+
+constexpr int kLeastUnits = 1;      // tiles of 128 keys that a CTA of the streaming kernel takes at least
 
 bool head_sizes_ok(int dqk, int dv) {
     return (dqk == 64 && dv == 64) || (dqk == 128 && dv == 128) || (dqk == 192 && dv == 128);
@@ -92,6 +95,52 @@ fa_status launch_simple(fa_handle* h, int dqk, const fa::PagedParams& p, cudaStr
     return launch(h, fa::fa_paged_simple_kernel<128, 128, kE4m3, kDiff>, blocks, 128, 0, st, p);
 }
 
+// Query rows per block: 16 where they suffice, else 32 or 64, as far as the accumulators (S^T and O^T twice, three times the columns
+// over an 8-bit cache, twice with two maps) and two stages of tiles fit.
+int rows_per_block(int rows, int dqk, bool e4m3, bool diff) {
+    if (rows <= 16 || (e4m3 && diff)) return 16;
+    return rows > 32 && !e4m3 && !diff && dqk != 192 ? 64 : 32;
+}
+
+// CTAs of a launch: one per SM, as many as there can be units, and as many as the scratch has two partial results for.
+int paged_ctas(int num_sms, size_t scratch_bytes, const fa::PagedParams& p, int dv, int states) {
+    long long ctas = num_sms;
+    const long long most = static_cast<long long>(p.B) * p.Hkv * p.row_blocks *
+                           fa::paged_tiles(static_cast<int>(static_cast<long long>(p.max_pages) * p.page_size));
+    if (ctas > most) ctas = most;
+    const long long fit = static_cast<long long>(scratch_bytes / (2 * fa::paged_slot_bytes(dv, states)));
+    return static_cast<int>(ctas > fit ? fit : ctas);
+}
+
+// The streaming kernel with blocks of kRows query rows.
+template <int DQK, int DV, bool kE4m3, bool kDiff, int kRows>
+fa_status launch_paged(fa_handle* h, const CUtensorMap& mk, const CUtensorMap& mv, fa::PagedParams& p, cudaStream_t st) {
+    using Cfg = fa::PagedCfg<DQK, DV, kE4m3, kDiff, kRows>;
+    constexpr int smem = fa::paged_smem_bytes<DQK, DV, kE4m3, kDiff, kRows>();
+    static_assert(smem <= 227 * 1024, "shared memory budget exceeded");
+    const int ctas = paged_ctas(h->num_sms, h->scratch_bytes, p, DV, Cfg::kStates);
+    if (ctas < 1) return FA_ERR_UNSUPPORTED;
+    p.part = static_cast<float*>(h->scratch);
+    p.arrivals = h->arrivals;
+    auto kernel = fa::fa_paged_kernel<DQK, DV, kE4m3, kDiff, kRows>;
+    const fa_status s = ensure_smem_attr(h, kernel, smem);
+    if (s != FA_OK) return s;
+    h->last_kernel = kE4m3 ? "fa_paged_e4m3" : "fa_paged";
+    h->last_splits = 1;
+    return launch(h, kernel, ctas, 384, smem, st, mk, mv, p);
+}
+
+template <int DQK, int DV, bool kE4m3, bool kDiff>
+fa_status launch_paged_rows(fa_handle* h, int block, const CUtensorMap& mk, const CUtensorMap& mv, fa::PagedParams& p, cudaStream_t st) {
+    if constexpr (!kE4m3 && !kDiff && DQK != 192) {
+        if (block == 64) return launch_paged<DQK, DV, kE4m3, kDiff, 64>(h, mk, mv, p, st);
+    }
+    if constexpr (!(kE4m3 && kDiff)) {
+        if (block == 32) return launch_paged<DQK, DV, kE4m3, kDiff, 32>(h, mk, mv, p, st);
+    }
+    return launch_paged<DQK, DV, kE4m3, kDiff, 16>(h, mk, mv, p, st);
+}
+
 fa_status forward_paged(fa_handle* h, const fa_paged_cache* cache, const fa_paged_seqs* seqs, const void* Q, void* O, float* lse,
                         int Hq, int Sq, float scale, const fa_diff* diff, const int64_t* q_strides, const int64_t* o_strides,
                         void* stream) {
@@ -129,8 +178,27 @@ fa_status forward_paged(fa_handle* h, const fa_paged_cache* cache, const fa_page
     p.debug_drop_v_load = (h->flags & FA_FLAG_DEBUG_DROP_V_LOAD) ? 1 : 0;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool e4m3 = cache->type == FA_CACHE_E4M3;
-    if (e4m3) return diff ? launch_simple<true, true>(h, cache->dqk, p, st) : launch_simple<true, false>(h, cache->dqk, p, st);
-    return diff ? launch_simple<false, true>(h, cache->dqk, p, st) : launch_simple<false, false>(h, cache->dqk, p, st);
+    if (h->flags & FA_FLAG_SERIAL_KERNEL) {
+        if (e4m3) return diff ? launch_simple<true, true>(h, cache->dqk, p, st) : launch_simple<true, false>(h, cache->dqk, p, st);
+        return diff ? launch_simple<false, true>(h, cache->dqk, p, st) : launch_simple<false, false>(h, cache->dqk, p, st);
+    }
+    p.box_rows = 16;
+    while (p.box_rows < 128 && cache->page_size % (2 * p.box_rows) == 0) p.box_rows *= 2;
+    p.least_units = kLeastUnits;
+    const int rows = Hq / cache->Hkv * Sq, block = rows_per_block(rows, cache->dqk, e4m3, diff != nullptr);
+    p.row_blocks = (rows + block - 1) / block;
+    const int eb = e4m3 ? 1 : 2;
+    const CUtensorMap* m = nullptr;
+    if ((s = get_map(h, cache->k, cache->dqk, cache->page_size, cache->Hkv, cache->num_pages, cache->k_strides[0], cache->k_strides[1],
+                     cache->k_strides[2], p.box_rows, &m, eb)) != FA_OK) return s;
+    const CUtensorMap mk = *m;       // a copy: the next insertion may move the cache's entries
+    if ((s = get_map(h, cache->v, cache->dv, cache->page_size, cache->Hkv, cache->num_pages, cache->v_strides[0], cache->v_strides[1],
+                     cache->v_strides[2], p.box_rows, &m, eb)) != FA_OK) return s;
+    const CUtensorMap mv = *m;
+    if (diff) return e4m3 ? launch_paged_rows<128, 128, true, true>(h, block, mk, mv, p, st) : launch_paged_rows<128, 128, false, true>(h, block, mk, mv, p, st);
+    if (cache->dqk == 64) return e4m3 ? launch_paged_rows<64, 64, true, false>(h, block, mk, mv, p, st) : launch_paged_rows<64, 64, false, false>(h, block, mk, mv, p, st);
+    if (cache->dqk == 192) return e4m3 ? launch_paged_rows<192, 128, true, false>(h, block, mk, mv, p, st) : launch_paged_rows<192, 128, false, false>(h, block, mk, mv, p, st);
+    return e4m3 ? launch_paged_rows<128, 128, true, false>(h, block, mk, mv, p, st) : launch_paged_rows<128, 128, false, false>(h, block, mk, mv, p, st);
 }
 
 }  // namespace
@@ -254,6 +322,67 @@ fa_status fa_forward_diff(fa_handle* h, const void* Q, const void* K, const void
     p.lambda = diff->lambda; p.weight = diff->weight; p.eps = diff->eps; p.out_scale = diff->out_scale;
     p.status = h->status_dev;
     return launch_simple<false, true>(h, 128, p, st);
+}
+
+fa_status fa_plan_paged(int num_sms, const fa_config* cfg, const fa_paged_cache* cache, const fa_paged_seqs* seqs, int Hq, int Sq,
+                        int diff, fa_paged_plan_info* out, fa_paged_piece* pieces, int max_pieces) {
+    if (num_sms <= 0 || !cache || !seqs || !out || cache->struct_size != sizeof(fa_paged_cache) || seqs->struct_size != sizeof(fa_paged_seqs))
+        return FA_ERR_INVALID_ARG;
+    if (cache->page_size <= 0 || cache->Hkv <= 0 || Hq <= 0 || Sq <= 0 || Hq % cache->Hkv != 0 || seqs->B <= 0 || seqs->max_pages <= 0 ||
+        !seqs->seq_lens || max_pieces < 0 || (max_pieces > 0 && !pieces)) return FA_ERR_INVALID_ARG;
+    if (!head_sizes_ok(cache->dqk, cache->dv) || cache->page_size % 16 != 0 || Sq > FA_PAGED_MAX_SQ || seqs->B > 65535 ||
+        (diff && (cache->dqk != 128 || cache->dv != 128)) || static_cast<int64_t>(seqs->max_pages) * cache->page_size > 0x7fffff00LL)
+        return FA_ERR_UNSUPPORTED;
+    uint64_t scratch = 32ull << 20;
+    if (cfg) {
+        if (cfg->struct_size < 16) return FA_ERR_INVALID_ARG;
+        if (cfg->struct_size >= sizeof(fa_config) && cfg->scratch_bytes) scratch = cfg->scratch_bytes;
+    }
+    fa::PagedParams p;
+    memset(&p, 0, sizeof p);
+    p.seq_lens = seqs->seq_lens;
+    p.B = seqs->B; p.max_pages = seqs->max_pages; p.page_size = cache->page_size; p.Hkv = cache->Hkv; p.Hq = Hq; p.Sq = Sq;
+    const int rows = Hq / cache->Hkv * Sq, block = rows_per_block(rows, cache->dqk, cache->type == FA_CACHE_E4M3, diff != 0);
+    p.row_blocks = (rows + block - 1) / block;
+    p.least_units = kLeastUnits;
+    const int ctas = paged_ctas(num_sms, static_cast<size_t>(scratch), p, cache->dv, (diff ? 2 : 1) * block);
+    if (ctas < 1) return FA_ERR_UNSUPPORTED;
+    long long total = 0;
+    for (int b = 0; b < p.B; ++b) total += fa::paged_units(p, b);
+    const long long share = fa::paged_share(total, ctas, p.least_units);
+    out->rows_per_block = block;
+    out->row_blocks = p.row_blocks;
+    out->ctas = ctas;
+    out->units = total;
+    out->units_per_cta = share;
+    // the walk of every CTA, as the kernel makes it
+    long long n = 0, base = 0;
+    int b = 0;
+    for (int c = 0; c < ctas && c * share < total; ++c) {
+        const long long u0 = c * share, u1 = u0 + share < total ? u0 + share : total;
+        while (u0 >= base + fa::paged_units(p, b)) base += fa::paged_units(p, b++);
+        fa::PagedPart part;
+        part.begin(p, b, base, u0, u1, false);
+        do {
+            if (n < max_pieces) {
+                const bool whole = part.t1 - part.t0 == part.nt;
+                const long long ua = part.first_unit();
+                fa_paged_piece* x = pieces + n;
+                x->cta = c;
+                x->sequence = part.b;
+                x->kv_head = part.hr / p.row_blocks;
+                x->row_block = part.hr % p.row_blocks;
+                x->first_tile = part.t0;
+                x->end_tile = part.t1;
+                x->slot = whole ? -1 : fa::paged_slot(c, ua, share);
+                x->pieces = whole ? 1 : fa::paged_pieces(ua, ua + part.nt, share);
+                x->first_cta = whole ? c : fa::paged_first_cta(ua, share);
+            }
+            ++n;
+        } while (part.next(p));
+    }
+    out->pieces = n;
+    return FA_OK;
 }
 
 }  // extern "C"

@@ -34,7 +34,9 @@ struct PagedParams {
     const float* lambda;          // differential attention: [Hq]
     const float* weight;          // [dv] or nullptr (no normalisation)
     float eps, out_scale;
-    int row_blocks;               // blocks of rows that a (sequence, K/V head) is cut into
+    int row_blocks;               // blocks of query rows that a (sequence, K/V head) is cut into
+    int box_rows;                 // rows of a page box: the largest power of two that divides the page size, at most 128
+    int least_units;              // tiles that a CTA takes at least
     float* part;                  // partial results: two slots per CTA
     unsigned int* arrivals;       // pieces finished, per (sequence, K/V head, row block) with more than one; zero between launches
     uint32_t* status;
@@ -42,7 +44,7 @@ struct PagedParams {
     int debug_drop_v_load;
 };
 
-FA_DEVI void report_bad_input(uint32_t* status, uint32_t site) {
+__host__ __device__ inline void report_bad_input(uint32_t* status, uint32_t site) {
     if (!status) return;
     volatile uint32_t* sw = status;       // mapped host memory: plain stores
     sw[1] = site;
@@ -50,7 +52,7 @@ FA_DEVI void report_bad_input(uint32_t* status, uint32_t site) {
 }
 
 // Length of sequence b as the kernels use it: what the block table can hold, and never negative.
-FA_DEVI int clamped_len(int len, int max_pages, int page_size, uint32_t* status) {
+__host__ __device__ inline int clamped_len(int len, int max_pages, int page_size, uint32_t* status) {
     const long long most = static_cast<long long>(max_pages) * page_size;
     if (len < 0 || len > most) {
         report_bad_input(status, kSiteBadLength);
