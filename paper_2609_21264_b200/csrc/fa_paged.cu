@@ -127,7 +127,7 @@ fa_status launch_paged(fa_handle* h, const CUtensorMap& mk, const CUtensorMap& m
     if (s != FA_OK) return s;
     h->last_kernel = kE4m3 ? "fa_paged_e4m3" : "fa_paged";
     h->last_splits = 1;
-    return launch(h, kernel, ctas, 384, smem, st, mk, mv, p);
+    return launch(h, kernel, ctas, 512, smem, st, mk, mv, p);
 }
 
 template <int DQK, int DV, bool kE4m3, bool kDiff>

@@ -13,11 +13,12 @@
 //     that several CTAs share is joined by the one that finishes last, in the order of the CTAs (equal calls give equal bits).
 //   * A ring of K/V tiles (two to five stages, all that the shared memory holds) runs across the boundaries of sequences.
 //
-// Two groups of four softmax warps take the tiles in turn; each has its own scores, probabilities, reference maximum, row
-// sums and accumulator (merged when a piece of the list ends), so that one group's exponentials run under the other's MMAs
-// and no tile waits for the one before it.  A thread owns a key of the tile: the row maximum runs across lanes, so it is
-// taken rarely: the reference of a row moves only when some score exceeds it by more than kTauLog2 (one barrier with a
-// vote per tile; the reductions, and the rescaling of O^T, on the few tiles where the vote says so).
+// Two groups of four softmax warps take the tiles in turn; each has its own scores (two buffers), probabilities (two), reference maximum,
+// row sums and accumulator, so that no tile waits for the one before it.  A thread owns a key of the tile: the row maximum runs
+// across lanes, so it is taken rarely: the reference of a row moves only when some score exceeds it by more than kTauLog2 (one
+// barrier with a vote per tile; the reductions, and the rescaling of O^T, on the few tiles where the vote says so).
+// When a part of the list ends (a sequence and head, or the CTA's share), a third group of warps merges the two accumulators and
+// writes the result or the partial result, under the next part's tiles.
 //
 // e4m3 caches: K and V enter the 8-bit MMA as they are; the bf16 queries and the fp32 probabilities as sums of three e5m2 terms,
 // each on columns of its own (N = 3 rows): x -> fp16, top byte, remainder, top byte, remainder, top byte, 9 significant bits.
@@ -27,8 +28,9 @@
 // Differential attention: two maps are two groups of columns.  Map a's scores are the k-steps of its half of K, its
 // probabilities meet the same V tile, and the epilogue subtracts and normalises: K and V are read once for both.
 //
-// Roles (384 threads): warp 0 TMA loads (a lane per page box), warp 1 MMA issue, warps 2-3 query rows into shared memory,
-// warps 4-7 and 8-11 softmax groups 0 and 1 (thread = key of the tile = lane of S^T, and output column = lane of O^T).
+// Roles (512 threads): warps 0 / 2 TMA loads of K / V (a lane per page box), warp 1 MMA issue, warp 3 the list of parts and the query
+// rows, warps 4-7 and 8-11 softmax groups 0 and 1 (thread = key of the tile = lane of S^T), warps 12-15 results (thread = output
+// column = lane of O^T).
 #pragma once
 
 #include <math.h>
@@ -148,14 +150,20 @@ struct PagedCfg {
     // bf16 values of 64: the upper 64 lanes of O^T multiply a block of zeros
     static constexpr bool kZeroBlock = !kE4m3 && DV == 64;
     static constexpr int kZeroBytes = kZeroBlock ? 2048 : 0;
-    static constexpr int kFixedBytes = 2 * kQBytes + 2 * kPBytes + kZeroBytes;
-    static constexpr int kBudget = 227 * 1024 - 12 * 1024;      // the rest is for PagedShared
+    static constexpr int kBudget = 227 * 1024 - (kStates <= 16 ? 4 : 8) * 1024;      // the rest is for PagedShared
+    // two probability buffers per group, one where two would not leave room for two stages
+    static constexpr int kPBufs = (kBudget - 2 * kQBytes - 4 * kPBytes - kZeroBytes) / (kKBytes + kVBytes) >= 2 ? 2 : 1;
+    static constexpr int kFixedBytes = 2 * kQBytes + 2 * kPBufs * kPBytes + kZeroBytes;
     static constexpr int kFit = (kBudget - kFixedBytes) / (kKBytes + kVBytes);
     static constexpr int kStages = kFit > 6 ? 6 : kFit;
     static_assert(kStages >= 2, "shared memory budget exceeded");
     static constexpr int kTileBytes = kFixedBytes + kStages * (kKBytes + kVBytes);
-    static constexpr int kTmemCols = 4 * kCols <= 64 ? 64 : 4 * kCols <= 128 ? 128 : 4 * kCols <= 256 ? 256 : 512;
-    static_assert(4 * kCols <= 512 && kCols % 16 == 0 && kCols <= 256, "accumulators");
+    // score buffers of both groups (4 or 2) and accumulators of both groups (for 2 parts or 1), as TMEM has room
+    static constexpr int kSBufs = 8 * kCols <= 512 ? 4 : 2;
+    static constexpr int kOBufs = kSBufs == 4 ? 2 : 1;
+    static constexpr int kUsedCols = (kSBufs + 2 * kOBufs) * kCols;
+    static constexpr int kTmemCols = kUsedCols <= 64 ? 64 : kUsedCols <= 128 ? 128 : kUsedCols <= 256 ? 256 : 512;
+    static_assert(kUsedCols <= 512 && kCols % 16 == 0 && kCols <= 256, "accumulators");
     static constexpr int kKSteps = DQK * kElem / 32;            // k-steps of 32 bytes
     static constexpr int kPSteps = 128 * kElem / 32;
     // exponents above the reference that a score may reach before the reference moves, and the scaling of P
@@ -163,25 +171,46 @@ struct PagedCfg {
     static constexpr float kBias = kE4m3 ? 13.f : 0.f;
 };
 
+// A part of the list as the roles of a CTA see it: tiles [t0, t1) of one (sequence, K/V head, row block).
+struct PagedEntry {
+    int b, kvh, rb, len, t0, t1;  // t1 < 0: the end of the CTA's share
+    int tile0;                    // index of the part's first tile in the CTA's share
+    int slot;                     // of the partial result, -1: the part is whole
+    int pieces, first_cta;        // of the whole (sequence, head, block), and the slot of its first piece
+    int first_slot;
+};
+constexpr int kPartRing = 8, kPartsAhead = 4;
+
+// Registers per thread after the per-role reallocation (512 threads start with 128 each): 128 x 80 + 256 x 152 + 128 x 128 = 65536.
+constexpr int kPagedRegsOther = 80, kPagedRegsSoftmax = 152;
+
 template <int kRows, int kMaps>
 struct PagedShared {
     uint64_t k_full[6], k_empty[6], v_full[6], v_empty[6];
     uint64_t q_full[2], q_empty[2];
-    uint64_t s_full[2], p_full[2], pv_done[2];
+    uint64_t s_full[2][2], p_full[2][2], pv_done[2][2];      // [group][buffer]
+    uint64_t stat_full[2], acc_full[2], acc_empty[2];        // [accumulator buffer]
+    uint64_t part_full[kPartRing], part_empty[kPartRing];
+    PagedEntry part[kPartRing];
     uint32_t tmem_base;
     uint32_t abort_flag;
     uint32_t is_last;
     int start_b;
-    long long start_base, total_units;
-    long long warp_sums[12];
-    struct Row { float c; int i; } row[2][kRows];        // factor of a score (log2 units), place among the new tokens
-    long long out_at[2][kRows];                          // offset of the row in O (-1: a padding row)
-    int out_hq[2][kRows];
-    float m[2][kMaps * kRows];                           // reference maximum per group and state
-    float rescale[2][kMaps * kRows];
-    float red[2][4][kMaps * kRows];                      // per group and warp: maxima, or row sums
-    float factor[2][kMaps * kRows];                      // weights of the two groups' accumulators
-    float sq[2][4][kRows];
+    long long start_base;
+    long long warp_sums[16];
+    alignas(16) float c[2][kRows];                       // per query buffer: factor of a score (log2 units)
+    int i[2][kRows];                                     // place among the new tokens
+    alignas(16) float neg_m[2][kMaps * kRows];           // per group: bias - reference maximum; +inf: no key seen yet
+    alignas(16) float rescale[2][kMaps * kRows];
+    float red[2][4][kMaps * kRows];
+    float stat_m[2][2][kMaps * kRows], stat_l[2][2][kMaps * kRows];      // [buffer][group]
+    // of the result warps
+    float factor[2][kMaps * kRows];
+    float out_m[kMaps * kRows], out_l[kMaps * kRows];
+    float weight[8][kMaps * kRows];
+    float sq[4][kRows];
+    long long out_at[kRows];                             // offset of the row in O (-1: a padding row)
+    int out_hq[kRows], out_i[kRows];
 };
 
 template <int DQK, int DV, bool kE4m3, bool kDiff, int kRows>
@@ -195,19 +224,21 @@ constexpr long long paged_slot_bytes(int dv, int states) { return states * (dv +
 // ------------------------------------------------------------------ kernel
 
 template <int DQK, int DV, bool kE4m3, bool kDiff, int kRows>
-__global__ void __launch_bounds__(384, 1)
+__global__ void __launch_bounds__(512, 1)
 fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const PagedParams p) {
     using Cfg = PagedCfg<DQK, DV, kE4m3, kDiff, kRows>;
     using Shared = PagedShared<kRows, Cfg::kMaps>;
     using namespace ptx;
     constexpr int NS = Cfg::kStages, kMaps = Cfg::kMaps, kTerms = Cfg::kTerms, kStates = Cfg::kStates, kCols = Cfg::kCols;
+    constexpr int kBufs = Cfg::kSBufs / 2;        // score buffers of a group
+    constexpr int kOBufs = Cfg::kOBufs, kPBufs = Cfg::kPBufs;
 
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     Shared& sh = *reinterpret_cast<Shared*>(smem_raw + Cfg::kTileBytes);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t smem_base = smem_addr(smem_raw);
     const uint32_t sK = smem_base, sV = sK + NS * Cfg::kKBytes, sQ = sV + NS * Cfg::kVBytes, sP = sQ + 2 * Cfg::kQBytes,
-                   sZero = sP + 2 * Cfg::kPBytes;
+                   sZero = sP + 2 * Cfg::kPBufs * Cfg::kPBytes;
 
     grid_launch_dependents();
     if ((smem_base & 1023u) != 0u) {          // uniform over the CTA; nothing has been set up yet
@@ -229,23 +260,38 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             mbar_init(smem_addr(&sh.v_empty[s]), 1);
         }
         for (int w = 0; w < 2; ++w) {
-            mbar_init(smem_addr(&sh.q_full[w]), 2);       // the two query warps
+            mbar_init(smem_addr(&sh.q_full[w]), 1);
             mbar_init(smem_addr(&sh.q_empty[w]), 3);      // the last score MMA and the two softmax groups
-            mbar_init(smem_addr(&sh.s_full[w]), 1);
-            mbar_init(smem_addr(&sh.p_full[w]), 4);       // four warps
-            mbar_init(smem_addr(&sh.pv_done[w]), 1);
+            for (int i = 0; i < 2; ++i) {
+                mbar_init(smem_addr(&sh.s_full[w][i]), 1);
+                mbar_init(smem_addr(&sh.p_full[w][i]), 4);      // four warps
+                mbar_init(smem_addr(&sh.pv_done[w][i]), 1);
+            }
+            mbar_init(smem_addr(&sh.stat_full[w]), 8);          // the softmax warps
+            mbar_init(smem_addr(&sh.acc_full[w]), 1);
+            mbar_init(smem_addr(&sh.acc_empty[w]), 1);
+        }
+        for (int i = 0; i < kPartRing; ++i) {
+            mbar_init(smem_addr(&sh.part_full[i]), 1);
+            mbar_init(smem_addr(&sh.part_empty[i]), 1);
         }
         fence_mbar_init();
         prefetch_tensormap(&tm_k);
         prefetch_tensormap(&tm_v);
     }
+    if (warp == 1) {
+        tmem_alloc(smem_addr(&sh.tmem_base), Cfg::kTmemCols);
+        tmem_relinquish_alloc_permit();
+    }
     if constexpr (Cfg::kZeroBlock) {
         if (tid < 128) st_shared_v4(sZero + tid * 16, 0, 0, 0, 0);
+        fence_proxy_async_smem();
     }
+    if (tid < 2 * kStates) sh.neg_m[tid / kStates][tid % kStates] = INFINITY;
     grid_dependency_wait();
 
     // ---- the shares: every thread sums up the units of consecutive sequences, a scan over the CTA finds the total
-    const int chunk = (p.B + 383) / 384;
+    const int chunk = (p.B + 511) / 512;
     const int b_first = tid * chunk, b_last = min(p.B, b_first + chunk);
     long long mine = 0;
     for (int b = b_first; b < b_last; ++b) mine += paged_units(p, b);
@@ -257,18 +303,23 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
     }
     if (lane == 31) sh.warp_sums[warp] = before;
     before -= mine;
-    if constexpr (Cfg::kZeroBlock) fence_proxy_async_smem();
+    tc_fence_before_sync();
     __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = sh.tmem_base;
     long long total = 0;
 #pragma unroll
-    for (int w = 0; w < 12; ++w) {
+    for (int w = 0; w < 16; ++w) {
         const long long x = sh.warp_sums[w];
         if (w < warp) before += x;
         total += x;
     }
     const long long share = paged_share(total, gridDim.x, p.least_units);
     const long long u0 = blockIdx.x * share, u1 = min(total, u0 + share);
-    if (u0 >= total) return;                  // uniform; no TMEM allocated yet
+    if (u0 >= total) {                        // uniform
+        if (warp == 1) tmem_dealloc(tmem, Cfg::kTmemCols);
+        return;
+    }
     if (before <= u0 && u0 < before + mine) {
         int b = b_first;
         long long base = before;
@@ -280,80 +331,70 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         sh.start_b = b;
         sh.start_base = base;
     }
-    if (warp == 1) {
-        tmem_alloc(smem_addr(&sh.tmem_base), Cfg::kTmemCols);
-        tmem_relinquish_alloc_permit();
-    }
-    if (tid < 2 * kStates) sh.m[tid / kStates][tid % kStates] = -INFINITY;
-    tc_fence_before_sync();
     __syncthreads();
-    tc_fence_after_sync();
-    const uint32_t tmem = sh.tmem_base;       // S^T of group w at w*kCols, O^T at (2 + w)*kCols
+    // TMEM: S^T of group w, buffer i at (w*kBufs + i)*kCols; O^T of accumulator buffer ob, group w behind them
+    auto s_col = [&](int w, int i) -> uint32_t { return (w * kBufs + i) * kCols; };
+    auto o_col = [&](int ob, int w) -> uint32_t { return (Cfg::kSBufs + ob * 2 + w) * kCols; };
     WaitCtx wctx{&sh.abort_flag, p.status, p.wait_limit_ns};
     const int group = p.Hq / p.Hkv;
-    PagedPart part;
+    auto wait_part = [&](int k) -> bool { return mbar_wait(smem_addr(&sh.part_full[k % kPartRing]), (k / kPartRing) & 1, wctx, kSiteItem); };
 
-    if (warp == 0) {
-        // ============================================================ TMA loads: lane i takes the i-th page box of a tile
-        part.begin(p, sh.start_b, sh.start_base, u0, u1, lane == 0);
-        const int box = p.box_rows, boxes = kTileN / box;
+    if (warp == 0 || warp == 2) {
+        // ============================================================ TMA loads of K (warp 0) or V (warp 2)
+        setmaxnreg_dec<kPagedRegsOther>();
+        const bool is_v = warp == 2;
+        const CUtensorMap* tm = is_v ? &tm_v : &tm_k;
+        uint64_t* const full = is_v ? sh.v_full : sh.k_full;
+        uint64_t* const empty = is_v ? sh.v_empty : sh.k_empty;
+        const uint32_t dst0 = is_v ? sV : sK, stage_bytes = is_v ? Cfg::kVBytes : Cfg::kKBytes;
+        const int chunks = is_v ? Cfg::kVChunks : Cfg::kKChunks;
+        const int box = p.box_rows, boxes = kTileN / box, tiles_ahead = 32 / boxes;
         int n = 0;
         bool ok = true;
-        do {
-            const int kvh = part.hr / p.row_blocks;
-            const long long row = part.b * p.table_stride;
-            // the box of this lane in tile t: its page (the pool's end, which reads as zeros, for a page that is none) and slot
-            auto look_up = [&](int t, int& page, int& slot) {
-                const int key = t * kTileN + lane * box;
-                page = -1;
-                if (lane < boxes && key < part.len) {
-                    const int at = key / p.page_size;
-                    slot = key - at * p.page_size;
-                    page = p.block_table[row + at];
-                    if (page < 0 || page >= p.num_pages) {
-                        report_bad_input(p.status, kSiteBadPage);
-                        page = p.num_pages;
+        for (int k = 0; ok; ++k) {
+            ok = __all_sync(0xffffffffu, wait_part(k));
+            if (!ok) break;
+            const PagedEntry e = sh.part[k % kPartRing];
+            if (e.t1 < 0) break;
+            const long long row = e.b * p.table_stride;
+            int pages = -1, slots = 0;        // of tile `first` + lane / boxes, box lane % boxes
+            int first = e.t0;
+            for (int t = e.t0; t < e.t1; ++t, ++n) {
+                if (t == e.t0 || t - first == tiles_ahead) {
+                    first = t;
+                    const int tile = t + lane / boxes, key = tile * kTileN + (lane % boxes) * box;
+                    pages = -1;
+                    if (tile < e.t1 && key < e.len) {
+                        const int at = key / p.page_size;
+                        slots = key - at * p.page_size;
+                        pages = p.block_table[row + at];
+                        if (pages < 0 || pages >= p.num_pages) {
+                            report_bad_input(p.status, kSiteBadPage);
+                            pages = p.num_pages;       // behind the pool: reads as zeros
+                        }
                     }
                 }
-            };
-            int page, slot = 0, next_page = -1, next_slot = 0;
-            look_up(part.t0, page, slot);
-            for (int t = part.t0; t < part.t1 && ok; ++t, ++n) {
-                if (t + 1 < part.t1) look_up(t + 1, next_page, next_slot);
+                const int from = (t - first) * boxes + lane;
+                const int page = __shfl_sync(0xffffffffu, pages, from & 31), slot = __shfl_sync(0xffffffffu, slots, from & 31);
                 const int s = n % NS;
-                const uint32_t parity = ((n / NS) & 1) ^ 1;
-                const int n_box = min(boxes, (max(0, part.len - t * kTileN) + box - 1) / box);
-                const uint32_t kb = smem_addr(&sh.k_full[s]), vb = smem_addr(&sh.v_full[s]);
-                ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&sh.k_empty[s]), parity, wctx, kSiteLoadKvEmpty));
+                ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&empty[s]), ((n / NS) & 1) ^ 1, wctx, kSiteLoadKvEmpty));
                 if (!ok) break;
-                if (lane == 0) mbar_arrive_expect_tx(kb, n_box * box * 128 * Cfg::kKChunks);
+                if (is_v && p.debug_drop_v_load && n == 0) continue;
+                const uint32_t bar = smem_addr(&full[s]);
+                const int n_box = min(boxes, (max(0, e.len - t * kTileN) + box - 1) / box);
+                if (lane == 0) mbar_arrive_expect_tx(bar, n_box * box * 128 * chunks);
                 __syncwarp();
-                if (page >= 0)
-#pragma unroll
-                    for (int c = 0; c < Cfg::kKChunks; ++c)
-                        tma_load_4d(sK + s * Cfg::kKBytes + c * kChunkBytes + lane * box * 128, &tm_k, kb, c * Cfg::kChunk, slot, kvh, page);
+                if (lane < n_box)
+                    for (int c = 0; c < chunks; ++c)
+                        tma_load_4d(dst0 + s * stage_bytes + c * kChunkBytes + lane * box * 128, tm, bar, c * Cfg::kChunk, slot, e.kvh, page);
                 __syncwarp();
-                if (!(p.debug_drop_v_load && n == 0)) {
-                    ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&sh.v_empty[s]), parity, wctx, kSiteLoadKvEmpty));
-                    if (!ok) break;
-                    if (lane == 0) mbar_arrive_expect_tx(vb, n_box * box * 128 * Cfg::kVChunks);
-                    __syncwarp();
-                    if (page >= 0)
-#pragma unroll
-                        for (int c = 0; c < Cfg::kVChunks; ++c)
-                            tma_load_4d(sV + s * Cfg::kVBytes + c * kChunkBytes + lane * box * 128, &tm_v, vb, c * Cfg::kChunk, slot, kvh, page);
-                    __syncwarp();
-                }
-                page = next_page;
-                slot = next_slot;
             }
-        } while (ok && part.next(p));
+        }
     } else if (warp == 1) {
         // ============================================================ MMA issue, one thread
+        setmaxnreg_dec<kPagedRegsOther>();
         if (elect_one()) {
-            part.begin(p, sh.start_b, sh.start_base, u0, u1, false);
-            const int n_total = static_cast<int>(u1 - u0);
-            constexpr uint32_t kIdescQK = kE4m3 ? (make_idesc_e4m3_f32(128, Cfg::kQRows, false, false) | (1u << 10))
+            constexpr uint32_t kIdescQK = kE4m3 ? (make_idesc_e4m3_f32(128, Cfg::kQRows, false, false) | (1u << 10))      // B: e5m2
                                                 : make_idesc_bf16_f32(128, Cfg::kQRows, false, false);
             constexpr uint32_t kIdescPV = kE4m3 ? (make_idesc_e4m3_f32(128, kCols, true, false) | (1u << 10))
                                                 : make_idesc_bf16_f32(128, kCols, true, false);
@@ -361,116 +402,159 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                 if constexpr (kE4m3) mma_ss_f8(d, a, b, idesc, acc);
                 else mma_ss(d, a, b, idesc, acc);
             };
-            bool ok = true;
-            int seg = 0, left = part.t1 - part.t0;           // of the score products: segment and its tiles to come
-            auto scores = [&](int n) -> bool {
-                const int w = n & 1, s = n % NS, qb = seg & 1;
-                if (left == part.t1 - part.t0 && !mbar_wait(smem_addr(&sh.q_full[qb]), (seg >> 1) & 1, wctx, kSiteMmaQFull)) return false;
-                if (!mbar_wait(smem_addr(&sh.k_full[s]), (n / NS) & 1, wctx, kSiteMmaKvFull)) return false;
+            bool ok = true, more = true;
+            int nq = 0, qk = -1, q_left = 0;           // score products issued; their part and its tiles to come
+            auto scores = [&]() {
+                if (q_left == 0) {
+                    ++qk;
+                    if (!(ok = wait_part(qk))) return;
+                    const PagedEntry& e = sh.part[qk % kPartRing];
+                    if (e.t1 < 0) { more = false; return; }
+                    q_left = e.t1 - e.t0;
+                    if (!(ok = mbar_wait(smem_addr(&sh.q_full[qk & 1]), (qk >> 1) & 1, wctx, kSiteMmaQFull))) return;
+                }
+                const int w = nq & 1, i = (nq >> 1) % kBufs, s = nq % NS;
+                if (!(ok = mbar_wait(smem_addr(&sh.k_full[s]), (nq / NS) & 1, wctx, kSiteMmaKvFull))) return;
                 tc_fence_after_sync();
-                const uint32_t a0 = sK + s * Cfg::kKBytes, b0 = sQ + qb * Cfg::kQBytes;
+                const uint32_t a0 = sK + s * Cfg::kKBytes, b0 = sQ + (qk & 1) * Cfg::kQBytes;
                 constexpr int kPerMap = Cfg::kKSteps / kMaps;
 #pragma unroll
                 for (int m = 0; m < kMaps; ++m)
 #pragma unroll
                     for (int j = 0; j < kPerMap; ++j) {
-                        const int k = m * kPerMap + j;
-                        mma(tmem + w * kCols + m * Cfg::kQRows,
-                            make_smem_desc_sw128(a0 + (k / 4) * kChunkBytes + (k % 4) * 32, 16, 1024),
-                            make_smem_desc_sw128(b0 + (k / 4) * Cfg::kQChunkBytes + (k % 4) * 32, 16, 1024), kIdescQK, j > 0 ? 1u : 0u);
+                        const int ks = m * kPerMap + j;
+                        mma(tmem + s_col(w, i) + m * Cfg::kQRows,
+                            make_smem_desc_sw128(a0 + (ks / 4) * kChunkBytes + (ks % 4) * 32, 16, 1024),
+                            make_smem_desc_sw128(b0 + (ks / 4) * Cfg::kQChunkBytes + (ks % 4) * 32, 16, 1024), kIdescQK, j > 0 ? 1u : 0u);
                     }
-                tc_commit(smem_addr(&sh.s_full[w]));
+                tc_commit(smem_addr(&sh.s_full[w][i]));
                 tc_commit(smem_addr(&sh.k_empty[s]));
-                if (--left == 0) {
-                    tc_commit(smem_addr(&sh.q_empty[qb]));
-                    ++seg;
-                    if (part.next(p)) left = part.t1 - part.t0;
-                }
-                return true;
+                if (--q_left == 0) tc_commit(smem_addr(&sh.q_empty[qk & 1]));
+                ++nq;
             };
-            // the same walk again for the second products: a group's accumulator starts anew with each part
-            PagedPart pv;
-            pv.begin(p, sh.start_b, sh.start_base, u0, u1, false);
-            int pv_done = 0, pv_tiles = pv.t1 - pv.t0;
-            ok = scores(0);
-            if (ok && n_total > 1) ok = scores(1);
-            for (int n = 0; n < n_total && ok; ++n) {
-                const int w = n & 1, s = n % NS;
+#pragma unroll 1
+            for (int i = 0; i < Cfg::kSBufs && ok && more; ++i) scores();
+            int pk = -1, p_left = 0, p_done = 0;       // part of the second products
+#pragma unroll 1
+            for (int n = 0; ok && n < nq; ++n) {
+                if (p_left == 0) {
+                    ++pk;
+                    const PagedEntry& e = sh.part[pk % kPartRing];       // (published: its scores have been issued)
+                    p_left = e.t1 - e.t0;
+                    p_done = 0;
+                    if (!(ok = mbar_wait(smem_addr(&sh.acc_empty[pk % kOBufs]), ((pk / kOBufs) & 1) ^ 1, wctx, kSiteMmaOReady))) break;
+                }
+                const int w = n & 1, i = (n >> 1) % kPBufs, s = n % NS;
                 ok = mbar_wait(smem_addr(&sh.v_full[s]), (n / NS) & 1, wctx, kSiteMmaKvFull) &&
-                     mbar_wait(smem_addr(&sh.p_full[w]), (n >> 1) & 1, wctx, kSiteMmaPFull);
+                     mbar_wait(smem_addr(&sh.p_full[w][i]), ((n >> 1) / kPBufs) & 1, wctx, kSiteMmaPFull);
                 if (!ok) break;
                 tc_fence_after_sync();
-                const uint32_t a0 = sV + s * Cfg::kVBytes, b0 = sP + w * Cfg::kPBytes;
+                const uint32_t a0 = sV + s * Cfg::kVBytes, b0 = sP + (w * kPBufs + i) * Cfg::kPBytes;
+                const uint32_t acc = p_done >= 2 ? 1u : 0u;              // the group's first tile of the part overwrites
 #pragma unroll
-                for (int k = 0; k < Cfg::kPSteps; ++k) {
+                for (int ks = 0; ks < Cfg::kPSteps; ++ks) {
                     constexpr int kStepBytes = (32 / Cfg::kElem) * 128;        // keys of a k-step x 128 bytes
-                    const uint32_t a = a0 + k * kStepBytes;
+                    const uint32_t a = a0 + ks * kStepBytes;
                     const uint32_t lbo = Cfg::kZeroBlock ? sZero - a : static_cast<uint32_t>(kChunkBytes);
-                    mma(tmem + (2 + w) * kCols, make_smem_desc_sw128(a, lbo, 1024),
-                        make_smem_desc_sw128(b0 + (k / 4) * Cfg::kPChunkBytes + (k % 4) * 32, 16, 1024), kIdescPV,
-                        (pv_done >= 2 || k > 0) ? 1u : 0u);
+                    mma(tmem + o_col(pk % kOBufs, w), make_smem_desc_sw128(a, lbo, 1024),
+                        make_smem_desc_sw128(b0 + (ks / 4) * Cfg::kPChunkBytes + (ks % 4) * 32, 16, 1024), kIdescPV, ks > 0 ? 1u : acc);
                 }
                 tc_commit(smem_addr(&sh.v_empty[s]));
-                tc_commit(smem_addr(&sh.pv_done[w]));
-                if (++pv_done == pv_tiles && pv.next(p)) {
-                    pv_done = 0;
-                    pv_tiles = pv.t1 - pv.t0;
-                }
-                if (n + 2 < n_total) ok = scores(n + 2);
+                tc_commit(smem_addr(&sh.pv_done[w][i]));
+                ++p_done;
+                if (--p_left == 0) tc_commit(smem_addr(&sh.acc_full[pk % kOBufs]));
+                if (more) scores();
             }
         }
-    } else if (warp < 4) {
-        // ============================================================ query rows -> shared memory, and what is known of each
-        part.begin(p, sh.start_b, sh.start_base, u0, u1, false);
-        int seg = 0;
-        bool ok = true;
-        do {
-            const int qb = seg & 1;
-            ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&sh.q_empty[qb]), ((seg >> 1) & 1) ^ 1, wctx, kSiteLoadQEmpty));
+    } else if (warp == 3) {
+        // ============================================================ the list of parts, kPartsAhead ahead of their query rows
+        setmaxnreg_dec<kPagedRegsOther>();
+        PagedPart walk;
+        walk.begin(p, sh.start_b, sh.start_base, u0, u1, lane == 0);
+        bool ended = false, ok = true;
+        int published = 0;
+        auto publish = [&]() {                     // uniform over the warp
+            if (ended) return;
+            const int at = published % kPartRing;
+            ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&sh.part_empty[at]), ((published / kPartRing) & 1) ^ 1, wctx, kSiteItem));
+            if (!ok) return;
+            if (lane == 0) {
+                PagedEntry& e = sh.part[at];
+                const bool whole = walk.t1 - walk.t0 == walk.nt;
+                const long long ua = walk.first_unit();
+                e.b = walk.b;
+                e.kvh = walk.hr / p.row_blocks;
+                e.rb = walk.hr - e.kvh * p.row_blocks;
+                e.len = walk.len;
+                e.t0 = walk.t0;
+                e.t1 = walk.u < u1 ? walk.t1 : -1;
+                e.tile0 = static_cast<int>(walk.u - u0);
+                e.slot = whole ? -1 : paged_slot(blockIdx.x, ua, share);
+                e.pieces = whole ? 1 : paged_pieces(ua, ua + walk.nt, share);
+                e.first_cta = whole ? 0 : paged_first_cta(ua, share);
+                e.first_slot = whole ? -1 : paged_slot(e.first_cta, ua, share);
+                mbar_arrive(smem_addr(&sh.part_full[at]));
+            }
+            __syncwarp();
+            ++published;
+            if (walk.u >= u1) ended = true;        // that was the end mark
+            else walk.next(p);
+        };
+        for (int i = 0; i < kPartsAhead; ++i) publish();
+        constexpr int kVecs = DQK / 8;                        // 16-byte pieces of a row
+        constexpr int kLanes = kVecs == 24 ? 32 : kVecs;      // lanes of a row
+        constexpr int kPass = 32 / kLanes;                    // rows of a pass over the warp
+        constexpr int kBatch = 8;                             // passes whose loads are in flight together
+        static_assert(kRows / kPass % kBatch == 0 || kRows / kPass < kBatch, "query rows");
+        constexpr int kInFlight = kRows / kPass < kBatch ? kRows / kPass : kBatch;
+        for (int k = 0; ok; ++k) {
+            publish();
             if (!ok) break;
-            const int kvh = part.hr / p.row_blocks, rb = part.hr - kvh * p.row_blocks;
-            constexpr int kVecs = DQK / 8;                        // 16-byte pieces of a row
-            const float ks = kE4m3 && p.k_scale ? p.k_scale[kvh] : 1.f;
-            // a warp takes every other row, a lane a piece of it
-            constexpr int kBatch = kRows / 2 < 8 ? kRows / 2 : 8;
+            const PagedEntry e = sh.part[k % kPartRing];
+            if (e.t1 < 0) break;
+            const int qb = k & 1;
+            const float ks = kE4m3 && p.k_scale ? p.k_scale[e.kvh] : 1.f;
+            const uint32_t sQb = sQ + qb * Cfg::kQBytes;
+            const int row_in = lane / kLanes, piece = lane % kLanes;
+            bool waited = false;
 #pragma unroll 1
-            for (int r0 = 0; r0 < kRows / 2; r0 += kBatch) {
-                uint4 x[kBatch];
+            for (int r0 = 0; r0 < kRows; r0 += kInFlight * kPass) {
+                uint4 x[kInFlight];
+                int place[kInFlight];
 #pragma unroll
-                for (int e = 0; e < kBatch; ++e) {
-                    const int r = 2 * (r0 + e) + (warp - 2), rr = rb * kRows + r, i = rr / group, hq = kvh * group + rr - i * group;
-                    const bool live = i < p.Sq;
-                    x[e] = make_uint4(0, 0, 0, 0);
-                    if (live && lane < kVecs)
-                        x[e] = *reinterpret_cast<const uint4*>(p.Q + part.b * p.q_sb + i * p.q_st + hq * p.q_sh + lane * 8);
-                    if (lane == 0) {
-                        sh.row[qb][r].i = live ? i : p.Sq - 1;
-                        sh.row[qb][r].c = p.scale_log2 * ks;
-                        sh.out_at[qb][r] = live ? part.b * p.o_sb + i * p.o_st + hq * p.o_sh : -1;
-                        sh.out_hq[qb][r] = hq;
-                    }
+                for (int j = 0; j < kInFlight; ++j) {
+                    const int r = r0 + j * kPass + row_in, rr = e.rb * kRows + r, i = rr / group, hq = e.kvh * group + rr - i * group;
+                    x[j] = make_uint4(0, 0, 0, 0);
+                    if (i < p.Sq && piece < kVecs)
+                        x[j] = *reinterpret_cast<const uint4*>(p.Q + e.b * p.q_sb + i * p.q_st + hq * p.q_sh + piece * 8);
+                    place[j] = min(i, p.Sq - 1);
+                }
+                if (!waited) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&sh.q_empty[qb]), ((k >> 1) & 1) ^ 1, wctx, kSiteLoadQEmpty));
+                    waited = true;
+                    if (!ok) break;
                 }
 #pragma unroll
-                for (int e = 0; e < kBatch; ++e) {
-                    const int r = 2 * (r0 + e) + (warp - 2);
+                for (int j = 0; j < kInFlight; ++j) {
+                    const int r = r0 + j * kPass + row_in;
+                    float c = p.scale_log2 * ks;
                     if constexpr (!kE4m3) {
-                        if (lane < kVecs)
-                            st_shared_v4(sQ + qb * Cfg::kQBytes + (lane >> 3) * Cfg::kQChunkBytes + r * 128 + (((lane & 7) ^ (r & 7)) << 4),
-                                         x[e].x, x[e].y, x[e].z, x[e].w);
+                        if (piece < kVecs)
+                            st_shared_v4(sQb + (piece >> 3) * Cfg::kQChunkBytes + r * 128 + (((piece & 7) ^ (r & 7)) << 4),
+                                         x[j].x, x[j].y, x[j].z, x[j].w);
                     } else {
                         // scaled by a power of two so that the row's largest entry is in [2^14, 2^15), then three e5m2 terms: exact for
                         // entries of 2^-24 of the largest and more, below that to 2^-31 of it
-                        const uint32_t w4[4] = {x[e].x, x[e].y, x[e].z, x[e].w};
+                        const uint32_t w4[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
                         uint32_t top = 0;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            top = max(top, (w4[i] & 0x7fffu) << 16);
-                            top = max(top, w4[i] & 0x7fff0000u);
-                        }
-                        top = __reduce_max_sync(0xffffffffu, top);
+                        for (int i = 0; i < 4; ++i) top = max(top, max((w4[i] & 0x7fffu) << 16, w4[i] & 0x7fff0000u));
+#pragma unroll
+                        for (int d = kLanes / 2; d > 0; d >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
                         int sft = top ? 14 - (static_cast<int>(top >> 23) - 127) : 0;
                         sft = sft > 100 ? 100 : (sft < -100 ? -100 : sft);
                         const float mult = __uint_as_float(static_cast<uint32_t>(sft + 127) << 23);
+                        c *= __uint_as_float(static_cast<uint32_t>(127 - sft) << 23);
                         uint32_t t8[3][2];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
@@ -483,104 +567,144 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                                 h = __hsub2(h, *reinterpret_cast<__half2*>(&bits));
                             }
                         }
-                        if (lane < kVecs) {
+                        if (piece < kVecs) {
 #pragma unroll
                             for (int t = 0; t < 3; ++t) {
-                                const int rq = t * kRows + r, piece = lane >> 1;
-                                st_shared_u64(sQ + qb * Cfg::kQBytes + (piece >> 3) * Cfg::kQChunkBytes + rq * 128 +
-                                                  (((piece & 7) ^ (rq & 7)) << 4) + (lane & 1) * 8, t8[t][0], t8[t][1]);
+                                const int rq = t * kRows + r, q16 = piece >> 1;
+                                st_shared_u64(sQb + (q16 >> 3) * Cfg::kQChunkBytes + rq * 128 + (((q16 & 7) ^ (rq & 7)) << 4) + (piece & 1) * 8,
+                                              t8[t][0], t8[t][1]);
                             }
                         }
-                        if (lane == 0) sh.row[qb][r].c = p.scale_log2 * ks * __uint_as_float(static_cast<uint32_t>(127 - sft) << 23);
+                    }
+                    if (piece == 0) {
+                        sh.c[qb][r] = c;
+                        sh.i[qb][r] = place[j];
                     }
                 }
             }
+            if (!ok) break;
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_addr(&sh.q_full[qb]));
-            ++seg;
-        } while (part.next(p));
-    } else {
+        }
+    } else if (warp < 12) {
         // ============================================================ softmax groups
-        // No thread leaves this branch early: after a wait that ran out every later wait returns at once, and the groups go on
-        // through their barriers (results are invalid then, every access stays in bounds).
+        // The four warps of a group stay together through their barriers: after a wait that ran out they go on to the end of
+        // the part without waiting (results are invalid then, every access stays in bounds) and leave together.
+        setmaxnreg_inc<kPagedRegsSoftmax>();
         const int w = (warp >> 2) - 1, key = tid & 127, wq = warp & 3;
         const uint32_t lane_sel = static_cast<uint32_t>(wq * 32) << 16;
-        const uint32_t tS = tmem + w * kCols + lane_sel, tO = tmem + (2 + w) * kCols + lane_sel;
-        const uint32_t sPw = sP + w * Cfg::kPBytes + (kE4m3 ? 0 : (key >> 6) * Cfg::kPChunkBytes);
         const uint32_t p_byte = kE4m3 ? key : (key & 63) * 2;            // of this key in a row of P
-        part.begin(p, sh.start_b, sh.start_base, u0, u1, false);
         float l[kStates];
 #pragma unroll
         for (int r = 0; r < kStates; ++r) l[r] = 0.f;
-        int n = 0, seg = 0;
+        int mine_n = 0;                                                  // tiles this group has done
         bool ok = true;
-        do {
-            const int qb = seg & 1;
-            ok = ok && mbar_wait(smem_addr(&sh.q_full[qb]), (seg >> 1) & 1, wctx, kSiteMmaQFull);
+        for (int k = 0;; ++k) {
+            const int qb = k & 1;
+            ok = ok && wait_part(k);
+            const PagedEntry e = sh.part[k % kPartRing];
+            if (named_barrier_or(1 + w, 128, !ok) || e.t1 < 0) break;
+            ok = mbar_wait(smem_addr(&sh.q_full[qb]), (k >> 1) & 1, wctx, kSiteMmaQFull);
             bool any_tile = false;
-            const int first_masked = part.len - p.Sq + 1;                // the first key that some row does not see
+            const int first_masked = e.len - p.Sq + 1;                   // the first key that some row does not see
+            int n = e.tile0 + ((e.tile0 & 1) == w ? 0 : 1);              // this group's first tile
+            const uint32_t tO = tmem + o_col(k % kOBufs, w) + lane_sel;
 #pragma unroll 1
-            for (int t = part.t0; t < part.t1; ++t, ++n) {
-                if ((n & 1) != w) continue;
-                ok = ok && mbar_wait(smem_addr(&sh.s_full[w]), (n >> 1) & 1, wctx, kSiteSoftmaxSFull);
+            for (int t = e.t0 + n - e.tile0; t < e.t1; t += 2, n += 2, ++mine_n) {
+                const int sb = mine_n % kBufs, pb = mine_n % kPBufs;
+                const uint32_t tS = tmem + s_col(w, sb) + lane_sel;
+                const uint32_t sPw = sP + (w * kPBufs + pb) * Cfg::kPBytes + (kE4m3 ? 0 : (key >> 6) * Cfg::kPChunkBytes);
+                ok = ok && mbar_wait(smem_addr(&sh.s_full[w][sb]), (mine_n / kBufs) & 1, wctx, kSiteSoftmaxSFull);
                 __syncwarp();
                 tc_fence_after_sync();
-                float x[kStates];
-#pragma unroll
-                for (int g = 0; g < kStates / 16; ++g) {
-                    // column of (map, term, row): (map * kTerms + term) * kRows + row
-                    const int map = g * 16 / kRows, r0 = g * 16 % kRows;
-                    uint32_t s0[16];
-                    tmem_ld_x16(tS + map * kTerms * kRows + r0, s0);
-                    if constexpr (kE4m3) {
-                        uint32_t s1[16], s2[16];
-                        tmem_ld_x16(tS + (map * kTerms + 1) * kRows + r0, s1);
-                        tmem_ld_x16(tS + (map * kTerms + 2) * kRows + r0, s2);
-                        tc_wait_ld();
-#pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            x[g * 16 + e] = __uint_as_float(s0[e]) + (__uint_as_float(s1[e]) + __uint_as_float(s2[e]));
-                    } else {
-                        tc_wait_ld();
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) x[g * 16 + e] = __uint_as_float(s0[e]);
-                    }
-                }
                 const int key_at = t * kTileN + key;
-                if (kE4m3) {
+                const bool masked = t * kTileN + kTileN > first_masked;
+                float x[kStates];
+                for (int pass = 0;; ++pass) {
 #pragma unroll
-                    for (int r = 0; r < kStates; ++r) x[r] *= sh.row[qb][r % kRows].c;
-                } else {
+                    for (int g = 0; g < kStates / 16; ++g) {
+                        // column of (map, term, row): (map * kTerms + term) * kRows + row
+                        const int map = g * 16 / kRows, r0 = g * 16 % kRows;
+                        uint32_t s0[16];
+                        tmem_ld_x16(tS + map * kTerms * kRows + r0, s0);
+                        if constexpr (kE4m3) {
+                            uint32_t s1[16], s2[16];
+                            tmem_ld_x16(tS + (map * kTerms + 1) * kRows + r0, s1);
+                            tmem_ld_x16(tS + (map * kTerms + 2) * kRows + r0, s2);
+                            tc_wait_ld();
 #pragma unroll
-                    for (int r = 0; r < kStates; ++r) x[r] *= p.scale_log2;
-                }
-                if (t * kTileN + kTileN > first_masked) {
+                            for (int j = 0; j < 16; ++j)
+                                s0[j] = __float_as_uint(__uint_as_float(s0[j]) + (__uint_as_float(s1[j]) + __uint_as_float(s2[j])));
+                        } else {
+                            tc_wait_ld();
+                        }
 #pragma unroll
-                    for (int r = 0; r < kStates; ++r)
-                        if (key_at >= first_masked + sh.row[qb][r % kRows].i) x[r] = -INFINITY;
-                }
-                bool over = false;
+                        for (int j = 0; j < 16; j += 4) {
+                            const float4 nm = *reinterpret_cast<const float4*>(&sh.neg_m[w][g * 16 + j]);
+                            float4 c = make_float4(p.scale_log2, p.scale_log2, p.scale_log2, p.scale_log2);
+                            if constexpr (kE4m3) c = *reinterpret_cast<const float4*>(&sh.c[qb][r0 + j]);
+                            // product and sum rounded apart: the score that the reference was taken from comes out as exactly
+                            // the bias, however large it is (a fused one could leave half a unit of its last place)
+                            const float2 lo = __fadd2_rn(__fmul2_rn(make_float2(__uint_as_float(s0[j]), __uint_as_float(s0[j + 1])),
+                                                                    make_float2(c.x, c.y)), make_float2(nm.x, nm.y));
+                            const float2 hi = __fadd2_rn(__fmul2_rn(make_float2(__uint_as_float(s0[j + 2]), __uint_as_float(s0[j + 3])),
+                                                                    make_float2(c.z, c.w)), make_float2(nm.z, nm.w));
+                            x[g * 16 + j] = lo.x;
+                            x[g * 16 + j + 1] = lo.y;
+                            x[g * 16 + j + 2] = hi.x;
+                            x[g * 16 + j + 3] = hi.y;
+                        }
+                    }
+                    if (masked) {
 #pragma unroll
-                for (int r = 0; r < kStates; ++r) over |= x[r] > sh.m[w][r] + Cfg::kTauLog2;
-                if (named_barrier_or(1 + w, 128, over)) {
+                        for (int r = 0; r < kStates; ++r)
+                            if (key_at >= first_masked + sh.i[qb][r % kRows]) x[r] = -INFINITY;
+                    }
+                    float top = x[0];
 #pragma unroll
-                    for (int r = 0; r < kStates; ++r) {
-                        const float mx = warp_max(x[r]);
-                        if (lane == 0) sh.red[w][wq][r] = mx;
+                    for (int r = 1; r + 1 < kStates; r += 2) top = fmax3(top, x[r], x[r + 1]);
+                    top = fmaxf(top, x[kStates - 1]);
+                    if (!named_barrier_or(1 + w, 128, top > Cfg::kTauLog2 + Cfg::kBias) || pass > 0) break;
+                    // some row's reference moves: the maxima of the tile's scores, in log2 units
+#pragma unroll
+                    for (int g = 0; g < kStates / 16; ++g) {
+                        const int map = g * 16 / kRows, r0 = g * 16 % kRows;
+                        uint32_t s0[16];
+                        tmem_ld_x16(tS + map * kTerms * kRows + r0, s0);
+                        if constexpr (kE4m3) {
+                            uint32_t s1[16], s2[16];
+                            tmem_ld_x16(tS + (map * kTerms + 1) * kRows + r0, s1);
+                            tmem_ld_x16(tS + (map * kTerms + 2) * kRows + r0, s2);
+                            tc_wait_ld();
+#pragma unroll
+                            for (int j = 0; j < 16; ++j)
+                                s0[j] = __float_as_uint(__uint_as_float(s0[j]) + (__uint_as_float(s1[j]) + __uint_as_float(s2[j])));
+                        } else {
+                            tc_wait_ld();
+                        }
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            float v = __uint_as_float(s0[j]) * (kE4m3 ? sh.c[qb][r0 + j] : p.scale_log2);
+                            if (masked && key_at >= first_masked + sh.i[qb][r0 + j]) v = -INFINITY;
+                            const float mx = warp_max(v);
+                            if (lane == 0) sh.red[w][wq][g * 16 + j] = mx;
+                        }
                     }
                     named_barrier_sync(1 + w, 128);
                     if (key < kStates) {
-                        const float old = sh.m[w][key];
+                        const float old = Cfg::kBias - sh.neg_m[w][key];
                         const float mx = fmaxf(fmaxf(fmaxf(sh.red[w][0][key], sh.red[w][1][key]), fmaxf(sh.red[w][2][key], sh.red[w][3][key])), old);
-                        sh.m[w][key] = mx;
+                        sh.neg_m[w][key] = Cfg::kBias - mx;
                         sh.rescale[w][key] = mx == -INFINITY ? 1.f : exp2_approx(old - mx);
                     }
+                    if (any_tile)         // the group's product before: it has been handed over, nothing else adds to this accumulator
+                        ok = ok && mbar_wait(smem_addr(&sh.pv_done[w][(mine_n - 1) % kPBufs]), ((mine_n - 1) / kPBufs) & 1, wctx, kSiteSoftmaxCorrFree);
                     named_barrier_sync(1 + w, 128);
 #pragma unroll
                     for (int r = 0; r < kStates; ++r) l[r] *= sh.rescale[w][r];
                     if (any_tile) {
-                        // PV of this group's tile before is complete (these scores were issued after it), the next one waits for us
+                        tc_fence_after_sync();
 #pragma unroll 1
                         for (int g = 0; g < kCols / 16; ++g) {
                             const int col = g * 16, st = col / (kTerms * kRows) * kRows + col % kRows;
@@ -588,18 +712,25 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                             tmem_ld_x16(tO + col, o);
                             tc_wait_ld();
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * sh.rescale[w][st + e]);
+                            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * sh.rescale[w][st + j]);
                             tmem_st_x16(tO + col, o);
                         }
                         tc_wait_st();
                     }
                 }
+                if (masked) {
+                    // (a row that has seen no key yet: -inf + inf)
+#pragma unroll
+                    for (int r = 0; r < kStates; ++r)
+                        if (sh.neg_m[w][r] == INFINITY) x[r] = -INFINITY;
+                }
 #pragma unroll
                 for (int r = 0; r < kStates; ++r) {
-                    const float m = sh.m[w][r];
-                    x[r] = exp2_approx(x[r] - ((m == -INFINITY ? 0.f : m) - Cfg::kBias));
+                    x[r] = exp2_approx(x[r]);
                     l[r] += x[r];
                 }
+                // the buffer's last reader: the product of the group's tile kPBufs before
+                if (mine_n >= kPBufs) ok = ok && mbar_wait(smem_addr(&sh.pv_done[w][pb]), ((mine_n / kPBufs) & 1) ^ 1, wctx, kSiteSoftmaxPFree);
                 // P^T: row = column of O^T, 128 keys of 1 or 2 bytes, 16-byte pieces swizzled
                 if constexpr (kE4m3) {
 #pragma unroll
@@ -622,11 +753,11 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                         st_shared_u16(sPw + (r + 1) * 128 + (p_byte ^ (((r + 1) & 7) << 4)), two >> 16);
                     }
                 }
-                if (t * kTileN + kTileN > part.len) {
+                if (t * kTileN + kTileN > e.len) {
                     // V rows behind the sequence's end hold whatever the page held, or were not loaded: zeros, since 0 * NaN is NaN
                     const int s = n % NS;
                     ok = ok && mbar_wait(smem_addr(&sh.v_full[s]), (n / NS) & 1, wctx, kSiteSoftmaxPFree);
-                    if (key_at >= part.len) {
+                    if (key_at >= e.len) {
 #pragma unroll
                         for (int c = 0; c < Cfg::kVChunks * 8; ++c)
                             st_shared_v4(sV + s * Cfg::kVBytes + (c >> 3) * kChunkBytes + key * 128 + (c & 7) * 16, 0, 0, 0, 0);
@@ -636,203 +767,211 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                 fence_proxy_async_smem();
                 tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_addr(&sh.p_full[w]));
+                if (lane == 0) mbar_arrive(smem_addr(&sh.p_full[w][pb]));
             }
 
-            // ---- end of a part: the groups' accumulators become one
-            // row sums over the 128 threads of the group: 16 columns at a time, halved at each exchange
+            // ---- end of the part: maxima and row sums to the result warps
+            const int ob = k % kOBufs;
+            ok = ok && mbar_wait(smem_addr(&sh.acc_empty[ob]), ((k / kOBufs) & 1) ^ 1, wctx, kSiteEpiState);
+            named_barrier_sync(1 + w, 128);                              // (neg_m has been read by all)
+            // sums over the 128 threads: 16 columns at a time, halved at each exchange
 #pragma unroll
             for (int g = 0; g < kStates / 16; ++g) {
                 float a[16];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) a[e] = l[g * 16 + e];
+                for (int j = 0; j < 16; ++j) a[j] = l[g * 16 + j];
 #pragma unroll
                 for (int d = 16, m = 8; d >= 2; d >>= 1, m >>= 1) {
                     const bool up = (lane & d) != 0;
 #pragma unroll
-                    for (int e = 0; e < m; ++e) {
-                        const float give = up ? a[e] : a[e + m], keep = up ? a[e + m] : a[e];
-                        a[e] = keep + __shfl_xor_sync(0xffffffffu, give, d);
+                    for (int j = 0; j < m; ++j) {
+                        const float give = up ? a[j] : a[j + m], keep = up ? a[j + m] : a[j];
+                        a[j] = keep + __shfl_xor_sync(0xffffffffu, give, d);
                     }
                 }
                 a[0] += __shfl_xor_sync(0xffffffffu, a[0], 1);
                 // lane bits 4, 3, 2, 1 chose the halves: column = bit4*8 + bit3*4 + bit2*2 + bit1
                 if ((lane & 1) == 0) sh.red[w][wq][g * 16 + (lane >> 1)] = a[0];
             }
-            if (any_tile) {
-                const int last = ((n - 1) & 1) == w ? n - 1 : n - 2;       // this group's last tile
-                ok = ok && mbar_wait(smem_addr(&sh.pv_done[w]), (last >> 1) & 1, wctx, kSiteEpiOFull);
+            named_barrier_sync(1 + w, 128);
+            if (key < kStates) {
+                sh.stat_l[ob][w][key] = (sh.red[w][0][key] + sh.red[w][1][key]) + (sh.red[w][2][key] + sh.red[w][3][key]);
+                sh.stat_m[ob][w][key] = Cfg::kBias - sh.neg_m[w][key];
+                sh.neg_m[w][key] = INFINITY;
             }
+#pragma unroll
+            for (int r = 0; r < kStates; ++r) l[r] = 0.f;
             __syncwarp();
-            tc_fence_before_sync();
-            named_barrier_sync(3, 256);
-            tc_fence_after_sync();
-            const long long ua = part.first_unit();
-            const bool whole = part.t1 - part.t0 == part.nt;
-            const int gt = tid - 128;                                     // 0..255
-            const int slot = whole ? 0 : paged_slot(blockIdx.x, ua, share);
-            float* const slot_o = p.part + static_cast<long long>(slot) * kStates * (DV + 2);
+            if (lane == 0) mbar_arrive(smem_addr(&sh.stat_full[ob]));
+            named_barrier_sync(1 + w, 128);                              // the next part reads neg_m
+            if (key == 0) mbar_arrive(smem_addr(&sh.q_empty[qb]));
+        }
+    } else {
+        // ============================================================ results: thread = output column
+        const int key = tid & 127, wq = warp & 3;
+        const uint32_t lane_sel = static_cast<uint32_t>(wq * 32) << 16;
+        constexpr uint32_t kBar = 3;
+        bool ok = true;
+        for (int k = 0;; ++k) {
+            ok = ok && wait_part(k);
+            const PagedEntry e = sh.part[k % kPartRing];
+            if (named_barrier_or(kBar, 128, !ok) || e.t1 < 0) break;
+            const int ob = k % kOBufs;
+            const bool whole = e.slot < 0;
+            if (key < kRows) {
+                const int rr = e.rb * kRows + key, i = rr / group, hq = e.kvh * group + rr - i * group;
+                sh.out_at[key] = i < p.Sq ? e.b * p.o_sb + i * p.o_st + hq * p.o_sh : -1;
+                sh.out_hq[key] = hq;
+                sh.out_i[key] = i;
+            }
+            const float vs = kE4m3 && p.v_scale ? p.v_scale[e.kvh] : 1.f;
+            float* const slot_o = p.part + static_cast<long long>(whole ? 0 : e.slot) * kStates * (DV + 2);
             float* const slot_ml = slot_o + kStates * DV;
-            // log-sum-exp of a row (natural units) from its maximum (log2 units) and sum, and where it goes
+            // log-sum-exp of a row (natural units) from its maximum (log2 units) and sum
             auto store_lse = [&](int r, float m, float sum) {
-                if (kDiff || !p.lse || sh.out_at[qb][r] < 0) return;
-                p.lse[static_cast<long long>(sh.out_hq[qb][r]) * p.B * p.Sq + static_cast<long long>(part.b) * p.Sq + sh.row[qb][r].i] =
+                if (kDiff || !p.lse || sh.out_at[r] < 0) return;
+                p.lse[static_cast<long long>(sh.out_hq[r]) * p.B * p.Sq + static_cast<long long>(e.b) * p.Sq + sh.out_i[r]] =
                     sum > 0.f ? (m - Cfg::kBias + log2f(sum)) * 0.6931471805599453f : -INFINITY;
             };
-            if (gt < kStates) {
-                float sum[2], mx[2];
+            ok = mbar_wait(smem_addr(&sh.stat_full[ob]), (k / kOBufs) & 1, wctx, kSiteEpiState);
+            named_barrier_sync(kBar, 128);
+            if (key < kStates) {
+                float f[2], sum[2], mx[2];
 #pragma unroll
-                for (int v = 0; v < 2; ++v) {
-                    mx[v] = sh.m[v][gt];
-                    sum[v] = sh.red[v][0][gt] + sh.red[v][1][gt] + sh.red[v][2][gt] + sh.red[v][3][gt];
-                }
+                for (int v = 0; v < 2; ++v) { mx[v] = sh.stat_m[ob][v][key]; sum[v] = sh.stat_l[ob][v][key]; }
                 const float m = fmaxf(mx[0], mx[1]);
-                float f[2];
 #pragma unroll
                 for (int v = 0; v < 2; ++v) f[v] = mx[v] == -INFINITY ? 0.f : exp2_approx(mx[v] - m);
                 const float all = f[0] * sum[0] + f[1] * sum[1];
                 const float norm = !whole ? 1.f : (all > 0.f || all != all ? 1.f / all : 0.f);
-                sh.factor[0][gt] = f[0] * norm;
-                sh.factor[1][gt] = f[1] * norm;
+                sh.factor[0][key] = f[0] * norm;
+                sh.factor[1][key] = f[1] * norm;
                 if (whole) {
-                    store_lse(gt % kRows, m, all);
+                    store_lse(key % kRows, m, all);
                 } else {
-                    slot_ml[gt] = m;
-                    slot_ml[kStates + gt] = all;
+                    slot_ml[key] = m;
+                    slot_ml[kStates + key] = all;
                 }
             }
-            named_barrier_sync(3, 256);
-            // thread = output column; group w takes its half of the rows
-            constexpr int kHalf = kRows / 2;
-            const float vs = kE4m3 && p.v_scale ? p.v_scale[part.hr / p.row_blocks] : 1.f;
-            // the rows' results [map][row] to O: the difference and its norm, or the result itself
-            auto store_rows = [&](float (&y)[kMaps][kHalf]) {
+            ok = ok && mbar_wait(smem_addr(&sh.acc_full[ob]), (k / kOBufs) & 1, wctx, kSiteEpiOFull);
+            named_barrier_sync(kBar, 128);
+            tc_fence_after_sync();
+            float y[kStates];
+#pragma unroll
+            for (int r = 0; r < kStates; ++r) y[r] = 0.f;
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+                // (uniform) an accumulator that got nothing of this part
+                if (e.t1 - e.t0 < 2 && (e.tile0 & 1) != v) continue;
+#pragma unroll
+                for (int g = 0; g < kCols / 16; ++g) {
+                    const int col = g * 16, st = col / (kTerms * kRows) * kRows + col % kRows;
+                    uint32_t o[16];
+                    tmem_ld_x16(tmem + o_col(ob, v) + lane_sel + col, o);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) y[st + j] = fmaf(sh.factor[v][st + j], __uint_as_float(o[j]), y[st + j]);
+                }
+            }
+            tc_fence_before_sync();
+            named_barrier_sync(kBar, 128);
+            if (key == 0) mbar_arrive(smem_addr(&sh.acc_empty[ob]));
+            // the rows' results (map 0, then map 1) to O: the result itself, or the difference and its norm
+            auto store_rows = [&]() {
                 if constexpr (kDiff) {
 #pragma unroll
-                    for (int e = 0; e < kHalf; ++e)
-                        y[0][e] = vs * (y[0][e] - p.lambda[sh.out_hq[qb][w * kHalf + e]] * y[1][e]);
+                    for (int r = 0; r < kRows; ++r) y[r] = vs * (y[r] - p.lambda[sh.out_hq[r]] * y[kRows + r]);
                     if (p.weight) {
 #pragma unroll
-                        for (int e = 0; e < kHalf; ++e) {
-                            float q = y[0][e] * y[0][e];
+                        for (int r = 0; r < kRows; ++r) {
+                            float q = y[r] * y[r];
 #pragma unroll
                             for (int d = 16; d > 0; d >>= 1) q += __shfl_xor_sync(0xffffffffu, q, d);
-                            if (lane == 0) sh.sq[w][wq][e] = q;
+                            if (lane == 0) sh.sq[wq][r] = q;
                         }
-                        named_barrier_sync(1 + w, 128);
+                        named_barrier_sync(kBar, 128);
                         const float wt = p.weight[key];
 #pragma unroll
-                        for (int e = 0; e < kHalf; ++e) {
-                            const float q = sh.sq[w][0][e] + sh.sq[w][1][e] + sh.sq[w][2][e] + sh.sq[w][3][e];
-                            y[0][e] *= wt * rsqrtf(q * (1.f / DV) + p.eps);
+                        for (int r = 0; r < kRows; ++r) {
+                            const float q = (sh.sq[0][r] + sh.sq[1][r]) + (sh.sq[2][r] + sh.sq[3][r]);
+                            y[r] *= wt * rsqrtf(q * (1.f / DV) + p.eps);
                         }
-                        named_barrier_sync(1 + w, 128);
                     }
 #pragma unroll
-                    for (int e = 0; e < kHalf; ++e) y[0][e] *= p.out_scale;
+                    for (int r = 0; r < kRows; ++r) y[r] *= p.out_scale;
                 } else {
 #pragma unroll
-                    for (int e = 0; e < kHalf; ++e) y[0][e] *= vs;
+                    for (int r = 0; r < kRows; ++r) y[r] *= vs;
                 }
                 if (key < DV) {
 #pragma unroll
-                    for (int e = 0; e < kHalf; ++e) {
-                        const long long at = sh.out_at[qb][w * kHalf + e];
-                        if (at >= 0) p.O[at + key] = __float2bfloat16(y[0][e]);
+                    for (int r = 0; r < kRows; ++r) {
+                        const long long at = sh.out_at[r];
+                        if (at >= 0) p.O[at + key] = __float2bfloat16(y[r]);
                     }
                 }
             };
-            const bool had0 = part.t1 - part.t0 > 1 || ((n - 1) & 1) == 0, had1 = part.t1 - part.t0 > 1 || ((n - 1) & 1) == 1;
-            float y[kMaps][kHalf];
-#pragma unroll
-            for (int a = 0; a < kMaps; ++a) {
-#pragma unroll
-                for (int e = 0; e < kHalf; ++e) y[a][e] = 0.f;
-#pragma unroll
-                for (int v = 0; v < 2; ++v) {
-                    if (!(v == 0 ? had0 : had1)) continue;                // (uniform) nothing of this part in that accumulator
-#pragma unroll
-                    for (int term = 0; term < kTerms; ++term)
-#pragma unroll
-                        for (int e0 = 0; e0 < kHalf; e0 += 8) {
-                            uint32_t o[8];
-                            tmem_ld_x8(tmem + (2 + v) * kCols + lane_sel + (a * kTerms + term) * kRows + w * kHalf + e0, o);
-                            tc_wait_ld();
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                const float f = sh.factor[v][a * kRows + w * kHalf + e0 + e];
-                                // (a row that saw no key in this group's tiles: its accumulator is all zeros)
-                                y[a][e0 + e] = fmaf(f, __uint_as_float(o[e]), y[a][e0 + e]);
-                            }
-                        }
-                }
-            }
             if (whole) {
-                store_rows(y);
+                store_rows();
             } else {
                 if (key < DV) {
 #pragma unroll
-                    for (int a = 0; a < kMaps; ++a)
-#pragma unroll
-                        for (int e = 0; e < kHalf; ++e) slot_o[(a * kRows + w * kHalf + e) * DV + key] = y[a][e];
+                    for (int r = 0; r < kStates; ++r) slot_o[r * DV + key] = y[r];
                 }
                 __threadfence();
-                named_barrier_sync(3, 256);
-                const int pieces = paged_pieces(ua, ua + part.nt, share), c0 = paged_first_cta(ua, share);
-                if (gt == 0) {
-                    const unsigned int got = atomicAdd(p.arrivals + c0, 1u);
-                    sh.is_last = got == static_cast<unsigned int>(pieces - 1) ? 1u : 0u;
-                    if (sh.is_last) p.arrivals[c0] = 0u;
+                named_barrier_sync(kBar, 128);
+                if (key == 0) {
+                    const bool last = atomicAdd(p.arrivals + e.first_cta, 1u) == static_cast<unsigned int>(e.pieces - 1);
+                    sh.is_last = last ? 1u : 0u;
+                    if (last) p.arrivals[e.first_cta] = 0u;
                     __threadfence();
                 }
-                named_barrier_sync(3, 256);
+                named_barrier_sync(kBar, 128);
                 if (sh.is_last) {
+                    // this CTA finished last: all pieces, in the order of the CTAs
                     __threadfence();
-                    auto piece = [&](int c) { return p.part + static_cast<long long>(paged_slot(c0 + c, ua, share)) * kStates * (DV + 2); };
-                    if (gt < kStates) {
+                    // (the other pieces are the first parts of their CTAs)
+                    auto piece = [&](int c) {
+                        return p.part + (c == 0 ? e.first_slot : 2ll * (e.first_cta + c)) * kStates * (DV + 2);
+                    };
+                    if (key < kStates) {
                         float m = -INFINITY, sum = 0.f;
-                        for (int c = 0; c < pieces; ++c) m = fmaxf(m, __ldcg(piece(c) + kStates * DV + gt));
-                        for (int c = 0; c < pieces; ++c) {
-                            const float mc = __ldcg(piece(c) + kStates * DV + gt);
+                        for (int c = 0; c < e.pieces; ++c) m = fmaxf(m, __ldcg(piece(c) + kStates * DV + key));
+                        for (int c = 0; c < e.pieces; ++c) {
+                            const float mc = __ldcg(piece(c) + kStates * DV + key);
                             // (a piece without a finite score counts nothing, but a NaN of its sum goes through)
-                            sum += (mc == -INFINITY ? 0.f : exp2_approx(mc - m)) * __ldcg(piece(c) + kStates * DV + kStates + gt);
+                            sum += (mc == -INFINITY ? 0.f : exp2_approx(mc - m)) * __ldcg(piece(c) + kStates * DV + kStates + key);
                         }
-                        store_lse(gt % kRows, m, sum);
-                        sh.factor[0][gt] = m;
-                        sh.factor[1][gt] = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+                        store_lse(key % kRows, m, sum);
+                        sh.out_m[key] = m;
+                        sh.out_l[key] = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
                     }
-                    named_barrier_sync(3, 256);
 #pragma unroll
-                    for (int a = 0; a < kMaps; ++a)
+                    for (int r = 0; r < kStates; ++r) y[r] = 0.f;
+                    for (int c0 = 0; c0 < e.pieces; c0 += 8) {
+                        const int nc = min(8, e.pieces - c0);
+                        named_barrier_sync(kBar, 128);
+                        for (int j = key; j < nc * kStates; j += 128) {
+                            const int c = j / kStates, r = j % kStates;
+                            const float mc = __ldcg(piece(c0 + c) + kStates * DV + r);
+                            sh.weight[c][r] = mc == -INFINITY ? 0.f : exp2_approx(mc - sh.out_m[r]) * sh.out_l[r];
+                        }
+                        named_barrier_sync(kBar, 128);
+                        if (key < DV) {
+#pragma unroll 2
+                            for (int c = 0; c < nc; ++c) {
+                                const float* po = piece(c0 + c) + key;
 #pragma unroll
-                        for (int e = 0; e < kHalf; ++e) y[a][e] = 0.f;
-                    if (key < DV) {
-                        for (int c = 0; c < pieces; ++c) {
-                            const float* po = piece(c);
-#pragma unroll
-                            for (int a = 0; a < kMaps; ++a)
-#pragma unroll
-                                for (int e = 0; e < kHalf; ++e) {
-                                    const int st = a * kRows + w * kHalf + e;
-                                    const float mc = __ldcg(po + kStates * DV + st);
-                                    const float f = mc == -INFINITY ? 0.f : exp2_approx(mc - sh.factor[0][st]) * sh.factor[1][st];
-                                    y[a][e] = fmaf(f, __ldcg(po + st * DV + key), y[a][e]);
-                                }
+                                for (int r = 0; r < kStates; ++r) y[r] = fmaf(sh.weight[c][r], __ldcg(po + r * DV), y[r]);
+                            }
                         }
                     }
-                    store_rows(y);
+                    store_rows();
                 }
             }
-            // both groups have read the accumulators, factors and rows: the next part may begin
-            if (key < kStates) sh.m[w][key] = -INFINITY;
-#pragma unroll
-            for (int r = 0; r < kStates; ++r) l[r] = 0.f;
-            tc_fence_before_sync();
-            named_barrier_sync(3, 256);
-            tc_fence_after_sync();
-            if (key == 0) mbar_arrive(smem_addr(&sh.q_empty[qb]));
-            ++seg;
-        } while (part.next(p));
+            named_barrier_sync(kBar, 128);
+            if (key == 0) mbar_arrive(smem_addr(&sh.part_empty[k % kPartRing]));
+        }
     }
 
     // ---------------------------------------------------------------- teardown (all warps)
