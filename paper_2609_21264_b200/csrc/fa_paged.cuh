@@ -22,18 +22,21 @@
 //
 // e4m3 caches: K and V enter the 8-bit MMA as they are; the bf16 queries and the fp32 probabilities as sums of three e5m2 terms,
 // each on columns of its own (N = 3 rows): x -> fp16, top byte, remainder, top byte, remainder, top byte, 9 significant bits.
-// Nothing is dequantised and both sides keep at least bf16's precision.  The probabilities are scaled by 2^13 so that weights of
-// 2^-20 of the largest still have 9 bits.
+// Nothing is dequantised and both sides keep at least bf16's precision.  The probabilities are scaled by 2^11 so that weights of
+// 2^-19 of the largest still have 9 bits.
 //
 // Differential attention: two maps are two groups of columns.  Map a's scores are the k-steps of its half of K, its
 // probabilities meet the same V tile, and the epilogue subtracts and normalises: K and V are read once for both.
 //
-// Roles (512 threads): warps 0 / 2 TMA loads of K / V (a lane per page box), warp 1 MMA issue, warp 3 the list of parts and the query
-// rows, warps 4-7 and 8-11 softmax groups 0 and 1 (thread = key of the tile = lane of S^T), warps 12-15 results (thread = output
-// column = lane of O^T).
+// Roles (512 threads): warps 0 / 2 TMA loads of K / V (a lane per page box), warps 1 / 3 issue of the score / value products (one thread
+// each: a tile costs an issuing thread 600 cycles of waits, descriptors and commits, as much as a tile of head size 64 has in
+// all), warps 4-7 and 8-11 softmax groups 0 and 1 (thread = key of the tile = lane of S^T), warps 12-15 the list of parts, the
+// query rows, and the results (thread = output column = lane of O^T).
 #pragma once
 
 #include <math.h>
+
+#include <type_traits>
 
 #include "fa_paged_common.cuh"
 
@@ -53,11 +56,6 @@ FA_DEVI bool named_barrier_or(uint32_t id, uint32_t nthreads, bool x) {
         "}\n"
         : "=r"(r) : "r"(x ? 1u : 0u), "r"(id), "r"(nthreads) : "memory");
     return r != 0;
-}
-FA_DEVI float warp_max(float x) {
-    float y;
-    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
-    return y;
 }
 FA_DEVI void st_shared_u16(uint32_t addr, uint32_t x) {
     asm volatile("st.shared.u16 [%0], %1;" ::"r"(addr), "h"(static_cast<uint16_t>(x)) : "memory");
@@ -129,6 +127,50 @@ struct PagedPart {
 
 // ------------------------------------------------------------------ configuration
 
+// A part of the list as the roles of a CTA see it: tiles [t0, t1) of one (sequence, K/V head, row block).
+struct PagedEntry {
+    int b, kvh, rb, len, t0, t1;  // t1 < 0: the end of the CTA's share
+    int tile0;                    // index of the part's first tile in the CTA's share
+    int slot;                     // of the partial result, -1: the part is whole
+    int pieces, first_cta;        // of the whole (sequence, head, block), and the slot of its first piece
+    int first_slot;
+};
+constexpr int kPartRing = 8, kPartsAhead = 6;
+
+// Registers per thread after the per-role reallocation (512 threads start with 128 each): 128 x 80 + 256 x 152 + 128 x 128 = 65536.
+constexpr int kPagedRegsOther = 80, kPagedRegsSoftmax = 152;
+
+template <int kRows, int kMaps>
+struct PagedShared {
+    uint64_t k_full[6], k_empty[6], v_full[6], v_empty[6];
+    uint64_t q_full[2], q_empty[2];
+    uint64_t s_full[2][2], s_empty[2][2], p_full[2][2], pv_done[2][2];      // [group][buffer]
+    uint64_t acc_full[2], acc_empty[2];                      // [accumulator buffer]
+    uint64_t part_full[kPartRing], part_empty[kPartRing], stat_full[kPartRing];
+    PagedEntry part[kPartRing];
+    uint32_t tmem_base;
+    uint32_t abort_flag;
+    uint32_t is_last;
+    int start_b;
+    long long start_base;
+    long long warp_sums[16];
+    alignas(16) float c[2][kRows];                       // per query buffer: factor of a score (log2 units)
+    int i[2][kRows];                                     // place among the new tokens
+    // per group: bias - reference maximum, +inf where no key has been seen; and the same with 0 there
+    alignas(16) float neg_m[2][kMaps * kRows];
+    alignas(16) float neg_p[2][kMaps * kRows];
+    alignas(16) float rescale[2][kMaps * kRows];
+    float red[2][4][kMaps * kRows], red_l[2][4][kMaps * kRows];
+    float stat_m[kPartRing][2][kMaps * kRows], stat_l[kPartRing][2][kMaps * kRows];      // [part][group]
+    // of the result warps
+    float factor[2][kMaps * kRows];
+    float out_m[kMaps * kRows], out_l[kMaps * kRows];
+    float weight[8][kMaps * kRows];
+    float sq[4][kRows];
+    long long out_at[kRows];                             // offset of the row in O (-1: a padding row)
+    int out_hq[kRows], out_i[kRows];
+};
+
 template <int DQK, int DV, bool kE4m3, bool kDiff, int kRows>
 struct PagedCfg {
     static constexpr int kMaps = kDiff ? 2 : 1;
@@ -150,9 +192,10 @@ struct PagedCfg {
     // bf16 values of 64: the upper 64 lanes of O^T multiply a block of zeros
     static constexpr bool kZeroBlock = !kE4m3 && DV == 64;
     static constexpr int kZeroBytes = kZeroBlock ? 2048 : 0;
-    static constexpr int kBudget = 227 * 1024 - (kStates <= 16 ? 4 : 8) * 1024;      // the rest is for PagedShared
-    // two probability buffers per group, one where two would not leave room for two stages
-    static constexpr int kPBufs = (kBudget - 2 * kQBytes - 4 * kPBytes - kZeroBytes) / (kKBytes + kVBytes) >= 2 ? 2 : 1;
+    static constexpr int kBudget = 227 * 1024 - static_cast<int>(sizeof(PagedShared<kRows, kMaps>));
+    // two probability buffers per group, one where that makes room for a second or third stage
+    static constexpr int stages_with(int p_bufs) { return (kBudget - 2 * kQBytes - 2 * p_bufs * kPBytes - kZeroBytes) / (kKBytes + kVBytes); }
+    static constexpr int kPBufs = stages_with(2) >= 3 || stages_with(2) == stages_with(1) ? 2 : 1;
     static constexpr int kFixedBytes = 2 * kQBytes + 2 * kPBufs * kPBytes + kZeroBytes;
     static constexpr int kFit = (kBudget - kFixedBytes) / (kKBytes + kVBytes);
     static constexpr int kStages = kFit > 6 ? 6 : kFit;
@@ -167,50 +210,8 @@ struct PagedCfg {
     static constexpr int kKSteps = DQK * kElem / 32;            // k-steps of 32 bytes
     static constexpr int kPSteps = 128 * kElem / 32;
     // exponents above the reference that a score may reach before the reference moves, and the scaling of P
-    static constexpr float kTauLog2 = kE4m3 ? 2.f : 8.f;
-    static constexpr float kBias = kE4m3 ? 13.f : 0.f;
-};
-
-// A part of the list as the roles of a CTA see it: tiles [t0, t1) of one (sequence, K/V head, row block).
-struct PagedEntry {
-    int b, kvh, rb, len, t0, t1;  // t1 < 0: the end of the CTA's share
-    int tile0;                    // index of the part's first tile in the CTA's share
-    int slot;                     // of the partial result, -1: the part is whole
-    int pieces, first_cta;        // of the whole (sequence, head, block), and the slot of its first piece
-    int first_slot;
-};
-constexpr int kPartRing = 8, kPartsAhead = 4;
-
-// Registers per thread after the per-role reallocation (512 threads start with 128 each): 128 x 80 + 256 x 152 + 128 x 128 = 65536.
-constexpr int kPagedRegsOther = 80, kPagedRegsSoftmax = 152;
-
-template <int kRows, int kMaps>
-struct PagedShared {
-    uint64_t k_full[6], k_empty[6], v_full[6], v_empty[6];
-    uint64_t q_full[2], q_empty[2];
-    uint64_t s_full[2][2], p_full[2][2], pv_done[2][2];      // [group][buffer]
-    uint64_t stat_full[2], acc_full[2], acc_empty[2];        // [accumulator buffer]
-    uint64_t part_full[kPartRing], part_empty[kPartRing];
-    PagedEntry part[kPartRing];
-    uint32_t tmem_base;
-    uint32_t abort_flag;
-    uint32_t is_last;
-    int start_b;
-    long long start_base;
-    long long warp_sums[16];
-    alignas(16) float c[2][kRows];                       // per query buffer: factor of a score (log2 units)
-    int i[2][kRows];                                     // place among the new tokens
-    alignas(16) float neg_m[2][kMaps * kRows];           // per group: bias - reference maximum; +inf: no key seen yet
-    alignas(16) float rescale[2][kMaps * kRows];
-    float red[2][4][kMaps * kRows];
-    float stat_m[2][2][kMaps * kRows], stat_l[2][2][kMaps * kRows];      // [buffer][group]
-    // of the result warps
-    float factor[2][kMaps * kRows];
-    float out_m[kMaps * kRows], out_l[kMaps * kRows];
-    float weight[8][kMaps * kRows];
-    float sq[4][kRows];
-    long long out_at[kRows];                             // offset of the row in O (-1: a padding row)
-    int out_hq[kRows], out_i[kRows];
+    static constexpr float kTauLog2 = kE4m3 ? 4.5f : 8.f;      // 2^15.5 is below e5m2's largest number, 57344
+    static constexpr float kBias = kE4m3 ? 11.f : 0.f;
 };
 
 template <int DQK, int DV, bool kE4m3, bool kDiff, int kRows>
@@ -222,6 +223,16 @@ constexpr int paged_smem_bytes() {
 constexpr long long paged_slot_bytes(int dv, int states) { return states * (dv + 2) * 4ll; }
 
 // ------------------------------------------------------------------ kernel
+
+// Low word of a shared-memory matrix descriptor with 128-byte swizzle; the high word is the same for all (8-row groups 1024 bytes
+// apart, version 1).
+FA_DEVI uint32_t desc_lo(uint32_t saddr, uint32_t lbo_bytes) { return ((saddr & 0x3ffffu) >> 4) | ((lbo_bytes >> 4) << 16); }
+template <bool kE4m3>
+FA_DEVI void paged_mma(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+    constexpr uint64_t kHi = static_cast<uint64_t>((1024u >> 4) | (1u << 14) | (2u << 29)) << 32;
+    if constexpr (kE4m3) ptx::mma_ss_f8(d, kHi | a_lo, kHi | b_lo, idesc, accumulate);
+    else ptx::mma_ss(d, kHi | a_lo, kHi | b_lo, idesc, accumulate);
+}
 
 template <int DQK, int DV, bool kE4m3, bool kDiff, int kRows>
 __global__ void __launch_bounds__(512, 1)
@@ -260,20 +271,21 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             mbar_init(smem_addr(&sh.v_empty[s]), 1);
         }
         for (int w = 0; w < 2; ++w) {
-            mbar_init(smem_addr(&sh.q_full[w]), 1);
+            mbar_init(smem_addr(&sh.q_full[w]), 4);       // the four warps that stage the rows
             mbar_init(smem_addr(&sh.q_empty[w]), 3);      // the last score MMA and the two softmax groups
             for (int i = 0; i < 2; ++i) {
                 mbar_init(smem_addr(&sh.s_full[w][i]), 1);
+                mbar_init(smem_addr(&sh.s_empty[w][i]), 4);     // four warps
                 mbar_init(smem_addr(&sh.p_full[w][i]), 4);      // four warps
                 mbar_init(smem_addr(&sh.pv_done[w][i]), 1);
             }
-            mbar_init(smem_addr(&sh.stat_full[w]), 8);          // the softmax warps
             mbar_init(smem_addr(&sh.acc_full[w]), 1);
             mbar_init(smem_addr(&sh.acc_empty[w]), 1);
         }
         for (int i = 0; i < kPartRing; ++i) {
             mbar_init(smem_addr(&sh.part_full[i]), 1);
             mbar_init(smem_addr(&sh.part_empty[i]), 1);
+            mbar_init(smem_addr(&sh.stat_full[i]), 8);          // the softmax warps
         }
         fence_mbar_init();
         prefetch_tensormap(&tm_k);
@@ -287,7 +299,6 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         if (tid < 128) st_shared_v4(sZero + tid * 16, 0, 0, 0, 0);
         fence_proxy_async_smem();
     }
-    if (tid < 2 * kStates) sh.neg_m[tid / kStates][tid % kStates] = INFINITY;
     grid_dependency_wait();
 
     // ---- the shares: every thread sums up the units of consecutive sequences, a scan over the CTA finds the total
@@ -342,141 +353,372 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
     if (warp == 0 || warp == 2) {
         // ============================================================ TMA loads of K (warp 0) or V (warp 2)
         setmaxnreg_dec<kPagedRegsOther>();
-        const bool is_v = warp == 2;
-        const CUtensorMap* tm = is_v ? &tm_v : &tm_k;
-        uint64_t* const full = is_v ? sh.v_full : sh.k_full;
-        uint64_t* const empty = is_v ? sh.v_empty : sh.k_empty;
-        const uint32_t dst0 = is_v ? sV : sK, stage_bytes = is_v ? Cfg::kVBytes : Cfg::kKBytes;
-        const int chunks = is_v ? Cfg::kVChunks : Cfg::kKChunks;
-        const int box = p.box_rows, boxes = kTileN / box, tiles_ahead = 32 / boxes;
-        int n = 0;
-        bool ok = true;
-        for (int k = 0; ok; ++k) {
-            ok = __all_sync(0xffffffffu, wait_part(k));
-            if (!ok) break;
-            const PagedEntry e = sh.part[k % kPartRing];
-            if (e.t1 < 0) break;
-            const long long row = e.b * p.table_stride;
-            int pages = -1, slots = 0;        // of tile `first` + lane / boxes, box lane % boxes
-            int first = e.t0;
-            for (int t = e.t0; t < e.t1; ++t, ++n) {
-                if (t == e.t0 || t - first == tiles_ahead) {
-                    first = t;
-                    const int tile = t + lane / boxes, key = tile * kTileN + (lane % boxes) * box;
-                    pages = -1;
-                    if (tile < e.t1 && key < e.len) {
-                        const int at = key / p.page_size;
-                        slots = key - at * p.page_size;
-                        pages = p.block_table[row + at];
-                        if (pages < 0 || pages >= p.num_pages) {
-                            report_bad_input(p.status, kSiteBadPage);
-                            pages = p.num_pages;       // behind the pool: reads as zeros
+        auto load_tiles = [&](auto v_tag) {
+            constexpr bool is_v = decltype(v_tag)::value;
+            constexpr int kChunks = is_v ? Cfg::kVChunks : Cfg::kKChunks, kStageBytes = is_v ? Cfg::kVBytes : Cfg::kKBytes;
+            const CUtensorMap* tm = is_v ? &tm_v : &tm_k;
+            uint64_t* const full = is_v ? sh.v_full : sh.k_full;
+            uint64_t* const empty = is_v ? sh.v_empty : sh.k_empty;
+            const uint32_t dst0 = is_v ? sV : sK;
+            const int box = p.box_rows, shift = __ffs(kTileN / box) - 1, boxes = 1 << shift, tiles_ahead = 32 >> shift;
+            int n = 0, s = 0;
+            uint32_t parity = 1;
+            bool ok = true;
+            for (int k = 0; ok; ++k) {
+                ok = __all_sync(0xffffffffu, wait_part(k));
+                if (!ok) break;
+                const PagedEntry e = sh.part[k % kPartRing];
+                if (e.t1 < 0) break;
+                const int* const table = p.block_table + e.b * p.table_stride;
+                int pages = 0, slots = 0;         // of tile `first` + lane / boxes, box lane % boxes
+                int first = e.t0;
+                for (int t = e.t0; t < e.t1; ++t, ++n) {
+                    if (t == e.t0 || t - first == tiles_ahead) {
+                        first = t;
+                        const int tile = t + (lane >> shift), key = tile * kTileN + (lane & (boxes - 1)) * box;
+                        if (tile < e.t1 && key < e.len) {
+                            const int at = key / p.page_size;
+                            slots = key - at * p.page_size;
+                            pages = table[at];
+                            if (pages < 0 || pages >= p.num_pages) {
+                                report_bad_input(p.status, kSiteBadPage);
+                                pages = p.num_pages;       // behind the pool: reads as zeros
+                            }
                         }
                     }
+                    const int from = ((t - first) << shift) + lane;
+                    const int page = __shfl_sync(0xffffffffu, pages, from & 31), slot = __shfl_sync(0xffffffffu, slots, from & 31);
+                    ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&empty[s]), parity, wctx, kSiteLoadKvEmpty));
+                    if (!ok) break;
+                    const uint32_t bar = smem_addr(&full[s]);
+                    const int n_box = min(boxes, (max(0, e.len - t * kTileN) + box - 1) / box);
+                    if (!(is_v && p.debug_drop_v_load && n == 0)) {
+                        if (lane == 0) mbar_arrive_expect_tx(bar, n_box * box * 128 * kChunks);
+                        __syncwarp();
+                        if (lane < n_box) {
+#pragma unroll
+                            for (int c = 0; c < kChunks; ++c)
+                                tma_load_4d(dst0 + s * kStageBytes + c * kChunkBytes + lane * box * 128, tm, bar, c * Cfg::kChunk, slot, e.kvh, page);
+                        }
+                        __syncwarp();
+                    }
+                    if (++s == NS) { s = 0; parity ^= 1u; }
                 }
-                const int from = (t - first) * boxes + lane;
-                const int page = __shfl_sync(0xffffffffu, pages, from & 31), slot = __shfl_sync(0xffffffffu, slots, from & 31);
-                const int s = n % NS;
-                ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&empty[s]), ((n / NS) & 1) ^ 1, wctx, kSiteLoadKvEmpty));
-                if (!ok) break;
-                if (is_v && p.debug_drop_v_load && n == 0) continue;
-                const uint32_t bar = smem_addr(&full[s]);
-                const int n_box = min(boxes, (max(0, e.len - t * kTileN) + box - 1) / box);
-                if (lane == 0) mbar_arrive_expect_tx(bar, n_box * box * 128 * chunks);
-                __syncwarp();
-                if (lane < n_box)
-                    for (int c = 0; c < chunks; ++c)
-                        tma_load_4d(dst0 + s * stage_bytes + c * kChunkBytes + lane * box * 128, tm, bar, c * Cfg::kChunk, slot, e.kvh, page);
-                __syncwarp();
             }
-        }
+        };
+        if (warp == 0) load_tiles(std::false_type{});
+        else load_tiles(std::true_type{});
     } else if (warp == 1) {
-        // ============================================================ MMA issue, one thread
+        // ============================================================ score products, one thread
         setmaxnreg_dec<kPagedRegsOther>();
         if (elect_one()) {
             constexpr uint32_t kIdescQK = kE4m3 ? (make_idesc_e4m3_f32(128, Cfg::kQRows, false, false) | (1u << 10))      // B: e5m2
                                                 : make_idesc_bf16_f32(128, Cfg::kQRows, false, false);
-            constexpr uint32_t kIdescPV = kE4m3 ? (make_idesc_e4m3_f32(128, kCols, true, false) | (1u << 10))
-                                                : make_idesc_bf16_f32(128, kCols, true, false);
-            auto mma = [](uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
-                if constexpr (kE4m3) mma_ss_f8(d, a, b, idesc, acc);
-                else mma_ss(d, a, b, idesc, acc);
-            };
-            bool ok = true, more = true;
-            int nq = 0, qk = -1, q_left = 0;           // score products issued; their part and its tiles to come
-            auto scores = [&]() {
-                if (q_left == 0) {
-                    ++qk;
-                    if (!(ok = wait_part(qk))) return;
-                    const PagedEntry& e = sh.part[qk % kPartRing];
-                    if (e.t1 < 0) { more = false; return; }
-                    q_left = e.t1 - e.t0;
-                    if (!(ok = mbar_wait(smem_addr(&sh.q_full[qk & 1]), (qk >> 1) & 1, wctx, kSiteMmaQFull))) return;
-                }
-                const int w = nq & 1, i = (nq >> 1) % kBufs, s = nq % NS;
-                if (!(ok = mbar_wait(smem_addr(&sh.k_full[s]), (nq / NS) & 1, wctx, kSiteMmaKvFull))) return;
-                tc_fence_after_sync();
-                const uint32_t a0 = sK + s * Cfg::kKBytes, b0 = sQ + (qk & 1) * Cfg::kQBytes;
-                constexpr int kPerMap = Cfg::kKSteps / kMaps;
+            constexpr int kPerMap = Cfg::kKSteps / kMaps;
+            const uint32_t k_lo0 = desc_lo(sK, 16), q_lo0 = desc_lo(sQ, 16);
+            int n = 0, s = 0;
+            uint32_t k_parity = 0;
+            bool ok = true;
+            for (int k = 0; ok; ++k) {
+                if (!wait_part(k)) break;
+                const int tiles = sh.part[k % kPartRing].t1 - sh.part[k % kPartRing].t0;
+                if (sh.part[k % kPartRing].t1 < 0) break;
+                if (!mbar_wait(smem_addr(&sh.q_full[k & 1]), (k >> 1) & 1, wctx, kSiteMmaQFull)) break;
+                const uint32_t q_lo = q_lo0 + (k & 1) * (Cfg::kQBytes >> 4);
+                for (int t = 0; t < tiles; ++t, ++n) {
+                    const int w = n & 1, i = (n >> 1) % kBufs;
+                    ok = mbar_wait(smem_addr(&sh.s_empty[w][i]), (((n >> 1) / kBufs) & 1) ^ 1, wctx, kSiteMmaSFree) &&
+                         mbar_wait(smem_addr(&sh.k_full[s]), k_parity, wctx, kSiteMmaKvFull);
+                    if (!ok) break;
+                    tc_fence_after_sync();
+                    const uint32_t k_lo = k_lo0 + s * (Cfg::kKBytes >> 4), d = tmem + s_col(w, i);
 #pragma unroll
-                for (int m = 0; m < kMaps; ++m)
+                    for (int m = 0; m < kMaps; ++m)
 #pragma unroll
-                    for (int j = 0; j < kPerMap; ++j) {
-                        const int ks = m * kPerMap + j;
-                        mma(tmem + s_col(w, i) + m * Cfg::kQRows,
-                            make_smem_desc_sw128(a0 + (ks / 4) * kChunkBytes + (ks % 4) * 32, 16, 1024),
-                            make_smem_desc_sw128(b0 + (ks / 4) * Cfg::kQChunkBytes + (ks % 4) * 32, 16, 1024), kIdescQK, j > 0 ? 1u : 0u);
-                    }
-                tc_commit(smem_addr(&sh.s_full[w][i]));
-                tc_commit(smem_addr(&sh.k_empty[s]));
-                if (--q_left == 0) tc_commit(smem_addr(&sh.q_empty[qk & 1]));
-                ++nq;
-            };
-#pragma unroll 1
-            for (int i = 0; i < Cfg::kSBufs && ok && more; ++i) scores();
-            int pk = -1, p_left = 0, p_done = 0;       // part of the second products
-#pragma unroll 1
-            for (int n = 0; ok && n < nq; ++n) {
-                if (p_left == 0) {
-                    ++pk;
-                    const PagedEntry& e = sh.part[pk % kPartRing];       // (published: its scores have been issued)
-                    p_left = e.t1 - e.t0;
-                    p_done = 0;
-                    if (!(ok = mbar_wait(smem_addr(&sh.acc_empty[pk % kOBufs]), ((pk / kOBufs) & 1) ^ 1, wctx, kSiteMmaOReady))) break;
+                        for (int j = 0; j < kPerMap; ++j) {
+                            const int ks = m * kPerMap + j;
+                            paged_mma<kE4m3>(d + m * Cfg::kQRows, k_lo + (((ks / 4) * kChunkBytes + (ks % 4) * 32) >> 4),
+                                             q_lo + (((ks / 4) * Cfg::kQChunkBytes + (ks % 4) * 32) >> 4), kIdescQK, j > 0 ? 1u : 0u);
+                        }
+                    tc_commit(smem_addr(&sh.s_full[w][i]));
+                    tc_commit(smem_addr(&sh.k_empty[s]));
+                    if (++s == NS) { s = 0; k_parity ^= 1u; }
                 }
-                const int w = n & 1, i = (n >> 1) % kPBufs, s = n % NS;
-                ok = mbar_wait(smem_addr(&sh.v_full[s]), (n / NS) & 1, wctx, kSiteMmaKvFull) &&
-                     mbar_wait(smem_addr(&sh.p_full[w][i]), ((n >> 1) / kPBufs) & 1, wctx, kSiteMmaPFull);
-                if (!ok) break;
-                tc_fence_after_sync();
-                const uint32_t a0 = sV + s * Cfg::kVBytes, b0 = sP + (w * kPBufs + i) * Cfg::kPBytes;
-                const uint32_t acc = p_done >= 2 ? 1u : 0u;              // the group's first tile of the part overwrites
-#pragma unroll
-                for (int ks = 0; ks < Cfg::kPSteps; ++ks) {
-                    constexpr int kStepBytes = (32 / Cfg::kElem) * 128;        // keys of a k-step x 128 bytes
-                    const uint32_t a = a0 + ks * kStepBytes;
-                    const uint32_t lbo = Cfg::kZeroBlock ? sZero - a : static_cast<uint32_t>(kChunkBytes);
-                    mma(tmem + o_col(pk % kOBufs, w), make_smem_desc_sw128(a, lbo, 1024),
-                        make_smem_desc_sw128(b0 + (ks / 4) * Cfg::kPChunkBytes + (ks % 4) * 32, 16, 1024), kIdescPV, ks > 0 ? 1u : acc);
-                }
-                tc_commit(smem_addr(&sh.v_empty[s]));
-                tc_commit(smem_addr(&sh.pv_done[w][i]));
-                ++p_done;
-                if (--p_left == 0) tc_commit(smem_addr(&sh.acc_full[pk % kOBufs]));
-                if (more) scores();
+                if (ok) tc_commit(smem_addr(&sh.q_empty[k & 1]));
             }
         }
     } else if (warp == 3) {
-        // ============================================================ the list of parts, kPartsAhead ahead of their query rows
+        // ============================================================ value products, one thread
         setmaxnreg_dec<kPagedRegsOther>();
+        if (elect_one()) {
+            constexpr uint32_t kIdescPV = kE4m3 ? (make_idesc_e4m3_f32(128, kCols, true, false) | (1u << 10))
+                                                : make_idesc_bf16_f32(128, kCols, true, false);
+            constexpr int kStepKeys = 32 / Cfg::kElem, kStep16 = (kStepKeys * 128) >> 4;
+            const uint32_t v_lo0 = desc_lo(sV, Cfg::kZeroBlock ? 0 : kChunkBytes), p_lo0 = desc_lo(sP, 16);
+            int n = 0, s = 0;
+            uint32_t v_parity = 0;
+            bool ok = true;
+            for (int k = 0; ok; ++k) {
+                if (!wait_part(k)) break;
+                const PagedEntry e = sh.part[k % kPartRing];
+                if (e.t1 < 0) break;
+                if (!mbar_wait(smem_addr(&sh.acc_empty[k % kOBufs]), ((k / kOBufs) & 1) ^ 1, wctx, kSiteMmaOReady)) break;
+                for (int t = e.t0; t < e.t1; ++t, ++n) {
+                    const int w = n & 1, i = (n >> 1) % kPBufs;
+                    ok = mbar_wait(smem_addr(&sh.v_full[s]), v_parity, wctx, kSiteMmaKvFull) &&
+                         mbar_wait(smem_addr(&sh.p_full[w][i]), ((n >> 1) / kPBufs) & 1, wctx, kSiteMmaPFull);
+                    if (!ok) break;
+                    tc_fence_after_sync();
+                    const uint32_t v_lo = v_lo0 + s * (Cfg::kVBytes >> 4), p_lo = p_lo0 + (w * kPBufs + i) * (Cfg::kPBytes >> 4);
+                    const uint32_t d = tmem + o_col(k % kOBufs, w);
+                    const uint32_t acc = t >= e.t0 + 2 ? 1u : 0u;        // the group's first tile of the part overwrites
+                    // the sequence's last tile: only the k-steps that hold keys (one at least)
+                    const int keys = t == e.t1 - 1 ? min(kTileN, e.len - t * kTileN) : kTileN;
+#pragma unroll
+                    for (int ks = 0; ks < Cfg::kPSteps; ++ks) {
+                        if (ks > 0 && ks * kStepKeys >= keys) break;
+                        // (values of 64: the second 64 rows of V^T are read from a block of zeros, wherever this k-step is)
+                        const uint32_t lo = v_lo + ks * kStep16;
+                        const uint32_t lbo = Cfg::kZeroBlock ? (((sZero >> 4) - (lo & 0x3fffu)) << 16) : 0u;
+                        paged_mma<kE4m3>(d, lo + lbo, p_lo + (((ks / 4) * Cfg::kPChunkBytes + (ks % 4) * 32) >> 4), kIdescPV, ks > 0 ? 1u : acc);
+                    }
+                    tc_commit(smem_addr(&sh.v_empty[s]));
+                    tc_commit(smem_addr(&sh.pv_done[w][i]));
+                    if (++s == NS) { s = 0; v_parity ^= 1u; }
+                }
+                if (ok) tc_commit(smem_addr(&sh.acc_full[k % kOBufs]));
+            }
+        }
+    } else if (warp < 12) {
+        // ============================================================ softmax groups
+        // The four warps of a group stay together through their barriers: after a wait that ran out they go on to the end of
+        // the part without waiting (results are invalid then, every access stays in bounds) and leave together.
+        setmaxnreg_inc<kPagedRegsSoftmax>();
+        const int w = (warp >> 2) - 1, key = tid & 127, wq = warp & 3;
+        const uint32_t lane_sel = static_cast<uint32_t>(wq * 32) << 16;
+        const uint32_t p_byte = kE4m3 ? key : (key & 63) * 2;            // of this key in a row of P
+        int mine_n = 0;                                                  // tiles this group has done
+        bool ok = true;
+        for (int k = 0;; ++k) {
+            const int qb = k & 1;
+            ok = ok && wait_part(k);
+            const PagedEntry& entry = sh.part[k % kPartRing];
+            const int t0 = entry.t0, t1 = entry.t1, len = entry.len, tile0 = entry.tile0;
+            if (named_barrier_or(1 + w, 128, !ok) || t1 < 0) break;
+            // (also by a group without a tile here: its arrival at q_empty must not run ahead into the buffer's next turn)
+            ok = mbar_wait(smem_addr(&sh.q_full[qb]), (k >> 1) & 1, wctx, kSiteMmaQFull);
+            const int skip = (tile0 & 1) == w ? 0 : 1;                   // this group's first tile of the part: t0 + skip
+            if (t0 + skip < t1) {
+                float l[kStates];
+#pragma unroll
+                for (int r = 0; r < kStates; ++r) l[r] = 0.f;
+                const int first_masked = len - p.Sq + 1;                 // the first key that some row does not see
+                const uint32_t tO = tmem + o_col(k % kOBufs, w) + lane_sel;
+#pragma unroll 1
+                for (int t = t0 + skip; t < t1; t += 2, ++mine_n) {
+                    const int sb = mine_n % kBufs, pb = mine_n % kPBufs;
+                    const bool first = t == t0 + skip;
+                    const uint32_t tS = tmem + s_col(w, sb) + lane_sel;
+                    const uint32_t sPw = sP + (w * kPBufs + pb) * Cfg::kPBytes + (kE4m3 ? 0 : (key >> 6) * Cfg::kPChunkBytes);
+                    ok = ok && mbar_wait(smem_addr(&sh.s_full[w][sb]), (mine_n / kBufs) & 1, wctx, kSiteSoftmaxSFull);
+                    __syncwarp();
+                    tc_fence_after_sync();
+                    const int key_at = t * kTileN + key;
+                    float x[kStates];                                    // scores in log2 units
+#pragma unroll
+                    for (int g = 0; g < kStates / 16; ++g) {
+                        // column of (map, term, row): (map * kTerms + term) * kRows + row
+                        const int map = g * 16 / kRows, r0 = g * 16 % kRows;
+                        uint32_t s0[16];
+                        tmem_ld_x16(tS + map * kTerms * kRows + r0, s0);
+                        if constexpr (kE4m3) {
+                            uint32_t s1[16], s2[16];
+                            tmem_ld_x16(tS + (map * kTerms + 1) * kRows + r0, s1);
+                            tmem_ld_x16(tS + (map * kTerms + 2) * kRows + r0, s2);
+                            tc_wait_ld();
+#pragma unroll
+                            for (int j = 0; j < 16; j += 4) {
+                                const float4 c = *reinterpret_cast<const float4*>(&sh.c[qb][r0 + j]);
+                                const float cc[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+                                for (int q = 0; q < 4; ++q)
+                                    x[g * 16 + j + q] = (__uint_as_float(s0[j + q]) +
+                                                         (__uint_as_float(s1[j + q]) + __uint_as_float(s2[j + q]))) * cc[q];
+                            }
+                        } else {
+                            tc_wait_ld();
+#pragma unroll
+                            for (int j = 0; j < 16; j += 2) {
+                                const float2 y = __fmul2_rn(make_float2(__uint_as_float(s0[j]), __uint_as_float(s0[j + 1])),
+                                                            make_float2(p.scale_log2, p.scale_log2));
+                                x[g * 16 + j] = y.x;
+                                x[g * 16 + j + 1] = y.y;
+                            }
+                        }
+                    }
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_addr(&sh.s_empty[w][sb]));
+                    if (t * kTileN + kTileN > first_masked) {
+#pragma unroll
+                        for (int r = 0; r < kStates; ++r)
+                            if (key_at >= first_masked + sh.i[qb][r % kRows]) x[r] = -INFINITY;
+                    }
+                    bool move = first;
+                    if (!first) {
+                        float top = -INFINITY;
+#pragma unroll
+                        for (int r = 0; r < kStates; r += 4) {
+                            const float4 nm = *reinterpret_cast<const float4*>(&sh.neg_m[w][r]);
+                            top = fmax3(top, x[r] + nm.x, x[r + 1] + nm.y);
+                            top = fmax3(top, x[r + 2] + nm.z, x[r + 3] + nm.w);
+                        }
+                        move = named_barrier_or(1 + w, 128, top > Cfg::kTauLog2 + Cfg::kBias);
+                    }
+                    if (move) {
+                        // maxima over the keys: 16 rows at a time, halved at each exchange (as the row sums below)
+#pragma unroll
+                        for (int g = 0; g < kStates / 16; ++g) {
+                            float a[16];
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) a[j] = x[g * 16 + j];
+#pragma unroll
+                            for (int d = 16, m = 8; d >= 2; d >>= 1, m >>= 1) {
+                                const bool up = (lane & d) != 0;
+#pragma unroll
+                                for (int j = 0; j < m; ++j) {
+                                    const float give = up ? a[j] : a[j + m], keep = up ? a[j + m] : a[j];
+                                    a[j] = fmaxf(keep, __shfl_xor_sync(0xffffffffu, give, d));
+                                }
+                            }
+                            a[0] = fmaxf(a[0], __shfl_xor_sync(0xffffffffu, a[0], 1));
+                            if ((lane & 1) == 0) sh.red[w][wq][g * 16 + (lane >> 1)] = a[0];
+                        }
+                        named_barrier_sync(1 + w, 128);
+                        if (key < kStates) {
+                            const float old = first ? -INFINITY : Cfg::kBias - sh.neg_m[w][key];
+                            const float mx = fmaxf(fmaxf(fmaxf(sh.red[w][0][key], sh.red[w][1][key]), fmaxf(sh.red[w][2][key], sh.red[w][3][key])), old);
+                            sh.neg_m[w][key] = Cfg::kBias - mx;
+                            sh.neg_p[w][key] = mx == -INFINITY ? 0.f : Cfg::kBias - mx;
+                            sh.rescale[w][key] = mx == -INFINITY ? 1.f : exp2_approx(old - mx);
+                        }
+                        if (!first)       // the group's product before: nothing else adds to this accumulator
+                            ok = ok && mbar_wait(smem_addr(&sh.pv_done[w][(mine_n - 1) % kPBufs]), ((mine_n - 1) / kPBufs) & 1, wctx, kSiteSoftmaxCorrFree);
+                        named_barrier_sync(1 + w, 128);
+                        if (!first) {
+#pragma unroll
+                            for (int r = 0; r < kStates; ++r) l[r] *= sh.rescale[w][r];
+                            tc_fence_after_sync();
+#pragma unroll 1
+                            for (int g = 0; g < kCols / 16; ++g) {
+                                const int col = g * 16, st = col / (kTerms * kRows) * kRows + col % kRows;
+                                uint32_t o[16];
+                                tmem_ld_x16(tO + col, o);
+                                tc_wait_ld();
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * sh.rescale[w][st + j]);
+                                tmem_st_x16(tO + col, o);
+                            }
+                            tc_wait_st();
+                        }
+                    }
+                    // The sum of score and reference is rounded apart from the score's own scaling: the score that the reference was
+                    // taken from comes out as exactly the bias, however large it is.
+#pragma unroll
+                    for (int r = 0; r < kStates; r += 4) {
+                        const float4 np = *reinterpret_cast<const float4*>(&sh.neg_p[w][r]);
+                        x[r] = exp2_approx(x[r] + np.x);
+                        x[r + 1] = exp2_approx(x[r + 1] + np.y);
+                        x[r + 2] = exp2_approx(x[r + 2] + np.z);
+                        x[r + 3] = exp2_approx(x[r + 3] + np.w);
+                    }
+#pragma unroll
+                    for (int r = 0; r < kStates; ++r) l[r] += x[r];
+                    // the buffer's last reader: the product of the group's tile kPBufs before
+                    if (mine_n >= kPBufs) ok = ok && mbar_wait(smem_addr(&sh.pv_done[w][pb]), ((mine_n / kPBufs) & 1) ^ 1, wctx, kSiteSoftmaxPFree);
+                    // P^T: row = column of O^T, 128 keys of 1 or 2 bytes, 16-byte pieces swizzled
+                    if constexpr (kE4m3) {
+#pragma unroll
+                        for (int r = 0; r < kStates; r += 2) {
+                            __half2 h = __floats2half2_rn(x[r], x[r + 1]);
+#pragma unroll
+                            for (int term = 0; term < 3; ++term) {
+                                uint32_t bits = *reinterpret_cast<uint32_t*>(&h) & 0xff00ff00u;
+                                const int col = (r / kRows * kTerms + term) * kRows + r % kRows;
+                                st_shared_u8(sPw + col * 128 + (p_byte ^ ((col & 7) << 4)), (bits >> 8) & 0xffu);
+                                st_shared_u8(sPw + (col + 1) * 128 + (p_byte ^ (((col + 1) & 7) << 4)), bits >> 24);
+                                h = __hsub2(h, *reinterpret_cast<__half2*>(&bits));
+                            }
+                        }
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < kStates; r += 2) {
+                            const uint32_t two = pack_bf16x2(x[r], x[r + 1]);
+                            st_shared_u16(sPw + r * 128 + (p_byte ^ ((r & 7) << 4)), two);
+                            st_shared_u16(sPw + (r + 1) * 128 + (p_byte ^ (((r + 1) & 7) << 4)), two >> 16);
+                        }
+                    }
+                    constexpr int kStepKeys = 32 / Cfg::kElem;
+                    const int keys = len - t * kTileN, steps_end = keys <= 0 ? kStepKeys : (keys + kStepKeys - 1) / kStepKeys * kStepKeys;
+                    if (key >= keys && key < steps_end) {
+                        // V rows behind the sequence's end, as far as the last k-step reaches, hold whatever the page held, or were not
+                        // loaded: zeros, since 0 * NaN is NaN
+                        const int s = (tile0 + t - t0) % NS;
+                        ok = ok && mbar_wait(smem_addr(&sh.v_full[s]), ((tile0 + t - t0) / NS) & 1, wctx, kSiteSoftmaxPFree);
+#pragma unroll
+                        for (int c = 0; c < Cfg::kVChunks * 8; ++c)
+                            st_shared_v4(sV + s * Cfg::kVBytes + (c >> 3) * kChunkBytes + key * 128 + (c & 7) * 16, 0, 0, 0, 0);
+                    }
+                    fence_proxy_async_smem();
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_addr(&sh.p_full[w][pb]));
+                }
+
+                // ---- end of the part: row sums over the 128 threads, 16 rows at a time, halved at each exchange
+#pragma unroll
+                for (int g = 0; g < kStates / 16; ++g) {
+                    float a[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) a[j] = l[g * 16 + j];
+#pragma unroll
+                    for (int d = 16, m = 8; d >= 2; d >>= 1, m >>= 1) {
+                        const bool up = (lane & d) != 0;
+#pragma unroll
+                        for (int j = 0; j < m; ++j) {
+                            const float give = up ? a[j] : a[j + m], keep = up ? a[j + m] : a[j];
+                            a[j] = keep + __shfl_xor_sync(0xffffffffu, give, d);
+                        }
+                    }
+                    a[0] += __shfl_xor_sync(0xffffffffu, a[0], 1);
+                    // lane bits 4, 3, 2, 1 chose the halves: row = bit4*8 + bit3*4 + bit2*2 + bit1
+                    if ((lane & 1) == 0) sh.red_l[w][wq][g * 16 + (lane >> 1)] = a[0];
+                }
+                named_barrier_sync(1 + w, 128);
+                if (key < kStates) {
+                    sh.stat_l[k % kPartRing][w][key] = (sh.red_l[w][0][key] + sh.red_l[w][1][key]) + (sh.red_l[w][2][key] + sh.red_l[w][3][key]);
+                    sh.stat_m[k % kPartRing][w][key] = Cfg::kBias - sh.neg_m[w][key];
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_addr(&sh.stat_full[k % kPartRing]));
+            if (key == 0) mbar_arrive(smem_addr(&sh.q_empty[qb]));       // (every thread of the group is past its last use: the barrier above)
+        }
+    } else {
+        // ============================================================ list of parts, query rows, results (thread = output column)
+        const int key = tid & 127, wq = warp & 3;
+        const uint32_t lane_sel = static_cast<uint32_t>(wq * 32) << 16;
+        constexpr uint32_t kBar = 3;
+        bool ok = true;
+        // the list, published by the group's last warp, kPartsAhead parts ahead of the results
         PagedPart walk;
-        walk.begin(p, sh.start_b, sh.start_base, u0, u1, lane == 0);
-        bool ended = false, ok = true;
+        bool ended = false;
         int published = 0;
+        if (wq == 3) walk.begin(p, sh.start_b, sh.start_base, u0, u1, lane == 0);
         auto publish = [&]() {                     // uniform over the warp
-            if (ended) return;
+            if (ended || wq != 3) return;
             const int at = published % kPartRing;
-            ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&sh.part_empty[at]), ((published / kPartRing) & 1) ^ 1, wctx, kSiteItem));
+            ok = __all_sync(0xffffffffu, ok && mbar_wait(smem_addr(&sh.part_empty[at]), ((published / kPartRing) & 1) ^ 1, wctx, kSiteItem));
             if (!ok) return;
             if (lane == 0) {
                 PagedEntry& e = sh.part[at];
@@ -500,322 +742,102 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             if (walk.u >= u1) ended = true;        // that was the end mark
             else walk.next(p);
         };
-        for (int i = 0; i < kPartsAhead; ++i) publish();
+        // the query rows of a part into buffer k & 1 (before k = 2: free; later: the part two before has ended)
         constexpr int kVecs = DQK / 8;                        // 16-byte pieces of a row
         constexpr int kLanes = kVecs == 24 ? 32 : kVecs;      // lanes of a row
-        constexpr int kPass = 32 / kLanes;                    // rows of a pass over the warp
-        constexpr int kBatch = 8;                             // passes whose loads are in flight together
-        static_assert(kRows / kPass % kBatch == 0 || kRows / kPass < kBatch, "query rows");
-        constexpr int kInFlight = kRows / kPass < kBatch ? kRows / kPass : kBatch;
-        for (int k = 0; ok; ++k) {
-            publish();
-            if (!ok) break;
-            const PagedEntry e = sh.part[k % kPartRing];
-            if (e.t1 < 0) break;
-            const int qb = k & 1;
-            const float ks = kE4m3 && p.k_scale ? p.k_scale[e.kvh] : 1.f;
-            const uint32_t sQb = sQ + qb * Cfg::kQBytes;
-            const int row_in = lane / kLanes, piece = lane % kLanes;
-            bool waited = false;
-#pragma unroll 1
-            for (int r0 = 0; r0 < kRows; r0 += kInFlight * kPass) {
-                uint4 x[kInFlight];
-                int place[kInFlight];
+        constexpr int kPass = 128 / kLanes;                   // rows of a pass over the group
+        constexpr int kPasses = (kRows + kPass - 1) / kPass;
+        const int row_in = key / kLanes, piece = key % kLanes;
+        uint4 xs[kPasses];
+        int place[kPasses];
+        float q_scale = 1.f;
+        auto load_queries = [&](int k) {
+            const PagedEntry& e = sh.part[k % kPartRing];
 #pragma unroll
-                for (int j = 0; j < kInFlight; ++j) {
-                    const int r = r0 + j * kPass + row_in, rr = e.rb * kRows + r, i = rr / group, hq = e.kvh * group + rr - i * group;
-                    x[j] = make_uint4(0, 0, 0, 0);
-                    if (i < p.Sq && piece < kVecs)
-                        x[j] = *reinterpret_cast<const uint4*>(p.Q + e.b * p.q_sb + i * p.q_st + hq * p.q_sh + piece * 8);
-                    place[j] = min(i, p.Sq - 1);
-                }
-                if (!waited) {
-                    ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&sh.q_empty[qb]), ((k >> 1) & 1) ^ 1, wctx, kSiteLoadQEmpty));
-                    waited = true;
-                    if (!ok) break;
-                }
-#pragma unroll
-                for (int j = 0; j < kInFlight; ++j) {
-                    const int r = r0 + j * kPass + row_in;
-                    float c = p.scale_log2 * ks;
-                    if constexpr (!kE4m3) {
-                        if (piece < kVecs)
-                            st_shared_v4(sQb + (piece >> 3) * Cfg::kQChunkBytes + r * 128 + (((piece & 7) ^ (r & 7)) << 4),
-                                         x[j].x, x[j].y, x[j].z, x[j].w);
-                    } else {
-                        // scaled by a power of two so that the row's largest entry is in [2^14, 2^15), then three e5m2 terms: exact for
-                        // entries of 2^-24 of the largest and more, below that to 2^-31 of it
-                        const uint32_t w4[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
-                        uint32_t top = 0;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) top = max(top, max((w4[i] & 0x7fffu) << 16, w4[i] & 0x7fff0000u));
-#pragma unroll
-                        for (int d = kLanes / 2; d > 0; d >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
-                        int sft = top ? 14 - (static_cast<int>(top >> 23) - 127) : 0;
-                        sft = sft > 100 ? 100 : (sft < -100 ? -100 : sft);
-                        const float mult = __uint_as_float(static_cast<uint32_t>(sft + 127) << 23);
-                        c *= __uint_as_float(static_cast<uint32_t>(127 - sft) << 23);
-                        uint32_t t8[3][2];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            __half2 h = __floats2half2_rn(__uint_as_float(w4[i] << 16) * mult, __uint_as_float(w4[i] & 0xffff0000u) * mult);
-#pragma unroll
-                            for (int t = 0; t < 3; ++t) {
-                                uint32_t bits = *reinterpret_cast<uint32_t*>(&h) & 0xff00ff00u;
-                                const uint32_t two = __byte_perm(bits, 0, 0x4431);       // the two top bytes
-                                if (i & 1) t8[t][i >> 1] |= two << 16; else t8[t][i >> 1] = two;
-                                h = __hsub2(h, *reinterpret_cast<__half2*>(&bits));
-                            }
-                        }
-                        if (piece < kVecs) {
-#pragma unroll
-                            for (int t = 0; t < 3; ++t) {
-                                const int rq = t * kRows + r, q16 = piece >> 1;
-                                st_shared_u64(sQb + (q16 >> 3) * Cfg::kQChunkBytes + rq * 128 + (((q16 & 7) ^ (rq & 7)) << 4) + (piece & 1) * 8,
-                                              t8[t][0], t8[t][1]);
-                            }
-                        }
-                    }
-                    if (piece == 0) {
-                        sh.c[qb][r] = c;
-                        sh.i[qb][r] = place[j];
-                    }
-                }
+            for (int j = 0; j < kPasses; ++j) {
+                const int r = j * kPass + row_in, rr = e.rb * kRows + r, i = rr / group, hq = e.kvh * group + rr - i * group;
+                xs[j] = make_uint4(0, 0, 0, 0);
+                if (r < kRows && i < p.Sq && piece < kVecs)
+                    xs[j] = *reinterpret_cast<const uint4*>(p.Q + e.b * p.q_sb + i * p.q_st + hq * p.q_sh + piece * 8);
+                place[j] = min(i, p.Sq - 1);
             }
-            if (!ok) break;
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_addr(&sh.q_full[qb]));
-        }
-    } else if (warp < 12) {
-        // ============================================================ softmax groups
-        // The four warps of a group stay together through their barriers: after a wait that ran out they go on to the end of
-        // the part without waiting (results are invalid then, every access stays in bounds) and leave together.
-        setmaxnreg_inc<kPagedRegsSoftmax>();
-        const int w = (warp >> 2) - 1, key = tid & 127, wq = warp & 3;
-        const uint32_t lane_sel = static_cast<uint32_t>(wq * 32) << 16;
-        const uint32_t p_byte = kE4m3 ? key : (key & 63) * 2;            // of this key in a row of P
-        float l[kStates];
-#pragma unroll
-        for (int r = 0; r < kStates; ++r) l[r] = 0.f;
-        int mine_n = 0;                                                  // tiles this group has done
-        bool ok = true;
-        for (int k = 0;; ++k) {
+            q_scale = p.scale_log2 * (kE4m3 && p.k_scale ? p.k_scale[e.kvh] : 1.f);
+        };
+        auto store_queries = [&](int k) {
             const int qb = k & 1;
-            ok = ok && wait_part(k);
-            const PagedEntry e = sh.part[k % kPartRing];
-            if (named_barrier_or(1 + w, 128, !ok) || e.t1 < 0) break;
-            ok = mbar_wait(smem_addr(&sh.q_full[qb]), (k >> 1) & 1, wctx, kSiteMmaQFull);
-            bool any_tile = false;
-            const int first_masked = e.len - p.Sq + 1;                   // the first key that some row does not see
-            int n = e.tile0 + ((e.tile0 & 1) == w ? 0 : 1);              // this group's first tile
-            const uint32_t tO = tmem + o_col(k % kOBufs, w) + lane_sel;
-#pragma unroll 1
-            for (int t = e.t0 + n - e.tile0; t < e.t1; t += 2, n += 2, ++mine_n) {
-                const int sb = mine_n % kBufs, pb = mine_n % kPBufs;
-                const uint32_t tS = tmem + s_col(w, sb) + lane_sel;
-                const uint32_t sPw = sP + (w * kPBufs + pb) * Cfg::kPBytes + (kE4m3 ? 0 : (key >> 6) * Cfg::kPChunkBytes);
-                ok = ok && mbar_wait(smem_addr(&sh.s_full[w][sb]), (mine_n / kBufs) & 1, wctx, kSiteSoftmaxSFull);
-                __syncwarp();
-                tc_fence_after_sync();
-                const int key_at = t * kTileN + key;
-                const bool masked = t * kTileN + kTileN > first_masked;
-                float x[kStates];
-                for (int pass = 0;; ++pass) {
+            const uint32_t sQb = sQ + qb * Cfg::kQBytes;
+            ok = ok && mbar_wait(smem_addr(&sh.q_empty[qb]), ((k >> 1) & 1) ^ 1, wctx, kSiteLoadQEmpty);
+            __syncwarp();
 #pragma unroll
-                    for (int g = 0; g < kStates / 16; ++g) {
-                        // column of (map, term, row): (map * kTerms + term) * kRows + row
-                        const int map = g * 16 / kRows, r0 = g * 16 % kRows;
-                        uint32_t s0[16];
-                        tmem_ld_x16(tS + map * kTerms * kRows + r0, s0);
-                        if constexpr (kE4m3) {
-                            uint32_t s1[16], s2[16];
-                            tmem_ld_x16(tS + (map * kTerms + 1) * kRows + r0, s1);
-                            tmem_ld_x16(tS + (map * kTerms + 2) * kRows + r0, s2);
-                            tc_wait_ld();
+            for (int j = 0; j < kPasses; ++j) {
+                const int r = j * kPass + row_in;
+                float c = q_scale;
+                if constexpr (!kE4m3) {
+                    if (r < kRows && piece < kVecs)
+                        st_shared_v4(sQb + (piece >> 3) * Cfg::kQChunkBytes + r * 128 + (((piece & 7) ^ (r & 7)) << 4), xs[j].x, xs[j].y, xs[j].z, xs[j].w);
+                } else {
+                    // scaled by a power of two so that the row's largest entry is in [2^14, 2^15), then three e5m2 terms: exact for
+                    // entries of 2^-24 of the largest and more, below that to 2^-31 of it
+                    const uint32_t w4[4] = {xs[j].x, xs[j].y, xs[j].z, xs[j].w};
+                    uint32_t top = 0;
 #pragma unroll
-                            for (int j = 0; j < 16; ++j)
-                                s0[j] = __float_as_uint(__uint_as_float(s0[j]) + (__uint_as_float(s1[j]) + __uint_as_float(s2[j])));
-                        } else {
-                            tc_wait_ld();
-                        }
+                    for (int i = 0; i < 4; ++i) top = max(top, max((w4[i] & 0x7fffu) << 16, w4[i] & 0x7fff0000u));
 #pragma unroll
-                        for (int j = 0; j < 16; j += 4) {
-                            const float4 nm = *reinterpret_cast<const float4*>(&sh.neg_m[w][g * 16 + j]);
-                            float4 c = make_float4(p.scale_log2, p.scale_log2, p.scale_log2, p.scale_log2);
-                            if constexpr (kE4m3) c = *reinterpret_cast<const float4*>(&sh.c[qb][r0 + j]);
-                            // product and sum rounded apart: the score that the reference was taken from comes out as exactly
-                            // the bias, however large it is (a fused one could leave half a unit of its last place)
-                            const float2 lo = __fadd2_rn(__fmul2_rn(make_float2(__uint_as_float(s0[j]), __uint_as_float(s0[j + 1])),
-                                                                    make_float2(c.x, c.y)), make_float2(nm.x, nm.y));
-                            const float2 hi = __fadd2_rn(__fmul2_rn(make_float2(__uint_as_float(s0[j + 2]), __uint_as_float(s0[j + 3])),
-                                                                    make_float2(c.z, c.w)), make_float2(nm.z, nm.w));
-                            x[g * 16 + j] = lo.x;
-                            x[g * 16 + j + 1] = lo.y;
-                            x[g * 16 + j + 2] = hi.x;
-                            x[g * 16 + j + 3] = hi.y;
-                        }
-                    }
-                    if (masked) {
+                    for (int d = kLanes / 2; d > 0; d >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+                    int sft = top ? 14 - (static_cast<int>(top >> 23) - 127) : 0;
+                    sft = sft > 100 ? 100 : (sft < -100 ? -100 : sft);
+                    const float mult = __uint_as_float(static_cast<uint32_t>(sft + 127) << 23);
+                    c *= __uint_as_float(static_cast<uint32_t>(127 - sft) << 23);
+                    uint32_t t8[3][2];
 #pragma unroll
-                        for (int r = 0; r < kStates; ++r)
-                            if (key_at >= first_masked + sh.i[qb][r % kRows]) x[r] = -INFINITY;
-                    }
-                    float top = x[0];
+                    for (int i = 0; i < 4; ++i) {
+                        __half2 h = __floats2half2_rn(__uint_as_float(w4[i] << 16) * mult, __uint_as_float(w4[i] & 0xffff0000u) * mult);
 #pragma unroll
-                    for (int r = 1; r + 1 < kStates; r += 2) top = fmax3(top, x[r], x[r + 1]);
-                    top = fmaxf(top, x[kStates - 1]);
-                    if (!named_barrier_or(1 + w, 128, top > Cfg::kTauLog2 + Cfg::kBias) || pass > 0) break;
-                    // some row's reference moves: the maxima of the tile's scores, in log2 units
-#pragma unroll
-                    for (int g = 0; g < kStates / 16; ++g) {
-                        const int map = g * 16 / kRows, r0 = g * 16 % kRows;
-                        uint32_t s0[16];
-                        tmem_ld_x16(tS + map * kTerms * kRows + r0, s0);
-                        if constexpr (kE4m3) {
-                            uint32_t s1[16], s2[16];
-                            tmem_ld_x16(tS + (map * kTerms + 1) * kRows + r0, s1);
-                            tmem_ld_x16(tS + (map * kTerms + 2) * kRows + r0, s2);
-                            tc_wait_ld();
-#pragma unroll
-                            for (int j = 0; j < 16; ++j)
-                                s0[j] = __float_as_uint(__uint_as_float(s0[j]) + (__uint_as_float(s1[j]) + __uint_as_float(s2[j])));
-                        } else {
-                            tc_wait_ld();
-                        }
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) {
-                            float v = __uint_as_float(s0[j]) * (kE4m3 ? sh.c[qb][r0 + j] : p.scale_log2);
-                            if (masked && key_at >= first_masked + sh.i[qb][r0 + j]) v = -INFINITY;
-                            const float mx = warp_max(v);
-                            if (lane == 0) sh.red[w][wq][g * 16 + j] = mx;
-                        }
-                    }
-                    named_barrier_sync(1 + w, 128);
-                    if (key < kStates) {
-                        const float old = Cfg::kBias - sh.neg_m[w][key];
-                        const float mx = fmaxf(fmaxf(fmaxf(sh.red[w][0][key], sh.red[w][1][key]), fmaxf(sh.red[w][2][key], sh.red[w][3][key])), old);
-                        sh.neg_m[w][key] = Cfg::kBias - mx;
-                        sh.rescale[w][key] = mx == -INFINITY ? 1.f : exp2_approx(old - mx);
-                    }
-                    if (any_tile)         // the group's product before: it has been handed over, nothing else adds to this accumulator
-                        ok = ok && mbar_wait(smem_addr(&sh.pv_done[w][(mine_n - 1) % kPBufs]), ((mine_n - 1) / kPBufs) & 1, wctx, kSiteSoftmaxCorrFree);
-                    named_barrier_sync(1 + w, 128);
-#pragma unroll
-                    for (int r = 0; r < kStates; ++r) l[r] *= sh.rescale[w][r];
-                    if (any_tile) {
-                        tc_fence_after_sync();
-#pragma unroll 1
-                        for (int g = 0; g < kCols / 16; ++g) {
-                            const int col = g * 16, st = col / (kTerms * kRows) * kRows + col % kRows;
-                            uint32_t o[16];
-                            tmem_ld_x16(tO + col, o);
-                            tc_wait_ld();
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * sh.rescale[w][st + j]);
-                            tmem_st_x16(tO + col, o);
-                        }
-                        tc_wait_st();
-                    }
-                }
-                if (masked) {
-                    // (a row that has seen no key yet: -inf + inf)
-#pragma unroll
-                    for (int r = 0; r < kStates; ++r)
-                        if (sh.neg_m[w][r] == INFINITY) x[r] = -INFINITY;
-                }
-#pragma unroll
-                for (int r = 0; r < kStates; ++r) {
-                    x[r] = exp2_approx(x[r]);
-                    l[r] += x[r];
-                }
-                // the buffer's last reader: the product of the group's tile kPBufs before
-                if (mine_n >= kPBufs) ok = ok && mbar_wait(smem_addr(&sh.pv_done[w][pb]), ((mine_n / kPBufs) & 1) ^ 1, wctx, kSiteSoftmaxPFree);
-                // P^T: row = column of O^T, 128 keys of 1 or 2 bytes, 16-byte pieces swizzled
-                if constexpr (kE4m3) {
-#pragma unroll
-                    for (int r = 0; r < kStates; r += 2) {
-                        __half2 h = __floats2half2_rn(x[r], x[r + 1]);
-#pragma unroll
-                        for (int term = 0; term < 3; ++term) {
+                        for (int t = 0; t < 3; ++t) {
                             uint32_t bits = *reinterpret_cast<uint32_t*>(&h) & 0xff00ff00u;
-                            const int col = (r / kRows * kTerms + term) * kRows + r % kRows;
-                            st_shared_u8(sPw + col * 128 + (p_byte ^ ((col & 7) << 4)), (bits >> 8) & 0xffu);
-                            st_shared_u8(sPw + (col + 1) * 128 + (p_byte ^ (((col + 1) & 7) << 4)), bits >> 24);
+                            const uint32_t two = __byte_perm(bits, 0, 0x4431);       // the two top bytes
+                            if (i & 1) t8[t][i >> 1] |= two << 16; else t8[t][i >> 1] = two;
                             h = __hsub2(h, *reinterpret_cast<__half2*>(&bits));
                         }
                     }
-                } else {
+                    if (r < kRows && piece < kVecs) {
 #pragma unroll
-                    for (int r = 0; r < kStates; r += 2) {
-                        const uint32_t two = pack_bf16x2(x[r], x[r + 1]);
-                        st_shared_u16(sPw + r * 128 + (p_byte ^ ((r & 7) << 4)), two);
-                        st_shared_u16(sPw + (r + 1) * 128 + (p_byte ^ (((r + 1) & 7) << 4)), two >> 16);
+                        for (int t = 0; t < 3; ++t) {
+                            const int rq = t * kRows + r, q16 = piece >> 1;
+                            st_shared_u64(sQb + (q16 >> 3) * Cfg::kQChunkBytes + rq * 128 + (((q16 & 7) ^ (rq & 7)) << 4) + (piece & 1) * 8,
+                                          t8[t][0], t8[t][1]);
+                        }
                     }
                 }
-                if (t * kTileN + kTileN > e.len) {
-                    // V rows behind the sequence's end hold whatever the page held, or were not loaded: zeros, since 0 * NaN is NaN
-                    const int s = n % NS;
-                    ok = ok && mbar_wait(smem_addr(&sh.v_full[s]), (n / NS) & 1, wctx, kSiteSoftmaxPFree);
-                    if (key_at >= e.len) {
-#pragma unroll
-                        for (int c = 0; c < Cfg::kVChunks * 8; ++c)
-                            st_shared_v4(sV + s * Cfg::kVBytes + (c >> 3) * kChunkBytes + key * 128 + (c & 7) * 16, 0, 0, 0, 0);
-                    }
+                if (r < kRows && piece == 0) {
+                    sh.c[qb][r] = c;
+                    sh.i[qb][r] = place[j];
                 }
-                any_tile = true;
-                fence_proxy_async_smem();
-                tc_fence_before_sync();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_addr(&sh.p_full[w][pb]));
             }
-
-            // ---- end of the part: maxima and row sums to the result warps
-            const int ob = k % kOBufs;
-            ok = ok && mbar_wait(smem_addr(&sh.acc_empty[ob]), ((k / kOBufs) & 1) ^ 1, wctx, kSiteEpiState);
-            named_barrier_sync(1 + w, 128);                              // (neg_m has been read by all)
-            // sums over the 128 threads: 16 columns at a time, halved at each exchange
-#pragma unroll
-            for (int g = 0; g < kStates / 16; ++g) {
-                float a[16];
-#pragma unroll
-                for (int j = 0; j < 16; ++j) a[j] = l[g * 16 + j];
-#pragma unroll
-                for (int d = 16, m = 8; d >= 2; d >>= 1, m >>= 1) {
-                    const bool up = (lane & d) != 0;
-#pragma unroll
-                    for (int j = 0; j < m; ++j) {
-                        const float give = up ? a[j] : a[j + m], keep = up ? a[j + m] : a[j];
-                        a[j] = keep + __shfl_xor_sync(0xffffffffu, give, d);
-                    }
-                }
-                a[0] += __shfl_xor_sync(0xffffffffu, a[0], 1);
-                // lane bits 4, 3, 2, 1 chose the halves: column = bit4*8 + bit3*4 + bit2*2 + bit1
-                if ((lane & 1) == 0) sh.red[w][wq][g * 16 + (lane >> 1)] = a[0];
-            }
-            named_barrier_sync(1 + w, 128);
-            if (key < kStates) {
-                sh.stat_l[ob][w][key] = (sh.red[w][0][key] + sh.red[w][1][key]) + (sh.red[w][2][key] + sh.red[w][3][key]);
-                sh.stat_m[ob][w][key] = Cfg::kBias - sh.neg_m[w][key];
-                sh.neg_m[w][key] = INFINITY;
-            }
-#pragma unroll
-            for (int r = 0; r < kStates; ++r) l[r] = 0.f;
+            fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_addr(&sh.stat_full[ob]));
-            named_barrier_sync(1 + w, 128);                              // the next part reads neg_m
-            if (key == 0) mbar_arrive(smem_addr(&sh.q_empty[qb]));
-        }
-    } else {
-        // ============================================================ results: thread = output column
-        const int key = tid & 127, wq = warp & 3;
-        const uint32_t lane_sel = static_cast<uint32_t>(wq * 32) << 16;
-        constexpr uint32_t kBar = 3;
-        bool ok = true;
-        for (int k = 0;; ++k) {
+            if (lane == 0) mbar_arrive(smem_addr(&sh.q_full[qb]));
+        };
+        for (int i = 0; i < kPartsAhead; ++i) publish();
+        // Rows of parts 0 and 1 now, those of part k + 2 as soon as part k has ended (loaded before that).
+        int end_at = 0x7fffffff;                   // the end mark's place, once seen
+#pragma unroll 1
+        for (int k = 0; k < 2; ++k) {
+            if (k >= end_at) break;
             ok = ok && wait_part(k);
+            if (named_barrier_or(kBar, 128, !ok)) break;
+            if (sh.part[k % kPartRing].t1 < 0) { end_at = k; break; }
+            load_queries(k);
+            store_queries(k);
+        }
+        for (int k = 0; k < end_at; ++k) {
+            if (k > 0) publish();
+            if (k + 2 < end_at) ok = ok && wait_part(k + 2);
+            if (named_barrier_or(kBar, 128, !ok)) break;
+            if (k + 2 < end_at && sh.part[(k + 2) % kPartRing].t1 < 0) end_at = k + 2;
+            const bool stage = k + 2 < end_at;
+            if (stage) load_queries(k + 2);
             const PagedEntry e = sh.part[k % kPartRing];
-            if (named_barrier_or(kBar, 128, !ok) || e.t1 < 0) break;
             const int ob = k % kOBufs;
             const bool whole = e.slot < 0;
             if (key < kRows) {
@@ -833,12 +855,19 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                 p.lse[static_cast<long long>(sh.out_hq[r]) * p.B * p.Sq + static_cast<long long>(e.b) * p.Sq + sh.out_i[r]] =
                     sum > 0.f ? (m - Cfg::kBias + log2f(sum)) * 0.6931471805599453f : -INFINITY;
             };
-            ok = mbar_wait(smem_addr(&sh.stat_full[ob]), (k / kOBufs) & 1, wctx, kSiteEpiState);
+            ok = ok && mbar_wait(smem_addr(&sh.stat_full[k % kPartRing]), (k / kPartRing) & 1, wctx, kSiteEpiState);
+            __syncwarp();
+            if (stage) store_queries(k + 2);
             named_barrier_sync(kBar, 128);
+            // (uniform) whether a group had a tile of this part
+            const bool had[2] = {e.t1 - e.t0 > 1 || (e.tile0 & 1) == 0, e.t1 - e.t0 > 1 || (e.tile0 & 1) == 1};
             if (key < kStates) {
                 float f[2], sum[2], mx[2];
 #pragma unroll
-                for (int v = 0; v < 2; ++v) { mx[v] = sh.stat_m[ob][v][key]; sum[v] = sh.stat_l[ob][v][key]; }
+                for (int v = 0; v < 2; ++v) {
+                    mx[v] = had[v] ? sh.stat_m[k % kPartRing][v][key] : -INFINITY;
+                    sum[v] = had[v] ? sh.stat_l[k % kPartRing][v][key] : 0.f;
+                }
                 const float m = fmaxf(mx[0], mx[1]);
 #pragma unroll
                 for (int v = 0; v < 2; ++v) f[v] = mx[v] == -INFINITY ? 0.f : exp2_approx(mx[v] - m);
@@ -861,8 +890,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             for (int r = 0; r < kStates; ++r) y[r] = 0.f;
 #pragma unroll
             for (int v = 0; v < 2; ++v) {
-                // (uniform) an accumulator that got nothing of this part
-                if (e.t1 - e.t0 < 2 && (e.tile0 & 1) != v) continue;
+                if (!had[v]) continue;
 #pragma unroll
                 for (int g = 0; g < kCols / 16; ++g) {
                     const int col = g * 16, st = col / (kTerms * kRows) * kRows + col % kRows;
