@@ -20,7 +20,7 @@ using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t
 
 struct MapEntry {
     const void* ptr;
-    int d, S, H, B, box_rows, box_heads, elem_bytes, swizzle_bytes;
+    int d, S, H, B, box_rows, box_heads, elem_bytes, swizzle_bytes, promotion;
     long long sb, sh, ss;      // batch / head / row strides in elements
     uint64_t stamp;
     CUtensorMap map;
@@ -81,10 +81,10 @@ class DeviceGuard {
 // x box_rows rows, 128-byte swizzle, rows past S read as zero.
 inline fa_status get_map(fa_handle* h, const void* ptr, int d, int S, int H, int B, long long sb, long long sh,
                   long long ss, int box_rows, const CUtensorMap** out, int elem_bytes = 2, int box_heads = 1,
-                  int swizzle_bytes = 128) {
+                  int swizzle_bytes = 128, int promotion = CU_TENSOR_MAP_L2_PROMOTION_L2_256B) {
     for (auto& e : h->maps) {
         if (e.ptr == ptr && e.d == d && e.S == S && e.H == H && e.B == B && e.box_rows == box_rows &&
-            e.sb == sb && e.sh == sh && e.ss == ss && e.elem_bytes == elem_bytes && e.box_heads == box_heads && e.swizzle_bytes == swizzle_bytes) {
+            e.sb == sb && e.sh == sh && e.ss == ss && e.elem_bytes == elem_bytes && e.box_heads == box_heads && e.swizzle_bytes == swizzle_bytes && e.promotion == promotion) {
             e.stamp = ++h->stamp;
             *out = &e.map;
             return FA_OK;
@@ -93,7 +93,7 @@ inline fa_status get_map(fa_handle* h, const void* ptr, int d, int S, int H, int
     MapEntry ne;
     memset(&ne, 0, sizeof ne);
     ne.ptr = ptr; ne.d = d; ne.S = S; ne.H = H; ne.B = B; ne.box_rows = box_rows;
-    ne.sb = sb; ne.sh = sh; ne.ss = ss; ne.elem_bytes = elem_bytes; ne.box_heads = box_heads; ne.swizzle_bytes = swizzle_bytes;
+    ne.sb = sb; ne.sh = sh; ne.ss = ss; ne.elem_bytes = elem_bytes; ne.box_heads = box_heads; ne.swizzle_bytes = swizzle_bytes; ne.promotion = promotion;
     const cuuint64_t eb = static_cast<cuuint64_t>(elem_bytes);
     const cuuint64_t dims[4] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(S),
                                 static_cast<cuuint64_t>(H), static_cast<cuuint64_t>(B)};
@@ -106,7 +106,7 @@ inline fa_status get_map(fa_handle* h, const void* ptr, int d, int S, int H, int
                                  4, const_cast<void*>(ptr),
                                  dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                                  swizzle_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
-                                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                 static_cast<CUtensorMapL2promotion>(promotion),
                                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return FA_ERR_INVALID_ARG;     // strides or extents the TMA unit cannot express
     ne.stamp = ++h->stamp;

@@ -69,6 +69,45 @@ FA_DEVI void st_shared_u64(uint32_t addr, uint32_t lo, uint32_t hi) {
 
 }  // namespace ptx
 
+// Bounded waits.  The result warps wait, directly or in turn, for every other role: they alone watch the clock.  Once one of their
+// waits has run out, the abort flag ends everybody's, and all roles fall through to the common exit.  (Every wait with a
+// clock of its own, as ptx::mbar_wait, in some twenty places would take more than the instruction cache holds.)
+struct PagedWait {
+    uint32_t abort_flag;
+    uint32_t* status;
+    unsigned long long limit_ns;
+};
+FA_DEVI bool paged_wait(uint64_t& bar, uint32_t parity, PagedWait* ctx) {
+    const uint32_t at = ptx::smem_addr(&bar);
+    while (!ptx::mbar_try_wait(at, parity))
+        if (*static_cast<volatile uint32_t*>(&ctx->abort_flag)) return false;
+    return true;
+}
+static __device__ __noinline__ bool paged_wait_timed(uint64_t* bar, uint32_t parity, PagedWait* ctx, uint32_t who) {
+    const uint32_t at = ptx::smem_addr(bar);
+    volatile uint32_t* abort_flag = &ctx->abort_flag;
+    uint64_t t0 = 0;
+    for (uint32_t it = 1;; ++it) {
+        if (ptx::mbar_try_wait(at, parity)) return true;
+        if ((it & 63u) == 0u) {
+            if (*abort_flag) return false;
+            const uint64_t now = ptx::globaltimer_ns();
+            if (t0 == 0) {
+                t0 = now;
+            } else if (now - t0 > ctx->limit_ns) {
+                *abort_flag = 1u;
+                if (ctx->status) {
+                    volatile uint32_t* sw = ctx->status;      // mapped host memory: plain stores
+                    sw[1] = who;
+                    sw[0] = 4u;                               // FA_ERR_DEVICE_TIMEOUT
+                    __threadfence_system();
+                }
+                return false;
+            }
+        }
+    }
+}
+
 // ------------------------------------------------------------------ the list of work units and its shares
 
 // A unit is one tile of 128 keys of one (sequence, K/V head, block of rows); a sequence without keys has one empty tile per
@@ -77,15 +116,19 @@ __host__ __device__ inline int paged_tiles(int len) { return len > 0 ? (len + kT
 __host__ __device__ inline long long paged_units(const PagedParams& p, int b) {
     return static_cast<long long>(paged_tiles(clamped_len(p.seq_lens[b], p.max_pages, p.page_size, nullptr))) * p.Hkv * p.row_blocks;
 }
+// a / b for non-negative numbers, nearly always of 32 bits
+__host__ __device__ inline long long paged_quot(long long a, long long b) {
+    return ((a | b) >> 32) == 0 ? static_cast<long long>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b)) : a / b;
+}
 __host__ __device__ inline long long paged_share(long long units, int ctas, int least) {
-    const long long per = (units + ctas - 1) / ctas;
+    const long long per = paged_quot(units + ctas - 1, ctas);
     return per < least ? least : per;
 }
 // First CTA of the (sequence, head, row block) whose units are [ua, ub), the number of CTAs that have a part of it, and the
 // partial-result slot of CTA c's part (a CTA leaves at most two parts unfinished: its first and its last).
-__host__ __device__ inline int paged_first_cta(long long ua, long long share) { return static_cast<int>(ua / share); }
+__host__ __device__ inline int paged_first_cta(long long ua, long long share) { return static_cast<int>(paged_quot(ua, share)); }
 __host__ __device__ inline int paged_pieces(long long ua, long long ub, long long share) {
-    return static_cast<int>((ub - 1) / share - ua / share) + 1;
+    return static_cast<int>(paged_quot(ub - 1, share) - paged_quot(ua, share)) + 1;
 }
 __host__ __device__ inline int paged_slot(int cta, long long ua, long long share) { return 2 * cta + (ua > cta * share ? 1 : 0); }
 
@@ -107,7 +150,7 @@ struct PagedPart {
     }
     __host__ __device__ void set() {
         const long long local = u - base;
-        hr = static_cast<int>(local / nt);
+        hr = static_cast<int>(paged_quot(local, nt));
         t0 = static_cast<int>(local - static_cast<long long>(hr) * nt);
         t1 = (u1 - u < nt - t0) ? t0 + static_cast<int>(u1 - u) : nt;
     }
@@ -149,11 +192,11 @@ struct PagedShared {
     uint64_t part_full[kPartRing], part_empty[kPartRing], stat_full[kPartRing];
     PagedEntry part[kPartRing];
     uint32_t tmem_base;
-    uint32_t abort_flag;
+    PagedWait wait;
     uint32_t is_last;
     int start_b;
     long long start_base;
-    long long warp_sums[16];
+    long long warp_sums[4];
     alignas(16) float c[2][kRows];                       // per query buffer: factor of a score (log2 units)
     int i[2][kRows];                                     // place among the new tokens
     // per group: bias - reference maximum, +inf where no key has been seen; and the same with 0 there
@@ -263,7 +306,9 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         return;
     }
     if (tid == 0) {
-        sh.abort_flag = 0;
+        sh.wait.abort_flag = 0;
+        sh.wait.status = p.status;
+        sh.wait.limit_ns = p.wait_limit_ns;
         for (int s = 0; s < NS; ++s) {
             mbar_init(smem_addr(&sh.k_full[s]), 1);
             mbar_init(smem_addr(&sh.k_empty[s]), 1);
@@ -299,56 +344,19 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         if (tid < 128) st_shared_v4(sZero + tid * 16, 0, 0, 0, 0);
         fence_proxy_async_smem();
     }
-    grid_dependency_wait();
-
-    // ---- the shares: every thread sums up the units of consecutive sequences, a scan over the CTA finds the total
-    const int chunk = (p.B + 511) / 512;
-    const int b_first = tid * chunk, b_last = min(p.B, b_first + chunk);
-    long long mine = 0;
-    for (int b = b_first; b < b_last; ++b) mine += paged_units(p, b);
-    long long before = mine;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const long long o = __shfl_up_sync(0xffffffffu, before, d);
-        if (lane >= d) before += o;
-    }
-    if (lane == 31) sh.warp_sums[warp] = before;
-    before -= mine;
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem = sh.tmem_base;
-    long long total = 0;
-#pragma unroll
-    for (int w = 0; w < 16; ++w) {
-        const long long x = sh.warp_sums[w];
-        if (w < warp) before += x;
-        total += x;
-    }
-    const long long share = paged_share(total, gridDim.x, p.least_units);
-    const long long u0 = blockIdx.x * share, u1 = min(total, u0 + share);
-    if (u0 >= total) {                        // uniform
-        if (warp == 1) tmem_dealloc(tmem, Cfg::kTmemCols);
-        return;
-    }
-    if (before <= u0 && u0 < before + mine) {
-        int b = b_first;
-        long long base = before;
-        for (;; ++b) {
-            const long long n = paged_units(p, b);
-            if (u0 < base + n) break;
-            base += n;
-        }
-        sh.start_b = b;
-        sh.start_base = base;
-    }
-    __syncthreads();
+    // (everything so far ran beside the kernel before; from here on its results may be read)
+    grid_dependency_wait();
     // TMEM: S^T of group w, buffer i at (w*kBufs + i)*kCols; O^T of accumulator buffer ob, group w behind them
     auto s_col = [&](int w, int i) -> uint32_t { return (w * kBufs + i) * kCols; };
     auto o_col = [&](int ob, int w) -> uint32_t { return (Cfg::kSBufs + ob * 2 + w) * kCols; };
-    WaitCtx wctx{&sh.abort_flag, p.status, p.wait_limit_ns};
+    PagedWait* const wait = &sh.wait;
     const int group = p.Hq / p.Hkv;
-    auto wait_part = [&](int k) -> bool { return mbar_wait(smem_addr(&sh.part_full[k % kPartRing]), (k / kPartRing) & 1, wctx, kSiteItem); };
+    auto wait_part_timed = [&](int k) -> bool { return paged_wait_timed(&sh.part_full[k % kPartRing], (k / kPartRing) & 1, wait, kSiteItem); };
+    auto wait_part = [&](int k) -> bool { return paged_wait(sh.part_full[k % kPartRing], (k / kPartRing) & 1, wait); };
 
     if (warp == 0 || warp == 2) {
         // ============================================================ TMA loads of K (warp 0) or V (warp 2)
@@ -388,7 +396,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                     }
                     const int from = ((t - first) << shift) + lane;
                     const int page = __shfl_sync(0xffffffffu, pages, from & 31), slot = __shfl_sync(0xffffffffu, slots, from & 31);
-                    ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&empty[s]), parity, wctx, kSiteLoadKvEmpty));
+                    ok = __all_sync(0xffffffffu, paged_wait(empty[s], parity, wait));
                     if (!ok) break;
                     const uint32_t bar = smem_addr(&full[s]);
                     const int n_box = min(boxes, (max(0, e.len - t * kTileN) + box - 1) / box);
@@ -423,12 +431,12 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                 if (!wait_part(k)) break;
                 const int tiles = sh.part[k % kPartRing].t1 - sh.part[k % kPartRing].t0;
                 if (sh.part[k % kPartRing].t1 < 0) break;
-                if (!mbar_wait(smem_addr(&sh.q_full[k & 1]), (k >> 1) & 1, wctx, kSiteMmaQFull)) break;
+                if (!paged_wait(sh.q_full[k & 1], (k >> 1) & 1, wait)) break;
                 const uint32_t q_lo = q_lo0 + (k & 1) * (Cfg::kQBytes >> 4);
                 for (int t = 0; t < tiles; ++t, ++n) {
                     const int w = n & 1, i = (n >> 1) % kBufs;
-                    ok = mbar_wait(smem_addr(&sh.s_empty[w][i]), (((n >> 1) / kBufs) & 1) ^ 1, wctx, kSiteMmaSFree) &&
-                         mbar_wait(smem_addr(&sh.k_full[s]), k_parity, wctx, kSiteMmaKvFull);
+                    ok = paged_wait(sh.s_empty[w][i], (((n >> 1) / kBufs) & 1) ^ 1, wait) &&
+                         paged_wait(sh.k_full[s], k_parity, wait);
                     if (!ok) break;
                     tc_fence_after_sync();
                     const uint32_t k_lo = k_lo0 + s * (Cfg::kKBytes >> 4), d = tmem + s_col(w, i);
@@ -462,11 +470,11 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                 if (!wait_part(k)) break;
                 const PagedEntry e = sh.part[k % kPartRing];
                 if (e.t1 < 0) break;
-                if (!mbar_wait(smem_addr(&sh.acc_empty[k % kOBufs]), ((k / kOBufs) & 1) ^ 1, wctx, kSiteMmaOReady)) break;
+                if (!paged_wait(sh.acc_empty[k % kOBufs], ((k / kOBufs) & 1) ^ 1, wait)) break;
                 for (int t = e.t0; t < e.t1; ++t, ++n) {
                     const int w = n & 1, i = (n >> 1) % kPBufs;
-                    ok = mbar_wait(smem_addr(&sh.v_full[s]), v_parity, wctx, kSiteMmaKvFull) &&
-                         mbar_wait(smem_addr(&sh.p_full[w][i]), ((n >> 1) / kPBufs) & 1, wctx, kSiteMmaPFull);
+                    ok = paged_wait(sh.v_full[s], v_parity, wait) &&
+                         paged_wait(sh.p_full[w][i], ((n >> 1) / kPBufs) & 1, wait);
                     if (!ok) break;
                     tc_fence_after_sync();
                     const uint32_t v_lo = v_lo0 + s * (Cfg::kVBytes >> 4), p_lo = p_lo0 + (w * kPBufs + i) * (Cfg::kPBytes >> 4);
@@ -506,7 +514,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             const int t0 = entry.t0, t1 = entry.t1, len = entry.len, tile0 = entry.tile0;
             if (named_barrier_or(1 + w, 128, !ok) || t1 < 0) break;
             // (also by a group without a tile here: its arrival at q_empty must not run ahead into the buffer's next turn)
-            ok = mbar_wait(smem_addr(&sh.q_full[qb]), (k >> 1) & 1, wctx, kSiteMmaQFull);
+            ok = paged_wait(sh.q_full[qb], (k >> 1) & 1, wait);
             const int skip = (tile0 & 1) == w ? 0 : 1;                   // this group's first tile of the part: t0 + skip
             if (t0 + skip < t1) {
                 float l[kStates];
@@ -520,7 +528,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                     const bool first = t == t0 + skip;
                     const uint32_t tS = tmem + s_col(w, sb) + lane_sel;
                     const uint32_t sPw = sP + (w * kPBufs + pb) * Cfg::kPBytes + (kE4m3 ? 0 : (key >> 6) * Cfg::kPChunkBytes);
-                    ok = ok && mbar_wait(smem_addr(&sh.s_full[w][sb]), (mine_n / kBufs) & 1, wctx, kSiteSoftmaxSFull);
+                    ok = ok && paged_wait(sh.s_full[w][sb], (mine_n / kBufs) & 1, wait);
                     __syncwarp();
                     tc_fence_after_sync();
                     const int key_at = t * kTileN + key;
@@ -603,7 +611,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                             sh.rescale[w][key] = mx == -INFINITY ? 1.f : exp2_approx(old - mx);
                         }
                         if (!first)       // the group's product before: nothing else adds to this accumulator
-                            ok = ok && mbar_wait(smem_addr(&sh.pv_done[w][(mine_n - 1) % kPBufs]), ((mine_n - 1) / kPBufs) & 1, wctx, kSiteSoftmaxCorrFree);
+                            ok = ok && paged_wait(sh.pv_done[w][(mine_n - 1) % kPBufs], ((mine_n - 1) / kPBufs) & 1, wait);
                         named_barrier_sync(1 + w, 128);
                         if (!first) {
 #pragma unroll
@@ -635,7 +643,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
 #pragma unroll
                     for (int r = 0; r < kStates; ++r) l[r] += x[r];
                     // the buffer's last reader: the product of the group's tile kPBufs before
-                    if (mine_n >= kPBufs) ok = ok && mbar_wait(smem_addr(&sh.pv_done[w][pb]), ((mine_n / kPBufs) & 1) ^ 1, wctx, kSiteSoftmaxPFree);
+                    if (mine_n >= kPBufs) ok = ok && paged_wait(sh.pv_done[w][pb], ((mine_n / kPBufs) & 1) ^ 1, wait);
                     // P^T: row = column of O^T, 128 keys of 1 or 2 bytes, 16-byte pieces swizzled
                     if constexpr (kE4m3) {
 #pragma unroll
@@ -664,7 +672,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                         // V rows behind the sequence's end, as far as the last k-step reaches, hold whatever the page held, or were not
                         // loaded: zeros, since 0 * NaN is NaN
                         const int s = (tile0 + t - t0) % NS;
-                        ok = ok && mbar_wait(smem_addr(&sh.v_full[s]), ((tile0 + t - t0) / NS) & 1, wctx, kSiteSoftmaxPFree);
+                        ok = ok && paged_wait(sh.v_full[s], ((tile0 + t - t0) / NS) & 1, wait);
 #pragma unroll
                         for (int c = 0; c < Cfg::kVChunks * 8; ++c)
                             st_shared_v4(sV + s * Cfg::kVBytes + (c >> 3) * kChunkBytes + key * 128 + (c & 7) * 16, 0, 0, 0, 0);
@@ -710,15 +718,54 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         const uint32_t lane_sel = static_cast<uint32_t>(wq * 32) << 16;
         constexpr uint32_t kBar = 3;
         bool ok = true;
-        // the list, published by the group's last warp, kPartsAhead parts ahead of the results
+        // the shares: every thread sums up the units of consecutive sequences, a scan over the group finds the total and the
+        // sequence that the CTA's share begins in
+        const int chunk = (p.B + 127) / 128;
+        const int b_first = key * chunk, b_last = min(p.B, b_first + chunk);
+        long long mine = 0;
+#pragma unroll 4
+        for (int b = b_first; b < b_last; ++b) mine += paged_units(p, b);
+        long long before = mine;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const long long o = __shfl_up_sync(0xffffffffu, before, d);
+            if (lane >= d) before += o;
+        }
+        if (lane == 31) sh.warp_sums[wq] = before;
+        before -= mine;
+        named_barrier_sync(kBar, 128);
+        long long total = 0;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const long long n = sh.warp_sums[v];
+            if (v < wq) before += n;
+            total += n;
+        }
+        const long long share = paged_share(total, gridDim.x, p.least_units);
+        const long long u0 = blockIdx.x * share, u1 = min(total, u0 + share);
+        if (before <= u0 && u0 < before + mine) {
+            int b = b_first;
+            long long base = before;
+            for (;; ++b) {
+                const long long n = paged_units(p, b);
+                if (u0 < base + n) break;
+                base += n;
+            }
+            sh.start_b = b;
+            sh.start_base = base;
+        }
+        named_barrier_sync(kBar, 128);
+        // the list, published by the group's last warp, kPartsAhead parts ahead of the results; a CTA without a share has the end
+        // mark alone
         PagedPart walk;
         bool ended = false;
         int published = 0;
-        if (wq == 3) walk.begin(p, sh.start_b, sh.start_base, u0, u1, lane == 0);
+        if (wq == 3 && u0 < total) walk.begin(p, sh.start_b, sh.start_base, u0, u1, lane == 0);
+        else walk = PagedPart{u1, u1, u1, 0, 0, 1, 0, 0, 0, false};
         auto publish = [&]() {                     // uniform over the warp
             if (ended || wq != 3) return;
             const int at = published % kPartRing;
-            ok = __all_sync(0xffffffffu, ok && mbar_wait(smem_addr(&sh.part_empty[at]), ((published / kPartRing) & 1) ^ 1, wctx, kSiteItem));
+            ok = __all_sync(0xffffffffu, ok && paged_wait_timed(&sh.part_empty[at], ((published / kPartRing) & 1) ^ 1, wait, kSiteItem));
             if (!ok) return;
             if (lane == 0) {
                 PagedEntry& e = sh.part[at];
@@ -729,7 +776,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                 e.rb = walk.hr - e.kvh * p.row_blocks;
                 e.len = walk.len;
                 e.t0 = walk.t0;
-                e.t1 = walk.u < u1 ? walk.t1 : -1;
+                e.t1 = walk.u < walk.u1 ? walk.t1 : -1;
                 e.tile0 = static_cast<int>(walk.u - u0);
                 e.slot = whole ? -1 : paged_slot(blockIdx.x, ua, share);
                 e.pieces = whole ? 1 : paged_pieces(ua, ua + walk.nt, share);
@@ -739,7 +786,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             }
             __syncwarp();
             ++published;
-            if (walk.u >= u1) ended = true;        // that was the end mark
+            if (walk.u >= walk.u1) ended = true;   // that was the end mark
             else walk.next(p);
         };
         // the query rows of a part into buffer k & 1 (before k = 2: free; later: the part two before has ended)
@@ -766,7 +813,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         auto store_queries = [&](int k) {
             const int qb = k & 1;
             const uint32_t sQb = sQ + qb * Cfg::kQBytes;
-            ok = ok && mbar_wait(smem_addr(&sh.q_empty[qb]), ((k >> 1) & 1) ^ 1, wctx, kSiteLoadQEmpty);
+            ok = ok && paged_wait_timed(&sh.q_empty[qb], ((k >> 1) & 1) ^ 1, wait, kSiteLoadQEmpty);
             __syncwarp();
 #pragma unroll
             for (int j = 0; j < kPasses; ++j) {
@@ -818,25 +865,21 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_addr(&sh.q_full[qb]));
         };
-        for (int i = 0; i < kPartsAhead; ++i) publish();
-        // Rows of parts 0 and 1 now, those of part k + 2 as soon as part k has ended (loaded before that).
+        // Rounds -2 and -1 stage the rows of parts 0 and 1; round k those of part k + 2 as soon as part k has ended (they are loaded
+        // before that), and then part k's results.
         int end_at = 0x7fffffff;                   // the end mark's place, once seen
+        for (int k = -2; k < end_at; ++k) {
 #pragma unroll 1
-        for (int k = 0; k < 2; ++k) {
-            if (k >= end_at) break;
-            ok = ok && wait_part(k);
-            if (named_barrier_or(kBar, 128, !ok)) break;
-            if (sh.part[k % kPartRing].t1 < 0) { end_at = k; break; }
-            load_queries(k);
-            store_queries(k);
-        }
-        for (int k = 0; k < end_at; ++k) {
-            if (k > 0) publish();
-            if (k + 2 < end_at) ok = ok && wait_part(k + 2);
+            for (int i = k == -2 ? kPartsAhead : 1; i > 0; --i) publish();
+            if (k + 2 < end_at) ok = ok && wait_part_timed(k + 2);
             if (named_barrier_or(kBar, 128, !ok)) break;
             if (k + 2 < end_at && sh.part[(k + 2) % kPartRing].t1 < 0) end_at = k + 2;
             const bool stage = k + 2 < end_at;
             if (stage) load_queries(k + 2);
+            if (k >= 0) ok = ok && paged_wait_timed(&sh.stat_full[k % kPartRing], (k / kPartRing) & 1, wait, kSiteEpiState);
+            __syncwarp();
+            if (stage) store_queries(k + 2);
+            if (k < 0) continue;
             const PagedEntry e = sh.part[k % kPartRing];
             const int ob = k % kOBufs;
             const bool whole = e.slot < 0;
@@ -855,9 +898,6 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                 p.lse[static_cast<long long>(sh.out_hq[r]) * p.B * p.Sq + static_cast<long long>(e.b) * p.Sq + sh.out_i[r]] =
                     sum > 0.f ? (m - Cfg::kBias + log2f(sum)) * 0.6931471805599453f : -INFINITY;
             };
-            ok = ok && mbar_wait(smem_addr(&sh.stat_full[k % kPartRing]), (k / kPartRing) & 1, wctx, kSiteEpiState);
-            __syncwarp();
-            if (stage) store_queries(k + 2);
             named_barrier_sync(kBar, 128);
             // (uniform) whether a group had a tile of this part
             const bool had[2] = {e.t1 - e.t0 > 1 || (e.tile0 & 1) == 0, e.t1 - e.t0 > 1 || (e.tile0 & 1) == 1};
@@ -882,7 +922,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                     slot_ml[kStates + key] = all;
                 }
             }
-            ok = ok && mbar_wait(smem_addr(&sh.acc_full[ob]), (k / kOBufs) & 1, wctx, kSiteEpiOFull);
+            ok = ok && paged_wait_timed(&sh.acc_full[ob], (k / kOBufs) & 1, wait, kSiteEpiOFull);
             named_barrier_sync(kBar, 128);
             tc_fence_after_sync();
             float y[kStates];
@@ -939,9 +979,8 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                     }
                 }
             };
-            if (whole) {
-                store_rows();
-            } else {
+            bool final_rows = whole;
+            if (!whole) {
                 if (key < DV) {
 #pragma unroll
                     for (int r = 0; r < kStates; ++r) slot_o[r * DV + key] = y[r];
@@ -955,7 +994,8 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                     __threadfence();
                 }
                 named_barrier_sync(kBar, 128);
-                if (sh.is_last) {
+                final_rows = sh.is_last != 0;
+                if (final_rows) {
                     // this CTA finished last: all pieces, in the order of the CTAs
                     __threadfence();
                     // (the other pieces are the first parts of their CTAs)
@@ -994,9 +1034,9 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                             }
                         }
                     }
-                    store_rows();
                 }
             }
+            if (final_rows) store_rows();
             named_barrier_sync(kBar, 128);
             if (key == 0) mbar_arrive(smem_addr(&sh.part_empty[k % kPartRing]));
         }
