@@ -102,12 +102,16 @@ int rows_per_block(int rows, int dqk, bool e4m3, bool diff) {
     return rows > 32 && !e4m3 && !diff && dqk != 192 ? 64 : 32;
 }
 
+// Tiles of 128 keys that a call's list of work can have at most; the kernel counts them in 32 bits.
+long long most_units(const fa::PagedParams& p) {
+    return static_cast<long long>(p.B) * p.Hkv * p.row_blocks *
+           fa::paged_tiles(static_cast<int>(static_cast<long long>(p.max_pages) * p.page_size));
+}
+
 // CTAs of a launch: one per SM, as many as there can be units, and as many as the scratch has two partial results for.
 int paged_ctas(int num_sms, size_t scratch_bytes, const fa::PagedParams& p, int dv, int states) {
     long long ctas = num_sms;
-    const long long most = static_cast<long long>(p.B) * p.Hkv * p.row_blocks *
-                           fa::paged_tiles(static_cast<int>(static_cast<long long>(p.max_pages) * p.page_size));
-    if (ctas > most) ctas = most;
+    if (ctas > most_units(p)) ctas = most_units(p);
     const long long fit = static_cast<long long>(scratch_bytes / (2 * fa::paged_slot_bytes(dv, states)));
     return static_cast<int>(ctas > fit ? fit : ctas);
 }
@@ -187,6 +191,7 @@ fa_status forward_paged(fa_handle* h, const fa_paged_cache* cache, const fa_page
     p.least_units = kLeastUnits;
     const int rows = Hq / cache->Hkv * Sq, block = rows_per_block(rows, cache->dqk, e4m3, diff != nullptr);
     p.row_blocks = (rows + block - 1) / block;
+    if (most_units(p) > 0x7fff0000LL) return FA_ERR_UNSUPPORTED;
     const int eb = e4m3 ? 1 : 2;
     const CUtensorMap* m = nullptr;
     // Rows of one head that lie apart (a [pages, slots, heads, d] pool) are fetched into L2 as they are; with the default of 256 bytes
@@ -353,28 +358,29 @@ fa_status fa_plan_paged(int num_sms, const fa_config* cfg, const fa_paged_cache*
     const int rows = Hq / cache->Hkv * Sq, block = rows_per_block(rows, cache->dqk, cache->type == FA_CACHE_E4M3, diff != 0);
     p.row_blocks = (rows + block - 1) / block;
     p.least_units = kLeastUnits;
+    if (most_units(p) > 0x7fff0000LL) return FA_ERR_UNSUPPORTED;
     const int ctas = paged_ctas(num_sms, static_cast<size_t>(scratch), p, cache->dv, (diff ? 2 : 1) * block);
     if (ctas < 1) return FA_ERR_UNSUPPORTED;
-    long long total = 0;
+    int total = 0;
     for (int b = 0; b < p.B; ++b) total += fa::paged_units(p, b);
-    const long long share = fa::paged_share(total, ctas, p.least_units);
+    const int share = fa::paged_share(total, ctas, p.least_units);
     out->rows_per_block = block;
     out->row_blocks = p.row_blocks;
     out->ctas = ctas;
     out->units = total;
     out->units_per_cta = share;
     // the walk of every CTA, as the kernel makes it
-    long long n = 0, base = 0;
-    int b = 0;
+    long long n = 0;
+    int b = 0, base = 0;
     for (int c = 0; c < ctas && c * share < total; ++c) {
-        const long long u0 = c * share, u1 = u0 + share < total ? u0 + share : total;
+        const int u0 = c * share, u1 = u0 + share < total ? u0 + share : total;
         while (u0 >= base + fa::paged_units(p, b)) base += fa::paged_units(p, b++);
         fa::PagedPart part;
         part.begin(p, b, base, u0, u1, false);
         do {
             if (n < max_pieces) {
                 const bool whole = part.t1 - part.t0 == part.nt;
-                const long long ua = part.first_unit();
+                const int ua = part.first_unit();
                 fa_paged_piece* x = pieces + n;
                 x->cta = c;
                 x->sequence = part.b;

@@ -79,8 +79,10 @@ struct PagedWait {
 };
 FA_DEVI bool paged_wait(uint64_t& bar, uint32_t parity, PagedWait* ctx) {
     const uint32_t at = ptx::smem_addr(&bar);
-    while (!ptx::mbar_try_wait(at, parity))
+    if (ptx::mbar_try_wait(at, parity)) return true;
+    do {
         if (*static_cast<volatile uint32_t*>(&ctx->abort_flag)) return false;
+    } while (!ptx::mbar_try_wait(at, parity));
     return true;
 }
 static __device__ __noinline__ bool paged_wait_timed(uint64_t* bar, uint32_t parity, PagedWait* ctx, uint32_t who) {
@@ -112,30 +114,25 @@ static __device__ __noinline__ bool paged_wait_timed(uint64_t* bar, uint32_t par
 
 // A unit is one tile of 128 keys of one (sequence, K/V head, block of rows); a sequence without keys has one empty tile per
 // head, so that its rows are written.  Units are ordered by sequence, head, row block, tile.
+// (The host refuses calls whose list could be longer than 32 bits can count.)
 __host__ __device__ inline int paged_tiles(int len) { return len > 0 ? (len + kTileN - 1) / kTileN : 1; }
-__host__ __device__ inline long long paged_units(const PagedParams& p, int b) {
-    return static_cast<long long>(paged_tiles(clamped_len(p.seq_lens[b], p.max_pages, p.page_size, nullptr))) * p.Hkv * p.row_blocks;
+__host__ __device__ inline int paged_units(const PagedParams& p, int b) {
+    return paged_tiles(clamped_len(p.seq_lens[b], p.max_pages, p.page_size, nullptr)) * p.Hkv * p.row_blocks;
 }
-// a / b for non-negative numbers, nearly always of 32 bits
-__host__ __device__ inline long long paged_quot(long long a, long long b) {
-    return ((a | b) >> 32) == 0 ? static_cast<long long>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b)) : a / b;
-}
-__host__ __device__ inline long long paged_share(long long units, int ctas, int least) {
-    const long long per = paged_quot(units + ctas - 1, ctas);
+__host__ __device__ inline int paged_share(int units, int ctas, int least) {
+    const int per = static_cast<int>((static_cast<unsigned>(units) + ctas - 1) / ctas);
     return per < least ? least : per;
 }
 // First CTA of the (sequence, head, row block) whose units are [ua, ub), the number of CTAs that have a part of it, and the
 // partial-result slot of CTA c's part (a CTA leaves at most two parts unfinished: its first and its last).
-__host__ __device__ inline int paged_first_cta(long long ua, long long share) { return static_cast<int>(paged_quot(ua, share)); }
-__host__ __device__ inline int paged_pieces(long long ua, long long ub, long long share) {
-    return static_cast<int>(paged_quot(ub - 1, share) - paged_quot(ua, share)) + 1;
-}
-__host__ __device__ inline int paged_slot(int cta, long long ua, long long share) { return 2 * cta + (ua > cta * share ? 1 : 0); }
+__host__ __device__ inline int paged_first_cta(int ua, int share) { return ua / share; }
+__host__ __device__ inline int paged_pieces(int ua, int ub, int share) { return (ub - 1) / share - ua / share + 1; }
+__host__ __device__ inline int paged_slot(int cta, int ua, int share) { return 2 * cta + (ua > cta * share ? 1 : 0); }
 
 // Position in the unit list: the part [t0, t1) of the tiles of (b, hr), hr = K/V head * row_blocks + row block.
 struct PagedPart {
-    long long u, u1;              // next unit, end of the CTA's share
-    long long base;               // first unit of sequence b
+    int u, u1;                    // next unit, end of the CTA's share
+    int base;                     // first unit of sequence b
     int b, len, nt;
     int hr, t0, t1;
     bool report;
@@ -143,29 +140,28 @@ struct PagedPart {
         len = clamped_len(p.seq_lens[b], p.max_pages, p.page_size, report ? p.status : nullptr);
         nt = paged_tiles(len);
     }
-    __host__ __device__ void begin(const PagedParams& p, int b0, long long base0, long long first, long long end, bool rep) {
+    __host__ __device__ void begin(const PagedParams& p, int b0, int base0, int first, int end, bool rep) {
         u = first; u1 = end; b = b0; base = base0; report = rep;
         load_len(p);
-        set();
+        hr = (u - base) / nt;
+        t0 = u - base - hr * nt;
+        t1 = t0 + (u1 - u < nt - t0 ? u1 - u : nt - t0);
     }
-    __host__ __device__ void set() {
-        const long long local = u - base;
-        hr = static_cast<int>(paged_quot(local, nt));
-        t0 = static_cast<int>(local - static_cast<long long>(hr) * nt);
-        t1 = (u1 - u < nt - t0) ? t0 + static_cast<int>(u1 - u) : nt;
-    }
+    // (every part but a share's first begins with its row block's first tile)
     __host__ __device__ bool next(const PagedParams& p) {
         u += t1 - t0;
         if (u >= u1) return false;
-        if (t1 == nt && hr + 1 == p.Hkv * p.row_blocks) {
+        if (++hr == p.Hkv * p.row_blocks) {
+            hr = 0;
             base = u;
             ++b;
             load_len(p);
         }
-        set();
+        t0 = 0;
+        t1 = u1 - u < nt ? u1 - u : nt;
         return true;
     }
-    __host__ __device__ long long first_unit() const { return base + static_cast<long long>(hr) * nt; }     // of (b, hr)
+    __host__ __device__ int first_unit() const { return base + hr * nt; }     // of (b, hr)
 };
 
 // ------------------------------------------------------------------ configuration
@@ -178,7 +174,7 @@ struct PagedEntry {
     int pieces, first_cta;        // of the whole (sequence, head, block), and the slot of its first piece
     int first_slot;
 };
-constexpr int kPartRing = 8, kPartsAhead = 6;
+constexpr int kPartRing = 8, kPartsAhead = 6, kMergePieces = 8;
 
 // Registers per thread after the per-role reallocation (512 threads start with 128 each): 128 x 80 + 256 x 152 + 128 x 128 = 65536.
 constexpr int kPagedRegsOther = 80, kPagedRegsSoftmax = 152;
@@ -194,9 +190,8 @@ struct PagedShared {
     uint32_t tmem_base;
     PagedWait wait;
     uint32_t is_last;
-    int start_b;
-    long long start_base;
-    long long warp_sums[4];
+    int start_b, start_base;
+    int warp_sums[4];
     alignas(16) float c[2][kRows];                       // per query buffer: factor of a score (log2 units)
     int i[2][kRows];                                     // place among the new tokens
     // per group: bias - reference maximum, +inf where no key has been seen; and the same with 0 there
@@ -207,8 +202,8 @@ struct PagedShared {
     float stat_m[kPartRing][2][kMaps * kRows], stat_l[kPartRing][2][kMaps * kRows];      // [part][group]
     // of the result warps
     float factor[2][kMaps * kRows];
-    float out_m[kMaps * kRows], out_l[kMaps * kRows];
-    float weight[8][kMaps * kRows];
+    float out_l[kMaps * kRows];
+    float piece_m[kMergePieces][kMaps * kRows], piece_l[kMergePieces][kMaps * kRows];
     float sq[4][kRows];
     long long out_at[kRows];                             // offset of the row in O (-1: a padding row)
     int out_hq[kRows], out_i[kRows];
@@ -229,9 +224,9 @@ struct PagedCfg {
     static constexpr int kQRows = kTerms * kRows;               // rows of the staged queries
     static constexpr int kQChunkBytes = kQRows * 128;
     static constexpr int kQBytes = kKChunks * kQChunkBytes;
-    static constexpr int kPChunks = kE4m3 ? 1 : 2;              // 128 keys of 1 or 2 bytes in rows of 128
-    static constexpr int kPChunkBytes = kCols * 128;
-    static constexpr int kPBytes = kPChunks * kPChunkBytes;
+    // P^T as it is multiplied: columns of O^T in groups of 16 bytes, a group is the 128 keys' 16 bytes one after the other
+    static constexpr int kPGroupBytes = 128 * 16;
+    static constexpr int kPBytes = kCols * kElem / 16 * kPGroupBytes;
     // bf16 values of 64: the upper 64 lanes of O^T multiply a block of zeros
     static constexpr bool kZeroBlock = !kE4m3 && DV == 64;
     static constexpr int kZeroBytes = kZeroBlock ? 2048 : 0;
@@ -267,14 +262,16 @@ constexpr long long paged_slot_bytes(int dv, int states) { return states * (dv +
 
 // ------------------------------------------------------------------ kernel
 
-// Low word of a shared-memory matrix descriptor with 128-byte swizzle; the high word is the same for all (8-row groups 1024 bytes
-// apart, version 1).
+// Low word of a shared-memory matrix descriptor; the high word is the same for all operands with 128-byte swizzle (8-row groups
+// 1024 bytes apart, version 1).  P^T is not swizzled: blocks of 8 keys x 16 bytes, 128 bytes apart along the keys (the low
+// word's offset) and a group (128 keys) apart along the columns.
 FA_DEVI uint32_t desc_lo(uint32_t saddr, uint32_t lbo_bytes) { return ((saddr & 0x3ffffu) >> 4) | ((lbo_bytes >> 4) << 16); }
-template <bool kE4m3>
+template <bool kE4m3, bool kPlainB = false>
 FA_DEVI void paged_mma(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
     constexpr uint64_t kHi = static_cast<uint64_t>((1024u >> 4) | (1u << 14) | (2u << 29)) << 32;
-    if constexpr (kE4m3) ptx::mma_ss_f8(d, kHi | a_lo, kHi | b_lo, idesc, accumulate);
-    else ptx::mma_ss(d, kHi | a_lo, kHi | b_lo, idesc, accumulate);
+    constexpr uint64_t kHiB = kPlainB ? static_cast<uint64_t>((2048u >> 4) | (1u << 14)) << 32 : kHi;
+    if constexpr (kE4m3) ptx::mma_ss_f8(d, kHi | a_lo, kHiB | b_lo, idesc, accumulate);
+    else ptx::mma_ss(d, kHi | a_lo, kHiB | b_lo, idesc, accumulate);
 }
 
 template <int DQK, int DV, bool kE4m3, bool kDiff, int kRows>
@@ -459,10 +456,11 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         // ============================================================ value products, one thread
         setmaxnreg_dec<kPagedRegsOther>();
         if (elect_one()) {
-            constexpr uint32_t kIdescPV = kE4m3 ? (make_idesc_e4m3_f32(128, kCols, true, false) | (1u << 10))
-                                                : make_idesc_bf16_f32(128, kCols, true, false);
+            // (both operands with the product's dimension as the slow one)
+            constexpr uint32_t kIdescPV = kE4m3 ? (make_idesc_e4m3_f32(128, kCols, true, true) | (1u << 10))
+                                                : make_idesc_bf16_f32(128, kCols, true, true);
             constexpr int kStepKeys = 32 / Cfg::kElem, kStep16 = (kStepKeys * 128) >> 4;
-            const uint32_t v_lo0 = desc_lo(sV, Cfg::kZeroBlock ? 0 : kChunkBytes), p_lo0 = desc_lo(sP, 16);
+            const uint32_t v_lo0 = desc_lo(sV, Cfg::kZeroBlock ? 0 : kChunkBytes), p_lo0 = desc_lo(sP, 128);
             int n = 0, s = 0;
             uint32_t v_parity = 0;
             bool ok = true;
@@ -488,7 +486,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                         // (values of 64: the second 64 rows of V^T are read from a block of zeros, wherever this k-step is)
                         const uint32_t lo = v_lo + ks * kStep16;
                         const uint32_t lbo = Cfg::kZeroBlock ? (((sZero >> 4) - (lo & 0x3fffu)) << 16) : 0u;
-                        paged_mma<kE4m3>(d, lo + lbo, p_lo + (((ks / 4) * Cfg::kPChunkBytes + (ks % 4) * 32) >> 4), kIdescPV, ks > 0 ? 1u : acc);
+                        paged_mma<kE4m3, true>(d, lo + lbo, p_lo + ks * kStepKeys, kIdescPV, ks > 0 ? 1u : acc);
                     }
                     tc_commit(smem_addr(&sh.v_empty[s]));
                     tc_commit(smem_addr(&sh.pv_done[w][i]));
@@ -504,7 +502,6 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         setmaxnreg_inc<kPagedRegsSoftmax>();
         const int w = (warp >> 2) - 1, key = tid & 127, wq = warp & 3;
         const uint32_t lane_sel = static_cast<uint32_t>(wq * 32) << 16;
-        const uint32_t p_byte = kE4m3 ? key : (key & 63) * 2;            // of this key in a row of P
         int mine_n = 0;                                                  // tiles this group has done
         bool ok = true;
         for (int k = 0;; ++k) {
@@ -527,7 +524,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                     const int sb = mine_n % kBufs, pb = mine_n % kPBufs;
                     const bool first = t == t0 + skip;
                     const uint32_t tS = tmem + s_col(w, sb) + lane_sel;
-                    const uint32_t sPw = sP + (w * kPBufs + pb) * Cfg::kPBytes + (kE4m3 ? 0 : (key >> 6) * Cfg::kPChunkBytes);
+                    const uint32_t sPw = sP + (w * kPBufs + pb) * Cfg::kPBytes + key * 16;
                     ok = ok && paged_wait(sh.s_full[w][sb], (mine_n / kBufs) & 1, wait);
                     __syncwarp();
                     tc_fence_after_sync();
@@ -644,27 +641,36 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                     for (int r = 0; r < kStates; ++r) l[r] += x[r];
                     // the buffer's last reader: the product of the group's tile kPBufs before
                     if (mine_n >= kPBufs) ok = ok && paged_wait(sh.pv_done[w][pb], ((mine_n / kPBufs) & 1) ^ 1, wait);
-                    // P^T: row = column of O^T, 128 keys of 1 or 2 bytes, 16-byte pieces swizzled
+                    // P^T: 16 bytes of this key at a time (8 columns of bf16, 16 of e5m2)
                     if constexpr (kE4m3) {
 #pragma unroll
-                        for (int r = 0; r < kStates; r += 2) {
-                            __half2 h = __floats2half2_rn(x[r], x[r + 1]);
+                        for (int r = 0; r < kStates; r += 16) {
+                            uint32_t h[8];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                const __half2 two = __floats2half2_rn(x[r + 2 * j], x[r + 2 * j + 1]);
+                                h[j] = *reinterpret_cast<const uint32_t*>(&two);
+                            }
 #pragma unroll
                             for (int term = 0; term < 3; ++term) {
-                                uint32_t bits = *reinterpret_cast<uint32_t*>(&h) & 0xff00ff00u;
                                 const int col = (r / kRows * kTerms + term) * kRows + r % kRows;
-                                st_shared_u8(sPw + col * 128 + (p_byte ^ ((col & 7) << 4)), (bits >> 8) & 0xffu);
-                                st_shared_u8(sPw + (col + 1) * 128 + (p_byte ^ (((col + 1) & 7) << 4)), bits >> 24);
-                                h = __hsub2(h, *reinterpret_cast<__half2*>(&bits));
+                                st_shared_v4(sPw + col / 16 * Cfg::kPGroupBytes, __byte_perm(h[0], h[1], 0x7531), __byte_perm(h[2], h[3], 0x7531),
+                                             __byte_perm(h[4], h[5], 0x7531), __byte_perm(h[6], h[7], 0x7531));      // the top bytes
+                                if (term < 2) {
+#pragma unroll
+                                    for (int j = 0; j < 8; ++j) {
+                                        const uint32_t top = h[j] & 0xff00ff00u;
+                                        const __half2 rest = __hsub2(*reinterpret_cast<const __half2*>(&h[j]), *reinterpret_cast<const __half2*>(&top));
+                                        h[j] = *reinterpret_cast<const uint32_t*>(&rest);
+                                    }
+                                }
                             }
                         }
                     } else {
 #pragma unroll
-                        for (int r = 0; r < kStates; r += 2) {
-                            const uint32_t two = pack_bf16x2(x[r], x[r + 1]);
-                            st_shared_u16(sPw + r * 128 + (p_byte ^ ((r & 7) << 4)), two);
-                            st_shared_u16(sPw + (r + 1) * 128 + (p_byte ^ (((r + 1) & 7) << 4)), two >> 16);
-                        }
+                        for (int r = 0; r < kStates; r += 8)
+                            st_shared_v4(sPw + r / 8 * Cfg::kPGroupBytes, pack_bf16x2(x[r], x[r + 1]), pack_bf16x2(x[r + 2], x[r + 3]),
+                                         pack_bf16x2(x[r + 4], x[r + 5]), pack_bf16x2(x[r + 6], x[r + 7]));
                     }
                     constexpr int kStepKeys = 32 / Cfg::kElem;
                     const int keys = len - t * kTileN, steps_end = keys <= 0 ? kStepKeys : (keys + kStepKeys - 1) / kStepKeys * kStepKeys;
@@ -722,32 +728,31 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         // sequence that the CTA's share begins in
         const int chunk = (p.B + 127) / 128;
         const int b_first = key * chunk, b_last = min(p.B, b_first + chunk);
-        long long mine = 0;
+        int mine = 0;
 #pragma unroll 4
         for (int b = b_first; b < b_last; ++b) mine += paged_units(p, b);
-        long long before = mine;
+        int before = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-            const long long o = __shfl_up_sync(0xffffffffu, before, d);
+            const int o = __shfl_up_sync(0xffffffffu, before, d);
             if (lane >= d) before += o;
         }
         if (lane == 31) sh.warp_sums[wq] = before;
         before -= mine;
         named_barrier_sync(kBar, 128);
-        long long total = 0;
+        int total = 0;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-            const long long n = sh.warp_sums[v];
+            const int n = sh.warp_sums[v];
             if (v < wq) before += n;
             total += n;
         }
-        const long long share = paged_share(total, gridDim.x, p.least_units);
-        const long long u0 = blockIdx.x * share, u1 = min(total, u0 + share);
+        const int share = paged_share(total, gridDim.x, p.least_units);
+        const int u0 = min(total, static_cast<int>(blockIdx.x) * share), u1 = min(total, u0 + share);
         if (before <= u0 && u0 < before + mine) {
-            int b = b_first;
-            long long base = before;
+            int b = b_first, base = before;
             for (;; ++b) {
-                const long long n = paged_units(p, b);
+                const int n = paged_units(p, b);
                 if (u0 < base + n) break;
                 base += n;
             }
@@ -770,14 +775,14 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             if (lane == 0) {
                 PagedEntry& e = sh.part[at];
                 const bool whole = walk.t1 - walk.t0 == walk.nt;
-                const long long ua = walk.first_unit();
+                const int ua = walk.first_unit();
                 e.b = walk.b;
                 e.kvh = walk.hr / p.row_blocks;
                 e.rb = walk.hr - e.kvh * p.row_blocks;
                 e.len = walk.len;
                 e.t0 = walk.t0;
                 e.t1 = walk.u < walk.u1 ? walk.t1 : -1;
-                e.tile0 = static_cast<int>(walk.u - u0);
+                e.tile0 = walk.u - u0;
                 e.slot = whole ? -1 : paged_slot(blockIdx.x, ua, share);
                 e.pieces = whole ? 1 : paged_pieces(ua, ua + walk.nt, share);
                 e.first_cta = whole ? 0 : paged_first_cta(ua, share);
@@ -985,9 +990,10 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
 #pragma unroll
                     for (int r = 0; r < kStates; ++r) slot_o[r * DV + key] = y[r];
                 }
-                __threadfence();
                 named_barrier_sync(kBar, 128);
                 if (key == 0) {
+                    // (the fence covers the stores of all threads of the group: the barrier orders them before it)
+                    __threadfence();
                     const bool last = atomicAdd(p.arrivals + e.first_cta, 1u) == static_cast<unsigned int>(e.pieces - 1);
                     sh.is_last = last ? 1u : 0u;
                     if (last) p.arrivals[e.first_cta] = 0u;
@@ -996,44 +1002,70 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                 named_barrier_sync(kBar, 128);
                 final_rows = sh.is_last != 0;
                 if (final_rows) {
-                    // this CTA finished last: all pieces, in the order of the CTAs
-                    __threadfence();
-                    // (the other pieces are the first parts of their CTAs)
+                    // This CTA finished last: all pieces, in the order of the CTAs, kMergePieces at a time under a running maximum, all
+                    // loads of a round in flight together.  (The pieces behind the first are the first parts of their CTAs.)
                     auto piece = [&](int c) {
                         return p.part + (c == 0 ? e.first_slot : 2ll * (e.first_cta + c)) * kStates * (DV + 2);
                     };
-                    if (key < kStates) {
-                        float m = -INFINITY, sum = 0.f;
-                        for (int c = 0; c < e.pieces; ++c) m = fmaxf(m, __ldcg(piece(c) + kStates * DV + key));
-                        for (int c = 0; c < e.pieces; ++c) {
-                            const float mc = __ldcg(piece(c) + kStates * DV + key);
-                            // (a piece without a finite score counts nothing, but a NaN of its sum goes through)
-                            sum += (mc == -INFINITY ? 0.f : exp2_approx(mc - m)) * __ldcg(piece(c) + kStates * DV + kStates + key);
-                        }
-                        store_lse(key % kRows, m, sum);
-                        sh.out_m[key] = m;
-                        sh.out_l[key] = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
-                    }
+                    float run_m = -INFINITY, run_l = 0.f;
 #pragma unroll
                     for (int r = 0; r < kStates; ++r) y[r] = 0.f;
-                    for (int c0 = 0; c0 < e.pieces; c0 += 8) {
-                        const int nc = min(8, e.pieces - c0);
-                        named_barrier_sync(kBar, 128);
+#pragma unroll 1
+                    for (int c0 = 0; c0 < e.pieces; c0 += kMergePieces) {
+                        const int nc = min(kMergePieces, e.pieces - c0);
                         for (int j = key; j < nc * kStates; j += 128) {
-                            const int c = j / kStates, r = j % kStates;
-                            const float mc = __ldcg(piece(c0 + c) + kStates * DV + r);
-                            sh.weight[c][r] = mc == -INFINITY ? 0.f : exp2_approx(mc - sh.out_m[r]) * sh.out_l[r];
+                            const float* ml = piece(c0 + j / kStates) + kStates * DV + j % kStates;
+                            sh.piece_m[j / kStates][j % kStates] = __ldcg(ml);
+                            sh.piece_l[j / kStates][j % kStates] = __ldcg(ml + kStates);
                         }
                         named_barrier_sync(kBar, 128);
-                        if (key < DV) {
-#pragma unroll 2
+                        if (key < kStates) {
+                            float m = run_m;
+                            for (int c = 0; c < nc; ++c) m = fmaxf(m, sh.piece_m[c][key]);
+                            const float keep = run_m == -INFINITY ? 0.f : exp2_approx(run_m - m);
+                            float sum = run_l * keep;
                             for (int c = 0; c < nc; ++c) {
-                                const float* po = piece(c0 + c) + key;
+                                const float mc = sh.piece_m[c][key];
+                                const float f = mc == -INFINITY ? 0.f : exp2_approx(mc - m);
+                                // (a piece without a finite score counts nothing, but a NaN of its sum goes through)
+                                sum += f * sh.piece_l[c][key];
+                                sh.piece_m[c][key] = f;
+                            }
+                            sh.out_l[key] = keep;
+                            run_m = m;
+                            run_l = sum;
+                        }
+                        named_barrier_sync(kBar, 128);
 #pragma unroll
-                                for (int r = 0; r < kStates; ++r) y[r] = fmaf(sh.weight[c][r], __ldcg(po + r * DV), y[r]);
+                        for (int r = 0; r < kStates; ++r) y[r] *= sh.out_l[r];
+                        if (key < DV) {
+                            constexpr int kBatch = kStates <= 16 ? 4 : (kStates <= 32 ? 2 : 1);
+#pragma unroll 1
+                            for (int c = 0; c < nc; c += kBatch) {
+                                float v[kBatch][kStates];
+#pragma unroll
+                                for (int q = 0; q < kBatch; ++q) {
+                                    const float* po = piece(c0 + min(c + q, nc - 1)) + key;
+#pragma unroll
+                                    for (int r = 0; r < kStates; ++r) v[q][r] = __ldcg(po + r * DV);
+                                }
+#pragma unroll
+                                for (int q = 0; q < kBatch; ++q) {
+                                    if (c + q >= nc) break;
+#pragma unroll
+                                    for (int r = 0; r < kStates; ++r) y[r] = fmaf(sh.piece_m[c + q][r], v[q][r], y[r]);
+                                }
                             }
                         }
+                        named_barrier_sync(kBar, 128);
                     }
+                    if (key < kStates) {
+                        store_lse(key % kRows, run_m, run_l);
+                        sh.out_l[key] = run_l > 0.f || run_l != run_l ? 1.f / run_l : 0.f;
+                    }
+                    named_barrier_sync(kBar, 128);
+#pragma unroll
+                    for (int r = 0; r < kStates; ++r) y[r] *= sh.out_l[r];
                 }
             }
             if (final_rows) store_rows();
