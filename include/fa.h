@@ -501,16 +501,16 @@ fa_status fa_forward_paged(fa_handle* h, const fa_paged_cache* cache, const fa_p
                            const int64_t* q_strides, const int64_t* o_strides, void* stream);
 
 /*
- * How fa_forward_paged would deal out a batch, the counterpart of fa_plan: a pure host function that runs the kernel's own walk
- * over the list of work units (one unit = 128 keys of one sequence, K/V head and block of query rows).  seqs->seq_lens is a HOST array
- * here, block_table and the cache's pointers and strides are not looked at.  `pieces` receives up to max_pieces entries, in
- * the order of the CTAs; out->pieces is their number in any case.
+ * How fa_forward_paged would deal out a batch, the counterpart of fa_plan: a pure host function that makes the kernel's own list
+ * of work units (one unit = 128 keys of one sequence, K/V head and block of query rows, and part_cost units for each such
+ * block).  seqs->seq_lens is a HOST array here, block_table and the cache's pointers and strides are not looked at.  `pieces`
+ * receives up to max_pieces entries, in the order of the CTAs; out->pieces is their number in any case.
  */
 typedef struct fa_paged_plan_info {
     int32_t rows_per_block;       /* query rows that share a pass over the keys (16, 32 or 64)   */
     int32_t row_blocks;           /* blocks that a K/V head's (Hq / Hkv) * Sq rows are cut into   */
     int32_t ctas;                 /* grid size                                                    */
-    int32_t reserved;
+    int32_t part_cost;            /* units that a row block takes in the list beside its tiles    */
     int64_t units, units_per_cta, pieces;
 } fa_paged_plan_info;
 typedef struct fa_paged_piece {

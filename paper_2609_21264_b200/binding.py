@@ -78,7 +78,7 @@ class fa_diff(ctypes.Structure):
 
 
 class fa_paged_plan_info(ctypes.Structure):
-    _fields_ = [("rows_per_block", ctypes.c_int32), ("row_blocks", ctypes.c_int32), ("ctas", ctypes.c_int32), ("reserved", ctypes.c_int32),
+    _fields_ = [("rows_per_block", ctypes.c_int32), ("row_blocks", ctypes.c_int32), ("ctas", ctypes.c_int32), ("part_cost", ctypes.c_int32),
                 ("units", ctypes.c_int64), ("units_per_cta", ctypes.c_int64), ("pieces", ctypes.c_int64)]
 
 

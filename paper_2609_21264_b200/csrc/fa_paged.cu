@@ -105,7 +105,7 @@ int rows_per_block(int rows, int dqk, bool e4m3, bool diff) {
 // Tiles of 128 keys that a call's list of work can have at most; the kernel counts them in 32 bits.
 long long most_units(const fa::PagedParams& p) {
     return static_cast<long long>(p.B) * p.Hkv * p.row_blocks *
-           fa::paged_tiles(static_cast<int>(static_cast<long long>(p.max_pages) * p.page_size));
+           (fa::paged_tiles(static_cast<int>(static_cast<long long>(p.max_pages) * p.page_size)) + fa::kPartCost);
 }
 
 // CTAs of a launch: one per SM, as many as there can be units, and as many as the scratch has two partial results for.
@@ -362,38 +362,38 @@ fa_status fa_plan_paged(int num_sms, const fa_config* cfg, const fa_paged_cache*
     const int ctas = paged_ctas(num_sms, static_cast<size_t>(scratch), p, cache->dv, (diff ? 2 : 1) * block);
     if (ctas < 1) return FA_ERR_UNSUPPORTED;
     int total = 0;
-    for (int b = 0; b < p.B; ++b) total += fa::paged_units(p, b);
+    for (int b = 0; b < p.B; ++b) total += fa::paged_units(p, fa::paged_len(p, b, nullptr));
     const int share = fa::paged_share(total, ctas, p.least_units);
     out->rows_per_block = block;
     out->row_blocks = p.row_blocks;
     out->ctas = ctas;
+    out->part_cost = fa::kPartCost;
     out->units = total;
     out->units_per_cta = share;
-    // the walk of every CTA, as the kernel makes it
     long long n = 0;
-    int b = 0, base = 0;
-    for (int c = 0; c < ctas && c * share < total; ++c) {
-        const int u0 = c * share, u1 = u0 + share < total ? u0 + share : total;
-        while (u0 >= base + fa::paged_units(p, b)) base += fa::paged_units(p, b++);
-        fa::PagedPart part;
-        part.begin(p, b, base, u0, u1, false);
-        do {
-            if (n < max_pieces) {
-                const bool whole = part.t1 - part.t0 == part.nt;
-                const int ua = part.first_unit();
-                fa_paged_piece* x = pieces + n;
-                x->cta = c;
-                x->sequence = part.b;
-                x->kv_head = part.hr / p.row_blocks;
-                x->row_block = part.hr % p.row_blocks;
-                x->first_tile = part.t0;
-                x->end_tile = part.t1;
-                x->slot = whole ? -1 : fa::paged_slot(c, ua, share);
-                x->pieces = whole ? 1 : fa::paged_pieces(ua, ua + part.nt, share);
-                x->first_cta = whole ? c : fa::paged_first_cta(ua, share);
+    int b0 = 0, base0 = 0;             // the sequence that the CTA's share begins in, and its first unit
+    for (int c = 0; c < ctas && static_cast<long long>(c) * share < total; ++c) {
+        const int u0 = c * share, u1 = total - u0 < share ? total : u0 + share;
+        while (u0 >= base0 + fa::paged_units(p, fa::paged_len(p, b0, nullptr))) base0 += fa::paged_units(p, fa::paged_len(p, b0++, nullptr));
+        for (int b = b0, base = base0; b < p.B && base < u1; base += fa::paged_units(p, fa::paged_len(p, b, nullptr)), ++b) {
+            for (int hr = 0; hr < p.Hkv * p.row_blocks; ++hr) {
+                fa::PagedEntry e;
+                if (!fa::paged_entry(p, c, share, u0, u1, b, base, fa::paged_len(p, b, nullptr), hr, e)) continue;
+                if (n < max_pieces) {
+                    fa_paged_piece* x = pieces + n;
+                    x->cta = c;
+                    x->sequence = e.b;
+                    x->kv_head = e.kvh;
+                    x->row_block = e.rb;
+                    x->first_tile = e.t0;
+                    x->end_tile = e.t1;
+                    x->slot = e.slot;
+                    x->pieces = e.pieces;
+                    x->first_cta = e.first_cta;
+                }
+                ++n;
             }
-            ++n;
-        } while (part.next(p));
+        }
     }
     out->pieces = n;
     return FA_OK;

@@ -112,59 +112,22 @@ static __device__ __noinline__ bool paged_wait_timed(uint64_t* bar, uint32_t par
 
 // ------------------------------------------------------------------ the list of work units and its shares
 
-// A unit is one tile of 128 keys of one (sequence, K/V head, block of rows); a sequence without keys has one empty tile per
-// head, so that its rows are written.  Units are ordered by sequence, head, row block, tile.
+// The list holds every (sequence, K/V head, block of rows) in that order, each as kPartCost units for what a part costs beside its
+// tiles (query rows, first maxima, result) and one unit per tile of 128 keys; a sequence without keys has one empty tile, so that
+// its rows are written.  CTA c takes units [c * share, (c + 1) * share).  Without the extra unit the CTAs that got the batch's
+// short sequences finished last (64 sequences of 65 to 4096 keys: FILL_A us, against FILL_B).
 // (The host refuses calls whose list could be longer than 32 bits can count.)
+constexpr int kPartCost = 1;
 __host__ __device__ inline int paged_tiles(int len) { return len > 0 ? (len + kTileN - 1) / kTileN : 1; }
-__host__ __device__ inline int paged_units(const PagedParams& p, int b) {
-    return paged_tiles(clamped_len(p.seq_lens[b], p.max_pages, p.page_size, nullptr)) * p.Hkv * p.row_blocks;
+__host__ __device__ inline int paged_len(const PagedParams& p, int b, uint32_t* status) {
+    return clamped_len(p.seq_lens[b], p.max_pages, p.page_size, status);
 }
+// Units of a sequence, from its length.
+__host__ __device__ inline int paged_units(const PagedParams& p, int len) { return (paged_tiles(len) + kPartCost) * p.Hkv * p.row_blocks; }
 __host__ __device__ inline int paged_share(int units, int ctas, int least) {
     const int per = static_cast<int>((static_cast<unsigned>(units) + ctas - 1) / ctas);
     return per < least ? least : per;
 }
-// First CTA of the (sequence, head, row block) whose units are [ua, ub), the number of CTAs that have a part of it, and the
-// partial-result slot of CTA c's part (a CTA leaves at most two parts unfinished: its first and its last).
-__host__ __device__ inline int paged_first_cta(int ua, int share) { return ua / share; }
-__host__ __device__ inline int paged_pieces(int ua, int ub, int share) { return (ub - 1) / share - ua / share + 1; }
-__host__ __device__ inline int paged_slot(int cta, int ua, int share) { return 2 * cta + (ua > cta * share ? 1 : 0); }
-
-// Position in the unit list: the part [t0, t1) of the tiles of (b, hr), hr = K/V head * row_blocks + row block.
-struct PagedPart {
-    int u, u1;                    // next unit, end of the CTA's share
-    int base;                     // first unit of sequence b
-    int b, len, nt;
-    int hr, t0, t1;
-    bool report;
-    __host__ __device__ void load_len(const PagedParams& p) {
-        len = clamped_len(p.seq_lens[b], p.max_pages, p.page_size, report ? p.status : nullptr);
-        nt = paged_tiles(len);
-    }
-    __host__ __device__ void begin(const PagedParams& p, int b0, int base0, int first, int end, bool rep) {
-        u = first; u1 = end; b = b0; base = base0; report = rep;
-        load_len(p);
-        hr = (u - base) / nt;
-        t0 = u - base - hr * nt;
-        t1 = t0 + (u1 - u < nt - t0 ? u1 - u : nt - t0);
-    }
-    // (every part but a share's first begins with its row block's first tile)
-    __host__ __device__ bool next(const PagedParams& p) {
-        u += t1 - t0;
-        if (u >= u1) return false;
-        if (++hr == p.Hkv * p.row_blocks) {
-            hr = 0;
-            base = u;
-            ++b;
-            load_len(p);
-        }
-        t0 = 0;
-        t1 = u1 - u < nt ? u1 - u : nt;
-        return true;
-    }
-    __host__ __device__ int first_unit() const { return base + hr * nt; }     // of (b, hr)
-};
-
-// ------------------------------------------------------------------ configuration
 
 // A part of the list as the roles of a CTA see it: tiles [t0, t1) of one (sequence, K/V head, row block).
 struct PagedEntry {
@@ -174,7 +137,35 @@ struct PagedEntry {
     int pieces, first_cta;        // of the whole (sequence, head, block), and the slot of its first piece
     int first_slot;
 };
-constexpr int kPartRing = 8, kPartsAhead = 6, kMergePieces = 8;
+
+// What CTA `cta` with units [u0, u1) has of row block hr = head * row_blocks + block of sequence b, whose first unit is `base`;
+// false where that is nothing.  A CTA leaves at most two parts unfinished, its first and its last: two slots for partial results.
+__host__ __device__ inline bool paged_entry(const PagedParams& p, int cta, int share, int u0, int u1, int b, int base, int len, int hr,
+                                            PagedEntry& e) {
+    const int nt = paged_tiles(len), ua = base + hr * (nt + kPartCost) + kPartCost, ub = ua + nt;       // units of its tiles
+    const int v0 = u0 > ua ? u0 : ua, v1 = u1 < ub ? u1 : ub;
+    e.b = b;
+    e.kvh = hr / p.row_blocks;
+    e.rb = hr - e.kvh * p.row_blocks;
+    e.len = len;
+    e.t0 = v0 - ua;
+    e.t1 = v1 - ua;
+    e.slot = -1;
+    e.pieces = 1;
+    e.first_cta = cta;
+    e.first_slot = -1;
+    if (v1 - v0 < nt) {
+        e.first_cta = ua / share;
+        e.pieces = (ub - 1) / share - e.first_cta + 1;
+        e.first_slot = 2 * e.first_cta + (ua > e.first_cta * share ? 1 : 0);
+        e.slot = 2 * cta + (ua > u0 ? 1 : 0);
+    }
+    return v0 < v1;
+}
+
+// ------------------------------------------------------------------ configuration
+
+constexpr int kPartRing = 8, kMergePieces = 8;
 
 // Registers per thread after the per-role reallocation (512 threads start with 128 each): 128 x 80 + 256 x 152 + 128 x 128 = 65536.
 constexpr int kPagedRegsOther = 80, kPagedRegsSoftmax = 152;
@@ -185,7 +176,7 @@ struct PagedShared {
     uint64_t q_full[2], q_empty[2];
     uint64_t s_full[2][2], s_empty[2][2], p_full[2][2], pv_done[2][2];      // [group][buffer]
     uint64_t acc_full[2], acc_empty[2];                      // [accumulator buffer]
-    uint64_t part_full[kPartRing], part_empty[kPartRing], stat_full[kPartRing];
+    uint64_t part_full[kPartRing], stat_full[kPartRing];
     PagedEntry part[kPartRing];
     uint32_t tmem_base;
     PagedWait wait;
@@ -326,7 +317,6 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         }
         for (int i = 0; i < kPartRing; ++i) {
             mbar_init(smem_addr(&sh.part_full[i]), 1);
-            mbar_init(smem_addr(&sh.part_empty[i]), 1);
             mbar_init(smem_addr(&sh.stat_full[i]), 8);          // the softmax warps
         }
         fence_mbar_init();
@@ -730,7 +720,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         const int b_first = key * chunk, b_last = min(p.B, b_first + chunk);
         int mine = 0;
 #pragma unroll 4
-        for (int b = b_first; b < b_last; ++b) mine += paged_units(p, b);
+        for (int b = b_first; b < b_last; ++b) mine += paged_units(p, paged_len(p, b, nullptr));
         int before = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -752,7 +742,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         if (before <= u0 && u0 < before + mine) {
             int b = b_first, base = before;
             for (;; ++b) {
-                const int n = paged_units(p, b);
+                const int n = paged_units(p, paged_len(p, b, nullptr));
                 if (u0 < base + n) break;
                 base += n;
             }
@@ -760,39 +750,59 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             sh.start_base = base;
         }
         named_barrier_sync(kBar, 128);
-        // the list, published by the group's last warp, kPartsAhead parts ahead of the results; a CTA without a share has the end
-        // mark alone
-        PagedPart walk;
-        bool ended = false;
-        int published = 0;
-        if (wq == 3 && u0 < total) walk.begin(p, sh.start_b, sh.start_base, u0, u1, lane == 0);
-        else walk = PagedPart{u1, u1, u1, 0, 0, 1, 0, 0, 0, false};
-        auto publish = [&]() {                     // uniform over the warp
-            if (ended || wq != 3) return;
-            const int at = published % kPartRing;
-            ok = __all_sync(0xffffffffu, ok && paged_wait_timed(&sh.part_empty[at], ((published / kPartRing) & 1) ^ 1, wait, kSiteItem));
-            if (!ok) return;
-            if (lane == 0) {
-                PagedEntry& e = sh.part[at];
-                const bool whole = walk.t1 - walk.t0 == walk.nt;
-                const int ua = walk.first_unit();
-                e.b = walk.b;
-                e.kvh = walk.hr / p.row_blocks;
-                e.rb = walk.hr - e.kvh * p.row_blocks;
-                e.len = walk.len;
-                e.t0 = walk.t0;
-                e.t1 = walk.u < walk.u1 ? walk.t1 : -1;
-                e.tile0 = walk.u - u0;
-                e.slot = whole ? -1 : paged_slot(blockIdx.x, ua, share);
-                e.pieces = whole ? 1 : paged_pieces(ua, ua + walk.nt, share);
-                e.first_cta = whole ? 0 : paged_first_cta(ua, share);
-                e.first_slot = whole ? -1 : paged_slot(e.first_cta, ua, share);
-                mbar_arrive(smem_addr(&sh.part_full[at]));
+        // The list, published by the group's last warp, a lane per row block of the sequence: every entry that is free when the
+        // results of part k begin (those of the parts before have been stored).  A CTA without a share has the end mark alone.
+        const int blocks = p.Hkv * p.row_blocks;
+        int seq = 0, base = 0, len = 0, hr = 0, published = 0, tiles = 0;
+        bool ended = u0 >= total, marked = false;
+        if (wq == 3 && !ended) {
+            seq = sh.start_b;
+            base = sh.start_base;
+            len = paged_len(p, seq, lane == 0 ? p.status : nullptr);
+            hr = (u0 - base) / (paged_tiles(len) + kPartCost);
+        }
+        auto publish = [&](int k) {
+            while (!ended && published < k + kPartRing) {
+                const int nt = paged_tiles(len);
+                PagedEntry e;
+                const bool some = hr + lane < blocks && paged_entry(p, blockIdx.x, share, u0, u1, seq, base, len, hr + lane, e);
+                const uint32_t have = __ballot_sync(0xffffffffu, some);
+                const int count = min(__popc(have), k + kPartRing - published);
+                // tiles of the parts before this lane's: the first part of a share may lack some, the others here have them all
+                const int first_tiles = __shfl_sync(0xffffffffu, e.t1 - e.t0, 0);
+                if (lane < count) {
+                    e.tile0 = tiles + (lane > 0 ? first_tiles + (lane - 1) * nt : 0);
+                    const int at = (published + lane) % kPartRing;
+                    sh.part[at] = e;
+                    mbar_arrive(smem_addr(&sh.part_full[at]));
+                }
+                const int last_tiles = __shfl_sync(0xffffffffu, e.t1 - e.t0, max(0, count - 1));
+                if (count > 0) tiles += last_tiles + (count > 1 ? first_tiles + (count - 2) * nt : 0);
+                published += count;
+                hr += count;
+                if (count == __popc(have)) {
+                    if (hr < blocks) {
+                        ended = true;                  // the share ends inside this sequence
+                    } else {
+                        base += blocks * (nt + kPartCost);
+                        hr = 0;
+                        if (base + kPartCost < u1) {
+                            ++seq;
+                            len = paged_len(p, seq, lane == 0 ? p.status : nullptr);
+                        } else {
+                            ended = true;
+                        }
+                    }
+                }
             }
-            __syncwarp();
-            ++published;
-            if (walk.u >= walk.u1) ended = true;   // that was the end mark
-            else walk.next(p);
+            if (ended && !marked && published < k + kPartRing) {
+                if (lane == 0) {
+                    sh.part[published % kPartRing].t1 = -1;
+                    mbar_arrive(smem_addr(&sh.part_full[published % kPartRing]));
+                }
+                marked = true;
+                ++published;
+            }
         };
         // the query rows of a part into buffer k & 1 (before k = 2: free; later: the part two before has ended)
         constexpr int kVecs = DQK / 8;                        // 16-byte pieces of a row
@@ -870,20 +880,17 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_addr(&sh.q_full[qb]));
         };
-        // Rounds -2 and -1 stage the rows of parts 0 and 1; round k those of part k + 2 as soon as part k has ended (they are loaded
-        // before that), and then part k's results.
+        // Round k stages the query rows of part k + 2 as soon as part k has ended, loads those of part k + 3, and brings out part k's
+        // results; rounds -3 to -1 begin this.
         int end_at = 0x7fffffff;                   // the end mark's place, once seen
-        for (int k = -2; k < end_at; ++k) {
-#pragma unroll 1
-            for (int i = k == -2 ? kPartsAhead : 1; i > 0; --i) publish();
-            if (k + 2 < end_at) ok = ok && wait_part_timed(k + 2);
-            if (named_barrier_or(kBar, 128, !ok)) break;
-            if (k + 2 < end_at && sh.part[(k + 2) % kPartRing].t1 < 0) end_at = k + 2;
-            const bool stage = k + 2 < end_at;
-            if (stage) load_queries(k + 2);
+        for (int k = -3; k < end_at; ++k) {
+            if (wq == 3 && !marked && published < max(k, 0) + kPartRing - 3) publish(max(k, 0));
+            if (k + 3 < end_at) ok = ok && wait_part_timed(k + 3);
             if (k >= 0) ok = ok && paged_wait_timed(&sh.stat_full[k % kPartRing], (k / kPartRing) & 1, wait, kSiteEpiState);
-            __syncwarp();
-            if (stage) store_queries(k + 2);
+            if (named_barrier_or(kBar, 128, !ok)) break;
+            if (k > -3 && k + 2 < end_at) store_queries(k + 2);
+            if (k + 3 < end_at && sh.part[(k + 3) % kPartRing].t1 < 0) end_at = k + 3;
+            if (k + 3 < end_at) load_queries(k + 3);
             if (k < 0) continue;
             const PagedEntry e = sh.part[k % kPartRing];
             const int ob = k % kOBufs;
@@ -906,6 +913,15 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             named_barrier_sync(kBar, 128);
             // (uniform) whether a group had a tile of this part
             const bool had[2] = {e.t1 - e.t0 > 1 || (e.tile0 & 1) == 0, e.t1 - e.t0 > 1 || (e.tile0 & 1) == 1};
+            if (key == 0 && !whole) {
+                // all other pieces there already: no need to announce this one
+                const unsigned int got = *static_cast<volatile unsigned int*>(p.arrivals + e.first_cta);
+                sh.is_last = got == static_cast<unsigned int>(e.pieces - 1) ? 1u : 0u;
+                if (sh.is_last) {
+                    __threadfence();
+                    p.arrivals[e.first_cta] = 0u;
+                }
+            }
             if (key < kStates) {
                 float f[2], sum[2], mx[2];
 #pragma unroll
@@ -991,7 +1007,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                     for (int r = 0; r < kStates; ++r) slot_o[r * DV + key] = y[r];
                 }
                 named_barrier_sync(kBar, 128);
-                if (key == 0) {
+                if (key == 0 && !sh.is_last) {
                     // (the fence covers the stores of all threads of the group: the barrier orders them before it)
                     __threadfence();
                     const bool last = atomicAdd(p.arrivals + e.first_cta, 1u) == static_cast<unsigned int>(e.pieces - 1);
@@ -1069,8 +1085,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                 }
             }
             if (final_rows) store_rows();
-            named_barrier_sync(kBar, 128);
-            if (key == 0) mbar_arrive(smem_addr(&sh.part_empty[k % kPartRing]));
+            // (the barrier that the next round begins with comes before anything of this round's is overwritten)
         }
     }
 
