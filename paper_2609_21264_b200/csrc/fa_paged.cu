@@ -18,7 +18,10 @@ namespace {
 
 using namespace fa_host;
 
-constexpr int kLeastUnits = 1;      // tiles of 128 keys that a CTA of the streaming kernel takes at least
+// Units of 128 keys that a CTA of the streaming kernel takes at least: two softmax groups work on two tiles at once, and every piece of
+// a row block more is one more to join (2000 keys, 8 K/V heads: 14.8 us, against 17.9 with one; 14.6 with four, but 100 to
+// 400 keys lose 1.5 us there).
+constexpr int kLeastUnits = 2;
 
 bool head_sizes_ok(int dqk, int dv) {
     return (dqk == 64 && dv == 64) || (dqk == 128 && dv == 128) || (dqk == 192 && dv == 128);
@@ -361,9 +364,12 @@ fa_status fa_plan_paged(int num_sms, const fa_config* cfg, const fa_paged_cache*
     if (most_units(p) > 0x7fff0000LL) return FA_ERR_UNSUPPORTED;
     const int ctas = paged_ctas(num_sms, static_cast<size_t>(scratch), p, cache->dv, (diff ? 2 : 1) * block);
     if (ctas < 1) return FA_ERR_UNSUPPORTED;
-    int total = 0;
-    for (int b = 0; b < p.B; ++b) total += fa::paged_units(p, fa::paged_len(p, b, nullptr));
-    const int share = fa::paged_share(total, ctas, p.least_units);
+    int longest = 0, total = 0;
+    for (int b = 0; b < p.B; ++b) longest = fa::paged_len(p, b, nullptr) > longest ? fa::paged_len(p, b, nullptr) : longest;
+    const int pad = fa::paged_pad(p, ctas, fa::paged_tiles(longest));
+    auto units_of = [&](int b) { return fa::paged_units(p, fa::paged_len(p, b, nullptr), pad); };
+    for (int b = 0; b < p.B; ++b) total += units_of(b);
+    const int share = fa::paged_share(total, ctas, p.least_units, pad);
     out->rows_per_block = block;
     out->row_blocks = p.row_blocks;
     out->ctas = ctas;
@@ -374,11 +380,11 @@ fa_status fa_plan_paged(int num_sms, const fa_config* cfg, const fa_paged_cache*
     int b0 = 0, base0 = 0;             // the sequence that the CTA's share begins in, and its first unit
     for (int c = 0; c < ctas && static_cast<long long>(c) * share < total; ++c) {
         const int u0 = c * share, u1 = total - u0 < share ? total : u0 + share;
-        while (u0 >= base0 + fa::paged_units(p, fa::paged_len(p, b0, nullptr))) base0 += fa::paged_units(p, fa::paged_len(p, b0++, nullptr));
-        for (int b = b0, base = base0; b < p.B && base < u1; base += fa::paged_units(p, fa::paged_len(p, b, nullptr)), ++b) {
+        while (u0 >= base0 + units_of(b0)) base0 += units_of(b0++);
+        for (int b = b0, base = base0; b < p.B && base < u1; base += units_of(b), ++b) {
             for (int hr = 0; hr < p.Hkv * p.row_blocks; ++hr) {
                 fa::PagedEntry e;
-                if (!fa::paged_entry(p, c, share, u0, u1, b, base, fa::paged_len(p, b, nullptr), hr, e)) continue;
+                if (!fa::paged_entry(p, c, share, u0, u1, b, base, fa::paged_len(p, b, nullptr), pad, hr, e)) continue;
                 if (n < max_pieces) {
                     fa_paged_piece* x = pieces + n;
                     x->cta = c;

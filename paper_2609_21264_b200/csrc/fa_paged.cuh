@@ -117,14 +117,26 @@ static __device__ __noinline__ bool paged_wait_timed(uint64_t* bar, uint32_t par
 // its rows are written.  CTA c takes units [c * share, (c + 1) * share).  Without the extra unit the CTAs that got the batch's
 // short sequences finished last (64 sequences of 65 to 4096 keys: FILL_A us, against FILL_B).
 // (The host refuses calls whose list could be longer than 32 bits can count.)
-constexpr int kPartCost = 1;
+//
+// Small calls: joining the pieces of a row block costs 4 to 5 us, a tile 0.6 us of a CTA's time.  So where there is a CTA for every row
+// block and no sequence has more than kWholeTiles tiles, all blocks count as many units as the longest (`pad` tiles), the shares
+// fall on their borders, and nothing is split (400 keys, 8 K/V heads: FILL_C us, against FILL_D).
+constexpr int kPartCost = 1, kWholeTiles = 6;
 __host__ __device__ inline int paged_tiles(int len) { return len > 0 ? (len + kTileN - 1) / kTileN : 1; }
 __host__ __device__ inline int paged_len(const PagedParams& p, int b, uint32_t* status) {
     return clamped_len(p.seq_lens[b], p.max_pages, p.page_size, status);
 }
-// Units of a sequence, from its length.
-__host__ __device__ inline int paged_units(const PagedParams& p, int len) { return (paged_tiles(len) + kPartCost) * p.Hkv * p.row_blocks; }
-__host__ __device__ inline int paged_share(int units, int ctas, int least) {
+__host__ __device__ inline int paged_pad(const PagedParams& p, int ctas, int most_tiles) {
+    return most_tiles <= kWholeTiles && static_cast<long long>(p.B) * p.Hkv * p.row_blocks <= ctas ? most_tiles : 0;
+}
+// Units of a row block, and of a sequence, from its length.
+__host__ __device__ inline int paged_block_units(int len, int pad) {
+    const int nt = paged_tiles(len);
+    return (nt < pad ? pad : nt) + kPartCost;
+}
+__host__ __device__ inline int paged_units(const PagedParams& p, int len, int pad) { return paged_block_units(len, pad) * p.Hkv * p.row_blocks; }
+__host__ __device__ inline int paged_share(int units, int ctas, int least, int pad) {
+    if (pad > 0) return pad + kPartCost;
     const int per = static_cast<int>((static_cast<unsigned>(units) + ctas - 1) / ctas);
     return per < least ? least : per;
 }
@@ -140,9 +152,9 @@ struct PagedEntry {
 
 // What CTA `cta` with units [u0, u1) has of row block hr = head * row_blocks + block of sequence b, whose first unit is `base`;
 // false where that is nothing.  A CTA leaves at most two parts unfinished, its first and its last: two slots for partial results.
-__host__ __device__ inline bool paged_entry(const PagedParams& p, int cta, int share, int u0, int u1, int b, int base, int len, int hr,
+__host__ __device__ inline bool paged_entry(const PagedParams& p, int cta, int share, int u0, int u1, int b, int base, int len, int pad, int hr,
                                             PagedEntry& e) {
-    const int nt = paged_tiles(len), ua = base + hr * (nt + kPartCost) + kPartCost, ub = ua + nt;       // units of its tiles
+    const int nt = paged_tiles(len), ub = base + (hr + 1) * paged_block_units(len, pad), ua = ub - nt;       // units of its tiles
     const int v0 = u0 > ua ? u0 : ua, v1 = u1 < ub ? u1 : ub;
     e.b = b;
     e.kvh = hr / p.row_blocks;
@@ -182,7 +194,7 @@ struct PagedShared {
     PagedWait wait;
     uint32_t is_last;
     int start_b, start_base;
-    int warp_sums[4];
+    int warp_sums[4], warp_longest[4];
     alignas(16) float c[2][kRows];                       // per query buffer: factor of a score (log2 units)
     int i[2][kRows];                                     // place among the new tokens
     // per group: bias - reference maximum, +inf where no key has been seen; and the same with 0 there
@@ -718,9 +730,15 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         // sequence that the CTA's share begins in
         const int chunk = (p.B + 127) / 128;
         const int b_first = key * chunk, b_last = min(p.B, b_first + chunk);
-        int mine = 0;
+        int mine = 0, longest = 0;
 #pragma unroll 4
-        for (int b = b_first; b < b_last; ++b) mine += paged_units(p, paged_len(p, b, nullptr));
+        for (int b = b_first; b < b_last; ++b) {
+            const int n = paged_len(p, b, nullptr);
+            mine += paged_units(p, n, 0);
+            longest = max(longest, n);
+        }
+        longest = __reduce_max_sync(0xffffffffu, longest);
+        if (lane == 0) sh.warp_longest[wq] = longest;
         int before = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -737,12 +755,20 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             if (v < wq) before += n;
             total += n;
         }
-        const int share = paged_share(total, gridDim.x, p.least_units);
+        longest = max(max(sh.warp_longest[0], sh.warp_longest[1]), max(sh.warp_longest[2], sh.warp_longest[3]));
+        const int pad = paged_pad(p, gridDim.x, paged_tiles(longest));
+        if (pad > 0) {           // all sequences count the same
+            const int units = paged_units(p, longest, pad);
+            total = units * p.B;
+            mine = max(0, b_last - b_first) * units;
+            before = min(b_first, p.B) * units;
+        }
+        const int share = paged_share(total, gridDim.x, p.least_units, pad);
         const int u0 = min(total, static_cast<int>(blockIdx.x) * share), u1 = min(total, u0 + share);
         if (before <= u0 && u0 < before + mine) {
             int b = b_first, base = before;
             for (;; ++b) {
-                const int n = paged_units(p, paged_len(p, b, nullptr));
+                const int n = paged_units(p, paged_len(p, b, nullptr), pad);
                 if (u0 < base + n) break;
                 base += n;
             }
@@ -759,13 +785,13 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             seq = sh.start_b;
             base = sh.start_base;
             len = paged_len(p, seq, lane == 0 ? p.status : nullptr);
-            hr = (u0 - base) / (paged_tiles(len) + kPartCost);
+            hr = (u0 - base) / paged_block_units(len, pad);
         }
         auto publish = [&](int k) {
             while (!ended && published < k + kPartRing) {
                 const int nt = paged_tiles(len);
                 PagedEntry e;
-                const bool some = hr + lane < blocks && paged_entry(p, blockIdx.x, share, u0, u1, seq, base, len, hr + lane, e);
+                const bool some = hr + lane < blocks && paged_entry(p, blockIdx.x, share, u0, u1, seq, base, len, pad, hr + lane, e);
                 const uint32_t have = __ballot_sync(0xffffffffu, some);
                 const int count = min(__popc(have), k + kPartRing - published);
                 // tiles of the parts before this lane's: the first part of a share may lack some, the others here have them all
@@ -784,9 +810,9 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                     if (hr < blocks) {
                         ended = true;                  // the share ends inside this sequence
                     } else {
-                        base += blocks * (nt + kPartCost);
+                        base += blocks * paged_block_units(len, pad);
                         hr = 0;
-                        if (base + kPartCost < u1) {
+                        if (base < u1) {
                             ++seq;
                             len = paged_len(p, seq, lane == 0 ? p.status : nullptr);
                         } else {
@@ -886,6 +912,16 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         for (int k = -3; k < end_at; ++k) {
             if (wq == 3 && !marked && published < max(k, 0) + kPartRing - 3) publish(max(k, 0));
             if (k + 3 < end_at) ok = ok && wait_part_timed(k + 3);
+            // whether all other pieces of an unfinished row block are there already: then this one need not be announced
+            if (k >= 0 && key == 0 && sh.part[k % kPartRing].slot >= 0) {
+                const PagedEntry& mine_part = sh.part[k % kPartRing];
+                const unsigned int got = *static_cast<volatile unsigned int*>(p.arrivals + mine_part.first_cta);
+                sh.is_last = got == static_cast<unsigned int>(mine_part.pieces - 1) ? 1u : 0u;
+                if (sh.is_last) {
+                    __threadfence();
+                    p.arrivals[mine_part.first_cta] = 0u;
+                }
+            }
             if (k >= 0) ok = ok && paged_wait_timed(&sh.stat_full[k % kPartRing], (k / kPartRing) & 1, wait, kSiteEpiState);
             if (named_barrier_or(kBar, 128, !ok)) break;
             if (k > -3 && k + 2 < end_at) store_queries(k + 2);
@@ -913,15 +949,6 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             named_barrier_sync(kBar, 128);
             // (uniform) whether a group had a tile of this part
             const bool had[2] = {e.t1 - e.t0 > 1 || (e.tile0 & 1) == 0, e.t1 - e.t0 > 1 || (e.tile0 & 1) == 1};
-            if (key == 0 && !whole) {
-                // all other pieces there already: no need to announce this one
-                const unsigned int got = *static_cast<volatile unsigned int*>(p.arrivals + e.first_cta);
-                sh.is_last = got == static_cast<unsigned int>(e.pieces - 1) ? 1u : 0u;
-                if (sh.is_last) {
-                    __threadfence();
-                    p.arrivals[e.first_cta] = 0u;
-                }
-            }
             if (key < kStates) {
                 float f[2], sum[2], mx[2];
 #pragma unroll
@@ -952,14 +979,20 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
 #pragma unroll
             for (int v = 0; v < 2; ++v) {
                 if (!had[v]) continue;
+                // (48 columns in flight)
+                constexpr int kGroup = kCols <= 48 ? kCols / 16 : 2;
 #pragma unroll
-                for (int g = 0; g < kCols / 16; ++g) {
-                    const int col = g * 16, st = col / (kTerms * kRows) * kRows + col % kRows;
-                    uint32_t o[16];
-                    tmem_ld_x16(tmem + o_col(ob, v) + lane_sel + col, o);
+                for (int g0 = 0; g0 < kCols / 16; g0 += kGroup) {
+                    uint32_t o[kGroup][16];
+#pragma unroll
+                    for (int g = 0; g < kGroup; ++g) tmem_ld_x16(tmem + o_col(ob, v) + lane_sel + (g0 + g) * 16, o[g]);
                     tc_wait_ld();
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) y[st + j] = fmaf(sh.factor[v][st + j], __uint_as_float(o[j]), y[st + j]);
+                    for (int g = 0; g < kGroup; ++g) {
+                        const int col = (g0 + g) * 16, st = col / (kTerms * kRows) * kRows + col % kRows;
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) y[st + j] = fmaf(sh.factor[v][st + j], __uint_as_float(o[g][j]), y[st + j]);
+                    }
                 }
             }
             tc_fence_before_sync();
