@@ -1,0 +1,340 @@
+// Differential attention over whole prompts for sm_100a, two maps of 64 over values of 128:
+//     Y = (softmax(s Q1 K1^T) - lambda softmax(s Q2 K2^T)) V,   O = out_scale * weight (*) Y / sqrt(mean(Y^2) + eps)
+//
+// The loop of fa_fwd_pair.cuh (read that file first), with the two MAPS of one query tile in the place of two query tiles: S_t is
+// the product of the t-th halves of Q and K (four k-steps of 16 and not eight), both maps' probabilities multiply the same
+// V tile, and Q, K and V are loaded once for both.  Run as two heads of ordinary attention (zeros in the other half of Q, the
+// difference and the norm in a kernel of their own), the scores would cost twice the MMAs, O would be written and read once
+// more in each map, and K and V would be read as often but for twice the heads.
+//
+// What bounds it: per K/V tile 24 MMAs of 64 cycles (1536) against 2 x 128 x 128 exponentials (2048 cycles of the special-function
+// unit): the softmax passes.
+//
+// Epilogue: both groups of softmax warps read BOTH accumulators (a warp reaches the same 32 TMEM lanes of every column), each for one
+// half of the 128 columns; row sums, lambda and the halves' sums of squares cross through shared memory, and each group
+// stages and stores its 64-column chunk.  Nothing but O leaves the SM.
+//
+// Roles (384 threads), TMEM: as in fa_fwd_pair.cuh (warps 0-3 / 4-7 softmax of map 0 / 1, warp 8 MMA issue, warp 9 loads).
+#pragma once
+
+#include <math.h>
+
+#include "fa_common.cuh"
+#include "fa_fwd_pair.cuh"
+#include "fa_softmax_pass.cuh"
+#include "ptx.cuh"
+
+namespace fa {
+
+struct DiffParams {
+    const float* lambda;          // [Hq]
+    const float* weight;          // [128] or nullptr: no normalisation
+    float eps, out_scale;
+};
+
+struct DiffCfg {
+    static constexpr int kQBytes = 2 * kChunkBytes;     // a query tile, both maps (chunk t = map t); K and V tiles alike
+    static constexpr int kKStages = 3, kVStages = 3;
+    static constexpr int kTileBytes = (1 + kKStages + kVStages) * kQBytes;
+    static constexpr int kColS0 = 0, kColO0 = 256;      // S_t at 128 t, O_t at 256 + 128 t; bf16 P_t overlays S_t
+    static constexpr int kThreads = 384;
+};
+
+struct DiffShared {
+    uint64_t q_full;
+    uint64_t k_full[DiffCfg::kKStages], k_empty[DiffCfg::kKStages];
+    uint64_t v_full[DiffCfg::kVStages], v_empty[DiffCfg::kVStages];
+    uint64_t s_full[2], p_first[2], p_rest[2], o_final[2], o_staged[2];
+    uint32_t tmem_base;
+    uint32_t abort_flag;
+    float inv_l[2][kTileM];
+    float sum_sq[2][kTileM];
+};
+
+constexpr int diff_smem_bytes() { return DiffCfg::kTileBytes + static_cast<int>(sizeof(DiffShared)); }
+
+__global__ void __launch_bounds__(384, 1)
+fa_fwd_diff_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                   const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_o, const FwdParams p,
+                   const DiffParams dp) {
+    using Cfg = DiffCfg;
+    using namespace ptx;
+    constexpr int NK = Cfg::kKStages, NV = Cfg::kVStages;
+
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    DiffShared& sh = *reinterpret_cast<DiffShared*>(smem_raw + Cfg::kTileBytes);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    grid_launch_dependents();
+    const uint32_t smem_base = smem_addr(smem_raw);
+    if ((smem_base & 1023u) != 0u) {          // uniform over the CTA; nothing has been set up yet
+        grid_dependency_wait();
+        if (tid == 0 && p.status) {
+            volatile uint32_t* sw = p.status;
+            sw[1] = kSiteSmemAlign;
+            sw[0] = 3u;                       // FA_ERR_CUDA
+            __threadfence_system();
+        }
+        return;
+    }
+    const uint32_t sQ = smem_base, sK = sQ + Cfg::kQBytes, sV = sK + NK * Cfg::kQBytes;
+
+    // items: (query tile, head), in L2-sized groups of heads, longest first (as in the other kernels)
+    const int n_bh = p.B * p.Hq, hpg = p.heads_per_group;
+    const int item = static_cast<int>(blockIdx.x);
+    const int group = item / (p.n_q_tiles * hpg);
+    const int bh0 = group * hpg;
+    const int group_size = (n_bh - bh0 < hpg) ? (n_bh - bh0) : hpg;
+    const int local = item - group * p.n_q_tiles * hpg;
+    const int q_tile = p.n_q_tiles - 1 - local / group_size;
+    const int bh = bh0 + local % group_size;
+    const int hq = bh % p.Hq, b = bh / p.Hq, kvh = hq / (p.Hq / p.Hkv);
+    const int i0 = q_tile * kTileM, off = p.Sk - p.Sq;
+    const int nkv = kv_tiles_for_q_tile(i0, kTileM, p.Sq, p.Sk, p.causal);
+
+    if (tid == 0) {
+        sh.abort_flag = 0;
+        mbar_init(smem_addr(&sh.q_full), 1);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            mbar_init(smem_addr(&sh.s_full[t]), 1);
+            mbar_init(smem_addr(&sh.p_first[t]), 4);      // 4 softmax warps
+            mbar_init(smem_addr(&sh.p_rest[t]), 4);
+            mbar_init(smem_addr(&sh.o_final[t]), 1);
+            mbar_init(smem_addr(&sh.o_staged[t]), 4);
+        }
+#pragma unroll
+        for (int s = 0; s < NK; ++s) {
+            mbar_init(smem_addr(&sh.k_full[s]), 1);
+            mbar_init(smem_addr(&sh.k_empty[s]), 1);
+        }
+#pragma unroll
+        for (int s = 0; s < NV; ++s) {
+            mbar_init(smem_addr(&sh.v_full[s]), 1);
+            mbar_init(smem_addr(&sh.v_empty[s]), 1);
+        }
+        fence_mbar_init();
+    }
+    if (warp == 8) {
+        tmem_alloc(smem_addr(&sh.tmem_base), 512);
+        tmem_relinquish_alloc_permit();
+    }
+    if (warp == 9 && lane == 0) {
+        prefetch_tensormap(&tm_q);
+        prefetch_tensormap(&tm_k);
+        prefetch_tensormap(&tm_v);
+        prefetch_tensormap(&tm_o);
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    grid_dependency_wait();
+
+    const uint32_t tmem_base = sh.tmem_base;
+    WaitCtx wctx{&sh.abort_flag, p.status, p.wait_limit_ns};
+    const float c = p.scale_log2;
+
+    if (warp < 8) {
+        // ============================================================ softmax of map t
+        setmaxnreg_inc<kPairRegsSoftmax>();
+        const int t = warp >> 2;
+        const int row = tid & (kTileM - 1);
+        const uint32_t lane_sel = static_cast<uint32_t>((warp & 3) * 32) << 16;
+        const uint32_t tS = tmem_base + Cfg::kColS0 + 128 * t + lane_sel;
+        const uint32_t tO = tmem_base + Cfg::kColO0 + lane_sel;
+        const uint32_t bar_s = smem_addr(&sh.s_full[t]), bar_pf = smem_addr(&sh.p_first[t]), bar_pr = smem_addr(&sh.p_rest[t]);
+        const int i_glob = i0 + row;
+        int kmax_row = p.Sk - 1;
+        if (p.causal && i_glob + off < kmax_row) kmax_row = i_glob + off;
+        const float tau_raw = kRescaleThresholdLog2 / c;
+        float m_ref = -INFINITY, l = 0.f;
+        bool ok = true;
+        for (int j = 0; j < nkv; ++j) {
+            ok = __all_sync(0xffffffffu, mbar_wait(bar_s, j & 1, wctx, kSiteSoftmaxSFull));
+            if (!ok) break;
+            tc_fence_after_sync();
+            softmax_pass_128<128>(tS, tO + 128 * t, c, tau_raw, j * kTileN, kmax_row, j == 0, m_ref, l, lane,
+                                  [&]() { mbar_arrive(bar_pf); }, [&]() { mbar_arrive(bar_pr); });
+        }
+        // Epilogue.  All 256 threads meet at its barriers, also after a wait that ran out (the result is not stored then).
+        sh.inv_l[t][row] = (l > 0.f) ? (1.f / l) : 0.f;
+        if (nkv > 0) {
+            ok = ok && mbar_wait(smem_addr(&sh.o_final[0]), 0, wctx, kSiteEpiOFull) &&
+                 mbar_wait(smem_addr(&sh.o_final[1]), 0, wctx, kSiteEpiOFull);
+            ok = __all_sync(0xffffffffu, ok);
+        }
+        named_barrier_sync(1, 256);
+        tc_fence_after_sync();
+        // group t: columns [64 t, 64 t + 64) of both accumulators
+        const float f0 = sh.inv_l[0][row], f1 = sh.inv_l[1][row] * dp.lambda[hq];
+        float y[64];
+        float sq = 0.f;
+        if (nkv > 0) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t r0[32], r1[32];
+                tmem_ld_x32(tO + 64 * t + 32 * h, r0);
+                tmem_ld_x32(tO + 128 + 64 * t + 32 * h, r1);
+                tc_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                    const float v = f0 * __uint_as_float(r0[e]) - f1 * __uint_as_float(r1[e]);
+                    y[32 * h + e] = v;
+                    sq = fmaf(v, v, sq);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 64; ++e) y[e] = 0.f;
+        }
+        float f = dp.out_scale;
+        if (dp.weight) {                        // (uniform)
+            sh.sum_sq[t][row] = sq;
+            named_barrier_sync(1, 256);
+            f *= rsqrtf((sh.sum_sq[0][row] + sh.sum_sq[1][row]) * (1.f / 128.f) + dp.eps);
+#pragma unroll
+            for (int e = 0; e < 64; e += 4) {
+                const float4 w = __ldg(reinterpret_cast<const float4*>(dp.weight + 64 * t + e));
+                y[e] *= f * w.x;
+                y[e + 1] *= f * w.y;
+                y[e + 2] *= f * w.z;
+                y[e + 3] *= f * w.w;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 64; ++e) y[e] *= f;
+        }
+        if (ok) {
+            // chunk t of the query tile's space (its last readers, the final score MMAs, are complete)
+            const uint32_t chunk = sQ + t * kChunkBytes;
+#pragma unroll
+            for (int v = 0; v < 8; ++v)
+                st_shared_v4(chunk + row * 128 + (static_cast<uint32_t>(v ^ (row & 7)) << 4),
+                             pack_bf16x2(y[8 * v], y[8 * v + 1]), pack_bf16x2(y[8 * v + 2], y[8 * v + 3]),
+                             pack_bf16x2(y[8 * v + 4], y[8 * v + 5]), pack_bf16x2(y[8 * v + 6], y[8 * v + 7]));
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_addr(&sh.o_staged[t]));
+            if ((warp & 3) == 0 && lane == 0 && mbar_wait(smem_addr(&sh.o_staged[t]), 0, wctx, kSiteEpiStaged)) {
+                tma_store_4d(&tm_o, chunk, 64 * t, i0, hq, b);
+                tma_store_commit();
+                tma_store_wait_read_all();     // the CTA's shared memory outlives the reads
+            }
+        }
+    } else if (warp == 8) {
+        // ============================================================ MMA issue, one thread for both maps
+        setmaxnreg_dec<kPairRegsOther>();
+        if (elect_one() && nkv > 0) {
+            constexpr uint32_t kIdescQK = make_idesc_bf16_f32(kTileM, kTileN, false, false);
+            constexpr uint32_t kIdescPV = make_idesc_bf16_f32(kTileM, 128, false, true);
+            constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);   // sbo, version, swizzle
+            const uint32_t q_lo0 = ((sQ & 0x3FFFFu) >> 4) | (1u << 16);
+            const uint32_t k_lo0 = ((sK & 0x3FFFFu) >> 4) | (1u << 16);
+            const uint32_t v_lo0 = ((sV & 0x3FFFFu) >> 4) | ((static_cast<uint32_t>(kChunkBytes) >> 4) << 16);
+            auto desc = [](uint32_t lo) -> uint64_t { return (static_cast<uint64_t>(kDescHi) << 32) | lo; };
+            // k-step k of map t: chunk t, 32 bytes a step
+            auto koff = [](int t, int k) -> uint32_t { return static_cast<uint32_t>((t * kChunkBytes + k * 32) >> 4); };
+            const uint32_t bar_always = smem_addr(&sh.q_full);     // its phase 0 has completed, it never moves again: unused probes
+
+            bool ok = mbar_wait(smem_addr(&sh.q_full), 0, wctx, kSiteMmaQFull) &&
+                      mbar_wait(smem_addr(&sh.k_full[0]), 0, wctx, kSiteMmaKvFull);
+            if (ok) {
+                tc_fence_after_sync();
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        mma_ss(tmem_base + Cfg::kColS0 + 128 * t, desc(q_lo0 + koff(t, k)), desc(k_lo0 + koff(t, k)), kIdescQK, k > 0 ? 1u : 0u);
+                    tc_commit(smem_addr(&sh.s_full[t]));
+                }
+                tc_commit(smem_addr(&sh.k_empty[0]));
+            }
+            int sv = 0, sk = 1;                       // stage of V_j and of K_{j+1}
+            uint32_t ph_v = 0, ph_k = 0;
+            uint32_t pre_p0 = 0u, pre_p1 = 0u, pre_v = 0u, pre_k = 0u;    // probes that succeeded: P_0 / P_1 first part, V_j, K_{j+1}
+
+            // One map's block of iteration j: PV_t(j), then QK_t(j+1); barriers to probe from inside the block as in the pair kernel.
+            auto map_block = [&](auto tc, int j, uint32_t pre_first, uint32_t b0, uint32_t par0, uint32_t b1, uint32_t par1, uint32_t b2,
+                                 uint32_t par2, uint32_t& probed) -> bool {
+                constexpr int t = decltype(tc)::value;
+                probed = 0u;
+                const uint32_t tS = tmem_base + Cfg::kColS0 + 128 * t, tO = tmem_base + Cfg::kColO0 + 128 * t;
+                const uint32_t vlo = v_lo0 + sv * (Cfg::kQBytes >> 4), klo = k_lo0 + sk * (Cfg::kQBytes >> 4);
+                if (!pre_first && !mbar_wait(smem_addr(&sh.p_first[t]), j & 1, wctx, kSiteMmaPFull)) return false;
+                tc_fence_after_sync();
+                mma_ts(tO, tS + 0, desc(vlo + 0 * (2048 >> 4)), kIdescPV, j > 0 ? 1u : 0u);
+                mma_ts(tO, tS + 8, desc(vlo + 1 * (2048 >> 4)), kIdescPV, 1u);
+                mma_ts(tO, tS + 16, desc(vlo + 2 * (2048 >> 4)), kIdescPV, 1u);
+                mma_ts(tO, tS + 24, desc(vlo + 3 * (2048 >> 4)), kIdescPV, 1u);
+                const uint32_t rest = probe_mma_ts2(smem_addr(&sh.p_rest[t]), j & 1, tO, tS + 32, desc(vlo + 4 * (2048 >> 4)),
+                                                    tS + 40, desc(vlo + 5 * (2048 >> 4)), kIdescPV);
+                if (!rest && !mbar_wait(smem_addr(&sh.p_rest[t]), j & 1, wctx, kSiteMmaPFull)) return false;
+                tc_fence_after_sync();
+                mma_ts(tO, tS + 48, desc(vlo + 6 * (2048 >> 4)), kIdescPV, 1u);
+                mma_ts(tO, tS + 56, desc(vlo + 7 * (2048 >> 4)), kIdescPV, 1u);
+                if (j + 1 < nkv) {
+                    mma_ss(tS, desc(q_lo0 + koff(t, 0)), desc(klo + koff(t, 0)), kIdescQK, 0u);
+                    probed = probe3_mma_ss3(b0, par0, b1, par1, b2, par2, tS, desc(q_lo0 + koff(t, 1)), desc(klo + koff(t, 1)),
+                                            desc(q_lo0 + koff(t, 2)), desc(klo + koff(t, 2)), desc(q_lo0 + koff(t, 3)), desc(klo + koff(t, 3)),
+                                            kIdescQK);
+                    tc_commit(smem_addr(&sh.s_full[t]));
+                } else {
+                    tc_commit(smem_addr(&sh.o_final[t]));
+                }
+                return true;
+            };
+
+            for (int j = 0; j < nkv && ok; ++j) {
+                if (!pre_v) ok = mbar_wait(smem_addr(&sh.v_full[sv]), ph_v, wctx, kSiteMmaKvFull);
+                if (ok && j + 1 < nkv && !pre_k) ok = mbar_wait(smem_addr(&sh.k_full[sk]), ph_k, wctx, kSiteMmaKvFull);
+                if (!ok) break;
+                uint32_t probed;
+                ok = map_block(IntC<0>{}, j, pre_p0, smem_addr(&sh.p_first[1]), j & 1, bar_always, 0u, bar_always, 0u, probed);
+                if (!ok) break;
+                pre_p1 = probed & 1u;
+                int sv_n = sv + 1; uint32_t ph_v_n = ph_v; if (sv_n == NV) { sv_n = 0; ph_v_n ^= 1u; }
+                int sk_n = sk + 1; uint32_t ph_k_n = ph_k; if (sk_n == NK) { sk_n = 0; ph_k_n ^= 1u; }
+                const bool next = j + 1 < nkv, next_k = j + 2 < nkv;
+                ok = map_block(IntC<1>{}, j, pre_p1, next ? smem_addr(&sh.p_first[0]) : bar_always, next ? ((j + 1) & 1) : 0u,
+                               next ? smem_addr(&sh.v_full[sv_n]) : bar_always, next ? ph_v_n : 0u,
+                               next_k ? smem_addr(&sh.k_full[sk_n]) : bar_always, next_k ? ph_k_n : 0u, probed);
+                if (!ok) break;
+                pre_p0 = next ? (probed & 1u) : 0u;
+                pre_v = next ? ((probed >> 1) & 1u) : 0u;
+                pre_k = next_k ? ((probed >> 2) & 1u) : 0u;
+                tc_commit(smem_addr(&sh.v_empty[sv]));
+                if (next) tc_commit(smem_addr(&sh.k_empty[sk]));
+                sv = sv_n; ph_v = ph_v_n; sk = sk_n; ph_k = ph_k_n;
+            }
+        }
+    } else if (warp == 9) {
+        // ============================================================ TMA loads
+        setmaxnreg_dec<kPairRegsOther>();
+        if (elect_one() && nkv > 0) {
+            auto load_tile = [&](uint32_t dst, const CUtensorMap* tm, uint64_t& full, int row0, int head) {
+                const uint32_t bar = smem_addr(&full);
+                mbar_arrive_expect_tx(bar, Cfg::kQBytes);
+#pragma unroll
+                for (int cc = 0; cc < 2; ++cc) tma_load_4d(dst + cc * kChunkBytes, tm, bar, cc * kChunkCols, row0, head, b);
+            };
+            load_tile(sQ, &tm_q, sh.q_full, i0, hq);
+            for (int j = 0; j < nkv; ++j) {
+                const int ks = j % NK, vs = j % NV;
+                if (!mbar_wait(smem_addr(&sh.k_empty[ks]), ((j / NK) & 1) ^ 1, wctx, kSiteLoadKvEmpty)) break;
+                load_tile(sK + ks * Cfg::kQBytes, &tm_k, sh.k_full[ks], j * kTileN, kvh);
+                if (p.debug_drop_v_load && j == 0) continue;
+                if (!mbar_wait(smem_addr(&sh.v_empty[vs]), ((j / NV) & 1) ^ 1, wctx, kSiteLoadKvEmpty)) break;
+                load_tile(sV + vs * Cfg::kQBytes, &tm_v, sh.v_full[vs], j * kTileN, kvh);
+            }
+        }
+    } else {
+        setmaxnreg_dec<kPairRegsOther>();     // idle warps of the third warpgroup
+    }
+
+    // ---------------------------------------------------------------- teardown (all warps)
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 8) tmem_dealloc(tmem_base, 512);
+}
+
+}  // namespace fa

@@ -140,4 +140,20 @@ fa_status ensure_smem_attr(fa_handle* h, Kernel kernel, int bytes) {
 
 inline bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 
+// Number of (batch, query head) instances scheduled together.  The K and V of a group (read again
+// by every query tile of its heads) should fit in about a third of the 126 MB L2, a group holds
+// whole GQA groups, and the groups are made equal in size: a small last group would start its
+// longest items late and leave most SMs idle under them.
+inline int heads_per_group(long long kv_bytes_per_head, int B, int Hq, int Hkv) {
+    const long long budget = 48ll << 20;      // 32 to 96 MB measure the same within 2 %
+    long long kv_heads = budget / kv_bytes_per_head;
+    if (kv_heads < 1) kv_heads = 1;
+    const long long gqa = Hq / Hkv;
+    const long long n_kv = static_cast<long long>(B) * Hkv;       // K/V heads in the batch
+    if (kv_heads > n_kv) kv_heads = n_kv;
+    const long long n_groups = (n_kv + kv_heads - 1) / kv_heads;
+    kv_heads = (n_kv + n_groups - 1) / n_groups;
+    return static_cast<int>(kv_heads * gqa);
+}
+
 }  // namespace fa_host

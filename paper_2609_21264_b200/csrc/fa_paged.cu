@@ -9,6 +9,7 @@
 #include "../../include/fa.h"
 #include "fa_append_paged.cuh"
 #include "fa_common.cuh"
+#include "fa_fwd_diff.cuh"
 #include "fa_handle.h"
 #include "fa_paged.cuh"
 #include "fa_paged_common.cuh"
@@ -323,6 +324,35 @@ fa_status fa_forward_diff(fa_handle* h, const void* Q, const void* K, const void
     if (!guard.ok()) return FA_ERR_CUDA;
     if (scale == 0.f) scale = 0.125f;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (!(h->flags & FA_FLAG_SERIAL_KERNEL)) {
+        const CUtensorMap* m = nullptr;
+        if ((s = get_map(h, Q, 128, Sq, Hq, B, q_strides[0], q_strides[1], q_strides[2], fa::kTileM, &m)) != FA_OK) return s;
+        const CUtensorMap mq = *m;       // copies: a later insertion may move the cache's entries
+        if ((s = get_map(h, K, 128, Sk, Hkv, B, k_strides[0], k_strides[1], k_strides[2], fa::kTileN, &m)) != FA_OK) return s;
+        const CUtensorMap mk = *m;
+        if ((s = get_map(h, V, 128, Sk, Hkv, B, v_strides[0], v_strides[1], v_strides[2], fa::kTileN, &m)) != FA_OK) return s;
+        const CUtensorMap mv = *m;
+        if ((s = get_map(h, O, 128, Sq, Hq, B, o_strides[0], o_strides[1], o_strides[2], fa::kTileM, &m)) != FA_OK) return s;
+        const CUtensorMap mo = *m;
+        fa::FwdParams f;
+        memset(&f, 0, sizeof f);
+        f.B = B; f.Hq = Hq; f.Hkv = Hkv; f.Sq = Sq; f.Sk = Sk;
+        f.causal = causal ? 1 : 0;
+        f.scale_log2 = scale * 1.4426950408889634f;
+        f.n_q_tiles = (Sq + fa::kTileM - 1) / fa::kTileM;
+        f.heads_per_group = heads_per_group(static_cast<long long>(Sk) * 512, B, Hq, Hkv);
+        f.kv_splits = 1;
+        f.status = h->status_dev;
+        f.wait_limit_ns = h->wait_limit_ns;
+        f.debug_drop_v_load = (h->flags & FA_FLAG_DEBUG_DROP_V_LOAD) ? 1 : 0;
+        const fa::DiffParams dp{diff->lambda, diff->weight, diff->eps, diff->out_scale};
+        constexpr int smem = fa::diff_smem_bytes();
+        static_assert(smem <= 227 * 1024, "shared memory budget exceeded");
+        if ((s = ensure_smem_attr(h, fa::fa_fwd_diff_kernel, smem)) != FA_OK) return s;
+        h->last_kernel = "fa_fwd_diff";
+        h->last_splits = 1;
+        return launch(h, fa::fa_fwd_diff_kernel, static_cast<long long>(f.n_q_tiles) * Hq * B, fa::DiffCfg::kThreads, smem, st, mq, mk, mv, mo, f, dp);
+    }
     fa::PagedParams p;
     memset(&p, 0, sizeof p);
     p.Q = static_cast<const __nv_bfloat16*>(Q);
