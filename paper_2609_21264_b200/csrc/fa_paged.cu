@@ -342,6 +342,7 @@ fa_status fa_forward_diff(fa_handle* h, const void* Q, const void* K, const void
         f.n_q_tiles = (Sq + fa::kTileM - 1) / fa::kTileM;
         f.heads_per_group = heads_per_group(static_cast<long long>(Sk) * 512, B, Hq, Hkv);
         f.kv_splits = 1;
+        f.sched_counter = h->sched_counter;
         f.status = h->status_dev;
         f.wait_limit_ns = h->wait_limit_ns;
         f.debug_drop_v_load = (h->flags & FA_FLAG_DEBUG_DROP_V_LOAD) ? 1 : 0;
@@ -351,7 +352,9 @@ fa_status fa_forward_diff(fa_handle* h, const void* Q, const void* K, const void
         if ((s = ensure_smem_attr(h, fa::fa_fwd_diff_kernel, smem)) != FA_OK) return s;
         h->last_kernel = "fa_fwd_diff";
         h->last_splits = 1;
-        return launch(h, fa::fa_fwd_diff_kernel, static_cast<long long>(f.n_q_tiles) * Hq * B, fa::DiffCfg::kThreads, smem, st, mq, mk, mv, mo, f, dp);
+        const long long items = static_cast<long long>(f.n_q_tiles) * Hq * B;
+        if (items > 0x3fffffffLL) return FA_ERR_UNSUPPORTED;
+        return launch(h, fa::fa_fwd_diff_kernel, items < h->num_sms ? items : h->num_sms, fa::DiffCfg::kThreads, smem, st, mq, mk, mv, mo, f, dp);
     }
     fa::PagedParams p;
     memset(&p, 0, sizeof p);

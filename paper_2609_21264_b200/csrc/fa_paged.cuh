@@ -44,25 +44,6 @@ namespace fa {
 
 namespace ptx {
 
-// OR of a predicate over the `nthreads` threads that meet at a named barrier.
-FA_DEVI bool named_barrier_or(uint32_t id, uint32_t nthreads, bool x) {
-    uint32_t r;
-    asm volatile(
-        "{\n"
-        ".reg .pred p, q;\n"
-        "setp.ne.u32 p, %1, 0;\n"
-        "barrier.cta.red.or.pred q, %2, %3, p;\n"
-        "selp.u32 %0, 1, 0, q;\n"
-        "}\n"
-        : "=r"(r) : "r"(x ? 1u : 0u), "r"(id), "r"(nthreads) : "memory");
-    return r != 0;
-}
-FA_DEVI void st_shared_u16(uint32_t addr, uint32_t x) {
-    asm volatile("st.shared.u16 [%0], %1;" ::"r"(addr), "h"(static_cast<uint16_t>(x)) : "memory");
-}
-FA_DEVI void st_shared_u8(uint32_t addr, uint32_t x) {
-    asm volatile("st.shared.u8 [%0], %1;" ::"r"(addr), "r"(x) : "memory");
-}
 FA_DEVI void st_shared_u64(uint32_t addr, uint32_t lo, uint32_t hi) {
     asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(lo), "r"(hi) : "memory");
 }

@@ -118,6 +118,20 @@ FA_DEVI void named_barrier_sync(uint32_t id, uint32_t nthreads) {
     asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(nthreads) : "memory");
 }
 
+// OR of a predicate over the `nthreads` threads that meet at a named barrier.
+FA_DEVI bool named_barrier_or(uint32_t id, uint32_t nthreads, bool x) {
+    uint32_t r;
+    asm volatile(
+        "{\n"
+        ".reg .pred p, q;\n"
+        "setp.ne.u32 p, %1, 0;\n"
+        "barrier.cta.red.or.pred q, %2, %3, p;\n"
+        "selp.u32 %0, 1, 0, q;\n"
+        "}\n"
+        : "=r"(r) : "r"(x ? 1u : 0u), "r"(id), "r"(nthreads) : "memory");
+    return r != 0;
+}
+
 // ------------------------------------------------------------------ mbarrier
 
 FA_DEVI void mbar_init(uint32_t bar, uint32_t count) {
