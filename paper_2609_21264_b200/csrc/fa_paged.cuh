@@ -436,36 +436,49 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             }
         }
     } else if (warp == 3) {
-        // ============================================================ value products, one thread
+        // ============================================================ value products: the warp waits together, one thread issues
         setmaxnreg_dec<kPagedRegsOther>();
-        if (elect_one()) {
-            // (both operands with the product's dimension as the slow one)
-            constexpr uint32_t kIdescPV = kE4m3 ? (make_idesc_e4m3_f32(128, kCols, true, true) | (1u << 10))
-                                                : make_idesc_bf16_f32(128, kCols, true, true);
-            constexpr int kStepKeys = 32 / Cfg::kElem, kStep16 = (kStepKeys * 128) >> 4;
-            const uint32_t v_lo0 = desc_lo(sV, Cfg::kZeroBlock ? 0 : kChunkBytes), p_lo0 = desc_lo(sP, 128);
-            int n = 0, s = 0;
-            uint32_t v_parity = 0;
-            bool ok = true;
-            for (int k = 0; ok; ++k) {
-                if (!wait_part(k)) break;
-                const PagedEntry e = sh.part[k % kPartRing];
-                if (e.t1 < 0) break;
-                if (!paged_wait(sh.acc_empty[k % kOBufs], ((k / kOBufs) & 1) ^ 1, wait)) break;
-                for (int t = e.t0; t < e.t1; ++t, ++n) {
-                    const int w = n & 1, i = (n >> 1) % kPBufs;
-                    ok = paged_wait(sh.v_full[s], v_parity, wait) &&
-                         paged_wait(sh.p_full[w][i], ((n >> 1) / kPBufs) & 1, wait);
-                    if (!ok) break;
-                    tc_fence_after_sync();
+        constexpr uint32_t kIdescPV = kE4m3 ? (make_idesc_e4m3_f32(128, kCols, true, true) | (1u << 10))      // (both operands with the
+                                            : make_idesc_bf16_f32(128, kCols, true, true);                  // keys as the slow dimension)
+        constexpr int kStepKeys = 32 / Cfg::kElem, kStep16 = (kStepKeys * 128) >> 4;
+        const uint32_t v_lo0 = desc_lo(sV, Cfg::kZeroBlock ? 0 : kChunkBytes), p_lo0 = desc_lo(sP, 128);
+        int n = 0, s = 0;
+        uint32_t v_parity = 0;
+        bool ok = true;
+        for (int k = 0; ok; ++k) {
+            ok = __all_sync(0xffffffffu, wait_part(k));
+            if (!ok) break;
+            const PagedEntry e = sh.part[k % kPartRing];
+            if (e.t1 < 0) break;
+            ok = __all_sync(0xffffffffu, paged_wait(sh.acc_empty[k % kOBufs], ((k / kOBufs) & 1) ^ 1, wait));
+            if (!ok) break;
+            for (int t = e.t0; t < e.t1; ++t, ++n) {
+                const int w = n & 1, i = (n >> 1) % kPBufs;
+                ok = paged_wait(sh.v_full[s], v_parity, wait);
+                // the sequence's last tile: only the k-steps that hold keys are multiplied (one at least).  V rows behind the
+                // sequence's end, as far as the last of them reaches, hold whatever the page held, or were not loaded: zeros, since
+                // 0 * NaN is NaN.  (Here, where the stage is known to be this tile's: the softmax warps may be a turn of the ring ahead.)
+                const int keys = t == e.t1 - 1 ? min(kTileN, e.len - t * kTileN) : kTileN;
+                const int steps_end = keys <= 0 ? kStepKeys : (keys + kStepKeys - 1) / kStepKeys * kStepKeys;
+                if (max(keys, 0) < steps_end) {
+                    __syncwarp();
+                    for (int j = lane; j < (steps_end - max(keys, 0)) * 8; j += 32) {
+                        const uint32_t row = sV + s * Cfg::kVBytes + (max(keys, 0) + (j >> 3)) * 128 + (j & 7) * 16;
+#pragma unroll
+                        for (int c = 0; c < Cfg::kVChunks; ++c) st_shared_v4(row + c * kChunkBytes, 0, 0, 0, 0);
+                    }
+                    fence_proxy_async_smem();
+                }
+                ok = __all_sync(0xffffffffu, ok && paged_wait(sh.p_full[w][i], ((n >> 1) / kPBufs) & 1, wait));
+                if (!ok) break;
+                tc_fence_after_sync();
+                if (elect_one()) {
                     const uint32_t v_lo = v_lo0 + s * (Cfg::kVBytes >> 4), p_lo = p_lo0 + (w * kPBufs + i) * (Cfg::kPBytes >> 4);
                     const uint32_t d = tmem + o_col(k % kOBufs, w);
                     const uint32_t acc = t >= e.t0 + 2 ? 1u : 0u;        // the group's first tile of the part overwrites
-                    // the sequence's last tile: only the k-steps that hold keys (one at least)
-                    const int keys = t == e.t1 - 1 ? min(kTileN, e.len - t * kTileN) : kTileN;
 #pragma unroll
                     for (int ks = 0; ks < Cfg::kPSteps; ++ks) {
-                        if (ks > 0 && ks * kStepKeys >= keys) break;
+                        if (ks * kStepKeys >= steps_end) break;
                         // (values of 64: the second 64 rows of V^T are read from a block of zeros, wherever this k-step is)
                         const uint32_t lo = v_lo + ks * kStep16;
                         const uint32_t lbo = Cfg::kZeroBlock ? (((sZero >> 4) - (lo & 0x3fffu)) << 16) : 0u;
@@ -473,9 +486,10 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                     }
                     tc_commit(smem_addr(&sh.v_empty[s]));
                     tc_commit(smem_addr(&sh.pv_done[w][i]));
-                    if (++s == NS) { s = 0; v_parity ^= 1u; }
+                    if (t == e.t1 - 1) tc_commit(smem_addr(&sh.acc_full[k % kOBufs]));
                 }
-                if (ok) tc_commit(smem_addr(&sh.acc_full[k % kOBufs]));
+                __syncwarp();
+                if (++s == NS) { s = 0; v_parity ^= 1u; }
             }
         }
     } else if (warp < 12) {
@@ -654,17 +668,6 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                         for (int r = 0; r < kStates; r += 8)
                             st_shared_v4(sPw + r / 8 * Cfg::kPGroupBytes, pack_bf16x2(x[r], x[r + 1]), pack_bf16x2(x[r + 2], x[r + 3]),
                                          pack_bf16x2(x[r + 4], x[r + 5]), pack_bf16x2(x[r + 6], x[r + 7]));
-                    }
-                    constexpr int kStepKeys = 32 / Cfg::kElem;
-                    const int keys = len - t * kTileN, steps_end = keys <= 0 ? kStepKeys : (keys + kStepKeys - 1) / kStepKeys * kStepKeys;
-                    if (key >= keys && key < steps_end) {
-                        // V rows behind the sequence's end, as far as the last k-step reaches, hold whatever the page held, or were not
-                        // loaded: zeros, since 0 * NaN is NaN
-                        const int s = (tile0 + t - t0) % NS;
-                        ok = ok && paged_wait(sh.v_full[s], ((tile0 + t - t0) / NS) & 1, wait);
-#pragma unroll
-                        for (int c = 0; c < Cfg::kVChunks * 8; ++c)
-                            st_shared_v4(sV + s * Cfg::kVBytes + (c >> 3) * kChunkBytes + key * 128 + (c & 7) * 16, 0, 0, 0, 0);
                     }
                     fence_proxy_async_smem();
                     tc_fence_before_sync();

@@ -26,7 +26,8 @@ namespace fa {
 // tS: TMEM address of this warp's lanes of the score tile (P overlays its first 64 columns); tO: of the accumulator
 // that P_t V_j goes to; c = scale * log2(e); tau_raw = kRescaleThresholdLog2 / c; keys j0 + e > kmax_row are masked;
 // first_tile: nothing has been accumulated into O yet (no rescale).  All 32 lanes of a warp call it together.
-template <int DV, typename ArriveFirst, typename ArriveRest>
+// kPolyEvery > 0: every kPolyEvery-th pair of exponentials on the FMA pipe instead of the special-function unit.
+template <int DV, int kPolyEvery = 0, typename ArriveFirst, typename ArriveRest>
 FA_DEVI void softmax_pass_128(uint32_t tS, uint32_t tO, float c, float tau_raw, int j0, int kmax_row, bool first_tile,
                               float& m_ref, float& l, int lane, ArriveFirst&& arrive_first, ArriveRest&& arrive_rest) {
     using namespace ptx;
@@ -40,6 +41,14 @@ FA_DEVI void softmax_pass_128(uint32_t tS, uint32_t tO, float c, float tau_raw, 
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
             const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[q * 32 + e]), __uint_as_float(s[q * 32 + e + 1])), c2, nmc2);
+            if constexpr (kPolyEvery > 0) {
+                if ((e / 2) % kPolyEvery == kPolyEvery - 1) {
+                    const float2 y = exp2_poly2(x);
+                    s[q * 32 + e] = __float_as_uint(y.x);
+                    s[q * 32 + e + 1] = __float_as_uint(y.y);
+                    continue;
+                }
+            }
             s[q * 32 + e] = __float_as_uint(exp2_approx(x.x));
             s[q * 32 + e + 1] = __float_as_uint(exp2_approx(x.y));
         }

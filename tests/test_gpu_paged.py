@@ -174,6 +174,45 @@ def test_shared_pages_and_repeated_calls_are_bit_equal(handle):
         assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
 
 
+@pytest.mark.parametrize("Hq,Hkv,dqk,dv,page,e4m3,diff", [(32, 8, 128, 128, 16, False, False), (32, 8, 128, 128, 64, True, False),
+                                                          (16, 16, 192, 128, 48, False, False), (14, 2, 64, 64, 32, False, False),
+                                                          (16, 4, 128, 128, 32, False, True), (16, 4, 128, 128, 32, True, True)])
+def test_a_serving_batch_fills_the_gpu_and_repeats_bit_for_bit(Hq, Hkv, dqk, dv, page, e4m3, diff):
+    """Lengths from 65 to 4096 that end anywhere in a tile, more row blocks than SMs, every page slot poisoned that is not a key's:
+    against the plain kernel, and ten times the same bits (loads of K and V that overtake one another show here)."""
+    from paper_2609_21264_b200 import binding as b
+    lens = [65 + (i * 7919 + 4201) % 4032 for i in range(48)]
+    k, v, table, lens_t, ks, vs = pool(lens, page, Hkv, dqk, dv, e4m3, False, 60)
+    q = torch.randn(48, Hq, dqk, device="cuda").bfloat16()
+    lam, w = torch.rand(Hq, device="cuda"), torch.rand(128, device="cuda")
+    cache = b.PagedCache(k, v, ks, vs)
+
+    def call(h):
+        if diff:
+            return b.forward_paged_diff(h, q, cache, table, lens_t, lam, norm_weight=w), None
+        return b.forward_paged(h, q, cache, table, lens_t)
+
+    plain, h = b.fa_create(flags=b.FA_FLAG_SERIAL_KERNEL), b.fa_create()
+    try:
+        want, want_lse = call(plain)
+        o, lse = call(h)
+        ok(plain)
+        ok(h)
+        # both round once to bf16, the streaming kernel rounds its probabilities too: a row's values differ by less than that of the
+        # largest of them
+        scale = want.double().abs().amax(-1, keepdim=True)
+        assert ((o.double() - want.double()).abs() <= 4 * 2.0 ** -8 * scale).all()
+        if lse is not None:
+            assert (lse - want_lse).abs().max() <= 3e-4
+        for _ in range(10):
+            again, again_lse = call(h)
+            ok(h)
+            assert torch.equal(again, o) and (lse is None or torch.equal(again_lse, lse))
+    finally:
+        b.fa_destroy(plain)
+        b.fa_destroy(h)
+
+
 def test_captured_step_with_the_append_follows_growing_lengths(handle):
     """One decode step (append with rotation, then attention), captured once and replayed while the sequences grow, against the
     eager calls on a copy."""
