@@ -99,11 +99,11 @@ fa_status launch_simple(fa_handle* h, int dqk, const fa::PagedParams& p, cudaStr
     return launch(h, fa::fa_paged_simple_kernel<128, 128, kE4m3, kDiff>, blocks, 128, 0, st, p);
 }
 
-// Query rows per block: 16 where they suffice, else 32 or 64, as far as the accumulators (S^T and O^T twice, three times the columns
-// over an 8-bit cache, twice with two maps) and two stages of tiles fit.
+// Query rows per block: 16 where they suffice, else 32 or 64, as far as the accumulators (S^T and O^T of both groups, three times the
+// columns over an 8-bit cache, four times with two maps) and two stages of tiles fit.
 int rows_per_block(int rows, int dqk, bool e4m3, bool diff) {
-    if (rows <= 16 || (e4m3 && diff)) return 16;
-    return rows > 32 && !e4m3 && !diff && dqk != 192 ? 64 : 32;
+    if (rows <= 16 || diff) return 16;
+    return rows > 32 && !e4m3 && dqk != 192 ? 64 : 32;
 }
 
 // Tiles of 128 keys that a call's list of work can have at most; the kernel counts them in 32 bits.
@@ -143,7 +143,7 @@ fa_status launch_paged_rows(fa_handle* h, int block, const CUtensorMap& mk, cons
     if constexpr (!kE4m3 && !kDiff && DQK != 192) {
         if (block == 64) return launch_paged<DQK, DV, kE4m3, kDiff, 64>(h, mk, mv, p, st);
     }
-    if constexpr (!(kE4m3 && kDiff)) {
+    if constexpr (!kDiff) {
         if (block == 32) return launch_paged<DQK, DV, kE4m3, kDiff, 32>(h, mk, mv, p, st);
     }
     return launch_paged<DQK, DV, kE4m3, kDiff, 16>(h, mk, mv, p, st);

@@ -196,9 +196,12 @@ struct PagedShared {
 template <int DQK, int DV, bool kE4m3, bool kDiff, int kRows>
 struct PagedCfg {
     static constexpr int kMaps = kDiff ? 2 : 1;
-    static constexpr int kTerms = kE4m3 ? 3 : 1;
+    static constexpr int kTerms = kE4m3 ? 3 : 1;                // of the queries
+    // of the probabilities: the difference of two maps loses what they have in common, so these keep 16 bits over a bf16 cache too
+    // (one bf16 term: 1.5 times the error of the rounded output alone; two: none that shows, at the same speed)
+    static constexpr int kPTerms = kE4m3 ? 3 : (kDiff ? 2 : 1);
     static constexpr int kStates = kMaps * kRows;               // softmax states of a group
-    static constexpr int kCols = kStates * kTerms;              // columns of S^T and of O^T
+    static constexpr int kSCols = kStates * kTerms, kCols = kStates * kPTerms;      // columns of S^T and of O^T
     static constexpr int kElem = kE4m3 ? 1 : 2;
     static constexpr int kChunk = 128 / kElem;                  // columns of a 128-byte row of a chunk
     static constexpr int kKChunks = (DQK + kChunk - 1) / kChunk;
@@ -224,11 +227,11 @@ struct PagedCfg {
     static_assert(kStages >= 2, "shared memory budget exceeded");
     static constexpr int kTileBytes = kFixedBytes + kStages * (kKBytes + kVBytes);
     // score buffers of both groups (4 or 2) and accumulators of both groups (for 2 parts or 1), as TMEM has room
-    static constexpr int kSBufs = 8 * kCols <= 512 ? 4 : 2;
-    static constexpr int kOBufs = kSBufs == 4 ? 2 : 1;
-    static constexpr int kUsedCols = (kSBufs + 2 * kOBufs) * kCols;
+    static constexpr int kSBufs = 4 * kSCols + 2 * kCols <= 512 ? 4 : 2;
+    static constexpr int kOBufs = kSBufs * kSCols + 4 * kCols <= 512 ? 2 : 1;
+    static constexpr int kUsedCols = kSBufs * kSCols + 2 * kOBufs * kCols;
     static constexpr int kTmemCols = kUsedCols <= 64 ? 64 : kUsedCols <= 128 ? 128 : kUsedCols <= 256 ? 256 : 512;
-    static_assert(kUsedCols <= 512 && kCols % 16 == 0 && kCols <= 256, "accumulators");
+    static_assert(kUsedCols <= 512 && kSCols % 16 == 0 && kCols <= 256, "accumulators");
     static constexpr int kKSteps = DQK * kElem / 32;            // k-steps of 32 bytes
     static constexpr int kPSteps = 128 * kElem / 32;
     // exponents above the reference that a score may reach before the reference moves, and the scaling of P
@@ -264,7 +267,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
     using Cfg = PagedCfg<DQK, DV, kE4m3, kDiff, kRows>;
     using Shared = PagedShared<kRows, Cfg::kMaps>;
     using namespace ptx;
-    constexpr int NS = Cfg::kStages, kMaps = Cfg::kMaps, kTerms = Cfg::kTerms, kStates = Cfg::kStates, kCols = Cfg::kCols;
+    constexpr int NS = Cfg::kStages, kMaps = Cfg::kMaps, kTerms = Cfg::kTerms, kPTerms = Cfg::kPTerms, kStates = Cfg::kStates, kCols = Cfg::kCols;
     constexpr int kBufs = Cfg::kSBufs / 2;        // score buffers of a group
     constexpr int kOBufs = Cfg::kOBufs, kPBufs = Cfg::kPBufs;
 
@@ -330,9 +333,9 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
     const uint32_t tmem = sh.tmem_base;
     // (everything so far ran beside the kernel before; from here on its results may be read)
     grid_dependency_wait();
-    // TMEM: S^T of group w, buffer i at (w*kBufs + i)*kCols; O^T of accumulator buffer ob, group w behind them
-    auto s_col = [&](int w, int i) -> uint32_t { return (w * kBufs + i) * kCols; };
-    auto o_col = [&](int ob, int w) -> uint32_t { return (Cfg::kSBufs + ob * 2 + w) * kCols; };
+    // TMEM: S^T of group w, buffer i; behind them O^T of accumulator buffer ob, group w
+    auto s_col = [&](int w, int i) -> uint32_t { return (w * kBufs + i) * Cfg::kSCols; };
+    auto o_col = [&](int ob, int w) -> uint32_t { return Cfg::kSBufs * Cfg::kSCols + (ob * 2 + w) * kCols; };
     PagedWait* const wait = &sh.wait;
     const int group = p.Hq / p.Hkv;
     auto wait_part_timed = [&](int k) -> bool { return paged_wait_timed(&sh.part_full[k % kPartRing], (k / kPartRing) & 1, wait, kSiteItem); };
@@ -529,7 +532,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                     float x[kStates];                                    // scores in log2 units
 #pragma unroll
                     for (int g = 0; g < kStates / 16; ++g) {
-                        // column of (map, term, row): (map * kTerms + term) * kRows + row
+                        // column of (map, term, row) in S^T: (map * kTerms + term) * kRows + row
                         const int map = g * 16 / kRows, r0 = g * 16 % kRows;
                         uint32_t s0[16];
                         tmem_ld_x16(tS + map * kTerms * kRows + r0, s0);
@@ -613,7 +616,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                             tc_fence_after_sync();
 #pragma unroll 1
                             for (int g = 0; g < kCols / 16; ++g) {
-                                const int col = g * 16, st = col / (kTerms * kRows) * kRows + col % kRows;
+                                const int col = g * 16, st = col / (kPTerms * kRows) * kRows + col % kRows;
                                 uint32_t o[16];
                                 tmem_ld_x16(tO + col, o);
                                 tc_wait_ld();
@@ -650,7 +653,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                             }
 #pragma unroll
                             for (int term = 0; term < 3; ++term) {
-                                const int col = (r / kRows * kTerms + term) * kRows + r % kRows;
+                                const int col = (r / kRows * kPTerms + term) * kRows + r % kRows;
                                 st_shared_v4(sPw + col / 16 * Cfg::kPGroupBytes, __byte_perm(h[0], h[1], 0x7531), __byte_perm(h[2], h[3], 0x7531),
                                              __byte_perm(h[4], h[5], 0x7531), __byte_perm(h[6], h[7], 0x7531));      // the top bytes
                                 if (term < 2) {
@@ -665,9 +668,23 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                         }
                     } else {
 #pragma unroll
-                        for (int r = 0; r < kStates; r += 8)
-                            st_shared_v4(sPw + r / 8 * Cfg::kPGroupBytes, pack_bf16x2(x[r], x[r + 1]), pack_bf16x2(x[r + 2], x[r + 3]),
-                                         pack_bf16x2(x[r + 4], x[r + 5]), pack_bf16x2(x[r + 6], x[r + 7]));
+                        for (int r = 0; r < kStates; r += 8) {
+#pragma unroll
+                            for (int term = 0; term < kPTerms; ++term) {
+                                uint32_t h[4];
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) h[j] = pack_bf16x2(x[r + 2 * j], x[r + 2 * j + 1]);
+                                const int col = (r / kRows * kPTerms + term) * kRows + r % kRows;
+                                st_shared_v4(sPw + col / 8 * Cfg::kPGroupBytes, h[0], h[1], h[2], h[3]);
+                                if (term + 1 < kPTerms) {
+#pragma unroll
+                                    for (int j = 0; j < 4; ++j) {
+                                        x[r + 2 * j] -= __uint_as_float(h[j] << 16);
+                                        x[r + 2 * j + 1] -= __uint_as_float(h[j] & 0xffff0000u);
+                                    }
+                                }
+                            }
+                        }
                     }
                     fence_proxy_async_smem();
                     tc_fence_before_sync();
@@ -973,7 +990,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                     tc_wait_ld();
 #pragma unroll
                     for (int g = 0; g < kGroup; ++g) {
-                        const int col = (g0 + g) * 16, st = col / (kTerms * kRows) * kRows + col % kRows;
+                        const int col = (g0 + g) * 16, st = col / (kPTerms * kRows) * kRows + col % kRows;
 #pragma unroll
                         for (int j = 0; j < 16; ++j) y[st + j] = fmaf(sh.factor[v][st + j], __uint_as_float(o[g][j]), y[st + j]);
                     }
