@@ -89,6 +89,10 @@ class fa_paged_piece(ctypes.Structure):
 
 _I64x2 = ctypes.c_int64 * 2
 _I64x3 = ctypes.c_int64 * 3
+_I64x4 = ctypes.c_int64 * 4
+_I64x8 = ctypes.c_int64 * 8
+_I64x12 = ctypes.c_int64 * 12
+_SEQS_SIZE = ctypes.sizeof(fa_paged_seqs)
 _lib = None
 
 
@@ -472,7 +476,8 @@ class PagedCache:
                                   tuple(t.shape) != (k.shape[1],) or k.dtype == torch.bfloat16):
                 raise ValueError("scales are contiguous fp32 tensors of Hkv values on the cache's device, for e4m3 caches only")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.device, self.dqk, self.dv = k.device, k.shape[3], v.shape[3]
+        load()                            # the calls that take a cache rely on the library being there
+        self.device, self.Hkv, self.dqk, self.dv = k.device, k.shape[1], k.shape[3], v.shape[3]
         self.c = fa_paged_cache(ctypes.sizeof(fa_paged_cache), FA_CACHE_BF16 if k.dtype == torch.bfloat16 else FA_CACHE_E4M3,
                                 k.data_ptr(), v.data_ptr(), k.shape[0], k.shape[2], k.shape[1], k.shape[3], v.shape[3], 0,
                                 _I64x3(*k.stride()[:3]), _I64x3(*v.stride()[:3]),
@@ -502,31 +507,48 @@ class Rope:
         return self.address
 
 
+# The calls below are made once per layer and token: their checks are written to cost little (one stride array per call, the raw
+# stream, attributes read once).
+
+def _raw_stream(device) -> int:
+    """The current stream's handle on `device` (torch.cuda.current_stream without the object around it)."""
+    import torch
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
 def _seqs(h, cache, block_table, seq_lens):
     """The fa_paged_seqs of a call, after the checks that all paged calls share."""
     import torch
-    if block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.stride(1) != 1 or block_table.device != cache.device:
-        raise ValueError("block_table must be a 2-D int32 tensor with contiguous rows on the cache's device")
+    i32, device = torch.int32, cache.device
+    if block_table.dtype is not i32 or block_table.device != device or block_table.dim() != 2:
+        raise ValueError("block_table must be a 2-D int32 tensor on the cache's device")
     B, max_pages = block_table.shape
-    if seq_lens.dtype != torch.int32 or seq_lens.device != cache.device or seq_lens.shape != (B,) or not seq_lens.is_contiguous():
+    stride, inner = block_table.stride()
+    if inner != 1 and max_pages > 1:
+        raise ValueError("the rows of block_table must be contiguous")
+    if seq_lens.dtype is not i32 or seq_lens.device != device or seq_lens.shape != (B,) or not seq_lens.is_contiguous():
         raise ValueError("seq_lens must be a contiguous int32 tensor of one length per row of block_table")
-    if load().fa_device(h) != cache.device.index:
+    if _lib.fa_device(h) != device.index:
         raise ValueError("the handle belongs to another device than the cache")
-    stride = block_table.stride(0)
-    return fa_paged_seqs(ctypes.sizeof(fa_paged_seqs), B, block_table.data_ptr(), stride if stride > max_pages else max_pages,
-                         seq_lens.data_ptr(), max_pages, 0)
+    return fa_paged_seqs(_SEQS_SIZE, B, block_table.data_ptr(), stride if stride > max_pages else max_pages, seq_lens.data_ptr(),
+                         max_pages, 0)
 
 
 def _rows(t, cache, d, what):
-    """(token, head) strides of a [tokens, heads, d] bf16 tensor on the cache's device."""
+    """Tokens, heads and (token, head) strides of a [tokens, heads, d] bf16 tensor on the cache's device."""
     import torch
-    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.device != cache.device or t.shape[2] != d:
-        raise ValueError("%s must be a 3-D bf16 tensor [tokens, heads, %d] on the cache's device" % (what, d))
+    if t.dtype is not torch.bfloat16 or t.device != cache.device or t.dim() != 3:
+        raise ValueError("%s must be a 3-D bf16 tensor on the cache's device" % what)
+    n, heads, width = t.shape
     st, sh, sd = t.stride()
-    if sd != 1:
-        raise ValueError("the last dimension of %s must be contiguous" % what)
+    if width != d or sd != 1:
+        raise ValueError("the last dimension of %s must be %d contiguous values" % (what, d))
     # (the stride of a dimension of one row is whatever the view left; the library wants it to be valid)
-    return _I64x2(st if t.shape[0] > 1 else max(d, (st + 7) // 8 * 8), sh if t.shape[1] > 1 else max(d, (sh + 7) // 8 * 8))
+    if n == 1:
+        st = max(d, (st + 7) // 8 * 8)
+    if heads == 1:
+        sh = max(d, (sh + 7) // 8 * 8)
+    return n, heads, st, sh
 
 
 def append_paged(h, k, v, cache: PagedCache, block_table, seq_lens, *, cu_seqlens=None, q=None, q_out=None, rope: Rope = None):
@@ -537,48 +559,58 @@ def append_paged(h, k, v, cache: PagedCache, block_table, seq_lens, *, cu_seqlen
     """
     import torch
     seqs = _seqs(h, cache, block_table, seq_lens)
-    ks, vs = _rows(k, cache, cache.dqk, "k"), _rows(v, cache, cache.dv, "v")
-    total = k.shape[0]
-    if v.shape[0] != total or k.shape[1] != cache.c.Hkv or v.shape[1] != cache.c.Hkv:
+    total, Hk, kt, kh = _rows(k, cache, cache.dqk, "k")
+    Tv, Hv, vt, vh = _rows(v, cache, cache.dv, "v")
+    if Tv != total or Hk != cache.Hkv or Hv != Hk:
         raise ValueError("k and v must have the same tokens and the cache's heads")
-    if cu_seqlens is not None and (cu_seqlens.dtype != torch.int32 or cu_seqlens.device != cache.device or
-                                   cu_seqlens.shape != (seqs.B + 1,) or not cu_seqlens.is_contiguous()):
-        raise ValueError("cu_seqlens must be a contiguous int32 tensor of B + 1 offsets on the cache's device")
-    if rope is not None and rope.device != cache.device:
-        raise ValueError("the rotation table must be on the cache's device")
-    q_ptr = qo_ptr = qs = qos = None
-    Hq = 0
+    cu_ptr = None
+    if cu_seqlens is not None:
+        if (cu_seqlens.dtype is not torch.int32 or cu_seqlens.device != cache.device or cu_seqlens.shape != (seqs.B + 1,) or
+                not cu_seqlens.is_contiguous()):
+            raise ValueError("cu_seqlens must be a contiguous int32 tensor of B + 1 offsets on the cache's device")
+        cu_ptr = cu_seqlens.data_ptr()
+    rope_ptr = None
+    if rope is not None:
+        if rope.device != cache.device:
+            raise ValueError("the rotation table must be on the cache's device")
+        rope_ptr = rope.struct_for(cache.dqk)
+    q_ptr = qo_ptr = None
+    Hq = qt = qh = ot = oh = 0
     if q is not None:
-        qs, Hq = _rows(q, cache, cache.dqk, "q"), q.shape[1]
-        if q.shape[0] != total:
+        Tq, Hq, qt, qh = _rows(q, cache, cache.dqk, "q")
+        if Tq != total:
             raise ValueError("q must have the tokens of k")
         if q_out is None:
             q_out = torch.empty((total, Hq, cache.dqk), dtype=torch.bfloat16, device=q.device)
-        elif q_out.shape != q.shape:
+        To, Ho, ot, oh = _rows(q_out, cache, cache.dqk, "q_out")
+        if To != total or Ho != Hq:
             raise ValueError("q_out must have q's shape")
-        qos = _rows(q_out, cache, cache.dqk, "q_out")
         q_ptr, qo_ptr = q.data_ptr(), q_out.data_ptr()
     elif q_out is not None:
         raise ValueError("q_out without q")
-    st = load().fa_append_paged(h, cache.address, ctypes.addressof(seqs), None if cu_seqlens is None else cu_seqlens.data_ptr(), total,
-                                k.data_ptr(), v.data_ptr(), q_ptr, qo_ptr, Hq, ks, vs, qs, qos,
-                                None if rope is None else rope.struct_for(cache.dqk),
-                                torch.cuda.current_stream(cache.device).cuda_stream)
+    strides = _I64x8(kt, kh, vt, vh, qt, qh, ot, oh)
+    at = ctypes.addressof(strides)
+    st = _lib.fa_append_paged(h, cache.address, ctypes.addressof(seqs), cu_ptr, total, k.data_ptr(), v.data_ptr(), q_ptr, qo_ptr, Hq,
+                              at, at + 16, at + 32, at + 48, rope_ptr, _raw_stream(cache.device))
     if st != FA_OK:
         raise FaError(st, "fa_append_paged")
     return q_out
 
 
 def _paged_out(q, cache, seqs, out):
+    """(Hq, tokens, Sq, stride array, out) of a paged attention call."""
     import torch
-    T, Hq = q.shape[0], q.shape[1]
+    T, Hq, qt, qh = _rows(q, cache, cache.dqk, "q")
     if seqs.B == 0 or T == 0 or T % seqs.B:
         raise ValueError("q must hold the same number of tokens for every sequence")
     if out is None:
-        return torch.empty((T, Hq, cache.dv), dtype=torch.bfloat16, device=q.device)
-    if tuple(out.shape) != (T, Hq, cache.dv):
-        raise ValueError("out must have shape %s" % ((T, Hq, cache.dv),))
-    return out
+        out = torch.empty((T, Hq, cache.dv), dtype=torch.bfloat16, device=q.device)
+        ot, oh = Hq * cache.dv, cache.dv
+    else:
+        To, Ho, ot, oh = _rows(out, cache, cache.dv, "out")
+        if To != T or Ho != Hq:
+            raise ValueError("out must have shape %s" % ((T, Hq, cache.dv),))
+    return Hq, T, T // seqs.B, _I64x4(qt, qh, ot, oh), out
 
 
 def forward_paged(h, q, cache: PagedCache, block_table, seq_lens, *, scale: float = 0.0, out=None, want_lse=True):
@@ -586,14 +618,11 @@ def forward_paged(h, q, cache: PagedCache, block_table, seq_lens, *, scale: floa
     lse [Hq, B*Sq] fp32 or None)."""
     import torch
     seqs = _seqs(h, cache, block_table, seq_lens)
-    qs = _rows(q, cache, cache.dqk, "q")
-    out = _paged_out(q, cache, seqs, out)
-    os_ = _rows(out, cache, cache.dv, "out")
-    T, Hq = q.shape[0], q.shape[1]
+    Hq, T, Sq, strides, out = _paged_out(q, cache, seqs, out)
     lse = torch.empty((Hq, T), dtype=torch.float32, device=q.device) if want_lse else None
-    st = load().fa_forward_paged(h, cache.address, ctypes.addressof(seqs), q.data_ptr(), out.data_ptr(),
-                                 None if lse is None else lse.data_ptr(), Hq, T // seqs.B, scale, qs, os_,
-                                 torch.cuda.current_stream(cache.device).cuda_stream)
+    at = ctypes.addressof(strides)
+    st = _lib.fa_forward_paged(h, cache.address, ctypes.addressof(seqs), q.data_ptr(), out.data_ptr(),
+                               None if lse is None else lse.data_ptr(), Hq, Sq, scale, at, at + 16, _raw_stream(cache.device))
     if st != FA_OK:
         raise FaError(st, "fa_forward_paged")
     return out, lse
@@ -612,15 +641,12 @@ def _diff(lam, norm_weight, eps, out_scale, Hq, device):
 def forward_paged_diff(h, q, cache: PagedCache, block_table, seq_lens, lam, *, norm_weight=None, eps: float = 1e-5,
                        out_scale: float = 1.0, scale: float = 0.0, out=None):
     """Differential attention of the last tokens over a paged cache whose heads are two maps of 64 and values of 128; returns O."""
-    import torch
     seqs = _seqs(h, cache, block_table, seq_lens)
-    qs = _rows(q, cache, cache.dqk, "q")
-    out = _paged_out(q, cache, seqs, out)
-    os_ = _rows(out, cache, cache.dv, "out")
-    T, Hq = q.shape[0], q.shape[1]
+    Hq, T, Sq, strides, out = _paged_out(q, cache, seqs, out)
     diff = _diff(lam, norm_weight, eps, out_scale, Hq, cache.device)
-    st = load().fa_forward_paged_diff(h, cache.address, ctypes.addressof(seqs), q.data_ptr(), out.data_ptr(), Hq, T // seqs.B, scale,
-                                      ctypes.addressof(diff), qs, os_, torch.cuda.current_stream(cache.device).cuda_stream)
+    at = ctypes.addressof(strides)
+    st = _lib.fa_forward_paged_diff(h, cache.address, ctypes.addressof(seqs), q.data_ptr(), out.data_ptr(), Hq, Sq, scale,
+                                    ctypes.addressof(diff), at, at + 16, _raw_stream(cache.device))
     if st != FA_OK:
         raise FaError(st, "fa_forward_paged_diff")
     return out
@@ -631,29 +657,37 @@ def forward_diff(h, q, k, v, lam, *, causal: bool, norm_weight=None, eps: float 
     """Differential attention on torch CUDA tensors (bf16, logical shape [B, H, S, 128], any batch/head/row strides; the two
     halves of a query and key are its two maps); returns O, in q's memory layout when `out` is not given."""
     import torch
-    for t in (q, k, v):
-        if t.dtype != torch.bfloat16 or not t.is_cuda or t.dim() != 4 or t.device != q.device:
-            raise ValueError("q, k, v must be 4-D bf16 tensors on one CUDA device")
+    lib, device, bf16 = load(), q.device, torch.bfloat16
+    if not q.is_cuda or any(t.dtype is not bf16 or t.dim() != 4 or t.device != device for t in (q, k, v)):
+        raise ValueError("q, k, v must be 4-D bf16 tensors on one CUDA device")
     B, Hq, Sq, dqk = q.shape
     _, Hkv, Sk, dv = v.shape
-    if tuple(k.shape) != (B, Hkv, Sk, dqk) or v.shape[0] != B:
+    if k.shape != (B, Hkv, Sk, dqk) or v.shape[0] != B:
         raise ValueError("k and v must have q's batch, the same heads and rows, and k q's head size")
-    if load().fa_device(h) != q.device.index:
+    if lib.fa_device(h) != device.index:
         raise ValueError("the handle belongs to another device than the tensors")
+    shape = (B, Hq, Sq, dv)
     if out is None:
-        order = sorted(range(3), key=lambda i: -q.stride(i)) + [3]
-        shape = (B, Hq, Sq, dv)
-        buf = torch.empty([shape[i] for i in order], dtype=torch.bfloat16, device=q.device)
-        out = buf.permute([order.index(i) for i in range(4)])
-    elif tuple(out.shape) != (B, Hq, Sq, dv) or out.dtype != torch.bfloat16 or out.device != q.device:
-        raise ValueError("out must be a bf16 tensor of shape %s on q's device" % ((B, Hq, Sq, dv),))
+        if q.is_contiguous():
+            out = torch.empty(shape, dtype=bf16, device=device)
+        else:
+            order = sorted(range(3), key=lambda i: -q.stride(i)) + [3]
+            buf = torch.empty([shape[i] for i in order], dtype=bf16, device=device)
+            out = buf.permute([order.index(i) for i in range(4)])
+    elif out.shape != shape or out.dtype is not bf16 or out.device != device:
+        raise ValueError("out must be a bf16 tensor of shape %s on q's device" % (shape,))
+    strides = []
     for t in (q, k, v, out):
-        if t.stride(3) != 1:
+        s = t.stride()
+        if s[3] != 1:
             raise ValueError("the last dimension must be contiguous")
-    diff = _diff(lam, norm_weight, eps, out_scale, Hq, q.device)
-    st = load().fa_forward_diff(h, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), B, Hq, Hkv, Sq, Sk, dqk, dv,
-                                int(bool(causal)), scale, ctypes.addressof(diff), _I64x3(*q.stride()[:3]), _I64x3(*k.stride()[:3]),
-                                _I64x3(*v.stride()[:3]), _I64x3(*out.stride()[:3]), torch.cuda.current_stream(q.device).cuda_stream)
+        # (a dimension of one entry may have any stride, the library wants a valid one; a row holds 128 values)
+        strides += s[:3] if min(t.shape) > 1 else [x if n > 1 else max(128, (x + 7) // 8 * 8) for x, n in zip(s[:3], t.shape)]
+    strides = _I64x12(*strides)
+    at = ctypes.addressof(strides)
+    diff = _diff(lam, norm_weight, eps, out_scale, Hq, device)
+    st = lib.fa_forward_diff(h, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), B, Hq, Hkv, Sq, Sk, dqk, dv, 1 if causal else 0,
+                             scale, ctypes.addressof(diff), at, at + 24, at + 48, at + 72, _raw_stream(device))
     if st != FA_OK:
         raise FaError(st, "fa_forward_diff")
     return out
