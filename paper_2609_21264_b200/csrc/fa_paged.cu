@@ -276,17 +276,34 @@ fa_status fa_append_paged(fa_handle* h, const fa_paged_cache* cache, const fa_pa
         p.max_pos = rope->max_pos; p.rot_dim = rope->dim; p.rot_offset = rope->offset; p.span = rope->span;
         p.interleaved = rope->interleaved ? 1 : 0;
     }
-    p.span_units = p.span / 8 - ((rope && !p.interleaved) ? p.rot_dim / 16 : 0);
+    // the span's vectors before, in and behind its turned part, and the units that they are cut into
+    const int before = p.rot_offset / 8, behind = (p.span - p.rot_offset - p.rot_dim) / 8;
+    p.before_step = before % 2 == 0 ? 2 : 1;
+    p.behind_step = behind % 2 == 0 ? 2 : 1;
+    p.before_units = before / p.before_step;
+    p.turned_units = p.rot_dim / 16;
+    p.span_units = p.before_units + p.turned_units + behind / p.behind_step;
     p.head_units = p.span_units * (p.dqk / p.span);
     p.k_units = p.Hkv * p.head_units;
-    p.v_units = p.Hkv * (p.dv / 8);
-    p.q_units = p.Hq * p.head_units;
+    p.v_units = p.Hkv * (p.dv / 16);
+    p.units = p.k_units + p.v_units + p.Hq * p.head_units;
+    if (p.units > 65535) return FA_ERR_UNSUPPORTED;          // (the quotients below are exact up to there)
+    auto magic = [](int d) -> uint32_t { return d == 1 ? 0u : static_cast<uint32_t>((0x100000000ull + d - 1) / d); };
+    p.head_magic = magic(p.head_units);
+    p.span_magic = magic(p.span_units);
+    p.v_magic = magic(p.dv / 16);
     p.status = h->status_dev;
+    // Tokens of a block: enough blocks for every SM's eight first, then up to kAppendMaxTokens, so that a block's look-ups are
+    // paid once for many tokens.
+    const long long slots = 8ll * h->num_sms;
+    p.tokens = static_cast<int>((total + slots - 1) / slots);
+    if (p.tokens > fa::kAppendMaxTokens) p.tokens = fa::kAppendMaxTokens;
     h->last_kernel = "fa_append_paged";
     h->last_splits = 1;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (cache->type == FA_CACHE_E4M3) return launch(h, fa::fa_append_paged_kernel<true>, total, 256, 0, st, p);
-    return launch(h, fa::fa_append_paged_kernel<false>, total, 256, 0, st, p);
+    const long long blocks = (static_cast<long long>(total) + p.tokens - 1) / p.tokens;
+    if (cache->type == FA_CACHE_E4M3) return launch(h, fa::fa_append_paged_kernel<true>, blocks, fa::kAppendThreads, 0, st, p);
+    return launch(h, fa::fa_append_paged_kernel<false>, blocks, fa::kAppendThreads, 0, st, p);
 }
 
 fa_status fa_forward_paged(fa_handle* h, const fa_paged_cache* cache, const fa_paged_seqs* seqs, const void* Q, void* O, float* lse,
