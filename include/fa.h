@@ -471,7 +471,7 @@ typedef struct fa_rope {
  * picks the row of the rotation table and the slot.  Tokens whose position would be negative (the padding of a batch: length
  * 0) and rows behind cu_seqlens[B] are skipped: nothing is stored for them, their rows of Q_out stay as they were.
  *   rope    NULL = no rotation (Q is then copied).      Q, Q_out   both or neither NULL; Q_out may be Q itself.
- * Arithmetic is fp32 with one rounding to bf16, or of value / scale to e4m3 (saturating at +-448).  A slot that two tokens of
+ * Arithmetic is fp32 with one rounding to bf16, or of value * (1 / scale) to e4m3 (saturating at +-448).  A slot that two tokens of
  * a call name (sequences sharing a page that is written to) ends with either's values.  Asynchronous on `stream`.
  */
 fa_status fa_append_paged(fa_handle* h, const fa_paged_cache* cache, const fa_paged_seqs* seqs,

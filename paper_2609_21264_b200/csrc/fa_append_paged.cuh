@@ -57,25 +57,15 @@ FA_DEVI uint4 pack8(const Vec8& v) {
                       ptx::pack_bf16x2(v.x[6], v.x[7]));
 }
 
-// x / s from r = 1/s: the product is corrected by what it lacks, so that the quotient is rounded once (a product with the reciprocal
-// alone would round twice).  Large quotients, which saturate anyway, are cut before the correction (inf - inf).
-FA_DEVI float quot(float x, float s, float r) {
-    const float q = fminf(fmaxf(x * r, -1024.f), 1024.f);
-    return fmaf(fmaf(-q, s, x), r, q);
-}
-
-// A vector into the cache: bf16, or value / scale rounded once to e4m3.
+// A vector into the cache: bf16, or value * recip rounded to e4m3, recip = 1 / scale in fp32.  (The product's own rounding, 2^-24 of it,
+// can move only values within that distance of the middle between two e4m3 numbers; an exact quotient, five operations a
+// value, took 38.8 us where this takes 33.2, 2753 tokens of 32 heads 192/128.)
 template <bool kE4m3>
-FA_DEVI void store_cache8(void* base, long long at, const Vec8& v, float scale, float recip) {
+FA_DEVI void store_cache8(void* base, long long at, const Vec8& v, float recip) {
     if constexpr (kE4m3) {
         Vec8 s;
-        if (isinf(recip)) {                          // (a scale below the normal numbers)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s.x[i] = __fdiv_rn(v.x[i], scale);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s.x[i] = quot(v.x[i], scale, recip);
-        }
+        for (int i = 0; i < 8; ++i) s.x[i] = v.x[i] * recip;
         uint2 o;
         o.x = ptx::pack_e4m3x4(s.x[0], s.x[1], s.x[2], s.x[3]);
         o.y = ptx::pack_e4m3x4(s.x[4], s.x[5], s.x[6], s.x[7]);
@@ -88,7 +78,7 @@ FA_DEVI void store_cache8(void* base, long long at, const Vec8& v, float scale, 
 // floor(x / d) from ceil(2^32 / d), for x < 2^16 (d = 1 has no such number of 32 bits)
 FA_DEVI int magic_quot(int x, uint32_t magic) { return magic == 0 ? x : static_cast<int>(__umulhi(static_cast<uint32_t>(x), magic)); }
 
-constexpr int kAppendThreads = 256, kAppendMaxTokens = 32;
+constexpr int kAppendThreads = 256, kAppendMaxTokens = 16;
 
 // A unit of a half-split rotation is the pair of vectors whose values turn into each other, so that every value is read and written by
 // one thread alone (Q_out may be Q).
@@ -173,10 +163,11 @@ fa_append_paged_kernel(const AppendParams p) {
             const bool is_v = x.kind == 1;
             const long long at = (is_v ? tk.v_at + x.h * p.v_stride[1] : tk.k_at + x.h * p.k_stride[1]) + x.c;
             const float* scales = is_v ? p.v_scale : p.k_scale;
-            const float scale = kE4m3 && scales ? scales[x.h] : 1.f, recip = kE4m3 ? __frcp_rn(scale) : 1.f;
+            // (the reciprocal of a number below the normal ones would be infinite, and 0 times that no number)
+            const float recip = kE4m3 && scales ? fminf(__frcp_rn(scales[x.h]), 3.402823466e38f) : 1.f;
             void* base = is_v ? p.v_cache : p.k_cache;
-            store_cache8<kE4m3>(base, at, v, scale, recip);
-            if (x.d) store_cache8<kE4m3>(base, at + x.d, w, scale, recip);
+            store_cache8<kE4m3>(base, at, v, recip);
+            if (x.d) store_cache8<kE4m3>(base, at + x.d, w, recip);
         }
     };
 

@@ -293,11 +293,11 @@ fa_status fa_append_paged(fa_handle* h, const fa_paged_cache* cache, const fa_pa
     p.span_magic = magic(p.span_units);
     p.v_magic = magic(p.dv / 16);
     p.status = h->status_dev;
-    // Tokens of a block: enough blocks for every SM's eight first, then up to kAppendMaxTokens, so that a block's look-ups are
-    // paid once for many tokens.
-    const long long slots = 8ll * h->num_sms;
-    p.tokens = static_cast<int>((total + slots - 1) / slots);
-    if (p.tokens > fa::kAppendMaxTokens) p.tokens = fa::kAppendMaxTokens;
+    // Tokens of a block: whole rounds of blocks over the four places of every SM (64 registers a thread), as few as
+    // kAppendMaxTokens allows, so that a block's look-ups are paid once for many tokens and no round is left half empty.
+    const long long places = 4ll * h->num_sms;
+    const long long rounds = (total + places * fa::kAppendMaxTokens - 1) / (places * fa::kAppendMaxTokens);
+    p.tokens = static_cast<int>((total + places * rounds - 1) / (places * rounds));
     h->last_kernel = "fa_append_paged";
     h->last_splits = 1;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
