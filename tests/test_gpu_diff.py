@@ -122,3 +122,61 @@ def test_refusals(handle):
         b.forward_diff(handle, q, k, v[:, :1], lam, causal=True)
     with pytest.raises(ValueError):
         b.forward_diff(handle, q, k, v, lam[:3], causal=True)
+
+
+def test_prompt_then_tokens_over_the_paged_cache():
+    """A prompt through forward_diff and the same tokens one by one through the paged cache give the same rows (to the rounding of
+    their probabilities)."""
+    from paged_util import BF16_HALF, FP32_SLACK, rope_table
+    from paper_2609_21264_b200 import binding as b
+    Hq, Hkv, S, page = 4, 2, 45, 16
+    g = torch.Generator().manual_seed(12)
+    q, k, v = (torch.randn(S, H, 128, generator=g).to(torch.bfloat16).cuda() for H in (Hq, Hkv, Hkv))
+    lam, w = torch.rand(Hq, device="cuda"), torch.rand(128, device="cuda") + 0.5
+    kc, vc = (torch.zeros(3, page, Hkv, 128, dtype=torch.bfloat16, device="cuda").permute(0, 2, 1, 3) for _ in range(2))
+    cache, rope = b.PagedCache(kc, vc), b.Rope(rope_table(S, 64), span=64)        # each map of 64 rotated by itself
+    table = torch.tensor([[2, 0, 1]], dtype=torch.int32, device="cuda")
+    h = b.fa_create()
+    rows = []
+    qr = torch.empty_like(q)
+    for t in range(S):
+        lens = torch.tensor([t + 1], dtype=torch.int32, device="cuda")
+        b.append_paged(h, k[t:t + 1], v[t:t + 1], cache, table, lens, q=q[t:t + 1], q_out=qr[t:t + 1], rope=rope)
+        rows.append(b.forward_paged_diff(h, qr[t:t + 1], cache, table, lens, lam, norm_weight=w, out_scale=0.8))
+    kr = torch.cat([kc[i].transpose(0, 1) for i in (2, 0, 1)])[:S]
+    vr = torch.cat([vc[i].transpose(0, 1) for i in (2, 0, 1)])[:S]
+    assert torch.equal(vr, v)
+    one = lambda x: x.transpose(0, 1)[None]  # noqa: E731
+    o = b.forward_diff(h, one(qr), one(kr), one(v), lam, causal=True, norm_weight=w, out_scale=0.8)
+    ok(h)
+    got = torch.cat(rows)
+    for head in range(Hq):
+        Y, A = diff_rows(qr[:, head].cpu().double(), kr[:, head // 2].cpu().double(), v[:, head // 2].cpu().double(), lam[head].item(), 0.125,
+                         torch.arange(S))
+        O, tol = diff_norm(Y, A, w.cpu().double(), 1e-5, 0.8)
+        assert_close(got[:, head], O, tol, "paged")
+        assert_close(o[0, head], O, tol, "prompt")
+    b.fa_destroy(h)
+
+
+def test_a_wait_that_runs_out_is_reported_and_the_handle_recovers():
+    from paper_2609_21264_b200 import binding as b
+    g = torch.Generator().manual_seed(13)
+    q, k, v = heads(2, 16, 400, g, False), heads(2, 4, 400, g, False), heads(2, 4, 400, g, False)
+    lam = torch.rand(16, device="cuda")
+    h, fresh = b.fa_create(flags=b.FA_FLAG_DEBUG_DROP_V_LOAD, wait_limit_ms=20), b.fa_create()
+    try:
+        want = b.forward_diff(fresh, q, k, v, lam, causal=True)
+        ok(fresh)
+        b.forward_diff(h, q, k, v, lam, causal=True)
+        torch.cuda.synchronize()
+        st, site = b.fa_last_status(h)
+        assert st == b.FA_ERR_DEVICE_TIMEOUT and site != 0
+        assert b.fa_debug_set_drop_v_load(h, False) == b.FA_OK
+        for _ in range(3):
+            o = b.forward_diff(h, q, k, v, lam, causal=True)
+            ok(h)
+            assert torch.equal(o, want)
+    finally:
+        b.fa_destroy(h)
+        b.fa_destroy(fresh)

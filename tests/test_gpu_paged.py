@@ -318,3 +318,144 @@ def test_refusals(handle):
         b.forward_paged(handle, q[:, :3], cache, table, lens)
     with pytest.raises(ValueError):
         b.forward_paged_diff(handle, q, cache, table, lens, lam[:2])
+
+
+def test_prompts_then_tokens_step_by_step():
+    """The operators as a server uses them: ragged prompts are appended (rotated on the way) and attended to in one packed call, then
+    four tokens a sequence are appended and attended to one at a time; every row against attention in 64 bits over the sequence's
+    whole history, rotated in 64 bits from what was appended."""
+    from paged_util import BF16_HALF, FP32_SLACK, rope_table, softmax64, turned
+    from paper_2609_21264_b200 import binding as b
+    Hq, Hkv, d, page = 8, 2, 128, 16
+    prompts, steps = [37, 150, 16], 4
+    B, G = len(prompts), 4
+    final = [n + steps for n in prompts]
+    k, v, table, _, _, _ = pool(final, page, Hkv, d, d, False, False, 70)
+    cache, tab = b.PagedCache(k, v), rope_table(256, d)
+    rope, cu = b.Rope(tab), torch.tensor([0, 37, 187, 203], dtype=torch.int32, device="cuda")
+    history = [torch.zeros(0, Hq + 2 * Hkv, d, dtype=torch.float64) for _ in range(B)]
+    h = b.fa_create()
+
+    def check(seq, rows, o, lse):
+        x = history[seq]
+        n = x.shape[0]
+        q, _ = turned(x[:, :Hq], tab[:n].cpu().double(), d, 0, d, False)
+        kk, _ = turned(x[:, Hq:Hq + Hkv], tab[:n].cpu().double(), d, 0, d, False)
+        for head in range(Hq):
+            # queries and keys as they are after their rounding to bf16
+            p, L = softmax64(q[n - rows:, head].bfloat16().double(), kk[:, head // G].bfloat16().double(), d ** -0.5, torch.arange(n - rows, n))
+            O, A = p @ x[:, Hq + Hkv + head // G], p @ x[:, Hq + Hkv + head // G].abs()
+            # a rotated value next to the middle between two bf16 numbers may be rounded either way: one step of one factor in a score
+            slack = FP32_SLACK + 2 * BF16_HALF * 1e-1
+            assert ((o[:, head].cpu().double() - O).abs() <= BF16_HALF * O.abs() + (BF16_HALF + slack) * A).all()
+            assert ((lse[head].cpu().double() - L).abs() <= slack).all()
+
+    x = torch.randn(203, Hq + 2 * Hkv, d, device="cuda").bfloat16()
+    lens = torch.tensor(prompts, dtype=torch.int32, device="cuda")
+    qr = b.append_paged(h, x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], cache, table, lens, cu_seqlens=cu, q=x[:, :Hq], rope=rope)
+    kr = torch.cat([torch.cat([k[int(table[i, j])].transpose(0, 1) for j in range(-(-n // page))])[:n] for i, n in enumerate(prompts)])
+    o, lse = b.forward_varlen(h, qr, kr.contiguous(), x[:, Hq + Hkv:].contiguous(), cu, cu, max(prompts), causal=True)
+    ok(h)
+    for i in range(B):
+        here = slice(int(cu[i]), int(cu[i + 1]))
+        history[i] = x[here].cpu().double()
+        check(i, prompts[i], o[here], lse[:, here])
+    for step in range(steps):
+        x = torch.randn(B, Hq + 2 * Hkv, d, device="cuda").bfloat16()
+        lens += 1
+        qr = b.append_paged(h, x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], cache, table, lens, q=x[:, :Hq], rope=rope)
+        o, lse = b.forward_paged(h, qr, cache, table, lens)
+        ok(h)
+        for i in range(B):
+            history[i] = torch.cat([history[i], x[i:i + 1].cpu().double()])
+            check(i, 1, o[i:i + 1], lse[:, i:i + 1])
+    b.fa_destroy(h)
+
+
+@pytest.mark.parametrize("e4m3,diff", [(False, False), (True, False), (False, True)], ids=["bf16", "e4m3", "diff"])
+def test_a_wait_that_runs_out_is_reported_and_the_handle_recovers(e4m3, diff):
+    """The hook leaves out each CTA's first V tile: the launch returns, the host reads FA_ERR_DEVICE_TIMEOUT, and the next launch
+    through the same handle (shared row blocks and their counters among its work) is right."""
+    from paper_2609_21264_b200 import binding as b
+    lens = [700, 3000, 40, 0, 129]
+    k, v, table, lens_t, ks, vs = pool(lens, 16, 2, 128, 128, e4m3, False, 80)
+    q = torch.randn(len(lens), 8, 128, device="cuda").bfloat16()
+    cache, lam = b.PagedCache(k, v, ks, vs), torch.rand(8, device="cuda")
+    h, fresh = b.fa_create(flags=b.FA_FLAG_DEBUG_DROP_V_LOAD, wait_limit_ms=20), b.fa_create()
+
+    def call(handle):
+        if diff:
+            return b.forward_paged_diff(handle, q, cache, table, lens_t, lam)
+        return b.forward_paged(handle, q, cache, table, lens_t)[0]
+
+    try:
+        want = call(fresh)
+        ok(fresh)
+        call(h)
+        torch.cuda.synchronize()
+        st, site = b.fa_last_status(h)
+        assert st == b.FA_ERR_DEVICE_TIMEOUT and site != 0
+        assert b.fa_debug_set_drop_v_load(h, False) == b.FA_OK
+        for _ in range(3):
+            o = call(h)
+            ok(h)
+            assert torch.equal(o, want)
+    finally:
+        b.fa_destroy(h)
+        b.fa_destroy(fresh)
+
+
+def test_small_scratch_and_two_handles_on_two_streams():
+    """A handle whose scratch holds a few partial results uses fewer CTAs; two handles may run at the same time."""
+    from paper_2609_21264_b200 import binding as b
+    lens = [9000, 200, 4000]
+    k, v, table, lens_t, _, _ = pool(lens, 64, 2, 128, 128, False, True, 81)
+    q = torch.randn(3, 16, 128, device="cuda").bfloat16()
+    cache = b.PagedCache(k, v)
+    ref = paged_reference(q, k, v, None, None, table, lens, 1, 128 ** -0.5)
+    handles = [b.fa_create(scratch_bytes=6 * 16 * 130 * 4), b.fa_create()]
+    streams = [torch.cuda.Stream() for _ in handles]
+    try:
+        for s in streams:
+            s.wait_stream(torch.cuda.current_stream())
+        outs = []
+        for _ in range(4):
+            for h, s in zip(handles, streams):
+                with torch.cuda.stream(s):
+                    outs.append(b.forward_paged(h, q, cache, table, lens_t))
+        for h in handles:
+            ok(h)
+        for o, lse in outs:
+            assert_attention(o, lse, *ref)
+        assert all(torch.equal(outs[0][0], outs[i][0]) for i in (2, 4, 6)) and all(torch.equal(outs[1][0], outs[i][0]) for i in (3, 5, 7))
+        tiny = b.fa_create(scratch_bytes=1024)
+        with pytest.raises(b.FaError) as e:
+            b.forward_paged(tiny, q, cache, table, lens_t)
+        assert e.value.status == b.FA_ERR_UNSUPPORTED
+        b.fa_destroy(tiny)
+    finally:
+        torch.cuda.synchronize()
+        for h in handles:
+            b.fa_destroy(h)
+
+
+def test_cache_of_more_than_2_31_elements(handle):
+    """Pages whose elements lie behind 2^31, of a pool of either order."""
+    from paper_2609_21264_b200 import binding
+    pages, Hkv, page, d = 17000, 8, 128, 128
+    for heads_first in (False, True):
+        shape = (pages, Hkv, page, d) if heads_first else (pages, page, Hkv, d)
+        k, v = (torch.empty(shape, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        if not heads_first:
+            k, v = k.permute(0, 2, 1, 3), v.permute(0, 2, 1, 3)
+        table = torch.tensor([[pages - 1, 3, pages - 2]], dtype=torch.int32, device="cuda")
+        for t in (k, v):
+            t[table[0].long()] = torch.randn(3, Hkv, page, d, device="cuda").bfloat16()
+        q = torch.randn(1, 16, d, device="cuda").bfloat16()
+        lens = torch.tensor([300], dtype=torch.int32, device="cuda")
+        o, lse = binding.forward_paged(handle, q, binding.PagedCache(k, v), table, lens)
+        ok(handle)
+        small_k, small_v = k[table[0].long()], v[table[0].long()]
+        assert_attention(o, lse, *paged_reference(q, small_k, small_v, None, None, torch.tensor([[0, 1, 2]]), [300], 1, d ** -0.5))
+        del k, v
+        torch.cuda.empty_cache()
