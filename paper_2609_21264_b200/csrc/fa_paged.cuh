@@ -160,8 +160,10 @@ __host__ __device__ inline bool paged_entry(const PagedParams& p, int cta, int s
 
 constexpr int kPartRing = 8, kMergePieces = 8;
 
-// Registers per thread after the per-role reallocation (512 threads start with 128 each): 128 x 80 + 256 x 152 + 128 x 128 = 65536.
-constexpr int kPagedRegsOther = 80, kPagedRegsSoftmax = 152;
+// Registers per thread after the per-role reallocation (512 threads start with 128 each): 128 x 80 + 256 x 136 + 128 x 160 = 65536;
+// with 64 states per softmax thread 256 x 152 and 128 x 128.
+constexpr int kPagedRegsOther = 80;
+__host__ __device__ constexpr int paged_regs_softmax(int states) { return states <= 32 ? 136 : 152; }
 
 template <int kRows, int kMaps>
 struct PagedShared {
@@ -173,7 +175,7 @@ struct PagedShared {
     PagedEntry part[kPartRing];
     uint32_t tmem_base;
     PagedWait wait;
-    uint32_t is_last;
+    uint32_t is_last[2];          // of even and odd parts
     int start_b, start_base;
     int warp_sums[4], warp_longest[4];
     alignas(16) float c[2][kRows];                       // per query buffer: factor of a score (log2 units)
@@ -186,7 +188,6 @@ struct PagedShared {
     float stat_m[kPartRing][2][kMaps * kRows], stat_l[kPartRing][2][kMaps * kRows];      // [part][group]
     // of the result warps
     float factor[2][kMaps * kRows];
-    float out_l[kMaps * kRows];
     float piece_m[kMergePieces][kMaps * kRows], piece_l[kMergePieces][kMaps * kRows];
     float sq[4][kRows];
     long long out_at[kRows];                             // offset of the row in O (-1: a padding row)
@@ -499,7 +500,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         // ============================================================ softmax groups
         // The four warps of a group stay together through their barriers: after a wait that ran out they go on to the end of
         // the part without waiting (results are invalid then, every access stays in bounds) and leave together.
-        setmaxnreg_inc<kPagedRegsSoftmax>();
+        setmaxnreg_inc<paged_regs_softmax(kStates)>();
         const int w = (warp >> 2) - 1, key = tid & 127, wq = warp & 3;
         const uint32_t lane_sel = static_cast<uint32_t>(wq * 32) << 16;
         int mine_n = 0;                                                  // tiles this group has done
@@ -723,6 +724,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         }
     } else {
         // ============================================================ list of parts, query rows, results (thread = output column)
+        if constexpr (kStates <= 32) setmaxnreg_inc<160>();
         const int key = tid & 127, wq = warp & 3;
         const uint32_t lane_sel = static_cast<uint32_t>(wq * 32) << 16;
         constexpr uint32_t kBar = 3;
@@ -917,8 +919,9 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             if (k >= 0 && key == 0 && sh.part[k % kPartRing].slot >= 0) {
                 const PagedEntry& mine_part = sh.part[k % kPartRing];
                 const unsigned int got = *static_cast<volatile unsigned int*>(p.arrivals + mine_part.first_cta);
-                sh.is_last = got == static_cast<unsigned int>(mine_part.pieces - 1) ? 1u : 0u;
-                if (sh.is_last) {
+                const bool last = got == static_cast<unsigned int>(mine_part.pieces - 1);
+                sh.is_last[k & 1] = last ? 1u : 0u;
+                if (last) {
                     __threadfence();
                     p.arrivals[mine_part.first_cta] = 0u;
                 }
@@ -1034,35 +1037,50 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                     }
                 }
             };
-            bool final_rows = whole;
-            if (!whole) {
+            if (whole) {
+                store_rows();
+            } else {
                 if (key < DV) {
 #pragma unroll
                     for (int r = 0; r < kStates; ++r) slot_o[r * DV + key] = y[r];
                 }
                 named_barrier_sync(kBar, 128);
-                if (key == 0 && !sh.is_last) {
+                if (key == 0 && !sh.is_last[k & 1]) {
                     // (the fence covers the stores of all threads of the group: the barrier orders them before it)
                     __threadfence();
                     const bool last = atomicAdd(p.arrivals + e.first_cta, 1u) == static_cast<unsigned int>(e.pieces - 1);
-                    sh.is_last = last ? 1u : 0u;
+                    sh.is_last[k & 1] = last ? 1u : 0u;
                     if (last) p.arrivals[e.first_cta] = 0u;
                     __threadfence();
                 }
                 named_barrier_sync(kBar, 128);
-                final_rows = sh.is_last != 0;
-                if (final_rows) {
-                    // This CTA finished last: all pieces, in the order of the CTAs, kMergePieces at a time under a running maximum, all
-                    // loads of a round in flight together.  (The pieces behind the first are the first parts of their CTAs.)
+                if (sh.is_last[k & 1]) {
+                    // This CTA finished last: all pieces, in the order of the CTAs, kMergePieces at a time under a running maximum.  A
+                    // thread has four columns of every kGroups-th state (both maps of a row are its own); the first loads go out
+                    // before the weights that they wait for.  (The pieces behind the first are the first parts of their CTAs.)
+                    constexpr int kGroups = 128 / (DV / 4), kMine = kStates / kGroups, kBatch = kMine <= 4 ? 2 : 1;
+                    static_assert(kRows % kGroups == 0, "both maps of a row in one thread");
+                    const int col = key % (DV / 4) * 4, g0 = key / (DV / 4);
                     auto piece = [&](int c) {
                         return p.part + (c == 0 ? e.first_slot : 2ll * (e.first_cta + c)) * kStates * (DV + 2);
                     };
-                    float run_m = -INFINITY, run_l = 0.f;
+                    float4 z[kMine], v[kBatch][kMine];
 #pragma unroll
-                    for (int r = 0; r < kStates; ++r) y[r] = 0.f;
+                    for (int j = 0; j < kMine; ++j) z[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    auto load_batch = [&](int c) {
+#pragma unroll
+                        for (int q = 0; q < kBatch; ++q) {
+                            if (c + q >= e.pieces) break;
+                            const float* po = piece(c + q) + g0 * DV + col;
+#pragma unroll
+                            for (int j = 0; j < kMine; ++j) v[q][j] = __ldcg(reinterpret_cast<const float4*>(po + j * kGroups * DV));
+                        }
+                    };
+                    float run_m = -INFINITY, run_l = 0.f;
 #pragma unroll 1
                     for (int c0 = 0; c0 < e.pieces; c0 += kMergePieces) {
                         const int nc = min(kMergePieces, e.pieces - c0);
+                        load_batch(c0);
                         for (int j = key; j < nc * kStates; j += 128) {
                             const float* ml = piece(c0 + j / kStates) + kStates * DV + j % kStates;
                             sh.piece_m[j / kStates][j % kStates] = __ldcg(ml);
@@ -1081,44 +1099,63 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                                 sum += f * sh.piece_l[c][key];
                                 sh.piece_m[c][key] = f;
                             }
-                            sh.out_l[key] = keep;
+                            sh.factor[0][key] = keep;
                             run_m = m;
                             run_l = sum;
+                            // (read after the last round)
+                            sh.factor[1][key] = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
                         }
                         named_barrier_sync(kBar, 128);
 #pragma unroll
-                        for (int r = 0; r < kStates; ++r) y[r] *= sh.out_l[r];
-                        if (key < DV) {
-                            constexpr int kBatch = kStates <= 16 ? 4 : (kStates <= 32 ? 2 : 1);
+                        for (int j = 0; j < kMine; ++j) {
+                            const float keep = sh.factor[0][g0 + j * kGroups];
+                            z[j].x *= keep; z[j].y *= keep; z[j].z *= keep; z[j].w *= keep;
+                        }
 #pragma unroll 1
-                            for (int c = 0; c < nc; c += kBatch) {
-                                float v[kBatch][kStates];
+                        for (int c = 0; c < nc; c += kBatch) {
+                            if (c > 0) load_batch(c0 + c);
 #pragma unroll
-                                for (int q = 0; q < kBatch; ++q) {
-                                    const float* po = piece(c0 + min(c + q, nc - 1)) + key;
+                            for (int q = 0; q < kBatch; ++q) {
+                                if (c + q >= nc) break;
 #pragma unroll
-                                    for (int r = 0; r < kStates; ++r) v[q][r] = __ldcg(po + r * DV);
-                                }
-#pragma unroll
-                                for (int q = 0; q < kBatch; ++q) {
-                                    if (c + q >= nc) break;
-#pragma unroll
-                                    for (int r = 0; r < kStates; ++r) y[r] = fmaf(sh.piece_m[c + q][r], v[q][r], y[r]);
+                                for (int j = 0; j < kMine; ++j) {
+                                    const float f = sh.piece_m[c + q][g0 + j * kGroups];
+                                    z[j].x = fmaf(f, v[q][j].x, z[j].x);
+                                    z[j].y = fmaf(f, v[q][j].y, z[j].y);
+                                    z[j].z = fmaf(f, v[q][j].z, z[j].z);
+                                    z[j].w = fmaf(f, v[q][j].w, z[j].w);
                                 }
                             }
                         }
-                        named_barrier_sync(kBar, 128);
+                        if (c0 + kMergePieces < e.pieces) named_barrier_sync(kBar, 128);
                     }
-                    if (key < kStates) {
-                        store_lse(key % kRows, run_m, run_l);
-                        sh.out_l[key] = run_l > 0.f || run_l != run_l ? 1.f / run_l : 0.f;
-                    }
-                    named_barrier_sync(kBar, 128);
 #pragma unroll
-                    for (int r = 0; r < kStates; ++r) y[r] *= sh.out_l[r];
+                    for (int j = 0; j < kRows / kGroups; ++j) {
+                        const int r = g0 + j * kGroups;
+                        const float f0 = vs * sh.factor[1][r];
+                        float4 o = make_float4(f0 * z[j].x, f0 * z[j].y, f0 * z[j].z, f0 * z[j].w);
+                        if constexpr (kDiff) {
+                            const float4 o1 = z[j + kRows / kGroups];
+                            const float f1 = vs * sh.factor[1][kRows + r] * p.lambda[sh.out_hq[r]];
+                            o.x -= f1 * o1.x; o.y -= f1 * o1.y; o.z -= f1 * o1.z; o.w -= f1 * o1.w;
+                            float f = p.out_scale;
+                            float4 w = make_float4(1.f, 1.f, 1.f, 1.f);
+                            if (p.weight) {
+                                float q = o.x * o.x + o.y * o.y + o.z * o.z + o.w * o.w;        // (a row is a warp's)
+#pragma unroll
+                                for (int d = 16; d > 0; d >>= 1) q += __shfl_xor_sync(0xffffffffu, q, d);
+                                f *= rsqrtf(q * (1.f / DV) + p.eps);
+                                w = __ldg(reinterpret_cast<const float4*>(p.weight + col));
+                            }
+                            o.x *= f * w.x; o.y *= f * w.y; o.z *= f * w.z; o.w *= f * w.w;
+                        }
+                        const long long at = sh.out_at[r];
+                        if (at >= 0)
+                            *reinterpret_cast<uint2*>(p.O + at + col) = make_uint2(pack_bf16x2(o.x, o.y), pack_bf16x2(o.z, o.w));
+                    }
+                    if (key < kStates) store_lse(key % kRows, run_m, run_l);
                 }
             }
-            if (final_rows) store_rows();
             // (the barrier that the next round begins with comes before anything of this round's is overwritten)
         }
     }
