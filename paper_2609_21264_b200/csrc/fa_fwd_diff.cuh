@@ -61,6 +61,7 @@ struct DiffShared {
     uint32_t tmem_base;
     uint32_t abort_flag;
     float inv_l[2][kTileM];
+    alignas(16) float weight[128];
     float sum_sq[2][kTileM];
 };
 
@@ -169,6 +170,7 @@ fa_fwd_diff_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         const uint32_t tO = tmem_base + Cfg::kColO0 + lane_sel;
         const uint32_t bar_s = smem_addr(&sh.s_full[t]), bar_pf = smem_addr(&sh.p_first[t]), bar_pr = smem_addr(&sh.p_rest[t]);
         const float tau_raw = kRescaleThresholdLog2 / c;
+        if (dp.weight && t == 0) sh.weight[row] = dp.weight[row];        // (read after the barriers of the first item)
         int n = 0, n_final = 0, stored_buf = -1;      // K/V tiles so far, items with one so far, buffer of a store not waited for
         bool ok = true;
         // the thread that stored the group's chunk of an item gives the buffer back once the store has read it
@@ -189,6 +191,7 @@ fa_fwd_diff_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_addr(&sh.item_empty[slot]));
             const Item x = decode(index);
+            const float lambda = dp.lambda[x.hq];
             const int i_glob = x.i0 + row;
             int kmax_row = p.Sk - 1;
             if (p.causal && i_glob + off < kmax_row) kmax_row = i_glob + off;
@@ -213,7 +216,7 @@ fa_fwd_diff_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             named_barrier_sync(1, 256);
             tc_fence_after_sync();
             // group t: columns [64 t, 64 t + 64) of both accumulators
-            const float f0 = sh.inv_l[0][row], f1 = sh.inv_l[1][row] * dp.lambda[x.hq];
+            const float f0 = sh.inv_l[0][row], f1 = sh.inv_l[1][row] * lambda;
             float y[64];
             float sq = 0.f;
             if (x.nkv > 0) {
@@ -242,7 +245,7 @@ fa_fwd_diff_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 f *= rsqrtf((sh.sum_sq[0][row] + sh.sum_sq[1][row]) * (1.f / 128.f) + dp.eps);
 #pragma unroll
                 for (int e = 0; e < 64; e += 4) {
-                    const float4 w = __ldg(reinterpret_cast<const float4*>(dp.weight + 64 * t + e));
+                    const float4 w = *reinterpret_cast<const float4*>(&sh.weight[64 * t + e]);
                     y[e] *= f * w.x;
                     y[e + 1] *= f * w.y;
                     y[e + 2] *= f * w.z;
@@ -384,9 +387,14 @@ fa_fwd_diff_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             int n = 0;
             for (int it = 0;; ++it) {
                 const int slot = it % Cfg::kItems, buf = it & 1;
-                unsigned int ticket = atomicAdd(p.sched_counter, 1u);
-                // every CTA's last draw is past the list; the last of those puts the counter back
-                if (ticket == static_cast<unsigned int>(n_items) + gridDim.x - 1u) *p.sched_counter = 0u;
+                // a CTA's first item is its own number, the others are drawn; every CTA draws past the list once, and the last of all
+                // draws (one per item in the end) puts the counter back
+                unsigned int ticket = blockIdx.x;
+                if (it > 0) {
+                    const unsigned int drawn = atomicAdd(p.sched_counter, 1u);
+                    if (drawn == static_cast<unsigned int>(n_items) - 1u) *p.sched_counter = 0u;
+                    ticket = gridDim.x + drawn;
+                }
                 const bool more = ticket < static_cast<unsigned int>(n_items);
                 if (!mbar_wait(smem_addr(&sh.item_empty[slot]), ((it / Cfg::kItems) & 1) ^ 1, wctx, kSiteItem)) break;
                 if (more && !mbar_wait(smem_addr(&sh.q_empty[buf]), ((it >> 1) & 1) ^ 1, wctx, kSiteLoadQEmpty)) break;
