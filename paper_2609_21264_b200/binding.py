@@ -478,9 +478,12 @@ class PagedCache:
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         load()                            # the calls that take a cache rely on the library being there
         self.device, self.Hkv, self.dqk, self.dv = k.device, k.shape[1], k.shape[3], v.shape[3]
+        # (a single page or head may have any stride, the library wants a valid one: whole 16-byte units)
+        unit = 16 // k.element_size()
+        strides = [_I64x3(*[s if n > 1 else max(t.shape[3], -(-s // unit) * unit) for s, n in zip(t.stride(), t.shape[:3])]) for t in (k, v)]
         self.c = fa_paged_cache(ctypes.sizeof(fa_paged_cache), FA_CACHE_BF16 if k.dtype == torch.bfloat16 else FA_CACHE_E4M3,
                                 k.data_ptr(), v.data_ptr(), k.shape[0], k.shape[2], k.shape[1], k.shape[3], v.shape[3], 0,
-                                _I64x3(*k.stride()[:3]), _I64x3(*v.stride()[:3]),
+                                *strides,
                                 None if k_scale is None else k_scale.data_ptr(), None if v_scale is None else v_scale.data_ptr())
         self.address = ctypes.addressof(self.c)
 
@@ -495,16 +498,17 @@ class Rope:
         if cos_sin.dtype != torch.float32 or not cos_sin.is_cuda or not cos_sin.is_contiguous() or cos_sin.dim() != 2:
             raise ValueError("cos_sin must be a contiguous 2-D fp32 CUDA tensor")
         self.cos_sin, self.device, self.span = cos_sin, cos_sin.device, int(span)
-        self.c = fa_rope(ctypes.sizeof(fa_rope), cos_sin.shape[0], cos_sin.data_ptr(), cos_sin.shape[1], int(offset), int(span),
-                         int(bool(interleaved)))
-        self.address = ctypes.addressof(self.c)
+        self.offset, self.interleaved = int(offset), int(bool(interleaved))
+        self.structs = {}                 # by span
 
     def struct_for(self, dqk: int) -> int:
         """Address of the C structure for heads of dqk dimensions."""
-        if self.span:
-            return self.address
-        self.c.span = dqk
-        return self.address
+        span = self.span or dqk
+        c = self.structs.get(span)
+        if c is None:
+            t = self.cos_sin
+            c = self.structs[span] = fa_rope(ctypes.sizeof(fa_rope), t.shape[0], t.data_ptr(), t.shape[1], self.offset, span, self.interleaved)
+        return ctypes.addressof(c)
 
 
 # The calls below are made once per layer and token: their checks are written to cost little (one stride array per call, the raw
@@ -524,13 +528,14 @@ def _seqs(h, cache, block_table, seq_lens):
         raise ValueError("block_table must be a 2-D int32 tensor on the cache's device")
     B, max_pages = block_table.shape
     stride, inner = block_table.stride()
-    if inner != 1 and max_pages > 1:
-        raise ValueError("the rows of block_table must be contiguous")
+    if (inner != 1 and max_pages > 1) or (stride < max_pages and B > 1):
+        raise ValueError("the rows of block_table must be contiguous and lie apart")
     if seq_lens.dtype is not i32 or seq_lens.device != device or seq_lens.shape != (B,) or not seq_lens.is_contiguous():
         raise ValueError("seq_lens must be a contiguous int32 tensor of one length per row of block_table")
     if _lib.fa_device(h) != device.index:
         raise ValueError("the handle belongs to another device than the cache")
-    return fa_paged_seqs(_SEQS_SIZE, B, block_table.data_ptr(), stride if stride > max_pages else max_pages, seq_lens.data_ptr(),
+    # (the stride of a single row is whatever the view left)
+    return fa_paged_seqs(_SEQS_SIZE, B, block_table.data_ptr(), stride if B > 1 else max_pages, seq_lens.data_ptr(),
                          max_pages, 0)
 
 

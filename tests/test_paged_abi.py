@@ -51,3 +51,22 @@ def test_host_tensors_are_refused():
         binding.Rope(torch.zeros(4, 64))
     with pytest.raises(ValueError):
         binding.forward_diff(0, k, k, k, torch.zeros(1), causal=True)
+
+
+@pytest.mark.parametrize("table_rows", ["shared", "overlapping", "columns"])
+def test_block_tables_whose_rows_do_not_lie_apart_are_refused(table_rows):
+    """(A row stride below the row's length would be read as the length: rows of another place in memory.)"""
+    import types
+
+    import torch
+    t = torch.zeros(64, dtype=torch.int32)
+    table = {"shared": t[:8].expand(4, 8), "overlapping": t.as_strided((4, 8), (4, 1)), "columns": t[:32].view(8, 4).t()}[table_rows]
+    cache = types.SimpleNamespace(device=t.device)
+    with pytest.raises(ValueError, match="block_table"):
+        binding._seqs(None, cache, table, torch.ones(4, dtype=torch.int32))
+
+
+def test_plans_of_more_heads_than_a_call_may_have_are_refused():
+    with pytest.raises(binding.FaError) as e:
+        binding.fa_plan_paged(148, [100], 1 << 28, 1, 16, 128, 128)
+    assert e.value.status == binding.FA_ERR_UNSUPPORTED
