@@ -329,7 +329,7 @@ fa_status fa_forward_host(fa_handle* h,
  * Device-side status of the kernels launched through `h` so far: FA_OK, or
  * FA_ERR_DEVICE_TIMEOUT if any bounded wait (mbarrier, TMEM allocation) ran
  * out since the handle was created or the status was last read (reading
- * clears it).  Synchronises nothing: meaningful after the caller has
+ * clears it), or FA_ERR_INVALID_ARG if a paged call found a length, page or position that it may not use.  Synchronises nothing: meaningful after the caller has
  * synchronised the stream(s) it launched on.  `detail`, if not NULL, receives
  * a diagnostic word (role and barrier that gave up; 0 when FA_OK).
  */
@@ -410,7 +410,7 @@ fa_status fa_noalloc_last_status(uint32_t* detail);
  *   type     FA_CACHE_BF16, or FA_CACHE_E4M3: one-byte values with one fp32 scale per K/V head,
  *            K = k_scale[h] * code, V = v_scale[h] * code (DEVICE arrays of Hkv positive numbers; NULL = 1).
  *   k, v     DEVICE pointers, 16-byte aligned; every stride a positive multiple of 16 bytes, strides[2] >= the head size.
- *   page_size  a multiple of 16, at most 65536.
+ *   page_size  a multiple of 16, at most 65536; Hkv at most 65535.
  *   (dqk, dv)  as for fa_forward.
  * Set struct_size = sizeof(fa_paged_cache).
  */
@@ -435,7 +435,8 @@ typedef struct fa_paged_cache {
  * sequence, the tokens of this step INCLUDED.  The host never reads them, so a captured call can be replayed with new
  * contents.  What the host cannot check the kernels do: a length that is negative or needs more than max_pages pages, a
  * page number outside the pool and a position past the rotation table make fa_last_status return FA_ERR_INVALID_ARG; nothing
- * out of range is read or written, and the outputs of the sequences concerned are unspecified.
+ * out of range is read or written, and the outputs of the sequences concerned are unspecified.  (fa_append_paged looks only
+ * at the sequences that have new tokens.)  max_pages * page_size is at most 2^31 - 256.
  */
 typedef struct fa_paged_seqs {
     uint32_t struct_size;         /* sizeof(fa_paged_seqs) */
@@ -473,6 +474,7 @@ typedef struct fa_rope {
  *   rope    NULL = no rotation (Q is then copied).      Q, Q_out   both or neither NULL; Q_out may be Q itself.
  * Arithmetic is fp32 with one rounding to bf16, or of value * (1 / scale) to e4m3 (saturating at +-448).  A slot that two tokens of
  * a call name (sequences sharing a page that is written to) ends with either's values.  Asynchronous on `stream`.
+ * FA_ERR_UNSUPPORTED also where a token has more than 65535 units of 32 bytes in all its heads.
  */
 fa_status fa_append_paged(fa_handle* h, const fa_paged_cache* cache, const fa_paged_seqs* seqs,
                           const int32_t* cu_seqlens, int total,
@@ -486,14 +488,17 @@ fa_status fa_append_paged(fa_handle* h, const fa_paged_cache* cache, const fa_pa
  * cache that holds their keys and values already.  Q [B*Sq, Hq, dqk] and O [B*Sq, Hq, dv] are bf16 DEVICE tensors,
  * 16-byte aligned, with {token, head} strides in elements, multiples of 8; lse is fp32 [Hq, B*Sq] or NULL.  Token i of
  * sequence b sees the keys j <= seq_lens[b] - Sq + i.  A token that sees no key (length 0, or less than its place among the new
- * tokens) gets O = 0 and lse = -inf.  Slots past a sequence's length take no part, whatever they hold.  Scores, softmax state
- * and both accumulators are fp32; the probabilities enter the second product as bf16, and over an e4m3 cache as the sum of three
- * 8-bit terms (at least 9 significant bits), the queries as such a sum too (exact for entries within 2^-22 of the head's
- * largest).  scale as for fa_forward.
+ * tokens) gets O = 0 and lse = -inf.  Slots past a sequence's length take no part, whatever they hold; the values (V) of the
+ * last Sq tokens must be finite where Sq > 1 (a token that does not see a key multiplies its value by a probability of zero).
+ * Scores, softmax state and both accumulators are fp32; the probabilities enter the second product as bf16, and over an e4m3 cache as
+ * the sum of three 8-bit terms (at least 9 significant bits), the queries as such a sum too (exact for entries of 2^-24 of
+ * their row's largest and more, to 2^-31 of it below).  scale as for fa_forward.
  * One launch: the K/V tiles of all sequences are dealt out evenly over the SMs on the device and the pieces of a
  * sequence are joined by the SM that finishes last, in a fixed order, so equal calls give equal bits.  The partial results use the
- * handle's scratch buffer, under the rule of fa_forward: launches through one handle must not overlap on the device.  Scratch
- * smaller than two partials per SM: FA_ERR_UNSUPPORTED.
+ * handle's scratch buffer, under the rule of fa_forward: launches through one handle must not overlap on the device.  With less
+ * scratch than two partials per SM fewer SMs are used; with less than two, and for batches of more than 2^31 tiles of 128
+ * keys (counted by max_pages), FA_ERR_UNSUPPORTED.  fa_config.kv_splits does not apply; FA_FLAG_SERIAL_KERNEL selects a
+ * plain kernel of one CTA per query row (a cross-check), here and in the differential calls.
  */
 #define FA_PAGED_MAX_SQ 16
 fa_status fa_forward_paged(fa_handle* h, const fa_paged_cache* cache, const fa_paged_seqs* seqs,
@@ -540,7 +545,8 @@ typedef struct fa_diff {
 } fa_diff;
 
 /* Differential attention over whole prompts: tensors, strides, mask and errors as for fa_forward_strided with
- * dqk = dv = 128.  A row that sees no key gets O = 0. */
+ * dqk = dv = 128.  A row that sees no key gets O = 0.  The probabilities are rounded to bf16 once; the inputs must be finite, masked
+ * values (V) too. */
 fa_status fa_forward_diff(fa_handle* h, const void* Q, const void* K, const void* V, void* O,
                           int B, int Hq, int Hkv, int Sq, int Sk, int dqk, int dv, int causal, float scale,
                           const fa_diff* diff,
@@ -548,7 +554,7 @@ fa_status fa_forward_diff(fa_handle* h, const void* Q, const void* K, const void
                           const int64_t* v_strides, const int64_t* o_strides, void* stream);
 
 /* Differential attention of the last Sq tokens of every sequence over a paged cache; everything else as for fa_forward_paged
- * with dqk = dv = 128. */
+ * with dqk = dv = 128; over a bf16 cache the probabilities keep 16 bits (two bf16 terms). */
 fa_status fa_forward_paged_diff(fa_handle* h, const fa_paged_cache* cache, const fa_paged_seqs* seqs,
                                 const void* Q, void* O, int Hq, int Sq, float scale, const fa_diff* diff,
                                 const int64_t* q_strides, const int64_t* o_strides, void* stream);

@@ -702,7 +702,12 @@ fa_status fa_create(fa_handle** out, const fa_config* cfg) {
     h->flags = flags;
     h->kv_splits_cfg = kv_splits_cfg;
     if (limit_ms) h->wait_limit_ns = static_cast<unsigned long long>(limit_ms) * 1000000ull;
-    h->maps.reserve(kMapCacheSize);
+    try {
+        h->maps.reserve(kMapCacheSize);       // (get_map never grows it)
+    } catch (...) {
+        delete h;
+        return FA_ERR_OOM;
+    }
 
     DeviceGuard guard(device);
     if (!guard.ok()) { delete h; return FA_ERR_CUDA; }

@@ -208,9 +208,12 @@ fa_append_paged_kernel(const AppendParams p) {
             count = p.cu_seqlens[b + 1] - first;
         }
         if (b >= 0) {
-            tk.pos = p.seq_lens[b] - count + (row - first);
+            const int len = p.seq_lens[b];
+            tk.pos = len - count + (row - first);
             const int at = tk.pos / p.page_size;
-            if (tk.pos < 0) {
+            if (len < 0) {
+                report_bad_input(p.status, kSiteBadLength);
+            } else if (tk.pos < 0) {
                 // (the padding of a batch)
             } else if (at >= p.max_pages) {
                 report_bad_input(p.status, kSiteBadLength);

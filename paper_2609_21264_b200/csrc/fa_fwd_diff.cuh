@@ -206,7 +206,7 @@ fa_fwd_diff_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             }
             release_buffer();
             // (a row that saw no key: the polynomial made 2^-125 of its masked scores, not zero)
-            sh.inv_l[t][row] = (m_ref != -INFINITY && l > 0.f) ? (1.f / l) : 0.f;
+            sh.inv_l[t][row] = l != l || (m_ref != -INFINITY && l > 0.f) ? (1.f / l) : 0.f;
             if (x.nkv > 0) {
                 ok = ok && mbar_wait(smem_addr(&sh.o_final[0]), n_final & 1, wctx, kSiteEpiOFull) &&
                      mbar_wait(smem_addr(&sh.o_final[1]), n_final & 1, wctx, kSiteEpiOFull);

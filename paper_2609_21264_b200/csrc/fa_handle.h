@@ -134,7 +134,11 @@ fa_status ensure_smem_attr(fa_handle* h, Kernel kernel, int bytes) {
         cudaGetLastError();
         return FA_ERR_CUDA;
     }
-    h->attr_done.push_back(key);
+    try {
+        h->attr_done.push_back(key);
+    } catch (...) {
+        // (no memory to remember it in: the next call sets the limit again)
+    }
     return FA_OK;
 }
 

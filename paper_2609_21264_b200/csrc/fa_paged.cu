@@ -34,7 +34,7 @@ fa_status check_cache(const fa_paged_cache* c) {
     if (!c->k || !c->v || misaligned(c->k, 16) || misaligned(c->v, 16)) return FA_ERR_INVALID_ARG;
     if (c->num_pages <= 0 || c->page_size <= 0 || c->Hkv <= 0 || c->dqk <= 0 || c->dv <= 0) return FA_ERR_INVALID_ARG;
     if (!head_sizes_ok(c->dqk, c->dv)) return FA_ERR_UNSUPPORTED;
-    if (c->page_size % 16 != 0 || c->page_size > 65536) return FA_ERR_UNSUPPORTED;
+    if (c->page_size % 16 != 0 || c->page_size > 65536 || c->Hkv > 65535) return FA_ERR_UNSUPPORTED;
     const int64_t unit = c->type == FA_CACHE_E4M3 ? 16 : 8;      // 16 bytes
     for (int i = 0; i < 3; ++i)
         if (c->k_strides[i] <= 0 || c->v_strides[i] <= 0 || c->k_strides[i] % unit != 0 || c->v_strides[i] % unit != 0)
@@ -48,7 +48,8 @@ fa_status check_cache(const fa_paged_cache* c) {
 fa_status check_seqs(const fa_paged_seqs* s, const fa_paged_cache* c) {
     if (!s || s->struct_size != sizeof(fa_paged_seqs) || s->reserved != 0) return FA_ERR_INVALID_ARG;
     if (s->B < 0 || s->max_pages <= 0 || s->table_stride < s->max_pages) return FA_ERR_INVALID_ARG;
-    if (!s->block_table || !s->seq_lens || misaligned(s->block_table, 4) || misaligned(s->seq_lens, 4)) return FA_ERR_INVALID_ARG;
+    if (s->B > 0 && (!s->block_table || !s->seq_lens)) return FA_ERR_INVALID_ARG;
+    if (misaligned(s->block_table, 4) || misaligned(s->seq_lens, 4)) return FA_ERR_INVALID_ARG;
     // positions are 32-bit
     if (static_cast<int64_t>(s->max_pages) * c->page_size > 0x7fffff00LL) return FA_ERR_UNSUPPORTED;
     return FA_OK;
@@ -155,7 +156,7 @@ fa_status forward_paged(fa_handle* h, const fa_paged_cache* cache, const fa_page
     fa_status s = check_cache(cache);
     if (s != FA_OK) return s;
     if ((s = check_seqs(seqs, cache)) != FA_OK) return s;
-    if (!Q || !O || misaligned(Q, 16) || misaligned(O, 16) || (lse && misaligned(lse, 4))) return FA_ERR_INVALID_ARG;
+    if ((seqs->B > 0 && (!Q || !O)) || misaligned(Q, 16) || misaligned(O, 16) || (lse && misaligned(lse, 4))) return FA_ERR_INVALID_ARG;
     if (Hq <= 0 || Sq <= 0 || Hq % cache->Hkv != 0 || !isfinite(scale) || scale < 0.f) return FA_ERR_INVALID_ARG;
     if (!row_strides_ok(q_strides, cache->dqk) || !row_strides_ok(o_strides, cache->dv)) return FA_ERR_INVALID_ARG;
     if (Sq > FA_PAGED_MAX_SQ || Hq > 65535 || seqs->B > 65535) return FA_ERR_UNSUPPORTED;
@@ -237,7 +238,8 @@ fa_status fa_append_paged(fa_handle* h, const fa_paged_cache* cache, const fa_pa
     if (!row_strides_ok(k_strides, cache->dqk) || !row_strides_ok(v_strides, cache->dv)) return FA_ERR_INVALID_ARG;
     if (!Q != !Q_out) return FA_ERR_INVALID_ARG;
     if (Q) {
-        if (misaligned(Q, 16) || misaligned(Q_out, 16) || Hq <= 0 || Hq > 65535) return FA_ERR_INVALID_ARG;
+        if (misaligned(Q, 16) || misaligned(Q_out, 16) || Hq <= 0) return FA_ERR_INVALID_ARG;
+        if (Hq > 65535) return FA_ERR_UNSUPPORTED;
         if (!row_strides_ok(q_strides, cache->dqk) || !row_strides_ok(qo_strides, cache->dqk)) return FA_ERR_INVALID_ARG;
     }
     if (rope) {
@@ -396,7 +398,7 @@ fa_status fa_plan_paged(int num_sms, const fa_config* cfg, const fa_paged_cache*
         return FA_ERR_INVALID_ARG;
     if (cache->page_size <= 0 || cache->Hkv <= 0 || Hq <= 0 || Sq <= 0 || Hq % cache->Hkv != 0 || seqs->B <= 0 || seqs->max_pages <= 0 ||
         !seqs->seq_lens || max_pieces < 0 || (max_pieces > 0 && !pieces)) return FA_ERR_INVALID_ARG;
-    if (!head_sizes_ok(cache->dqk, cache->dv) || cache->page_size % 16 != 0 || Sq > FA_PAGED_MAX_SQ || seqs->B > 65535 ||
+    if (!head_sizes_ok(cache->dqk, cache->dv) || cache->page_size % 16 != 0 || Sq > FA_PAGED_MAX_SQ || Hq > 65535 || seqs->B > 65535 ||
         (diff && (cache->dqk != 128 || cache->dv != 128)) || static_cast<int64_t>(seqs->max_pages) * cache->page_size > 0x7fffff00LL)
         return FA_ERR_UNSUPPORTED;
     uint64_t scratch = 32ull << 20;

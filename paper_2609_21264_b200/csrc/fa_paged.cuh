@@ -949,7 +949,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             auto store_lse = [&](int r, float m, float sum) {
                 if (kDiff || !p.lse || sh.out_at[r] < 0) return;
                 p.lse[static_cast<long long>(sh.out_hq[r]) * p.B * p.Sq + static_cast<long long>(e.b) * p.Sq + sh.out_i[r]] =
-                    sum > 0.f ? (m - Cfg::kBias + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+                    sum > 0.f || sum != sum ? (m - Cfg::kBias + log2f(sum)) * 0.6931471805599453f : -INFINITY;
             };
             named_barrier_sync(kBar, 128);
             // (uniform) whether a group had a tile of this part

@@ -92,10 +92,11 @@ fa_paged_simple_kernel(const PagedParams p) {
             sum += f * sm_l[w][a];
             if (c < DV) acc += f * sm_o[w][a][c];
         }
-        const float part = sum > 0.f ? acc / sum * vs : 0.f;
+        const bool any = sum > 0.f || sum != sum;        // (a NaN goes through)
+        const float part = any ? acc / sum * vs : 0.f;
         y += a == 0 ? part : -p.lambda[hq] * part;
         if (!kDiff && p.lse && c == 0)
-            p.lse[static_cast<long long>(hq) * p.B * p.Sq + t] = sum > 0.f ? (mx + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+            p.lse[static_cast<long long>(hq) * p.B * p.Sq + t] = any ? (mx + log2f(sum)) * 0.6931471805599453f : -INFINITY;
     }
     if constexpr (kDiff) {
         float f = p.out_scale;

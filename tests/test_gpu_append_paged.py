@@ -226,3 +226,67 @@ def test_refusals(handle):
         b.PagedCache(k, v.float())
     with pytest.raises(b.FaError):
         b.append_paged(handle, torch.cat([kn, kn, kn]), torch.cat([vn, vn, vn]), cache, table.expand(2, -1).contiguous(), lens.expand(2).contiguous())
+
+
+def test_negative_lengths_are_reported_and_empty_batches_are_nothing(handle):
+    from paper_2609_21264_b200 import binding as b
+    k, v, table, lens, _, _ = pool([20, 40], 16, 2, 64, 64, False, False, 6, poison=False)
+    kn, vn = (torch.randn(2, 2, 64, device="cuda").bfloat16() for _ in range(2))
+    k0, v0 = k.clone(), v.clone()
+    cache = b.PagedCache(k, v)
+    for least in (-1, -2 ** 31):
+        b.append_paged(handle, kn, vn, cache, table, torch.full_like(lens, least))
+        torch.cuda.synchronize()
+        assert b.fa_last_status(handle) == (b.FA_ERR_INVALID_ARG, 0x0901) and torch.equal(k, k0) and torch.equal(v, v0)
+    b.append_paged(handle, kn[:0], vn[:0], cache, table[:0], lens[:0])
+    assert b.append_paged(handle, kn[:0], vn[:0], cache, table[:0], lens[:0], q=kn[:0]).shape == (0, 2, 64)
+    ok(handle)
+    assert torch.equal(k, k0)
+
+
+def test_more_heads_than_a_call_may_have(handle):
+    from paper_2609_21264_b200 import binding as b
+    k, v, table, lens, _, _ = pool([20], 16, 2, 64, 64, False, False, 7)
+    kn = torch.randn(1, 2, 64, device="cuda").bfloat16()
+    seqs = b.fa_paged_seqs(ctypes.sizeof(b.fa_paged_seqs), 1, table.data_ptr(), table.shape[1], lens.data_ptr(), table.shape[1], 0)
+    c = b.fa_paged_cache.from_buffer_copy(b.PagedCache(k, v).c)
+    call = lambda Hq: b.fa_append_paged(handle, c, seqs, None, 1, kn.data_ptr(), kn.data_ptr(), kn.data_ptr(), kn.data_ptr(), Hq,  # noqa: E731
+                                        (128, 64), (128, 64), (128, 64), (128, 64), None)
+    assert call(65536) == b.FA_ERR_UNSUPPORTED and call(65535) == b.FA_ERR_UNSUPPORTED       # (too many 32-byte units a token)
+    c.Hkv = 2 ** 31 - 1
+    assert call(2) == b.FA_ERR_UNSUPPORTED
+
+
+def test_one_rotation_for_two_head_sizes(handle):
+    """span 0 is the whole head of whichever cache a call has."""
+    from paper_2609_21264_b200 import binding as b
+    rope, tab = None, rope_table(64, 64)
+    rope = b.Rope(tab)
+    for d, dv in ((64, 64), (192, 128), (128, 128), (64, 64)):
+        k, v, table, lens, _, _ = pool([37], 16, 2, d, dv, False, False, 8, poison=False)
+        kn = torch.randn(1, 2, d, device="cuda").bfloat16()
+        b.append_paged(handle, kn, torch.randn(1, 2, dv, device="cuda").bfloat16(), b.PagedCache(k, v), table, lens, rope=rope)
+        ok(handle)
+        x, cs = kn[0].double(), tab[36].double()
+        lo, hi, c, s = x[:, :32], x[:, 32:64], cs[:32], cs[32:]
+        want = torch.cat([lo * c - hi * s, hi * c + lo * s, x[:, 64:]], 1)
+        got = k[int(table[0, 2]), :, 4].double()
+        # one rounding to bf16, fp32 products of numbers below 8 before it
+        assert ((got - want).abs() <= want.abs() * 2.0 ** -8 + 8 * 2.0 ** -22).all()
+
+
+def test_a_cache_of_one_page_and_head_with_strides_of_no_use(handle):
+    from paper_2609_21264_b200 import binding as b
+    store = torch.zeros(2, 64, 128, device="cuda").bfloat16()
+    k, v = (x.as_strided((1, 1, 64, 128), (0, 3, 128, 1), x.storage_offset()) for x in store)
+    table, lens = torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.tensor([5], dtype=torch.int32, device="cuda")
+    kn, vn, q = (torch.randn(5, 1, 128, device="cuda").bfloat16() for _ in range(3))
+    cache = b.PagedCache(k, v)
+    b.append_paged(handle, kn, vn, cache, table, lens)
+    o, _ = b.forward_paged(handle, q[:1], cache, table, lens)
+    ok(handle)
+    assert torch.equal(store[0, :5], kn[:, 0]) and torch.equal(store[1, :5], vn[:, 0]) and not store[:, 5:].any()
+    w = torch.softmax(q[0].double() @ kn[:, 0].double().t() * 128 ** -0.5, 1)
+    want = w @ vn[:, 0].double()
+    # probabilities and result rounded to bf16
+    assert ((o[0].double() - want).abs() <= 2.0 ** -8 * (w @ vn[:, 0].double().abs() + want.abs()) + 3e-4).all()

@@ -180,3 +180,17 @@ def test_a_wait_that_runs_out_is_reported_and_the_handle_recovers():
     finally:
         b.fa_destroy(h)
         b.fa_destroy(fresh)
+
+
+def test_a_query_that_is_no_number_shows_in_its_row_alone(handle):
+    from paper_2609_21264_b200 import binding as b
+    q, k, v = (torch.randn(1, 2, 300, 128, device="cuda").bfloat16() for _ in range(3))
+    for half in (3, 100):
+        x = q.clone()
+        x[0, 1, 170, half] = float("nan")
+        o = b.forward_diff(handle, x, k, v, torch.full((2,), 0.5, device="cuda"), causal=True)
+        torch.cuda.synchronize()
+        assert b.fa_last_status(handle) == (b.FA_OK, 0)
+        assert o[0, 1, 170].isnan().all()
+        o[0, 1, 170] = 0
+        assert o.isfinite().all()

@@ -459,3 +459,29 @@ def test_cache_of_more_than_2_31_elements(handle):
         assert_attention(o, lse, *paged_reference(q, small_k, small_v, None, None, torch.tensor([[0, 1, 2]]), [300], 1, d ** -0.5))
         del k, v
         torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("lens", [[200, 90], [6000, 90]], ids=["whole", "split"])
+def test_a_key_that_is_no_number_shows_in_its_own_rows_alone(handle, e4m3, lens):
+    from paper_2609_21264_b200 import binding as b
+    k, v, table, lens_t, ks, vs = pool(lens, 16, 2, 128, 128, e4m3, False, 60)
+    q = torch.randn(2, 8, 128, device="cuda").bfloat16()
+    at = lens[0] - 70
+    k.view(torch.uint8 if e4m3 else torch.bfloat16)[int(table[0, at // 16]), 1, at % 16, 5] = 0x7F if e4m3 else float("nan")
+    o, lse = b.forward_paged(handle, q, b.PagedCache(k, v, ks, vs), table, lens_t)
+    ok(handle)
+    assert o[0, 4:].isnan().all() and lse[4:, 0].isnan().all()
+    assert o[0, :4].isfinite().all() and o[1].isfinite().all() and lse[:4].isfinite().all() and lse[:, 1].isfinite().all()
+    # a query that is none, against keys that all are numbers
+    q[1, 2, 7] = float("nan")
+    o, lse = b.forward_paged(handle, q, b.PagedCache(k, v, ks, vs), table, lens_t)
+    ok(handle)
+    assert o[1, 2].isnan().all() and lse[2, 1].isnan() and o[1, [0, 1, 3]].isfinite().all()
+
+
+def test_an_empty_batch_is_nothing(handle):
+    from paper_2609_21264_b200 import binding as b
+    c = b.PagedCache(*pool([20], 16, 2, 64, 64, False, False, 5)[:2])
+    seqs = b.fa_paged_seqs(ctypes.sizeof(b.fa_paged_seqs), 0, None, 1, None, 1, 0)
+    assert b.fa_forward_paged(handle, c.c, seqs, None, None, None, 4, 1, 0.0, (256, 64), (256, 64)) == b.FA_OK
