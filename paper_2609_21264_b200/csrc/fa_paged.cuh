@@ -36,8 +36,6 @@
 
 #include <math.h>
 
-#include <type_traits>
-
 #include "fa_paged_common.cuh"
 
 namespace fa {
@@ -47,6 +45,8 @@ namespace ptx {
 FA_DEVI void st_shared_u64(uint32_t addr, uint32_t lo, uint32_t hi) {
     asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(lo), "r"(hi) : "memory");
 }
+
+FA_DEVI void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
 }  // namespace ptx
 
@@ -66,7 +66,7 @@ FA_DEVI bool paged_wait(uint64_t& bar, uint32_t parity, PagedWait* ctx) {
     } while (!ptx::mbar_try_wait(at, parity));
     return true;
 }
-static __device__ __noinline__ bool paged_wait_timed(uint64_t* bar, uint32_t parity, PagedWait* ctx, uint32_t who) {
+static __device__ __noinline__ bool paged_wait_long(uint64_t* bar, uint32_t parity, PagedWait* ctx, uint32_t who) {
     const uint32_t at = ptx::smem_addr(bar);
     volatile uint32_t* abort_flag = &ctx->abort_flag;
     uint64_t t0 = 0;
@@ -89,6 +89,11 @@ static __device__ __noinline__ bool paged_wait_timed(uint64_t* bar, uint32_t par
             }
         }
     }
+}
+
+// (a call costs some 400 cycles, so the first look is taken here)
+FA_DEVI bool paged_wait_timed(uint64_t* bar, uint32_t parity, PagedWait* ctx, uint32_t who) {
+    return ptx::mbar_try_wait(ptx::smem_addr(bar), parity) || paged_wait_long(bar, parity, ctx, who);
 }
 
 // ------------------------------------------------------------------ the list of work units and its shares
@@ -191,8 +196,10 @@ struct PagedShared {
     float factor[2][kMaps * kRows];
     float piece_m[kMergePieces][kMaps * kRows], piece_l[kMergePieces][kMaps * kRows];
     float sq[4][kRows];
-    long long out_at[kRows];                             // offset of the row in O (-1: a padding row)
-    int out_hq[kRows], out_i[kRows];
+    // The rows of a block, apart from the part's sequence and K/V head: offsets in Q and O (-1: a padding row), place among the new
+    // tokens (Q: of the last one for padding), query head of the group.  They change with the block of rows alone.
+    long long row_q[kRows], row_o[kRows];
+    int row_place[kRows], row_i[kRows], row_h[kRows];
 };
 
 template <int DQK, int DV, bool kE4m3, bool kDiff, int kRows>
@@ -329,6 +336,29 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         if (tid < 128) st_shared_v4(sZero + tid * 16, 0, 0, 0, 0);
         fence_proxy_async_smem();
     }
+    const int group = p.Hq / p.Hkv;
+    auto rows_of_q = [&](int rb, int r) {
+        const int rr = rb * kRows + r, i = rr / group;
+        sh.row_q[r] = i < p.Sq ? i * p.q_st + (rr - i * group) * p.q_sh : -1;
+        sh.row_place[r] = min(i, p.Sq - 1);
+    };
+    auto rows_of_o = [&](int rb, int r) {
+        const int rr = rb * kRows + r, i = rr / group;
+        sh.row_o[r] = i < p.Sq ? i * p.o_st + (rr - i * group) * p.o_sh : -1;
+        sh.row_i[r] = i;
+        sh.row_h[r] = rr - i * group;
+    };
+    if (warp >= 12) {
+        if ((tid & 127) < kRows) {
+            rows_of_q(0, tid & 127);
+            rows_of_o(0, tid & 127);
+        }
+        // lengths and block table towards L2 (a line each; the streams of other calls have usually driven them out): list and loads
+        // wait for one after the other
+        const int at = tid & 127, per_row = (p.max_pages + 31) / 32, line = blockIdx.x * 128 + at, b = line / per_row;
+        if (at * 32 < p.B) prefetch_l2(p.seq_lens + at * 32);
+        if (b < p.B) prefetch_l2(p.block_table + b * p.table_stride + (line - b * per_row) * 32);
+    }
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
@@ -339,16 +369,16 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
     auto s_col = [&](int w, int i) -> uint32_t { return (w * kBufs + i) * Cfg::kSCols; };
     auto o_col = [&](int ob, int w) -> uint32_t { return Cfg::kSBufs * Cfg::kSCols + (ob * 2 + w) * kCols; };
     PagedWait* const wait = &sh.wait;
-    const int group = p.Hq / p.Hkv;
-    auto wait_part_timed = [&](int k) -> bool { return paged_wait_timed(&sh.part_full[k % kPartRing], (k / kPartRing) & 1, wait, kSiteItem); };
     auto wait_part = [&](int k) -> bool { return paged_wait(sh.part_full[k % kPartRing], (k / kPartRing) & 1, wait); };
 
     if (warp == 0 || warp == 2) {
         // ============================================================ TMA loads of K (warp 0) or V (warp 2)
         setmaxnreg_dec<kPagedRegsOther>();
-        auto load_tiles = [&](auto v_tag) {
-            constexpr bool is_v = decltype(v_tag)::value;
-            constexpr int kChunks = is_v ? Cfg::kVChunks : Cfg::kKChunks, kStageBytes = is_v ? Cfg::kVBytes : Cfg::kKBytes;
+        // (one piece of code for both: the instruction cache is what short sequences run into)
+        {
+            const bool is_v = warp == 2;
+            constexpr int kMaxChunks = Cfg::kKChunks > Cfg::kVChunks ? Cfg::kKChunks : Cfg::kVChunks;
+            const int chunks = is_v ? Cfg::kVChunks : Cfg::kKChunks, stage_bytes = is_v ? Cfg::kVBytes : Cfg::kKBytes;
             const CUtensorMap* tm = is_v ? &tm_v : &tm_k;
             uint64_t* const full = is_v ? sh.v_full : sh.k_full;
             uint64_t* const empty = is_v ? sh.v_empty : sh.k_empty;
@@ -386,21 +416,19 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                     const uint32_t bar = smem_addr(&full[s]);
                     const int n_box = min(boxes, (max(0, e.len - t * kTileN) + box - 1) / box);
                     if (!(is_v && p.debug_drop_v_load && n == 0)) {
-                        if (lane == 0) mbar_arrive_expect_tx(bar, n_box * box * 128 * kChunks);
+                        if (lane == 0) mbar_arrive_expect_tx(bar, n_box * box * 128 * chunks);
                         __syncwarp();
                         if (lane < n_box) {
 #pragma unroll
-                            for (int c = 0; c < kChunks; ++c)
-                                tma_load_4d(dst0 + s * kStageBytes + c * kChunkBytes + lane * box * 128, tm, bar, c * Cfg::kChunk, slot, e.kvh, page);
+                            for (int c = 0; c < kMaxChunks; ++c)
+                                if (c < chunks) tma_load_4d(dst0 + s * stage_bytes + c * kChunkBytes + lane * box * 128, tm, bar, c * Cfg::kChunk, slot, e.kvh, page);
                         }
                         __syncwarp();
                     }
                     if (++s == NS) { s = 0; parity ^= 1u; }
                 }
             }
-        };
-        if (warp == 0) load_tiles(std::false_type{});
-        else load_tiles(std::true_type{});
+        }
     } else if (warp == 1) {
         // ============================================================ score products, one thread
         setmaxnreg_dec<kPagedRegsOther>();
@@ -841,17 +869,25 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         constexpr int kPasses = (kRows + kPass - 1) / kPass;
         const int row_in = key / kLanes, piece = key % kLanes;
         uint4 xs[kPasses];
-        int place[kPasses];
         float q_scale = 1.f;
+        int q_rb = 0, o_rb = 0;       // the blocks whose rows sh.row_q and sh.row_o are
         auto load_queries = [&](int k) {
             const PagedEntry& e = sh.part[k % kPartRing];
+            if (e.rb != q_rb) {       // (uniform)
+                q_rb = e.rb;
+                named_barrier_sync(kBar, 128);         // (the rows before have been stored)
+                if (key < kRows) rows_of_q(q_rb, key);
+                named_barrier_sync(kBar, 128);
+            }
+            const __nv_bfloat16* const q = p.Q + e.b * p.q_sb + static_cast<long long>(e.kvh * group) * p.q_sh + piece * 8;
 #pragma unroll
             for (int j = 0; j < kPasses; ++j) {
-                const int r = j * kPass + row_in, rr = e.rb * kRows + r, i = rr / group, hq = e.kvh * group + rr - i * group;
+                const int r = j * kPass + row_in;
                 xs[j] = make_uint4(0, 0, 0, 0);
-                if (r < kRows && i < p.Sq && piece < kVecs)
-                    xs[j] = *reinterpret_cast<const uint4*>(p.Q + e.b * p.q_sb + i * p.q_st + hq * p.q_sh + piece * 8);
-                place[j] = min(i, p.Sq - 1);
+                if (r < kRows && piece < kVecs) {
+                    const long long at = sh.row_q[r];
+                    if (at >= 0) xs[j] = *reinterpret_cast<const uint4*>(q + at);
+                }
             }
             q_scale = p.scale_log2 * (kE4m3 && p.k_scale ? p.k_scale[e.kvh] : 1.f);
         };
@@ -902,8 +938,8 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                     }
                 }
                 if (r < kRows && piece == 0) {
-                    sh.c[qb][r] = c;
-                    sh.i[qb][r] = place[j];
+                    if constexpr (kE4m3) sh.c[qb][r] = c;
+                    sh.i[qb][r] = sh.row_place[r];
                 }
             }
             fence_proxy_async_smem();
@@ -915,7 +951,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         int end_at = 0x7fffffff;                   // the end mark's place, once seen
         for (int k = -3; k < end_at; ++k) {
             if (wq == 3 && !marked && published < max(k, 0) + kPartRing - 3) publish(max(k, 0));
-            if (k + 3 < end_at) ok = ok && wait_part_timed(k + 3);
+            if (k + 3 < end_at) ok = ok && wait_part(k + 3);       // (which waits for nobody)
             // whether all other pieces of an unfinished row block are there already: then this one need not be announced
             if (k >= 0 && key == 0 && sh.part[k % kPartRing].slot >= 0) {
                 const PagedEntry& mine_part = sh.part[k % kPartRing];
@@ -936,43 +972,68 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             const PagedEntry e = sh.part[k % kPartRing];
             const int ob = k % kOBufs;
             const bool whole = e.slot < 0;
-            if (key < kRows) {
-                const int rr = e.rb * kRows + key, i = rr / group, hq = e.kvh * group + rr - i * group;
-                sh.out_at[key] = i < p.Sq ? e.b * p.o_sb + i * p.o_st + hq * p.o_sh : -1;
-                sh.out_hq[key] = hq;
-                sh.out_i[key] = i;
+            if (e.rb != o_rb) {           // (uniform; the barrier that the round began with: nobody reads the old ones any more)
+                o_rb = e.rb;
+                if (key < kRows) rows_of_o(o_rb, key);
+                named_barrier_sync(kBar, 128);
             }
+            const int hq0 = e.kvh * group;
+            __nv_bfloat16* const out = p.O + e.b * p.o_sb + hq0 * p.o_sh;
             const float vs = kE4m3 && p.v_scale ? p.v_scale[e.kvh] : 1.f;
             float* const slot_o = p.part + static_cast<long long>(whole ? 0 : e.slot) * kStates * (DV + 2);
             float* const slot_ml = slot_o + kStates * DV;
+            // A row block of two pieces: the CTA that joins them takes its own from registers, and where the other's is known to be there
+            // its loads run under the last products.  (Other blocks are joined from memory, further below.)
+            const bool two = !whole && e.pieces == 2, own_first = static_cast<int>(blockIdx.x) == e.first_cta;
+            const bool known = two && sh.is_last[k & 1] != 0u;
+            const float* const other_o = p.part + (own_first ? 2ll * (e.first_cta + 1) : e.first_slot) * kStates * (DV + 2);
+            float other[kStates <= 16 ? kStates : 1], other_m = -INFINITY, other_l = 0.f, own_m = -INFINITY, own_l = 0.f;
+            auto load_other = [&]() {
+                if (key < kStates) {
+                    other_m = __ldcg(other_o + kStates * DV + key);
+                    other_l = __ldcg(other_o + kStates * DV + kStates + key);
+                }
+                if constexpr (kStates <= 16) {
+#pragma unroll
+                    for (int r = 0; r < kStates; ++r) other[r] = key < DV ? __ldcg(other_o + r * DV + key) : 0.f;
+                }
+            };
+            if (known) load_other();
             // log-sum-exp of a row (natural units) from its maximum (log2 units) and sum
             auto store_lse = [&](int r, float m, float sum) {
-                if (kDiff || !p.lse || sh.out_at[r] < 0) return;
-                p.lse[static_cast<long long>(sh.out_hq[r]) * p.B * p.Sq + static_cast<long long>(e.b) * p.Sq + sh.out_i[r]] =
+                if (kDiff || !p.lse || sh.row_o[r] < 0) return;
+                p.lse[static_cast<long long>(hq0 + sh.row_h[r]) * p.B * p.Sq + static_cast<long long>(e.b) * p.Sq + sh.row_i[r]] =
                     sum > 0.f || sum != sum ? (m - Cfg::kBias + log2f(sum)) * 0.6931471805599453f : -INFINITY;
             };
-            named_barrier_sync(kBar, 128);
             // (uniform) whether a group had a tile of this part
             const bool had[2] = {e.t1 - e.t0 > 1 || (e.tile0 & 1) == 0, e.t1 - e.t0 > 1 || (e.tile0 & 1) == 1};
-            if (key < kStates) {
+            // (the first two warps the factors, the other two the log-sum-exps: each takes some 300 cycles)
+            const int st = key & 63;
+            if (st < kStates) {
                 float f[2], sum[2], mx[2];
 #pragma unroll
                 for (int v = 0; v < 2; ++v) {
-                    mx[v] = had[v] ? sh.stat_m[k % kPartRing][v][key] : -INFINITY;
-                    sum[v] = had[v] ? sh.stat_l[k % kPartRing][v][key] : 0.f;
+                    mx[v] = had[v] ? sh.stat_m[k % kPartRing][v][st] : -INFINITY;
+                    sum[v] = had[v] ? sh.stat_l[k % kPartRing][v][st] : 0.f;
                 }
                 const float m = fmaxf(mx[0], mx[1]);
 #pragma unroll
                 for (int v = 0; v < 2; ++v) f[v] = mx[v] == -INFINITY ? 0.f : exp2_approx(mx[v] - m);
                 const float all = f[0] * sum[0] + f[1] * sum[1];
-                const float norm = !whole ? 1.f : (all > 0.f || all != all ? 1.f / all : 0.f);
-                sh.factor[0][key] = f[0] * norm;
-                sh.factor[1][key] = f[1] * norm;
-                if (whole) {
-                    store_lse(key % kRows, m, all);
+                if (key >= 64) {
+                    if (whole) store_lse(st % kRows, m, all);
                 } else {
-                    slot_ml[key] = m;
-                    slot_ml[kStates + key] = all;
+                    const float norm = !whole ? 1.f : (all > 0.f || all != all ? 1.f / all : 0.f);
+                    sh.factor[0][st] = f[0] * norm;
+                    sh.factor[1][st] = f[1] * norm;
+                    if (!whole) {
+                        own_m = m;
+                        own_l = all;
+                        if (!known) {
+                            slot_ml[st] = m;
+                            slot_ml[kStates + st] = all;
+                        }
+                    }
                 }
             }
             ok = ok && paged_wait_timed(&sh.acc_full[ob], (k / kOBufs) & 1, wait, kSiteEpiOFull);
@@ -1007,7 +1068,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             auto store_rows = [&]() {
                 if constexpr (kDiff) {
 #pragma unroll
-                    for (int r = 0; r < kRows; ++r) y[r] = vs * (y[r] - p.lambda[sh.out_hq[r]] * y[kRows + r]);
+                    for (int r = 0; r < kRows; ++r) y[r] = vs * (y[r] - p.lambda[hq0 + sh.row_h[r]] * y[kRows + r]);
                     if (p.weight) {
 #pragma unroll
                         for (int r = 0; r < kRows; ++r) {
@@ -1033,14 +1094,16 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                 if (key < DV) {
 #pragma unroll
                     for (int r = 0; r < kRows; ++r) {
-                        const long long at = sh.out_at[r];
-                        if (at >= 0) p.O[at + key] = __float2bfloat16(y[r]);
+                        const long long at = sh.row_o[r];
+                        if (at >= 0) out[at + key] = __float2bfloat16(y[r]);
                     }
                 }
             };
             if (whole) {
                 store_rows();
-            } else {
+                continue;
+            }
+            if (!known) {
                 if (key < DV) {
 #pragma unroll
                     for (int r = 0; r < kStates; ++r) slot_o[r * DV + key] = y[r];
@@ -1055,107 +1118,129 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                     __threadfence();
                 }
                 named_barrier_sync(kBar, 128);
-                if (sh.is_last[k & 1]) {
-                    // This CTA finished last: all pieces, in the order of the CTAs, kMergePieces at a time under a running maximum.  A
-                    // thread has four columns of every kGroups-th state (both maps of a row are its own); the first loads go out
-                    // before the weights that they wait for.  (The pieces behind the first are the first parts of their CTAs.)
-                    constexpr int kGroups = 128 / (DV / 4), kMine = kStates / kGroups, kBatch = kMine <= 4 ? 2 : 1;
-                    static_assert(kRows % kGroups == 0, "both maps of a row in one thread");
-                    const int col = key % (DV / 4) * 4, g0 = key / (DV / 4);
-                    auto piece = [&](int c) {
-                        return p.part + (c == 0 ? e.first_slot : 2ll * (e.first_cta + c)) * kStates * (DV + 2);
-                    };
-                    float4 z[kMine], v[kBatch][kMine];
+            }
+            if (!sh.is_last[k & 1]) continue;
+            if (two) {
+                // the two pieces' sum, in the order of the CTAs whichever of them has it
+                if (!known) load_other();
+                if (key < kStates) {
+                    const float m = fmaxf(own_m, other_m);
+                    const float f_own = own_m == -INFINITY ? 0.f : exp2_approx(own_m - m), f_other = other_m == -INFINITY ? 0.f : exp2_approx(other_m - m);
+                    const float l0 = own_first ? f_own * own_l : f_other * other_l;
+                    const float sum = own_first ? fmaf(f_other, other_l, l0) : fmaf(f_own, own_l, l0);
+                    const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+                    sh.factor[0][key] = f_own * inv;
+                    sh.factor[1][key] = f_other * inv;
+                    store_lse(key % kRows, m, sum);
+                }
+                named_barrier_sync(kBar, 128);
 #pragma unroll
-                    for (int j = 0; j < kMine; ++j) z[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-                    auto load_batch = [&](int c) {
+                for (int r = 0; r < kStates; ++r) {
+                    const float x = kStates <= 16 ? other[kStates <= 16 ? r : 0] : key < DV ? __ldcg(other_o + r * DV + key) : 0.f;
+                    const float f_own = sh.factor[0][r], f_other = sh.factor[1][r];
+                    y[r] = own_first ? fmaf(f_other, x, f_own * y[r]) : fmaf(f_own, y[r], f_other * x);
+                }
+                store_rows();
+            } else {
+                // This CTA finished last: all pieces, in the order of the CTAs, kMergePieces at a time under a running maximum.  A
+                // thread has four columns of every kGroups-th state (both maps of a row are its own); the first loads go out
+                // before the weights that they wait for.  (The pieces behind the first are the first parts of their CTAs.)
+                constexpr int kGroups = 128 / (DV / 4), kMine = kStates / kGroups, kBatch = kMine <= 4 ? 2 : 1;
+                static_assert(kRows % kGroups == 0, "both maps of a row in one thread");
+                const int col = key % (DV / 4) * 4, g0 = key / (DV / 4);
+                auto piece = [&](int c) {
+                    return p.part + (c == 0 ? e.first_slot : 2ll * (e.first_cta + c)) * kStates * (DV + 2);
+                };
+                float4 z[kMine], v[kBatch][kMine];
+#pragma unroll
+                for (int j = 0; j < kMine; ++j) z[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                auto load_batch = [&](int c) {
+#pragma unroll
+                    for (int q = 0; q < kBatch; ++q) {
+                        if (c + q >= e.pieces) break;
+                        const float* po = piece(c + q) + g0 * DV + col;
+#pragma unroll
+                        for (int j = 0; j < kMine; ++j) v[q][j] = __ldcg(reinterpret_cast<const float4*>(po + j * kGroups * DV));
+                    }
+                };
+                float run_m = -INFINITY, run_l = 0.f;
+#pragma unroll 1
+                for (int c0 = 0; c0 < e.pieces; c0 += kMergePieces) {
+                    const int nc = min(kMergePieces, e.pieces - c0);
+                    load_batch(c0);
+                    for (int j = key; j < nc * kStates; j += 128) {
+                        const float* ml = piece(c0 + j / kStates) + kStates * DV + j % kStates;
+                        sh.piece_m[j / kStates][j % kStates] = __ldcg(ml);
+                        sh.piece_l[j / kStates][j % kStates] = __ldcg(ml + kStates);
+                    }
+                    named_barrier_sync(kBar, 128);
+                    if (key < kStates) {
+                        float m = run_m;
+                        for (int c = 0; c < nc; ++c) m = fmaxf(m, sh.piece_m[c][key]);
+                        const float keep = run_m == -INFINITY ? 0.f : exp2_approx(run_m - m);
+                        float sum = run_l * keep;
+                        for (int c = 0; c < nc; ++c) {
+                            const float mc = sh.piece_m[c][key];
+                            const float f = mc == -INFINITY ? 0.f : exp2_approx(mc - m);
+                            // (a piece without a finite score counts nothing, but a NaN of its sum goes through)
+                            sum += f * sh.piece_l[c][key];
+                            sh.piece_m[c][key] = f;
+                        }
+                        sh.factor[0][key] = keep;
+                        run_m = m;
+                        run_l = sum;
+                        // (read after the last round)
+                        sh.factor[1][key] = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+                    }
+                    named_barrier_sync(kBar, 128);
+#pragma unroll
+                    for (int j = 0; j < kMine; ++j) {
+                        const float keep = sh.factor[0][g0 + j * kGroups];
+                        z[j].x *= keep; z[j].y *= keep; z[j].z *= keep; z[j].w *= keep;
+                    }
+#pragma unroll 1
+                    for (int c = 0; c < nc; c += kBatch) {
+                        if (c > 0) load_batch(c0 + c);
 #pragma unroll
                         for (int q = 0; q < kBatch; ++q) {
-                            if (c + q >= e.pieces) break;
-                            const float* po = piece(c + q) + g0 * DV + col;
+                            if (c + q >= nc) break;
 #pragma unroll
-                            for (int j = 0; j < kMine; ++j) v[q][j] = __ldcg(reinterpret_cast<const float4*>(po + j * kGroups * DV));
-                        }
-                    };
-                    float run_m = -INFINITY, run_l = 0.f;
-#pragma unroll 1
-                    for (int c0 = 0; c0 < e.pieces; c0 += kMergePieces) {
-                        const int nc = min(kMergePieces, e.pieces - c0);
-                        load_batch(c0);
-                        for (int j = key; j < nc * kStates; j += 128) {
-                            const float* ml = piece(c0 + j / kStates) + kStates * DV + j % kStates;
-                            sh.piece_m[j / kStates][j % kStates] = __ldcg(ml);
-                            sh.piece_l[j / kStates][j % kStates] = __ldcg(ml + kStates);
-                        }
-                        named_barrier_sync(kBar, 128);
-                        if (key < kStates) {
-                            float m = run_m;
-                            for (int c = 0; c < nc; ++c) m = fmaxf(m, sh.piece_m[c][key]);
-                            const float keep = run_m == -INFINITY ? 0.f : exp2_approx(run_m - m);
-                            float sum = run_l * keep;
-                            for (int c = 0; c < nc; ++c) {
-                                const float mc = sh.piece_m[c][key];
-                                const float f = mc == -INFINITY ? 0.f : exp2_approx(mc - m);
-                                // (a piece without a finite score counts nothing, but a NaN of its sum goes through)
-                                sum += f * sh.piece_l[c][key];
-                                sh.piece_m[c][key] = f;
-                            }
-                            sh.factor[0][key] = keep;
-                            run_m = m;
-                            run_l = sum;
-                            // (read after the last round)
-                            sh.factor[1][key] = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
-                        }
-                        named_barrier_sync(kBar, 128);
-#pragma unroll
-                        for (int j = 0; j < kMine; ++j) {
-                            const float keep = sh.factor[0][g0 + j * kGroups];
-                            z[j].x *= keep; z[j].y *= keep; z[j].z *= keep; z[j].w *= keep;
-                        }
-#pragma unroll 1
-                        for (int c = 0; c < nc; c += kBatch) {
-                            if (c > 0) load_batch(c0 + c);
-#pragma unroll
-                            for (int q = 0; q < kBatch; ++q) {
-                                if (c + q >= nc) break;
-#pragma unroll
-                                for (int j = 0; j < kMine; ++j) {
-                                    const float f = sh.piece_m[c + q][g0 + j * kGroups];
-                                    z[j].x = fmaf(f, v[q][j].x, z[j].x);
-                                    z[j].y = fmaf(f, v[q][j].y, z[j].y);
-                                    z[j].z = fmaf(f, v[q][j].z, z[j].z);
-                                    z[j].w = fmaf(f, v[q][j].w, z[j].w);
-                                }
+                            for (int j = 0; j < kMine; ++j) {
+                                const float f = sh.piece_m[c + q][g0 + j * kGroups];
+                                z[j].x = fmaf(f, v[q][j].x, z[j].x);
+                                z[j].y = fmaf(f, v[q][j].y, z[j].y);
+                                z[j].z = fmaf(f, v[q][j].z, z[j].z);
+                                z[j].w = fmaf(f, v[q][j].w, z[j].w);
                             }
                         }
-                        if (c0 + kMergePieces < e.pieces) named_barrier_sync(kBar, 128);
                     }
-#pragma unroll
-                    for (int j = 0; j < kRows / kGroups; ++j) {
-                        const int r = g0 + j * kGroups;
-                        const float f0 = vs * sh.factor[1][r];
-                        float4 o = make_float4(f0 * z[j].x, f0 * z[j].y, f0 * z[j].z, f0 * z[j].w);
-                        if constexpr (kDiff) {
-                            const float4 o1 = z[j + kRows / kGroups];
-                            const float f1 = vs * sh.factor[1][kRows + r] * p.lambda[sh.out_hq[r]];
-                            o.x -= f1 * o1.x; o.y -= f1 * o1.y; o.z -= f1 * o1.z; o.w -= f1 * o1.w;
-                            float f = p.out_scale;
-                            float4 w = make_float4(1.f, 1.f, 1.f, 1.f);
-                            if (p.weight) {
-                                float q = o.x * o.x + o.y * o.y + o.z * o.z + o.w * o.w;        // (a row is a warp's)
-#pragma unroll
-                                for (int d = 16; d > 0; d >>= 1) q += __shfl_xor_sync(0xffffffffu, q, d);
-                                f *= rsqrtf(q * (1.f / DV) + p.eps);
-                                w = __ldg(reinterpret_cast<const float4*>(p.weight + col));
-                            }
-                            o.x *= f * w.x; o.y *= f * w.y; o.z *= f * w.z; o.w *= f * w.w;
-                        }
-                        const long long at = sh.out_at[r];
-                        if (at >= 0)
-                            *reinterpret_cast<uint2*>(p.O + at + col) = make_uint2(pack_bf16x2(o.x, o.y), pack_bf16x2(o.z, o.w));
-                    }
-                    if (key < kStates) store_lse(key % kRows, run_m, run_l);
+                    if (c0 + kMergePieces < e.pieces) named_barrier_sync(kBar, 128);
                 }
+#pragma unroll
+                for (int j = 0; j < kRows / kGroups; ++j) {
+                    const int r = g0 + j * kGroups;
+                    const float f0 = vs * sh.factor[1][r];
+                    float4 o = make_float4(f0 * z[j].x, f0 * z[j].y, f0 * z[j].z, f0 * z[j].w);
+                    if constexpr (kDiff) {
+                        const float4 o1 = z[j + kRows / kGroups];
+                        const float f1 = vs * sh.factor[1][kRows + r] * p.lambda[hq0 + sh.row_h[r]];
+                        o.x -= f1 * o1.x; o.y -= f1 * o1.y; o.z -= f1 * o1.z; o.w -= f1 * o1.w;
+                        float f = p.out_scale;
+                        float4 w = make_float4(1.f, 1.f, 1.f, 1.f);
+                        if (p.weight) {
+                            float q = o.x * o.x + o.y * o.y + o.z * o.z + o.w * o.w;        // (a row is a warp's)
+#pragma unroll
+                            for (int d = 16; d > 0; d >>= 1) q += __shfl_xor_sync(0xffffffffu, q, d);
+                            f *= rsqrtf(q * (1.f / DV) + p.eps);
+                            w = __ldg(reinterpret_cast<const float4*>(p.weight + col));
+                        }
+                        o.x *= f * w.x; o.y *= f * w.y; o.z *= f * w.z; o.w *= f * w.w;
+                    }
+                    const long long at = sh.row_o[r];
+                    if (at >= 0)
+                        *reinterpret_cast<uint2*>(out + at + col) = make_uint2(pack_bf16x2(o.x, o.y), pack_bf16x2(o.z, o.w));
+                }
+                if (key < kStates) store_lse(key % kRows, run_m, run_l);
             }
             // (the barrier that the next round begins with comes before anything of this round's is overwritten)
         }
