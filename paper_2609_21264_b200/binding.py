@@ -556,6 +556,12 @@ def _rows(t, cache, d, what):
     return n, heads, st, sh
 
 
+def _new(q, tokens, heads, d):
+    """A contiguous [tokens, heads, d] tensor of q's type (the cheapest way to it)."""
+    import torch
+    return torch.empty_like(q) if q.shape[2] == d and q.is_contiguous() else q.new_empty((tokens, heads, d))
+
+
 def append_paged(h, k, v, cache: PagedCache, block_table, seq_lens, *, cu_seqlens=None, q=None, q_out=None, rope: Rope = None):
     """New keys and values [T, Hkv, d] of packed tokens into `cache`, rotated by their positions; returns q_out.
 
@@ -586,10 +592,12 @@ def append_paged(h, k, v, cache: PagedCache, block_table, seq_lens, *, cu_seqlen
         if Tq != total:
             raise ValueError("q must have the tokens of k")
         if q_out is None:
-            q_out = torch.empty((total, Hq, cache.dqk), dtype=torch.bfloat16, device=q.device)
-        To, Ho, ot, oh = _rows(q_out, cache, cache.dqk, "q_out")
-        if To != total or Ho != Hq:
-            raise ValueError("q_out must have q's shape")
+            q_out = _new(q, total, Hq, cache.dqk)
+            ot, oh = Hq * cache.dqk, cache.dqk
+        else:
+            To, Ho, ot, oh = _rows(q_out, cache, cache.dqk, "q_out")
+            if To != total or Ho != Hq:
+                raise ValueError("q_out must have q's shape")
         q_ptr, qo_ptr = q.data_ptr(), q_out.data_ptr()
     elif q_out is not None:
         raise ValueError("q_out without q")
@@ -609,7 +617,7 @@ def _paged_out(q, cache, seqs, out):
     if seqs.B == 0 or T == 0 or T % seqs.B:
         raise ValueError("q must hold the same number of tokens for every sequence")
     if out is None:
-        out = torch.empty((T, Hq, cache.dv), dtype=torch.bfloat16, device=q.device)
+        out = _new(q, T, Hq, cache.dv)
         ot, oh = Hq * cache.dv, cache.dv
     else:
         To, Ho, ot, oh = _rows(out, cache, cache.dv, "out")
@@ -624,7 +632,7 @@ def forward_paged(h, q, cache: PagedCache, block_table, seq_lens, *, scale: floa
     import torch
     seqs = _seqs(h, cache, block_table, seq_lens)
     Hq, T, Sq, strides, out = _paged_out(q, cache, seqs, out)
-    lse = torch.empty((Hq, T), dtype=torch.float32, device=q.device) if want_lse else None
+    lse = q.new_empty((Hq, T), dtype=torch.float32) if want_lse else None
     at = ctypes.addressof(strides)
     st = _lib.fa_forward_paged(h, cache.address, ctypes.addressof(seqs), q.data_ptr(), out.data_ptr(),
                                None if lse is None else lse.data_ptr(), Hq, Sq, scale, at, at + 16, _raw_stream(cache.device))

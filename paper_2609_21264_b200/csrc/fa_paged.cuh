@@ -164,7 +164,9 @@ __host__ __device__ inline bool paged_entry(const PagedParams& p, int cta, int s
 
 // ------------------------------------------------------------------ configuration
 
-constexpr int kPartRing = 8, kMergePieces = 8;
+constexpr int kPartRing = 8;
+// pieces whose weights are found at a time (16 against 8: 8000 keys, 8 K/V heads, 18 pieces a row block, 18.7 to 18.2 us)
+__host__ __device__ constexpr int paged_merge_pieces(int states) { return states <= 32 ? 16 : 8; }
 
 // Registers per thread after the per-role reallocation (512 threads start with 128 each): 128 x 80 + 256 x 136 + 128 x 160 = 65536;
 // with 64 states per softmax thread 256 x 152 and 128 x 128.
@@ -194,6 +196,7 @@ struct PagedShared {
     float stat_m[kPartRing][2][kMaps * kRows], stat_l[kPartRing][2][kMaps * kRows];      // [part][group]
     // of the result warps
     float factor[2][kMaps * kRows];
+    static constexpr int kMergePieces = paged_merge_pieces(kMaps * kRows);
     float piece_m[kMergePieces][kMaps * kRows], piece_l[kMergePieces][kMaps * kRows];
     float sq[4][kRows];
     // The rows of a block, apart from the part's sequence and K/V head: offsets in Q and O (-1: a padding row), place among the new
@@ -1145,6 +1148,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                 // This CTA finished last: all pieces, in the order of the CTAs, kMergePieces at a time under a running maximum.  A
                 // thread has four columns of every kGroups-th state (both maps of a row are its own); the first loads go out
                 // before the weights that they wait for.  (The pieces behind the first are the first parts of their CTAs.)
+                constexpr int kMergePieces = Shared::kMergePieces;
                 constexpr int kGroups = 128 / (DV / 4), kMine = kStates / kGroups, kBatch = kMine <= 4 ? 2 : 1;
                 static_assert(kRows % kGroups == 0, "both maps of a row in one thread");
                 const int col = key % (DV / 4) * 4, g0 = key / (DV / 4);
