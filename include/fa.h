@@ -508,7 +508,7 @@ fa_status fa_forward_paged(fa_handle* h, const fa_paged_cache* cache, const fa_p
 /*
  * How fa_forward_paged would deal out a batch, the counterpart of fa_plan: a pure host function that makes the kernel's own list
  * of work units (one unit = 128 keys of one sequence, K/V head and block of query rows, and part_cost units for each such
- * block).  seqs->seq_lens is a HOST array here, block_table and the cache's pointers and strides are not looked at.  `pieces`
+ * block; in small calls the tiles of a block count as a multiple of units_per_cta, so that a CTA has one part).  seqs->seq_lens is a HOST array here, block_table and the cache's pointers and strides are not looked at.  `pieces`
  * receives up to max_pieces entries, in the order of the CTAs; out->pieces is their number in any case.
  */
 typedef struct fa_paged_plan_info {

@@ -110,7 +110,7 @@ int rows_per_block(int rows, int dqk, bool e4m3, bool diff) {
 // Tiles of 128 keys that a call's list of work can have at most; the kernel counts them in 32 bits.
 long long most_units(const fa::PagedParams& p) {
     return static_cast<long long>(p.B) * p.Hkv * p.row_blocks *
-           (fa::paged_tiles(static_cast<int>(static_cast<long long>(p.max_pages) * p.page_size)) + fa::kPartCost);
+           (fa::paged_tiles(static_cast<int>(static_cast<long long>(p.max_pages) * p.page_size)) + fa::kMostPartCost);
 }
 
 // CTAs of a launch: one per SM, as many as there can be units, and as many as the scratch has two partial results for.
@@ -119,6 +119,15 @@ int paged_ctas(int num_sms, size_t scratch_bytes, const fa::PagedParams& p, int 
     if (ctas > most_units(p)) ctas = most_units(p);
     const long long fit = static_cast<long long>(scratch_bytes / (2 * fa::paged_slot_bytes(dv, states)));
     return static_cast<int>(ctas > fit ? fit : ctas);
+}
+
+// The list's constants (fa_paged.cuh): the units that a row block counts beside its tiles are what 128 KB of tiles are, and it
+// counts them up to 768 KB.
+void set_list(fa::PagedParams& p, int dqk, int dv, bool e4m3) {
+    const int tile = 128 * (dqk + dv) * (e4m3 ? 1 : 2), units = (128 << 10) / tile;
+    p.least_units = kLeastUnits;
+    p.part_cost = units > fa::kMostPartCost ? fa::kMostPartCost : units;
+    p.long_tiles = (768 << 10) / tile;
 }
 
 // The streaming kernel with blocks of kRows query rows.
@@ -193,7 +202,7 @@ fa_status forward_paged(fa_handle* h, const fa_paged_cache* cache, const fa_page
     }
     p.box_rows = 16;
     while (p.box_rows < 128 && cache->page_size % (2 * p.box_rows) == 0) p.box_rows *= 2;
-    p.least_units = kLeastUnits;
+    set_list(p, cache->dqk, cache->dv, e4m3);
     const int rows = Hq / cache->Hkv * Sq, block = rows_per_block(rows, cache->dqk, e4m3, diff != nullptr);
     p.row_blocks = (rows + block - 1) / block;
     if (most_units(p) > 0x7fff0000LL) return FA_ERR_UNSUPPORTED;
@@ -412,20 +421,25 @@ fa_status fa_plan_paged(int num_sms, const fa_config* cfg, const fa_paged_cache*
     p.B = seqs->B; p.max_pages = seqs->max_pages; p.page_size = cache->page_size; p.Hkv = cache->Hkv; p.Hq = Hq; p.Sq = Sq;
     const int rows = Hq / cache->Hkv * Sq, block = rows_per_block(rows, cache->dqk, cache->type == FA_CACHE_E4M3, diff != 0);
     p.row_blocks = (rows + block - 1) / block;
-    p.least_units = kLeastUnits;
+    set_list(p, cache->dqk, cache->dv, cache->type == FA_CACHE_E4M3);
     if (most_units(p) > 0x7fff0000LL) return FA_ERR_UNSUPPORTED;
     const int ctas = paged_ctas(num_sms, static_cast<size_t>(scratch), p, cache->dv, (diff ? 2 : 1) * block);
     if (ctas < 1) return FA_ERR_UNSUPPORTED;
     int longest = 0, total = 0;
-    for (int b = 0; b < p.B; ++b) longest = fa::paged_len(p, b, nullptr) > longest ? fa::paged_len(p, b, nullptr) : longest;
-    const int pad = fa::paged_pad(p, ctas, fa::paged_tiles(longest));
-    auto units_of = [&](int b) { return fa::paged_units(p, fa::paged_len(p, b, nullptr), pad); };
+    for (int b = 0; b < p.B; ++b) {
+        const int n = fa::paged_len(p, b, nullptr);
+        longest = n > longest ? n : longest;
+        total += fa::paged_units(p, n, fa::PagedCount{0, 0, 0});
+    }
+    const fa::PagedCount cnt = fa::paged_count(p, ctas, fa::paged_tiles(longest), total);
+    auto units_of = [&](int b) { return fa::paged_units(p, fa::paged_len(p, b, nullptr), cnt); };
+    total = 0;
     for (int b = 0; b < p.B; ++b) total += units_of(b);
-    const int share = fa::paged_share(total, ctas, p.least_units, pad);
+    const int share = fa::paged_share(p, total, ctas, cnt);
     out->rows_per_block = block;
     out->row_blocks = p.row_blocks;
     out->ctas = ctas;
-    out->part_cost = fa::kPartCost;
+    out->part_cost = cnt.cost;
     out->units = total;
     out->units_per_cta = share;
     long long n = 0;
@@ -436,7 +450,7 @@ fa_status fa_plan_paged(int num_sms, const fa_config* cfg, const fa_paged_cache*
         for (int b = b0, base = base0; b < p.B && base < u1; base += units_of(b), ++b) {
             for (int hr = 0; hr < p.Hkv * p.row_blocks; ++hr) {
                 fa::PagedEntry e;
-                if (!fa::paged_entry(p, c, share, u0, u1, b, base, fa::paged_len(p, b, nullptr), pad, hr, e)) continue;
+                if (!fa::paged_entry(p, c, share, u0, u1, b, base, fa::paged_len(p, b, nullptr), cnt, hr, e)) continue;
                 if (n < max_pieces) {
                     fa_paged_piece* x = pieces + n;
                     x->cta = c;

@@ -11,7 +11,7 @@
 //   * The tiles of all sequences and heads form one list; CTA c takes the c-th of equal consecutive shares (the lengths are read on
 //     the device).  Lengths that differ by orders of magnitude cost nothing, and no SM waits for a wave.  A (sequence, head)
 //     that several CTAs share is joined by the one that finishes last, in the order of the CTAs (equal calls give equal bits).
-//   * A ring of K/V tiles (two to five stages, all that the shared memory holds) runs across the boundaries of sequences.
+//   * A ring of K/V tiles (two to six stages, all that the shared memory holds) runs across the boundaries of sequences.
 //
 // Two groups of four softmax warps take the tiles in turn; each has its own scores (two buffers), probabilities (two), reference maximum,
 // row sums and accumulator, so that no tile waits for the one before it.  A thread owns a key of the tile: the row maximum runs
@@ -98,34 +98,53 @@ FA_DEVI bool paged_wait_timed(uint64_t* bar, uint32_t parity, PagedWait* ctx, ui
 
 // ------------------------------------------------------------------ the list of work units and its shares
 
-// The list holds every (sequence, K/V head, block of rows) in that order, each as kPartCost units for what a part costs beside its
-// tiles (query rows, first maxima, result) and one unit per tile of 128 keys; a sequence without keys has one empty tile, so that
-// its rows are written.  CTA c takes units [c * share, (c + 1) * share).  Without the extra unit the CTAs that got the batch's
-// short sequences finish last (64 sequences of 65 to 4096 keys: 97.4 us, against 99.5; 4096 row blocks of 200 keys 95.4, against
-// 96.4; but 160 row blocks of 192/128 over 148 CTAs 31.6, against 30.2).
+// The list holds every (sequence, K/V head, block of rows) in that order, one unit per tile of 128 keys; a sequence without keys has
+// one empty tile, so that its rows are written.  CTA c takes units [c * share, (c + 1) * share).
+//
+// What a row block costs beside its tiles (query rows, first maxima, result: about what 128 KB take to load) is counted in units
+// too where there are row blocks for all CTAs and they are short, or the CTAs that got the batch's short sequences would
+// finish last: 48 sequences of 65 to 1000 keys, 8 K/V heads, 25.2 us with two units for it, 27.7 with one, 34.5 without; over
+// e4m3 23.2 with three, 36 without.  With more than 768 KB in a block on average most CTAs have equally many parts and the bytes
+// alone decide (160 row blocks 192/128 of 10 tiles 29.8 us, with one unit 31.2; 64 sequences of 65 to 4096 keys level).
 // (The host refuses calls whose list could be longer than 32 bits can count.)
 //
 // Small calls: joining the pieces of a row block costs 4 to 5 us, a tile 0.6 us of a CTA's time.  So where there is a CTA for every row
 // block and no sequence has more than kWholeTiles tiles, all blocks count as many units as the longest (`pad` tiles), the shares
-// fall on their borders, and nothing is split (400 keys, 8 K/V heads: 9.4 us, against 11.3).
-constexpr int kPartCost = 1, kWholeTiles = 6;
+// fall on their borders, and nothing is split (400 keys, 8 K/V heads: 9.4 us, against 11.3).  The blocks of a single sequence
+// count a multiple of the share, so that a CTA has one part (777 keys 11.1 us, against 12.3; 8000 keys 18.3, against 20.1).
+constexpr int kMostPartCost = 3, kWholeTiles = 6;
 __host__ __device__ inline int paged_tiles(int len) { return len > 0 ? (len + kTileN - 1) / kTileN : 1; }
 __host__ __device__ inline int paged_len(const PagedParams& p, int b, uint32_t* status) {
     return clamped_len(p.seq_lens[b], p.max_pages, p.page_size, status);
 }
-__host__ __device__ inline int paged_pad(const PagedParams& p, int ctas, int most_tiles) {
-    return most_tiles <= kWholeTiles && static_cast<long long>(p.B) * p.Hkv * p.row_blocks <= ctas ? most_tiles : 0;
+// How a call's units are counted: tiles that every row block has at least (0: its own), units beside them, a CTA's share (0: what
+// the total gives).
+struct PagedCount { int pad, cost, share; };
+__host__ __device__ inline PagedCount paged_count(const PagedParams& p, int ctas, int most_tiles, int all_tiles) {
+    const long long blocks = static_cast<long long>(p.B) * p.Hkv * p.row_blocks;
+    PagedCount c{0, 0, 0};
+    if (most_tiles <= kWholeTiles && blocks <= ctas) {
+        c.pad = c.share = most_tiles;
+    } else if (p.B == 1 && 2 * blocks <= ctas) {
+        // (a block has less than one share more than its tiles fill: the shares do not outnumber the CTAs)
+        const int spare = ctas - static_cast<int>(blocks), per = (all_tiles + spare - 1) / spare;
+        c.share = per < p.least_units ? p.least_units : per;
+        c.pad = (most_tiles + c.share - 1) / c.share * c.share;
+    } else if (blocks >= ctas && all_tiles < p.long_tiles * blocks) {
+        c.cost = p.part_cost;
+    }
+    return c;
 }
 // Units of a row block, and of a sequence, from its length.
-__host__ __device__ inline int paged_block_units(int len, int pad) {
+__host__ __device__ inline int paged_block_units(int len, PagedCount c) {
     const int nt = paged_tiles(len);
-    return (nt < pad ? pad : nt) + kPartCost;
+    return (nt < c.pad ? c.pad : nt) + c.cost;
 }
-__host__ __device__ inline int paged_units(const PagedParams& p, int len, int pad) { return paged_block_units(len, pad) * p.Hkv * p.row_blocks; }
-__host__ __device__ inline int paged_share(int units, int ctas, int least, int pad) {
-    if (pad > 0) return pad + kPartCost;
+__host__ __device__ inline int paged_units(const PagedParams& p, int len, PagedCount c) { return paged_block_units(len, c) * p.Hkv * p.row_blocks; }
+__host__ __device__ inline int paged_share(const PagedParams& p, int units, int ctas, PagedCount c) {
+    if (c.share > 0) return c.share;
     const int per = static_cast<int>((static_cast<unsigned>(units) + ctas - 1) / ctas);
-    return per < least ? least : per;
+    return per < p.least_units ? p.least_units : per;
 }
 
 // A part of the list as the roles of a CTA see it: tiles [t0, t1) of one (sequence, K/V head, row block).
@@ -139,9 +158,9 @@ struct PagedEntry {
 
 // What CTA `cta` with units [u0, u1) has of row block hr = head * row_blocks + block of sequence b, whose first unit is `base`;
 // false where that is nothing.  A CTA leaves at most two parts unfinished, its first and its last: two slots for partial results.
-__host__ __device__ inline bool paged_entry(const PagedParams& p, int cta, int share, int u0, int u1, int b, int base, int len, int pad, int hr,
+__host__ __device__ inline bool paged_entry(const PagedParams& p, int cta, int share, int u0, int u1, int b, int base, int len, PagedCount c, int hr,
                                             PagedEntry& e) {
-    const int nt = paged_tiles(len), ub = base + (hr + 1) * paged_block_units(len, pad), ua = ub - nt;       // units of its tiles
+    const int nt = paged_tiles(len), ub = base + (hr + 1) * paged_block_units(len, c), ua = ub - nt;       // units of its tiles
     const int v0 = u0 > ua ? u0 : ua, v1 = u1 < ub ? u1 : ub;
     e.b = b;
     e.kvh = hr / p.row_blocks;
@@ -761,15 +780,15 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         const uint32_t lane_sel = static_cast<uint32_t>(wq * 32) << 16;
         constexpr uint32_t kBar = 3;
         bool ok = true;
-        // the shares: every thread sums up the units of consecutive sequences, a scan over the group finds the total and the
-        // sequence that the CTA's share begins in
+        // the shares: every thread sums up the tiles of consecutive sequences, a scan over the group finds the total, which decides how
+        // units are counted, and the sequence that the CTA's share begins in
         const int chunk = (p.B + 127) / 128;
         const int b_first = key * chunk, b_last = min(p.B, b_first + chunk);
         int mine = 0, longest = 0;
 #pragma unroll 4
         for (int b = b_first; b < b_last; ++b) {
             const int n = paged_len(p, b, nullptr);
-            mine += paged_units(p, n, 0);
+            mine += paged_units(p, n, PagedCount{0, 0, 0});
             longest = max(longest, n);
         }
         longest = __reduce_max_sync(0xffffffffu, longest);
@@ -791,19 +810,25 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             total += n;
         }
         longest = max(max(sh.warp_longest[0], sh.warp_longest[1]), max(sh.warp_longest[2], sh.warp_longest[3]));
-        const int pad = paged_pad(p, gridDim.x, paged_tiles(longest));
-        if (pad > 0) {           // all sequences count the same
-            const int units = paged_units(p, longest, pad);
+        const PagedCount cnt = paged_count(p, gridDim.x, paged_tiles(longest), total);
+        const int b_mine = max(0, b_last - b_first), b_before = min(b_first, p.B);
+        if (cnt.pad > 0) {           // all sequences count the same
+            const int units = paged_units(p, longest, cnt);
             total = units * p.B;
-            mine = max(0, b_last - b_first) * units;
-            before = min(b_first, p.B) * units;
+            mine = b_mine * units;
+            before = b_before * units;
+        } else if (cnt.cost > 0) {
+            const int more = cnt.cost * p.Hkv * p.row_blocks;
+            total += more * p.B;
+            mine += more * b_mine;
+            before += more * b_before;
         }
-        const int share = paged_share(total, gridDim.x, p.least_units, pad);
+        const int share = paged_share(p, total, gridDim.x, cnt);
         const int u0 = min(total, static_cast<int>(blockIdx.x) * share), u1 = min(total, u0 + share);
         if (before <= u0 && u0 < before + mine) {
             int b = b_first, base = before;
             for (;; ++b) {
-                const int n = paged_units(p, paged_len(p, b, nullptr), pad);
+                const int n = paged_units(p, paged_len(p, b, nullptr), cnt);
                 if (u0 < base + n) break;
                 base += n;
             }
@@ -820,13 +845,13 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             seq = sh.start_b;
             base = sh.start_base;
             len = paged_len(p, seq, lane == 0 ? p.status : nullptr);
-            hr = (u0 - base) / paged_block_units(len, pad);
+            hr = (u0 - base) / paged_block_units(len, cnt);
         }
         auto publish = [&](int k) {
             while (!ended && published < k + kPartRing) {
                 const int nt = paged_tiles(len);
                 PagedEntry e;
-                const bool some = hr + lane < blocks && paged_entry(p, blockIdx.x, share, u0, u1, seq, base, len, pad, hr + lane, e);
+                const bool some = hr + lane < blocks && paged_entry(p, blockIdx.x, share, u0, u1, seq, base, len, cnt, hr + lane, e);
                 const uint32_t have = __ballot_sync(0xffffffffu, some);
                 const int count = min(__popc(have), k + kPartRing - published);
                 // tiles of the parts before this lane's: the first part of a share may lack some, the others here have them all
@@ -845,7 +870,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                     if (hr < blocks) {
                         ended = true;                  // the share ends inside this sequence
                     } else {
-                        base += blocks * paged_block_units(len, pad);
+                        base += blocks * paged_block_units(len, cnt);
                         hr = 0;
                         if (base < u1) {
                             ++seq;

@@ -37,6 +37,7 @@ struct PagedParams {
     int row_blocks;               // blocks of query rows that a (sequence, K/V head) is cut into
     int box_rows;                 // rows of a page box: the largest power of two that divides the page size, at most 128
     int least_units;              // tiles that a CTA takes at least
+    int part_cost, long_tiles;    // units that a row block takes in the list beside its tiles, where they are fewer than long_tiles on average
     float* part;                  // partial results: two slots per CTA
     unsigned int* arrivals;       // pieces finished, per (sequence, K/V head, row block) with more than one; zero between launches
     uint32_t* status;

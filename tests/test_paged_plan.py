@@ -19,10 +19,14 @@ def check(num_sms, lens, Hq, Hkv, Sq, dqk, dv, e4m3=False, diff=False, page=16, 
     most = (max_pages or max(1, -(-max(lens) // page))) * page
     tiles = [max(1, -(-max(0, min(n, most)) // 128)) for n in lens]
     blocks = len(lens) * Hkv * info["row_blocks"]
-    pad = max(tiles) if info["units"] == blocks * (max(tiles) + info["part_cost"]) else 0
-    assert info["units"] == sum(max(n, pad) + info["part_cost"] for n in tiles) * Hkv * info["row_blocks"]
-    if pad and blocks <= info["ctas"] and max(tiles) <= 6:
+    unsplit = max(tiles) <= 6 and blocks <= info["ctas"]
+    aligned = unsplit or (len(lens) == 1 and 2 * blocks <= info["ctas"])        # a block's tiles count as a multiple of the share
+    share = info["units_per_cta"] if aligned else 1
+    assert info["units"] == sum(-(-n // share) * share + info["part_cost"] for n in tiles) * Hkv * info["row_blocks"]
+    if unsplit:
         assert all(x["slot"] < 0 for x in pieces)               # a CTA for every row block, nothing split
+    if aligned:
+        assert info["part_cost"] == 0 and len({x["cta"] for x in pieces}) == len(pieces)      # a CTA has one part
     assert info["units_per_cta"] * info["ctas"] >= info["units"]
     states = info["rows_per_block"] * (2 if diff else 1)
     slots = (scratch or 32 << 20) // (states * (dv + 2) * 4)
