@@ -107,7 +107,9 @@ int rows_per_block(int rows, int dqk, bool e4m3, bool diff) {
     return rows > 32 && !e4m3 && dqk != 192 ? 64 : 32;
 }
 
-// Tiles of 128 keys that a call's list of work can have at most; the kernel counts them in 32 bits.
+// Units that a call's list of work can have at most; the kernel counts them in 32 bits, and the blocks of a single sequence, rounded
+// up to a share, can count twice their tiles.
+constexpr long long kMostUnits = 1ll << 30;
 long long most_units(const fa::PagedParams& p) {
     return static_cast<long long>(p.B) * p.Hkv * p.row_blocks *
            (fa::paged_tiles(static_cast<int>(static_cast<long long>(p.max_pages) * p.page_size)) + fa::kMostPartCost);
@@ -205,7 +207,7 @@ fa_status forward_paged(fa_handle* h, const fa_paged_cache* cache, const fa_page
     set_list(p, cache->dqk, cache->dv, e4m3);
     const int rows = Hq / cache->Hkv * Sq, block = rows_per_block(rows, cache->dqk, e4m3, diff != nullptr);
     p.row_blocks = (rows + block - 1) / block;
-    if (most_units(p) > 0x7fff0000LL) return FA_ERR_UNSUPPORTED;
+    if (most_units(p) > kMostUnits) return FA_ERR_UNSUPPORTED;
     const int eb = e4m3 ? 1 : 2;
     const CUtensorMap* m = nullptr;
     // Rows of one head that lie apart (a [pages, slots, heads, d] pool) are fetched into L2 as they are; with the default of 256 bytes
@@ -422,7 +424,7 @@ fa_status fa_plan_paged(int num_sms, const fa_config* cfg, const fa_paged_cache*
     const int rows = Hq / cache->Hkv * Sq, block = rows_per_block(rows, cache->dqk, cache->type == FA_CACHE_E4M3, diff != 0);
     p.row_blocks = (rows + block - 1) / block;
     set_list(p, cache->dqk, cache->dv, cache->type == FA_CACHE_E4M3);
-    if (most_units(p) > 0x7fff0000LL) return FA_ERR_UNSUPPORTED;
+    if (most_units(p) > kMostUnits) return FA_ERR_UNSUPPORTED;
     const int ctas = paged_ctas(num_sms, static_cast<size_t>(scratch), p, cache->dv, (diff ? 2 : 1) * block);
     if (ctas < 1) return FA_ERR_UNSUPPORTED;
     int longest = 0, total = 0;

@@ -1271,7 +1271,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                 }
                 if (key < kStates) store_lse(key % kRows, run_m, run_l);
             }
-            // (the barrier that the next round begins with comes before anything of this round's is overwritten)
+            // (the barrier at the head of the loop comes before anything that is read here is overwritten)
         }
     }
 

@@ -102,3 +102,12 @@ def test_refusals():
             b.fa_plan_paged(args.pop("num_sms"), args.pop("seq_lens"), args.pop("Hq"), args.pop("Hkv"), args.pop("Sq"), args.pop("dqk"),
                             args.pop("dv"), **args)
         assert e.value.status == want, kw
+
+
+def test_lists_that_32_bits_cannot_count_are_refused():
+    """(74 blocks of one sequence count up to twice their tiles.)"""
+    with pytest.raises(b.FaError) as e:
+        b.fa_plan_paged(148, [2 ** 31 - 256], 74, 74, 1, 64, 64, page_size=128)
+    assert e.value.status == b.FA_ERR_UNSUPPORTED
+    info, pieces = b.fa_plan_paged(148, [2 ** 31 - 256], 63, 63, 1, 64, 64, page_size=128)
+    assert 63 * (2 ** 24 - 2) <= info["units"] < 2 ** 31 and sum(x["end_tile"] - x["first_tile"] for x in pieces) == 63 * (2 ** 24 - 2)
