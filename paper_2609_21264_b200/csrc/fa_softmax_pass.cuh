@@ -43,7 +43,7 @@ FA_DEVI void softmax_pass_128(uint32_t tS, uint32_t tO, float c, float tau_raw, 
             const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[q * 32 + e]), __uint_as_float(s[q * 32 + e + 1])), c2, nmc2);
             if constexpr (kPolyEvery > 0) {
                 if ((e / 2) % kPolyEvery == kPolyEvery - 1) {
-                    const float2 y = exp2_poly2(x);
+                    const float2 y = exp2_poly2<true>(x);
                     s[q * 32 + e] = __float_as_uint(y.x);
                     s[q * 32 + e + 1] = __float_as_uint(y.y);
                     continue;

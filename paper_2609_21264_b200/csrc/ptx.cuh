@@ -47,8 +47,11 @@ FA_DEVI float exp2_approx(float x) {
 // f = x - n in [0, 1) goes through a cubic (minimax fit of 2^f, relative error 7.5e-5, far below the rounding of P
 // to bf16 or e4m3 that follows), and n is put back with a shift and an integer add into the exponent field.
 // Valid for x < 127.  x below -125 (masked scores are -inf) is clamped there and comes out as about 2^-125, which
-// rounds to zero in P and vanishes in the row sum; the clamp must stay above -126, where the integer add would
-// carry out of the exponent field and produce a NaN pattern.
+// vanishes in the row sum, and in P where that is rounded to e4m3; the clamp must stay above -126, where the integer add would
+// carry out of the exponent field and produce a NaN pattern.  In bf16 2^-125 is a number, and times a value near the largest one
+// no small one: with kZero the polynomial's own value times 2^-125 is taken off again (a clamped x has f = 0, its
+// result is exactly that; for others it is below the rounding), and masked scores come out as zero.
+template <bool kZero = false>
 FA_DEVI float2 exp2_poly2(float2 x) {
     const float kMagic = 12582912.f;
     x.x = fmaxf(x.x, -125.f);
@@ -67,6 +70,7 @@ FA_DEVI float2 exp2_poly2(float2 x) {
     float2 r;
     r.x = __uint_as_float(__float_as_uint(p.x) + (__float_as_uint(y.x) << 23));
     r.y = __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(y.y) << 23));
+    if constexpr (kZero) r = __ffma2_rn(p, make_float2(-0x1p-125f, -0x1p-125f), r);
     return r;
 }
 
