@@ -42,6 +42,13 @@ FA_DEVI float exp2_approx(float x) {
     return y;
 }
 
+// max that a NaN goes through
+FA_DEVI float fmax_nan(float a, float b) {
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+
 // exp2 of two values on the FMA pipe instead of the MUFU: the integer part n = floor(x) is taken with the
 // 1.5 * 2^23 trick (an addition rounded towards minus infinity leaves n in the low mantissa bits), the fraction
 // f = x - n in [0, 1) goes through a cubic (minimax fit of 2^f, relative error 7.5e-5, far below the rounding of P
@@ -50,12 +57,13 @@ FA_DEVI float exp2_approx(float x) {
 // vanishes in the row sum, and in P where that is rounded to e4m3; the clamp must stay above -126, where the integer add would
 // carry out of the exponent field and produce a NaN pattern.  In bf16 2^-125 is a number, and times a value near the largest one
 // no small one: with kZero the polynomial's own value times 2^-125 is taken off again (a clamped x has f = 0, its
-// result is exactly that; for others it is below the rounding), and masked scores come out as zero.
+// result is exactly that; for others it is below the rounding), and masked scores come out as zero.  A NaN (a score that is none, or
+// +inf under a reference of +inf) goes through the clamp and, by that product, through the exponent's bits.
 template <bool kZero = false>
 FA_DEVI float2 exp2_poly2(float2 x) {
     const float kMagic = 12582912.f;
-    x.x = fmaxf(x.x, -125.f);
-    x.y = fmaxf(x.y, -125.f);
+    x.x = kZero ? fmax_nan(x.x, -125.f) : fmaxf(x.x, -125.f);
+    x.y = kZero ? fmax_nan(x.y, -125.f) : fmaxf(x.y, -125.f);
     unsigned long long xb, yb, mb;
     asm("mov.b64 %0, {%1, %2};" : "=l"(xb) : "f"(x.x), "f"(x.y));
     asm("mov.b64 %0, {%1, %1};" : "=l"(mb) : "f"(kMagic));
