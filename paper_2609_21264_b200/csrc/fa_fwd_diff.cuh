@@ -205,8 +205,9 @@ fa_fwd_diff_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 if (j == 0) release_buffer();
             }
             release_buffer();
-            // (a row that saw no key: the polynomial made 2^-125 of its masked scores, not zero)
-            sh.inv_l[t][row] = l != l || (m_ref != -INFINITY && l > 0.f) ? (1.f / l) : 0.f;
+            // (a row that saw no key has a sum of exactly zero; the reference says nothing: at scales below 2.4e-38 tau_raw is infinite
+            // and no reference is ever taken, all weights are 1; a NaN goes through)
+            sh.inv_l[t][row] = l > 0.f || l != l ? (1.f / l) : 0.f;
             if (x.nkv > 0) {
                 ok = ok && mbar_wait(smem_addr(&sh.o_final[0]), n_final & 1, wctx, kSiteEpiOFull) &&
                      mbar_wait(smem_addr(&sh.o_final[1]), n_final & 1, wctx, kSiteEpiOFull);

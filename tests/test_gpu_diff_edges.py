@@ -1,12 +1,12 @@
 """Differential attention over prompts at the edges of its types: masked values of the largest size, keys that
-are no numbers, scores past the largest one."""
+are no numbers, scores past the largest one, the smallest scales."""
 
 import math
 
 import pytest
 import torch
 
-from paged_util import assert_close, diff_norm, ok
+from paged_util import assert_close, diff_norm, diff_rows, ok
 
 pytestmark = pytest.mark.gpu
 
@@ -97,3 +97,17 @@ def test_a_score_past_the_largest_number_shows(handle, half):
             Y += sign * p @ v[0, h, :199].double()
             A += abs(sign) * p @ v[0, h, :199].double().abs()
         assert_close(o[0, h, 198:199], *diff_norm(Y.cpu(), A.cpu(), None, 1e-5, 1.0), "key %d" % j)
+
+
+@pytest.mark.parametrize("scale", [1e-38, 2e-38, 1e-40, 1e-30])
+@pytest.mark.parametrize("causal", [False, True], ids=["full", "causal"])
+def test_the_smallest_scales_weigh_all_keys_alike(handle, scale, causal):
+    from paper_2609_21264_b200 import binding as b
+    q, k, v = inputs(2, 200, 24)
+    lam = torch.tensor([0.3, -0.2], device="cuda")
+    o = b.forward_diff(handle, q, k, v, lam, causal=causal, scale=scale)
+    ok(handle)
+    last = torch.arange(200) if causal else torch.full((200,), 200)
+    for h in range(2):
+        Y, A = diff_rows(q[0, h].cpu().double(), k[0, h].cpu().double(), v[0, h].cpu().double(), lam[h].item(), scale, last)
+        assert_close(o[0, h], *diff_norm(Y, A, None, 1e-5, 1.0), "h%d" % h)
