@@ -940,8 +940,9 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                     for (int i = 0; i < 4; ++i) top = max(top, max((w4[i] & 0x7fffu) << 16, w4[i] & 0x7fff0000u));
 #pragma unroll
                     for (int d = kLanes / 2; d > 0; d >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+                    // (from 2^127 down to 2^-112; a smaller row is scaled by 2^126, which makes its entries, multiples of 2^-133, exact too)
                     int sft = top ? 14 - (static_cast<int>(top >> 23) - 127) : 0;
-                    sft = sft > 100 ? 100 : (sft < -100 ? -100 : sft);
+                    sft = sft > 126 ? 126 : (sft < -113 ? -113 : sft);
                     const float mult = __uint_as_float(static_cast<uint32_t>(sft + 127) << 23);
                     c *= __uint_as_float(static_cast<uint32_t>(127 - sft) << 23);
                     uint32_t t8[3][2];
