@@ -326,12 +326,16 @@ fa_status fa_forward_host(fa_handle* h,
                           int causal, float scale, void* stream);
 
 /*
- * Device-side status of the kernels launched through `h` so far: FA_OK, or
- * FA_ERR_DEVICE_TIMEOUT if any bounded wait (mbarrier, TMEM allocation) ran
- * out since the handle was created or the status was last read (reading
- * clears it), or FA_ERR_INVALID_ARG if a paged call found a length, page or position that it may not use.  Synchronises nothing: meaningful after the caller has
- * synchronised the stream(s) it launched on.  `detail`, if not NULL, receives
- * a diagnostic word (role and barrier that gave up; 0 when FA_OK).
+ * Device-side status of the kernels launched through `h` since it was created or the status was last read (reading
+ * clears it):
+ *   FA_OK
+ *   FA_ERR_DEVICE_TIMEOUT if any bounded wait (mbarrier, TMEM allocation) ran out, FA_ERR_CUDA if a kernel could not run.  The results
+ *     of every launch since are invalid, of those that followed it too: it leaves the handle's counters half-way, and this
+ *     call puts them back.
+ *   FA_ERR_INVALID_ARG if a paged call found a length, page or position that it may not use (and none of the above happened): the
+ *     results of the sequences concerned are unspecified, all others hold.
+ * Waits for no launch: meaningful after the caller has synchronised the stream(s) it launched on.  `detail`, if not
+ * NULL, receives a diagnostic word (role and barrier that gave up, or the kind of bad contents; 0 when FA_OK).
  */
 fa_status fa_last_status(fa_handle* h, uint32_t* detail);
 

@@ -776,22 +776,21 @@ fa_status fa_destroy(fa_handle* h) {
 fa_status fa_last_status(fa_handle* h, uint32_t* detail) {
     if (!h) return FA_ERR_INVALID_ARG;
     volatile uint32_t* sw = h->status_host;
-    const uint32_t code = sw[0];
-    const uint32_t who = sw[1];
-    if (detail) *detail = code ? who : 0u;
-    if (code) {
-        sw[0] = 0;
-        sw[1] = 0;
-        // A persistent launch that gave up has not made all of its draws from the ticket counter, which the last
-        // draw of a complete launch puts back to zero: zero it here, or the next persistent launch would start in the
-        // middle of its item list.  (The caller synchronised before asking, so no launch is using the counter.)
-        if (h->sched_counter) {
-            DeviceGuard guard(h->device);
-            if (guard.ok()) cudaMemset(h->sched_counter, 0, 256 + static_cast<size_t>(h->num_sms) * sizeof(unsigned int));
-        }
+    const uint32_t code = sw[0], who = sw[1], bad = sw[2];
+    if (detail) *detail = code ? who : bad;
+    if (bad) sw[2] = 0;
+    if (!code) return bad ? FA_ERR_INVALID_ARG : FA_OK;
+    sw[0] = 0;
+    sw[1] = 0;
+    // A persistent launch that gave up has not made all of its draws from the ticket counter, which the last
+    // draw of a complete launch puts back to zero, and a paged one not all of its joins: zero the counters here, or the next
+    // launch would start in the middle of its item list.  (The caller synchronised before asking, so no launch is
+    // using them.)
+    if (h->sched_counter) {
+        DeviceGuard guard(h->device);
+        if (guard.ok()) cudaMemset(h->sched_counter, 0, 256 + static_cast<size_t>(h->num_sms) * sizeof(unsigned int));
     }
-    if (code == FA_OK || code == FA_ERR_DEVICE_TIMEOUT || code == FA_ERR_INVALID_ARG) return static_cast<fa_status>(code);
-    return FA_ERR_CUDA;
+    return code == FA_ERR_DEVICE_TIMEOUT ? FA_ERR_DEVICE_TIMEOUT : FA_ERR_CUDA;
 }
 
 fa_status fa_debug_set_drop_v_load(fa_handle* h, int enabled) {

@@ -34,7 +34,7 @@ struct fa_handle {
     int device = 0;
     int num_sms = 1;
     uint32_t flags = 0;
-    uint32_t* status_host = nullptr;   // pinned + mapped: [0] status, [1] wait site
+    uint32_t* status_host = nullptr;   // pinned + mapped: [0] status, [1] wait site, [2] kind of bad contents (0: none)
     uint32_t* status_dev = nullptr;
     uint32_t kv_splits_cfg = 0;              // 0 auto, 1 never, n force
     void* scratch = nullptr;                 // split-KV partials

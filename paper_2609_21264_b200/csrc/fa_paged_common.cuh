@@ -45,11 +45,12 @@ struct PagedParams {
     int debug_drop_v_load;
 };
 
+// The place is the report (one store, so that reports of several CTAs cannot mix), in a word of its own behind the code and place of a
+// launch that gave up: bad contents concern their own sequences alone and must not hide one whose results are all invalid.
 __host__ __device__ inline void report_bad_input(uint32_t* status, uint32_t site) {
     if (!status) return;
     volatile uint32_t* sw = status;       // mapped host memory: plain stores
-    sw[1] = site;
-    sw[0] = 1u;                           // FA_ERR_INVALID_ARG
+    sw[2] = site;                         // FA_ERR_INVALID_ARG
 }
 
 // Length of sequence b as the kernels use it: what the block table can hold, and never negative.

@@ -1,4 +1,4 @@
-"""Paged entry points at the edges: queries of any size over 8-bit caches."""
+"""Paged entry points at the edges: queries of any size over 8-bit caches, statuses of several kinds."""
 import pytest
 import torch
 
@@ -27,3 +27,44 @@ def test_queries_of_any_size_over_an_8_bit_cache(handle, shift, dqk, dv):
     o, lse = b.forward_paged(handle, q, b.PagedCache(k, v, ks, vs), table, lens_t)
     ok(handle)
     assert_attention(o, lse, *paged_reference(q, k, v, ks, vs, table, lens, 1, dqk ** -0.5))
+
+
+def bad_append(h):
+    """An append into a page that the pool does not have."""
+    from paper_2609_21264_b200 import binding as b
+    k, v = (torch.zeros(2, 1, 16, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    x = torch.ones(1, 1, 64, dtype=torch.bfloat16, device="cuda")
+    b.append_paged(h, x, x, b.PagedCache(k, v), torch.full((1, 1), 7, dtype=torch.int32, device="cuda"),
+                   torch.ones(1, dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("order", ["timeout first", "timeout last"])
+def test_a_wait_that_ran_out_is_not_hidden_by_bad_contents(order):
+    """A launch that gave up (its first V tiles are left out) and one that met a page outside the pool, before the status is read: the
+    status is the one that makes every result doubtful."""
+    from paper_2609_21264_b200 import binding as b
+    lens = [700, 40]
+    k, v, table, lens_t, _, _ = pool(lens, 16, 2, 128, 128, False, False, 32)
+    q = torch.randn(2, 8, 128, device="cuda").bfloat16()
+    cache = b.PagedCache(k, v)
+    h = b.fa_create(flags=b.FA_FLAG_DEBUG_DROP_V_LOAD, wait_limit_ms=20)
+    try:
+        if order == "timeout last":
+            bad_append(h)
+        b.forward_paged(h, q, cache, table, lens_t)
+        torch.cuda.synchronize()
+        if order == "timeout first":
+            bad_append(h)
+        st, site = b.fa_last_status(h)
+        assert st == b.FA_ERR_DEVICE_TIMEOUT and site != 0 and site >> 8 != 9
+        assert b.fa_last_status(h) == (b.FA_OK, 0)       # one reading clears both
+        bad_append(h)
+        assert b.fa_last_status(h) == (b.FA_ERR_INVALID_ARG, 0x0902)
+        assert b.fa_last_status(h) == (b.FA_OK, 0)
+        assert b.fa_debug_set_drop_v_load(h, False) == b.FA_OK
+        o, lse = b.forward_paged(h, q, cache, table, lens_t)
+        ok(h)
+        assert_attention(o, lse, *paged_reference(q, k, v, None, None, table, lens, 1, 128 ** -0.5))
+    finally:
+        b.fa_destroy(h)
