@@ -741,7 +741,8 @@ fa_status fa_create(fa_handle** out, const fa_config* cfg) {
     h->scratch_bytes = scratch_bytes;
     const size_t counter_bytes = 256 + static_cast<size_t>(num_sms) * sizeof(unsigned int);
     if (cudaMalloc(reinterpret_cast<void**>(&h->sched_counter), counter_bytes) != cudaSuccess ||
-        cudaMemset(h->sched_counter, 0, counter_bytes) != cudaSuccess) {
+        cudaMemset(h->sched_counter, 0, counter_bytes) != cudaSuccess ||
+        cudaStreamSynchronize(cudaStreamLegacy) != cudaSuccess) {       // (the first launch may be on a stream that waits for no other)
         cudaGetLastError();
         if (h->sched_counter) cudaFree(h->sched_counter);
         cudaFree(h->scratch);
@@ -785,10 +786,14 @@ fa_status fa_last_status(fa_handle* h, uint32_t* detail) {
     // A persistent launch that gave up has not made all of its draws from the ticket counter, which the last
     // draw of a complete launch puts back to zero, and a paged one not all of its joins: zero the counters here, or the next
     // launch would start in the middle of its item list.  (The caller synchronised before asking, so no launch is
-    // using them.)
+    // using them.)  The memset may still be under way when it returns, and streams made without the default stream's
+    // ordering would not wait for it: it is waited for here.
     if (h->sched_counter) {
         DeviceGuard guard(h->device);
-        if (guard.ok()) cudaMemset(h->sched_counter, 0, 256 + static_cast<size_t>(h->num_sms) * sizeof(unsigned int));
+        if (guard.ok()) {
+            cudaMemset(h->sched_counter, 0, 256 + static_cast<size_t>(h->num_sms) * sizeof(unsigned int));
+            cudaStreamSynchronize(cudaStreamLegacy);
+        }
     }
     return code == FA_ERR_DEVICE_TIMEOUT ? FA_ERR_DEVICE_TIMEOUT : FA_ERR_CUDA;
 }

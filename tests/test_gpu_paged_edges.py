@@ -68,3 +68,48 @@ def test_a_wait_that_ran_out_is_not_hidden_by_bad_contents(order):
         assert_attention(o, lse, *paged_reference(q, k, v, None, None, table, lens, 1, 128 ** -0.5))
     finally:
         b.fa_destroy(h)
+
+
+def test_counters_are_back_before_the_next_launch_on_any_stream():
+    """fa_last_status puts the counters back that a launch which gave up left half-way; the next launch, on a stream that does not wait for the
+    default one, finds them so."""
+    from paper_2609_21264_b200 import binding as b
+    lens = [700, 3000, 40]
+    k, v, table, lens_t, _, _ = pool(lens, 16, 2, 128, 128, False, False, 36)
+    q = torch.randn(3, 8, 128, device="cuda").bfloat16()
+    cache, side = b.PagedCache(k, v), torch.cuda.Stream()
+    h = b.fa_create(wait_limit_ms=20)
+    try:
+        want = b.forward_paged(h, q, cache, table, lens_t)
+        ok(h)
+        for _ in range(3):
+            assert b.fa_debug_set_drop_v_load(h, True) == b.FA_OK
+            with torch.cuda.stream(side):
+                b.forward_paged(h, q, cache, table, lens_t)
+            torch.cuda.synchronize()
+            assert b.fa_debug_set_drop_v_load(h, False) == b.FA_OK
+            assert b.fa_last_status(h)[0] == b.FA_ERR_DEVICE_TIMEOUT
+            with torch.cuda.stream(side):
+                o, lse = b.forward_paged(h, q, cache, table, lens_t)
+            ok(h)
+            assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
+    finally:
+        b.fa_destroy(h)
+
+
+def test_counters_of_a_new_handle_are_there_for_its_first_launch_on_any_stream():
+    from paper_2609_21264_b200 import binding as b
+    lens = [700, 3000, 40]
+    k, v, table, lens_t, _, _ = pool(lens, 16, 2, 128, 128, False, False, 37)
+    q = torch.randn(3, 8, 128, device="cuda").bfloat16()
+    cache, side, want = b.PagedCache(k, v), torch.cuda.Stream(), None
+    torch.cuda.synchronize()
+    for _ in range(10):
+        h = b.fa_create()
+        with torch.cuda.stream(side):
+            o, _ = b.forward_paged(h, q, cache, table, lens_t)
+        ok(h)
+        want = o if want is None else want
+        assert torch.equal(o, want)
+        b.fa_destroy(h)
+    assert_attention(want, None, *paged_reference(q, k, v, None, None, table, lens, 1, 128 ** -0.5))
