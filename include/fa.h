@@ -441,6 +441,7 @@ typedef struct fa_paged_cache {
  * page number outside the pool and a position past the rotation table make fa_last_status return FA_ERR_INVALID_ARG; nothing
  * out of range is read or written, and the outputs of the sequences concerned are unspecified.  (fa_append_paged looks only
  * at the sequences that have new tokens.)  max_pages * page_size is at most 2^31 - 256.
+ * An empty batch (B = 0) is FA_OK without a launch; its pointers may be NULL and its max_pages 0.
  */
 typedef struct fa_paged_seqs {
     uint32_t struct_size;         /* sizeof(fa_paged_seqs) */

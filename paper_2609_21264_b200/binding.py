@@ -549,7 +549,7 @@ def _rows(t, cache, d, what):
     if width != d or sd != 1:
         raise ValueError("the last dimension of %s must be %d contiguous values" % (what, d))
     # (the stride of a dimension of one row is whatever the view left; the library wants it to be valid)
-    if n == 1:
+    if n <= 1:
         st = max(d, (st + 7) // 8 * 8)
     if heads == 1:
         sh = max(d, (sh + 7) // 8 * 8)
@@ -614,7 +614,8 @@ def _paged_out(q, cache, seqs, out):
     """(Hq, tokens, Sq, stride array, out) of a paged attention call."""
     import torch
     T, Hq, qt, qh = _rows(q, cache, cache.dqk, "q")
-    if seqs.B == 0 or T == 0 or T % seqs.B:
+    B = seqs.B
+    if T != 0 if B == 0 else T == 0 or T % B:
         raise ValueError("q must hold the same number of tokens for every sequence")
     if out is None:
         out = _new(q, T, Hq, cache.dv)
@@ -623,12 +624,12 @@ def _paged_out(q, cache, seqs, out):
         To, Ho, ot, oh = _rows(out, cache, cache.dv, "out")
         if To != T or Ho != Hq:
             raise ValueError("out must have shape %s" % ((T, Hq, cache.dv),))
-    return Hq, T, T // seqs.B, _I64x4(qt, qh, ot, oh), out
+    return Hq, T, T // B if B else 1, _I64x4(qt, qh, ot, oh), out
 
 
 def forward_paged(h, q, cache: PagedCache, block_table, seq_lens, *, scale: float = 0.0, out=None, want_lse=True):
     """Attention of the last tokens of every sequence over a paged cache: q [B*Sq, Hq, dqk] bf16; returns (O [B*Sq, Hq, dv],
-    lse [Hq, B*Sq] fp32 or None)."""
+    lse [Hq, B*Sq] fp32 or None).  A batch of no sequences launches nothing."""
     import torch
     seqs = _seqs(h, cache, block_table, seq_lens)
     Hq, T, Sq, strides, out = _paged_out(q, cache, seqs, out)

@@ -47,8 +47,8 @@ fa_status check_cache(const fa_paged_cache* c) {
 
 fa_status check_seqs(const fa_paged_seqs* s, const fa_paged_cache* c) {
     if (!s || s->struct_size != sizeof(fa_paged_seqs) || s->reserved != 0) return FA_ERR_INVALID_ARG;
-    if (s->B < 0 || s->max_pages <= 0 || s->table_stride < s->max_pages) return FA_ERR_INVALID_ARG;
-    if (s->B > 0 && (!s->block_table || !s->seq_lens)) return FA_ERR_INVALID_ARG;
+    if (s->B < 0 || s->max_pages < 0 || s->table_stride < s->max_pages) return FA_ERR_INVALID_ARG;
+    if (s->B > 0 && (s->max_pages == 0 || !s->block_table || !s->seq_lens)) return FA_ERR_INVALID_ARG;
     if (misaligned(s->block_table, 4) || misaligned(s->seq_lens, 4)) return FA_ERR_INVALID_ARG;
     // positions are 32-bit
     if (static_cast<int64_t>(s->max_pages) * c->page_size > 0x7fffff00LL) return FA_ERR_UNSUPPORTED;

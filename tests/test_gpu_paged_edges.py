@@ -1,4 +1,5 @@
-"""Paged entry points at the edges: queries of any size over 8-bit caches, statuses of several kinds."""
+"""Paged entry points at the edges: queries of any size over 8-bit caches, statuses of several kinds, empty
+batches."""
 import pytest
 import torch
 
@@ -113,3 +114,26 @@ def test_counters_of_a_new_handle_are_there_for_its_first_launch_on_any_stream()
         assert torch.equal(o, want)
         b.fa_destroy(h)
     assert_attention(want, None, *paged_reference(q, k, v, None, None, table, lens, 1, 128 ** -0.5))
+
+
+@pytest.mark.parametrize("max_pages", [0, 3])
+def test_an_empty_batch_through_the_binding(handle, max_pages):
+    """A server that has drained its batch goes on making the same calls."""
+    from paper_2609_21264_b200 import binding as b
+    k, v, _, _, _, _ = pool([20], 16, 2, 128, 128, False, False, 33)
+    cache, before = b.PagedCache(k, v), b.fa_launch_count(handle)
+    none = dict(dtype=torch.int32, device="cuda")
+    table, lens, cu = torch.empty(0, max_pages, **none), torch.empty(0, **none), torch.zeros(1, **none)
+    rows = lambda H: torch.empty(0, H, 128, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    for offsets in (None, cu):
+        out = b.append_paged(handle, rows(2), rows(2), cache, table, lens, cu_seqlens=offsets, q=rows(8))
+        assert out.shape == (0, 8, 128)
+    o, lse = b.forward_paged(handle, rows(8), cache, table, lens)
+    assert o.shape == (0, 8, 128) and o.dtype == torch.bfloat16 and lse.shape == (8, 0)
+    given = rows(8)
+    assert b.forward_paged(handle, rows(8), cache, table, lens, out=given, want_lse=False) == (given, None)
+    assert b.forward_paged_diff(handle, rows(8), cache, table, lens, torch.ones(8, device="cuda")).shape == (0, 8, 128)
+    ok(handle)
+    assert b.fa_launch_count(handle) == before
+    with pytest.raises(ValueError):
+        b.forward_paged(handle, torch.zeros(2, 8, 128, dtype=torch.bfloat16, device="cuda"), cache, table, lens)
