@@ -496,8 +496,8 @@ fa_status fa_append_paged(fa_handle* h, const fa_paged_cache* cache, const fa_pa
  * tokens) gets O = 0 and lse = -inf.  Slots past a sequence's length take no part, whatever they hold; the values (V) of the
  * last Sq tokens must be finite where Sq > 1 (a token that does not see a key multiplies its value by a probability of zero).
  * Scores, softmax state and both accumulators are fp32; the probabilities enter the second product as bf16, and over an e4m3 cache as
- * the sum of three 8-bit terms (at least 9 significant bits), the queries as such a sum too (exact for entries of 2^-24 of
- * their row's largest and more, to 2^-31 of it below).  scale as for fa_forward.
+ * the sum of three 8-bit terms (at least 9 significant bits), the queries as such a sum too (exact for entries of 2^-23 of
+ * their row's largest and more, to 2^-30 of it below).  scale as for fa_forward.
  * One launch: the K/V tiles of all sequences are dealt out evenly over the SMs on the device and the pieces of a
  * sequence are joined by the SM that finishes last, in a fixed order, so equal calls give equal bits.  The partial results use the
  * handle's scratch buffer, under the rule of fa_forward: launches through one handle must not overlap on the device.  With less

@@ -933,7 +933,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                         st_shared_v4(sQb + (piece >> 3) * Cfg::kQChunkBytes + r * 128 + (((piece & 7) ^ (r & 7)) << 4), xs[j].x, xs[j].y, xs[j].z, xs[j].w);
                 } else {
                     // scaled by a power of two so that the row's largest entry is in [2^14, 2^15), then three e5m2 terms: exact for
-                    // entries of 2^-24 of the largest and more, below that to 2^-31 of it
+                    // entries of 2^-23 of the largest and more, below that to 2^-30 of it
                     const uint32_t w4[4] = {xs[j].x, xs[j].y, xs[j].z, xs[j].w};
                     uint32_t top = 0;
 #pragma unroll
