@@ -501,8 +501,10 @@ fa_status fa_append_paged(fa_handle* h, const fa_paged_cache* cache, const fa_pa
  * One launch: the K/V tiles of all sequences are dealt out evenly over the SMs on the device and the pieces of a
  * sequence are joined by the SM that finishes last, in a fixed order, so equal calls give equal bits.  The partial results use the
  * handle's scratch buffer, under the rule of fa_forward: launches through one handle must not overlap on the device.  With less
- * scratch than two partials per SM fewer SMs are used; with less than two, and for batches of more than 2^30 tiles of 128
- * keys (counted by max_pages), FA_ERR_UNSUPPORTED.  fa_config.kv_splits does not apply; FA_FLAG_SERIAL_KERNEL selects a
+ * scratch than two partials per SM fewer SMs are used; with less than two, FA_ERR_UNSUPPORTED.  The list of work is counted in 32
+ * bits: B * Hkv * (blocks of query rows of a K/V head) * (tiles of 128 keys in max_pages pages + 3) is at most 2^30, else
+ * FA_ERR_UNSUPPORTED (the (Hq / Hkv) * Sq rows of a K/V head are one block up to 16, blocks of 32 or 64 above that, fa_plan_paged says
+ * which; of 16 in the differential call).  Every block makes a pass over the keys of its own.  fa_config.kv_splits does not apply; FA_FLAG_SERIAL_KERNEL selects a
  * plain kernel of one CTA per query row (a cross-check), here and in the differential calls.
  */
 #define FA_PAGED_MAX_SQ 16
