@@ -1,9 +1,9 @@
 """Paged entry points at the edges: queries of any size over 8-bit caches, statuses of several kinds, empty
-batches."""
+batches, precision of the difference of two maps."""
 import pytest
 import torch
 
-from paged_util import assert_attention, ok, paged_reference, pool
+from paged_util import assert_attention, assert_close, ok, paged_reference, pool
 
 pytestmark = pytest.mark.gpu
 
@@ -137,3 +137,42 @@ def test_an_empty_batch_through_the_binding(handle, max_pages):
     assert b.fa_launch_count(handle) == before
     with pytest.raises(ValueError):
         b.forward_paged(handle, torch.zeros(2, 8, 128, dtype=torch.bfloat16, device="cuda"), cache, table, lens)
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("lens", [[333, 64], [5000, 90]], ids=["whole", "split"])
+def test_differential_probabilities_keep_their_bits_where_the_maps_are_nearly_equal(handle, e4m3, lens):
+    """Maps that differ little, lambda close to 1: what is left of the difference is as small as one bf16 rounding of the
+    probabilities.  Over a bf16 cache they keep two bf16 terms (2^-16 of the value), over an 8-bit one three e5m2 terms behind a rounding to
+    fp16 (2^-8 + 2^-11, and 2^-27 of the largest weight).  With A = sum_j (p1 + lambda p2) |v_j| the other errors are: a score, 64
+    products added with up to 2^-23 of their sizes' sum z each, turns into a relative error 64 * 2^-23 * z of its probability, with room for
+    the exponential, the references and the division in z + 1; n / 16 additions to the accumulator, 2^-23 each; the output's bf16."""
+    from paged_util import diff_rows, rows_of, softmax64
+    from paper_2609_21264_b200 import binding as b
+    Hq, Hkv = 8, 2
+    k, v, table, lens_t, ks, vs = pool(lens, 16, Hkv, 128, 128, e4m3, False, 34)
+    raw = k.view(torch.uint8) if e4m3 else k
+    raw[..., 64:] = raw[..., :64].clone()
+    q = torch.randn(2, Hq, 128, generator=torch.Generator().manual_seed(35))
+    q[..., 64:] = q[..., :64] * (1 + 2.0 ** -6)
+    q = q.to(torch.bfloat16).cuda()
+    lam = torch.full((Hq,), 0.998, device="cuda")
+    o = b.forward_paged_diff(handle, q, b.PagedCache(k, v, ks, vs), table, lens_t, lam, out_scale=0.5)
+    ok(handle)
+    one_term = 0.0
+    for i, n in enumerate(lens):
+        kd, vd, last = rows_of(k, ks, table, i, n), rows_of(v, vs, table, i, n), torch.tensor([n - 1])
+        for h in range(Hq):
+            x, kh, vh, lm = q[i:i + 1, h].cpu().double(), kd[h // 4], vd[h // 4], lam[h].item()
+            y, a = diff_rows(x, kh, vh, lm, 0.125, last)
+            z = max((x[:, s].abs() @ kh[:, s].abs().T).max().item() * 0.125 for s in (slice(0, 64), slice(64, 128)))
+            tol = (2.0 ** -23 * (64 * (z + 1) + n / 8 + 32) + (2.0 ** -8 + 2.0 ** -11 if e4m3 else 2.0 ** -16)) * a
+            if e4m3:
+                tol = tol + 2.0 ** -26 * vh.abs().sum(0)
+            tol = 0.5 * tol + 2.0 ** -8 * (0.5 * y).abs() + 1e-30
+            assert_close(o[i, h], 0.5 * y[0], tol[0], "sequence %d head %d" % (i, h))
+            # what one bf16 term would have given is outside of that
+            p1, p2 = (softmax64(x[:, s], kh[:, s], 0.125, last)[0] for s in (slice(0, 64), slice(64, 128)))
+            cut = lambda p: (p / p.max()).to(torch.bfloat16).double() * p.max()  # noqa: E731
+            one_term = max(one_term, (((cut(p1) - lm * cut(p2)) @ vh - y).abs() * 0.5 / tol).max().item())
+    assert e4m3 or one_term > 1.5
