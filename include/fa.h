@@ -496,7 +496,7 @@ fa_status fa_append_paged(fa_handle* h, const fa_paged_cache* cache, const fa_pa
  * tokens) gets O = 0 and lse = -inf.  Slots past a sequence's length take no part, whatever they hold; the values (V) of the
  * last Sq tokens must be finite where Sq > 1 (a token that does not see a key multiplies its value by a probability of zero).
  * Scores, softmax state and both accumulators are fp32; the probabilities enter the second product as bf16, and over an e4m3 cache as
- * the sum of three 8-bit terms (at least 9 significant bits), the queries as such a sum too (exact for entries of 2^-23 of
+ * the sum of three 8-bit terms (at least 9 significant bits for weights of 2^-19 of the row's largest and more, to 2^-27 of it below), the queries as such a sum too (exact for entries of 2^-23 of
  * their row's largest and more, to 2^-30 of it below).  scale as for fa_forward.
  * One launch: the K/V tiles of all sequences are dealt out evenly over the SMs on the device and the pieces of a
  * sequence are joined by the SM that finishes last, in a fixed order, so equal calls give equal bits.  The partial results use the
@@ -552,8 +552,10 @@ typedef struct fa_diff {
 } fa_diff;
 
 /* Differential attention over whole prompts: tensors, strides, mask and errors as for fa_forward_strided with
- * dqk = dv = 128.  A row that sees no key gets O = 0.  The probabilities are rounded to bf16 once; the inputs must be finite, masked
- * values (V) too. */
+ * dqk = dv = 128.  A row that sees no key gets O = 0.  The probabilities (fp32; a third of the exponentials are a cubic with a
+ * relative error of 7.5e-5) are rounded to bf16 once: against 64 bits the error is 2.5e-3 of the result, where its own rounding makes
+ * 1.7e-3; the paged call below keeps 16 bits.  The values (V) must be finite, masked ones too (their weight is exactly zero).  A query
+ * or key that is no number, and a score of +inf, makes the rows that see it NaN, no others. */
 fa_status fa_forward_diff(fa_handle* h, const void* Q, const void* K, const void* V, void* O,
                           int B, int Hq, int Hkv, int Sq, int Sk, int dqk, int dv, int causal, float scale,
                           const fa_diff* diff,

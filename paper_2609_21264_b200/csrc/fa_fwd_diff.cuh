@@ -7,8 +7,13 @@
 // difference and the norm in a kernel of their own), the scores would cost twice the MMAs, O would be written and read once
 // more in each map, and K and V would be read as often but for twice the heads.
 //
-// What bounds it: per K/V tile 24 MMAs of 64 cycles (1536) against 2 x 128 x 128 exponentials (2048 cycles of the special-function
-// unit): the softmax passes.
+// What bounds it: the chain softmax -> P V_j -> Q K_{j+1} -> softmax of each map, which has one S with P over it.  A K/V tile takes some
+// 3400 cycles (4096 tokens causal, 114 tiles an SM), of which 24 MMAs of 64 cycles are 1536 (tensor pipe 46 % busy) and two thirds of
+// 2 x 128 x 128 exponentials 1365 (special-function unit 45 %); 52 % of the issue slots are used, two warps a scheduler.
+//
+// P is rounded to bf16 once (error 2.5e-3 of the result; the output's own rounding makes 1.65e-3).  The second half of S has room for a
+// second term, and that makes the error 1.65e-3, but its 16 MMAs a tile and its arithmetic lie on the chain: 327 us, against 237
+// (4096 tokens causal, 32/8 heads, back to back), 26.1 against 20 (2 x 8 heads, 1001 tokens).
 //
 // Epilogue: both groups of softmax warps read BOTH accumulators (a warp reaches the same 32 TMEM lanes of every column), each for one
 // half of the 128 columns; row sums, lambda and the halves' sums of squares cross through shared memory, and each group
@@ -39,7 +44,8 @@ struct DiffParams {
 
 // Every third pair of exponentials is computed on the FMA pipe (exp2_poly2): with half of the score MMAs gone the special-function
 // unit is what the two passes of a round wait for.  4096 tokens causal, 32/8 heads: 207.6 us, against 218.4 without, 211.1
-// with every fourth and 218.7 with every second; 16 x 300 tokens 80.7 us, against 90.
+// with every fourth and 218.7 with every second; 16 x 300 tokens 80.7 us, against 90.  (That masked scores come out as exact
+// zeros costs 1 % of it: 211.9 us, against 209.5 in the same run.)
 constexpr int kDiffPolyEvery = 3;
 
 struct DiffCfg {

@@ -1,7 +1,8 @@
 // Attention of the last few tokens of every sequence over a paged key/value cache, for sm_100a.
 //
-// Per (sequence, K/V head) there are R = (Hq / Hkv) * Sq query rows, one to a few dozen, against thousands of keys: every byte
-// of K and V is read once and used for R rows, 2 R (dqk + dv) / ((dqk + dv) * bytes) = R .. 2R flops a byte, far below the 250 that
+// Per (sequence, K/V head) there are R = (Hq / Hkv) * Sq query rows, one to a few dozen, against thousands of keys: a byte
+// of K and V is read once for a block of rows (up to 16, 32 or 64 of them; more rows are more blocks, each with a pass over the keys of
+// its own, next to one another in the list) and used for its R rows, 2 R (dqk + dv) / ((dqk + dv) * bytes) = R .. 2R flops a byte, far below the 250 that
 // the tensor cores need to be the bound.  The kernel is built to stream HBM:
 //
 //   * The products are turned around, keys on the 128 lanes of the accumulator and query rows on its columns:
@@ -26,7 +27,8 @@
 // 2^-19 of the largest still have 9 bits.
 //
 // Differential attention: two maps are two groups of columns.  Map a's scores are the k-steps of its half of K, its
-// probabilities meet the same V tile, and the epilogue subtracts and normalises: K and V are read once for both.
+// probabilities meet the same V tile, and the epilogue subtracts and normalises: K and V are read once for both maps of a block, of
+// 16 rows here (group * Sq = 64 rows read the cache four times).
 //
 // Roles (512 threads): warps 0 / 2 TMA loads of K / V (a lane per page box), warps 1 / 3 issue of the score / value products (one thread
 // each: a tile costs an issuing thread 600 cycles of waits, descriptors and commits, as much as a tile of head size 64 has in
@@ -229,7 +231,8 @@ struct PagedCfg {
     static constexpr int kMaps = kDiff ? 2 : 1;
     static constexpr int kTerms = kE4m3 ? 3 : 1;                // of the queries
     // of the probabilities: the difference of two maps loses what they have in common, so these keep 16 bits over a bf16 cache too
-    // (one bf16 term: 1.5 times the error of the rounded output alone; two: none that shows, at the same speed)
+    // (one bf16 term: 1.5 times the error of the rounded output alone; two: none that shows, at the same speed).  One map over a bf16
+    // cache keeps one term, as the other kernels on 16-bit inputs do: 2.2e-3 of the result, where its rounding alone makes 1.7e-3.
     static constexpr int kPTerms = kE4m3 ? 3 : (kDiff ? 2 : 1);
     static constexpr int kStates = kMaps * kRows;               // softmax states of a group
     static constexpr int kSCols = kStates * kTerms, kCols = kStates * kPTerms;      // columns of S^T and of O^T

@@ -26,7 +26,8 @@ namespace fa {
 // tS: TMEM address of this warp's lanes of the score tile (P overlays its first 64 columns); tO: of the accumulator
 // that P_t V_j goes to; c = scale * log2(e); tau_raw = kRescaleThresholdLog2 / c; keys j0 + e > kmax_row are masked;
 // first_tile: nothing has been accumulated into O yet (no rescale).  All 32 lanes of a warp call it together.
-// kPolyEvery > 0: every kPolyEvery-th pair of exponentials on the FMA pipe instead of the special-function unit.
+// kPolyEvery > 0: every kPolyEvery-th pair of exponentials on the FMA pipe instead of the special-function unit (a masked
+// score still weighs exactly nothing, and a NaN stays one).
 template <int DV, int kPolyEvery = 0, typename ArriveFirst, typename ArriveRest>
 FA_DEVI void softmax_pass_128(uint32_t tS, uint32_t tO, float c, float tau_raw, int j0, int kmax_row, bool first_tile,
                               float& m_ref, float& l, int lane, ArriveFirst&& arrive_first, ArriveRest&& arrive_rest) {
