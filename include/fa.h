@@ -489,6 +489,33 @@ fa_status fa_append_paged(fa_handle* h, const fa_paged_cache* cache, const fa_pa
                           const fa_rope* rope, void* stream);
 
 /*
+ * Positions of the new tokens where they do not follow from the slots: a tree of drafted tokens (siblings share a position), or the
+ * several positions that a token of a picture or a film has (time, row, column), each of which turns pairs of its own.
+ *   pos           DEVICE [axes, total] int32, the axes' rows `stride` elements apart (stride >= total where axes > 1)
+ *   axis_of_pair  HOST array of rope->dim / 2 axis numbers below `axes`, read during the call: pair i of every span is turned by row
+ *                 pos[axis_of_pair[i]][t] of the rotation table.  NULL = every pair by axis 0.
+ * axes is 1 to FA_MAX_AXES, and every axis' position has to be a row of the table: a token with another one is not stored, its row
+ * of Q_out stays as it was, and fa_last_status reports FA_ERR_INVALID_ARG.  Set struct_size = sizeof(fa_positions).
+ */
+#define FA_MAX_AXES 4
+typedef struct fa_positions {
+    uint32_t struct_size;
+    int32_t axes;
+    const int32_t* pos;
+    int64_t stride;
+    const uint8_t* axis_of_pair;
+} fa_positions;
+
+/* fa_append_paged with the rotation's positions given (positions NULL: fa_append_paged itself; else rope is needed).  The slots
+ * follow seq_lens as there; positions of tokens that are skipped are not looked at. */
+fa_status fa_append_paged_at(fa_handle* h, const fa_paged_cache* cache, const fa_paged_seqs* seqs,
+                             const int32_t* cu_seqlens, int total,
+                             const void* K, const void* V, const void* Q, void* Q_out, int Hq,
+                             const int64_t* k_strides, const int64_t* v_strides,
+                             const int64_t* q_strides, const int64_t* qo_strides,
+                             const fa_rope* rope, const fa_positions* positions, void* stream);
+
+/*
  * Attention of the last Sq tokens of every sequence (1 <= Sq <= FA_PAGED_MAX_SQ; one in ordinary decoding) over a paged
  * cache that holds their keys and values already.  Q [B*Sq, Hq, dqk] and O [B*Sq, Hq, dv] are bf16 DEVICE tensors,
  * 16-byte aligned, with {token, head} strides in elements, multiples of 8; lse is fp32 [Hq, B*Sq] or NULL.  Token i of
@@ -567,6 +594,75 @@ fa_status fa_forward_diff(fa_handle* h, const void* Q, const void* K, const void
 fa_status fa_forward_paged_diff(fa_handle* h, const fa_paged_cache* cache, const fa_paged_seqs* seqs,
                                 const void* Q, void* O, int Hq, int Sq, float scale, const fa_diff* diff,
                                 const int64_t* q_strides, const int64_t* o_strides, void* stream);
+
+/*
+ * Drafted tokens (speculative decoding).  A draft model grows a tree of tokens behind each sequence; one step of the large model looks at
+ * all of them, and the path that it accepts stays.  In the order of a step: fa_tree_layout makes what the drafts see and their
+ * positions out of their parents, fa_append_paged_at puts their keys and values into the cache, fa_forward_paged_tree is their
+ * attention, fa_compact_paged moves the accepted ones up.  The drafts of a sequence are its last keys, in the order of the call's
+ * rows: packed, sequence b's rows are [cu_seqlens[b], cu_seqlens[b+1]) (DEVICE array of B+1 int32, non-decreasing from 0), or with
+ * cu_seqlens NULL total / B each.  A sequence has at most max_tokens of them (<= FA_TREE_MAX_TOKENS); one whose rows do not lie in
+ * [0, total] or are more is reported by fa_last_status (FA_ERR_INVALID_ARG) and left out.  Rows behind the last sequence stay as they were.
+ */
+#define FA_TREE_MAX_TOKENS 256
+
+/*
+ * What drafted tokens see, and their positions.  parents: DEVICE int32 [total], the number of a token's parent among the drafts of its
+ * sequence, smaller than its own, or -1: the last token before the drafts (another number counts as -1 and is reported).  Writes
+ *   mask       [total, ceil(max_tokens / 32)] uint32, rows mask_stride words apart: bit j % 32 of word j / 32 is set where draft j is
+ *              the token itself or one of its ancestors; NULL: not wanted
+ *   positions  [total] int32: seq_lens[b] - n + depth, n the sequence's drafts, depth 0 behind the last token before them; NULL: not wanted
+ * seq_lens [B] counts the drafts in (only `positions` needs it).
+ */
+fa_status fa_tree_layout(fa_handle* h, const int32_t* parents, const int32_t* cu_seqlens, int total, int B,
+                         const int32_t* seq_lens, int max_tokens, uint32_t* mask, int64_t mask_stride,
+                         int32_t* positions, void* stream);
+
+/*
+ * Attention of the drafted tokens of every sequence over a paged cache that holds their keys and values already.  Token i of the n of
+ * sequence b sees the keys j < seq_lens[b] - n, and of the drafts those whose bit its row of `mask` has (bits of n and more are not
+ * looked at; mask NULL: the drafts up to itself, a causal chain of any number of tokens).  A token that sees no key gets O = 0 and
+ * lse = -inf.  Q [total, Hq, dqk], O [total, Hq, dv], lse [Hq, total] and everything else as for fa_forward_paged; the values (V) of the
+ * drafts have to be finite, their keys where no token sees them need not be.  A key that is no number makes the rows that see it NaN.
+ * Scores, softmax state and accumulators are fp32.  Over a bf16 cache the probabilities enter the second product as bf16.  Over an e4m3
+ * cache both products are fp16 ones: the codes as they are, the queries scaled by a power of two per row (exact for entries of 2^-29 of
+ * their row's largest and more), the probabilities with 11 significant bits down to 2^-21 of the row's reference.
+ * Two launches: the K/V tiles of all sequences are dealt out evenly over the SMs, and a second kernel joins the pieces of what several SMs
+ * share, in a fixed order, so equal calls give equal bits.  The partial results use scratch of the handle under the rule of fa_forward.
+ * FA_FLAG_SERIAL_KERNEL selects a plain kernel of one CTA per query row.
+ */
+typedef struct fa_tree {
+    uint32_t struct_size;         /* sizeof(fa_tree) */
+    int32_t max_tokens;           /* of a sequence, 1 .. FA_TREE_MAX_TOKENS */
+    const int32_t* cu_seqlens;
+    const uint32_t* mask;
+    int64_t mask_stride;          /* words between rows, >= ceil(max_tokens / 32) */
+} fa_tree;
+fa_status fa_forward_paged_tree(fa_handle* h, const fa_paged_cache* cache, const fa_paged_seqs* seqs, const fa_tree* tree, int total,
+                                const void* Q, void* O, float* lse, int Hq, float scale,
+                                const int64_t* q_strides, const int64_t* o_strides, void* stream);
+
+/*
+ * The accepted drafts move up: of the n drafts of sequence b those with the numbers keep[b][0] < keep[b][1] < ... (keep_counts[b] of
+ * them, at most max_keep <= FA_TREE_MAX_TOKENS; keep is a DEVICE int32 array with rows keep_stride elements apart) go to the slots of
+ * the sequence's first drafts, in `caches` (HOST array of num_caches structures that differ in k and v alone: the caches of a model's
+ * layers, one block table for all), and new_lens[b] = seq_lens[b] - n + keep_counts[b] (DEVICE [B] int32, not seq_lens itself; NULL:
+ * not wanted; not below 0).  The slots behind them hold what they held.  Drafts in front of position 0 (the padding of a batch) are left alone.
+ * The pages of the drafts must not be shared.  A sequence whose numbers do not rise, or are no drafts', and one with more than n
+ * or max_keep of them is reported, nothing of it moves and its length stays.  One launch per 128 caches.
+ */
+fa_status fa_compact_paged(fa_handle* h, const fa_paged_cache* caches, int num_caches, const fa_paged_seqs* seqs,
+                           const int32_t* cu_seqlens, int total, const int32_t* keep, int64_t keep_stride,
+                           const int32_t* keep_counts, int max_keep, int32_t* new_lens, void* stream);
+
+/*
+ * Copies pages in `caches` (as for fa_compact_paged): page dst[i] receives what page src[i] holds, K and V, for i < n (DEVICE int32
+ * arrays).  slots: DEVICE int32 [n], the number of leading slots that are copied (a forked sequence's last page is filled in part; more
+ * than page_size is page_size, less than 1 nothing), NULL = all.  Entries with a negative page are skipped (the padding of a captured call); a page behind the pool
+ * is reported and skipped.  The destinations are distinct and no sources.  One launch per 128 caches.
+ */
+fa_status fa_copy_pages(fa_handle* h, const fa_paged_cache* caches, int num_caches, const int32_t* src, const int32_t* dst,
+                        const int32_t* slots, int n, void* stream);
 
 /* CUDA device ordinal that the handle is bound to (-1 for NULL). */
 int fa_device(const fa_handle* h);

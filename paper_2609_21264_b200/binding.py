@@ -36,10 +36,12 @@ EXPORTS = ("fa_create", "fa_forward", "fa_forward_strided", "fa_forward_varlen",
            "fa_strerror", "fa_launch_count", "fa_last_kernel_name", "fa_last_kv_splits",
            "fa_forward_split_noalloc", "fa_noalloc_scratch_bytes", "fa_noalloc_last_status", "fa_debug_set_drop_v_load",
            "fa_append_paged", "fa_forward_paged", "fa_forward_paged_diff", "fa_forward_diff", "fa_device",
-           "fa_plan_paged")
+           "fa_plan_paged", "fa_append_paged_at", "fa_tree_layout", "fa_forward_paged_tree", "fa_compact_paged", "fa_copy_pages")
 FA_CACHE_BF16 = 0
 FA_CACHE_E4M3 = 1
 FA_PAGED_MAX_SQ = 16
+FA_MAX_AXES = 4
+FA_TREE_MAX_TOKENS = 256
 
 
 class FaError(RuntimeError):
@@ -72,6 +74,16 @@ class fa_rope(ctypes.Structure):
                 ("dim", ctypes.c_int32), ("offset", ctypes.c_int32), ("span", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
 
 
+class fa_positions(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("axes", ctypes.c_int32), ("pos", ctypes.c_void_p), ("stride", ctypes.c_int64),
+                ("axis_of_pair", ctypes.c_void_p)]
+
+
+class fa_tree(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("max_tokens", ctypes.c_int32), ("cu_seqlens", ctypes.c_void_p), ("mask", ctypes.c_void_p),
+                ("mask_stride", ctypes.c_int64)]
+
+
 class fa_diff(ctypes.Structure):
     _fields_ = [("struct_size", ctypes.c_uint32), ("eps", ctypes.c_float), ("lambda_", ctypes.c_void_p),
                 ("weight", ctypes.c_void_p), ("out_scale", ctypes.c_float), ("reserved", ctypes.c_float)]
@@ -93,6 +105,9 @@ _I64x4 = ctypes.c_int64 * 4
 _I64x8 = ctypes.c_int64 * 8
 _I64x12 = ctypes.c_int64 * 12
 _SEQS_SIZE = ctypes.sizeof(fa_paged_seqs)
+_POSITIONS_SIZE = ctypes.sizeof(fa_positions)
+_TREE_SIZE = ctypes.sizeof(fa_tree)
+_INT_MAX = 2 ** 31 - 1
 _lib = None
 
 
@@ -153,6 +168,16 @@ def load():
     lib.fa_debug_set_drop_v_load.argtypes = [vp, i32]
     lib.fa_append_paged.restype = i32
     lib.fa_append_paged.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp]
+    lib.fa_append_paged_at.restype = i32
+    lib.fa_append_paged_at.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp]
+    lib.fa_tree_layout.restype = i32
+    lib.fa_tree_layout.argtypes = [vp, vp, vp, i32, i32, vp, i32, vp, ctypes.c_int64, vp, vp]
+    lib.fa_forward_paged_tree.restype = i32
+    lib.fa_forward_paged_tree.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, i32, f32, vp, vp, vp]
+    lib.fa_compact_paged.restype = i32
+    lib.fa_compact_paged.argtypes = [vp, vp, i32, vp, vp, i32, vp, ctypes.c_int64, vp, i32, vp, vp]
+    lib.fa_copy_pages.restype = i32
+    lib.fa_copy_pages.argtypes = [vp, vp, i32, vp, vp, vp, i32, vp]
     lib.fa_forward_paged.restype = i32
     lib.fa_forward_paged.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, f32, vp, vp, vp]
     lib.fa_forward_paged_diff.restype = i32
@@ -433,6 +458,38 @@ def fa_append_paged(h, cache, seqs, cu_seqlens, total, K, V, Q, Q_out, Hq, k_str
     return load().fa_append_paged(h, ref(cache), ref(seqs), cu_seqlens, total, K, V, Q, Q_out, Hq, *arr, ref(rope), stream)
 
 
+def fa_append_paged_at(h, cache, seqs, cu_seqlens, total, K, V, Q, Q_out, Hq, k_strides, v_strides, q_strides, qo_strides, rope, positions,
+                       stream=0) -> int:
+    """Raw call: fa_append_paged with an fa_positions structure (or None); returns the status code."""
+    arr = [None if x is None else _I64x2(*[int(i) for i in x]) for x in (k_strides, v_strides, q_strides, qo_strides)]
+    ref = lambda x: None if x is None else ctypes.addressof(x)
+    return load().fa_append_paged_at(h, ref(cache), ref(seqs), cu_seqlens, total, K, V, Q, Q_out, Hq, *arr, ref(rope), ref(positions), stream)
+
+
+def fa_tree_layout(h, parents, cu_seqlens, total, B, seq_lens, max_tokens, mask, mask_stride, positions, stream=0) -> int:
+    """Raw call: pointers as integers; returns the status code."""
+    return load().fa_tree_layout(h, parents, cu_seqlens, total, B, seq_lens, max_tokens, mask, mask_stride, positions, stream)
+
+
+def fa_forward_paged_tree(h, cache, seqs, tree, total, Q, O, lse, Hq, scale, q_strides, o_strides, stream=0) -> int:
+    """Raw call on a paged cache (structures above, pointers as integers, (token, head) strides); returns the status code."""
+    arr = [None if x is None else _I64x2(*[int(i) for i in x]) for x in (q_strides, o_strides)]
+    ref = lambda x: None if x is None else ctypes.addressof(x)
+    return load().fa_forward_paged_tree(h, ref(cache), ref(seqs), ref(tree), total, Q, O, lse, Hq, float(scale), *arr, stream)
+
+
+def fa_compact_paged(h, caches, num_caches, seqs, cu_seqlens, total, keep, keep_stride, keep_counts, max_keep, new_lens, stream=0) -> int:
+    """Raw call: `caches` is an array of fa_paged_cache structures; returns the status code."""
+    ref = lambda x: None if x is None else ctypes.addressof(x)
+    return load().fa_compact_paged(h, ref(caches), num_caches, ref(seqs), cu_seqlens, total, keep, keep_stride, keep_counts, max_keep, new_lens,
+                                   stream)
+
+
+def fa_copy_pages(h, caches, num_caches, src, dst, slots, n, stream=0) -> int:
+    """Raw call: `caches` is an array of fa_paged_cache structures; returns the status code."""
+    return load().fa_copy_pages(h, None if caches is None else ctypes.addressof(caches), num_caches, src, dst, slots, n, stream)
+
+
 def fa_forward_paged(h, cache, seqs, Q, O, lse, Hq, Sq, scale, q_strides, o_strides, stream=0) -> int:
     """Raw call on a paged cache (structures above, pointers as integers, (token, head) strides); returns the status code."""
     arr = [None if x is None else _I64x2(*[int(i) for i in x]) for x in (q_strides, o_strides)]
@@ -488,18 +545,38 @@ class PagedCache:
         self.address = ctypes.addressof(self.c)
 
 
+class PagedCaches:
+    """The caches of a model's layers for `compact_paged` and `copy_pages`: PagedCache objects of one geometry (type, sizes and
+    strides) on one device.  Make it once; it keeps the caches alive."""
+
+    def __init__(self, caches):
+        caches = list(caches)
+        if not caches or any(c.device != caches[0].device for c in caches):
+            raise ValueError("caches must be PagedCache objects on one device, at least one")
+        self.caches, self.device, self.count = caches, caches[0].device, len(caches)
+        self.c = (fa_paged_cache * self.count)(*[c.c for c in caches])
+        self.address = ctypes.addressof(self.c)
+
+
 class Rope:
     """Rotation by position for `append_paged`: cos_sin is a contiguous fp32 CUDA tensor [max_pos, dim] (dim/2 cosines, then
     dim/2 sines per position); of every `span` dimensions of a head (0: the whole head) those from `offset` on are turned, as
-    halves or in interleaved pairs."""
+    halves or in interleaved pairs.  axis_of_pair (dim/2 numbers; None: all 0) says which axis of given positions turns each pair."""
 
-    def __init__(self, cos_sin, *, offset: int = 0, span: int = 0, interleaved: bool = False):
+    def __init__(self, cos_sin, *, offset: int = 0, span: int = 0, interleaved: bool = False, axis_of_pair=None):
         import torch
         if cos_sin.dtype != torch.float32 or not cos_sin.is_cuda or not cos_sin.is_contiguous() or cos_sin.dim() != 2:
             raise ValueError("cos_sin must be a contiguous 2-D fp32 CUDA tensor")
         self.cos_sin, self.device, self.span = cos_sin, cos_sin.device, int(span)
         self.offset, self.interleaved = int(offset), int(bool(interleaved))
         self.structs = {}                 # by span
+        self.axes, self.axis_of_pair = 1, None
+        if axis_of_pair is not None:
+            numbers = [int(a) for a in axis_of_pair]
+            if len(numbers) != cos_sin.shape[1] // 2 or any(not 0 <= a < FA_MAX_AXES for a in numbers):
+                raise ValueError("axis_of_pair must be dim / 2 numbers from 0 to %d" % (FA_MAX_AXES - 1))
+            self.axes = max(numbers) + 1
+            self.axis_of_pair = (ctypes.c_uint8 * len(numbers))(*numbers)
 
     def struct_for(self, dqk: int) -> int:
         """Address of the C structure for heads of dqk dimensions."""
@@ -539,6 +616,33 @@ def _seqs(h, cache, block_table, seq_lens):
                          max_pages, 0)
 
 
+def _offsets(cu_seqlens, B, device):
+    """Pointer of a call's offsets, None where the sequences have equally many rows."""
+    import torch
+    if cu_seqlens is None:
+        return None
+    if (cu_seqlens.dtype is not torch.int32 or cu_seqlens.device != device or cu_seqlens.shape != (B + 1,) or
+            not cu_seqlens.is_contiguous()):
+        raise ValueError("cu_seqlens must be a contiguous int32 tensor of B + 1 offsets on the cache's device")
+    return cu_seqlens.data_ptr()
+
+
+def _most_tokens(max_tokens, cu_seqlens, total, B):
+    """The largest number of drafts of a sequence."""
+    if max_tokens > 0:
+        return int(max_tokens)
+    if cu_seqlens is not None or max_tokens < 0:
+        raise ValueError("max_tokens is needed with cu_seqlens")
+    return max(1, total // max(1, B))
+
+
+def _check_mask(mask, total, words, device):
+    import torch
+    if (mask.dtype is not torch.int32 or mask.device != device or mask.dim() != 2 or mask.shape[0] != total or mask.shape[1] < words or
+            (mask.shape[1] > 1 and mask.stride(1) != 1) or (total > 1 and mask.stride(0) < words)):
+        raise ValueError("mask must be int32 of shape [tokens, %d or more], its rows contiguous and apart" % words)
+
+
 def _rows(t, cache, d, what):
     """Tokens, heads and (token, head) strides of a [tokens, heads, d] bf16 tensor on the cache's device."""
     import torch
@@ -562,11 +666,13 @@ def _new(q, tokens, heads, d):
     return torch.empty_like(q) if q.shape[2] == d and q.is_contiguous() else q.new_empty((tokens, heads, d))
 
 
-def append_paged(h, k, v, cache: PagedCache, block_table, seq_lens, *, cu_seqlens=None, q=None, q_out=None, rope: Rope = None):
+def append_paged(h, k, v, cache: PagedCache, block_table, seq_lens, *, cu_seqlens=None, q=None, q_out=None, rope: Rope = None,
+                 positions=None):
     """New keys and values [T, Hkv, d] of packed tokens into `cache`, rotated by their positions; returns q_out.
 
     seq_lens [B] int32 counts the new tokens in; cu_seqlens [B+1] int32 gives each sequence's rows (None: T / B each).  With q
-    [T, Hq, dqk] the queries are rotated too, into q_out (allocated when not given; may be q itself).
+    [T, Hq, dqk] the queries are rotated too, into q_out (allocated when not given; may be q itself).  positions ([T] or [axes, T]
+    int32): the rows of the rotation table, where they do not follow from the slots (drafted trees, pictures).
     """
     import torch
     seqs = _seqs(h, cache, block_table, seq_lens)
@@ -574,12 +680,7 @@ def append_paged(h, k, v, cache: PagedCache, block_table, seq_lens, *, cu_seqlen
     Tv, Hv, vt, vh = _rows(v, cache, cache.dv, "v")
     if Tv != total or Hk != cache.Hkv or Hv != Hk:
         raise ValueError("k and v must have the same tokens and the cache's heads")
-    cu_ptr = None
-    if cu_seqlens is not None:
-        if (cu_seqlens.dtype is not torch.int32 or cu_seqlens.device != cache.device or cu_seqlens.shape != (seqs.B + 1,) or
-                not cu_seqlens.is_contiguous()):
-            raise ValueError("cu_seqlens must be a contiguous int32 tensor of B + 1 offsets on the cache's device")
-        cu_ptr = cu_seqlens.data_ptr()
+    cu_ptr = _offsets(cu_seqlens, seqs.B, cache.device)
     rope_ptr = None
     if rope is not None:
         if rope.device != cache.device:
@@ -603,11 +704,61 @@ def append_paged(h, k, v, cache: PagedCache, block_table, seq_lens, *, cu_seqlen
         raise ValueError("q_out without q")
     strides = _I64x8(kt, kh, vt, vh, qt, qh, ot, oh)
     at = ctypes.addressof(strides)
-    st = _lib.fa_append_paged(h, cache.address, ctypes.addressof(seqs), cu_ptr, total, k.data_ptr(), v.data_ptr(), q_ptr, qo_ptr, Hq,
-                              at, at + 16, at + 32, at + 48, rope_ptr, _raw_stream(cache.device))
+    if positions is None:
+        st = _lib.fa_append_paged(h, cache.address, ctypes.addressof(seqs), cu_ptr, total, k.data_ptr(), v.data_ptr(), q_ptr, qo_ptr, Hq,
+                                  at, at + 16, at + 32, at + 48, rope_ptr, _raw_stream(cache.device))
+    else:
+        if rope is None:
+            raise ValueError("positions without a rotation")
+        one = positions.dim() == 1
+        if (positions.dtype is not torch.int32 or positions.device != cache.device or positions.dim() not in (1, 2) or
+                positions.shape[-1] != total or (total > 1 and positions.stride(-1) != 1)):
+            raise ValueError("positions must be int32 of shape [T] or [axes, T] on the cache's device, contiguous along the tokens")
+        axes = 1 if one else positions.shape[0]
+        if axes < rope.axes or not 1 <= axes <= FA_MAX_AXES:
+            raise ValueError("positions must have the %d to %d axes that turn the pairs" % (rope.axes, FA_MAX_AXES))
+        p = fa_positions(_POSITIONS_SIZE, axes, positions.data_ptr(), total if axes == 1 else positions.stride(0),
+                         None if rope.axis_of_pair is None else ctypes.addressof(rope.axis_of_pair))
+        st = _lib.fa_append_paged_at(h, cache.address, ctypes.addressof(seqs), cu_ptr, total, k.data_ptr(), v.data_ptr(), q_ptr, qo_ptr, Hq,
+                                     at, at + 16, at + 32, at + 48, rope_ptr, ctypes.addressof(p), _raw_stream(cache.device))
     if st != FA_OK:
         raise FaError(st, "fa_append_paged")
     return q_out
+
+
+def tree_layout(h, parents, seq_lens, *, cu_seqlens=None, max_tokens: int = 0, mask=None, positions=None):
+    """What the tokens of drafted trees see, and their positions, from their parents.
+
+    parents [T] int32: a token's parent among the drafts of its sequence (a smaller number than its own), or -1.  seq_lens [B] int32
+    counts the drafts in, cu_seqlens [B+1] int32 gives each sequence's rows (None: T / B each), max_tokens is the largest number
+    of drafts of a sequence (0: T / B).  Returns (mask [T, ceil(max_tokens / 32)] int32, positions [T] int32), new tensors where none
+    are given (rows behind the last sequence stay as they were).
+    """
+    import torch
+    i32, device = torch.int32, parents.device
+    if parents.dtype is not i32 or not parents.is_cuda or parents.dim() != 1 or not parents.is_contiguous():
+        raise ValueError("parents must be a contiguous 1-D int32 CUDA tensor")
+    if seq_lens.dtype is not i32 or seq_lens.device != device or seq_lens.dim() != 1 or not seq_lens.is_contiguous():
+        raise ValueError("seq_lens must be a contiguous 1-D int32 tensor on parents' device")
+    if load().fa_device(h) != device.index:
+        raise ValueError("the handle belongs to another device than the tensors")
+    total, B = parents.shape[0], seq_lens.shape[0]
+    cu_ptr = _offsets(cu_seqlens, B, device)
+    most = _most_tokens(max_tokens, cu_seqlens, total, B)
+    words = (most + 31) // 32
+    if mask is None:
+        mask = parents.new_empty((total, words))
+    else:
+        _check_mask(mask, total, words, device)
+    if positions is None:
+        positions = torch.empty_like(parents)
+    elif positions.dtype is not i32 or positions.device != device or positions.shape != (total,) or not positions.is_contiguous():
+        raise ValueError("positions must be a contiguous int32 tensor of one number per token")
+    st = _lib.fa_tree_layout(h, parents.data_ptr(), cu_ptr, total, B, seq_lens.data_ptr(), most, mask.data_ptr(),
+                             mask.stride(0) if total > 1 else words, positions.data_ptr(), _raw_stream(device))
+    if st != FA_OK:
+        raise FaError(st, "fa_tree_layout")
+    return mask, positions
 
 
 def _paged_out(q, cache, seqs, out):
@@ -640,6 +791,90 @@ def forward_paged(h, q, cache: PagedCache, block_table, seq_lens, *, scale: floa
     if st != FA_OK:
         raise FaError(st, "fa_forward_paged")
     return out, lse
+
+
+def forward_paged_tree(h, q, cache: PagedCache, block_table, seq_lens, mask, *, cu_seqlens=None, max_tokens: int = 0, scale: float = 0.0,
+                       out=None, want_lse=True):
+    """Attention of the drafted tokens of every sequence over a paged cache that holds them: q [T, Hq, dqk] bf16, packed.
+
+    A token sees all keys before the drafts, and of the drafts those whose bit its row of `mask` has ([T, ceil(max_tokens / 32)] int32,
+    as tree_layout makes it; None: the drafts up to itself).  seq_lens [B] int32 counts the drafts in, cu_seqlens [B+1] int32
+    gives each sequence's rows (None: T / B each), max_tokens is the largest number of drafts of a sequence (0: T / B).  Returns
+    (O [T, Hq, dv], lse [Hq, T] fp32 or None); rows behind the last sequence are not written.
+    """
+    import torch
+    seqs = _seqs(h, cache, block_table, seq_lens)
+    T, Hq, qt, qh = _rows(q, cache, cache.dqk, "q")
+    B = seqs.B
+    if T and (B == 0 or cu_seqlens is None and T % B):
+        raise ValueError("q must hold the same number of tokens for every sequence, or cu_seqlens say how many")
+    cu_ptr = _offsets(cu_seqlens, B, cache.device)
+    most = _most_tokens(max_tokens, cu_seqlens, T, B)
+    tree = fa_tree(_TREE_SIZE, most, cu_ptr, None, 0)
+    if mask is not None:
+        _check_mask(mask, T, (most + 31) // 32, cache.device)
+        tree.mask = mask.data_ptr()
+        tree.mask_stride = mask.stride(0) if T > 1 else (most + 31) // 32
+    if out is None:
+        out = _new(q, T, Hq, cache.dv)
+        ot, oh = Hq * cache.dv, cache.dv
+    else:
+        To, Ho, ot, oh = _rows(out, cache, cache.dv, "out")
+        if To != T or Ho != Hq:
+            raise ValueError("out must have shape %s" % ((T, Hq, cache.dv),))
+    lse = q.new_empty((Hq, T), dtype=torch.float32) if want_lse else None
+    strides = _I64x4(qt, qh, ot, oh)
+    at = ctypes.addressof(strides)
+    st = _lib.fa_forward_paged_tree(h, cache.address, ctypes.addressof(seqs), ctypes.addressof(tree), T, q.data_ptr(), out.data_ptr(),
+                                    None if lse is None else lse.data_ptr(), Hq, scale, at, at + 16, _raw_stream(cache.device))
+    if st != FA_OK:
+        raise FaError(st, "fa_forward_paged_tree")
+    return out, lse
+
+
+def compact_paged(h, caches, block_table, seq_lens, keep, keep_counts, *, cu_seqlens=None, total: int = 0, new_lens=None):
+    """The accepted drafts of every sequence move up to its first drafts' slots, in one or several caches (PagedCache, PagedCaches).
+
+    seq_lens [B] int32 counts the drafts in; cu_seqlens [B+1] int32 as for forward_paged_tree (None: total / B drafts each).  keep
+    [B, most] int32 holds the accepted drafts' numbers in rising order, keep_counts [B] int32 how many.  Returns the new lengths [B]
+    int32 (a new tensor where none is given; not seq_lens itself).
+    """
+    import torch
+    i32, device = torch.int32, caches.device
+    seqs = _seqs(h, caches, block_table, seq_lens)
+    B = seqs.B
+    if (keep.dtype is not i32 or keep.device != device or keep.dim() != 2 or keep.shape[0] != B or keep.shape[1] < 1 or
+            (keep.shape[1] > 1 and keep.stride(1) != 1) or (B > 1 and keep.stride(0) < keep.shape[1])):
+        raise ValueError("keep must be int32 of shape [B, most], its rows contiguous and apart")
+    if keep_counts.dtype is not i32 or keep_counts.device != device or keep_counts.shape != (B,) or not keep_counts.is_contiguous():
+        raise ValueError("keep_counts must be a contiguous int32 tensor of B numbers")
+    if new_lens is None:
+        new_lens = torch.empty_like(seq_lens)
+    elif (new_lens.dtype is not i32 or new_lens.device != device or new_lens.shape != (B,) or not new_lens.is_contiguous() or
+          (B and new_lens.data_ptr() == seq_lens.data_ptr())):
+        raise ValueError("new_lens must be a contiguous int32 tensor of B numbers, another one than seq_lens")
+    st = _lib.fa_compact_paged(h, caches.address, getattr(caches, "count", 1), ctypes.addressof(seqs), _offsets(cu_seqlens, B, device), int(total)
+                               if cu_seqlens is None else _INT_MAX, keep.data_ptr(), keep.stride(0) if B > 1 else keep.shape[1],
+                               keep_counts.data_ptr(), keep.shape[1], new_lens.data_ptr(), _raw_stream(device))
+    if st != FA_OK:
+        raise FaError(st, "fa_compact_paged")
+    return new_lens
+
+
+def copy_pages(h, caches, src, dst, *, slots=None):
+    """Page dst[i] receives what page src[i] holds, in one or several caches (PagedCache, PagedCaches): int32 tensors of one length on their
+    device, negative entries are skipped.  slots (int32, the same length): how many leading slots of each page; None: all."""
+    import torch
+    device = caches.device
+    for t in (src, dst) if slots is None else (src, dst, slots):
+        if t.dtype is not torch.int32 or t.device != device or t.dim() != 1 or t.shape != src.shape or not t.is_contiguous():
+            raise ValueError("src, dst and slots must be contiguous 1-D int32 tensors of one length on the caches' device")
+    if _lib.fa_device(h) != device.index:
+        raise ValueError("the handle belongs to another device than the caches")
+    st = _lib.fa_copy_pages(h, caches.address, getattr(caches, "count", 1), src.data_ptr(), dst.data_ptr(),
+                            None if slots is None else slots.data_ptr(), src.shape[0], _raw_stream(device))
+    if st != FA_OK:
+        raise FaError(st, "fa_copy_pages")
 
 
 def _diff(lam, norm_weight, eps, out_scale, Hq, device):

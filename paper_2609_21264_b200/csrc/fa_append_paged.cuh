@@ -12,6 +12,8 @@
 
 namespace fa {
 
+constexpr int kMostAxes = 4, kMostPairs = 96;
+
 struct AppendParams {
     const __nv_bfloat16 *K, *V, *Q;          // element (t, h, c) at K + t*k_st + h*k_sh + c
     __nv_bfloat16* Q_out;
@@ -37,6 +39,11 @@ struct AppendParams {
     uint32_t head_magic, span_magic, v_magic;       // ceil(2^32 / divisor): exact quotients of numbers below 2^16
     int tokens;                                     // of a block
     uint32_t* status;
+    // Positions given for every token (kAt): row `pos[axis * pos_stride + token]` of the table turns the pairs of `axis`; two bits a pair
+    const int* pos;
+    long long pos_stride;
+    int axes;
+    uint32_t axis_bits[kMostPairs / 16];
 };
 
 // Eight neighbouring values of a row.
@@ -82,12 +89,16 @@ constexpr int kAppendThreads = 256, kAppendMaxTokens = 16;
 
 // A unit of a half-split rotation is the pair of vectors whose values turn into each other, so that every value is read and written by
 // one thread alone (Q_out may be Q).
-template <bool kE4m3>
+//
+// kAt: the table's rows are given, one per token and axis.  The rows of a block's tokens are looked up with their slots; four pairs of one
+// axis (sections of the pairs, as a rule) take their angles in two 16-byte loads, four of several axes in eight of 4 bytes.
+template <bool kE4m3, bool kAt = false>
 __global__ void __launch_bounds__(kAppendThreads)
 fa_append_paged_kernel(const AppendParams p) {
     constexpr int kDeep = 2;
     struct Token { long long k_at, v_at; int pos, live; };      // offsets of its slot in the two caches
     __shared__ Token token[kAppendMaxTokens];
+    __shared__ int token_row[kAt ? kAppendMaxTokens : 1][kMostAxes];
     ptx::grid_launch_dependents();
     ptx::grid_dependency_wait();
     const int t0 = blockIdx.x * p.tokens, n_tokens = min(p.tokens, p.total - t0);
@@ -140,10 +151,25 @@ fa_append_paged_kernel(const AppendParams p) {
         if (x.j >= 0) {
             const float* cs = p.cos_sin + static_cast<long long>(tk.pos) * p.rot_dim + x.j;
             const float* sn = cs + (p.rot_dim >> 1);
+            const uint32_t axes8 = kAt ? p.axis_bits[x.j >> 4] >> (2 * (x.j & 15)) : 0u;
 #pragma unroll
             for (int e = 0; e < 8; e += 4) {
-                const float4 c4 = __ldg(reinterpret_cast<const float4*>(cs + e)), s4 = __ldg(reinterpret_cast<const float4*>(sn + e));
-                const float cc[4] = {c4.x, c4.y, c4.z, c4.w}, ss[4] = {s4.x, s4.y, s4.z, s4.w};
+                float cc[4], ss[4];
+                const uint32_t axes4 = (axes8 >> (2 * e)) & 255u;
+                if (!kAt || axes4 == (axes4 & 3u) * 0x55u) {
+                    const float* ce = kAt ? p.cos_sin + static_cast<long long>(token_row[kAt ? x.t : 0][axes4 & 3u]) * p.rot_dim + x.j : cs;
+                    const float* se = kAt ? ce + (p.rot_dim >> 1) : sn;
+                    const float4 c4 = __ldg(reinterpret_cast<const float4*>(ce + e)), s4 = __ldg(reinterpret_cast<const float4*>(se + e));
+                    cc[0] = c4.x; cc[1] = c4.y; cc[2] = c4.z; cc[3] = c4.w;
+                    ss[0] = s4.x; ss[1] = s4.y; ss[2] = s4.z; ss[3] = s4.w;
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const float* ce = p.cos_sin + static_cast<long long>(token_row[kAt ? x.t : 0][(axes4 >> (2 * q)) & 3u]) * p.rot_dim + x.j + e + q;
+                        cc[q] = __ldg(ce);
+                        ss[q] = __ldg(ce + (p.rot_dim >> 1));
+                    }
+                }
                 Vec8& z = e == 0 ? v : w;            // interleaved: four pairs of each vector
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
@@ -217,16 +243,25 @@ fa_append_paged_kernel(const AppendParams p) {
                 // (the padding of a batch)
             } else if (at >= p.max_pages) {
                 report_bad_input(p.status, kSiteBadLength);
-            } else if (p.rot_dim && tk.pos >= p.max_pos) {
+            } else if (!kAt && p.rot_dim && tk.pos >= p.max_pos) {
                 report_bad_input(p.status, kSiteBadPosition);
             } else {
+                bool rows_ok = true;
+                if constexpr (kAt) {
+                    for (int a = 0; a < p.axes; ++a) {
+                        const int r = p.pos[a * p.pos_stride + row];
+                        rows_ok = rows_ok && r >= 0 && r < p.max_pos;
+                        token_row[threadIdx.x][a] = r;
+                    }
+                    if (!rows_ok) report_bad_input(p.status, kSiteBadPosition);
+                }
                 const int page = p.block_table[b * p.table_stride + at], slot = tk.pos - at * p.page_size;
                 if (page < 0 || page >= p.num_pages) {
                     report_bad_input(p.status, kSiteBadPage);
                 } else {
                     tk.k_at = page * p.k_stride[0] + slot * p.k_stride[2];
                     tk.v_at = page * p.v_stride[0] + slot * p.v_stride[2];
-                    tk.live = 1;
+                    tk.live = rows_ok ? 1 : 0;
                 }
             }
         }

@@ -13,6 +13,7 @@
 #include "fa_handle.h"
 #include "fa_paged.cuh"
 #include "fa_paged_common.cuh"
+#include "fa_paged_host.h"
 #include "fa_paged_simple.cuh"
 
 namespace {
@@ -24,67 +25,11 @@ using namespace fa_host;
 // 400 keys lose 1.5 us there).
 constexpr int kLeastUnits = 2;
 
-bool head_sizes_ok(int dqk, int dv) {
-    return (dqk == 64 && dv == 64) || (dqk == 128 && dv == 128) || (dqk == 192 && dv == 128);
-}
-
-fa_status check_cache(const fa_paged_cache* c) {
-    if (!c || c->struct_size != sizeof(fa_paged_cache) || c->reserved != 0) return FA_ERR_INVALID_ARG;
-    if (c->type != FA_CACHE_BF16 && c->type != FA_CACHE_E4M3) return FA_ERR_INVALID_ARG;
-    if (!c->k || !c->v || misaligned(c->k, 16) || misaligned(c->v, 16)) return FA_ERR_INVALID_ARG;
-    if (c->num_pages <= 0 || c->page_size <= 0 || c->Hkv <= 0 || c->dqk <= 0 || c->dv <= 0) return FA_ERR_INVALID_ARG;
-    if (!head_sizes_ok(c->dqk, c->dv)) return FA_ERR_UNSUPPORTED;
-    if (c->page_size % 16 != 0 || c->page_size > 65536 || c->Hkv > 65535) return FA_ERR_UNSUPPORTED;
-    const int64_t unit = c->type == FA_CACHE_E4M3 ? 16 : 8;      // 16 bytes
-    for (int i = 0; i < 3; ++i)
-        if (c->k_strides[i] <= 0 || c->v_strides[i] <= 0 || c->k_strides[i] % unit != 0 || c->v_strides[i] % unit != 0)
-            return FA_ERR_INVALID_ARG;
-    if (c->k_strides[2] < c->dqk || c->v_strides[2] < c->dv) return FA_ERR_INVALID_ARG;
-    if (c->type == FA_CACHE_BF16 && (c->k_scale || c->v_scale)) return FA_ERR_INVALID_ARG;
-    if ((c->k_scale && misaligned(c->k_scale, 4)) || (c->v_scale && misaligned(c->v_scale, 4))) return FA_ERR_INVALID_ARG;
-    return FA_OK;
-}
-
-fa_status check_seqs(const fa_paged_seqs* s, const fa_paged_cache* c) {
-    if (!s || s->struct_size != sizeof(fa_paged_seqs) || s->reserved != 0) return FA_ERR_INVALID_ARG;
-    if (s->B < 0 || s->max_pages < 0 || s->table_stride < s->max_pages) return FA_ERR_INVALID_ARG;
-    if (s->B > 0 && (s->max_pages == 0 || !s->block_table || !s->seq_lens)) return FA_ERR_INVALID_ARG;
-    if (misaligned(s->block_table, 4) || misaligned(s->seq_lens, 4)) return FA_ERR_INVALID_ARG;
-    // positions are 32-bit
-    if (static_cast<int64_t>(s->max_pages) * c->page_size > 0x7fffff00LL) return FA_ERR_UNSUPPORTED;
-    return FA_OK;
-}
-
-// {token, head} strides of a row-major [tokens, heads, d] tensor
-bool row_strides_ok(const int64_t* s, int d) { return s && s[0] > 0 && s[1] >= d && ((s[0] | s[1]) & 7) == 0; }
-
 fa_status check_diff(const fa_diff* d) {
     if (!d || d->struct_size != sizeof(fa_diff) || d->reserved != 0.f) return FA_ERR_INVALID_ARG;
     if (!d->lambda || misaligned(d->lambda, 4)) return FA_ERR_INVALID_ARG;
     if (d->weight && (misaligned(d->weight, 16) || !isfinite(d->eps) || d->eps <= 0.f)) return FA_ERR_INVALID_ARG;
     if (!isfinite(d->out_scale)) return FA_ERR_INVALID_ARG;
-    return FA_OK;
-}
-
-// Launch with programmatic stream serialisation (see FA_FLAG_NO_DEPENDENT_LAUNCH).
-template <typename... Params, typename... Args>
-fa_status launch(fa_handle* h, void (*kernel)(Params...), long long blocks, int threads, int smem, cudaStream_t st, const Args&... args) {
-    if (blocks <= 0 || blocks > 0x7fffffffLL) return FA_ERR_UNSUPPORTED;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(blocks), 1, 1);
-    cfg.blockDim = dim3(threads, 1, 1);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cfg.attrs = attr;
-    cfg.numAttrs = (h->flags & FA_FLAG_NO_DEPENDENT_LAUNCH) ? 0 : 1;
-    if (cudaLaunchKernelEx(&cfg, kernel, args...) != cudaSuccess) {
-        cudaGetLastError();
-        return FA_ERR_CUDA;
-    }
-    h->launches += 1;
     return FA_OK;
 }
 
@@ -238,6 +183,14 @@ fa_status fa_append_paged(fa_handle* h, const fa_paged_cache* cache, const fa_pa
                           const void* K, const void* V, const void* Q, void* Q_out, int Hq, const int64_t* k_strides,
                           const int64_t* v_strides, const int64_t* q_strides, const int64_t* qo_strides, const fa_rope* rope,
                           void* stream) {
+    return fa_append_paged_at(h, cache, seqs, cu_seqlens, total, K, V, Q, Q_out, Hq, k_strides, v_strides, q_strides, qo_strides, rope, nullptr,
+                              stream);
+}
+
+fa_status fa_append_paged_at(fa_handle* h, const fa_paged_cache* cache, const fa_paged_seqs* seqs, const int32_t* cu_seqlens, int total,
+                             const void* K, const void* V, const void* Q, void* Q_out, int Hq, const int64_t* k_strides,
+                             const int64_t* v_strides, const int64_t* q_strides, const int64_t* qo_strides, const fa_rope* rope,
+                             const fa_positions* positions, void* stream) {
     if (!h) return FA_ERR_INVALID_ARG;
     fa_status s = check_cache(cache);
     if (s != FA_OK) return s;
@@ -258,6 +211,13 @@ fa_status fa_append_paged(fa_handle* h, const fa_paged_cache* cache, const fa_pa
         if (rope->max_pos <= 0 || rope->dim <= 0 || rope->offset < 0 || rope->span <= 0) return FA_ERR_INVALID_ARG;
         if (rope->dim % 16 != 0 || rope->span % 16 != 0 || rope->offset % 8 != 0) return FA_ERR_UNSUPPORTED;
         if (cache->dqk % rope->span != 0 || rope->dim > rope->span || rope->offset > rope->span - rope->dim) return FA_ERR_INVALID_ARG;
+    }
+    if (positions) {
+        if (!rope || positions->struct_size != sizeof(fa_positions) || !positions->pos || misaligned(positions->pos, 4)) return FA_ERR_INVALID_ARG;
+        if (positions->axes <= 0 || (positions->axes > 1 && positions->stride < total)) return FA_ERR_INVALID_ARG;
+        if (positions->axes > FA_MAX_AXES) return FA_ERR_UNSUPPORTED;
+        for (int i = 0; positions->axis_of_pair && i < rope->dim / 2; ++i)
+            if (positions->axis_of_pair[i] >= positions->axes) return FA_ERR_INVALID_ARG;
     }
     DeviceGuard guard(h->device);
     if (!guard.ok()) return FA_ERR_CUDA;
@@ -289,6 +249,14 @@ fa_status fa_append_paged(fa_handle* h, const fa_paged_cache* cache, const fa_pa
         p.max_pos = rope->max_pos; p.rot_dim = rope->dim; p.rot_offset = rope->offset; p.span = rope->span;
         p.interleaved = rope->interleaved ? 1 : 0;
     }
+    if (positions) {
+        static_assert(fa::kMostAxes == FA_MAX_AXES, "axis numbers are two bits");
+        p.pos = positions->pos;
+        p.pos_stride = positions->stride;
+        p.axes = positions->axes;
+        for (int i = 0; positions->axis_of_pair && i < rope->dim / 2; ++i)       // (dim is at most the head size, 192)
+            p.axis_bits[i / 16] |= static_cast<uint32_t>(positions->axis_of_pair[i]) << (2 * (i % 16));
+    }
     // the span's vectors before, in and behind its turned part, and the units that they are cut into
     const int before = p.rot_offset / 8, behind = (p.span - p.rot_offset - p.rot_dim) / 8;
     p.before_step = before % 2 == 0 ? 2 : 1;
@@ -315,6 +283,10 @@ fa_status fa_append_paged(fa_handle* h, const fa_paged_cache* cache, const fa_pa
     h->last_splits = 1;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const long long blocks = (static_cast<long long>(total) + p.tokens - 1) / p.tokens;
+    if (positions) {
+        if (cache->type == FA_CACHE_E4M3) return launch(h, fa::fa_append_paged_kernel<true, true>, blocks, fa::kAppendThreads, 0, st, p);
+        return launch(h, fa::fa_append_paged_kernel<false, true>, blocks, fa::kAppendThreads, 0, st, p);
+    }
     if (cache->type == FA_CACHE_E4M3) return launch(h, fa::fa_append_paged_kernel<true>, blocks, fa::kAppendThreads, 0, st, p);
     return launch(h, fa::fa_append_paged_kernel<false>, blocks, fa::kAppendThreads, 0, st, p);
 }

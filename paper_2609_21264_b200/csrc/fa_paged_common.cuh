@@ -12,7 +12,8 @@
 namespace fa {
 
 // Contents that only the device sees and that a call may not have: reported as FA_ERR_INVALID_ARG with one of these.
-constexpr uint32_t kSiteBadLength = 0x0901, kSiteBadPage = 0x0902, kSiteBadPosition = 0x0903;
+constexpr uint32_t kSiteBadLength = 0x0901, kSiteBadPage = 0x0902, kSiteBadPosition = 0x0903, kSiteBadRows = 0x0904,
+                   kSiteBadParent = 0x0905, kSiteBadKeep = 0x0906;
 
 struct PagedParams {
     const __nv_bfloat16* Q;       // token i of sequence b: element (hq, c) at Q + b*q_sb + i*q_st + hq*q_sh + c
@@ -61,6 +62,26 @@ __host__ __device__ inline int clamped_len(int len, int max_pages, int page_size
         return len < 0 ? 0 : static_cast<int>(most);
     }
     return len;
+}
+
+// The drafted tokens of sequence b: its rows of the call's tensors.  A sequence whose rows do not lie in [0, total], or that has
+// more than `most`, counts as one without.
+struct DraftRows { int first, count; };
+__host__ __device__ inline DraftRows draft_rows(const int* cu_seqlens, int b, int B, int total, int most, uint32_t* status) {
+    DraftRows r;
+    if (!cu_seqlens) {
+        r.count = total / B;
+        r.first = b * r.count;
+        return r;
+    }
+    r.first = cu_seqlens[b];
+    const long long n = static_cast<long long>(cu_seqlens[b + 1]) - r.first;
+    r.count = static_cast<int>(n);
+    if (r.first < 0 || n < 0 || n > most || r.first + n > total) {
+        report_bad_input(status, kSiteBadRows);
+        r.first = r.count = 0;
+    }
+    return r;
 }
 
 FA_DEVI float e4m3_to_float(uint8_t code) {
