@@ -677,6 +677,8 @@ fa_status fa_create(fa_handle** out, const fa_config* cfg) {
                       FA_FLAG_TWO_CTA_KERNEL | FA_FLAG_QUAD_KERNEL)) return FA_ERR_INVALID_ARG;
         if (kv_splits_cfg > 256) return FA_ERR_INVALID_ARG;
     }
+    // (the default: 32 MiB, and 40 for attention of drafted tokens, whose two partial results per SM are up to 130 KB each)
+    const uint64_t tree_scratch_bytes = scratch_bytes == 0 ? 40ull << 20 : scratch_bytes;
     if (scratch_bytes == 0) scratch_bytes = 32ull << 20;
     int count = 0;
     if (cudaGetDeviceCount(&count) != cudaSuccess || count <= 0) {
@@ -732,13 +734,14 @@ fa_status fa_create(fa_handle** out, const fa_config* cfg) {
         delete h;
         return FA_ERR_CUDA;
     }
-    if (cudaMalloc(&h->scratch, scratch_bytes) != cudaSuccess) {
+    if (cudaMalloc(&h->scratch, tree_scratch_bytes) != cudaSuccess) {
         cudaGetLastError();
         cudaFreeHost(h->status_host);
         delete h;
         return FA_ERR_OOM;
     }
     h->scratch_bytes = scratch_bytes;
+    h->tree_scratch_bytes = tree_scratch_bytes;
     const size_t counter_bytes = 256 + static_cast<size_t>(num_sms) * sizeof(unsigned int);
     if (cudaMalloc(reinterpret_cast<void**>(&h->sched_counter), counter_bytes) != cudaSuccess ||
         cudaMemset(h->sched_counter, 0, counter_bytes) != cudaSuccess ||

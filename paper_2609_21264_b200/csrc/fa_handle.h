@@ -41,6 +41,7 @@ struct fa_handle {
     unsigned int* sched_counter = nullptr;   // work-item ticket counter of the persistent kernel
     unsigned int* arrivals = nullptr;        // paged kernel: finished pieces of a shared row block, one counter per SM (zero between launches)
     size_t scratch_bytes = 0;
+    size_t tree_scratch_bytes = 0;           // of the same buffer, what attention of drafted tokens may use
     int last_splits = 1;
     unsigned long long wait_limit_ns = 2000ull * 1000000ull;
     fa_host::EncodeTiledFn encode = nullptr;

@@ -155,14 +155,7 @@ fa_status forward_paged(fa_handle* h, const fa_paged_cache* cache, const fa_page
     if (most_units(p) > kMostUnits) return FA_ERR_UNSUPPORTED;
     const int eb = e4m3 ? 1 : 2;
     const CUtensorMap* m = nullptr;
-    // Rows of one head that lie apart (a [pages, slots, heads, d] pool) are fetched into L2 as they are; with the default of 256 bytes
-    // their neighbours, other heads' rows, would be fetched too, long before or after their own turn (head size 64,
-    // 2 K/V heads, 402 MB: 75 us, against 97 with the default).
-    auto promotion = [&](int d, const int64_t* strides) -> int {
-        const int64_t row = static_cast<int64_t>(d) * eb;
-        if (strides[2] * eb == row || row % 256 == 0) return CU_TENSOR_MAP_L2_PROMOTION_L2_256B;
-        return row % 128 == 0 ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B : CU_TENSOR_MAP_L2_PROMOTION_L2_64B;
-    };
+    auto promotion = [&](int d, const int64_t* strides) { return map_promotion(d, eb, strides); };
     if ((s = get_map(h, cache->k, cache->dqk, cache->page_size, cache->Hkv, cache->num_pages, cache->k_strides[0], cache->k_strides[1],
                      cache->k_strides[2], p.box_rows, &m, eb, 1, 128, promotion(cache->dqk, cache->k_strides))) != FA_OK) return s;
     const CUtensorMap mk = *m;       // a copy: the next insertion may move the cache's entries

@@ -9,6 +9,7 @@
 #include "fa_handle.h"
 #include "fa_paged_common.cuh"
 #include "fa_paged_host.h"
+#include "fa_tree.cuh"
 #include "fa_tree_simple.cuh"
 
 namespace {
@@ -23,6 +24,44 @@ fa_status launch_simple(fa_handle* h, int dqk, const fa::PagedParams& p, const f
     if (dqk == 64) return launch(h, fa::fa_tree_simple_kernel<64, 64, kE4m3>, blocks, 128, 0, st, p, tp);
     if (dqk == 192) return launch(h, fa::fa_tree_simple_kernel<192, 128, kE4m3>, blocks, 128, 0, st, p, tp);
     return launch(h, fa::fa_tree_simple_kernel<128, 128, kE4m3>, blocks, 128, 0, st, p, tp);
+}
+
+// How the list of work is made (fa_tree.cuh).  A row tile's tokens are as many as fit, and no more than a sequence can have.  A tile of keys
+// counts what it takes: where two row tiles share it HBM still bounds 16-bit caches of head size 128, so it counts as for one; smaller tiles
+// (head size 64, 8 bits) are bound by the exponentials, which two row tiles have twice.
+fa::TreeList make_list(int group, int max_tokens, int dqk, bool e4m3) {
+    fa::TreeList li;
+    li.row_heads = group < 128 ? group : 128;
+    li.head_chunks = (group + li.row_heads - 1) / li.row_heads;
+    li.row_tokens = 128 / li.row_heads < max_tokens ? 128 / li.row_heads : max_tokens;
+    li.two = dqk != 192;
+    li.w1 = 1;
+    li.w2 = e4m3 || dqk == 64 ? 2 : 1;
+    li.cost = 1;
+    li.least = 2 * li.w2;
+    return li;
+}
+
+constexpr long long kMostUnits = 1ll << 30;      // the kernel counts units in 32 bits
+
+template <int DQK, int DV, bool kE4m3>
+fa_status launch_tree(fa_handle* h, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const fa::PagedParams& p, fa::TreeArgs& a,
+                      cudaStream_t st) {
+    using Cfg = fa::TreeCfg<DQK, DV, kE4m3>;
+    constexpr int smem = fa::tree_smem_bytes<DQK, DV, kE4m3>();
+    static_assert(smem <= 227 * 1024, "shared memory budget exceeded");
+    // a CTA per SM, as far as the scratch has two partial results and an entry of the list of what is joined for each
+    const size_t per_cta = 2 * sizeof(float) * fa::tree_slot_floats(DV, Cfg::kTwo) + sizeof(fa::TreeJoin);
+    const long long fit = static_cast<long long>(h->tree_scratch_bytes / per_cta);
+    const int ctas = static_cast<int>(fit < h->num_sms ? fit : h->num_sms);
+    if (ctas < 1) return FA_ERR_UNSUPPORTED;
+    a.part = static_cast<float*>(h->scratch);
+    a.join = reinterpret_cast<fa::TreeJoin*>(a.part + 2ll * ctas * fa::tree_slot_floats(DV, Cfg::kTwo));
+    auto kernel = fa::fa_tree_kernel<DQK, DV, kE4m3>;
+    fa_status s = ensure_smem_attr(h, kernel, smem);
+    if (s != FA_OK) return s;
+    if ((s = launch(h, kernel, ctas, Cfg::kThreads, smem, st, mq, mk, mv, p, a)) != FA_OK) return s;
+    return launch(h, fa::fa_tree_join_kernel<DV, Cfg::kTwo>, static_cast<long long>(ctas) * 4 * (Cfg::kTwo ? 2 : 1), 2 * DV, 0, st, p, a);
 }
 
 }  // namespace
@@ -69,7 +108,34 @@ fa_status fa_forward_paged_tree(fa_handle* h, const fa_paged_cache* cache, const
     p.debug_drop_v_load = (h->flags & FA_FLAG_DEBUG_DROP_V_LOAD) ? 1 : 0;
     const fa::TreeParams tp{tree->cu_seqlens, total, tree->max_tokens, tree->mask, tree->mask_stride};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return cache->type == FA_CACHE_E4M3 ? launch_simple<true>(h, cache->dqk, p, tp, st) : launch_simple<false>(h, cache->dqk, p, tp, st);
+    const bool e4m3 = cache->type == FA_CACHE_E4M3;
+    if (h->flags & FA_FLAG_SERIAL_KERNEL) return e4m3 ? launch_simple<true>(h, cache->dqk, p, tp, st) : launch_simple<false>(h, cache->dqk, p, tp, st);
+    fa::TreeArgs a;
+    memset(&a, 0, sizeof a);
+    a.t = tp;
+    a.group = Hq / cache->Hkv;
+    a.list = make_list(a.group, tree->max_tokens, cache->dqk, e4m3);
+    const long long row_tiles = fa::tree_row_tiles(a.list, tree->max_tokens);
+    const long long most_tiles = (static_cast<long long>(seqs->max_pages) * cache->page_size + fa::kTileN - 1) / fa::kTileN;
+    if (static_cast<long long>(seqs->B) * cache->Hkv > kMostUnits / row_tiles / (most_tiles * a.list.w2 + a.list.cost)) return FA_ERR_UNSUPPORTED;
+    p.box_rows = 16;
+    while (p.box_rows < 128 && cache->page_size % (2 * p.box_rows) == 0) p.box_rows *= 2;
+    const int eb = e4m3 ? 1 : 2;
+    const CUtensorMap* m = nullptr;
+    // (queries: heads in the place of rows, tokens in that of heads; one head may have any stride)
+    if ((s = get_map(h, Q, cache->dqk, Hq, total, 1, q_strides[0], q_strides[0], q_strides[1], a.list.row_heads, &m, 2, a.list.row_tokens)) != FA_OK) return s;
+    const CUtensorMap mq = *m;       // copies: a later insertion may move the cache's entries
+    if ((s = get_map(h, cache->k, cache->dqk, cache->page_size, cache->Hkv, cache->num_pages, cache->k_strides[0], cache->k_strides[1],
+                     cache->k_strides[2], p.box_rows, &m, eb, 1, 128, map_promotion(cache->dqk, eb, cache->k_strides))) != FA_OK) return s;
+    const CUtensorMap mk = *m;
+    if ((s = get_map(h, cache->v, cache->dv, cache->page_size, cache->Hkv, cache->num_pages, cache->v_strides[0], cache->v_strides[1],
+                     cache->v_strides[2], p.box_rows, &m, eb, 1, 128, map_promotion(cache->dv, eb, cache->v_strides))) != FA_OK) return s;
+    const CUtensorMap mv = *m;
+    h->last_kernel = e4m3 ? "fa_tree_e4m3" : "fa_tree";
+    h->last_splits = 1;
+    if (cache->dqk == 64) return e4m3 ? launch_tree<64, 64, true>(h, mq, mk, mv, p, a, st) : launch_tree<64, 64, false>(h, mq, mk, mv, p, a, st);
+    if (cache->dqk == 192) return e4m3 ? launch_tree<192, 128, true>(h, mq, mk, mv, p, a, st) : launch_tree<192, 128, false>(h, mq, mk, mv, p, a, st);
+    return e4m3 ? launch_tree<128, 128, true>(h, mq, mk, mv, p, a, st) : launch_tree<128, 128, false>(h, mq, mk, mv, p, a, st);
 }
 
 }  // extern "C"

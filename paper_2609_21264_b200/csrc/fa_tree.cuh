@@ -1,0 +1,1088 @@
+// Attention of drafted tokens over a paged key/value cache, for sm_100a.
+//
+// A tree of n drafts gives R = n * (Hq / Hkv) query rows per (sequence, K/V head), a handful to some hundred, against thousands of keys that
+// all of them see and n that a mask of bits decides about.  2 R (dqk + dv) flops stand against (dqk + dv) * bytes a key: up to 256
+// rows over a 16-bit cache HBM is the bound, behind that the tensor cores and, as in every kernel here, the exponentials.  So a CTA
+// takes up to 256 rows in one pass over the keys, as two tiles of 128 rows on the accumulator's lanes:
+//
+//   * Two streams t = 0, 1, each with scores S_t, probabilities P_t (over S_t) and accumulator O_t, the loop of fa_fwd_pair.cuh (read that
+//     file first).  With more than 128 rows the streams are the two row tiles and share every K/V tile; with up to 128 they
+//     are the even and the odd K/V tiles of the same rows, merged at the end.  Either way one stream's softmax runs under the other's
+//     MMAs.  (Head sizes 192/128 have no room for a second query tile: always the latter.)
+//   * A row tile is tt tokens x ht heads of the group (ht = the group, tt = 128 / ht), which is one TMA box of Q: rows lie in the tile as
+//     token, head.  Rows that the sequence does not have are computed and not stored.
+//   * The tiles of all (sequence, K/V head, row block)s form one list that the CTAs cut into equal consecutive shares on the device, as
+//     in fa_paged.cuh.  What several CTAs share is joined by a second kernel: its pieces are up to 130 KB each, which the CTA that
+//     finishes last would read alone at the speed of one SM.
+//   * The mask concerns the last tiles alone: a thread has one row, takes its 128 bits for a tile out of the row's words by funnel shifts,
+//     and hides keys past the length with the same bits.
+//
+// Over an e4m3 cache both products are fp16 ones: four more warps turn the codes into fp16, which holds them exactly, on their way
+// from the tiles that TMA has filled to those that are multiplied; the queries are scaled by a power of two per row so that fp16 holds
+// them, the probabilities by 2^7.  (The 8-bit MMA would need three terms for a query and a probability, on the softmax warps, which are
+// the bound already.)
+//
+// Roles: warps 0-3 / 4-7 softmax of stream 0 / 1 and results, warp 8 MMA issue, warp 9 loads of Q and K, warp 10 of V, warp 11 the list
+// and the zeros behind a sequence's last value, over e4m3 caches warps 12-13 / 14-15 the codes of K / V.
+// TMEM: S_0 [0,128) S_1 [128,256) O_0 [256,384) O_1 [384,512); P_t over S_t[0,64).
+#pragma once
+
+#include <cuda_fp16.h>
+#include <math.h>
+
+#include "fa_common.cuh"
+#include "fa_fwd_pair.cuh"
+#include "fa_paged_common.cuh"
+#include "fa_tree_simple.cuh"
+#include "ptx.cuh"
+
+namespace fa {
+
+// ------------------------------------------------------------------ the list of work units and its shares
+
+// A row block (up to two row tiles of a sequence and K/V head) has `cost` units for what it takes beside its tiles, and then `w2` or `w1` units
+// per tile of 128 keys, as it has two row tiles or one.  A tile belongs to the CTA whose share its first unit is in.
+struct TreeList {
+    int row_tokens, row_heads;    // tokens and heads of a row tile
+    int head_chunks;              // row tiles that a token's group is cut into
+    int two;                      // blocks have two row tiles where there are two
+    int cost, w1, w2, least;
+};
+// Row tiles of n drafts.
+__host__ __device__ inline int tree_row_tiles(const TreeList& li, int n) { return (n + li.row_tokens - 1) / li.row_tokens * li.head_chunks; }
+__host__ __device__ inline int tree_tiles(int len) { return (len + kTileN - 1) / kTileN; }
+struct TreeUnits { int pairs, pair, single; };      // blocks of two row tiles, units of each, units of the one behind them (0: none)
+__host__ __device__ inline TreeUnits tree_units(const TreeList& li, int n, int len) {
+    const int rt = tree_row_tiles(li, n), nt = tree_tiles(len);
+    TreeUnits u;
+    if (li.two) {
+        u.pairs = rt / 2;
+        u.pair = li.cost + li.w2 * nt;
+        u.single = rt % 2 ? li.cost + li.w1 * nt : 0;
+    } else {
+        u.pairs = rt;
+        u.pair = li.cost + li.w1 * nt;
+        u.single = 0;
+    }
+    return u;
+}
+__host__ __device__ inline int tree_head_units(const TreeUnits& u) { return u.pairs * u.pair + u.single; }
+__host__ __device__ inline int tree_share(const TreeList& li, int total, int ctas) {
+    const int per = static_cast<int>((static_cast<unsigned>(total) + ctas - 1) / ctas);
+    return per < li.least ? li.least : per;
+}
+
+// A part of the list as the roles of a CTA see it: tiles [t0, t1) of one row block.
+struct TreePart {
+    int b, kvh, row_tile, two;    // first row tile; whether the block has a second one
+    int len, n, row0;             // keys, drafts and first row of the sequence
+    int t0, t1;                   // t1 < 0: the end of the CTA's share
+    int tile0;                    // index of the part's first tile in the CTA's share
+    int slot;                     // of the partial result, -1: the part is whole
+    int pieces;
+};
+// A row block in several pieces as the joining kernel sees it, one per CTA (the one with the first piece; pieces = 0: none).  Piece 0
+// is in slot 2 * CTA + 1, piece i in slot 2 * (CTA + i).
+struct TreeJoin { int kvh, row_tile, two, n, row0, pieces, unused0, unused1; };
+
+// Tiles [t0, t1) that units [u0, u1) hold of a block of nt tiles whose first unit is ub.
+__host__ __device__ inline int tree_tile_at(int u, int ub, int cost, int w, int nt) {
+    const int x = u - ub - cost;
+    const int t = x <= 0 ? 0 : (x + w - 1) / w;
+    return t < nt ? t : nt;
+}
+
+// The list from the unit u0 on: the block that holds it, and the ones behind it.  `next` gives the next part, or false at the end.
+struct TreeWalk {
+    int u0, u1, share, cta;
+    int seq, base, kvh, block;    // the block that is looked at, base: first unit of its K/V head
+    int n, row0, len, tiles;      // of the sequence; tiles handed out
+    TreeUnits u;
+    bool ended;
+};
+template <typename SeqOf>
+__host__ __device__ inline void tree_walk_begin(TreeWalk& w, const TreeList& li, int cta, int share, int total, int seq, int base, SeqOf&& seq_of) {
+    w.cta = cta;
+    w.share = share;
+    w.u0 = static_cast<long long>(cta) * share < total ? cta * share : total;
+    w.u1 = total - w.u0 < share ? total : w.u0 + share;
+    w.ended = w.u0 >= total;
+    w.seq = seq;
+    w.tiles = 0;
+    if (w.ended) return;
+    seq_of(seq, w.n, w.row0, w.len);
+    w.u = tree_units(li, w.n, w.len);
+    const int per = tree_head_units(w.u);
+    w.kvh = (w.u0 - base) / per;
+    w.base = base + w.kvh * per;
+    const int in = w.u0 - w.base, at = in / w.u.pair;
+    w.block = at < w.u.pairs ? at : w.u.pairs;
+}
+template <typename SeqOf>
+__host__ __device__ inline bool tree_walk_next(TreeWalk& w, const TreeList& li, int Hkv, int B, SeqOf&& seq_of, TreePart& e) {
+    while (!w.ended) {
+        const int rt = tree_row_tiles(li, w.n), blocks = w.u.pairs + (w.u.single ? 1 : 0);
+        const int ub = w.base + w.block * w.u.pair, nt = tree_tiles(w.len);
+        const bool pair = w.block < w.u.pairs;
+        const int wt = li.two && pair ? li.w2 : li.w1, end = ub + (pair ? w.u.pair : w.u.single);
+        e.b = w.seq;
+        e.kvh = w.kvh;
+        e.two = li.two && pair ? 1 : 0;
+        e.row_tile = li.two ? 2 * w.block : w.block;
+        e.len = w.len;
+        e.n = w.n;
+        e.row0 = w.row0;
+        e.t0 = tree_tile_at(w.u0, ub, li.cost, wt, nt);
+        e.t1 = tree_tile_at(w.u1, ub, li.cost, wt, nt);
+        e.tile0 = w.tiles;
+        e.slot = -1;
+        e.pieces = 1;
+        const bool some = nt > 0 ? e.t0 < e.t1 : ub >= w.u0;
+        if (some && e.t1 - e.t0 < nt) {
+            e.slot = 2 * w.cta + (e.t0 == 0 ? 1 : 0);
+            e.pieces = (ub + li.cost + (nt - 1) * wt) / w.share - (ub + li.cost) / w.share + 1;
+        }
+        w.tiles += some ? e.t1 - e.t0 : 0;
+        (void)rt;
+        // the block behind it
+        if (end >= w.u1) {
+            w.ended = true;
+        } else if (++w.block == blocks) {
+            w.block = 0;
+            w.base += tree_head_units(w.u);
+            if (++w.kvh == Hkv) {
+                w.kvh = 0;
+                do {
+                    if (++w.seq >= B) { w.ended = true; break; }      // (not reached: the share ends before)
+                    seq_of(w.seq, w.n, w.row0, w.len);
+                } while (w.n == 0);
+                if (!w.ended) w.u = tree_units(li, w.n, w.len);
+            }
+        }
+        if (some) return true;
+    }
+    return false;
+}
+
+// ------------------------------------------------------------------ configuration
+
+template <int DQK, int DV, bool kE4m3>
+struct TreeCfg {
+    static constexpr bool kTwo = DQK != 192;                    // room for a second query tile
+    static constexpr int kQTiles = kTwo ? 2 : 1;
+    static constexpr int kQChunks = DQK / kChunkCols, kVChunks = DV / kChunkCols;
+    static constexpr int kQBytes = kQChunks * kChunkBytes;      // a query tile; a K tile alike
+    static constexpr int kKBytes = kQBytes, kVBytes = kVChunks * kChunkBytes;
+    // tiles that are multiplied, and over e4m3 caches the codes before them (rows of 128 bytes, whatever the head size)
+    static constexpr int kKStages = kE4m3 ? (DQK == 192 ? 1 : 2) : (DQK == 64 ? 6 : DQK == 128 ? 3 : 2);
+    static constexpr int kVStages = kE4m3 ? (DQK == 64 ? 2 : 1) : (DQK == 64 ? 6 : 2);
+    static constexpr int kRawKChunks = (DQK + 127) / 128;
+    static constexpr int kRawKBytes = kE4m3 ? kRawKChunks * kChunkBytes : 0, kRawVBytes = kE4m3 ? kChunkBytes : 0;
+    static constexpr int kRaw = kE4m3 ? (DQK == 64 ? 4 : 2) : 0;
+    static constexpr int kTileBytes = kQTiles * kQBytes + kKStages * kKBytes + kVStages * kVBytes + kRaw * (kRawKBytes + kRawVBytes);
+    static constexpr int kThreads = kE4m3 ? 512 : 384;
+    // registers per thread: 256 x 216 + 128 x 72 of 384 x 168, or 256 x 184 + 256 x 72 of 512 x 128
+    static constexpr int kRegsSoftmax = kE4m3 ? 184 : 216, kRegsOther = 72;
+    static constexpr float kBias = kE4m3 ? 7.f : 0.f;           // P in fp16: below 2^(8 + 7), 11 bits down to 2^-21
+    static constexpr int kParts = 4;
+};
+
+template <int DQK, int DV, bool kE4m3>
+struct TreeShared {
+    using Cfg = TreeCfg<DQK, DV, kE4m3>;
+    uint64_t q_full, q_ready[2], q_empty;
+    uint64_t k_full[Cfg::kKStages], k_empty[Cfg::kKStages], v_full[Cfg::kVStages], v_empty[Cfg::kVStages];
+    uint64_t raw_full[2][kE4m3 ? Cfg::kRaw : 1], raw_empty[2][kE4m3 ? Cfg::kRaw : 1];      // of K, of V
+    uint64_t v_tail[kE4m3 ? 1 : Cfg::kVStages];       // the rows behind a sequence's last value are zeros
+    uint64_t s_full[2], p_first[2], p_rest[2], o_final[2];
+    uint64_t part_full[Cfg::kParts], part_empty[Cfg::kParts];
+    TreePart part[Cfg::kParts];
+    uint32_t tmem_base, abort_flag;
+    int start_seq, start_base;
+    int v_issued;                 // V tiles whose loads have been issued
+    float stat_m[2][kTileM], stat_l[2][kTileM];       // (of two streams on the same rows; at the start the sums of the list)
+    uint8_t q_shift[kE4m3 ? 2 : 1][kE4m3 ? kTileM : 4];      // 127 - exponent that a row was scaled by
+};
+
+template <int DQK, int DV, bool kE4m3>
+constexpr int tree_smem_bytes() {
+    return TreeCfg<DQK, DV, kE4m3>::kTileBytes + static_cast<int>(sizeof(TreeShared<DQK, DV, kE4m3>));
+}
+// Floats of a partial result: unnormalised O as [tile][column / 4][row][4], then every row's reference (log2 units) and sum.
+__host__ __device__ constexpr int tree_slot_floats(int dv, bool two) { return (two ? 2 : 1) * kTileM * (dv + 2); }
+
+struct TreeArgs {
+    TreeParams t;
+    TreeList list;
+    int group;
+    TreeJoin* join;               // one per CTA
+    float* part;                  // two slots per CTA
+};
+
+__host__ __device__ constexpr uint32_t make_idesc_f16_f32(int m, int n, bool b_mn_major) {
+    return (1u << 4) | ((b_mn_major ? 1u : 0u) << 16) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
+}
+
+namespace ptx {
+
+// Two e4m3 codes (low byte first) -> two fp16, exactly (NaN stays NaN).
+FA_DEVI uint32_t e4m3x2_to_f16x2(uint32_t codes) {
+    uint32_t r;
+    asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %1; cvt.rn.f16x2.e4m3x2 %0, lo; }" : "=r"(r) : "r"(codes));
+    return r;
+}
+FA_DEVI uint32_t pack_f16x2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+}  // namespace ptx
+
+// Bounded wait for a count in shared memory that another warp moves up, as mbar_wait.
+FA_DEVI bool wait_count(const int* count, int least, const ptx::WaitCtx& ctx, uint32_t who) {
+    volatile const int* const c = count;
+    uint64_t t0 = 0;
+    while (*c < least) {
+        __nanosleep(100);
+        if (*ctx.abort_flag) return false;
+        const uint64_t now = ptx::globaltimer_ns();
+        if (t0 == 0) {
+            t0 = now;
+        } else if (now - t0 > ctx.limit_ns) {
+            *ctx.abort_flag = 1u;
+            if (ctx.status) {
+                volatile uint32_t* sw = ctx.status;       // mapped host memory: plain stores
+                sw[1] = who;
+                sw[0] = 4u;                               // FA_ERR_DEVICE_TIMEOUT
+                __threadfence_system();
+            }
+            return false;
+        }
+    }
+    __threadfence_block();
+    return true;
+}
+
+// ------------------------------------------------------------------ softmax pass
+
+// The pass of fa_softmax_pass.cuh with a mask of bits (vis[w] bit e: key 32 w + e of the tile is seen) and, over e4m3 caches, P as fp16 under a
+// bias.  P = 2^(s c + off), off = bias - u c with the reference u; all exponentials on the special-function unit: HBM is the bound here.
+template <int DV, bool kHalf, typename ArriveFirst, typename ArriveRest>
+FA_DEVI void tree_pass(uint32_t tS, uint32_t tO, float c, float tau_raw, float bias, bool masked, const uint32_t (&vis)[4], bool first_tile,
+                       float& m_ref, float& l, int lane, ArriveFirst&& arrive_first, ArriveRest&& arrive_rest) {
+    using namespace ptx;
+    const float2 c2 = make_float2(c, c);
+    float2 off2;
+    float2 sum_a = make_float2(0.f, 0.f), sum_b = make_float2(0.f, 0.f);
+    float alpha = 1.f;
+    uint32_t s[kTileN];
+    auto exp_chunk = [&](int q) {
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) {
+            const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[q * 32 + e]), __uint_as_float(s[q * 32 + e + 1])), c2, off2);
+            s[q * 32 + e] = __float_as_uint(exp2_approx(x.x));
+            s[q * 32 + e + 1] = __float_as_uint(exp2_approx(x.y));
+        }
+    };
+    auto emit_chunk = [&](int q) {
+        uint32_t pk[16];
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) {
+            const float x = __uint_as_float(s[q * 32 + e]), y = __uint_as_float(s[q * 32 + e + 1]);
+            pk[e / 2] = kHalf ? pack_f16x2(x, y) : pack_bf16x2(x, y);
+        }
+        tmem_st_x16(tS + q * 16, pk);
+    };
+    auto sum_chunk = [&](int q) {
+#pragma unroll
+        for (int e = 0; e < 32; e += 4) {
+            sum_a = fadd2_ftz(sum_a, make_float2(__uint_as_float(s[q * 32 + e]), __uint_as_float(s[q * 32 + e + 1])));
+            sum_b = fadd2_ftz(sum_b, make_float2(__uint_as_float(s[q * 32 + e + 2]), __uint_as_float(s[q * 32 + e + 3])));
+        }
+    };
+#pragma unroll 1
+    for (;;) {
+        tmem_ld_x32(tS + 0, s + 0);
+        tmem_ld_x32(tS + 32, s + 32);
+        tmem_ld_x32(tS + 64, s + 64);
+        tmem_ld_x32(tS + 96, s + 96);
+        tc_wait_ld();
+        if (masked) {
+#pragma unroll
+            for (int e = 0; e < kTileN; ++e)
+                if (!(vis[e / 32] & (1u << (e % 32)))) s[e] = 0xff800000u;   // -inf
+        }
+        const float off = m_ref == -INFINITY ? bias : bias - m_ref * c;
+        off2 = make_float2(off, off);
+        float a[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) a[q] = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < kTileN; e += 16) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                a[q] = fmax3(a[q], __uint_as_float(s[e + 2 * q]), __uint_as_float(s[e + 2 * q + 1]));
+        }
+        exp_chunk(0);
+        float mx = fmaxf(fmax3(a[0], a[1], a[2]), fmax3(a[3], a[4], a[5]));
+        mx = fmax3(mx, a[6], a[7]);
+        const bool grow = mx > m_ref + tau_raw;
+        if (!__any_sync(0xffffffffu, grow)) break;
+        if (grow) {
+            alpha = exp2_approx((m_ref - mx) * c);    // 0 on the first tile
+            m_ref = mx;
+        }
+    }
+    if (!first_tile && __any_sync(0xffffffffu, alpha != 1.f)) {
+#pragma unroll 1
+        for (int cc = 0; cc < DV / 32; ++cc) {
+            uint32_t r[32];
+            tmem_ld_x32(tO + cc * 32, r);
+            tc_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+                r[e] = __float_as_uint(__uint_as_float(r[e]) * alpha);
+            tmem_st_x32(tO + cc * 32, reinterpret_cast<uint32_t(&)[32]>(r));
+        }
+    }
+    exp_chunk(1);
+    emit_chunk(0);
+    exp_chunk(2);
+    emit_chunk(1);
+    emit_chunk(2);
+    tc_wait_st();
+    tc_fence_before_sync();
+    __syncwarp();
+    if (lane == 0) arrive_first();
+    exp_chunk(3);
+    emit_chunk(3);
+    tc_wait_st();
+    tc_fence_before_sync();
+    __syncwarp();
+    if (lane == 0) arrive_rest();
+    sum_chunk(0);
+    sum_chunk(1);
+    sum_chunk(2);
+    sum_chunk(3);
+    l = l * alpha + ((sum_a.x + sum_a.y) + (sum_b.x + sum_b.y));
+}
+
+// ------------------------------------------------------------------ kernel
+
+template <int DQK, int DV, bool kE4m3>
+__global__ void __launch_bounds__((TreeCfg<DQK, DV, kE4m3>::kThreads), 1)
+fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+               const PagedParams p, const TreeArgs a) {
+    using Cfg = TreeCfg<DQK, DV, kE4m3>;
+    using Shared = TreeShared<DQK, DV, kE4m3>;
+    using namespace ptx;
+    constexpr int NK = Cfg::kKStages, NV = Cfg::kVStages, NR = kE4m3 ? Cfg::kRaw : 1, NP = Cfg::kParts;
+    constexpr int kWarps = Cfg::kThreads / 32;
+
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    Shared& sh = *reinterpret_cast<Shared*>(smem_raw + Cfg::kTileBytes);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t smem_base = smem_addr(smem_raw);
+    const uint32_t sQ = smem_base, sK = sQ + Cfg::kQTiles * Cfg::kQBytes, sV = sK + NK * Cfg::kKBytes, sRawK = sV + NV * Cfg::kVBytes,
+                   sRawV = sRawK + Cfg::kRaw * Cfg::kRawKBytes;
+
+    grid_launch_dependents();
+    if ((smem_base & 1023u) != 0u) {          // uniform over the CTA; nothing has been set up yet
+        grid_dependency_wait();
+        if (tid == 0) {
+            a.join[blockIdx.x].pieces = 0;
+            if (p.status) {
+                volatile uint32_t* sw = p.status;
+                sw[1] = kSiteSmemAlign;
+                sw[0] = 3u;                   // FA_ERR_CUDA
+                __threadfence_system();
+            }
+        }
+        return;
+    }
+    if (tid == 0) {
+        sh.abort_flag = 0;
+        mbar_init(smem_addr(&sh.q_full), 1);
+        mbar_init(smem_addr(&sh.q_empty), 1);
+        sh.v_issued = 0;
+#pragma unroll
+        for (int s = 0; s < NK; ++s) {
+            mbar_init(smem_addr(&sh.k_full[s]), kE4m3 ? 2 : 1);     // the two warps that convert, or the copy
+            mbar_init(smem_addr(&sh.k_empty[s]), 1);
+        }
+#pragma unroll
+        for (int s = 0; s < NV; ++s) {
+            mbar_init(smem_addr(&sh.v_full[s]), kE4m3 ? 2 : 1);
+            mbar_init(smem_addr(&sh.v_empty[s]), 1);
+            if constexpr (!kE4m3) mbar_init(smem_addr(&sh.v_tail[s]), 1);
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            mbar_init(smem_addr(&sh.q_ready[t]), 4);      // 4 softmax warps
+            mbar_init(smem_addr(&sh.s_full[t]), 1);
+            mbar_init(smem_addr(&sh.p_first[t]), 4);
+            mbar_init(smem_addr(&sh.p_rest[t]), 4);
+            mbar_init(smem_addr(&sh.o_final[t]), 1);
+#pragma unroll
+            for (int s = 0; s < NR; ++s) {
+                mbar_init(smem_addr(&sh.raw_full[t][s]), 1);
+                mbar_init(smem_addr(&sh.raw_empty[t][s]), 2);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            mbar_init(smem_addr(&sh.part_full[i]), 1);
+            mbar_init(smem_addr(&sh.part_empty[i]), 8 + 3 + (kE4m3 ? 4 : 0));      // softmax warps, MMA thread, two loading warps, converting warps
+        }
+        fence_mbar_init();
+        prefetch_tensormap(&tm_q);
+        prefetch_tensormap(&tm_k);
+        prefetch_tensormap(&tm_v);
+    }
+    if (warp == 8) {
+        tmem_alloc(smem_addr(&sh.tmem_base), 512);
+        tmem_relinquish_alloc_permit();
+    }
+    grid_dependency_wait();
+
+    // ------------------------------------------------------------ the list: its length, and where this CTA's share begins
+    auto seq_of = [&](int b, int& n, int& row0, int& len) {
+        const DraftRows d = draft_rows(a.t.cu_seqlens, b, p.B, a.t.total, a.t.max_tokens, nullptr);
+        n = d.count;
+        row0 = d.first;
+        len = clamped_len(p.seq_lens[b], p.max_pages, p.page_size, nullptr);
+    };
+    int total, share;
+    {
+        const int chunk = (p.B + Cfg::kThreads - 1) / Cfg::kThreads, b_first = min(p.B, tid * chunk), b_last = min(p.B, b_first + chunk);
+        int* const sums = reinterpret_cast<int*>(&sh.stat_m[0][0]);
+        int mine = 0;
+#pragma unroll 2
+        for (int b = b_first; b < b_last; ++b) {
+            int n, row0, len;
+            seq_of(b, n, row0, len);
+            mine += p.Hkv * tree_head_units(tree_units(a.list, n, len));
+        }
+        int before = mine;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int o = __shfl_up_sync(0xffffffffu, before, d);
+            if (lane >= d) before += o;
+        }
+        if (lane == 31) sums[warp] = before;
+        before -= mine;
+        tc_fence_before_sync();
+        __syncthreads();
+        tc_fence_after_sync();
+        total = 0;
+#pragma unroll
+        for (int v = 0; v < kWarps; ++v) {
+            const int n = sums[v];
+            if (v < warp) before += n;
+            total += n;
+        }
+        share = tree_share(a.list, total, gridDim.x);
+        const long long at = static_cast<long long>(blockIdx.x) * share;
+        if (at < total && before <= at && at < before + mine) {
+            int b = b_first, base = before;
+            for (;; ++b) {
+                int n, row0, len;
+                seq_of(b, n, row0, len);
+                const int units = p.Hkv * tree_head_units(tree_units(a.list, n, len));
+                if (at < base + units) break;
+                base += units;
+            }
+            sh.start_seq = b;
+            sh.start_base = base;
+        }
+        __syncthreads();
+    }
+    const uint32_t tmem = sh.tmem_base;
+    WaitCtx wctx{&sh.abort_flag, p.status, p.wait_limit_ns};
+    auto wait = [&](uint64_t& bar, uint32_t parity, uint32_t who) -> bool { return mbar_wait(smem_addr(&bar), parity, wctx, who); };
+    // Part k for a warp as a whole; false at the end of the list or after a wait that ran out.
+    auto take_part = [&](int k, TreePart& e) -> bool {
+        if (!__all_sync(0xffffffffu, wait(sh.part_full[k % NP], (k / NP) & 1, kSiteItem))) return false;
+        e = sh.part[k % NP];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_addr(&sh.part_empty[k % NP]));
+        return e.t1 >= 0;
+    };
+
+    if (warp < 8) {
+        // ============================================================ softmax of stream t
+        setmaxnreg_inc<Cfg::kRegsSoftmax>();
+        const int t = warp >> 2, row = tid & (kTileM - 1);
+        const uint32_t lane_sel = static_cast<uint32_t>((warp & 3) * 32) << 16;
+        const uint32_t tS = tmem + 128 * t + lane_sel, tO = tmem + 256 + lane_sel;
+        const uint32_t bar_pf = smem_addr(&sh.p_first[t]), bar_pr = smem_addr(&sh.p_rest[t]);
+        const int row_token = row / a.list.row_heads, row_head = row - row_token * a.list.row_heads;
+        int n_s = 0, n_q = 0, n_final[2] = {0, 0};       // score tiles, parts with queries, parts with a result of stream 0 / 1 so far
+        bool ok = true;
+        // All 256 threads meet at the barriers of a part, also after a wait that ran out (nothing is stored then), and leave together.
+        for (int k = 0;; ++k) {
+            TreePart e;
+            e.t1 = -1;
+            ok = ok && wait(sh.part_full[k % NP], (k / NP) & 1, kSiteItem);
+            if (named_barrier_or(1, 256, !ok)) break;
+            e = sh.part[k % NP];
+            if (e.t1 < 0) break;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_addr(&sh.part_empty[k % NP]));
+            const int nt = e.t1 - e.t0;
+            const bool two = Cfg::kTwo && e.two;
+            const int steps0 = two ? nt : (nt + 1) / 2, steps1 = two ? nt : nt / 2, steps = t == 0 ? steps0 : steps1;
+            // the row: its token and head
+            const int tile = e.row_tile + (two ? t : 0), tc = tile / a.list.head_chunks, hc = tile - tc * a.list.head_chunks;
+            const int token = tc * a.list.row_tokens + row_token, head = hc * a.list.row_heads + row_head;
+            const bool live = row_token < a.list.row_tokens && token < e.n && head < a.group;
+            const bool warp_live = __any_sync(0xffffffffu, live);
+            const int first_draft = e.len - e.n, q_row = e.row0 + (live ? token : 0);
+            if (live && a.t.mask) asm volatile("prefetch.global.L1 [%0];" ::"l"(a.t.mask + q_row * a.t.mask_stride));
+            float c = p.scale_log2;
+            if constexpr (kE4m3) {
+                c *= p.k_scale ? p.k_scale[e.kvh] : 1.f;
+                if (nt > 0) {
+                    // the row's queries as fp16, scaled by a power of two that puts the largest into [2^14, 2^15) (from 2^127 down to
+                    // 2^-112; a smaller row by 2^126, which makes its entries, multiples of 2^-133, exact too)
+                    if (two || t == 0) {
+                        ok = ok && wait(sh.q_full, n_q & 1, kSiteMmaQFull);
+                        __syncwarp();
+                        const uint32_t base = sQ + (two ? t : 0) * Cfg::kQBytes + row * 128;
+                        uint32_t top = 0;
+#pragma unroll 4
+                        for (int v = 0; v < DQK / 8; ++v) {
+                            const uint4 x = ld_shared_v4(base + (v >> 3) * kChunkBytes + (((v & 7) ^ (row & 7)) << 4));
+                            const uint32_t w4[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) top = max(top, max((w4[i] & 0x7fffu) << 16, w4[i] & 0x7fff0000u));
+                        }
+                        int sft = top ? 14 - (static_cast<int>(top >> 23) - 127) : 0;
+                        sft = sft > 126 ? 126 : (sft < -113 ? -113 : sft);
+                        const float mult = __uint_as_float(static_cast<uint32_t>(sft + 127) << 23);
+#pragma unroll 4
+                        for (int v = 0; v < DQK / 8; ++v) {
+                            const uint32_t at = base + (v >> 3) * kChunkBytes + (((v & 7) ^ (row & 7)) << 4);
+                            const uint4 x = ld_shared_v4(at);
+                            const uint32_t w4[4] = {x.x, x.y, x.z, x.w};
+                            uint32_t h[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) h[i] = pack_f16x2(__uint_as_float(w4[i] << 16) * mult, __uint_as_float(w4[i] & 0xffff0000u) * mult);
+                            st_shared_v4(at, h[0], h[1], h[2], h[3]);
+                        }
+                        sh.q_shift[two ? t : 0][row] = static_cast<uint8_t>(127 - sft);
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_addr(&sh.q_ready[t]));
+                    } else if (lane == 0) {
+                        mbar_arrive(smem_addr(&sh.q_ready[1]));       // (keeps the barrier's phases in step with the parts)
+                    }
+                    ++n_q;
+                }
+            }
+            float m_ref = -INFINITY, l = 0.f, tau_raw = kRescaleThresholdLog2 / c;
+            for (int j = 0; j < steps; ++j, ++n_s) {
+                ok = __all_sync(0xffffffffu, ok && wait(sh.s_full[t], n_s & 1, kSiteSoftmaxSFull));
+                if (!ok) break;
+                tc_fence_after_sync();
+                if constexpr (kE4m3) {
+                    if (j == 0) {
+                        c *= __uint_as_float(static_cast<uint32_t>(sh.q_shift[two ? t : 0][row]) << 23);
+                        tau_raw = kRescaleThresholdLog2 / c;
+                    }
+                }
+                if (!warp_live) {            // (what P holds then meets rows that are not stored)
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(bar_pf);
+                        mbar_arrive(bar_pr);
+                    }
+                    continue;
+                }
+                const int key0 = (e.t0 + (two ? j : 2 * j + t)) * kTileN;
+                const bool masked = key0 + kTileN > first_draft;
+                uint32_t vis[4];
+                if (masked) {
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const int j0 = key0 + 32 * w - first_draft;          // the draft of this word's first key
+                        auto word = [&](int i) { return draft_word(a.t, q_row, token, e.n, i); };
+                        if (j0 <= -32) vis[w] = 0xffffffffu;
+                        else if (j0 < 0) vis[w] = (word(0) << -j0) | ((1u << -j0) - 1u);
+                        else vis[w] = __funnelshift_r(word(j0 >> 5), word((j0 >> 5) + 1), j0 & 31);
+                    }
+                }
+                tree_pass<DV, kE4m3>(tS, tO + 128 * t, c, tau_raw, Cfg::kBias, masked, vis, j == 0, m_ref, l, lane,
+                                     [&]() { mbar_arrive(bar_pf); }, [&]() { mbar_arrive(bar_pr); });
+            }
+            // ---- the part's result: sum and reference of a row that saw a key, O of one stream or of both
+            const float off = m_ref == -INFINITY ? Cfg::kBias : Cfg::kBias - m_ref * c;
+            float m = l > 0.f || l != l ? -off : -INFINITY;       // (a NaN goes through)
+            const bool whole = e.slot < 0;
+            const float vs = kE4m3 && p.v_scale ? p.v_scale[e.kvh] : 1.f;
+            float f0 = 1.f, f1 = 0.f;
+            if (!two) {
+                sh.stat_m[t][row] = m;
+                sh.stat_l[t][row] = l;
+                named_barrier_sync(1, 256);
+                const float m0 = sh.stat_m[0][row], m1 = sh.stat_m[1][row];
+                m = fmaxf(m0, m1);
+                f0 = m0 == -INFINITY ? 0.f : exp2_approx(m0 - m);
+                f1 = m1 == -INFINITY ? 0.f : exp2_approx(m1 - m);
+                l = f0 * sh.stat_l[0][row] + f1 * sh.stat_l[1][row];
+            }
+            const bool any = l > 0.f || l != l;
+            const float norm = whole ? (any ? vs / l : 0.f) : 1.f;
+            f0 *= norm;
+            f1 *= norm;
+            if (steps0 > 0 && (!two || t == 0)) ok = ok && wait(sh.o_final[0], n_final[0] & 1, kSiteEpiOFull);
+            if (steps1 > 0 && (!two || t == 1)) ok = ok && wait(sh.o_final[1], n_final[1] & 1, kSiteEpiOFull);
+            n_final[0] += steps0 > 0;
+            n_final[1] += steps1 > 0;
+            ok = __all_sync(0xffffffffu, ok);
+            tc_fence_after_sync();
+            // columns [col0, col1) are this thread's: all of its own stream's, or half of both streams'
+            const int col0 = two ? 0 : t * (DV / 2), col1 = two ? DV : col0 + DV / 2;
+            const int hq = e.kvh * a.group + head;
+            __nv_bfloat16* const out = p.O + q_row * p.o_st + hq * p.o_sh;
+            float* const slot = a.part + static_cast<long long>(whole ? 0 : e.slot) * tree_slot_floats(DV, Cfg::kTwo);
+            float4* const slot_o = reinterpret_cast<float4*>(slot) + (two ? t : 0) * (DV / 4) * kTileM + row;
+#pragma unroll 1
+            for (int col = col0; col < col1; col += 32) {
+                float y[32];
+                if (nt > 0 && ok) {
+                    uint32_t r0[32];
+                    tmem_ld_x32(tO + (two ? 128 * t : 0) + col, r0);
+                    if (!two && steps1 > 0) {
+                        uint32_t r1[32];
+                        tmem_ld_x32(tO + 128 + col, r1);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) y[i] = f0 * __uint_as_float(r0[i]) + f1 * __uint_as_float(r1[i]);
+                    } else {
+                        tc_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) y[i] = f0 * __uint_as_float(r0[i]);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) y[i] = 0.f;
+                }
+                if (ok && live) {
+                    if (whole) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8) {
+                            uint4 v = make_uint4(pack_bf16x2(y[i], y[i + 1]), pack_bf16x2(y[i + 2], y[i + 3]), pack_bf16x2(y[i + 4], y[i + 5]),
+                                                 pack_bf16x2(y[i + 6], y[i + 7]));
+                            // (nothing seen: zeros, whatever the products of zero probabilities gave)
+                            if (!any) v = make_uint4(0, 0, 0, 0);
+                            *reinterpret_cast<uint4*>(out + col + i) = v;
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4) slot_o[(col + i) / 4 * kTileM] = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
+                    }
+                }
+            }
+            if (ok && live && (two || t == 0)) {
+                if (whole) {
+                    if (p.lse) p.lse[static_cast<long long>(hq) * a.t.total + q_row] = any ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+                } else {
+                    float* const ml = slot + (Cfg::kTwo ? 2 : 1) * kTileM * DV + (two ? t : 0) * 2 * kTileM + row;
+                    ml[0] = m;
+                    ml[kTileM] = l;
+                }
+            }
+            // (both groups have read both accumulators, and each other's sums, at the barrier that the next part begins with)
+            tc_fence_before_sync();
+        }
+    } else if (warp == 8) {
+        // ============================================================ MMA issue, one thread for both streams
+        setmaxnreg_dec<Cfg::kRegsOther>();
+        if (elect_one()) {
+            constexpr uint32_t kIdescQK = kE4m3 ? make_idesc_f16_f32(kTileM, kTileN, false) : make_idesc_bf16_f32(kTileM, kTileN, false, false);
+            constexpr uint32_t kIdescPV = kE4m3 ? make_idesc_f16_f32(kTileM, DV, true) : make_idesc_bf16_f32(kTileM, DV, false, true);
+            constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);   // sbo, version, swizzle
+            constexpr int kSteps = DQK / 16;
+            const uint32_t q_lo0 = ((sQ & 0x3FFFFu) >> 4) | (1u << 16);
+            const uint32_t k_lo0 = ((sK & 0x3FFFFu) >> 4) | (1u << 16);
+            const uint32_t v_lo0 = ((sV & 0x3FFFFu) >> 4) | ((static_cast<uint32_t>(kChunkBytes) >> 4) << 16);
+            auto desc = [](uint32_t lo) -> uint64_t { return (static_cast<uint64_t>(kDescHi) << 32) | lo; };
+            auto koff = [](int ks) -> uint32_t { return static_cast<uint32_t>(((ks / 4) * kChunkBytes + (ks % 4) * 32) >> 4); };
+            int sk = 0, sv = 0, n_p[2] = {0, 0}, n_q = 0;       // stages, steps of each stream, parts with queries so far
+            uint32_t ph_k = 0, ph_v = 0, ph_tail = 0;                       // (of the last tiles, a bit per stage)
+            bool two = false, tail = false;
+            int nt = 0, k_tile = 0, v_tile = 0;                             // of the part: tiles, tile that stage sk / sv holds
+            uint32_t pre_p = 0, pre_v = 0, pre_k = 0;                       // probes that succeeded for the next block
+            auto step_k = [&]() { ++k_tile; if (++sk == NK) { sk = 0; ph_k ^= 1u; } };
+            auto step_v = [&]() { ++v_tile; if (++sv == NV) { sv = 0; ph_v ^= 1u; } };
+            auto q_lo = [&](int t) -> uint32_t { return q_lo0 + (two ? t : 0) * (Cfg::kQBytes >> 4); };
+            // Behind the score products of stream t with the K tile in stage sk: who may go on.
+            auto scores_done = [&](int t) {
+                tc_commit(smem_addr(&sh.s_full[t]));
+                if (!two || t == 1) {
+                    tc_commit(smem_addr(&sh.k_empty[sk]));
+                    if (k_tile == nt - 1) tc_commit(smem_addr(&sh.q_empty));
+                    step_k();
+                }
+            };
+            // Stream t's block of step j: P_t V, then the next scores.  Barriers that the next block needs are probed from inside it.
+            auto block = [&](auto tc, int j, int steps) -> bool {
+                constexpr int t = decltype(tc)::value;
+                const bool fresh = !two || t == 0;                   // (the streams of two row tiles share the K/V tiles)
+                const bool next = j + 1 < steps;
+                if (fresh) {
+                    if (!pre_v && !wait(sh.v_full[sv], ph_v, kSiteMmaKvFull)) return false;
+                    if constexpr (!kE4m3) {
+                        if (tail && v_tile == nt - 1) {
+                            if (!wait(sh.v_tail[sv], (ph_tail >> sv) & 1u, kSiteMmaTail)) return false;
+                            ph_tail ^= 1u << sv;
+                        }
+                    }
+                    if (next && !pre_k && !wait(sh.k_full[sk], ph_k, kSiteMmaKvFull)) return false;
+                }
+                const uint32_t parity = n_p[t] & 1;
+                const uint32_t tS = tmem + 128 * t, tO = tmem + 256 + 128 * t;
+                const uint32_t vlo = v_lo0 + sv * (Cfg::kVBytes >> 4), klo = k_lo0 + sk * (Cfg::kKBytes >> 4);
+                if (!pre_p && !wait(sh.p_first[t], parity, kSiteMmaPFull)) return false;
+                pre_p = pre_v = pre_k = 0u;
+                tc_fence_after_sync();
+                mma_ts(tO, tS + 0, desc(vlo + 0 * (2048 >> 4)), kIdescPV, j > 0 ? 1u : 0u);
+                mma_ts(tO, tS + 8, desc(vlo + 1 * (2048 >> 4)), kIdescPV, 1u);
+                mma_ts(tO, tS + 16, desc(vlo + 2 * (2048 >> 4)), kIdescPV, 1u);
+                mma_ts(tO, tS + 24, desc(vlo + 3 * (2048 >> 4)), kIdescPV, 1u);
+                const uint32_t rest = probe_mma_ts2(smem_addr(&sh.p_rest[t]), parity, tO, tS + 32, desc(vlo + 4 * (2048 >> 4)),
+                                                    tS + 40, desc(vlo + 5 * (2048 >> 4)), kIdescPV);
+                if (!rest && !wait(sh.p_rest[t], parity, kSiteMmaPFull)) return false;
+                tc_fence_after_sync();
+                mma_ts(tO, tS + 48, desc(vlo + 6 * (2048 >> 4)), kIdescPV, 1u);
+                mma_ts(tO, tS + 56, desc(vlo + 7 * (2048 >> 4)), kIdescPV, 1u);
+                ++n_p[t];
+                if (next) {
+                    // (the next block's: the other stream's probabilities; its V and K tile where they are not this block's)
+                    const bool same = two && t == 0;
+                    const int sv_n = sv + 1 == NV ? 0 : sv + 1, sk_n = sk + 1 == NK ? 0 : sk + 1;
+                    const uint32_t ph_v_n = sv + 1 == NV ? ph_v ^ 1u : ph_v, ph_k_n = sk + 1 == NK ? ph_k ^ 1u : ph_k;
+                    mma_ss(tS, desc(q_lo(t) + koff(0)), desc(klo + koff(0)), kIdescQK, 0u);
+                    const uint32_t got = probe3_mma_ss3(smem_addr(&sh.p_first[1 - t]), n_p[1 - t] & 1, smem_addr(&sh.v_full[same ? sv : sv_n]), same ? ph_v : ph_v_n,
+                                                        smem_addr(&sh.k_full[same ? sk : sk_n]), same ? ph_k : ph_k_n, tS,
+                                                        desc(q_lo(t) + koff(1)), desc(klo + koff(1)), desc(q_lo(t) + koff(2)), desc(klo + koff(2)),
+                                                        desc(q_lo(t) + koff(3)), desc(klo + koff(3)), kIdescQK);
+#pragma unroll
+                    for (int ks = 4; ks < kSteps; ++ks) mma_ss(tS, desc(q_lo(t) + koff(ks)), desc(klo + koff(ks)), kIdescQK, 1u);
+                    pre_p = got & 1u;
+                    pre_v = (got >> 1) & 1u;
+                    pre_k = (got >> 2) & 1u;
+                    scores_done(t);
+                } else {
+                    tc_commit(smem_addr(&sh.o_final[t]));
+                }
+                if (!two || t == 1) {
+                    tc_commit(smem_addr(&sh.v_empty[sv]));
+                    step_v();
+                }
+                return true;
+            };
+            bool ok = true;
+            for (int k = 0; ok; ++k) {
+                ok = wait(sh.part_full[k % NP], (k / NP) & 1, kSiteItem);
+                if (!ok) break;
+                const TreePart e = sh.part[k % NP];
+                mbar_arrive(smem_addr(&sh.part_empty[k % NP]));
+                if (e.t1 < 0) break;
+                nt = e.t1 - e.t0;
+                if (nt == 0) continue;
+                two = Cfg::kTwo && e.two;
+                tail = !kE4m3 && e.t1 * kTileN > e.len;
+                k_tile = v_tile = 0;
+                pre_p = pre_v = pre_k = 0u;
+                const int steps0 = two ? nt : (nt + 1) / 2, steps1 = two ? nt : nt / 2;
+                if constexpr (kE4m3) ok = wait(sh.q_ready[0], n_q & 1, kSiteMmaQFull) && wait(sh.q_ready[1], n_q & 1, kSiteMmaQFull);
+                else ok = wait(sh.q_full, n_q & 1, kSiteMmaQFull);
+                ++n_q;
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    if (!ok || (t == 1 && steps1 == 0)) break;
+                    if (t == 0 || !two) ok = wait(sh.k_full[sk], ph_k, kSiteMmaKvFull);
+                    if (!ok) break;
+                    tc_fence_after_sync();
+                    const uint32_t klo = k_lo0 + sk * (Cfg::kKBytes >> 4);
+#pragma unroll
+                    for (int ks = 0; ks < kSteps; ++ks) mma_ss(tmem + 128 * t, desc(q_lo(t) + koff(ks)), desc(klo + koff(ks)), kIdescQK, ks > 0 ? 1u : 0u);
+                    scores_done(t);
+                }
+                for (int j = 0; j < steps0 && ok; ++j) {
+                    ok = block(IntC<0>{}, j, steps0);
+                    if (ok && j < steps1) ok = block(IntC<1>{}, j, steps1);
+                }
+            }
+        }
+    } else if (warp == 9 || warp == 10) {
+        // ============================================================ TMA loads of Q and K (warp 9), or of V (warp 10)
+        setmaxnreg_dec<Cfg::kRegsOther>();
+        const bool is_v = warp == 10;
+        constexpr int NL = kE4m3 ? NR : (NK > NV ? NK : NV);
+        (void)NL;
+        constexpr int kKC = kE4m3 ? Cfg::kRawKChunks : Cfg::kQChunks, kVC = kE4m3 ? 1 : Cfg::kVChunks, kMaxChunks = kKC > kVC ? kKC : kVC;
+        constexpr int kChunk = kE4m3 ? 128 : kChunkCols;             // columns of a 128-byte row
+        const int chunks = is_v ? kVC : kKC, stages = kE4m3 ? NR : (is_v ? NV : NK);
+        const int stage_bytes = kE4m3 ? (is_v ? Cfg::kRawVBytes : Cfg::kRawKBytes) : (is_v ? Cfg::kVBytes : Cfg::kKBytes);
+        const CUtensorMap* tm = is_v ? &tm_v : &tm_k;
+        uint64_t* const full = kE4m3 ? sh.raw_full[is_v] : (is_v ? sh.v_full : sh.k_full);
+        uint64_t* const empty = kE4m3 ? sh.raw_empty[is_v] : (is_v ? sh.v_empty : sh.k_empty);
+        const uint32_t dst0 = kE4m3 ? (is_v ? sRawV : sRawK) : (is_v ? sV : sK);
+        const int box = p.box_rows, shift = __ffs(kTileN / box) - 1, boxes = 1 << shift, tiles_ahead = 32 >> shift;
+        int n = 0, n_q = 0, s = 0;
+        uint32_t parity = 1;
+        bool ok = true;
+        TreePart e;
+        for (int k = 0; ok && take_part(k, e); ++k) {
+            if (e.t0 == e.t1) continue;
+            if (!is_v) {
+                const bool two = Cfg::kTwo && e.two;
+                ok = __all_sync(0xffffffffu, wait(sh.q_empty, (n_q & 1) ^ 1, kSiteLoadQEmpty));
+                if (!ok) break;
+                ++n_q;
+                if (lane == 0) {
+                    const uint32_t bar = smem_addr(&sh.q_full);
+                    mbar_arrive_expect_tx(bar, (two ? 2 : 1) * Cfg::kQChunks * a.list.row_tokens * a.list.row_heads * 128);
+                    for (int t = 0; t < (two ? 2 : 1); ++t) {
+                        const int tile = e.row_tile + t, tc = tile / a.list.head_chunks, hc = tile - tc * a.list.head_chunks;
+#pragma unroll
+                        for (int cc = 0; cc < Cfg::kQChunks; ++cc)
+                            tma_load_4d(sQ + t * Cfg::kQBytes + cc * kChunkBytes, &tm_q, bar, cc * kChunkCols, e.kvh * a.group + hc * a.list.row_heads,
+                                        e.row0 + tc * a.list.row_tokens, 0);
+                    }
+                }
+                __syncwarp();
+            }
+            const int* const table = p.block_table + e.b * p.table_stride;
+            int pages = 0, slots = 0;         // of tile `first` + lane / boxes, box lane % boxes
+            int first = e.t0;
+            for (int t = e.t0; t < e.t1; ++t, ++n) {
+                if (t == e.t0 || t - first == tiles_ahead) {
+                    first = t;
+                    const int tile = t + (lane >> shift), key = tile * kTileN + (lane & (boxes - 1)) * box;
+                    if (tile < e.t1 && key < e.len) {
+                        const int at = key / p.page_size;
+                        slots = key - at * p.page_size;
+                        pages = table[at];
+                        if (pages < 0 || pages >= p.num_pages) {
+                            report_bad_input(p.status, kSiteBadPage);
+                            pages = p.num_pages;       // behind the pool: reads as zeros
+                        }
+                    }
+                }
+                const int from = ((t - first) << shift) + lane;
+                const int page = __shfl_sync(0xffffffffu, pages, from & 31), slot = __shfl_sync(0xffffffffu, slots, from & 31);
+                ok = __all_sync(0xffffffffu, wait(empty[s], parity, kSiteLoadKvEmpty));
+                if (!ok) break;
+                const uint32_t bar = smem_addr(&full[s]);
+                const int n_box = min(boxes, (e.len - t * kTileN + box - 1) / box);
+                if (!(is_v && p.debug_drop_v_load && n == 0)) {
+                    if (lane == 0) mbar_arrive_expect_tx(bar, n_box * box * 128 * chunks);
+                    __syncwarp();
+                    if (lane < n_box) {
+#pragma unroll
+                        for (int cc = 0; cc < kMaxChunks; ++cc)
+                            if (cc < chunks) tma_load_4d(dst0 + s * stage_bytes + cc * kChunkBytes + lane * box * 128, tm, bar, cc * kChunk, slot, e.kvh, page);
+                    }
+                    __syncwarp();
+                }
+                if (!kE4m3 && is_v && lane == 0) {
+                    __threadfence_block();
+                    *static_cast<volatile int*>(&sh.v_issued) = n + 1;
+                }
+                if (++s == stages) { s = 0; parity ^= 1u; }
+            }
+        }
+    } else if (warp == 11) {
+        // ============================================================ the list of parts; zeros behind the last value of a sequence
+        setmaxnreg_dec<Cfg::kRegsOther>();
+        TreeWalk w;
+        tree_walk_begin(w, a.list, blockIdx.x, share, total, sh.start_seq, sh.start_base, seq_of);
+        TreeJoin join{0, 0, 0, 0, 0, 0, 0, 0};
+        TreePart cur, e;
+        bool ok = true;
+        auto publish = [&](int k) {
+            if (!tree_walk_next(w, a.list, p.Hkv, p.B, seq_of, e)) e.t1 = -1;
+            ok = __all_sync(0xffffffffu, ok && wait(sh.part_empty[k % NP], ((k / NP) & 1) ^ 1, kSiteItem));
+            if (!ok) return;
+            if (e.t1 >= 0 && e.slot >= 0 && e.t0 == 0) join = TreeJoin{e.kvh, e.row_tile, e.two, e.n, e.row0, e.pieces, 0, 0};
+            if (lane == 0) {
+                sh.part[k % NP] = e;
+                mbar_arrive(smem_addr(&sh.part_full[k % NP]));
+            }
+            __syncwarp();
+        };
+        // (contents that the other reads of the list clamp are reported here, by the CTAs whose share a sequence begins in)
+        if (blockIdx.x == 0) {
+            for (int b = lane; b < p.B; b += 32) {
+                draft_rows(a.t.cu_seqlens, b, p.B, a.t.total, a.t.max_tokens, p.status);
+                clamped_len(p.seq_lens[b], p.max_pages, p.page_size, p.status);
+            }
+            __syncwarp();
+        }
+        publish(0);
+        for (int k = 0; ok && e.t1 >= 0; ++k) {
+            cur = e;
+            publish(k + 1);
+            if (!ok) break;
+            // the part's last tile holds the sequence's last key: V rows behind it hold whatever the page held, or were not loaded,
+            // and 0 * NaN is NaN
+            if (!kE4m3 && cur.t1 > cur.t0 && cur.t1 * kTileN > cur.len) {
+                const int at = cur.tile0 + cur.t1 - cur.t0 - 1, s = at % NV;
+                // (The list runs ahead of the loads, by more than a turn of the ring where parts are short: a phase of v_full says that it
+                // is this tile's only once its load has been issued.  From there on the stage waits for the zeros.)
+                ok = __all_sync(0xffffffffu, wait_count(&sh.v_issued, at + 1, wctx, kSiteTailIssued) && wait(sh.v_full[s], (at / NV) & 1, kSiteTailVFull));
+                if (!ok) break;
+                const int keys = cur.len - (cur.t1 - 1) * kTileN;
+                for (int i = lane; i < (kTileN - keys) * 8; i += 32) {
+                    const uint32_t to = sV + s * Cfg::kVBytes + (keys + (i >> 3)) * 128 + (i & 7) * 16;
+#pragma unroll
+                    for (int cc = 0; cc < Cfg::kVChunks; ++cc) st_shared_v4(to + cc * kChunkBytes, 0, 0, 0, 0);
+                }
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_addr(&sh.v_tail[kE4m3 ? 0 : s]));
+            }
+        }
+        // (after a wait that ran out the pieces are not joined; the results are invalid either way)
+        if (lane == 0) {
+            if (!ok) join.pieces = 0;
+            a.join[blockIdx.x] = join;
+        }
+        __syncwarp();
+    } else {
+        // ============================================================ e4m3 codes of K (warps 12, 13) or V (14, 15) into fp16
+        setmaxnreg_dec<Cfg::kRegsOther>();
+        if constexpr (kE4m3) {
+            const bool is_v = warp >= 14;
+            const int half = tid & 63, stages = is_v ? NV : NK;
+            constexpr int kKPieces = DQK / 16, kVPieces = DV / 16;       // 16-byte pieces of a row of codes
+            uint64_t* const full = is_v ? sh.v_full : sh.k_full;
+            uint64_t* const empty = is_v ? sh.v_empty : sh.k_empty;
+            int s = 0, r = 0;
+            uint32_t ph = 1, ph_r = 0;
+            bool ok = true;
+            TreePart e;
+            for (int k = 0; ok && take_part(k, e); ++k) {
+                for (int t = e.t0; t < e.t1; ++t) {
+                    ok = wait(sh.raw_full[is_v][r], ph_r, kSiteLoadKvEmpty) && wait(empty[s], ph, kSiteLoadKvEmpty);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    const uint32_t src = is_v ? sRawV + r * Cfg::kRawVBytes : sRawK + r * Cfg::kRawKBytes;
+                    const uint32_t dst = is_v ? sV + s * Cfg::kVBytes : sK + s * Cfg::kKBytes;
+                    const int keys = e.len - t * kTileN;
+                    auto convert = [&](auto pieces_c) {
+                        constexpr int kPieces = decltype(pieces_c)::value;
+#pragma unroll 4
+                        for (int i = half; i < kTileN * kPieces; i += 64) {
+                            const int row = i / kPieces, q = i - row * kPieces;
+                            const uint4 x = ld_shared_v4(src + (q >> 3) * kChunkBytes + row * 128 + (((q & 7) ^ (row & 7)) << 4));
+                            const uint32_t w4[4] = {x.x, x.y, x.z, x.w};
+                            uint32_t h[8];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                h[2 * j] = e4m3x2_to_f16x2(w4[j]);
+                                h[2 * j + 1] = e4m3x2_to_f16x2(w4[j] >> 16);
+                            }
+                            // (values behind the sequence's end hold whatever the page held: 0 * NaN is NaN)
+                            if (is_v && row >= keys) {
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) h[j] = 0u;
+                            }
+                            // the two 16-byte pieces of fp16, in an order in which eight neighbouring lanes meet all banks
+                            const uint32_t to = dst + (q >> 2) * kChunkBytes + row * 128;
+                            const int p0 = 2 * (q & 3), odd = (q >> 2) & 1;
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
+                                const int which = j ^ odd;
+                                st_shared_v4(to + (((p0 + which) ^ (row & 7)) << 4), which ? h[4] : h[0], which ? h[5] : h[1], which ? h[6] : h[2],
+                                             which ? h[7] : h[3]);
+                            }
+                        }
+                    };
+                    if (is_v) convert(IntC<kVPieces>{}); else convert(IntC<kKPieces>{});
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(smem_addr(&full[s]));
+                        mbar_arrive(smem_addr(&sh.raw_empty[is_v][r]));
+                    }
+                    if (++s == stages) { s = 0; ph ^= 1u; }
+                    if (++r == NR) { r = 0; ph_r ^= 1u; }
+                }
+            }
+        }
+    }
+
+    // ---------------------------------------------------------------- teardown (all warps)
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 8) tmem_dealloc(tmem, 512);
+}
+
+// ------------------------------------------------------------------ joining
+
+// The pieces of a row block that several CTAs share, in their order: O = sum_c 2^(m_c - m) O_c / sum_c 2^(m_c - m) l_c.  32 rows a CTA (a
+// lane each), 16 columns a warp, so that loads are 512 neighbouring bytes and a thread stores 32.  Bound by the pieces' bytes, which
+// are in L2.
+template <int DV, bool kTwo>
+__global__ void __launch_bounds__(DV * 2)
+fa_tree_join_kernel(const PagedParams p, const TreeArgs a) {
+    constexpr int kRowBlocks = kTileM / 32;
+    ptx::grid_launch_dependents();
+    ptx::grid_dependency_wait();
+    const int cta = blockIdx.x / (kRowBlocks * (kTwo ? 2 : 1)), at = blockIdx.x - cta * (kRowBlocks * (kTwo ? 2 : 1));
+    const TreeJoin e = a.join[cta];
+    const int t = at / kRowBlocks, row = (at - t * kRowBlocks) * 32 + (threadIdx.x & 31);
+    if (e.pieces == 0 || (t == 1 && !e.two)) return;
+    const int tile = e.row_tile + t, tc = tile / a.list.head_chunks, hc = tile - tc * a.list.head_chunks;
+    const int in = row / a.list.row_heads, token = tc * a.list.row_tokens + in, head = hc * a.list.row_heads + row - in * a.list.row_heads;
+    if (in >= a.list.row_tokens || token >= e.n || head >= a.group) return;
+    auto slot = [&](int c) { return a.part + (c == 0 ? 2ll * cta + 1 : 2ll * (cta + c)) * tree_slot_floats(DV, kTwo); };
+    constexpr int kMl = (kTwo ? 2 : 1) * kTileM * DV;
+    float m = -INFINITY;
+#pragma unroll 4
+    for (int c = 0; c < e.pieces; ++c) m = fmaxf(m, __ldcg(slot(c) + kMl + t * 2 * kTileM + row));
+    const int col = (threadIdx.x >> 5) * 16;
+    float4 y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    float l = 0.f;
+#pragma unroll 2
+    for (int c = 0; c < e.pieces; ++c) {
+        const float* const s = slot(c);
+        const float mc = __ldcg(s + kMl + t * 2 * kTileM + row), lc = __ldcg(s + kMl + (t * 2 + 1) * kTileM + row);
+        const float4* const o = reinterpret_cast<const float4*>(s) + (t * (DV / 4) + col / 4) * kTileM + row;
+        const float f = mc == -INFINITY ? 0.f : ptx::exp2_approx(mc - m);
+        l = fmaf(f, lc, l);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float4 x = __ldcg(o + i * kTileM);
+            y[i].x = fmaf(f, x.x, y[i].x);
+            y[i].y = fmaf(f, x.y, y[i].y);
+            y[i].z = fmaf(f, x.z, y[i].z);
+            y[i].w = fmaf(f, x.w, y[i].w);
+        }
+    }
+    const bool any = l > 0.f || l != l;
+    const int hq = e.kvh * a.group + head;
+    const long long q_row = e.row0 + token;
+    const float f = (p.v_scale ? p.v_scale[e.kvh] : 1.f) / l;
+    uint32_t r[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        r[2 * i] = any ? ptx::pack_bf16x2(f * y[i].x, f * y[i].y) : 0u;
+        r[2 * i + 1] = any ? ptx::pack_bf16x2(f * y[i].z, f * y[i].w) : 0u;
+    }
+    uint4* const out = reinterpret_cast<uint4*>(p.O + q_row * p.o_st + hq * p.o_sh + col);
+    out[0] = make_uint4(r[0], r[1], r[2], r[3]);
+    out[1] = make_uint4(r[4], r[5], r[6], r[7]);
+    if (threadIdx.x < 32 && p.lse) p.lse[static_cast<long long>(hq) * a.t.total + q_row] = any ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+}
+
+}  // namespace fa

@@ -293,18 +293,22 @@ def test_contents_the_device_refuses(handle):
     cache = b.PagedCache(k, v)
     good, lse = b.forward_paged_tree(handle, q, cache, table, lens_t, None)
     ok(handle)
+    O, L, A = tree_reference(q, k, v, None, None, table, [40, 300], [0, 6, 12], [torch.ones(6, 6).tril() > 0] * 2, 0.125)
+    # (other lengths deal the work out otherwise: the same values, within their rounding)
+    holds = lambda o: assert_attention(o[6:], None, O[6:], L[:, 6:], A[6:]) <= 1  # noqa: E731
+    assert assert_attention(good, lse, O, L, A) <= 1
     for page in (-1, k.shape[0], 2 ** 31 - 1, -2 ** 31):
         bad = table.clone()
         bad[0, 1] = page
         o, _ = b.forward_paged_tree(handle, q, cache, bad, lens_t, None)
         torch.cuda.synchronize()
-        assert b.fa_last_status(handle) == (b.FA_ERR_INVALID_ARG, 0x0902) and torch.equal(o[6:], good[6:])
+        assert b.fa_last_status(handle) == (b.FA_ERR_INVALID_ARG, 0x0902) and holds(o)
     for n in (-1, -2 ** 31, 16 * table.shape[1] + 1, 2 ** 31 - 1):
         bad = lens_t.clone()
         bad[0] = n
         o, _ = b.forward_paged_tree(handle, q, cache, table.clamp(0, k.shape[0] - 1), bad, None)
         torch.cuda.synchronize()
-        assert b.fa_last_status(handle) == (b.FA_ERR_INVALID_ARG, 0x0901) and torch.equal(o[6:], good[6:])
+        assert b.fa_last_status(handle) == (b.FA_ERR_INVALID_ARG, 0x0901) and holds(o)
     # (the second sequence keeps its rows 6 to 11 in each)
     for cu, most in (([-3, 6, 12], 10), ([7, 6, 12], 10), ([0, 6, 13], 10), ([0, 6, 2 ** 31 - 1], 10), ([-2 ** 31, 6, 12], 10), ([0, 6, 12], 5)):
         out = torch.full_like(good, 7)
@@ -312,7 +316,7 @@ def test_contents_the_device_refuses(handle):
         torch.cuda.synchronize()
         assert b.fa_last_status(handle) == (b.FA_ERR_INVALID_ARG, 0x0904)
         whole = cu[2] == 12 and most == 10
-        assert torch.equal(out[6:], good[6:]) if whole else (out[6:] == 7).all()
+        assert holds(out) if whole else (out[6:] == 7).all()
     assert b.fa_last_status(handle) == (b.FA_OK, 0)
 
 
