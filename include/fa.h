@@ -624,9 +624,9 @@ fa_status fa_tree_layout(fa_handle* h, const int32_t* parents, const int32_t* cu
  * looked at; mask NULL: the drafts up to itself, a causal chain of any number of tokens).  A token that sees no key gets O = 0 and
  * lse = -inf.  Q [total, Hq, dqk], O [total, Hq, dv], lse [Hq, total] and everything else as for fa_forward_paged; the values (V) of the
  * drafts have to be finite, their keys where no token sees them need not be.  A key that is no number makes the rows that see it NaN.
- * Scores, softmax state and accumulators are fp32.  Over a bf16 cache the probabilities enter the second product as bf16.  Over an e4m3
- * cache both products are fp16 ones: the codes as they are, the queries scaled by a power of two per row (exact for entries of 2^-29 of
- * their row's largest and more), the probabilities with 11 significant bits down to 2^-21 of the row's reference.
+ * Scores, softmax state and accumulators are fp32.  Over a bf16 cache the probabilities enter the second product as bf16, over an e4m3
+ * cache as fp16 (11 significant bits down to 2^-21 of the row's reference), and the queries as a sum of three 8-bit terms (exact for
+ * entries of 2^-23 of their row's largest and more, to 2^-30 of it below).
  * Two launches: the K/V tiles of all sequences are dealt out evenly over the SMs, and a second kernel joins the pieces of what several SMs
  * share, in a fixed order, so equal calls give equal bits.  The partial results use scratch of the handle under the rule of fa_forward.
  * FA_FLAG_SERIAL_KERNEL selects a plain kernel of one CTA per query row.

@@ -27,18 +27,19 @@ fa_status launch_simple(fa_handle* h, int dqk, const fa::PagedParams& p, const f
 }
 
 // How the list of work is made (fa_tree.cuh).  A row tile's tokens are as many as fit, and no more than a sequence can have.  A tile of keys
-// counts what it takes: where two row tiles share it HBM still bounds 16-bit caches of head size 128, so it counts as for one; smaller tiles
-// (head size 64, 8 bits) are bound by the exponentials, which two row tiles have twice.
+// counts what it takes: two row tiles have twice the exponentials.
 fa::TreeList make_list(int group, int max_tokens, int dqk, bool e4m3) {
     fa::TreeList li;
     li.row_heads = group < 128 ? group : 128;
     li.head_chunks = (group + li.row_heads - 1) / li.row_heads;
     li.row_tokens = 128 / li.row_heads < max_tokens ? 128 / li.row_heads : max_tokens;
-    li.two = dqk != 192;
+    li.two = dqk != 192 && !e4m3;      // (as in TreeCfg)
+    li.token_magic = li.row_tokens == 1 ? 0u : static_cast<uint32_t>((0x100000000ull + li.row_tokens - 1) / li.row_tokens);
     li.w1 = 1;
-    li.w2 = e4m3 || dqk == 64 ? 2 : 1;
+    li.w2 = li.two ? 2 : 1;
     li.cost = 1;
     li.least = 2 * li.w2;
+    li.pad = 0;
     return li;
 }
 
@@ -68,6 +69,9 @@ fa_status launch_tree(fa_handle* h, const CUtensorMap& mq, const CUtensorMap& mk
 
 extern "C" {
 
+#ifdef FA_TREE_TRACE
+int fa_tree_trace(void* to) { return cudaMemcpyFromSymbol(to, fa::g_tree_trace, sizeof fa::g_tree_trace); }
+#endif
 fa_status fa_forward_paged_tree(fa_handle* h, const fa_paged_cache* cache, const fa_paged_seqs* seqs, const fa_tree* tree, int total,
                                 const void* Q, void* O, float* lse, int Hq, float scale, const int64_t* q_strides, const int64_t* o_strides,
                                 void* stream) {

@@ -17,13 +17,13 @@
 //   * The mask concerns the last tiles alone: a thread has one row, takes its 128 bits for a tile out of the row's words by funnel shifts,
 //     and hides keys past the length with the same bits.
 //
-// Over an e4m3 cache both products are fp16 ones: four more warps turn the codes into fp16, which holds them exactly, on their way
-// from the tiles that TMA has filled to those that are multiplied; the queries are scaled by a power of two per row so that fp16 holds
-// them, the probabilities by 2^7.  (The 8-bit MMA would need three terms for a query and a probability, on the softmax warps, which are
-// the bound already.)
+// Over an e4m3 cache K is multiplied as it is (kind::f8f6f4), the queries as three e5m2 terms like in fa_paged.cuh, added up in one
+// accumulator (half as many MMAs again); P V is an fp16 product, since terms of P would be work of the softmax warps, which are the
+// bound: four more warps turn V's codes into fp16, which holds them exactly, and P is scaled by 2^7.  (K through fp16 too: 255 us, 48
+// sequences of 300 to 8192 keys, 13 drafts, 64/8 heads; the conversions slow the softmax down by what they share with it.)
 //
-// Roles: warps 0-3 / 4-7 softmax of stream 0 / 1 and results, warp 8 MMA issue, warp 9 loads of Q and K, warp 10 of V, warp 11 the list
-// and the zeros behind a sequence's last value, over e4m3 caches warps 12-13 / 14-15 the codes of K / V.
+// Roles: warps 0-3 / 4-7 softmax of stream 0 / 1 and results, warp 8 MMA issue, warp 9 loads of K, warp 10 of Q and V, warp 11 the list
+// and the zeros behind a sequence's last value, over e4m3 caches warps 12-15 the terms of Q and the codes of V.
 // TMEM: S_0 [0,128) S_1 [128,256) O_0 [256,384) O_1 [384,512); P_t over S_t[0,64).
 #pragma once
 
@@ -41,19 +41,25 @@ namespace fa {
 // ------------------------------------------------------------------ the list of work units and its shares
 
 // A row block (up to two row tiles of a sequence and K/V head) has `cost` units for what it takes beside its tiles, and then `w2` or `w1` units
-// per tile of 128 keys, as it has two row tiles or one.  A tile belongs to the CTA whose share its first unit is in.
+// per tile of 128 keys, as it has two row tiles or one; with `pad` it counts as many tiles at least.  A tile belongs to the CTA whose
+// share its first unit is in.
 struct TreeList {
     int row_tokens, row_heads;    // tokens and heads of a row tile
+    uint32_t token_magic;         // ceil(2^32 / row_tokens): exact quotients of numbers below 2^16 (0: row_tokens is 1)
     int head_chunks;              // row tiles that a token's group is cut into
     int two;                      // blocks have two row tiles where there are two
-    int cost, w1, w2, least;
+    int cost, w1, w2, least, pad;
 };
 // Row tiles of n drafts.
-__host__ __device__ inline int tree_row_tiles(const TreeList& li, int n) { return (n + li.row_tokens - 1) / li.row_tokens * li.head_chunks; }
+__host__ __device__ inline int tree_row_tiles(const TreeList& li, int n) {
+    const uint32_t x = static_cast<uint32_t>(n + li.row_tokens - 1);
+    const int tiles = li.token_magic ? static_cast<int>((static_cast<unsigned long long>(x) * li.token_magic) >> 32) : static_cast<int>(x);
+    return li.head_chunks == 1 ? tiles : tiles * li.head_chunks;
+}
 __host__ __device__ inline int tree_tiles(int len) { return (len + kTileN - 1) / kTileN; }
 struct TreeUnits { int pairs, pair, single; };      // blocks of two row tiles, units of each, units of the one behind them (0: none)
 __host__ __device__ inline TreeUnits tree_units(const TreeList& li, int n, int len) {
-    const int rt = tree_row_tiles(li, n), nt = tree_tiles(len);
+    const int rt = tree_row_tiles(li, n), nt = tree_tiles(len) > li.pad ? tree_tiles(len) : li.pad;
     TreeUnits u;
     if (li.two) {
         u.pairs = rt / 2;
@@ -67,6 +73,30 @@ __host__ __device__ inline TreeUnits tree_units(const TreeList& li, int n, int l
     return u;
 }
 __host__ __device__ inline int tree_head_units(const TreeUnits& u) { return u.pairs * u.pair + u.single; }
+
+// What a batch is, as far as the rules below ask: row blocks, key tiles of its longest and shortest sequence, whether blocks of one and of
+// two row tiles are among it.
+struct TreeBatch { int blocks, longest, shortest, kinds; };
+constexpr int kTreeWholeTiles = 4;
+// Small batches.  A join costs about as much as two rounds of tiles: where there is a CTA for every block and none has more than four
+// tiles, all count the same and nothing is split.  Where there are two CTAs for every block at least and all are equally long, their pieces
+// are equally long too, and a CTA has one.  Returns the share (0: what the total gives).
+__host__ __device__ inline int tree_rules(TreeList& li, const TreeBatch& b, int ctas) {
+    if (b.blocks <= ctas && b.longest <= kTreeWholeTiles) {
+        li.w1 = li.w2;
+        li.pad = b.longest;
+        return li.cost + li.w2 * li.pad;
+    }
+    if (2 * b.blocks <= ctas && b.longest == b.shortest && b.kinds != 3) {
+        const int pieces = ctas / b.blocks, per = (b.longest + pieces - 1) / pieces;
+        li.cost = 0;
+        li.w1 = li.w2 = 1;
+        const int share = per < 2 ? 2 : per;
+        li.pad = (b.longest + share - 1) / share * share;
+        return share;
+    }
+    return 0;
+}
 __host__ __device__ inline int tree_share(const TreeList& li, int total, int ctas) {
     const int per = static_cast<int>((static_cast<unsigned>(total) + ctas - 1) / ctas);
     return per < li.least ? li.least : per;
@@ -88,7 +118,7 @@ struct TreeJoin { int kvh, row_tile, two, n, row0, pieces, unused0, unused1; };
 // Tiles [t0, t1) that units [u0, u1) hold of a block of nt tiles whose first unit is ub.
 __host__ __device__ inline int tree_tile_at(int u, int ub, int cost, int w, int nt) {
     const int x = u - ub - cost;
-    const int t = x <= 0 ? 0 : (x + w - 1) / w;
+    const int t = x <= 0 ? 0 : w == 1 ? x : (x + 1) >> 1;         // (w is 1 or 2)
     return t < nt ? t : nt;
 }
 
@@ -100,8 +130,8 @@ struct TreeWalk {
     TreeUnits u;
     bool ended;
 };
-template <typename SeqOf>
-__host__ __device__ inline void tree_walk_begin(TreeWalk& w, const TreeList& li, int cta, int share, int total, int seq, int base, SeqOf&& seq_of) {
+// (n, row0 and len of the sequence that the share begins in have been set)
+__host__ __device__ inline void tree_walk_begin(TreeWalk& w, const TreeList& li, int cta, int share, int total, int seq, int base) {
     w.cta = cta;
     w.share = share;
     w.u0 = static_cast<long long>(cta) * share < total ? cta * share : total;
@@ -110,7 +140,6 @@ __host__ __device__ inline void tree_walk_begin(TreeWalk& w, const TreeList& li,
     w.seq = seq;
     w.tiles = 0;
     if (w.ended) return;
-    seq_of(seq, w.n, w.row0, w.len);
     w.u = tree_units(li, w.n, w.len);
     const int per = tree_head_units(w.u);
     w.kvh = (w.u0 - base) / per;
@@ -121,7 +150,7 @@ __host__ __device__ inline void tree_walk_begin(TreeWalk& w, const TreeList& li,
 template <typename SeqOf>
 __host__ __device__ inline bool tree_walk_next(TreeWalk& w, const TreeList& li, int Hkv, int B, SeqOf&& seq_of, TreePart& e) {
     while (!w.ended) {
-        const int rt = tree_row_tiles(li, w.n), blocks = w.u.pairs + (w.u.single ? 1 : 0);
+        const int blocks = w.u.pairs + (w.u.single ? 1 : 0);
         const int ub = w.base + w.block * w.u.pair, nt = tree_tiles(w.len);
         const bool pair = w.block < w.u.pairs;
         const int wt = li.two && pair ? li.w2 : li.w1, end = ub + (pair ? w.u.pair : w.u.single);
@@ -143,7 +172,6 @@ __host__ __device__ inline bool tree_walk_next(TreeWalk& w, const TreeList& li, 
             e.pieces = (ub + li.cost + (nt - 1) * wt) / w.share - (ub + li.cost) / w.share + 1;
         }
         w.tiles += some ? e.t1 - e.t0 : 0;
-        (void)rt;
         // the block behind it
         if (end >= w.u1) {
             w.ended = true;
@@ -168,18 +196,24 @@ __host__ __device__ inline bool tree_walk_next(TreeWalk& w, const TreeList& li, 
 
 template <int DQK, int DV, bool kE4m3>
 struct TreeCfg {
-    static constexpr bool kTwo = DQK != 192;                    // room for a second query tile
+    static constexpr bool kTwo = DQK != 192 && !kE4m3;          // room for a second query tile
     static constexpr int kQTiles = kTwo ? 2 : 1;
     static constexpr int kQChunks = DQK / kChunkCols, kVChunks = DV / kChunkCols;
     static constexpr int kQBytes = kQChunks * kChunkBytes;      // a query tile; a K tile alike
-    static constexpr int kKBytes = kQBytes, kVBytes = kVChunks * kChunkBytes;
-    // tiles that are multiplied, and over e4m3 caches the codes before them (rows of 128 bytes, whatever the head size)
-    static constexpr int kKStages = kE4m3 ? (DQK == 192 ? 1 : 2) : (DQK == 64 ? 6 : DQK == 128 ? 3 : 2);
-    static constexpr int kVStages = kE4m3 ? (DQK == 64 ? 2 : 1) : (DQK == 64 ? 6 : 2);
-    static constexpr int kRawKChunks = (DQK + 127) / 128;
-    static constexpr int kRawKBytes = kE4m3 ? kRawKChunks * kChunkBytes : 0, kRawVBytes = kE4m3 ? kChunkBytes : 0;
-    static constexpr int kRaw = kE4m3 ? (DQK == 64 ? 4 : 2) : 0;
-    static constexpr int kTileBytes = kQTiles * kQBytes + kKStages * kKBytes + kVStages * kVBytes + kRaw * (kRawKBytes + kRawVBytes);
+    // tiles of K as they are multiplied: 64 columns of bf16, or 128 codes, to a 128-byte row
+    static constexpr int kKChunks = kE4m3 ? (DQK + 127) / 128 : kQChunks;
+    static constexpr int kKBytes = kKChunks * kChunkBytes, kVBytes = kVChunks * kChunkBytes;
+    static constexpr int kTerms = 3;                            // of the queries, over e4m3 caches
+    static constexpr int kQSpace = kE4m3 ? kTerms * kKBytes : kQTiles * kQBytes;
+    // where 64 columns of the queries are loaded to (over e4m3 caches, into the space of their terms)
+    static __host__ __device__ constexpr int q_place(int chunk) {
+        return (!kE4m3 ? chunk : DQK == 192 ? 2 * chunk + 1 : 2 * chunk) * kChunkBytes;
+    }
+    static_assert(kQSpace >= kQTiles * kQBytes, "the queries are loaded into the space of their terms");
+    static constexpr int kKStages = kE4m3 ? (DQK == 192 ? 2 : 4) : (DQK == 64 ? 6 : DQK == 128 ? 3 : 2);
+    static constexpr int kVStages = kE4m3 ? (DQK == 192 ? 1 : 2) : (DQK == 64 ? 6 : 2);
+    static constexpr int kRaw = kE4m3 ? (DQK == 64 ? 4 : DQK == 128 ? 3 : 2) : 0;      // tiles of V's codes
+    static constexpr int kTileBytes = kQSpace + kKStages * kKBytes + kVStages * kVBytes + kRaw * kChunkBytes;
     static constexpr int kThreads = kE4m3 ? 512 : 384;
     // registers per thread: 256 x 216 + 128 x 72 of 384 x 168, or 256 x 184 + 256 x 72 of 512 x 128
     static constexpr int kRegsSoftmax = kE4m3 ? 184 : 216, kRegsOther = 72;
@@ -187,21 +221,27 @@ struct TreeCfg {
     static constexpr int kParts = 4;
 };
 
+struct TreeWait {
+    uint32_t abort_flag;
+    uint32_t* status;
+    unsigned long long limit_ns;
+};
+
 template <int DQK, int DV, bool kE4m3>
 struct TreeShared {
     using Cfg = TreeCfg<DQK, DV, kE4m3>;
-    uint64_t q_full, q_ready[2], q_empty;
+    uint64_t q_full, q_ready, q_empty;
     uint64_t k_full[Cfg::kKStages], k_empty[Cfg::kKStages], v_full[Cfg::kVStages], v_empty[Cfg::kVStages];
-    uint64_t raw_full[2][kE4m3 ? Cfg::kRaw : 1], raw_empty[2][kE4m3 ? Cfg::kRaw : 1];      // of K, of V
+    uint64_t raw_full[kE4m3 ? Cfg::kRaw : 1], raw_empty[kE4m3 ? Cfg::kRaw : 1];      // codes of V
     uint64_t v_tail[kE4m3 ? 1 : Cfg::kVStages];       // the rows behind a sequence's last value are zeros
     uint64_t s_full[2], p_first[2], p_rest[2], o_final[2];
     uint64_t part_full[Cfg::kParts], part_empty[Cfg::kParts];
     TreePart part[Cfg::kParts];
-    uint32_t tmem_base, abort_flag;
-    int start_seq, start_base;
+    uint32_t tmem_base;
+    TreeWait wait;
     int v_issued;                 // V tiles whose loads have been issued
-    float stat_m[2][kTileM], stat_l[2][kTileM];       // (of two streams on the same rows; at the start the sums of the list)
-    uint8_t q_shift[kE4m3 ? 2 : 1][kE4m3 ? kTileM : 4];      // 127 - exponent that a row was scaled by
+    float stat_m[2][kTileM], stat_l[2][kTileM];       // (of two streams on the same rows)
+    uint8_t q_shift[2][kE4m3 ? kTileM : 4];      // of even and odd parts: 127 - exponent that a row was scaled by
 };
 
 template <int DQK, int DV, bool kE4m3>
@@ -225,11 +265,45 @@ __host__ __device__ constexpr uint32_t make_idesc_f16_f32(int m, int n, bool b_m
 
 namespace ptx {
 
+FA_DEVI void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+
 // Two e4m3 codes (low byte first) -> two fp16, exactly (NaN stays NaN).
 FA_DEVI uint32_t e4m3x2_to_f16x2(uint32_t codes) {
     uint32_t r;
     asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %1; cvt.rn.f16x2.e4m3x2 %0, lo; }" : "=r"(r) : "r"(codes));
     return r;
+}
+// probe3_mma_ss3 (fa_fwd_pair.cuh), or the same around three 8-bit products
+template <bool kF8>
+FA_DEVI uint32_t probe3_scores(uint32_t bar0, uint32_t par0, uint32_t bar1, uint32_t par1, uint32_t bar2, uint32_t par2, uint32_t d_tmem, uint64_t a0,
+                               uint64_t b0, uint64_t a1, uint64_t b1, uint64_t a2, uint64_t b2, uint32_t idesc) {
+    if constexpr (!kF8) {
+        return probe3_mma_ss3(bar0, par0, bar1, par1, bar2, par2, d_tmem, a0, b0, a1, b1, a2, b2, idesc);
+    } else {
+        uint32_t r;
+        asm volatile(
+            "{\n"
+            ".reg .pred p0, p1, p2, q;\n"
+            ".reg .b32 t0, t1, t2;\n"
+            "setp.ne.b32 q, 1, 0;\n"
+            "mbarrier.try_wait.parity.shared::cta.b64 p0, [%1], %2;\n"
+            "mbarrier.try_wait.parity.shared::cta.b64 p1, [%3], %4;\n"
+            "mbarrier.try_wait.parity.shared::cta.b64 p2, [%5], %6;\n"
+            "tcgen05.mma.cta_group::1.kind::f8f6f4 [%7], %8, %9, %14, q;\n"
+            "tcgen05.mma.cta_group::1.kind::f8f6f4 [%7], %10, %11, %14, q;\n"
+            "tcgen05.mma.cta_group::1.kind::f8f6f4 [%7], %12, %13, %14, q;\n"
+            "selp.u32 t0, 1, 0, p0;\n"
+            "selp.u32 t1, 2, 0, p1;\n"
+            "selp.u32 t2, 4, 0, p2;\n"
+            "or.b32 t0, t0, t1;\n"
+            "or.b32 %0, t0, t2;\n"
+            "}\n"
+            : "=r"(r)
+            : "r"(bar0), "r"(par0), "r"(bar1), "r"(par1), "r"(bar2), "r"(par2), "r"(d_tmem), "l"(a0), "l"(b0), "l"(a1), "l"(b1), "l"(a2),
+              "l"(b2), "r"(idesc)
+            : "memory");
+        return r;
+    }
 }
 FA_DEVI uint32_t pack_f16x2(float lo, float hi) {
     uint32_t r;
@@ -239,38 +313,67 @@ FA_DEVI uint32_t pack_f16x2(float lo, float hi) {
 
 }  // namespace ptx
 
-// Bounded wait for a count in shared memory that another warp moves up, as mbar_wait.
-FA_DEVI bool wait_count(const int* count, int least, const ptx::WaitCtx& ctx, uint32_t who) {
-    volatile const int* const c = count;
+// Bounded waits, as in fa_paged.cuh: the softmax warps wait, directly or in turn, for every other role and alone watch the clock; once one
+// of their waits has run out, the abort flag ends everybody's.  (A clock in each of some twenty waits is code that the SM's instruction
+// cache would have to hold: what is run once in a part, its list entry, masked tile and result, took 2000 to 7000 cycles each.)
+FA_DEVI bool tree_wait(uint64_t& bar, uint32_t parity, const TreeWait* ctx) {
+    const uint32_t at = ptx::smem_addr(&bar);
+    if (ptx::mbar_try_wait(at, parity)) return true;
+    do {
+        if (*static_cast<const volatile uint32_t*>(&ctx->abort_flag)) return false;
+    } while (!ptx::mbar_try_wait(at, parity));
+    return true;
+}
+static __device__ __noinline__ bool tree_wait_long(uint64_t* bar, uint32_t parity, TreeWait* ctx, uint32_t who) {
+    const uint32_t at = ptx::smem_addr(bar);
+    volatile uint32_t* abort_flag = &ctx->abort_flag;
     uint64_t t0 = 0;
-    while (*c < least) {
-        __nanosleep(100);
-        if (*ctx.abort_flag) return false;
-        const uint64_t now = ptx::globaltimer_ns();
-        if (t0 == 0) {
-            t0 = now;
-        } else if (now - t0 > ctx.limit_ns) {
-            *ctx.abort_flag = 1u;
-            if (ctx.status) {
-                volatile uint32_t* sw = ctx.status;       // mapped host memory: plain stores
-                sw[1] = who;
-                sw[0] = 4u;                               // FA_ERR_DEVICE_TIMEOUT
-                __threadfence_system();
+    for (uint32_t it = 1;; ++it) {
+        if (ptx::mbar_try_wait(at, parity)) return true;
+        if ((it & 63u) == 0u) {
+            if (*abort_flag) return false;
+            const uint64_t now = ptx::globaltimer_ns();
+            if (t0 == 0) {
+                t0 = now;
+            } else if (now - t0 > ctx->limit_ns) {
+                *abort_flag = 1u;
+                if (ctx->status) {
+                    volatile uint32_t* sw = ctx->status;      // mapped host memory: plain stores
+                    sw[1] = who;
+                    sw[0] = 4u;                               // FA_ERR_DEVICE_TIMEOUT
+                    __threadfence_system();
+                }
+                return false;
             }
-            return false;
         }
     }
-    __threadfence_block();
-    return true;
+}
+FA_DEVI bool tree_wait_timed(uint64_t& bar, uint32_t parity, TreeWait* ctx, uint32_t who) {
+    return ptx::mbar_try_wait(ptx::smem_addr(&bar), parity) || tree_wait_long(&bar, parity, ctx, who);
 }
 
 // ------------------------------------------------------------------ softmax pass
 
-// The pass of fa_softmax_pass.cuh with a mask of bits (vis[w] bit e: key 32 w + e of the tile is seen) and, over e4m3 caches, P as fp16 under a
-// bias.  P = 2^(s c + off), off = bias - u c with the reference u; all exponentials on the special-function unit: HBM is the bound here.
+// Scores that a row does not see become -inf in TMEM, 32 at a time (bit e of `seen`: the e-th of them), ahead of the pass: a loop of 50
+// instructions for the few tiles that are masked, where 128 selections in the pass would be 4 KB of its code.
+FA_DEVI void tree_hide(uint32_t tS, uint32_t seen) {
+#pragma unroll 1
+    for (int e = 0; e < 32; e += 16, seen >>= 16) {
+        uint32_t s[16];
+        ptx::tmem_ld_x16(tS + e, s);
+        ptx::tc_wait_ld();
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (!(seen & (1u << i))) s[i] = 0xff800000u;
+        ptx::tmem_st_x16(tS + e, s);
+    }
+}
+
+// The pass of fa_softmax_pass.cuh, over e4m3 caches with P as fp16 under a bias.  P = 2^(s c + off), off = bias - u c with the reference u; all
+// exponentials on the special-function unit.
 template <int DV, bool kHalf, typename ArriveFirst, typename ArriveRest>
-FA_DEVI void tree_pass(uint32_t tS, uint32_t tO, float c, float tau_raw, float bias, bool masked, const uint32_t (&vis)[4], bool first_tile,
-                       float& m_ref, float& l, int lane, ArriveFirst&& arrive_first, ArriveRest&& arrive_rest) {
+FA_DEVI void tree_pass(uint32_t tS, uint32_t tO, float c, float tau_raw, float bias, bool first_tile, float& m_ref, float& l, int lane,
+                       ArriveFirst&& arrive_first, ArriveRest&& arrive_rest) {
     using namespace ptx;
     const float2 c2 = make_float2(c, c);
     float2 off2;
@@ -308,11 +411,6 @@ FA_DEVI void tree_pass(uint32_t tS, uint32_t tO, float c, float tau_raw, float b
         tmem_ld_x32(tS + 64, s + 64);
         tmem_ld_x32(tS + 96, s + 96);
         tc_wait_ld();
-        if (masked) {
-#pragma unroll
-            for (int e = 0; e < kTileN; ++e)
-                if (!(vis[e / 32] & (1u << (e % 32)))) s[e] = 0xff800000u;   // -inf
-        }
         const float off = m_ref == -INFINITY ? bias : bias - m_ref * c;
         off2 = make_float2(off, off);
         float a[8];
@@ -370,6 +468,12 @@ FA_DEVI void tree_pass(uint32_t tS, uint32_t tO, float c, float tau_raw, float b
 
 // ------------------------------------------------------------------ kernel
 
+#ifdef FA_TREE_TRACE
+__device__ long long g_tree_trace[148][4][256];
+#define TT(w, id) do { if (tt_n < 250) { g_tree_trace[blockIdx.x][w][tt_n++] = (static_cast<long long>(id) << 48) | (clock64() & 0xffffffffffffll); } } while (0)
+#else
+#define TT(w, id) do { } while (0)
+#endif
 template <int DQK, int DV, bool kE4m3>
 __global__ void __launch_bounds__((TreeCfg<DQK, DV, kE4m3>::kThreads), 1)
 fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
@@ -378,15 +482,16 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     using Shared = TreeShared<DQK, DV, kE4m3>;
     using namespace ptx;
     constexpr int NK = Cfg::kKStages, NV = Cfg::kVStages, NR = kE4m3 ? Cfg::kRaw : 1, NP = Cfg::kParts;
-    constexpr int kWarps = Cfg::kThreads / 32;
 
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     Shared& sh = *reinterpret_cast<Shared*>(smem_raw + Cfg::kTileBytes);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t smem_base = smem_addr(smem_raw);
-    const uint32_t sQ = smem_base, sK = sQ + Cfg::kQTiles * Cfg::kQBytes, sV = sK + NK * Cfg::kKBytes, sRawK = sV + NV * Cfg::kVBytes,
-                   sRawV = sRawK + Cfg::kRaw * Cfg::kRawKBytes;
+    const uint32_t sQ = smem_base, sK = sQ + Cfg::kQSpace, sV = sK + NK * Cfg::kKBytes, sRaw = sV + NV * Cfg::kVBytes;
 
+    int tt_n = 0;
+    (void)tt_n;
+    if (tid == 0) TT(0, 1);
     grid_launch_dependents();
     if ((smem_base & 1023u) != 0u) {          // uniform over the CTA; nothing has been set up yet
         grid_dependency_wait();
@@ -402,32 +507,36 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
         return;
     }
     if (tid == 0) {
-        sh.abort_flag = 0;
+        sh.wait.abort_flag = 0;
+        sh.wait.status = p.status;
+        sh.wait.limit_ns = p.wait_limit_ns;
         mbar_init(smem_addr(&sh.q_full), 1);
         mbar_init(smem_addr(&sh.q_empty), 1);
         sh.v_issued = 0;
 #pragma unroll
         for (int s = 0; s < NK; ++s) {
-            mbar_init(smem_addr(&sh.k_full[s]), kE4m3 ? 2 : 1);     // the two warps that convert, or the copy
+            mbar_init(smem_addr(&sh.k_full[s]), 1);
             mbar_init(smem_addr(&sh.k_empty[s]), 1);
         }
 #pragma unroll
         for (int s = 0; s < NV; ++s) {
-            mbar_init(smem_addr(&sh.v_full[s]), kE4m3 ? 2 : 1);
+            mbar_init(smem_addr(&sh.v_full[s]), kE4m3 ? 4 : 1);     // the four warps that convert, or the copy
             mbar_init(smem_addr(&sh.v_empty[s]), 1);
             if constexpr (!kE4m3) mbar_init(smem_addr(&sh.v_tail[s]), 1);
         }
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            mbar_init(smem_addr(&sh.q_ready[t]), 4);      // 4 softmax warps
             mbar_init(smem_addr(&sh.s_full[t]), 1);
-            mbar_init(smem_addr(&sh.p_first[t]), 4);
+            mbar_init(smem_addr(&sh.p_first[t]), 4);      // 4 softmax warps
             mbar_init(smem_addr(&sh.p_rest[t]), 4);
             mbar_init(smem_addr(&sh.o_final[t]), 1);
+        }
+        if constexpr (kE4m3) {
+            mbar_init(smem_addr(&sh.q_ready), 4);
 #pragma unroll
             for (int s = 0; s < NR; ++s) {
-                mbar_init(smem_addr(&sh.raw_full[t][s]), 1);
-                mbar_init(smem_addr(&sh.raw_empty[t][s]), 2);
+                mbar_init(smem_addr(&sh.raw_full[s]), 1);
+                mbar_init(smem_addr(&sh.raw_empty[s]), 4);
             }
         }
 #pragma unroll
@@ -444,66 +553,37 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
         tmem_alloc(smem_addr(&sh.tmem_base), 512);
         tmem_relinquish_alloc_permit();
     }
+    if (warp >= 9 && warp < 11) {
+        // lengths, offsets and block table towards L2 (a line each; the streams of other calls have usually driven them out): list and loads
+        // wait for one after the other
+        const int per_row = (p.max_pages + 31) / 32, line = blockIdx.x * 32 + lane, b = line / per_row;
+        if (warp == 9) {
+            if (lane * 32 < p.B) {
+                prefetch_l2(p.seq_lens + lane * 32);
+                if (a.t.cu_seqlens) prefetch_l2(a.t.cu_seqlens + lane * 32);
+            }
+        } else if (b < p.B) {
+            prefetch_l2(p.block_table + b * p.table_stride + (line - b * per_row) * 32);
+        }
+    }
     grid_dependency_wait();
 
-    // ------------------------------------------------------------ the list: its length, and where this CTA's share begins
+    if (tid == 0) TT(0, 2);
     auto seq_of = [&](int b, int& n, int& row0, int& len) {
         const DraftRows d = draft_rows(a.t.cu_seqlens, b, p.B, a.t.total, a.t.max_tokens, nullptr);
         n = d.count;
         row0 = d.first;
         len = clamped_len(p.seq_lens[b], p.max_pages, p.page_size, nullptr);
     };
-    int total, share;
-    {
-        const int chunk = (p.B + Cfg::kThreads - 1) / Cfg::kThreads, b_first = min(p.B, tid * chunk), b_last = min(p.B, b_first + chunk);
-        int* const sums = reinterpret_cast<int*>(&sh.stat_m[0][0]);
-        int mine = 0;
-#pragma unroll 2
-        for (int b = b_first; b < b_last; ++b) {
-            int n, row0, len;
-            seq_of(b, n, row0, len);
-            mine += p.Hkv * tree_head_units(tree_units(a.list, n, len));
-        }
-        int before = mine;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int o = __shfl_up_sync(0xffffffffu, before, d);
-            if (lane >= d) before += o;
-        }
-        if (lane == 31) sums[warp] = before;
-        before -= mine;
-        tc_fence_before_sync();
-        __syncthreads();
-        tc_fence_after_sync();
-        total = 0;
-#pragma unroll
-        for (int v = 0; v < kWarps; ++v) {
-            const int n = sums[v];
-            if (v < warp) before += n;
-            total += n;
-        }
-        share = tree_share(a.list, total, gridDim.x);
-        const long long at = static_cast<long long>(blockIdx.x) * share;
-        if (at < total && before <= at && at < before + mine) {
-            int b = b_first, base = before;
-            for (;; ++b) {
-                int n, row0, len;
-                seq_of(b, n, row0, len);
-                const int units = p.Hkv * tree_head_units(tree_units(a.list, n, len));
-                if (at < base + units) break;
-                base += units;
-            }
-            sh.start_seq = b;
-            sh.start_base = base;
-        }
-        __syncthreads();
-    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    if (tid == 352) TT(2, 21);
     const uint32_t tmem = sh.tmem_base;
-    WaitCtx wctx{&sh.abort_flag, p.status, p.wait_limit_ns};
-    auto wait = [&](uint64_t& bar, uint32_t parity, uint32_t who) -> bool { return mbar_wait(smem_addr(&bar), parity, wctx, who); };
+    auto wait = [&](uint64_t& bar, uint32_t parity) -> bool { return tree_wait(bar, parity, &sh.wait); };
     // Part k for a warp as a whole; false at the end of the list or after a wait that ran out.
     auto take_part = [&](int k, TreePart& e) -> bool {
-        if (!__all_sync(0xffffffffu, wait(sh.part_full[k % NP], (k / NP) & 1, kSiteItem))) return false;
+        if (!__all_sync(0xffffffffu, wait(sh.part_full[k % NP], (k / NP) & 1))) return false;
         e = sh.part[k % NP];
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_addr(&sh.part_empty[k % NP]));
@@ -524,17 +604,18 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
         for (int k = 0;; ++k) {
             TreePart e;
             e.t1 = -1;
-            ok = ok && wait(sh.part_full[k % NP], (k / NP) & 1, kSiteItem);
+            ok = ok && tree_wait_timed(sh.part_full[k % NP], (k / NP) & 1, &sh.wait, kSiteItem);
             if (named_barrier_or(1, 256, !ok)) break;
             e = sh.part[k % NP];
             if (e.t1 < 0) break;
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_addr(&sh.part_empty[k % NP]));
+            if ((tid & 127) == 0) TT(t, 3);
             const int nt = e.t1 - e.t0;
             const bool two = Cfg::kTwo && e.two;
             const int steps0 = two ? nt : (nt + 1) / 2, steps1 = two ? nt : nt / 2, steps = t == 0 ? steps0 : steps1;
             // the row: its token and head
-            const int tile = e.row_tile + (two ? t : 0), tc = tile / a.list.head_chunks, hc = tile - tc * a.list.head_chunks;
+            const int tile = e.row_tile + (two ? t : 0), tc = a.list.head_chunks == 1 ? tile : tile / a.list.head_chunks, hc = tile - tc * a.list.head_chunks;
             const int token = tc * a.list.row_tokens + row_token, head = hc * a.list.row_heads + row_head;
             const bool live = row_token < a.list.row_tokens && token < e.n && head < a.group;
             const bool warp_live = __any_sync(0xffffffffu, live);
@@ -543,52 +624,17 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             float c = p.scale_log2;
             if constexpr (kE4m3) {
                 c *= p.k_scale ? p.k_scale[e.kvh] : 1.f;
-                if (nt > 0) {
-                    // the row's queries as fp16, scaled by a power of two that puts the largest into [2^14, 2^15) (from 2^127 down to
-                    // 2^-112; a smaller row by 2^126, which makes its entries, multiples of 2^-133, exact too)
-                    if (two || t == 0) {
-                        ok = ok && wait(sh.q_full, n_q & 1, kSiteMmaQFull);
-                        __syncwarp();
-                        const uint32_t base = sQ + (two ? t : 0) * Cfg::kQBytes + row * 128;
-                        uint32_t top = 0;
-#pragma unroll 4
-                        for (int v = 0; v < DQK / 8; ++v) {
-                            const uint4 x = ld_shared_v4(base + (v >> 3) * kChunkBytes + (((v & 7) ^ (row & 7)) << 4));
-                            const uint32_t w4[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) top = max(top, max((w4[i] & 0x7fffu) << 16, w4[i] & 0x7fff0000u));
-                        }
-                        int sft = top ? 14 - (static_cast<int>(top >> 23) - 127) : 0;
-                        sft = sft > 126 ? 126 : (sft < -113 ? -113 : sft);
-                        const float mult = __uint_as_float(static_cast<uint32_t>(sft + 127) << 23);
-#pragma unroll 4
-                        for (int v = 0; v < DQK / 8; ++v) {
-                            const uint32_t at = base + (v >> 3) * kChunkBytes + (((v & 7) ^ (row & 7)) << 4);
-                            const uint4 x = ld_shared_v4(at);
-                            const uint32_t w4[4] = {x.x, x.y, x.z, x.w};
-                            uint32_t h[4];
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) h[i] = pack_f16x2(__uint_as_float(w4[i] << 16) * mult, __uint_as_float(w4[i] & 0xffff0000u) * mult);
-                            st_shared_v4(at, h[0], h[1], h[2], h[3]);
-                        }
-                        sh.q_shift[two ? t : 0][row] = static_cast<uint8_t>(127 - sft);
-                        fence_proxy_async_smem();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(smem_addr(&sh.q_ready[t]));
-                    } else if (lane == 0) {
-                        mbar_arrive(smem_addr(&sh.q_ready[1]));       // (keeps the barrier's phases in step with the parts)
-                    }
-                    ++n_q;
-                }
+                n_q += nt > 0;
             }
             float m_ref = -INFINITY, l = 0.f, tau_raw = kRescaleThresholdLog2 / c;
             for (int j = 0; j < steps; ++j, ++n_s) {
-                ok = __all_sync(0xffffffffu, ok && wait(sh.s_full[t], n_s & 1, kSiteSoftmaxSFull));
+                ok = __all_sync(0xffffffffu, ok && tree_wait_timed(sh.s_full[t], n_s & 1, &sh.wait, kSiteSoftmaxSFull));
                 if (!ok) break;
                 tc_fence_after_sync();
+                if ((tid & 127) == 0) TT(t, 4);
                 if constexpr (kE4m3) {
                     if (j == 0) {
-                        c *= __uint_as_float(static_cast<uint32_t>(sh.q_shift[two ? t : 0][row]) << 23);
+                        c *= __uint_as_float(static_cast<uint32_t>(sh.q_shift[(n_q - 1) & 1][row]) << 23);
                         tau_raw = kRescaleThresholdLog2 / c;
                     }
                 }
@@ -603,20 +649,26 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 }
                 const int key0 = (e.t0 + (two ? j : 2 * j + t)) * kTileN;
                 const bool masked = key0 + kTileN > first_draft;
-                uint32_t vis[4];
                 if (masked) {
-#pragma unroll
+#pragma unroll 1
                     for (int w = 0; w < 4; ++w) {
-                        const int j0 = key0 + 32 * w - first_draft;          // the draft of this word's first key
-                        auto word = [&](int i) { return draft_word(a.t, q_row, token, e.n, i); };
-                        if (j0 <= -32) vis[w] = 0xffffffffu;
-                        else if (j0 < 0) vis[w] = (word(0) << -j0) | ((1u << -j0) - 1u);
-                        else vis[w] = __funnelshift_r(word(j0 >> 5), word((j0 >> 5) + 1), j0 & 31);
+                        const int j0 = key0 + 32 * w - first_draft;          // the draft of these 32 keys' first
+                        uint32_t seen = 0xffffffffu;
+                        if (j0 > -32) {
+                            const int at = j0 >> 5;                          // (from -1 on; there is no word -1: its bits, the keys before the drafts, are seen)
+                            const uint32_t lo = at < 0 ? 0xffffffffu : draft_word(a.t, q_row, token, e.n, at), hi = draft_word(a.t, q_row, token, e.n, at + 1);
+                            seen = __funnelshift_r(lo, hi, j0 & 31);
+                        }
+                        tree_hide(tS + 32 * w, seen);
                     }
+                    tc_wait_st();
                 }
-                tree_pass<DV, kE4m3>(tS, tO + 128 * t, c, tau_raw, Cfg::kBias, masked, vis, j == 0, m_ref, l, lane,
+                if ((tid & 127) == 0) TT(t, masked ? 11 : 10);
+                tree_pass<DV, kE4m3>(tS, tO + 128 * t, c, tau_raw, Cfg::kBias, j == 0, m_ref, l, lane,
                                      [&]() { mbar_arrive(bar_pf); }, [&]() { mbar_arrive(bar_pr); });
+                if ((tid & 127) == 0) TT(t, 5);
             }
+            if ((tid & 127) == 0) TT(t, 6);
             // ---- the part's result: sum and reference of a row that saw a key, O of one stream or of both
             const float off = m_ref == -INFINITY ? Cfg::kBias : Cfg::kBias - m_ref * c;
             float m = l > 0.f || l != l ? -off : -INFINITY;       // (a NaN goes through)
@@ -637,16 +689,24 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             const float norm = whole ? (any ? vs / l : 0.f) : 1.f;
             f0 *= norm;
             f1 *= norm;
-            if (steps0 > 0 && (!two || t == 0)) ok = ok && wait(sh.o_final[0], n_final[0] & 1, kSiteEpiOFull);
-            if (steps1 > 0 && (!two || t == 1)) ok = ok && wait(sh.o_final[1], n_final[1] & 1, kSiteEpiOFull);
+            if (steps0 > 0 && (!two || t == 0)) ok = ok && tree_wait_timed(sh.o_final[0], n_final[0] & 1, &sh.wait, kSiteEpiOFull);
+            if (steps1 > 0 && (!two || t == 1)) ok = ok && tree_wait_timed(sh.o_final[1], n_final[1] & 1, &sh.wait, kSiteEpiOFull);
             n_final[0] += steps0 > 0;
             n_final[1] += steps1 > 0;
             ok = __all_sync(0xffffffffu, ok);
             tc_fence_after_sync();
+            if ((tid & 127) == 0) TT(t, 7);
             // columns [col0, col1) are this thread's: all of its own stream's, or half of both streams'
             const int col0 = two ? 0 : t * (DV / 2), col1 = two ? DV : col0 + DV / 2;
             const int hq = e.kvh * a.group + head;
+            // Whole results: four neighbouring lanes exchange 16-byte pieces of their rows, so that they store 64 neighbouring bytes of one row
+            // at a time (a lane's own row: 32 lines a store, which held up the next part's begin by 4000 cycles).
             __nv_bfloat16* const out = p.O + q_row * p.o_st + hq * p.o_sh;
+            __nv_bfloat16* out4[4];
+            uint32_t live4 = __ballot_sync(0xffffffffu, ok && live) >> (lane & 28);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                out4[i] = reinterpret_cast<__nv_bfloat16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(out), (lane & 28) + i)) + (lane & 3) * 8;
             float* const slot = a.part + static_cast<long long>(whole ? 0 : e.slot) * tree_slot_floats(DV, Cfg::kTwo);
             float4* const slot_o = reinterpret_cast<float4*>(slot) + (two ? t : 0) * (DV / 4) * kTileM + row;
 #pragma unroll 1
@@ -670,20 +730,30 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
 #pragma unroll
                     for (int i = 0; i < 32; ++i) y[i] = 0.f;
                 }
-                if (ok && live) {
-                    if (whole) {
+                if (whole) {
+                    // (nothing seen: zeros, whatever the products of zero probabilities gave)
+                    uint32_t v[4][4];
 #pragma unroll
-                        for (int i = 0; i < 32; i += 8) {
-                            uint4 v = make_uint4(pack_bf16x2(y[i], y[i + 1]), pack_bf16x2(y[i + 2], y[i + 3]), pack_bf16x2(y[i + 4], y[i + 5]),
-                                                 pack_bf16x2(y[i + 6], y[i + 7]));
-                            // (nothing seen: zeros, whatever the products of zero probabilities gave)
-                            if (!any) v = make_uint4(0, 0, 0, 0);
-                            *reinterpret_cast<uint4*>(out + col + i) = v;
+                    for (int i = 0; i < 32; i += 2) v[i / 8][i % 8 / 2] = any ? pack_bf16x2(y[i], y[i + 1]) : 0u;
+#pragma unroll
+                    for (int bit = 1; bit <= 2; bit <<= 1) {
+                        const bool up = (lane & bit) != 0;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if (i & bit) continue;
+#pragma unroll
+                            for (int w = 0; w < 4; ++w) {
+                                const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? v[i][w] : v[i | bit][w], bit);
+                                if (up) v[i][w] = got; else v[i | bit][w] = got;
+                            }
                         }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 32; i += 4) slot_o[(col + i) / 4 * kTileM] = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
                     }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (live4 & (1u << i)) *reinterpret_cast<uint4*>(out4[i] + col) = make_uint4(v[i][0], v[i][1], v[i][2], v[i][3]);
+                } else if (ok && live) {
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) slot_o[(col + i) / 4 * kTileM] = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
                 }
             }
             if (ok && live && (two || t == 0)) {
@@ -697,22 +767,29 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             }
             // (both groups have read both accumulators, and each other's sums, at the barrier that the next part begins with)
             tc_fence_before_sync();
+            if ((tid & 127) == 0) TT(t, 8);
         }
     } else if (warp == 8) {
         // ============================================================ MMA issue, one thread for both streams
         setmaxnreg_dec<Cfg::kRegsOther>();
         if (elect_one()) {
-            constexpr uint32_t kIdescQK = kE4m3 ? make_idesc_f16_f32(kTileM, kTileN, false) : make_idesc_bf16_f32(kTileM, kTileN, false, false);
+            constexpr uint32_t kIdescQK = kE4m3 ? (make_idesc_e4m3_f32(kTileM, kTileN, false, false) | (1u << 7))        // A: e5m2
+                                                : make_idesc_bf16_f32(kTileM, kTileN, false, false);
             constexpr uint32_t kIdescPV = kE4m3 ? make_idesc_f16_f32(kTileM, DV, true) : make_idesc_bf16_f32(kTileM, DV, false, true);
             constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);   // sbo, version, swizzle
-            constexpr int kSteps = DQK / 16;
+            constexpr int kPerTerm = kE4m3 ? DQK / 32 : DQK / 16, kSteps = kE4m3 ? Cfg::kTerms * kPerTerm : kPerTerm;      // of 32 bytes of a row
             const uint32_t q_lo0 = ((sQ & 0x3FFFFu) >> 4) | (1u << 16);
             const uint32_t k_lo0 = ((sK & 0x3FFFFu) >> 4) | (1u << 16);
             const uint32_t v_lo0 = ((sV & 0x3FFFFu) >> 4) | ((static_cast<uint32_t>(kChunkBytes) >> 4) << 16);
             auto desc = [](uint32_t lo) -> uint64_t { return (static_cast<uint64_t>(kDescHi) << 32) | lo; };
-            auto koff = [](int ks) -> uint32_t { return static_cast<uint32_t>(((ks / 4) * kChunkBytes + (ks % 4) * 32) >> 4); };
-            int sk = 0, sv = 0, n_p[2] = {0, 0}, n_q = 0;       // stages, steps of each stream, parts with queries so far
-            uint32_t ph_k = 0, ph_v = 0, ph_tail = 0;                       // (of the last tiles, a bit per stage)
+            auto koff = [](int ks) -> uint32_t { ks %= kPerTerm; return static_cast<uint32_t>(((ks / 4) * kChunkBytes + (ks % 4) * 32) >> 4); };
+            auto qoff = [&](int ks) -> uint32_t { return koff(ks) + static_cast<uint32_t>(ks / kPerTerm * (Cfg::kKBytes >> 4)); };
+            auto score = [&](uint32_t tS, uint32_t q, uint32_t k, int ks) {
+                if constexpr (kE4m3) mma_ss_f8(tS, desc(q + qoff(ks)), desc(k + koff(ks)), kIdescQK, ks > 0 ? 1u : 0u);
+                else mma_ss(tS, desc(q + qoff(ks)), desc(k + koff(ks)), kIdescQK, ks > 0 ? 1u : 0u);
+            };
+            int sk = 0, sv = 0, n_q = 0;       // stages, parts with queries so far
+            uint32_t ph_k = 0, ph_v = 0, ph_tail = 0, ph_p = 0;             // (of the last tiles, a bit per stage; of the steps, a bit per stream)
             bool two = false, tail = false;
             int nt = 0, k_tile = 0, v_tile = 0;                             // of the part: tiles, tile that stage sk / sv holds
             uint32_t pre_p = 0, pre_v = 0, pre_k = 0;                       // probes that succeeded for the next block
@@ -729,24 +806,24 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 }
             };
             // Stream t's block of step j: P_t V, then the next scores.  Barriers that the next block needs are probed from inside it.
-            auto block = [&](auto tc, int j, int steps) -> bool {
-                constexpr int t = decltype(tc)::value;
+            // (one body for both streams: see TreeWait on code)
+            auto block = [&](int t, int j, int steps) -> bool {
                 const bool fresh = !two || t == 0;                   // (the streams of two row tiles share the K/V tiles)
                 const bool next = j + 1 < steps;
                 if (fresh) {
-                    if (!pre_v && !wait(sh.v_full[sv], ph_v, kSiteMmaKvFull)) return false;
+                    if (!pre_v && !wait(sh.v_full[sv], ph_v)) return false;
                     if constexpr (!kE4m3) {
                         if (tail && v_tile == nt - 1) {
-                            if (!wait(sh.v_tail[sv], (ph_tail >> sv) & 1u, kSiteMmaTail)) return false;
+                            if (!wait(sh.v_tail[sv], (ph_tail >> sv) & 1u)) return false;
                             ph_tail ^= 1u << sv;
                         }
                     }
-                    if (next && !pre_k && !wait(sh.k_full[sk], ph_k, kSiteMmaKvFull)) return false;
+                    if (next && !pre_k && !wait(sh.k_full[sk], ph_k)) return false;
                 }
-                const uint32_t parity = n_p[t] & 1;
+                const uint32_t parity = (ph_p >> t) & 1u;
                 const uint32_t tS = tmem + 128 * t, tO = tmem + 256 + 128 * t;
                 const uint32_t vlo = v_lo0 + sv * (Cfg::kVBytes >> 4), klo = k_lo0 + sk * (Cfg::kKBytes >> 4);
-                if (!pre_p && !wait(sh.p_first[t], parity, kSiteMmaPFull)) return false;
+                if (!pre_p && !wait(sh.p_first[t], parity)) return false;
                 pre_p = pre_v = pre_k = 0u;
                 tc_fence_after_sync();
                 mma_ts(tO, tS + 0, desc(vlo + 0 * (2048 >> 4)), kIdescPV, j > 0 ? 1u : 0u);
@@ -755,23 +832,25 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 mma_ts(tO, tS + 24, desc(vlo + 3 * (2048 >> 4)), kIdescPV, 1u);
                 const uint32_t rest = probe_mma_ts2(smem_addr(&sh.p_rest[t]), parity, tO, tS + 32, desc(vlo + 4 * (2048 >> 4)),
                                                     tS + 40, desc(vlo + 5 * (2048 >> 4)), kIdescPV);
-                if (!rest && !wait(sh.p_rest[t], parity, kSiteMmaPFull)) return false;
+                if (!rest && !wait(sh.p_rest[t], parity)) return false;
                 tc_fence_after_sync();
                 mma_ts(tO, tS + 48, desc(vlo + 6 * (2048 >> 4)), kIdescPV, 1u);
                 mma_ts(tO, tS + 56, desc(vlo + 7 * (2048 >> 4)), kIdescPV, 1u);
-                ++n_p[t];
+                ph_p ^= 1u << t;
+                const bool v_done = !two || t == 1;
+                if (v_done) tc_commit(smem_addr(&sh.v_empty[sv]));       // (here: behind the scores it would come 512 cycles later)
                 if (next) {
                     // (the next block's: the other stream's probabilities; its V and K tile where they are not this block's)
                     const bool same = two && t == 0;
                     const int sv_n = sv + 1 == NV ? 0 : sv + 1, sk_n = sk + 1 == NK ? 0 : sk + 1;
                     const uint32_t ph_v_n = sv + 1 == NV ? ph_v ^ 1u : ph_v, ph_k_n = sk + 1 == NK ? ph_k ^ 1u : ph_k;
-                    mma_ss(tS, desc(q_lo(t) + koff(0)), desc(klo + koff(0)), kIdescQK, 0u);
-                    const uint32_t got = probe3_mma_ss3(smem_addr(&sh.p_first[1 - t]), n_p[1 - t] & 1, smem_addr(&sh.v_full[same ? sv : sv_n]), same ? ph_v : ph_v_n,
+                    score(tS, q_lo(t), klo, 0);
+                    const uint32_t got = probe3_scores<kE4m3>(smem_addr(&sh.p_first[1 - t]), (ph_p >> (1 - t)) & 1u, smem_addr(&sh.v_full[same ? sv : sv_n]), same ? ph_v : ph_v_n,
                                                         smem_addr(&sh.k_full[same ? sk : sk_n]), same ? ph_k : ph_k_n, tS,
-                                                        desc(q_lo(t) + koff(1)), desc(klo + koff(1)), desc(q_lo(t) + koff(2)), desc(klo + koff(2)),
-                                                        desc(q_lo(t) + koff(3)), desc(klo + koff(3)), kIdescQK);
+                                                        desc(q_lo(t) + qoff(1)), desc(klo + koff(1)), desc(q_lo(t) + qoff(2)), desc(klo + koff(2)),
+                                                        desc(q_lo(t) + qoff(3)), desc(klo + koff(3)), kIdescQK);
 #pragma unroll
-                    for (int ks = 4; ks < kSteps; ++ks) mma_ss(tS, desc(q_lo(t) + koff(ks)), desc(klo + koff(ks)), kIdescQK, 1u);
+                    for (int ks = 4; ks < kSteps; ++ks) score(tS, q_lo(t), klo, ks);
                     pre_p = got & 1u;
                     pre_v = (got >> 1) & 1u;
                     pre_k = (got >> 2) & 1u;
@@ -779,15 +858,12 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 } else {
                     tc_commit(smem_addr(&sh.o_final[t]));
                 }
-                if (!two || t == 1) {
-                    tc_commit(smem_addr(&sh.v_empty[sv]));
-                    step_v();
-                }
+                if (v_done) step_v();
                 return true;
             };
             bool ok = true;
             for (int k = 0; ok; ++k) {
-                ok = wait(sh.part_full[k % NP], (k / NP) & 1, kSiteItem);
+                ok = wait(sh.part_full[k % NP], (k / NP) & 1);
                 if (!ok) break;
                 const TreePart e = sh.part[k % NP];
                 mbar_arrive(smem_addr(&sh.part_empty[k % NP]));
@@ -799,66 +875,66 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 k_tile = v_tile = 0;
                 pre_p = pre_v = pre_k = 0u;
                 const int steps0 = two ? nt : (nt + 1) / 2, steps1 = two ? nt : nt / 2;
-                if constexpr (kE4m3) ok = wait(sh.q_ready[0], n_q & 1, kSiteMmaQFull) && wait(sh.q_ready[1], n_q & 1, kSiteMmaQFull);
-                else ok = wait(sh.q_full, n_q & 1, kSiteMmaQFull);
+                if constexpr (kE4m3) ok = wait(sh.q_ready, n_q & 1);
+                else ok = wait(sh.q_full, n_q & 1);
                 ++n_q;
-#pragma unroll
+#pragma unroll 1
                 for (int t = 0; t < 2; ++t) {
                     if (!ok || (t == 1 && steps1 == 0)) break;
-                    if (t == 0 || !two) ok = wait(sh.k_full[sk], ph_k, kSiteMmaKvFull);
+                    if (t == 0 || !two) ok = wait(sh.k_full[sk], ph_k);
                     if (!ok) break;
                     tc_fence_after_sync();
                     const uint32_t klo = k_lo0 + sk * (Cfg::kKBytes >> 4);
 #pragma unroll
-                    for (int ks = 0; ks < kSteps; ++ks) mma_ss(tmem + 128 * t, desc(q_lo(t) + koff(ks)), desc(klo + koff(ks)), kIdescQK, ks > 0 ? 1u : 0u);
+                    for (int ks = 0; ks < kSteps; ++ks) score(tmem + 128 * t, q_lo(t), klo, ks);
                     scores_done(t);
                 }
                 for (int j = 0; j < steps0 && ok; ++j) {
-                    ok = block(IntC<0>{}, j, steps0);
-                    if (ok && j < steps1) ok = block(IntC<1>{}, j, steps1);
+#pragma unroll 1
+                    for (int t = 0; t < 2 && ok; ++t)
+                        if (t == 0 || j < steps1) ok = block(t, j, t == 0 ? steps0 : steps1);
                 }
             }
         }
     } else if (warp == 9 || warp == 10) {
-        // ============================================================ TMA loads of Q and K (warp 9), or of V (warp 10)
+        // ============================================================ TMA loads of K (warp 9), or of Q and V (warp 10)
         setmaxnreg_dec<Cfg::kRegsOther>();
         const bool is_v = warp == 10;
-        constexpr int NL = kE4m3 ? NR : (NK > NV ? NK : NV);
-        (void)NL;
-        constexpr int kKC = kE4m3 ? Cfg::kRawKChunks : Cfg::kQChunks, kVC = kE4m3 ? 1 : Cfg::kVChunks, kMaxChunks = kKC > kVC ? kKC : kVC;
+        constexpr int kVC = kE4m3 ? 1 : Cfg::kVChunks, kMaxChunks = Cfg::kKChunks > kVC ? Cfg::kKChunks : kVC;
         constexpr int kChunk = kE4m3 ? 128 : kChunkCols;             // columns of a 128-byte row
-        const int chunks = is_v ? kVC : kKC, stages = kE4m3 ? NR : (is_v ? NV : NK);
-        const int stage_bytes = kE4m3 ? (is_v ? Cfg::kRawVBytes : Cfg::kRawKBytes) : (is_v ? Cfg::kVBytes : Cfg::kKBytes);
+        const int chunks = is_v ? kVC : Cfg::kKChunks, stages = is_v ? (kE4m3 ? NR : NV) : NK;
+        const int stage_bytes = is_v ? kVC * kChunkBytes : Cfg::kKBytes;
         const CUtensorMap* tm = is_v ? &tm_v : &tm_k;
-        uint64_t* const full = kE4m3 ? sh.raw_full[is_v] : (is_v ? sh.v_full : sh.k_full);
-        uint64_t* const empty = kE4m3 ? sh.raw_empty[is_v] : (is_v ? sh.v_empty : sh.k_empty);
-        const uint32_t dst0 = kE4m3 ? (is_v ? sRawV : sRawK) : (is_v ? sV : sK);
+        uint64_t* const full = is_v ? (kE4m3 ? sh.raw_full : sh.v_full) : sh.k_full;
+        uint64_t* const empty = is_v ? (kE4m3 ? sh.raw_empty : sh.v_empty) : sh.k_empty;
+        const uint32_t dst0 = is_v ? (kE4m3 ? sRaw : sV) : sK;
         const int box = p.box_rows, shift = __ffs(kTileN / box) - 1, boxes = 1 << shift, tiles_ahead = 32 >> shift;
         int n = 0, n_q = 0, s = 0;
         uint32_t parity = 1;
         bool ok = true;
         TreePart e;
         for (int k = 0; ok && take_part(k, e); ++k) {
+            if (lane == 0 && !is_v) TT(3, 30);
             if (e.t0 == e.t1) continue;
-            if (!is_v) {
+            const int* const table = p.block_table + e.b * p.table_stride;
+            if (is_v) {              // (its tiles are needed later than those of K)
                 const bool two = Cfg::kTwo && e.two;
-                ok = __all_sync(0xffffffffu, wait(sh.q_empty, (n_q & 1) ^ 1, kSiteLoadQEmpty));
+                ok = __all_sync(0xffffffffu, wait(sh.q_empty, (n_q & 1) ^ 1));
                 if (!ok) break;
                 ++n_q;
                 if (lane == 0) {
                     const uint32_t bar = smem_addr(&sh.q_full);
                     mbar_arrive_expect_tx(bar, (two ? 2 : 1) * Cfg::kQChunks * a.list.row_tokens * a.list.row_heads * 128);
                     for (int t = 0; t < (two ? 2 : 1); ++t) {
-                        const int tile = e.row_tile + t, tc = tile / a.list.head_chunks, hc = tile - tc * a.list.head_chunks;
+                        const int tile = e.row_tile + t, tc = a.list.head_chunks == 1 ? tile : tile / a.list.head_chunks, hc = tile - tc * a.list.head_chunks;
 #pragma unroll
                         for (int cc = 0; cc < Cfg::kQChunks; ++cc)
-                            tma_load_4d(sQ + t * Cfg::kQBytes + cc * kChunkBytes, &tm_q, bar, cc * kChunkCols, e.kvh * a.group + hc * a.list.row_heads,
+                            tma_load_4d(sQ + t * Cfg::kQBytes + Cfg::q_place(cc), &tm_q, bar, cc * kChunkCols, e.kvh * a.group + hc * a.list.row_heads,
                                         e.row0 + tc * a.list.row_tokens, 0);
                     }
                 }
                 __syncwarp();
             }
-            const int* const table = p.block_table + e.b * p.table_stride;
             int pages = 0, slots = 0;         // of tile `first` + lane / boxes, box lane % boxes
             int first = e.t0;
             for (int t = e.t0; t < e.t1; ++t, ++n) {
@@ -875,9 +951,10 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                         }
                     }
                 }
+                if (lane == 0 && !is_v) TT(3, 31);
                 const int from = ((t - first) << shift) + lane;
                 const int page = __shfl_sync(0xffffffffu, pages, from & 31), slot = __shfl_sync(0xffffffffu, slots, from & 31);
-                ok = __all_sync(0xffffffffu, wait(empty[s], parity, kSiteLoadKvEmpty));
+                ok = __all_sync(0xffffffffu, wait(empty[s], parity));
                 if (!ok) break;
                 const uint32_t bar = smem_addr(&full[s]);
                 const int n_box = min(boxes, (e.len - t * kTileN + box - 1) / box);
@@ -901,14 +978,80 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     } else if (warp == 11) {
         // ============================================================ the list of parts; zeros behind the last value of a sequence
         setmaxnreg_dec<Cfg::kRegsOther>();
+        // its length, and where this CTA's share begins: a lane has `chunk` sequences
+        TreeList li = a.list;
+        const int chunk = (p.B + 31) >> 5, b_first = min(p.B, lane * chunk), b_last = min(p.B, b_first + chunk);
+        int n_mine = 0, row_mine = 0, len_mine = 0;          // the lane's last sequence
+        TreeBatch batch{0, 0, 0x7fffffff, 0};
+        int mine = 0;
+#pragma unroll 4
+        for (int b = b_first; b < b_last; ++b) {
+            seq_of(b, n_mine, row_mine, len_mine);
+            const TreeUnits u = tree_units(li, n_mine, len_mine);
+            mine += p.Hkv * tree_head_units(u);
+            if (n_mine > 0) {
+                batch.blocks += p.Hkv * (u.pairs + (u.single ? 1 : 0));
+                batch.longest = max(batch.longest, tree_tiles(len_mine));
+                batch.shortest = min(batch.shortest, tree_tiles(len_mine));
+                batch.kinds |= (u.pairs ? 1 : 0) | (u.single ? 2 : 0);
+            }
+        }
+        batch.blocks = __reduce_add_sync(0xffffffffu, batch.blocks);
+        batch.longest = __reduce_max_sync(0xffffffffu, batch.longest);
+        batch.shortest = __reduce_min_sync(0xffffffffu, batch.shortest);
+        batch.kinds = __reduce_or_sync(0xffffffffu, batch.kinds);
+        int share = tree_rules(li, batch, gridDim.x);
+        if (share > 0) {             // (few sequences: units are counted otherwise)
+            mine = 0;
+            for (int b = b_first; b < b_last; ++b) {
+                if (chunk > 1) seq_of(b, n_mine, row_mine, len_mine);
+                mine += p.Hkv * tree_head_units(tree_units(li, n_mine, len_mine));
+            }
+        }
+        int before = mine;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int o = __shfl_up_sync(0xffffffffu, before, d);
+            if (lane >= d) before += o;
+        }
+        const int total = __shfl_sync(0xffffffffu, before, 31);
+        before -= mine;
+        if (share == 0) share = tree_share(li, total, gridDim.x);
+        const long long u0 = static_cast<long long>(blockIdx.x) * share;
+        int start_seq = b_first, start_base = before;
+        const uint32_t holds = __ballot_sync(0xffffffffu, before <= u0 && u0 < before + mine);
+        if (holds && lane == __ffs(holds) - 1 && chunk > 1) {
+            for (;; ++start_seq) {
+                seq_of(start_seq, n_mine, row_mine, len_mine);
+                const int units = p.Hkv * tree_head_units(tree_units(li, n_mine, len_mine));
+                if (u0 < start_base + units) break;
+                start_base += units;
+            }
+        }
+        const int from = holds ? __ffs(holds) - 1 : 0;
+        start_seq = __shfl_sync(0xffffffffu, start_seq, from);
+        start_base = __shfl_sync(0xffffffffu, start_base, from);
         TreeWalk w;
-        tree_walk_begin(w, a.list, blockIdx.x, share, total, sh.start_seq, sh.start_base, seq_of);
+        w.n = __shfl_sync(0xffffffffu, n_mine, from);
+        w.row0 = __shfl_sync(0xffffffffu, row_mine, from);
+        w.len = __shfl_sync(0xffffffffu, len_mine, from);
+        tree_walk_begin(w, li, blockIdx.x, share, total, start_seq, start_base);
         TreeJoin join{0, 0, 0, 0, 0, 0, 0, 0};
+        if (lane == 0) TT(2, 22);
         TreePart cur, e;
+        e.t1 = 0;
         bool ok = true;
+        auto issued = [&](int count) -> bool {
+            while (*static_cast<volatile int*>(&sh.v_issued) < count) {
+                __nanosleep(100);
+                if (*static_cast<volatile uint32_t*>(&sh.wait.abort_flag)) return false;
+            }
+            __threadfence_block();
+            return true;
+        };
         auto publish = [&](int k) {
-            if (!tree_walk_next(w, a.list, p.Hkv, p.B, seq_of, e)) e.t1 = -1;
-            ok = __all_sync(0xffffffffu, ok && wait(sh.part_empty[k % NP], ((k / NP) & 1) ^ 1, kSiteItem));
+            if (!tree_walk_next(w, li, p.Hkv, p.B, seq_of, e)) e.t1 = -1;
+            ok = __all_sync(0xffffffffu, ok && wait(sh.part_empty[k % NP], ((k / NP) & 1) ^ 1));
             if (!ok) return;
             if (e.t1 >= 0 && e.slot >= 0 && e.t0 == 0) join = TreeJoin{e.kvh, e.row_tile, e.two, e.n, e.row0, e.pieces, 0, 0};
             if (lane == 0) {
@@ -917,26 +1060,22 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             }
             __syncwarp();
         };
-        // (contents that the other reads of the list clamp are reported here, by the CTAs whose share a sequence begins in)
-        if (blockIdx.x == 0) {
-            for (int b = lane; b < p.B; b += 32) {
-                draft_rows(a.t.cu_seqlens, b, p.B, a.t.total, a.t.max_tokens, p.status);
-                clamped_len(p.seq_lens[b], p.max_pages, p.page_size, p.status);
-            }
-            __syncwarp();
-        }
-        publish(0);
-        for (int k = 0; ok && e.t1 >= 0; ++k) {
+        if (lane == 0) TT(2, 23);
+        for (int k = 0; ok; ++k) {
             cur = e;
-            publish(k + 1);
+            publish(k);
             if (!ok) break;
+            if (k == 0) {
+                if (e.t1 < 0) break;
+                continue;
+            }
             // the part's last tile holds the sequence's last key: V rows behind it hold whatever the page held, or were not loaded,
             // and 0 * NaN is NaN
             if (!kE4m3 && cur.t1 > cur.t0 && cur.t1 * kTileN > cur.len) {
                 const int at = cur.tile0 + cur.t1 - cur.t0 - 1, s = at % NV;
                 // (The list runs ahead of the loads, by more than a turn of the ring where parts are short: a phase of v_full says that it
                 // is this tile's only once its load has been issued.  From there on the stage waits for the zeros.)
-                ok = __all_sync(0xffffffffu, wait_count(&sh.v_issued, at + 1, wctx, kSiteTailIssued) && wait(sh.v_full[s], (at / NV) & 1, kSiteTailVFull));
+                ok = __all_sync(0xffffffffu, issued(at + 1) && wait(sh.v_full[s], (at / NV) & 1));
                 if (!ok) break;
                 const int keys = cur.len - (cur.t1 - 1) * kTileN;
                 for (int i = lane; i < (kTileN - keys) * 8; i += 32) {
@@ -948,6 +1087,15 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_addr(&sh.v_tail[kE4m3 ? 0 : s]));
             }
+            if (e.t1 < 0) break;
+        }
+        // (contents that the other reads of the list clamp are reported here, by one CTA)
+        if (blockIdx.x == 0) {
+            for (int b = lane; b < p.B; b += 32) {
+                draft_rows(a.t.cu_seqlens, b, p.B, a.t.total, a.t.max_tokens, p.status);
+                clamped_len(p.seq_lens[b], p.max_pages, p.page_size, p.status);
+            }
+            __syncwarp();
         }
         // (after a wait that ran out the pieces are not joined; the results are invalid either way)
         if (lane == 0) {
@@ -956,63 +1104,119 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
         }
         __syncwarp();
     } else {
-        // ============================================================ e4m3 codes of K (warps 12, 13) or V (14, 15) into fp16
+        // ============================================================ queries into their terms, codes of V into fp16
         setmaxnreg_dec<Cfg::kRegsOther>();
         if constexpr (kE4m3) {
-            const bool is_v = warp >= 14;
-            const int half = tid & 63, stages = is_v ? NV : NK;
-            constexpr int kKPieces = DQK / 16, kVPieces = DV / 16;       // 16-byte pieces of a row of codes
-            uint64_t* const full = is_v ? sh.v_full : sh.k_full;
-            uint64_t* const empty = is_v ? sh.v_empty : sh.k_empty;
-            int s = 0, r = 0;
+            const int mine = warp & 3;
+            // A lane has one row of every fourth group of 8 and one 16-byte piece of codes in 64 columns, two of fp16.  Eight neighbouring lanes
+            // have four pieces of two rows r and r ^ 5: under the swizzle they meet all banks in the load and in both stores, and all
+            // addresses of a lane are its own constants plus multiples of 1024.
+            const int row = lane & 4 ? (lane >> 3) ^ 5 : lane >> 3, piece = lane & 3;
+            const uint32_t in_even = row * 128 + ((piece ^ row) << 4), in_odd = in_even ^ 64u;
+            const uint32_t out0 = row * 128 + (((2 * piece) ^ row) << 4), out1 = out0 ^ 16u;
+            constexpr int kDeep = 4;          // loads ahead of the conversions: all of 64 columns
+            const int q_row = tid & (kTileM - 1);
+            int s = 0, r = 0, n_q = 0;
             uint32_t ph = 1, ph_r = 0;
             bool ok = true;
             TreePart e;
             for (int k = 0; ok && take_part(k, e); ++k) {
-                for (int t = e.t0; t < e.t1; ++t) {
-                    ok = wait(sh.raw_full[is_v][r], ph_r, kSiteLoadKvEmpty) && wait(empty[s], ph, kSiteLoadKvEmpty);
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
-                    const uint32_t src = is_v ? sRawV + r * Cfg::kRawVBytes : sRawK + r * Cfg::kRawKBytes;
-                    const uint32_t dst = is_v ? sV + s * Cfg::kVBytes : sK + s * Cfg::kKBytes;
-                    const int keys = e.len - t * kTileN;
-                    auto convert = [&](auto pieces_c) {
-                        constexpr int kPieces = decltype(pieces_c)::value;
-#pragma unroll 4
-                        for (int i = half; i < kTileN * kPieces; i += 64) {
-                            const int row = i / kPieces, q = i - row * kPieces;
-                            const uint4 x = ld_shared_v4(src + (q >> 3) * kChunkBytes + row * 128 + (((q & 7) ^ (row & 7)) << 4));
-                            const uint32_t w4[4] = {x.x, x.y, x.z, x.w};
-                            uint32_t h[8];
+                if (e.t0 == e.t1) continue;
+                // The row's queries, scaled by a power of two that puts the largest into [2^14, 2^15) (from 2^127 down to 2^-112; a
+                // smaller row by 2^126, which makes its entries, multiples of 2^-133, exact too), as fp16 and then as three
+                // e5m2 terms: top byte, remainder, top byte, remainder, top byte.  They go where the queries were loaded to: a thread's row
+                // lies in its own bytes before and after, and its pieces are taken in an order in which none is overwritten unread
+                // (128 columns: the last term of the first 64 waits in local memory).  (Here and not by the softmax warps, which are
+                // still at the part before: the first scores of a part came 7000 cycles after its beginning.)
+                ok = __all_sync(0xffffffffu, wait(sh.q_full, n_q & 1));
+                uint32_t top = 0;
+#pragma unroll 1
+                for (int cc = 0; cc < Cfg::kQChunks; ++cc) {
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                h[2 * j] = e4m3x2_to_f16x2(w4[j]);
-                                h[2 * j + 1] = e4m3x2_to_f16x2(w4[j] >> 16);
-                            }
-                            // (values behind the sequence's end hold whatever the page held: 0 * NaN is NaN)
-                            if (is_v && row >= keys) {
+                    for (int v = 0; v < 8; ++v) {
+                        const uint4 x = ld_shared_v4(sQ + Cfg::q_place(cc) + q_row * 128 + ((v ^ (q_row & 7)) << 4));
+                        const uint32_t w4[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-                                for (int j = 0; j < 8; ++j) h[j] = 0u;
-                            }
-                            // the two 16-byte pieces of fp16, in an order in which eight neighbouring lanes meet all banks
-                            const uint32_t to = dst + (q >> 2) * kChunkBytes + row * 128;
-                            const int p0 = 2 * (q & 3), odd = (q >> 2) & 1;
+                        for (int i = 0; i < 4; ++i) top = max(top, max((w4[i] & 0x7fffu) << 16, w4[i] & 0x7fff0000u));
+                    }
+                }
+                int sft = top ? 14 - (static_cast<int>(top >> 23) - 127) : 0;
+                sft = sft > 126 ? 126 : (sft < -113 ? -113 : sft);
+                const float mult = __uint_as_float(static_cast<uint32_t>(sft + 127) << 23);
+                uint4 held[4];
+#pragma unroll 1
+                for (int cc = 0; cc < Cfg::kQChunks; ++cc) {
+#pragma unroll 1
+                    for (int u0 = 0; u0 < 4; ++u0) {               // 16 values: 16 bytes of each term
+                        const int u = DQK == 128 && cc == 1 ? 3 - u0 : u0;
+                        const uint32_t in = sQ + Cfg::q_place(cc) + q_row * 128;
+                        const uint4 lo = ld_shared_v4(in + (((2 * u) ^ (q_row & 7)) << 4)), hi = ld_shared_v4(in + (((2 * u + 1) ^ (q_row & 7)) << 4));
+                        const uint32_t w8[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+                        uint32_t h[8];
 #pragma unroll
-                            for (int j = 0; j < 2; ++j) {
-                                const int which = j ^ odd;
-                                st_shared_v4(to + (((p0 + which) ^ (row & 7)) << 4), which ? h[4] : h[0], which ? h[5] : h[1], which ? h[6] : h[2],
-                                             which ? h[7] : h[3]);
+                        for (int i = 0; i < 8; ++i) h[i] = pack_f16x2(__uint_as_float(w8[i] << 16) * mult, __uint_as_float(w8[i] & 0xffff0000u) * mult);
+                        const uint32_t at = sQ + (cc >> 1) * kChunkBytes + q_row * 128 + ((((cc & 1) * 4 + u) ^ (q_row & 7)) << 4);
+#pragma unroll
+                        for (int term = 0; term < Cfg::kTerms; ++term) {
+                            const uint4 bytes = make_uint4(__byte_perm(h[0], h[1], 0x7531), __byte_perm(h[2], h[3], 0x7531),
+                                                           __byte_perm(h[4], h[5], 0x7531), __byte_perm(h[6], h[7], 0x7531));
+                            if (DQK == 128 && cc == 0 && term == 2) held[u] = bytes;
+                            else st_shared_v4(at + term * Cfg::kKBytes, bytes.x, bytes.y, bytes.z, bytes.w);
+                            if (term + 1 < Cfg::kTerms) {
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) {
+                                    const uint32_t bits = h[i] & 0xff00ff00u;
+                                    const __half2 rest = __hsub2(*reinterpret_cast<const __half2*>(&h[i]), *reinterpret_cast<const __half2*>(&bits));
+                                    h[i] = *reinterpret_cast<const uint32_t*>(&rest);
+                                }
                             }
                         }
-                    };
-                    if (is_v) convert(IntC<kVPieces>{}); else convert(IntC<kKPieces>{});
+                    }
+                }
+                if constexpr (DQK == 128) {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) st_shared_v4(sQ + 2 * Cfg::kKBytes + q_row * 128 + ((u ^ (q_row & 7)) << 4), held[u].x, held[u].y, held[u].z, held[u].w);
+                }
+                sh.q_shift[n_q & 1][q_row] = static_cast<uint8_t>(127 - sft);
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_addr(&sh.q_ready));
+                ++n_q;
+                for (int t = e.t0; ok && t < e.t1; ++t) {
+                    ok = wait(sh.raw_full[r], ph_r) && wait(sh.v_empty[s], ph);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    const uint32_t src = sRaw + r * kChunkBytes + mine * 1024, dst = sV + s * Cfg::kVBytes + mine * 1024;
+                    const int keys = e.len - t * kTileN;
+                    // (values behind the sequence's end hold whatever the page held: 0 * NaN is NaN)
+                    const bool zeros = keys < kTileN;
+#pragma unroll
+                    for (int c = 0; c < DV / 64; ++c) {
+                        const uint32_t from = src + (c & 1 ? in_odd : in_even), to = dst + c * kChunkBytes;
+                        uint4 x[kDeep];
+#pragma unroll
+                        for (int g = 0; g < kDeep; ++g) x[g] = ld_shared_v4(from + g * 4096);
+                        if (zeros) {
+#pragma unroll
+                            for (int g = 0; g < kDeep; ++g)
+                                if ((4 * g + mine) * 8 + row >= keys) x[g] = make_uint4(0, 0, 0, 0);
+                        }
+#pragma unroll
+                        for (int g = 0; g < kDeep; ++g) {
+                            const uint32_t at = to + g * 4096;
+                            st_shared_v4(at + out0, e4m3x2_to_f16x2(x[g].x), e4m3x2_to_f16x2(x[g].x >> 16), e4m3x2_to_f16x2(x[g].y),
+                                         e4m3x2_to_f16x2(x[g].y >> 16));
+                            st_shared_v4(at + out1, e4m3x2_to_f16x2(x[g].z), e4m3x2_to_f16x2(x[g].z >> 16), e4m3x2_to_f16x2(x[g].w),
+                                         e4m3x2_to_f16x2(x[g].w >> 16));
+                        }
+                    }
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) {
-                        mbar_arrive(smem_addr(&full[s]));
-                        mbar_arrive(smem_addr(&sh.raw_empty[is_v][r]));
+                        mbar_arrive(smem_addr(&sh.v_full[s]));
+                        mbar_arrive(smem_addr(&sh.raw_empty[r]));
                     }
-                    if (++s == stages) { s = 0; ph ^= 1u; }
+                    if (++s == NV) { s = 0; ph ^= 1u; }
                     if (++r == NR) { r = 0; ph_r ^= 1u; }
                 }
             }
@@ -1022,6 +1226,7 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     // ---------------------------------------------------------------- teardown (all warps)
     tc_fence_before_sync();
     __syncthreads();
+    if (tid == 0) TT(0, 9);
     if (warp == 8) tmem_dealloc(tmem, 512);
 }
 
