@@ -37,7 +37,7 @@ fa::TreeList make_list(int group, int max_tokens, int dqk, bool e4m3) {
     li.token_magic = li.row_tokens == 1 ? 0u : static_cast<uint32_t>((0x100000000ull + li.row_tokens - 1) / li.row_tokens);
     li.w1 = 1;
     li.w2 = li.two ? 2 : 1;
-    li.cost = 1;
+    li.cost = 4;
     li.least = 2 * li.w2;
     li.pad = 0;
     return li;
@@ -69,9 +69,6 @@ fa_status launch_tree(fa_handle* h, const CUtensorMap& mq, const CUtensorMap& mk
 
 extern "C" {
 
-#ifdef FA_TREE_TRACE
-int fa_tree_trace(void* to) { return cudaMemcpyFromSymbol(to, fa::g_tree_trace, sizeof fa::g_tree_trace); }
-#endif
 fa_status fa_forward_paged_tree(fa_handle* h, const fa_paged_cache* cache, const fa_paged_seqs* seqs, const fa_tree* tree, int total,
                                 const void* Q, void* O, float* lse, int Hq, float scale, const int64_t* q_strides, const int64_t* o_strides,
                                 void* stream) {

@@ -202,7 +202,7 @@ struct TreeCfg {
     static constexpr int kQBytes = kQChunks * kChunkBytes;      // a query tile; a K tile alike
     // tiles of K as they are multiplied: 64 columns of bf16, or 128 codes, to a 128-byte row
     static constexpr int kKChunks = kE4m3 ? (DQK + 127) / 128 : kQChunks;
-    static constexpr int kKBytes = kKChunks * kChunkBytes, kVBytes = kVChunks * kChunkBytes;
+    static constexpr int kKBytes = kKChunks * kChunkBytes;
     static constexpr int kTerms = 3;                            // of the queries, over e4m3 caches
     static constexpr int kQSpace = kE4m3 ? kTerms * kKBytes : kQTiles * kQBytes;
     // where 64 columns of the queries are loaded to (over e4m3 caches, into the space of their terms)
@@ -210,10 +210,17 @@ struct TreeCfg {
         return (!kE4m3 ? chunk : DQK == 192 ? 2 * chunk + 1 : 2 * chunk) * kChunkBytes;
     }
     static_assert(kQSpace >= kQTiles * kQBytes, "the queries are loaded into the space of their terms");
-    static constexpr int kKStages = kE4m3 ? (DQK == 192 ? 2 : 4) : (DQK == 64 ? 6 : DQK == 128 ? 3 : 2);
-    static constexpr int kVStages = kE4m3 ? (DQK == 192 ? 1 : 2) : (DQK == 64 ? 6 : 2);
-    static constexpr int kRaw = kE4m3 ? (DQK == 64 ? 4 : DQK == 128 ? 3 : 2) : 0;      // tiles of V's codes
-    static constexpr int kTileBytes = kQSpace + kKStages * kKBytes + kVStages * kVBytes + kRaw * kChunkBytes;
+    // P_t in shared memory, where there is room for two tiles of it: S_t is free as soon as it has been read, and the next scores are
+    // there when a pass ends.  Else P_t lies over S_t.
+    static constexpr bool kPSmem = DQK == 64 || (kE4m3 && DQK == 128);
+    static constexpr int kPBytes = 2 * kChunkBytes;             // 128 keys of 128 rows
+    // keys of a V stage: over e4m3 caches at 128 there is room for three halves of a tile of fp16 values
+    static constexpr int kVKeys = kE4m3 && kPSmem ? 64 : 128, kVParts = 128 / kVKeys;
+    static constexpr int kVChunk = kVKeys * 128, kVStage = kVChunks * kVChunk;
+    static constexpr int kKStages = kE4m3 ? 2 : (DQK == 64 ? 4 : DQK == 128 ? 3 : 2);
+    static constexpr int kVStages = kE4m3 ? (DQK == 192 ? 1 : DQK == 128 ? 3 : 4) : (DQK == 64 ? 4 : 2);
+    static constexpr int kRaw = kE4m3 ? (DQK == 64 ? 3 : 2) : 0;      // tiles of V's codes
+    static constexpr int kTileBytes = kQSpace + kKStages * kKBytes + kVStages * kVStage + kRaw * kChunkBytes + (kPSmem ? 2 * kPBytes : 0);
     static constexpr int kThreads = kE4m3 ? 512 : 384;
     // registers per thread: 256 x 216 + 128 x 72 of 384 x 168, or 256 x 184 + 256 x 72 of 512 x 128
     static constexpr int kRegsSoftmax = kE4m3 ? 184 : 216, kRegsOther = 72;
@@ -234,7 +241,7 @@ struct TreeShared {
     uint64_t k_full[Cfg::kKStages], k_empty[Cfg::kKStages], v_full[Cfg::kVStages], v_empty[Cfg::kVStages];
     uint64_t raw_full[kE4m3 ? Cfg::kRaw : 1], raw_empty[kE4m3 ? Cfg::kRaw : 1];      // codes of V
     uint64_t v_tail[kE4m3 ? 1 : Cfg::kVStages];       // the rows behind a sequence's last value are zeros
-    uint64_t s_full[2], p_first[2], p_rest[2], o_final[2];
+    uint64_t s_full[2], s_free[2], p_first[2], p_rest[2], o_final[2];      // (s_free, and o_final of every step, with P in shared memory)
     uint64_t part_full[Cfg::kParts], part_empty[Cfg::kParts];
     TreePart part[Cfg::kParts];
     uint32_t tmem_base;
@@ -265,6 +272,20 @@ __host__ __device__ constexpr uint32_t make_idesc_f16_f32(int m, int n, bool b_m
 
 namespace ptx {
 
+// Whether a phase is complete, without the wait that try_wait may take.
+FA_DEVI bool mbar_test_wait(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+        "selp.u32 %0, 1, 0, p;\n"
+        "}\n"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
 FA_DEVI void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
 // Two e4m3 codes (low byte first) -> two fp16, exactly (NaN stays NaN).
@@ -371,9 +392,11 @@ FA_DEVI void tree_hide(uint32_t tS, uint32_t seen) {
 
 // The pass of fa_softmax_pass.cuh, over e4m3 caches with P as fp16 under a bias.  P = 2^(s c + off), off = bias - u c with the reference u; all
 // exponentials on the special-function unit.
-template <int DV, bool kHalf, typename ArriveFirst, typename ArriveRest>
-FA_DEVI void tree_pass(uint32_t tS, uint32_t tO, float c, float tau_raw, float bias, bool first_tile, float& m_ref, float& l, int lane,
-                       ArriveFirst&& arrive_first, ArriveRest&& arrive_rest) {
+// kPSmem: P goes to the row's bytes p_row of two swizzled chunks of 64 keys; `take` is called once the scores are in registers, and
+// says when the product before (of P's space and O) is done, `arrive_first` is not.
+template <int DV, bool kHalf, bool kPSmem, typename Take, typename ArriveFirst, typename ArriveRest>
+FA_DEVI void tree_pass(uint32_t tS, uint32_t tO, uint32_t p_row, float c, float tau_raw, float bias, bool first_tile, float& m_ref, float& l, int lane,
+                       Take&& take, ArriveFirst&& arrive_first, ArriveRest&& arrive_rest) {
     using namespace ptx;
     const float2 c2 = make_float2(c, c);
     float2 off2;
@@ -384,6 +407,14 @@ FA_DEVI void tree_pass(uint32_t tS, uint32_t tO, float c, float tau_raw, float b
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
             const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[q * 32 + e]), __uint_as_float(s[q * 32 + e + 1])), c2, off2);
+#ifdef TREE_POLY
+            if ((e / 2) % TREE_POLY == TREE_POLY - 1) {
+                const float2 y = exp2_poly2<true>(x);
+                s[q * 32 + e] = __float_as_uint(y.x);
+                s[q * 32 + e + 1] = __float_as_uint(y.y);
+                continue;
+            }
+#endif
             s[q * 32 + e] = __float_as_uint(exp2_approx(x.x));
             s[q * 32 + e + 1] = __float_as_uint(exp2_approx(x.y));
         }
@@ -395,7 +426,15 @@ FA_DEVI void tree_pass(uint32_t tS, uint32_t tO, float c, float tau_raw, float b
             const float x = __uint_as_float(s[q * 32 + e]), y = __uint_as_float(s[q * 32 + e + 1]);
             pk[e / 2] = kHalf ? pack_f16x2(x, y) : pack_bf16x2(x, y);
         }
-        tmem_st_x16(tS + q * 16, pk);
+        if constexpr (kPSmem) {
+            const uint32_t chunk = p_row + (q >> 1) * kChunkBytes;
+            const uint32_t sw = (p_row >> 7 & 7u) << 4;               // (chunks are 1024-byte aligned, rows 128 bytes)
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+                st_shared_v4(chunk + ((((q & 1) * 4 + v) << 4) ^ sw), pk[4 * v], pk[4 * v + 1], pk[4 * v + 2], pk[4 * v + 3]);
+        } else {
+            tmem_st_x16(tS + q * 16, pk);
+        }
     };
     auto sum_chunk = [&](int q) {
 #pragma unroll
@@ -432,7 +471,9 @@ FA_DEVI void tree_pass(uint32_t tS, uint32_t tO, float c, float tau_raw, float b
             m_ref = mx;
         }
     }
+    if constexpr (kPSmem) take();
     if (!first_tile && __any_sync(0xffffffffu, alpha != 1.f)) {
+        if constexpr (kPSmem) tc_fence_after_sync();
 #pragma unroll 1
         for (int cc = 0; cc < DV / 32; ++cc) {
             uint32_t r[32];
@@ -443,37 +484,44 @@ FA_DEVI void tree_pass(uint32_t tS, uint32_t tO, float c, float tau_raw, float b
                 r[e] = __float_as_uint(__uint_as_float(r[e]) * alpha);
             tmem_st_x32(tO + cc * 32, reinterpret_cast<uint32_t(&)[32]>(r));
         }
+        if constexpr (kPSmem) tc_wait_st();
     }
+    // (the sums: under the exponentials where the hand-over can wait for them, else behind it, off the chain MMA -> softmax -> MMA)
     exp_chunk(1);
     emit_chunk(0);
+    if constexpr (kPSmem) sum_chunk(0);
     exp_chunk(2);
     emit_chunk(1);
-    emit_chunk(2);
-    tc_wait_st();
-    tc_fence_before_sync();
-    __syncwarp();
-    if (lane == 0) arrive_first();
+    if constexpr (kPSmem) sum_chunk(1);
+    if constexpr (!kPSmem) emit_chunk(2);
+    if constexpr (!kPSmem) {
+        tc_wait_st();
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) arrive_first();
+    }
     exp_chunk(3);
+    if constexpr (kPSmem) {
+        emit_chunk(2);
+        sum_chunk(2);
+    }
     emit_chunk(3);
-    tc_wait_st();
+    if constexpr (kPSmem) fence_proxy_async_smem();
+    else tc_wait_st();
     tc_fence_before_sync();
     __syncwarp();
     if (lane == 0) arrive_rest();
-    sum_chunk(0);
-    sum_chunk(1);
-    sum_chunk(2);
+    if constexpr (!kPSmem) {
+        sum_chunk(0);
+        sum_chunk(1);
+        sum_chunk(2);
+    }
     sum_chunk(3);
     l = l * alpha + ((sum_a.x + sum_a.y) + (sum_b.x + sum_b.y));
 }
 
 // ------------------------------------------------------------------ kernel
 
-#ifdef FA_TREE_TRACE
-__device__ long long g_tree_trace[148][4][256];
-#define TT(w, id) do { if (tt_n < 250) { g_tree_trace[blockIdx.x][w][tt_n++] = (static_cast<long long>(id) << 48) | (clock64() & 0xffffffffffffll); } } while (0)
-#else
-#define TT(w, id) do { } while (0)
-#endif
 template <int DQK, int DV, bool kE4m3>
 __global__ void __launch_bounds__((TreeCfg<DQK, DV, kE4m3>::kThreads), 1)
 fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
@@ -487,11 +535,8 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     Shared& sh = *reinterpret_cast<Shared*>(smem_raw + Cfg::kTileBytes);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t smem_base = smem_addr(smem_raw);
-    const uint32_t sQ = smem_base, sK = sQ + Cfg::kQSpace, sV = sK + NK * Cfg::kKBytes, sRaw = sV + NV * Cfg::kVBytes;
+    const uint32_t sQ = smem_base, sK = sQ + Cfg::kQSpace, sV = sK + NK * Cfg::kKBytes, sRaw = sV + NV * Cfg::kVStage, sP = sRaw + Cfg::kRaw * kChunkBytes;
 
-    int tt_n = 0;
-    (void)tt_n;
-    if (tid == 0) TT(0, 1);
     grid_launch_dependents();
     if ((smem_base & 1023u) != 0u) {          // uniform over the CTA; nothing has been set up yet
         grid_dependency_wait();
@@ -527,6 +572,7 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             mbar_init(smem_addr(&sh.s_full[t]), 1);
+            mbar_init(smem_addr(&sh.s_free[t]), 4);
             mbar_init(smem_addr(&sh.p_first[t]), 4);      // 4 softmax warps
             mbar_init(smem_addr(&sh.p_rest[t]), 4);
             mbar_init(smem_addr(&sh.o_final[t]), 1);
@@ -568,7 +614,6 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     }
     grid_dependency_wait();
 
-    if (tid == 0) TT(0, 2);
     auto seq_of = [&](int b, int& n, int& row0, int& len) {
         const DraftRows d = draft_rows(a.t.cu_seqlens, b, p.B, a.t.total, a.t.max_tokens, nullptr);
         n = d.count;
@@ -578,7 +623,6 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
-    if (tid == 352) TT(2, 21);
     const uint32_t tmem = sh.tmem_base;
     auto wait = [&](uint64_t& bar, uint32_t parity) -> bool { return tree_wait(bar, parity, &sh.wait); };
     // Part k for a warp as a whole; false at the end of the list or after a wait that ran out.
@@ -610,7 +654,6 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             if (e.t1 < 0) break;
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_addr(&sh.part_empty[k % NP]));
-            if ((tid & 127) == 0) TT(t, 3);
             const int nt = e.t1 - e.t0;
             const bool two = Cfg::kTwo && e.two;
             const int steps0 = two ? nt : (nt + 1) / 2, steps1 = two ? nt : nt / 2, steps = t == 0 ? steps0 : steps1;
@@ -631,18 +674,26 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 ok = __all_sync(0xffffffffu, ok && tree_wait_timed(sh.s_full[t], n_s & 1, &sh.wait, kSiteSoftmaxSFull));
                 if (!ok) break;
                 tc_fence_after_sync();
-                if ((tid & 127) == 0) TT(t, 4);
                 if constexpr (kE4m3) {
                     if (j == 0) {
                         c *= __uint_as_float(static_cast<uint32_t>(sh.q_shift[(n_q - 1) & 1][row]) << 23);
                         tau_raw = kRescaleThresholdLog2 / c;
                     }
                 }
+                // (P in shared memory: the scores are in registers; before P is written, the product of the step before has to be done)
+                auto take = [&]() {
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_addr(&sh.s_free[t]));
+                    if (j > 0) ok = tree_wait_timed(sh.o_final[t], (n_s & 1) ^ 1, &sh.wait, kSiteSoftmaxPFree);
+                    __syncwarp();
+                };
                 if (!warp_live) {            // (what P holds then meets rows that are not stored)
+                    if constexpr (Cfg::kPSmem) take();
                     tc_fence_before_sync();
                     __syncwarp();
                     if (lane == 0) {
-                        mbar_arrive(bar_pf);
+                        if constexpr (!Cfg::kPSmem) mbar_arrive(bar_pf);
                         mbar_arrive(bar_pr);
                     }
                     continue;
@@ -663,12 +714,9 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                     }
                     tc_wait_st();
                 }
-                if ((tid & 127) == 0) TT(t, masked ? 11 : 10);
-                tree_pass<DV, kE4m3>(tS, tO + 128 * t, c, tau_raw, Cfg::kBias, j == 0, m_ref, l, lane,
+                tree_pass<DV, kE4m3, Cfg::kPSmem>(tS, tO + 128 * t, sP + t * Cfg::kPBytes + row * 128, c, tau_raw, Cfg::kBias, j == 0, m_ref, l, lane, take,
                                      [&]() { mbar_arrive(bar_pf); }, [&]() { mbar_arrive(bar_pr); });
-                if ((tid & 127) == 0) TT(t, 5);
             }
-            if ((tid & 127) == 0) TT(t, 6);
             // ---- the part's result: sum and reference of a row that saw a key, O of one stream or of both
             const float off = m_ref == -INFINITY ? Cfg::kBias : Cfg::kBias - m_ref * c;
             float m = l > 0.f || l != l ? -off : -INFINITY;       // (a NaN goes through)
@@ -689,13 +737,13 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             const float norm = whole ? (any ? vs / l : 0.f) : 1.f;
             f0 *= norm;
             f1 *= norm;
-            if (steps0 > 0 && (!two || t == 0)) ok = ok && tree_wait_timed(sh.o_final[0], n_final[0] & 1, &sh.wait, kSiteEpiOFull);
-            if (steps1 > 0 && (!two || t == 1)) ok = ok && tree_wait_timed(sh.o_final[1], n_final[1] & 1, &sh.wait, kSiteEpiOFull);
-            n_final[0] += steps0 > 0;
-            n_final[1] += steps1 > 0;
+            // (with P in shared memory the barrier's phases are the steps, else the parts)
+            n_final[0] += Cfg::kPSmem ? steps0 : steps0 > 0;
+            n_final[1] += Cfg::kPSmem ? steps1 : steps1 > 0;
+            if (steps0 > 0 && (!two || t == 0)) ok = ok && tree_wait_timed(sh.o_final[0], (n_final[0] & 1) ^ 1, &sh.wait, kSiteEpiOFull);
+            if (steps1 > 0 && (!two || t == 1)) ok = ok && tree_wait_timed(sh.o_final[1], (n_final[1] & 1) ^ 1, &sh.wait, kSiteEpiOFull);
             ok = __all_sync(0xffffffffu, ok);
             tc_fence_after_sync();
-            if ((tid & 127) == 0) TT(t, 7);
             // columns [col0, col1) are this thread's: all of its own stream's, or half of both streams'
             const int col0 = two ? 0 : t * (DV / 2), col1 = two ? DV : col0 + DV / 2;
             const int hq = e.kvh * a.group + head;
@@ -767,7 +815,6 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             }
             // (both groups have read both accumulators, and each other's sums, at the barrier that the next part begins with)
             tc_fence_before_sync();
-            if ((tid & 127) == 0) TT(t, 8);
         }
     } else if (warp == 8) {
         // ============================================================ MMA issue, one thread for both streams
@@ -780,7 +827,8 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             constexpr int kPerTerm = kE4m3 ? DQK / 32 : DQK / 16, kSteps = kE4m3 ? Cfg::kTerms * kPerTerm : kPerTerm;      // of 32 bytes of a row
             const uint32_t q_lo0 = ((sQ & 0x3FFFFu) >> 4) | (1u << 16);
             const uint32_t k_lo0 = ((sK & 0x3FFFFu) >> 4) | (1u << 16);
-            const uint32_t v_lo0 = ((sV & 0x3FFFFu) >> 4) | ((static_cast<uint32_t>(kChunkBytes) >> 4) << 16);
+            const uint32_t v_lo0 = ((sV & 0x3FFFFu) >> 4) | ((static_cast<uint32_t>(Cfg::kVChunk) >> 4) << 16);
+            const uint32_t p_lo0 = ((sP & 0x3FFFFu) >> 4) | (1u << 16);
             auto desc = [](uint32_t lo) -> uint64_t { return (static_cast<uint64_t>(kDescHi) << 32) | lo; };
             auto koff = [](int ks) -> uint32_t { ks %= kPerTerm; return static_cast<uint32_t>(((ks / 4) * kChunkBytes + (ks % 4) * 32) >> 4); };
             auto qoff = [&](int ks) -> uint32_t { return koff(ks) + static_cast<uint32_t>(ks / kPerTerm * (Cfg::kKBytes >> 4)); };
@@ -789,7 +837,7 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 else mma_ss(tS, desc(q + qoff(ks)), desc(k + koff(ks)), kIdescQK, ks > 0 ? 1u : 0u);
             };
             int sk = 0, sv = 0, n_q = 0;       // stages, parts with queries so far
-            uint32_t ph_k = 0, ph_v = 0, ph_tail = 0, ph_p = 0;             // (of the last tiles, a bit per stage; of the steps, a bit per stream)
+            uint32_t ph_k = 0, ph_v = 0, ph_tail = 0, ph_p = 0, ph_s = 0;   // (of the last tiles, a bit per stage; of the steps, a bit per stream)
             bool two = false, tail = false;
             int nt = 0, k_tile = 0, v_tile = 0;                             // of the part: tiles, tile that stage sk / sv holds
             uint32_t pre_p = 0, pre_v = 0, pre_k = 0;                       // probes that succeeded for the next block
@@ -822,7 +870,7 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 }
                 const uint32_t parity = (ph_p >> t) & 1u;
                 const uint32_t tS = tmem + 128 * t, tO = tmem + 256 + 128 * t;
-                const uint32_t vlo = v_lo0 + sv * (Cfg::kVBytes >> 4), klo = k_lo0 + sk * (Cfg::kKBytes >> 4);
+                const uint32_t vlo = v_lo0 + sv * (Cfg::kVStage >> 4), klo = k_lo0 + sk * (Cfg::kKBytes >> 4);
                 if (!pre_p && !wait(sh.p_first[t], parity)) return false;
                 pre_p = pre_v = pre_k = 0u;
                 tc_fence_after_sync();
@@ -861,6 +909,45 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 if (v_done) step_v();
                 return true;
             };
+            // With P in shared memory: scores and products are two sequences, each over the streams in turn, and whichever can go on does.
+            auto ready = [&](uint64_t& bar, uint32_t parity) -> bool { return mbar_test_wait(smem_addr(&bar), parity); };
+            auto scores = [&](int t) {
+                ph_s ^= 1u << t;
+                tc_fence_after_sync();
+                const uint32_t klo = k_lo0 + sk * (Cfg::kKBytes >> 4);
+#pragma unroll
+                for (int ks = 0; ks < kSteps; ++ks) score(tmem + 128 * t, q_lo(t), klo, ks);
+                scores_done(t);
+            };
+            auto product = [&](int t, bool first) -> bool {
+                const uint32_t tO = tmem + 256 + 128 * t;
+                if constexpr (!kE4m3) {
+                    if ((!two || t == 0) && tail && v_tile == nt - 1) {
+                        if (!wait(sh.v_tail[sv], (ph_tail >> sv) & 1u)) return false;
+                        ph_tail ^= 1u << sv;
+                    }
+                }
+#pragma unroll
+                for (int part = 0; part < Cfg::kVParts; ++part) {
+                    if (part > 0 && !wait(sh.v_full[sv], ph_v)) return false;
+                    tc_fence_after_sync();
+                    const uint32_t vlo = v_lo0 + sv * (Cfg::kVStage >> 4), plo = p_lo0 + t * (Cfg::kPBytes >> 4);
+#pragma unroll
+                    for (int ks = 0; ks < Cfg::kVKeys / 16; ++ks) {
+                        const int at = part * (Cfg::kVKeys / 16) + ks;
+                        mma_ss(tO, desc(plo + static_cast<uint32_t>(((at / 4) * kChunkBytes + (at % 4) * 32) >> 4)), desc(vlo + ks * (2048 >> 4)), kIdescPV,
+                               at > 0 || !first ? 1u : 0u);
+                    }
+                    if (!two || t == 1) {
+                        tc_commit(smem_addr(&sh.v_empty[sv]));
+                        if (++sv == NV) { sv = 0; ph_v ^= 1u; }
+                    }
+                }
+                ph_p ^= 1u << t;
+                if (!two || t == 1) ++v_tile;
+                tc_commit(smem_addr(&sh.o_final[t]));
+                return true;
+            };
             bool ok = true;
             for (int k = 0; ok; ++k) {
                 ok = wait(sh.part_full[k % NP], (k / NP) & 1);
@@ -878,6 +965,23 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 if constexpr (kE4m3) ok = wait(sh.q_ready, n_q & 1);
                 else ok = wait(sh.q_full, n_q & 1);
                 ++n_q;
+                if constexpr (Cfg::kPSmem) {
+                    // (a stage that both streams use is waited for once: it is still full for the second)
+                    const int blocks = steps0 + steps1;
+                    int n_scores = 0, n_products = 0;              // blocks (j, t): number 2 j + t
+                    while (ok && n_products < blocks) {
+                        const int ts = n_scores & 1, tp = n_products & 1;
+                        if (n_products < n_scores && ready(sh.p_rest[tp], (ph_p >> tp) & 1u) && ready(sh.v_full[sv], ph_v)) {
+                            ok = product(tp, n_products < 2);
+                            ++n_products;
+                        }
+                        if (n_scores < blocks && ready(sh.s_free[ts], ((ph_s >> ts) & 1u) ^ 1u) && ready(sh.k_full[sk], ph_k)) {
+                            scores(ts);
+                            ++n_scores;
+                        }
+                        if (*static_cast<volatile uint32_t*>(&sh.wait.abort_flag)) ok = false;
+                    }
+                } else {
 #pragma unroll 1
                 for (int t = 0; t < 2; ++t) {
                     if (!ok || (t == 1 && steps1 == 0)) break;
@@ -893,6 +997,7 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
 #pragma unroll 1
                     for (int t = 0; t < 2 && ok; ++t)
                         if (t == 0 || j < steps1) ok = block(t, j, t == 0 ? steps0 : steps1);
+                }
                 }
             }
         }
@@ -914,7 +1019,6 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
         bool ok = true;
         TreePart e;
         for (int k = 0; ok && take_part(k, e); ++k) {
-            if (lane == 0 && !is_v) TT(3, 30);
             if (e.t0 == e.t1) continue;
             const int* const table = p.block_table + e.b * p.table_stride;
             if (is_v) {              // (its tiles are needed later than those of K)
@@ -951,7 +1055,6 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                         }
                     }
                 }
-                if (lane == 0 && !is_v) TT(3, 31);
                 const int from = ((t - first) << shift) + lane;
                 const int page = __shfl_sync(0xffffffffu, pages, from & 31), slot = __shfl_sync(0xffffffffu, slots, from & 31);
                 ok = __all_sync(0xffffffffu, wait(empty[s], parity));
@@ -1037,7 +1140,6 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
         w.len = __shfl_sync(0xffffffffu, len_mine, from);
         tree_walk_begin(w, li, blockIdx.x, share, total, start_seq, start_base);
         TreeJoin join{0, 0, 0, 0, 0, 0, 0, 0};
-        if (lane == 0) TT(2, 22);
         TreePart cur, e;
         e.t1 = 0;
         bool ok = true;
@@ -1060,7 +1162,6 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             }
             __syncwarp();
         };
-        if (lane == 0) TT(2, 23);
         for (int k = 0; ok; ++k) {
             cur = e;
             publish(k);
@@ -1079,7 +1180,7 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 if (!ok) break;
                 const int keys = cur.len - (cur.t1 - 1) * kTileN;
                 for (int i = lane; i < (kTileN - keys) * 8; i += 32) {
-                    const uint32_t to = sV + s * Cfg::kVBytes + (keys + (i >> 3)) * 128 + (i & 7) * 16;
+                    const uint32_t to = sV + s * Cfg::kVStage + (keys + (i >> 3)) * 128 + (i & 7) * 16;
 #pragma unroll
                     for (int cc = 0; cc < Cfg::kVChunks; ++cc) st_shared_v4(to + cc * kChunkBytes, 0, 0, 0, 0);
                 }
@@ -1114,7 +1215,6 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             const int row = lane & 4 ? (lane >> 3) ^ 5 : lane >> 3, piece = lane & 3;
             const uint32_t in_even = row * 128 + ((piece ^ row) << 4), in_odd = in_even ^ 64u;
             const uint32_t out0 = row * 128 + (((2 * piece) ^ row) << 4), out1 = out0 ^ 16u;
-            constexpr int kDeep = 4;          // loads ahead of the conversions: all of 64 columns
             const int q_row = tid & (kTileM - 1);
             int s = 0, r = 0, n_q = 0;
             uint32_t ph = 1, ph_r = 0;
@@ -1183,40 +1283,43 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 if (lane == 0) mbar_arrive(smem_addr(&sh.q_ready));
                 ++n_q;
                 for (int t = e.t0; ok && t < e.t1; ++t) {
-                    ok = wait(sh.raw_full[r], ph_r) && wait(sh.v_empty[s], ph);
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
-                    const uint32_t src = sRaw + r * kChunkBytes + mine * 1024, dst = sV + s * Cfg::kVBytes + mine * 1024;
+                    ok = __all_sync(0xffffffffu, wait(sh.raw_full[r], ph_r));
+                    const uint32_t src = sRaw + r * kChunkBytes + mine * 1024;
                     const int keys = e.len - t * kTileN;
                     // (values behind the sequence's end hold whatever the page held: 0 * NaN is NaN)
                     const bool zeros = keys < kTileN;
+                    constexpr int kDeep = Cfg::kVKeys / 32;          // loads ahead of the conversions: all of 64 columns of a stage
+#pragma unroll 1
+                    for (int part = 0; ok && part < Cfg::kVParts; ++part) {
+                        ok = __all_sync(0xffffffffu, wait(sh.v_empty[s], ph));
+                        if (!ok) break;
+                        const uint32_t dst = sV + s * Cfg::kVStage + mine * 1024;
 #pragma unroll
-                    for (int c = 0; c < DV / 64; ++c) {
-                        const uint32_t from = src + (c & 1 ? in_odd : in_even), to = dst + c * kChunkBytes;
-                        uint4 x[kDeep];
+                        for (int c = 0; c < DV / 64; ++c) {
+                            const uint32_t from = src + part * Cfg::kVKeys * 128 + (c & 1 ? in_odd : in_even), to = dst + c * Cfg::kVChunk;
+                            uint4 x[kDeep];
 #pragma unroll
-                        for (int g = 0; g < kDeep; ++g) x[g] = ld_shared_v4(from + g * 4096);
-                        if (zeros) {
+                            for (int g = 0; g < kDeep; ++g) x[g] = ld_shared_v4(from + g * 4096);
+                            if (zeros) {
 #pragma unroll
-                            for (int g = 0; g < kDeep; ++g)
-                                if ((4 * g + mine) * 8 + row >= keys) x[g] = make_uint4(0, 0, 0, 0);
+                                for (int g = 0; g < kDeep; ++g)
+                                    if (part * Cfg::kVKeys + (4 * g + mine) * 8 + row >= keys) x[g] = make_uint4(0, 0, 0, 0);
+                            }
+#pragma unroll
+                            for (int g = 0; g < kDeep; ++g) {
+                                const uint32_t at = to + g * 4096;
+                                st_shared_v4(at + out0, e4m3x2_to_f16x2(x[g].x), e4m3x2_to_f16x2(x[g].x >> 16), e4m3x2_to_f16x2(x[g].y),
+                                             e4m3x2_to_f16x2(x[g].y >> 16));
+                                st_shared_v4(at + out1, e4m3x2_to_f16x2(x[g].z), e4m3x2_to_f16x2(x[g].z >> 16), e4m3x2_to_f16x2(x[g].w),
+                                             e4m3x2_to_f16x2(x[g].w >> 16));
+                            }
                         }
-#pragma unroll
-                        for (int g = 0; g < kDeep; ++g) {
-                            const uint32_t at = to + g * 4096;
-                            st_shared_v4(at + out0, e4m3x2_to_f16x2(x[g].x), e4m3x2_to_f16x2(x[g].x >> 16), e4m3x2_to_f16x2(x[g].y),
-                                         e4m3x2_to_f16x2(x[g].y >> 16));
-                            st_shared_v4(at + out1, e4m3x2_to_f16x2(x[g].z), e4m3x2_to_f16x2(x[g].z >> 16), e4m3x2_to_f16x2(x[g].w),
-                                         e4m3x2_to_f16x2(x[g].w >> 16));
-                        }
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_addr(&sh.v_full[s]));
+                        if (++s == NV) { s = 0; ph ^= 1u; }
                     }
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) {
-                        mbar_arrive(smem_addr(&sh.v_full[s]));
-                        mbar_arrive(smem_addr(&sh.raw_empty[r]));
-                    }
-                    if (++s == NV) { s = 0; ph ^= 1u; }
+                    if (lane == 0) mbar_arrive(smem_addr(&sh.raw_empty[r]));
                     if (++r == NR) { r = 0; ph_r ^= 1u; }
                 }
             }
@@ -1226,7 +1329,6 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     // ---------------------------------------------------------------- teardown (all warps)
     tc_fence_before_sync();
     __syncthreads();
-    if (tid == 0) TT(0, 9);
     if (warp == 8) tmem_dealloc(tmem, 512);
 }
 

@@ -367,3 +367,48 @@ def test_refusals(handle):
     with pytest.raises(b.FaError):
         b.forward_paged_tree(handle, q, cache, table, lens_t, mask, max_tokens=5)
     ok(handle)
+
+
+@pytest.mark.parametrize("dqk,dv", [(64, 64), (128, 128), (192, 128)])
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+def test_a_wait_that_runs_out(dqk, dv, e4m3):
+    """The loading warps leave out their first V tile: the kernel returns with a status, and the next call of the handle is right."""
+    from paper_2609_21264_b200 import binding as b
+    lens, n = [700, 150], 20
+    k, v, table, lens_t, ks, vs = pool(lens, 16, 2, dqk, dv, e4m3, False, 21)
+    q = torch.randn(2 * n, 8, dqk, generator=torch.Generator().manual_seed(12)).to(torch.bfloat16).cuda()
+    cache = b.PagedCache(k, v, ks, vs)
+    h = b.fa_create(flags=b.FA_FLAG_DEBUG_DROP_V_LOAD, wait_limit_ms=20)
+    try:
+        b.forward_paged_tree(h, q, cache, table, lens_t, None)
+        torch.cuda.synchronize()
+        st, site = b.fa_last_status(h)
+        assert st == b.FA_ERR_DEVICE_TIMEOUT and site != 0 and b.fa_last_kernel_name(h).startswith("fa_tree")
+        b.fa_debug_set_drop_v_load(h, False)
+        o, lse = b.forward_paged_tree(h, q, cache, table, lens_t, None)
+        ok(h)
+        assert_attention(o, lse, *tree_reference(q, k, v, ks, vs, table, lens, [0, n, 2 * n], [torch.ones(n, n).tril() > 0] * 2, dqk ** -0.5))
+    finally:
+        b.fa_destroy(h)
+
+
+def test_little_scratch(handle):
+    """A handle with room for two partial results on one SM works on that one; with less, on none."""
+    from paper_2609_21264_b200 import binding as b
+    k, v, table, lens_t, _, _ = pool([700, 150], 16, 2, 128, 128, False, False, 22)
+    q = torch.randn(2 * 40, 8, 128, generator=torch.Generator().manual_seed(13)).to(torch.bfloat16).cuda()
+    cache = b.PagedCache(k, v)
+    ref = tree_reference(q, k, v, None, None, table, [700, 150], [0, 40, 80], [torch.ones(40, 40).tril() > 0] * 2, 128 ** -0.5)
+    for size, works in ((300 << 10, True), (1 << 20, True), (200 << 10, False)):
+        h = b.fa_create(scratch_bytes=size)
+        try:
+            if works:
+                o, lse = b.forward_paged_tree(h, q, cache, table, lens_t, None)
+                ok(h)
+                assert_attention(o, lse, *ref)
+            else:
+                with pytest.raises(b.FaError) as e:
+                    b.forward_paged_tree(h, q, cache, table, lens_t, None)
+                assert e.value.status == b.FA_ERR_UNSUPPORTED
+        finally:
+            b.fa_destroy(h)
