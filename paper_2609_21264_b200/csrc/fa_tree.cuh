@@ -1351,29 +1351,49 @@ fa_tree_join_kernel(const PagedParams p, const TreeArgs a) {
     const int in = row / a.list.row_heads, token = tc * a.list.row_tokens + in, head = hc * a.list.row_heads + row - in * a.list.row_heads;
     if (in >= a.list.row_tokens || token >= e.n || head >= a.group) return;
     auto slot = [&](int c) { return a.part + (c == 0 ? 2ll * cta + 1 : 2ll * (cta + c)) * tree_slot_floats(DV, kTwo); };
-    constexpr int kMl = (kTwo ? 2 : 1) * kTileM * DV;
-    float m = -INFINITY;
-#pragma unroll 4
-    for (int c = 0; c < e.pieces; ++c) m = fmaxf(m, __ldcg(slot(c) + kMl + t * 2 * kTileM + row));
+    constexpr int kMl = (kTwo ? 2 : 1) * kTileM * DV, kBatch = 2;
     const int col = (threadIdx.x >> 5) * 16;
     float4 y[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) y[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    float l = 0.f;
-#pragma unroll 2
-    for (int c = 0; c < e.pieces; ++c) {
-        const float* const s = slot(c);
-        const float mc = __ldcg(s + kMl + t * 2 * kTileM + row), lc = __ldcg(s + kMl + (t * 2 + 1) * kTileM + row);
-        const float4* const o = reinterpret_cast<const float4*>(s) + (t * (DV / 4) + col / 4) * kTileM + row;
-        const float f = mc == -INFINITY ? 0.f : ptx::exp2_approx(mc - m);
-        l = fmaf(f, lc, l);
+    // (under a running maximum, so that references, sums and values of two pieces are all loaded at once)
+    float m = -INFINITY, l = 0.f;
+#pragma unroll 1
+    for (int c = 0; c < e.pieces; c += kBatch) {
+        float mc[kBatch], lc[kBatch];
+        float4 x[kBatch][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float4 x = __ldcg(o + i * kTileM);
-            y[i].x = fmaf(f, x.x, y[i].x);
-            y[i].y = fmaf(f, x.y, y[i].y);
-            y[i].z = fmaf(f, x.z, y[i].z);
-            y[i].w = fmaf(f, x.w, y[i].w);
+        for (int q = 0; q < kBatch; ++q) {
+            mc[q] = -INFINITY;
+            lc[q] = 0.f;
+            if (c + q >= e.pieces) break;
+            const float* const s = slot(c + q);
+            mc[q] = __ldcg(s + kMl + t * 2 * kTileM + row);
+            lc[q] = __ldcg(s + kMl + (t * 2 + 1) * kTileM + row);
+            const float4* const o = reinterpret_cast<const float4*>(s) + (t * (DV / 4) + col / 4) * kTileM + row;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[q][i] = __ldcg(o + i * kTileM);
+        }
+        float top = m;
+#pragma unroll
+        for (int q = 0; q < kBatch; ++q) top = fmaxf(top, mc[q]);
+        const float keep = m == -INFINITY ? 0.f : ptx::exp2_approx(m - top);
+        m = top;
+        l *= keep;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { y[i].x *= keep; y[i].y *= keep; y[i].z *= keep; y[i].w *= keep; }
+#pragma unroll
+        for (int q = 0; q < kBatch; ++q) {
+            if (c + q >= e.pieces) break;
+            const float f = mc[q] == -INFINITY ? 0.f : ptx::exp2_approx(mc[q] - top);
+            l = fmaf(f, lc[q], l);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                y[i].x = fmaf(f, x[q][i].x, y[i].x);
+                y[i].y = fmaf(f, x[q][i].y, y[i].y);
+                y[i].z = fmaf(f, x[q][i].z, y[i].z);
+                y[i].w = fmaf(f, x[q][i].w, y[i].w);
+            }
         }
     }
     const bool any = l > 0.f || l != l;
