@@ -105,10 +105,8 @@ _I64x4 = ctypes.c_int64 * 4
 _I64x8 = ctypes.c_int64 * 8
 _I64x12 = ctypes.c_int64 * 12
 _SEQS_SIZE = ctypes.sizeof(fa_paged_seqs)
-_POSITIONS_SIZE = ctypes.sizeof(fa_positions)
-_TREE_SIZE = ctypes.sizeof(fa_tree)
-_INT_MAX = 2 ** 31 - 1
 _lib = None
+_calls = None
 
 
 def library_path() -> str:
@@ -192,6 +190,20 @@ def load():
     lib.fa_noalloc_last_status.argtypes = [ctypes.POINTER(ctypes.c_uint32)]
     _lib = lib
     return lib
+
+
+def _native():
+    """The extension module with the checks and outputs of the calls on drafted tokens (csrc/fa_calls.cpp), bound to the library."""
+    global _calls
+    import torch  # noqa: F401  (its libraries have to be there)
+    lib = load()
+    if not os.path.exists(_build.CALLS_PATH):
+        raise ImportError("extension module %s is missing; run `python -m paper_2609_21264_b200.build`" % _build.CALLS_PATH)
+    from . import _fa_calls
+    _fa_calls.bind(*[ctypes.cast(f, ctypes.c_void_p).value for f in (lib.fa_device, lib.fa_tree_layout, lib.fa_append_paged_at,
+                                                                     lib.fa_forward_paged_tree, lib.fa_compact_paged, lib.fa_copy_pages)])
+    _calls = _fa_calls
+    return _calls
 
 
 def fa_strerror(status: int) -> str:
@@ -542,7 +554,7 @@ class PagedCache:
                                 k.data_ptr(), v.data_ptr(), k.shape[0], k.shape[2], k.shape[1], k.shape[3], v.shape[3], 0,
                                 *strides,
                                 None if k_scale is None else k_scale.data_ptr(), None if v_scale is None else v_scale.data_ptr())
-        self.address = ctypes.addressof(self.c)
+        self.address, self.index, self.count = ctypes.addressof(self.c), k.device.index, 1
 
 
 class PagedCaches:
@@ -553,7 +565,7 @@ class PagedCaches:
         caches = list(caches)
         if not caches or any(c.device != caches[0].device for c in caches):
             raise ValueError("caches must be PagedCache objects on one device, at least one")
-        self.caches, self.device, self.count = caches, caches[0].device, len(caches)
+        self.caches, self.device, self.index, self.count = caches, caches[0].device, caches[0].index, len(caches)
         self.c = (fa_paged_cache * self.count)(*[c.c for c in caches])
         self.address = ctypes.addressof(self.c)
 
@@ -570,13 +582,14 @@ class Rope:
         self.cos_sin, self.device, self.span = cos_sin, cos_sin.device, int(span)
         self.offset, self.interleaved = int(offset), int(bool(interleaved))
         self.structs = {}                 # by span
-        self.axes, self.axis_of_pair = 1, None
+        self.axes, self.axis_of_pair, self.axis_address, self.index = 1, None, None, cos_sin.device.index
         if axis_of_pair is not None:
             numbers = [int(a) for a in axis_of_pair]
             if len(numbers) != cos_sin.shape[1] // 2 or any(not 0 <= a < FA_MAX_AXES for a in numbers):
                 raise ValueError("axis_of_pair must be dim / 2 numbers from 0 to %d" % (FA_MAX_AXES - 1))
             self.axes = max(numbers) + 1
             self.axis_of_pair = (ctypes.c_uint8 * len(numbers))(*numbers)
+            self.axis_address = ctypes.addressof(self.axis_of_pair)
 
     def struct_for(self, dqk: int) -> int:
         """Address of the C structure for heads of dqk dimensions."""
@@ -627,22 +640,6 @@ def _offsets(cu_seqlens, B, device):
     return cu_seqlens.data_ptr()
 
 
-def _most_tokens(max_tokens, cu_seqlens, total, B):
-    """The largest number of drafts of a sequence."""
-    if max_tokens > 0:
-        return int(max_tokens)
-    if cu_seqlens is not None or max_tokens < 0:
-        raise ValueError("max_tokens is needed with cu_seqlens")
-    return max(1, total // max(1, B))
-
-
-def _check_mask(mask, total, words, device):
-    import torch
-    if (mask.dtype is not torch.int32 or mask.device != device or mask.dim() != 2 or mask.shape[0] != total or mask.shape[1] < words or
-            (mask.shape[1] > 1 and mask.stride(1) != 1) or (total > 1 and mask.stride(0) < words)):
-        raise ValueError("mask must be int32 of shape [tokens, %d or more], its rows contiguous and apart" % words)
-
-
 def _rows(t, cache, d, what):
     """Tokens, heads and (token, head) strides of a [tokens, heads, d] bf16 tensor on the cache's device."""
     import torch
@@ -675,6 +672,14 @@ def append_paged(h, k, v, cache: PagedCache, block_table, seq_lens, *, cu_seqlen
     int32): the rows of the rotation table, where they do not follow from the slots (drafted trees, pictures).
     """
     import torch
+    if positions is not None:
+        if rope is None:
+            raise ValueError("positions without a rotation")
+        r = (_calls or _native()).append_at(h, cache.address, cache.index, cache.Hkv, cache.dqk, cache.dv, k, v, block_table, seq_lens, cu_seqlens, q,
+                                            q_out, rope.struct_for(cache.dqk), rope.index, rope.axes, rope.axis_address, positions)
+        if r.__class__ is int:
+            raise FaError(r, "fa_append_paged_at")
+        return r
     seqs = _seqs(h, cache, block_table, seq_lens)
     total, Hk, kt, kh = _rows(k, cache, cache.dqk, "k")
     Tv, Hv, vt, vh = _rows(v, cache, cache.dv, "v")
@@ -704,23 +709,8 @@ def append_paged(h, k, v, cache: PagedCache, block_table, seq_lens, *, cu_seqlen
         raise ValueError("q_out without q")
     strides = _I64x8(kt, kh, vt, vh, qt, qh, ot, oh)
     at = ctypes.addressof(strides)
-    if positions is None:
-        st = _lib.fa_append_paged(h, cache.address, ctypes.addressof(seqs), cu_ptr, total, k.data_ptr(), v.data_ptr(), q_ptr, qo_ptr, Hq,
-                                  at, at + 16, at + 32, at + 48, rope_ptr, _raw_stream(cache.device))
-    else:
-        if rope is None:
-            raise ValueError("positions without a rotation")
-        one = positions.dim() == 1
-        if (positions.dtype is not torch.int32 or positions.device != cache.device or positions.dim() not in (1, 2) or
-                positions.shape[-1] != total or (total > 1 and positions.stride(-1) != 1)):
-            raise ValueError("positions must be int32 of shape [T] or [axes, T] on the cache's device, contiguous along the tokens")
-        axes = 1 if one else positions.shape[0]
-        if axes < rope.axes or not 1 <= axes <= FA_MAX_AXES:
-            raise ValueError("positions must have the %d to %d axes that turn the pairs" % (rope.axes, FA_MAX_AXES))
-        p = fa_positions(_POSITIONS_SIZE, axes, positions.data_ptr(), total if axes == 1 else positions.stride(0),
-                         None if rope.axis_of_pair is None else ctypes.addressof(rope.axis_of_pair))
-        st = _lib.fa_append_paged_at(h, cache.address, ctypes.addressof(seqs), cu_ptr, total, k.data_ptr(), v.data_ptr(), q_ptr, qo_ptr, Hq,
-                                     at, at + 16, at + 32, at + 48, rope_ptr, ctypes.addressof(p), _raw_stream(cache.device))
+    st = _lib.fa_append_paged(h, cache.address, ctypes.addressof(seqs), cu_ptr, total, k.data_ptr(), v.data_ptr(), q_ptr, qo_ptr, Hq,
+                              at, at + 16, at + 32, at + 48, rope_ptr, _raw_stream(cache.device))
     if st != FA_OK:
         raise FaError(st, "fa_append_paged")
     return q_out
@@ -734,31 +724,10 @@ def tree_layout(h, parents, seq_lens, *, cu_seqlens=None, max_tokens: int = 0, m
     of drafts of a sequence (0: T / B).  Returns (mask [T, ceil(max_tokens / 32)] int32, positions [T] int32), new tensors where none
     are given (rows behind the last sequence stay as they were).
     """
-    import torch
-    i32, device = torch.int32, parents.device
-    if parents.dtype is not i32 or not parents.is_cuda or parents.dim() != 1 or not parents.is_contiguous():
-        raise ValueError("parents must be a contiguous 1-D int32 CUDA tensor")
-    if seq_lens.dtype is not i32 or seq_lens.device != device or seq_lens.dim() != 1 or not seq_lens.is_contiguous():
-        raise ValueError("seq_lens must be a contiguous 1-D int32 tensor on parents' device")
-    if load().fa_device(h) != device.index:
-        raise ValueError("the handle belongs to another device than the tensors")
-    total, B = parents.shape[0], seq_lens.shape[0]
-    cu_ptr = _offsets(cu_seqlens, B, device)
-    most = _most_tokens(max_tokens, cu_seqlens, total, B)
-    words = (most + 31) // 32
-    if mask is None:
-        mask = parents.new_empty((total, words))
-    else:
-        _check_mask(mask, total, words, device)
-    if positions is None:
-        positions = torch.empty_like(parents)
-    elif positions.dtype is not i32 or positions.device != device or positions.shape != (total,) or not positions.is_contiguous():
-        raise ValueError("positions must be a contiguous int32 tensor of one number per token")
-    st = _lib.fa_tree_layout(h, parents.data_ptr(), cu_ptr, total, B, seq_lens.data_ptr(), most, mask.data_ptr(),
-                             mask.stride(0) if total > 1 else words, positions.data_ptr(), _raw_stream(device))
-    if st != FA_OK:
-        raise FaError(st, "fa_tree_layout")
-    return mask, positions
+    r = (_calls or _native()).tree_layout(h, parents, seq_lens, cu_seqlens, max_tokens, mask, positions)
+    if r.__class__ is int:
+        raise FaError(r, "fa_tree_layout")
+    return r
 
 
 def _paged_out(q, cache, seqs, out):
@@ -802,34 +771,11 @@ def forward_paged_tree(h, q, cache: PagedCache, block_table, seq_lens, mask, *, 
     gives each sequence's rows (None: T / B each), max_tokens is the largest number of drafts of a sequence (0: T / B).  Returns
     (O [T, Hq, dv], lse [Hq, T] fp32 or None); rows behind the last sequence are not written.
     """
-    import torch
-    seqs = _seqs(h, cache, block_table, seq_lens)
-    T, Hq, qt, qh = _rows(q, cache, cache.dqk, "q")
-    B = seqs.B
-    if T and (B == 0 or cu_seqlens is None and T % B):
-        raise ValueError("q must hold the same number of tokens for every sequence, or cu_seqlens say how many")
-    cu_ptr = _offsets(cu_seqlens, B, cache.device)
-    most = _most_tokens(max_tokens, cu_seqlens, T, B)
-    tree = fa_tree(_TREE_SIZE, most, cu_ptr, None, 0)
-    if mask is not None:
-        _check_mask(mask, T, (most + 31) // 32, cache.device)
-        tree.mask = mask.data_ptr()
-        tree.mask_stride = mask.stride(0) if T > 1 else (most + 31) // 32
-    if out is None:
-        out = _new(q, T, Hq, cache.dv)
-        ot, oh = Hq * cache.dv, cache.dv
-    else:
-        To, Ho, ot, oh = _rows(out, cache, cache.dv, "out")
-        if To != T or Ho != Hq:
-            raise ValueError("out must have shape %s" % ((T, Hq, cache.dv),))
-    lse = q.new_empty((Hq, T), dtype=torch.float32) if want_lse else None
-    strides = _I64x4(qt, qh, ot, oh)
-    at = ctypes.addressof(strides)
-    st = _lib.fa_forward_paged_tree(h, cache.address, ctypes.addressof(seqs), ctypes.addressof(tree), T, q.data_ptr(), out.data_ptr(),
-                                    None if lse is None else lse.data_ptr(), Hq, scale, at, at + 16, _raw_stream(cache.device))
-    if st != FA_OK:
-        raise FaError(st, "fa_forward_paged_tree")
-    return out, lse
+    r = (_calls or _native()).paged_tree(h, cache.address, cache.index, cache.dqk, cache.dv, q, block_table, seq_lens, mask, cu_seqlens, max_tokens,
+                                         scale, out, want_lse)
+    if r.__class__ is int:
+        raise FaError(r, "fa_forward_paged_tree")
+    return r
 
 
 def compact_paged(h, caches, block_table, seq_lens, keep, keep_counts, *, cu_seqlens=None, total: int = 0, new_lens=None):
@@ -839,41 +785,18 @@ def compact_paged(h, caches, block_table, seq_lens, keep, keep_counts, *, cu_seq
     [B, most] int32 holds the accepted drafts' numbers in rising order, keep_counts [B] int32 how many.  Returns the new lengths [B]
     int32 (a new tensor where none is given; not seq_lens itself).
     """
-    import torch
-    i32, device = torch.int32, caches.device
-    seqs = _seqs(h, caches, block_table, seq_lens)
-    B = seqs.B
-    if (keep.dtype is not i32 or keep.device != device or keep.dim() != 2 or keep.shape[0] != B or keep.shape[1] < 1 or
-            (keep.shape[1] > 1 and keep.stride(1) != 1) or (B > 1 and keep.stride(0) < keep.shape[1])):
-        raise ValueError("keep must be int32 of shape [B, most], its rows contiguous and apart")
-    if keep_counts.dtype is not i32 or keep_counts.device != device or keep_counts.shape != (B,) or not keep_counts.is_contiguous():
-        raise ValueError("keep_counts must be a contiguous int32 tensor of B numbers")
-    if new_lens is None:
-        new_lens = torch.empty_like(seq_lens)
-    elif (new_lens.dtype is not i32 or new_lens.device != device or new_lens.shape != (B,) or not new_lens.is_contiguous() or
-          (B and new_lens.data_ptr() == seq_lens.data_ptr())):
-        raise ValueError("new_lens must be a contiguous int32 tensor of B numbers, another one than seq_lens")
-    st = _lib.fa_compact_paged(h, caches.address, getattr(caches, "count", 1), ctypes.addressof(seqs), _offsets(cu_seqlens, B, device), int(total)
-                               if cu_seqlens is None else _INT_MAX, keep.data_ptr(), keep.stride(0) if B > 1 else keep.shape[1],
-                               keep_counts.data_ptr(), keep.shape[1], new_lens.data_ptr(), _raw_stream(device))
-    if st != FA_OK:
-        raise FaError(st, "fa_compact_paged")
-    return new_lens
+    r = (_calls or _native()).compact(h, caches.address, caches.count, caches.index, block_table, seq_lens, keep, keep_counts, cu_seqlens, total,
+                                      new_lens)
+    if r.__class__ is int:
+        raise FaError(r, "fa_compact_paged")
+    return r
 
 
 def copy_pages(h, caches, src, dst, *, slots=None):
     """Page dst[i] receives what page src[i] holds, in one or several caches (PagedCache, PagedCaches): int32 tensors of one length on their
     device, negative entries are skipped.  slots (int32, the same length): how many leading slots of each page; None: all."""
-    import torch
-    device = caches.device
-    for t in (src, dst) if slots is None else (src, dst, slots):
-        if t.dtype is not torch.int32 or t.device != device or t.dim() != 1 or t.shape != src.shape or not t.is_contiguous():
-            raise ValueError("src, dst and slots must be contiguous 1-D int32 tensors of one length on the caches' device")
-    if _lib.fa_device(h) != device.index:
-        raise ValueError("the handle belongs to another device than the caches")
-    st = _lib.fa_copy_pages(h, caches.address, getattr(caches, "count", 1), src.data_ptr(), dst.data_ptr(),
-                            None if slots is None else slots.data_ptr(), src.shape[0], _raw_stream(device))
-    if st != FA_OK:
+    st = (_calls or _native()).copy_pages(h, caches.address, caches.count, caches.index, src, dst, slots)
+    if st is not None:
         raise FaError(st, "fa_copy_pages")
 
 

@@ -8,6 +8,7 @@ import subprocess
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libfa_b200.so")
+CALLS_PATH = os.path.join(_HERE, "_fa_calls.so")
 SOURCES = ("fa_api.cu", "fa_noalloc.cu", "fa_paged.cu", "fa_drafts.cu", "fa_tree.cu")
 NVCC_FLAGS = ("-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-shared", "-Xcompiler", "-fPIC", "-Xptxas", "-v", "--threads", "0")
@@ -34,7 +35,8 @@ def is_stale() -> bool:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile csrc/*.cu into libfa_b200.so next to this file; returns its path."""
+    """Compile csrc/*.cu into libfa_b200.so next to this file (and the Python calls of csrc/fa_calls.cpp); returns its path."""
+    build_calls(force)
     if not force and not is_stale():
         return LIB_PATH
     tmp = LIB_PATH + ".tmp.%d" % os.getpid()
@@ -47,6 +49,29 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if verbose:
         print(res.stdout + res.stderr)
     return LIB_PATH
+
+
+def build_calls(force: bool = False) -> str:
+    """Compile csrc/fa_calls.cpp into the extension module _fa_calls.so next to this file; returns its path."""
+    sources = max(os.path.getmtime(os.path.join(CSRC, "fa_calls.cpp")), os.path.getmtime(os.path.join(os.path.dirname(_HERE), "include", "fa.h")))
+    if not force and os.path.exists(CALLS_PATH) and os.path.getmtime(CALLS_PATH) >= sources:
+        return CALLS_PATH
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    tmp = CALLS_PATH + ".tmp.%d" % os.getpid()
+    cuda = os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include")
+    includes = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
+                sysconfig.get_paths()["include"], cuda]
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI),
+           *["-I" + i for i in includes], "-o", tmp, os.path.join(CSRC, "fa_calls.cpp"), "-L" + os.path.join(root, "lib"),
+           "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError("%s failed:\n" % cmd[0] + res.stdout + res.stderr)
+    os.replace(tmp, CALLS_PATH)
+    return CALLS_PATH
 
 
 if __name__ == "__main__":

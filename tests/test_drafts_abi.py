@@ -2,6 +2,7 @@
 import ctypes
 import os
 import re
+import types
 
 import pytest
 import torch
@@ -38,19 +39,28 @@ def test_host_tensors_and_wrong_types_are_refused():
     x = torch.zeros(4, dtype=torch.int32)
     with pytest.raises(ValueError):
         b.tree_layout(0, x, x)
+    with pytest.raises(TypeError):
+        b.tree_layout(0, [1, 2], x)
+    with pytest.raises(ValueError):
+        b.tree_layout(0, None, x)
     with pytest.raises(ValueError):
         b.PagedCaches([])
-    with pytest.raises(ValueError):
-        b._check_mask(x, 4, 1, x.device)
-    for mask, words in ((x[:, None].float(), 1), (x[:, None], 2), (x[:3, None], 1), (x[:2, None].expand(2, 2), 2), (x.view(2, 2).t(), 2)):
+    cache = types.SimpleNamespace(address=0, index=0, count=1, dqk=64, dv=64, Hkv=1)
+    q = torch.zeros(4, 1, 64, dtype=torch.bfloat16)
+    for call in (lambda: b.forward_paged_tree(0, q, cache, x.view(2, 2), x, None), lambda: b.compact_paged(0, cache, x.view(2, 2), x, x.view(2, 2), x),
+                 lambda: b.copy_pages(0, cache, x, x), lambda: b.append_paged(0, q, q, cache, x.view(2, 2), x, positions=x)):
         with pytest.raises(ValueError):
-            b._check_mask(mask, mask.shape[0] if mask.shape[0] != 3 else 4, words, x.device)
-    b._check_mask(x.view(2, 2), 2, 2, x.device)
+            call()
     assert b._offsets(None, 3, x.device) is None and b._offsets(x, 3, x.device) == x.data_ptr()
     for bad in (x[:3], x.long(), torch.zeros(8, dtype=torch.int32)[::2]):
         with pytest.raises(ValueError):
             b._offsets(bad, 3, x.device)
-    assert b._most_tokens(0, None, 12, 4) == 3 and b._most_tokens(7, None, 12, 4) == 7 and b._most_tokens(0, None, 0, 0) == 1
-    for args in ((0, x, 12, 4), (-1, None, 12, 4)):
+
+
+def test_the_calls_module_asks_for_its_arguments():
+    calls = b._native()
+    for f in (calls.tree_layout, calls.append_at, calls.paged_tree, calls.compact, calls.copy_pages):
         with pytest.raises(ValueError):
-            b._most_tokens(*args)
+            f()
+        with pytest.raises((TypeError, ValueError)):
+            f(*["no"] * 18)
