@@ -105,6 +105,7 @@ _I64x4 = ctypes.c_int64 * 4
 _I64x8 = ctypes.c_int64 * 8
 _I64x12 = ctypes.c_int64 * 12
 _SEQS_SIZE = ctypes.sizeof(fa_paged_seqs)
+_CACHE_SIZE = ctypes.sizeof(fa_paged_cache)
 _lib = None
 _calls = None
 
@@ -534,27 +535,32 @@ class PagedCache:
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
         import torch
-        if k.dim() != 4 or v.dim() != 4 or k.shape[:3] != v.shape[:3] or k.dtype != v.dtype:
+        ks, vs, dtype, device = k.shape, v.shape, k.dtype, k.device
+        if len(ks) != 4 or len(vs) != 4 or ks[:3] != vs[:3] or dtype != v.dtype:
             raise ValueError("k and v must be 4-D tensors of one dtype with the same pages, heads and page size")
-        if k.dtype not in (torch.bfloat16, torch.float8_e4m3fn, torch.uint8):
+        if dtype not in (torch.bfloat16, torch.float8_e4m3fn, torch.uint8):
             raise ValueError("the cache must be bf16 or e4m3")
-        if not k.is_cuda or v.device != k.device or k.stride(3) != 1 or v.stride(3) != 1:
+        kt, vt = k.stride(), v.stride()
+        if not k.is_cuda or v.device != device or kt[3] != 1 or vt[3] != 1:
             raise ValueError("k and v must be on one CUDA device, their last dimension contiguous")
+        bf16 = dtype is torch.bfloat16
         for t in (k_scale, v_scale):
-            if t is not None and (t.dtype != torch.float32 or t.device != k.device or not t.is_contiguous() or
-                                  tuple(t.shape) != (k.shape[1],) or k.dtype == torch.bfloat16):
+            if t is not None and (t.dtype != torch.float32 or t.device != device or not t.is_contiguous() or
+                                  tuple(t.shape) != (ks[1],) or bf16):
                 raise ValueError("scales are contiguous fp32 tensors of Hkv values on the cache's device, for e4m3 caches only")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         load()                            # the calls that take a cache rely on the library being there
-        self.device, self.Hkv, self.dqk, self.dv = k.device, k.shape[1], k.shape[3], v.shape[3]
-        # (a single page or head may have any stride, the library wants a valid one: whole 16-byte units)
-        unit = 16 // k.element_size()
-        strides = [_I64x3(*[s if n > 1 else max(t.shape[3], -(-s // unit) * unit) for s, n in zip(t.stride(), t.shape[:3])]) for t in (k, v)]
-        self.c = fa_paged_cache(ctypes.sizeof(fa_paged_cache), FA_CACHE_BF16 if k.dtype == torch.bfloat16 else FA_CACHE_E4M3,
-                                k.data_ptr(), v.data_ptr(), k.shape[0], k.shape[2], k.shape[1], k.shape[3], v.shape[3], 0,
-                                *strides,
+        pages, self.Hkv, page, self.dqk = ks
+        self.device, self.dv = device, vs[3]
+        kt, vt = kt[:3], vt[:3]
+        if pages == 1 or self.Hkv == 1 or page == 1:
+            # (a single page or head may have any stride, the library wants a valid one: whole 16-byte units)
+            unit = 8 if bf16 else 16
+            kt, vt = ([x if n > 1 else max(d, -(-x // unit) * unit) for x, n in zip(st, ks)] for st, d in ((kt, self.dqk), (vt, self.dv)))
+        self.c = fa_paged_cache(_CACHE_SIZE, FA_CACHE_BF16 if bf16 else FA_CACHE_E4M3, k.data_ptr(), v.data_ptr(), pages, page, self.Hkv,
+                                self.dqk, self.dv, 0, _I64x3(*kt), _I64x3(*vt),
                                 None if k_scale is None else k_scale.data_ptr(), None if v_scale is None else v_scale.data_ptr())
-        self.address, self.index, self.count = ctypes.addressof(self.c), k.device.index, 1
+        self.address, self.index, self.count = ctypes.addressof(self.c), device.index, 1
 
 
 class PagedCaches:

@@ -74,16 +74,19 @@ __host__ __device__ inline TreeUnits tree_units(const TreeList& li, int n, int l
 }
 __host__ __device__ inline int tree_head_units(const TreeUnits& u) { return u.pairs * u.pair + u.single; }
 
-// What a batch is, as far as the rules below ask: row blocks, key tiles of its longest and shortest sequence, whether blocks of one and of
+// What a batch is, as far as the rules below ask: row blocks, units, key tiles of its longest and shortest sequence, whether blocks of one and of
 // two row tiles are among it.
-struct TreeBatch { int blocks, longest, shortest, kinds; };
-constexpr int kTreeWholeTiles = 4;
-// Small batches.  A join costs about as much as two rounds of tiles: where there is a CTA for every block and none has more than four
-// tiles, all count the same and nothing is split.  Where there are two CTAs for every block at least and all are equally long, their pieces
-// are equally long too, and a CTA has one.  Returns the share (0: what the total gives).
+struct TreeBatch { int blocks, units, longest, shortest, kinds; };
+constexpr int kTreeSplitCost = 3;
+// Small batches.  Where there is a CTA for every block, the longest block, unsplit, is what the call takes; split, it takes an equal share and
+// what the join of the pieces costs, about three tiles' time.  Where that is not less, all blocks count the same and nothing is split (16
+// sequences of 1003 keys, 8 K/V heads, 8 drafts: 18.3 us, against 21.0 split; one of 500 keys, 26 drafts: 12.2 split, against 13.7).  Where
+// there are two CTAs for every block at least and all are equally long, their pieces are equally long too, and a CTA has one.
+// Returns the share (0: what the total gives).
 __host__ __device__ inline int tree_rules(TreeList& li, const TreeBatch& b, int ctas) {
-    if (b.blocks <= ctas && b.longest <= kTreeWholeTiles) {
-        li.w1 = li.w2;
+    const int w = b.kinds & 1 ? li.w2 : li.w1;
+    if (b.blocks <= ctas && li.cost + w * (b.longest - kTreeSplitCost) <= b.units / ctas) {
+        li.w1 = li.w2 = w;
         li.pad = b.longest;
         return li.cost + li.w2 * li.pad;
     }
@@ -1085,7 +1088,7 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
         TreeList li = a.list;
         const int chunk = (p.B + 31) >> 5, b_first = min(p.B, lane * chunk), b_last = min(p.B, b_first + chunk);
         int n_mine = 0, row_mine = 0, len_mine = 0;          // the lane's last sequence
-        TreeBatch batch{0, 0, 0x7fffffff, 0};
+        TreeBatch batch{0, 0, 0, 0x7fffffff, 0};
         int mine = 0;
 #pragma unroll 4
         for (int b = b_first; b < b_last; ++b) {
@@ -1100,6 +1103,7 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             }
         }
         batch.blocks = __reduce_add_sync(0xffffffffu, batch.blocks);
+        batch.units = __reduce_add_sync(0xffffffffu, mine);
         batch.longest = __reduce_max_sync(0xffffffffu, batch.longest);
         batch.shortest = __reduce_min_sync(0xffffffffu, batch.shortest);
         batch.kinds = __reduce_or_sync(0xffffffffu, batch.kinds);
