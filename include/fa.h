@@ -643,6 +643,16 @@ fa_status fa_forward_paged_tree(fa_handle* h, const fa_paged_cache* cache, const
                                 const int64_t* q_strides, const int64_t* o_strides, void* stream);
 
 /*
+ * How fa_forward_paged_tree would deal out a batch, as fa_plan_paged does for fa_forward_paged: a pure host function, seqs->seq_lens and
+ * tree->cu_seqlens are HOST arrays here (no other pointer is looked at).  out->rows_per_block is a row tile's rows (tokens times heads of the
+ * group, 128 at most), out->row_blocks the row tiles of a sequence of max_tokens, part_cost the units that a row block counts beside its
+ * tiles of 128 keys.  A piece's row_block is the first row tile of its block (blocks have two where a head size has room for them and the
+ * sequence has them); slot 2 * cta + 1 holds the first piece of a block, 2 * cta any other.
+ */
+fa_status fa_plan_paged_tree(int num_sms, const fa_config* cfg, const fa_paged_cache* cache, const fa_paged_seqs* seqs, const fa_tree* tree,
+                             int total, int Hq, fa_paged_plan_info* out, fa_paged_piece* pieces, int max_pieces);
+
+/*
  * The accepted drafts move up: of the n drafts of sequence b those with the numbers keep[b][0] < keep[b][1] < ... (keep_counts[b] of
  * them, at most max_keep <= FA_TREE_MAX_TOKENS; keep is a DEVICE int32 array with rows keep_stride elements apart) go to the slots of
  * the sequence's first drafts, in `caches` (HOST array of num_caches structures that differ in k and v alone: the caches of a model's

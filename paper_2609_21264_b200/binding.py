@@ -36,7 +36,8 @@ EXPORTS = ("fa_create", "fa_forward", "fa_forward_strided", "fa_forward_varlen",
            "fa_strerror", "fa_launch_count", "fa_last_kernel_name", "fa_last_kv_splits",
            "fa_forward_split_noalloc", "fa_noalloc_scratch_bytes", "fa_noalloc_last_status", "fa_debug_set_drop_v_load",
            "fa_append_paged", "fa_forward_paged", "fa_forward_paged_diff", "fa_forward_diff", "fa_device",
-           "fa_plan_paged", "fa_append_paged_at", "fa_tree_layout", "fa_forward_paged_tree", "fa_compact_paged", "fa_copy_pages")
+           "fa_plan_paged", "fa_append_paged_at", "fa_tree_layout", "fa_forward_paged_tree", "fa_compact_paged", "fa_copy_pages",
+           "fa_plan_paged_tree")
 FA_CACHE_BF16 = 0
 FA_CACHE_E4M3 = 1
 FA_PAGED_MAX_SQ = 16
@@ -185,6 +186,8 @@ def load():
     lib.fa_forward_diff.argtypes = [vp] * 5 + [i32] * 8 + [f32] + [vp] * 6
     lib.fa_plan_paged.restype = i32
     lib.fa_plan_paged.argtypes = [i32, vp, vp, vp, i32, i32, i32, vp, vp, i32]
+    lib.fa_plan_paged_tree.restype = i32
+    lib.fa_plan_paged_tree.argtypes = [i32, vp, vp, vp, vp, i32, i32, vp, vp, i32]
     lib.fa_device.restype = i32
     lib.fa_device.argtypes = [vp]
     lib.fa_noalloc_last_status.restype = i32
@@ -458,6 +461,30 @@ def fa_plan_paged(num_sms, seq_lens, Hq, Hkv, Sq, dqk, dv, *, page_size=16, max_
                                   ctypes.addressof(out), ctypes.addressof(pieces), count)
         if st != FA_OK:
             raise FaError(st, "fa_plan_paged")
+    as_dict = lambda x: {f: getattr(x, f) for f, _ in x._fields_ if f != "reserved"}
+    return as_dict(out), [as_dict(x) for x in pieces[:out.pieces]]
+
+
+def fa_plan_paged_tree(num_sms, seq_lens, counts, Hq, Hkv, dqk, dv, *, max_tokens=0, page_size=16, max_pages=0, e4m3=False, scratch_bytes=0):
+    """How fa_forward_paged_tree deals out sequences of these lengths with these numbers of drafts on a device with `num_sms` SMs (no GPU
+    needed): (info dict, list of piece dicts)."""
+    B, offsets = len(seq_lens), [0]
+    for n in counts:
+        offsets.append(offsets[-1] + int(n))
+    lens, cu = (ctypes.c_int32 * B)(*[int(n) for n in seq_lens]), (ctypes.c_int32 * (B + 1))(*offsets)
+    most = max_pages or max(1, -(-max(seq_lens) // page_size))
+    cfg = fa_config(ctypes.sizeof(fa_config), -1, 0, 0, 0, scratch_bytes)
+    cache = fa_paged_cache(_CACHE_SIZE, FA_CACHE_E4M3 if e4m3 else FA_CACHE_BF16, None, None, 1, page_size, Hkv, dqk, dv)
+    seqs = fa_paged_seqs(_SEQS_SIZE, B, None, most, ctypes.addressof(lens), most, 0)
+    tree = fa_tree(ctypes.sizeof(fa_tree), max_tokens or max(1, max(counts)), ctypes.addressof(cu), None, 0)
+    out, pieces = fa_paged_plan_info(), None
+    for n in (0, None):          # how many, then which
+        count = int(out.pieces) if n is None else 0
+        pieces = (fa_paged_piece * max(1, count))()
+        st = load().fa_plan_paged_tree(num_sms, ctypes.addressof(cfg), ctypes.addressof(cache), ctypes.addressof(seqs), ctypes.addressof(tree), offsets[-1],
+                                       Hq, ctypes.addressof(out), ctypes.addressof(pieces), count)
+        if st != FA_OK:
+            raise FaError(st, "fa_plan_paged_tree")
     as_dict = lambda x: {f: getattr(x, f) for f, _ in x._fields_ if f != "reserved"}
     return as_dict(out), [as_dict(x) for x in pieces[:out.pieces]]
 

@@ -45,16 +45,25 @@ fa::TreeList make_list(int group, int max_tokens, int dqk, bool e4m3) {
 
 constexpr long long kMostUnits = 1ll << 30;      // the kernel counts units in 32 bits
 
+// Units that a call's list can have at most.
+bool too_long(const fa::TreeList& li, int B, int Hkv, int max_tokens, long long most_keys) {
+    const long long row_tiles = fa::tree_row_tiles(li, max_tokens), most_tiles = (most_keys + fa::kTileN - 1) / fa::kTileN;
+    return static_cast<long long>(B) * Hkv > kMostUnits / row_tiles / (most_tiles * li.w2 + li.cost);
+}
+
+// CTAs of a launch: one per SM, as far as the scratch has two partial results and an entry of the list of what is joined for each.
+int tree_ctas(int num_sms, size_t scratch_bytes, int dv, bool two) {
+    const long long fit = static_cast<long long>(scratch_bytes / (2 * sizeof(float) * fa::tree_slot_floats(dv, two) + sizeof(fa::TreeJoin)));
+    return static_cast<int>(fit < num_sms ? fit : num_sms);
+}
+
 template <int DQK, int DV, bool kE4m3>
 fa_status launch_tree(fa_handle* h, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const fa::PagedParams& p, fa::TreeArgs& a,
                       cudaStream_t st) {
     using Cfg = fa::TreeCfg<DQK, DV, kE4m3>;
     constexpr int smem = fa::tree_smem_bytes<DQK, DV, kE4m3>();
     static_assert(smem <= 227 * 1024, "shared memory budget exceeded");
-    // a CTA per SM, as far as the scratch has two partial results and an entry of the list of what is joined for each
-    const size_t per_cta = 2 * sizeof(float) * fa::tree_slot_floats(DV, Cfg::kTwo) + sizeof(fa::TreeJoin);
-    const long long fit = static_cast<long long>(h->tree_scratch_bytes / per_cta);
-    const int ctas = static_cast<int>(fit < h->num_sms ? fit : h->num_sms);
+    const int ctas = tree_ctas(h->num_sms, h->tree_scratch_bytes, DV, Cfg::kTwo);
     if (ctas < 1) return FA_ERR_UNSUPPORTED;
     a.part = static_cast<float*>(h->scratch);
     a.join = reinterpret_cast<fa::TreeJoin*>(a.part + 2ll * ctas * fa::tree_slot_floats(DV, Cfg::kTwo));
@@ -116,9 +125,7 @@ fa_status fa_forward_paged_tree(fa_handle* h, const fa_paged_cache* cache, const
     a.t = tp;
     a.group = Hq / cache->Hkv;
     a.list = make_list(a.group, tree->max_tokens, cache->dqk, e4m3);
-    const long long row_tiles = fa::tree_row_tiles(a.list, tree->max_tokens);
-    const long long most_tiles = (static_cast<long long>(seqs->max_pages) * cache->page_size + fa::kTileN - 1) / fa::kTileN;
-    if (static_cast<long long>(seqs->B) * cache->Hkv > kMostUnits / row_tiles / (most_tiles * a.list.w2 + a.list.cost)) return FA_ERR_UNSUPPORTED;
+    if (too_long(a.list, seqs->B, cache->Hkv, tree->max_tokens, static_cast<long long>(seqs->max_pages) * cache->page_size)) return FA_ERR_UNSUPPORTED;
     p.box_rows = 16;
     while (p.box_rows < 128 && cache->page_size % (2 * p.box_rows) == 0) p.box_rows *= 2;
     const int eb = e4m3 ? 1 : 2;
@@ -137,6 +144,80 @@ fa_status fa_forward_paged_tree(fa_handle* h, const fa_paged_cache* cache, const
     if (cache->dqk == 64) return e4m3 ? launch_tree<64, 64, true>(h, mq, mk, mv, p, a, st) : launch_tree<64, 64, false>(h, mq, mk, mv, p, a, st);
     if (cache->dqk == 192) return e4m3 ? launch_tree<192, 128, true>(h, mq, mk, mv, p, a, st) : launch_tree<192, 128, false>(h, mq, mk, mv, p, a, st);
     return e4m3 ? launch_tree<128, 128, true>(h, mq, mk, mv, p, a, st) : launch_tree<128, 128, false>(h, mq, mk, mv, p, a, st);
+}
+
+fa_status fa_plan_paged_tree(int num_sms, const fa_config* cfg, const fa_paged_cache* cache, const fa_paged_seqs* seqs, const fa_tree* tree, int total,
+                             int Hq, fa_paged_plan_info* out, fa_paged_piece* pieces, int max_pieces) {
+    if (num_sms <= 0 || !cache || !seqs || !tree || !out || cache->struct_size != sizeof(fa_paged_cache) || seqs->struct_size != sizeof(fa_paged_seqs) ||
+        tree->struct_size != sizeof(fa_tree)) return FA_ERR_INVALID_ARG;
+    if (cache->page_size <= 0 || cache->Hkv <= 0 || Hq <= 0 || Hq % cache->Hkv != 0 || seqs->B <= 0 || seqs->max_pages <= 0 || !seqs->seq_lens ||
+        tree->max_tokens <= 0 || total <= 0 || max_pieces < 0 || (max_pieces > 0 && !pieces)) return FA_ERR_INVALID_ARG;
+    if (!tree->cu_seqlens && (total % seqs->B != 0 || total / seqs->B > tree->max_tokens)) return FA_ERR_INVALID_ARG;
+    if (!head_sizes_ok(cache->dqk, cache->dv) || cache->page_size % 16 != 0 || tree->max_tokens > FA_TREE_MAX_TOKENS || Hq > 65535 || seqs->B > 65535 ||
+        static_cast<int64_t>(seqs->max_pages) * cache->page_size > 0x7fffff00LL) return FA_ERR_UNSUPPORTED;
+    uint64_t scratch = 40ull << 20;
+    if (cfg) {
+        if (cfg->struct_size < 16) return FA_ERR_INVALID_ARG;
+        if (cfg->struct_size >= sizeof(fa_config) && cfg->scratch_bytes) scratch = cfg->scratch_bytes;
+    }
+    fa::TreeList li = make_list(Hq / cache->Hkv, tree->max_tokens, cache->dqk, cache->type == FA_CACHE_E4M3);
+    if (too_long(li, seqs->B, cache->Hkv, tree->max_tokens, static_cast<long long>(seqs->max_pages) * cache->page_size)) return FA_ERR_UNSUPPORTED;
+    const int ctas = tree_ctas(num_sms, scratch, cache->dv, li.two != 0), B = seqs->B;
+    if (ctas < 1) return FA_ERR_UNSUPPORTED;
+    const fa::TreeSeqs seq_of{tree->cu_seqlens, seqs->seq_lens, B, total, tree->max_tokens, seqs->max_pages, cache->page_size};
+    auto units_of = [&](int b) {
+        int n, row0, len;
+        seq_of(b, n, row0, len);
+        return cache->Hkv * fa::tree_head_units(fa::tree_units(li, n, len));
+    };
+    fa::TreeBatch batch{0, 0, 0, 0x7fffffff, 0};
+    for (int b = 0; b < B; ++b) {
+        int n, row0, len;
+        seq_of(b, n, row0, len);
+        const fa::TreeUnits u = fa::tree_units(li, n, len);
+        batch.units += cache->Hkv * fa::tree_head_units(u);
+        if (n == 0) continue;
+        const int nt = fa::tree_tiles(len);
+        batch.blocks += cache->Hkv * (u.pairs + (u.single ? 1 : 0));
+        batch.longest = nt > batch.longest ? nt : batch.longest;
+        batch.shortest = nt < batch.shortest ? nt : batch.shortest;
+        batch.kinds |= (u.pairs ? 1 : 0) | (u.single ? 2 : 0);
+    }
+    int share = fa::tree_rules(li, batch, ctas), all = 0;
+    for (int b = 0; b < B; ++b) all += units_of(b);
+    if (share == 0) share = fa::tree_share(li, all, ctas);
+    out->rows_per_block = li.row_tokens * li.row_heads;
+    out->row_blocks = fa::tree_row_tiles(li, tree->max_tokens);
+    out->ctas = ctas;
+    out->part_cost = li.cost;
+    out->units = all;
+    out->units_per_cta = share;
+    long long n_pieces = 0;
+    int b0 = 0, base0 = 0;             // the sequence that the CTA's share begins in, and its first unit
+    for (int c = 0; c < ctas && static_cast<long long>(c) * share < all; ++c) {
+        while (c * share >= base0 + units_of(b0)) base0 += units_of(b0++);
+        fa::TreeWalk w;
+        seq_of(b0, w.n, w.row0, w.len);
+        fa::tree_walk_begin(w, li, c, share, all, b0, base0);
+        fa::TreePart e;
+        while (fa::tree_walk_next(w, li, cache->Hkv, seq_of, e)) {
+            if (n_pieces < max_pieces) {
+                fa_paged_piece* x = pieces + n_pieces;
+                x->cta = c;
+                x->sequence = e.b;
+                x->kv_head = e.kvh;
+                x->row_block = e.row_tile;
+                x->first_tile = e.t0;
+                x->end_tile = e.t1;
+                x->slot = e.slot;
+                x->pieces = e.pieces;
+                x->first_cta = e.first_cta;
+            }
+            ++n_pieces;
+        }
+    }
+    out->pieces = n_pieces;
+    return FA_OK;
 }
 
 }  // extern "C"

@@ -90,7 +90,7 @@ __host__ __device__ inline int tree_rules(TreeList& li, const TreeBatch& b, int 
         li.pad = b.longest;
         return li.cost + li.w2 * li.pad;
     }
-    if (2 * b.blocks <= ctas && b.longest == b.shortest && b.kinds != 3) {
+    if (2 * b.blocks <= ctas && b.longest == b.shortest && b.longest > 0 && b.kinds != 3) {
         const int pieces = ctas / b.blocks, per = (b.longest + pieces - 1) / pieces;
         li.cost = 0;
         li.w1 = li.w2 = 1;
@@ -112,7 +112,7 @@ struct TreePart {
     int t0, t1;                   // t1 < 0: the end of the CTA's share
     int tile0;                    // index of the part's first tile in the CTA's share
     int slot;                     // of the partial result, -1: the part is whole
-    int pieces;
+    int pieces, first_cta;        // of the whole block, and the CTA of its first piece
 };
 // A row block in several pieces as the joining kernel sees it, one per CTA (the one with the first piece; pieces = 0: none).  Piece 0
 // is in slot 2 * CTA + 1, piece i in slot 2 * (CTA + i).
@@ -124,6 +124,19 @@ __host__ __device__ inline int tree_tile_at(int u, int ub, int cost, int w, int 
     const int t = x <= 0 ? 0 : w == 1 ? x : (x + 1) >> 1;         // (w is 1 or 2)
     return t < nt ? t : nt;
 }
+
+// A sequence's drafts, its first row and its length, as the list takes them (and without reports).
+struct TreeSeqs {
+    const int* cu_seqlens;
+    const int* seq_lens;
+    int B, total, max_tokens, max_pages, page_size;
+    __host__ __device__ void operator()(int b, int& n, int& row0, int& len) const {
+        const DraftRows d = draft_rows(cu_seqlens, b, B, total, max_tokens, nullptr);
+        n = d.count;
+        row0 = d.first;
+        len = clamped_len(seq_lens[b], max_pages, page_size, nullptr);
+    }
+};
 
 // The list from the unit u0 on: the block that holds it, and the ones behind it.  `next` gives the next part, or false at the end.
 struct TreeWalk {
@@ -150,8 +163,7 @@ __host__ __device__ inline void tree_walk_begin(TreeWalk& w, const TreeList& li,
     const int in = w.u0 - w.base, at = in / w.u.pair;
     w.block = at < w.u.pairs ? at : w.u.pairs;
 }
-template <typename SeqOf>
-__host__ __device__ inline bool tree_walk_next(TreeWalk& w, const TreeList& li, int Hkv, int B, SeqOf&& seq_of, TreePart& e) {
+__host__ __device__ inline bool tree_walk_next(TreeWalk& w, const TreeList& li, int Hkv, const TreeSeqs& seq_of, TreePart& e) {
     while (!w.ended) {
         const int blocks = w.u.pairs + (w.u.single ? 1 : 0);
         const int ub = w.base + w.block * w.u.pair, nt = tree_tiles(w.len);
@@ -169,10 +181,12 @@ __host__ __device__ inline bool tree_walk_next(TreeWalk& w, const TreeList& li, 
         e.tile0 = w.tiles;
         e.slot = -1;
         e.pieces = 1;
+        e.first_cta = w.cta;
         const bool some = nt > 0 ? e.t0 < e.t1 : ub >= w.u0;
         if (some && e.t1 - e.t0 < nt) {
             e.slot = 2 * w.cta + (e.t0 == 0 ? 1 : 0);
-            e.pieces = (ub + li.cost + (nt - 1) * wt) / w.share - (ub + li.cost) / w.share + 1;
+            e.first_cta = (ub + li.cost) / w.share;
+            e.pieces = (ub + li.cost + (nt - 1) * wt) / w.share - e.first_cta + 1;
         }
         w.tiles += some ? e.t1 - e.t0 : 0;
         // the block behind it
@@ -184,7 +198,7 @@ __host__ __device__ inline bool tree_walk_next(TreeWalk& w, const TreeList& li, 
             if (++w.kvh == Hkv) {
                 w.kvh = 0;
                 do {
-                    if (++w.seq >= B) { w.ended = true; break; }      // (not reached: the share ends before)
+                    if (++w.seq >= seq_of.B) { w.ended = true; break; }      // (not reached: the share ends before)
                     seq_of(w.seq, w.n, w.row0, w.len);
                 } while (w.n == 0);
                 if (!w.ended) w.u = tree_units(li, w.n, w.len);
@@ -617,12 +631,7 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     }
     grid_dependency_wait();
 
-    auto seq_of = [&](int b, int& n, int& row0, int& len) {
-        const DraftRows d = draft_rows(a.t.cu_seqlens, b, p.B, a.t.total, a.t.max_tokens, nullptr);
-        n = d.count;
-        row0 = d.first;
-        len = clamped_len(p.seq_lens[b], p.max_pages, p.page_size, nullptr);
-    };
+    const TreeSeqs seq_of{a.t.cu_seqlens, p.seq_lens, p.B, a.t.total, a.t.max_tokens, p.max_pages, p.page_size};
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
@@ -1156,7 +1165,7 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             return true;
         };
         auto publish = [&](int k) {
-            if (!tree_walk_next(w, li, p.Hkv, p.B, seq_of, e)) e.t1 = -1;
+            if (!tree_walk_next(w, li, p.Hkv, seq_of, e)) e.t1 = -1;
             ok = __all_sync(0xffffffffu, ok && wait(sh.part_empty[k % NP], ((k / NP) & 1) ^ 1));
             if (!ok) return;
             if (e.t1 >= 0 && e.slot >= 0 && e.t0 == 0) join = TreeJoin{e.kvh, e.row_tile, e.two, e.n, e.row0, e.pieces, 0, 0};

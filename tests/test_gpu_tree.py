@@ -94,6 +94,10 @@ def test_sequences_shorter_than_their_drafts(handle):
     run(handle, [0, 3, 200, 0], [4, 4, 4, 4], 8, 2, 128, 128, 16, masks="random", cu=False)
     run(handle, [0, 3, 200, 0], [4, 4, 4, 4], 8, 2, 128, 128, 16, True, masks="chain", cu=False)
     run(handle, [60, 3, 200, 129], [64, 64, 64, 64], 8, 2, 128, 128, 16, masks="tree", cu=False)
+    # a batch of nothing but padding: its rows are written all the same
+    for dqk, dv, e4m3 in ((128, 128, False), (64, 64, True), (192, 128, False)):
+        run(handle, [0], [4], 8, 2, dqk, dv, 16, e4m3, cu=False)
+        run(handle, [0, 0, 0], [40, 0, 3], 8, 2, dqk, dv, 16, e4m3, pad=2)
 
 
 @pytest.mark.parametrize("Hq,Hkv", [(32, 1), (40, 1), (128, 1), (130, 1), (300, 2), (10, 2)])
