@@ -467,8 +467,11 @@ FA_DEVI void tree_pass(uint32_t tS, uint32_t tO, uint32_t p_row, float c, float 
         tmem_ld_x32(tS + 64, s + 64);
         tmem_ld_x32(tS + 96, s + 96);
         tc_wait_ld();
-        const float off = m_ref == -INFINITY ? bias : bias - m_ref * c;
-        off2 = make_float2(off, off);
+        auto set_off = [&]() {
+            const float off = m_ref == -INFINITY ? bias : bias - m_ref * c;
+            off2 = make_float2(off, off);
+        };
+        set_off();
         float a[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) a[q] = -INFINITY;
@@ -478,9 +481,15 @@ FA_DEVI void tree_pass(uint32_t tS, uint32_t tO, uint32_t p_row, float c, float 
             for (int q = 0; q < 8; ++q)
                 a[q] = fmax3(a[q], __uint_as_float(s[e + 2 * q]), __uint_as_float(s[e + 2 * q + 1]));
         }
-        exp_chunk(0);
+        if (!first_tile) exp_chunk(0);
         float mx = fmaxf(fmax3(a[0], a[1], a[2]), fmax3(a[3], a[4], a[5]));
         mx = fmax3(mx, a[6], a[7]);
+        if (first_tile) {            // (nothing to guess with: the row's first reference is this maximum)
+            m_ref = mx;
+            set_off();
+            exp_chunk(0);
+            break;
+        }
         const bool grow = mx > m_ref + tau_raw;
         if (!__any_sync(0xffffffffu, grow)) break;
         if (grow) {
