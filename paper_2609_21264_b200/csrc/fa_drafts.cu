@@ -106,8 +106,13 @@ fa_status fa_compact_paged(fa_handle* h, const fa_paged_cache* caches, int num_c
         memset(&c, 0, sizeof c);
         set_caches(c, caches, i, num_caches - i < fa::kMostCaches ? num_caches - i : fa::kMostCaches);
         p.new_lens = i == 0 ? new_lens : nullptr;
-        p.blocks_per_row = (c.Hkv * (c.k_vecs + c.v_vecs) + fa::kCompactThreads - 1) / fa::kCompactThreads;      // (at most 65535 heads of 40)
-        s = launch(h, fa::fa_compact_kernel, static_cast<long long>(p.blocks_per_row) * p.B * c.layers, fa::kCompactThreads, 0,
+        p.columns = c.Hkv * (c.k_vecs + c.v_vecs);                  // (at most 65535 heads of 40)
+        // As many columns a CTA as put all CTAs into one wave of four an SM (60 registers a thread), so that look-ups are not waited for twice.
+        const long long all = static_cast<long long>(c.layers) * p.columns, blocks = (all + fa::kCompactThreads - 1) / fa::kCompactThreads;
+        const long long rounds = (blocks * p.B + 4ll * h->num_sms - 1) / (4ll * h->num_sms);
+        p.rounds = static_cast<int>(rounds < 1 ? 1 : rounds > 16 ? 16 : rounds);
+        p.ctas = static_cast<int>((blocks + p.rounds - 1) / p.rounds);
+        s = launch(h, fa::fa_compact_kernel, static_cast<long long>(p.ctas) * p.B, fa::kCompactThreads, 0,
                    static_cast<cudaStream_t>(stream), c, p);
         if (s != FA_OK) return s;
     }

@@ -690,6 +690,9 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 c *= p.k_scale ? p.k_scale[e.kvh] : 1.f;
                 n_q += nt > 0;
             }
+            // Rows that are not the block's hold what the space held before, whose scores may rise from tile to tile and would have their warp
+            // move references all the time: they count as zeros, whose reference never moves.
+            if (!live) c = 0.f;
             float m_ref = -INFINITY, l = 0.f, tau_raw = kRescaleThresholdLog2 / c;
             for (int j = 0; j < steps; ++j, ++n_s) {
                 ok = __all_sync(0xffffffffu, ok && tree_wait_timed(sh.s_full[t], n_s & 1, &sh.wait, kSiteSoftmaxSFull));
