@@ -416,3 +416,91 @@ def test_little_scratch(handle):
                 assert e.value.status == b.FA_ERR_UNSUPPORTED
         finally:
             b.fa_destroy(h)
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("dqk,dv", [(64, 64), (128, 128), (192, 128)])
+def test_queries_that_are_no_numbers(handle, e4m3, dqk, dv):
+    """A query of NaN makes its own row NaN, no other."""
+    from paper_2609_21264_b200 import binding as b
+    k, v, table, lens_t, ks, vs = pool([300, 150], 16, 2, dqk, dv, e4m3, False, 23)
+    q = torch.randn(2 * 20, 8, dqk, generator=torch.Generator().manual_seed(14)).to(torch.bfloat16).cuda()
+    cache = b.PagedCache(k, v, ks, vs)
+    o0, lse0 = b.forward_paged_tree(handle, q, cache, table, lens_t, None)
+    ok(handle)
+    q[7, 3, 5] = float("nan")
+    q[25, 0] = float("nan")
+    o1, lse1 = b.forward_paged_tree(handle, q, cache, table, lens_t, None)
+    ok(handle)
+    hit = torch.zeros(40, 8, dtype=torch.bool, device="cuda")
+    hit[7, 3] = hit[25, 0] = True
+    assert torch.isnan(o1[hit]).all() and torch.isnan(lse1.T[hit]).all()
+    assert torch.equal(o1[~hit], o0[~hit]) and torch.equal(lse1.T[~hit], lse0.T[~hit])
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("scale", [1e-30, 0.01, 1.0])
+def test_scales(handle, e4m3, scale):
+    """Scores that hardly differ (the mean of the values), and large ones; an 8-bit cache without scales of its own."""
+    from paper_2609_21264_b200 import binding as b
+    k, v, table, lens_t, _, _ = pool([300, 140, 20], 16, 2, 128, 128, e4m3, True, 24)
+    if e4m3:
+        k, v = ((x.float() / 16).nan_to_num(0.0).clamp(-3, 3).to(torch.float8_e4m3fn) for x in (k, v))
+    q = torch.randn(3 * 15, 8, 128, generator=torch.Generator().manual_seed(15)).to(torch.bfloat16).cuda()
+    o, lse = b.forward_paged_tree(handle, q, b.PagedCache(k, v), table, lens_t, None, scale=scale)
+    ok(handle)
+    O, L, A = tree_reference(q, k, v, None, None, table, [300, 140, 20], [0, 15, 30, 45], [torch.ones(15, 15).tril() > 0] * 3, scale)
+    assert_attention(o, lse, O, L, A)
+
+
+def test_masked_values_near_the_largest_number(handle):
+    """A draft whose values are 2^120, seen by a few: it weighs exactly nothing in the others."""
+    from paper_2609_21264_b200 import binding as b
+    n = 20
+    k, v, table, lens_t, _, _ = pool([150], 16, 1, 128, 128, False, False, 25)
+    seen, _ = seen_by(random_parents(n, torch.Generator().manual_seed(4)))
+    q = torch.randn(n, 4, 128, generator=torch.Generator().manual_seed(16)).to(torch.bfloat16).cuda()
+    mask, cache = pack(seen, 1).cuda(), b.PagedCache(k, v)
+    o0, _ = b.forward_paged_tree(handle, q, cache, table, lens_t, mask)
+    ok(handle)
+    at = 130 + 7
+    v[int(table[0, at // 16]), :, at % 16] = 2.0 ** 120
+    o1, _ = b.forward_paged_tree(handle, q, cache, table, lens_t, mask)
+    ok(handle)
+    hit = seen[:, 7].cuda()
+    assert torch.equal(o1[~hit], o0[~hit]) and not torch.equal(o1[hit], o0[hit])
+
+
+def test_many_sequences(handle):
+    """More sequences than a warp has lanes many times over, most of them short."""
+    lens = [(i * 29) % 150 + (3000 if i % 97 == 5 else 0) for i in range(1500)]
+    counts = [min(n, i % 4) for i, n in enumerate(lens)]
+    run(handle, lens, counts, 2, 1, 64, 64, 16, seed=26, pad=1)
+
+
+def test_launches_without_overlap_and_two_handles_at_once():
+    from paper_2609_21264_b200 import binding as b
+    cases = []
+    for seed, (lens, n, e4m3) in enumerate((([5000, 300], 40, False), ([4000, 900, 20], 13, True))):
+        k, v, table, lens_t, ks, vs = pool(lens, 32, 2, 128, 128, e4m3, False, 27 + seed)
+        q = torch.randn(len(lens) * n, 8, 128, generator=torch.Generator().manual_seed(17)).to(torch.bfloat16).cuda()
+        cases.append((q, b.PagedCache(k, v, ks, vs), table, lens_t))
+    handles = [b.fa_create(), b.fa_create(flags=b.FA_FLAG_NO_DEPENDENT_LAUNCH)]
+    try:
+        want = [b.forward_paged_tree(handles[0], q, c, t, l, None) for q, c, t, l in cases]
+        torch.cuda.synchronize()
+        streams = [torch.cuda.Stream() for _ in handles]
+        got = [[], []]
+        for _ in range(10):
+            for i in range(2):
+                with torch.cuda.stream(streams[i]):
+                    q, c, t, l = cases[i]
+                    got[i].append(b.forward_paged_tree(handles[i], q, c, t, l, None))
+        for h in handles:
+            ok(h)
+        for i in range(2):
+            for o, lse in got[i]:
+                assert torch.equal(o, want[i][0]) and torch.equal(lse, want[i][1])
+    finally:
+        for h in handles:
+            b.fa_destroy(h)
