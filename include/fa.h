@@ -126,7 +126,7 @@ typedef struct fa_config {
     uint32_t kv_splits;       /* split-KV: 0 = library decides, 1 = never split, 2..256 = use n
                                  splits whenever the scratch buffer can hold the partials      */
     uint64_t scratch_bytes;   /* device scratch for split-KV partials, allocated by fa_create;
-                                 0 = default (32 MiB)                                          */
+                                 0 = default (32 MiB; fa_forward_paged_tree may use 40)        */
 } fa_config;
 
 /*
@@ -628,7 +628,11 @@ fa_status fa_tree_layout(fa_handle* h, const int32_t* parents, const int32_t* cu
  * cache as fp16 (11 significant bits down to 2^-21 of the row's reference), and the queries as a sum of three 8-bit terms (exact for
  * entries of 2^-23 of their row's largest and more, to 2^-30 of it below).
  * Two launches: the K/V tiles of all sequences are dealt out evenly over the SMs, and a second kernel joins the pieces of what several SMs
- * share, in a fixed order, so equal calls give equal bits.  The partial results use scratch of the handle under the rule of fa_forward.
+ * share, in a fixed order, so equal calls give equal bits.  The partial results use the handle's scratch buffer, under the rule of
+ * fa_forward: launches through one handle must not overlap on the device.  With less scratch than two partials per SM (130 KB each, 65 KB
+ * at 192/128 and over e4m3 caches, half of that at head size 64) fewer SMs are used; with less than two, FA_ERR_UNSUPPORTED.  The list of work
+ * is counted in 32 bits, as in fa_forward_paged: B * Hkv * (row tiles of max_tokens drafts) * (twice the tiles of 128 keys in max_pages
+ * pages + 4) is at most 2^30, else FA_ERR_UNSUPPORTED (a row tile: 128 / (Hq / Hkv) tokens, or 128 of a token's heads).
  * FA_FLAG_SERIAL_KERNEL selects a plain kernel of one CTA per query row.
  */
 typedef struct fa_tree {
