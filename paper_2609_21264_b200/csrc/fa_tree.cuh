@@ -5,17 +5,25 @@
 // rows over a 16-bit cache HBM is the bound, behind that the tensor cores and, as in every kernel here, the exponentials.  So a CTA
 // takes up to 256 rows in one pass over the keys, as two tiles of 128 rows on the accumulator's lanes:
 //
-//   * Two streams t = 0, 1, each with scores S_t, probabilities P_t (over S_t) and accumulator O_t, the loop of fa_fwd_pair.cuh (read that
-//     file first).  With more than 128 rows the streams are the two row tiles and share every K/V tile; with up to 128 they
-//     are the even and the odd K/V tiles of the same rows, merged at the end.  Either way one stream's softmax runs under the other's
-//     MMAs.  (Head sizes 192/128 have no room for a second query tile: always the latter.)
+//   * Two streams t = 0, 1, each with scores S_t, probabilities P_t and accumulator O_t, the loop of fa_fwd_pair.cuh (read that file
+//     first).  With more than 128 rows the streams are the two row tiles and share every K/V tile; with up to 128 they are the even
+//     and the odd K/V tiles of the same rows, merged at the end.  Either way one stream's softmax runs under the other's MMAs.
+//     (192/128 and e4m3 caches have no room for a second query tile: always the latter.)  P_t lies over S_t, or where there is room
+//     (head size 64, e4m3 at 128) in shared memory, and the next scores need not wait for P_t V (e4m3 198 to 168 us).
 //   * A row tile is tt tokens x ht heads of the group (ht = the group, tt = 128 / ht), which is one TMA box of Q: rows lie in the tile as
 //     token, head.  Rows that the sequence does not have are computed and not stored.
 //   * The tiles of all (sequence, K/V head, row block)s form one list that the CTAs cut into equal consecutive shares on the device, as
 //     in fa_paged.cuh.  What several CTAs share is joined by a second kernel: its pieces are up to 130 KB each, which the CTA that
-//     finishes last would read alone at the speed of one SM.
-//   * The mask concerns the last tiles alone: a thread has one row, takes its 128 bits for a tile out of the row's words by funnel shifts,
+//     finishes last would read alone at the speed of one SM (up to three pieces joined that way: 71.4 us, against 68.6).
+//   * The mask concerns the last tiles alone: a thread has one row, takes its bits for 32 keys out of the row's words by a funnel shift,
 //     and hides keys past the length with the same bits.
+//
+// What bounds it.  16 sequences of 129 to 8192 keys, trees of 16 to 64 drafts, 32/8 heads of 128, bf16: 67.6 us, where 248 MB take 38 at the
+// copy rate.  With 256 rows a tile of keys takes a CTA 3000 cycles, the chain softmax (2000) -> P V and next scores (1024 cycles of MMAs) of each
+// stream; 28 tiles a CTA.  Beside them: 9000 cycles from the launch to the first scores (list, block table, first loads), 6000 from
+// one block's last tile to the next one's first (result, barrier, first pass), 5 us for the join.  2 x 20000 keys of 192/128 heads, 31 drafts:
+// HBM, 91 % of the copy rate.  48 sequences of 300 to 8192 keys over e4m3, 13 drafts, 64/8 heads: 154 us, where 521 MB take 80: two tiles
+// take 3600 cycles, of which MMAs 2630 (8-bit scores in three terms, fp16 products), and each CTA has four blocks.
 //
 // Over an e4m3 cache K is multiplied as it is (kind::f8f6f4), the queries as three e5m2 terms like in fa_paged.cuh, added up in one
 // accumulator (half as many MMAs again); P V is an fp16 product, since terms of P would be work of the softmax warps, which are the
@@ -24,7 +32,7 @@
 //
 // Roles: warps 0-3 / 4-7 softmax of stream 0 / 1 and results, warp 8 MMA issue, warp 9 loads of K, warp 10 of Q and V, warp 11 the list
 // and the zeros behind a sequence's last value, over e4m3 caches warps 12-15 the terms of Q and the codes of V.
-// TMEM: S_0 [0,128) S_1 [128,256) O_0 [256,384) O_1 [384,512); P_t over S_t[0,64).
+// TMEM: S_0 [0,128) S_1 [128,256) O_0 [256,384) O_1 [384,512); P_t over S_t[0,64), where it is not in shared memory.
 #pragma once
 
 #include <cuda_fp16.h>
@@ -1007,21 +1015,21 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                     }
                 } else {
 #pragma unroll 1
-                for (int t = 0; t < 2; ++t) {
-                    if (!ok || (t == 1 && steps1 == 0)) break;
-                    if (t == 0 || !two) ok = wait(sh.k_full[sk], ph_k);
-                    if (!ok) break;
-                    tc_fence_after_sync();
-                    const uint32_t klo = k_lo0 + sk * (Cfg::kKBytes >> 4);
+                    for (int t = 0; t < 2; ++t) {
+                        if (!ok || (t == 1 && steps1 == 0)) break;
+                        if (t == 0 || !two) ok = wait(sh.k_full[sk], ph_k);
+                        if (!ok) break;
+                        tc_fence_after_sync();
+                        const uint32_t klo = k_lo0 + sk * (Cfg::kKBytes >> 4);
 #pragma unroll
-                    for (int ks = 0; ks < kSteps; ++ks) score(tmem + 128 * t, q_lo(t), klo, ks);
-                    scores_done(t);
-                }
-                for (int j = 0; j < steps0 && ok; ++j) {
+                        for (int ks = 0; ks < kSteps; ++ks) score(tmem + 128 * t, q_lo(t), klo, ks);
+                        scores_done(t);
+                    }
+                    for (int j = 0; j < steps0 && ok; ++j) {
 #pragma unroll 1
-                    for (int t = 0; t < 2 && ok; ++t)
-                        if (t == 0 || j < steps1) ok = block(t, j, t == 0 ? steps0 : steps1);
-                }
+                        for (int t = 0; t < 2 && ok; ++t)
+                            if (t == 0 || j < steps1) ok = block(t, j, t == 0 ? steps0 : steps1);
+                    }
                 }
             }
         }
