@@ -603,6 +603,7 @@ fa_status fa_forward_paged_diff(fa_handle* h, const fa_paged_cache* cache, const
  * rows: packed, sequence b's rows are [cu_seqlens[b], cu_seqlens[b+1]) (DEVICE array of B+1 int32, non-decreasing from 0), or with
  * cu_seqlens NULL total / B each.  A sequence has at most max_tokens of them (<= FA_TREE_MAX_TOKENS); one whose rows do not lie in
  * [0, total] or are more is reported by fa_last_status (FA_ERR_INVALID_ARG) and left out.  Rows behind the last sequence stay as they were.
+ * Outputs overlap no inputs, and the keys and values of all caches of a call lie apart.
  */
 #define FA_TREE_MAX_TOKENS 256
 
@@ -660,7 +661,7 @@ fa_status fa_plan_paged_tree(int num_sms, const fa_config* cfg, const fa_paged_c
  * The accepted drafts move up: of the n drafts of sequence b those with the numbers keep[b][0] < keep[b][1] < ... (keep_counts[b] of
  * them, at most max_keep <= FA_TREE_MAX_TOKENS; keep is a DEVICE int32 array with rows keep_stride elements apart) go to the slots of
  * the sequence's first drafts, in `caches` (HOST array of num_caches structures that differ in k and v alone: the caches of a model's
- * layers, one block table for all), and new_lens[b] = seq_lens[b] - n + keep_counts[b] (DEVICE [B] int32, not seq_lens itself; NULL:
+ * layers, one block table for all), and new_lens[b] = seq_lens[b] - n + keep_counts[b] (DEVICE [B] int32, none of the inputs; NULL:
  * not wanted; not below 0).  The slots behind them hold what they held.  Drafts in front of position 0 (the padding of a batch) are left alone.
  * The pages of the drafts must not be shared.  A sequence whose numbers do not rise, or are no drafts', and one with more than n
  * or max_keep of them is reported, nothing of it moves and its length stays.  One launch per 128 caches.

@@ -816,7 +816,7 @@ def compact_paged(h, caches, block_table, seq_lens, keep, keep_counts, *, cu_seq
 
     seq_lens [B] int32 counts the drafts in; cu_seqlens [B+1] int32 as for forward_paged_tree (None: total / B drafts each).  keep
     [B, most] int32 holds the accepted drafts' numbers in rising order, keep_counts [B] int32 how many.  Returns the new lengths [B]
-    int32 (a new tensor where none is given; not seq_lens itself).
+    int32 (a new tensor where none is given; none of the inputs).
     """
     r = (_calls or _native()).compact(h, caches.address, caches.count, caches.index, block_table, seq_lens, keep, keep_counts, cu_seqlens, total,
                                       new_lens)

@@ -87,7 +87,9 @@ fa_status fa_compact_paged(fa_handle* h, const fa_paged_cache* caches, int num_c
     if (misaligned(cu_seqlens, 4) || misaligned(keep, 4) || misaligned(keep_counts, 4) || misaligned(new_lens, 4)) return FA_ERR_INVALID_ARG;
     if (max_keep > FA_TREE_MAX_TOKENS) return FA_ERR_UNSUPPORTED;
     if (seqs->B == 0) return FA_OK;
-    if (!keep || !keep_counts || new_lens == seqs->seq_lens) return FA_ERR_INVALID_ARG;
+    if (!keep || !keep_counts) return FA_ERR_INVALID_ARG;
+    // (the CTAs of a sequence read all of these, each in its own time)
+    if (new_lens && (new_lens == seqs->seq_lens || new_lens == keep_counts || new_lens == keep || new_lens == cu_seqlens)) return FA_ERR_INVALID_ARG;
     if (!cu_seqlens && (total % seqs->B != 0)) return FA_ERR_INVALID_ARG;
     if (!cu_seqlens && total / seqs->B > FA_TREE_MAX_TOKENS) return FA_ERR_UNSUPPORTED;
     DeviceGuard guard(h->device);

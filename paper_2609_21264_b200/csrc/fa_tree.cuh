@@ -268,10 +268,12 @@ struct TreeShared {
     uint64_t v_tail[kE4m3 ? 1 : Cfg::kVStages];       // the rows behind a sequence's last value are zeros
     uint64_t s_full[2], s_free[2], p_first[2], p_rest[2], o_final[2];      // (s_free, and o_final of every step, with P in shared memory)
     uint64_t part_full[Cfg::kParts], part_empty[Cfg::kParts];
+    uint64_t mma_done;            // (only after a wait that ran out)
     TreePart part[Cfg::kParts];
     uint32_t tmem_base;
     TreeWait wait;
     int v_issued;                 // V tiles whose loads have been issued
+    int loads[3];                 // of K and V tiles and of queries, at the end
     float stat_m[2][kTileM], stat_l[2][kTileM];       // (of two streams on the same rows)
     uint8_t q_shift[2][kE4m3 ? kTileM : 4];      // of even and odd parts: 127 - exponent that a row was scaled by
 };
@@ -398,6 +400,15 @@ FA_DEVI bool tree_wait_timed(uint64_t& bar, uint32_t parity, TreeWait* ctx, uint
     return ptx::mbar_try_wait(ptx::smem_addr(&bar), parity) || tree_wait_long(&bar, parity, ctx, who);
 }
 
+// After a wait that ran out: the end of what a barrier counts, for 100 us at most (a load that was never issued does not end).
+static __device__ __noinline__ void tree_settle(uint64_t& bar, uint32_t parity) {
+    for (int i = 0; i < 1000 && !ptx::mbar_test_wait(ptx::smem_addr(&bar), parity); ++i) __nanosleep(100);
+}
+// The last of n loads in turn into each of `stages` stages.
+static __device__ __noinline__ void tree_settle_ring(uint64_t* full, int stages, int n) {
+    for (int i = 0; i < stages && i < n; ++i) tree_settle(full[i], static_cast<uint32_t>((n - 1 - i) / stages) & 1u);
+}
+
 // ------------------------------------------------------------------ softmax pass
 
 // Scores that a row does not see become -inf in TMEM, 32 at a time (bit e of `seen`: the e-th of them), ahead of the pass: a loop of 50
@@ -432,14 +443,6 @@ FA_DEVI void tree_pass(uint32_t tS, uint32_t tO, uint32_t p_row, float c, float 
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
             const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[q * 32 + e]), __uint_as_float(s[q * 32 + e + 1])), c2, off2);
-#ifdef TREE_POLY
-            if ((e / 2) % TREE_POLY == TREE_POLY - 1) {
-                const float2 y = exp2_poly2<true>(x);
-                s[q * 32 + e] = __float_as_uint(y.x);
-                s[q * 32 + e + 1] = __float_as_uint(y.y);
-                continue;
-            }
-#endif
             s[q * 32 + e] = __float_as_uint(exp2_approx(x.x));
             s[q * 32 + e + 1] = __float_as_uint(exp2_approx(x.y));
         }
@@ -591,6 +594,7 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
         sh.wait.limit_ns = p.wait_limit_ns;
         mbar_init(smem_addr(&sh.q_full), 1);
         mbar_init(smem_addr(&sh.q_empty), 1);
+        mbar_init(smem_addr(&sh.mma_done), 1);
         sh.v_issued = 0;
 #pragma unroll
         for (int s = 0; s < NK; ++s) {
@@ -1110,6 +1114,10 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 if (++s == stages) { s = 0; parity ^= 1u; }
             }
         }
+        if (lane == 0) {
+            sh.loads[is_v ? 1 : 0] = n;
+            if (is_v) sh.loads[2] = n_q;
+        }
     } else if (warp == 11) {
         // ============================================================ the list of parts; zeros behind the last value of a sequence
         setmaxnreg_dec<Cfg::kRegsOther>();
@@ -1362,6 +1370,20 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     // ---------------------------------------------------------------- teardown (all warps)
     tc_fence_before_sync();
     __syncthreads();
+    if (sh.wait.abort_flag) {         // (uniform: it is set before the barrier or not at all)
+        // copies and MMAs that are still under way end before their memory is given back
+        if (warp == 8 && elect_one()) {
+            tc_commit(smem_addr(&sh.mma_done));
+            tree_settle(sh.mma_done, 0);
+        }
+        if (tid == 0) {
+            tree_settle_ring(sh.k_full, NK, sh.loads[0]);
+            if constexpr (kE4m3) tree_settle_ring(sh.raw_full, NR, sh.loads[1]);
+            else tree_settle_ring(sh.v_full, NV, sh.loads[1]);
+            tree_settle_ring(&sh.q_full, 1, sh.loads[2]);
+        }
+        __syncthreads();
+    }
     if (warp == 8) tmem_dealloc(tmem, 512);
 }
 

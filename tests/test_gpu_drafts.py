@@ -498,3 +498,19 @@ def test_a_step_and_the_step_behind_it(serial, e4m3):
             assert torch.equal(k.view(torch.uint8), after[0].view(torch.uint8)) and torch.equal(v.view(torch.uint8), after[1].view(torch.uint8))
     finally:
         b.fa_destroy(h)
+
+
+def test_new_lengths_are_a_tensor_of_their_own(handle):
+    """The CTAs of a sequence read lengths, offsets and kept numbers each in its own time: none of them may be written meanwhile."""
+    from paper_2609_21264_b200 import binding as b
+    k = torch.randn(4, 2, 16, 64, device="cuda").to(torch.bfloat16)
+    v = torch.randn(4, 2, 16, 64, device="cuda").to(torch.bfloat16)
+    k0, v0 = k.clone(), v.clone()
+    table, lens, keep, counts, cu = ints([[0, 1], [2, 3]]), ints([20, 30]), ints([[1], [2]]), ints([1, 1]), ints([0, 5, 10])
+    for new in (counts, cu[:2], keep.view(-1)):
+        with pytest.raises(b.FaError) as e:
+            b.compact_paged(handle, b.PagedCache(k, v), table, lens, keep, counts, cu_seqlens=cu, new_lens=new)
+        assert e.value.status == b.FA_ERR_INVALID_ARG
+    torch.cuda.synchronize()
+    ok(handle)
+    assert torch.equal(k, k0) and torch.equal(v, v0) and counts.tolist() == [1, 1] and cu.tolist() == [0, 5, 10] and keep.tolist() == [[1], [2]]
