@@ -650,6 +650,9 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             prefetch_l2(p.block_table + b * p.table_stride + (line - b * per_row) * 32);
         }
     }
+    // Rows of the query tiles that no load fills count as zeros (see the softmax warps)
+    for (int i = tid; i < Cfg::kQSpace / 16; i += Cfg::kThreads) st_shared_v4(sQ + 16 * i, 0, 0, 0, 0);
+    fence_proxy_async_smem();
     grid_dependency_wait();
 
     const TreeSeqs seq_of{a.t.cu_seqlens, p.seq_lens, p.B, a.t.total, a.t.max_tokens, p.max_pages, p.page_size};
@@ -702,9 +705,10 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 c *= p.k_scale ? p.k_scale[e.kvh] : 1.f;
                 n_q += nt > 0;
             }
-            // Rows that are not the block's hold what the space held before, whose scores may rise from tile to tile and would have their warp
-            // move references all the time: they count as zeros, whose reference never moves.
+            // Rows that are not the block's (zeros, or other sequences' queries) count as zeros with probabilities of zero: scores that rise from
+            // tile to tile would have their warp move references all the time, and products of zeros take less of the power limit.
             if (!live) c = 0.f;
+            const float bias = live ? Cfg::kBias : -INFINITY;
             float m_ref = -INFINITY, l = 0.f, tau_raw = kRescaleThresholdLog2 / c;
             for (int j = 0; j < steps; ++j, ++n_s) {
                 ok = __all_sync(0xffffffffu, ok && tree_wait_timed(sh.s_full[t], n_s & 1, &sh.wait, kSiteSoftmaxSFull));
@@ -724,8 +728,20 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                     if (j > 0) ok = tree_wait_timed(sh.o_final[t], (n_s & 1) ^ 1, &sh.wait, kSiteSoftmaxPFree);
                     __syncwarp();
                 };
-                if (!warp_live) {            // (what P holds then meets rows that are not stored)
-                    if constexpr (Cfg::kPSmem) take();
+                if (!warp_live) {            // (its rows are not stored)
+                    if constexpr (Cfg::kPSmem) {
+                        take();
+                        if (j == 0) {
+#pragma unroll
+                            for (int v = 0; v < 16; ++v) st_shared_v4(sP + t * Cfg::kPBytes + (v >> 3) * kChunkBytes + row * 128 + (v & 7) * 16, 0, 0, 0, 0);
+                            fence_proxy_async_smem();
+                        }
+                    } else {
+                        const uint32_t zeros[16] = {};
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) tmem_st_x16(tS + 16 * q, zeros);
+                        tc_wait_st();
+                    }
                     tc_fence_before_sync();
                     __syncwarp();
                     if (lane == 0) {
@@ -750,7 +766,7 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                     }
                     tc_wait_st();
                 }
-                tree_pass<DV, kE4m3, Cfg::kPSmem>(tS, tO + 128 * t, sP + t * Cfg::kPBytes + row * 128, c, tau_raw, Cfg::kBias, j == 0, m_ref, l, lane, take,
+                tree_pass<DV, kE4m3, Cfg::kPSmem>(tS, tO + 128 * t, sP + t * Cfg::kPBytes + row * 128, c, tau_raw, bias, j == 0, m_ref, l, lane, take,
                                      [&]() { mbar_arrive(bar_pf); }, [&]() { mbar_arrive(bar_pr); });
             }
             // ---- the part's result: sum and reference of a row that saw a key, O of one stream or of both
@@ -1256,7 +1272,7 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             const int row = lane & 4 ? (lane >> 3) ^ 5 : lane >> 3, piece = lane & 3;
             const uint32_t in_even = row * 128 + ((piece ^ row) << 4), in_odd = in_even ^ 64u;
             const uint32_t out0 = row * 128 + (((2 * piece) ^ row) << 4), out1 = out0 ^ 16u;
-            const int q_row = tid & (kTileM - 1);
+            const int q_row = tid & (kTileM - 1), row_token = q_row / a.list.row_heads, row_head = q_row - row_token * a.list.row_heads;
             int s = 0, r = 0, n_q = 0;
             uint32_t ph = 1, ph_r = 0;
             bool ok = true;
@@ -1270,6 +1286,8 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 // (128 columns: the last term of the first 64 waits in local memory).  (Here and not by the softmax warps, which are
                 // still at the part before: the first scores of a part came 7000 cycles after its beginning.)
                 ok = __all_sync(0xffffffffu, wait(sh.q_full, n_q & 1));
+                const int tc = a.list.head_chunks == 1 ? e.row_tile : e.row_tile / a.list.head_chunks, hc = e.row_tile - tc * a.list.head_chunks;
+                const bool live = row_token < a.list.row_tokens && tc * a.list.row_tokens + row_token < e.n && hc * a.list.row_heads + row_head < a.group;
                 uint32_t top = 0;
 #pragma unroll 1
                 for (int cc = 0; cc < Cfg::kQChunks; ++cc) {
@@ -1295,7 +1313,7 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                         const uint32_t w8[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
                         uint32_t h[8];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) h[i] = pack_f16x2(__uint_as_float(w8[i] << 16) * mult, __uint_as_float(w8[i] & 0xffff0000u) * mult);
+                        for (int i = 0; i < 8; ++i) h[i] = live ? pack_f16x2(__uint_as_float(w8[i] << 16) * mult, __uint_as_float(w8[i] & 0xffff0000u) * mult) : 0u;
                         const uint32_t at = sQ + (cc >> 1) * kChunkBytes + q_row * 128 + ((((cc & 1) * 4 + u) ^ (q_row & 7)) << 4);
 #pragma unroll
                         for (int term = 0; term < Cfg::kTerms; ++term) {
