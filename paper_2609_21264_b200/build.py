@@ -9,7 +9,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libfa_b200.so")
 CALLS_PATH = os.path.join(_HERE, "_fa_calls.so")
-SOURCES = ("fa_api.cu", "fa_noalloc.cu", "fa_paged.cu", "fa_drafts.cu", "fa_tree.cu")
+SOURCES = ("fa_api.cu", "fa_noalloc.cu", "fa_paged.cu", "fa_drafts.cu", "fa_tree.cu", "fa_tree_few.cu")
 NVCC_FLAGS = ("-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-shared", "-Xcompiler", "-fPIC", "-Xptxas", "-v", "--threads", "0")
 

@@ -38,6 +38,8 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 #include "fa_paged_common.cuh"
 
 namespace fa {
@@ -225,6 +227,9 @@ struct PagedShared {
     long long row_q[kRows], row_o[kRows];
     int row_place[kRows], row_i[kRows], row_h[kRows];
 };
+// Drafted tokens: those of a part's sequence, and the first one's row (PagedShared::i holds every row's word of the mask).
+template <int kRows, int kMaps>
+struct PagedTreeShared : PagedShared<kRows, kMaps> { int n[kPartRing], row0[kPartRing]; };
 
 template <int DQK, int DV, bool kE4m3, bool kDiff, int kRows>
 struct PagedCfg {
@@ -273,10 +278,10 @@ struct PagedCfg {
     static constexpr float kBias = kE4m3 ? 11.f : 0.f;
 };
 
-template <int DQK, int DV, bool kE4m3, bool kDiff, int kRows>
+template <int DQK, int DV, bool kE4m3, bool kDiff, int kRows, bool kTree = false>
 constexpr int paged_smem_bytes() {
     using Cfg = PagedCfg<DQK, DV, kE4m3, kDiff, kRows>;
-    return Cfg::kTileBytes + static_cast<int>(sizeof(PagedShared<kRows, Cfg::kMaps>));
+    return Cfg::kTileBytes + static_cast<int>(kTree ? sizeof(PagedTreeShared<kRows, Cfg::kMaps>) : sizeof(PagedShared<kRows, Cfg::kMaps>));
 }
 // Bytes of a partial result: unnormalised O of every state (fp32) and its maximum and sum.
 constexpr long long paged_slot_bytes(int dv, int states) { return states * (dv + 2) * 4ll; }
@@ -295,11 +300,14 @@ FA_DEVI void paged_mma(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc,
     else ptx::mma_ss(d, kHi | a_lo, kHiB | b_lo, idesc, accumulate);
 }
 
-template <int DQK, int DV, bool kE4m3, bool kDiff, int kRows>
+// kTree: drafted tokens, one block of rows (so 32 drafts at most: a word of the mask each).  Every sequence has a number of tokens of its own,
+// and what it sees of them is in its row's word; a sequence without drafts counts as one without keys.
+template <int DQK, int DV, bool kE4m3, bool kDiff, int kRows, bool kTree = false>
 __global__ void __launch_bounds__(512, 1)
 fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const PagedParams p) {
+    static_assert(!kTree || (!kDiff && kRows <= 32), "one map, one word of a mask");
     using Cfg = PagedCfg<DQK, DV, kE4m3, kDiff, kRows>;
-    using Shared = PagedShared<kRows, Cfg::kMaps>;
+    using Shared = std::conditional_t<kTree, PagedTreeShared<kRows, Cfg::kMaps>, PagedShared<kRows, Cfg::kMaps>>;
     using namespace ptx;
     constexpr int NS = Cfg::kStages, kMaps = Cfg::kMaps, kTerms = Cfg::kTerms, kPTerms = Cfg::kPTerms, kStates = Cfg::kStates, kCols = Cfg::kCols;
     constexpr int kBufs = Cfg::kSBufs / 2;        // score buffers of a group
@@ -382,6 +390,9 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         // wait for one after the other
         const int at = tid & 127, per_row = (p.max_pages + 31) / 32, line = blockIdx.x * 128 + at, b = line / per_row;
         if (at * 32 < p.B) prefetch_l2(p.seq_lens + at * 32);
+        if constexpr (kTree) {
+            if (p.cu_seqlens && at * 32 < p.B) prefetch_l2(p.cu_seqlens + at * 32);
+        }
         if (b < p.B) prefetch_l2(p.block_table + b * p.table_stride + (line - b * per_row) * 32);
     }
     tc_fence_before_sync();
@@ -394,6 +405,13 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
     auto s_col = [&](int w, int i) -> uint32_t { return (w * kBufs + i) * Cfg::kSCols; };
     auto o_col = [&](int ob, int w) -> uint32_t { return Cfg::kSBufs * Cfg::kSCols + (ob * 2 + w) * kCols; };
     PagedWait* const wait = &sh.wait;
+    // length of sequence b in the list, and (d) its drafts
+    auto seq_len = [&](int b, uint32_t* status, DraftRows& d) -> int {
+        const int len = paged_len(p, b, status);
+        if constexpr (!kTree) return len;
+        d = draft_rows(p.cu_seqlens, b, p.B, p.total, p.Sq, status);
+        return d.count > 0 ? len : 0;
+    };
     auto wait_part = [&](int k) -> bool { return paged_wait(sh.part_full[k % kPartRing], (k / kPartRing) & 1, wait); };
 
     if (warp == 0 || warp == 2) {
@@ -564,6 +582,8 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             ok = ok && wait_part(k);
             const PagedEntry& entry = sh.part[k % kPartRing];
             const int t0 = entry.t0, t1 = entry.t1, len = entry.len, tile0 = entry.tile0;
+            int n_drafts = 0;
+            if constexpr (kTree) n_drafts = sh.n[k % kPartRing];
             if (named_barrier_or(1 + w, 128, !ok) || t1 < 0) break;
             // (also by a group without a tile here: its arrival at q_empty must not run ahead into the buffer's next turn)
             ok = paged_wait(sh.q_full[qb], (k >> 1) & 1, wait);
@@ -572,7 +592,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                 float l[kStates];
 #pragma unroll
                 for (int r = 0; r < kStates; ++r) l[r] = 0.f;
-                const int first_masked = len - p.Sq + 1;                 // the first key that some row does not see
+                const int first_masked = kTree ? len - n_drafts : len - p.Sq + 1;      // the first key that some row does not see
                 const uint32_t tO = tmem + o_col(k % kOBufs, w) + lane_sel;
 #pragma unroll 1
                 for (int t = t0 + skip; t < t1; t += 2, ++mine_n) {
@@ -620,9 +640,20 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                     __syncwarp();
                     if (lane == 0) mbar_arrive(smem_addr(&sh.s_empty[w][sb]));
                     if (t * kTileN + kTileN > first_masked) {
+                        if constexpr (kTree) {
+                            // (no row has a bit for keys behind the drafts; a key before them is seen by all)
+                            const int draft = key_at - first_masked;
+                            const uint32_t bit = draft < 0 ? 0u : draft < 32 ? 1u << draft : 0u;
+                            if (draft >= 0) {
 #pragma unroll
-                        for (int r = 0; r < kStates; ++r)
-                            if (key_at >= first_masked + sh.i[qb][r % kRows]) x[r] = -INFINITY;
+                                for (int r = 0; r < kStates; ++r)
+                                    if (!(static_cast<uint32_t>(sh.i[qb][r]) & bit)) x[r] = -INFINITY;
+                            }
+                        } else {
+#pragma unroll
+                            for (int r = 0; r < kStates; ++r)
+                                if (key_at >= first_masked + sh.i[qb][r % kRows]) x[r] = -INFINITY;
+                        }
                     }
                     bool move = first;
                     if (!first) {
@@ -790,7 +821,8 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         int mine = 0, longest = 0;
 #pragma unroll 4
         for (int b = b_first; b < b_last; ++b) {
-            const int n = paged_len(p, b, nullptr);
+            DraftRows d;
+            const int n = seq_len(b, nullptr, d);
             mine += paged_units(p, n, PagedCount{0, 0, 0});
             longest = max(longest, n);
         }
@@ -831,7 +863,8 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         if (before <= u0 && u0 < before + mine) {
             int b = b_first, base = before;
             for (;; ++b) {
-                const int n = paged_units(p, paged_len(p, b, nullptr), cnt);
+                DraftRows d;
+                const int n = paged_units(p, seq_len(b, nullptr, d), cnt);
                 if (u0 < base + n) break;
                 base += n;
             }
@@ -843,11 +876,12 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         // results of part k begin (those of the parts before have been stored).  A CTA without a share has the end mark alone.
         const int blocks = p.Hkv * p.row_blocks;
         int seq = 0, base = 0, len = 0, hr = 0, published = 0, tiles = 0;
+        DraftRows drafts{0, 0};       // of the sequence
         bool ended = u0 >= total, marked = false;
         if (wq == 3 && !ended) {
             seq = sh.start_b;
             base = sh.start_base;
-            len = paged_len(p, seq, lane == 0 ? p.status : nullptr);
+            len = seq_len(seq, lane == 0 ? p.status : nullptr, drafts);
             hr = (u0 - base) / paged_block_units(len, cnt);
         }
         auto publish = [&](int k) {
@@ -863,6 +897,10 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                     e.tile0 = tiles + (lane > 0 ? first_tiles + (lane - 1) * nt : 0);
                     const int at = (published + lane) % kPartRing;
                     sh.part[at] = e;
+                    if constexpr (kTree) {
+                        sh.n[at] = drafts.count;
+                        sh.row0[at] = drafts.first;
+                    }
                     mbar_arrive(smem_addr(&sh.part_full[at]));
                 }
                 const int last_tiles = __shfl_sync(0xffffffffu, e.t1 - e.t0, max(0, count - 1));
@@ -877,7 +915,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                         hr = 0;
                         if (base < u1) {
                             ++seq;
-                            len = paged_len(p, seq, lane == 0 ? p.status : nullptr);
+                            len = seq_len(seq, lane == 0 ? p.status : nullptr, drafts);
                         } else {
                             ended = true;
                         }
@@ -900,6 +938,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
         constexpr int kPasses = (kRows + kPass - 1) / kPass;
         const int row_in = key / kLanes, piece = key % kLanes;
         uint4 xs[kPasses];
+        uint32_t seen[kTree ? kPasses : 1];      // what the rows see of the drafts
         float q_scale = 1.f;
         int q_rb = 0, o_rb = 0;       // the blocks whose rows sh.row_q and sh.row_o are
         auto load_queries = [&](int k) {
@@ -910,14 +949,28 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                 if (key < kRows) rows_of_q(q_rb, key);
                 named_barrier_sync(kBar, 128);
             }
-            const __nv_bfloat16* const q = p.Q + e.b * p.q_sb + static_cast<long long>(e.kvh * group) * p.q_sh + piece * 8;
+            int n = 0, row0 = 0;
+            if constexpr (kTree) {
+                n = sh.n[k % kPartRing];
+                row0 = sh.row0[k % kPartRing];
+            }
+            const __nv_bfloat16* const q = p.Q + (kTree ? row0 * p.q_st : e.b * p.q_sb) + static_cast<long long>(e.kvh * group) * p.q_sh + piece * 8;
 #pragma unroll
             for (int j = 0; j < kPasses; ++j) {
                 const int r = j * kPass + row_in;
                 xs[j] = make_uint4(0, 0, 0, 0);
+                if constexpr (kTree) seen[j] = 0u;
                 if (r < kRows && piece < kVecs) {
                     const long long at = sh.row_q[r];
-                    if (at >= 0) xs[j] = *reinterpret_cast<const uint4*>(q + at);
+                    if constexpr (kTree) {
+                        const int i = sh.row_place[r];
+                        if (at >= 0 && i < n) {
+                            xs[j] = *reinterpret_cast<const uint4*>(q + at);
+                            if (piece == 0) seen[j] = draft_word(TreeParams{nullptr, 0, 0, p.mask, p.mask_stride}, row0 + i, i, n, 0);
+                        }
+                    } else if (at >= 0) {
+                        xs[j] = *reinterpret_cast<const uint4*>(q + at);
+                    }
                 }
             }
             q_scale = p.scale_log2 * (kE4m3 && p.k_scale ? p.k_scale[e.kvh] : 1.f);
@@ -971,7 +1024,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                 }
                 if (r < kRows && piece == 0) {
                     if constexpr (kE4m3) sh.c[qb][r] = c;
-                    sh.i[qb][r] = sh.row_place[r];
+                    sh.i[qb][r] = kTree ? static_cast<int>(seen[kTree ? j : 0]) : sh.row_place[r];
                 }
             }
             fence_proxy_async_smem();
@@ -1010,7 +1063,13 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                 named_barrier_sync(kBar, 128);
             }
             const int hq0 = e.kvh * group;
-            __nv_bfloat16* const out = p.O + e.b * p.o_sb + hq0 * p.o_sh;
+            int n_drafts = 0, row0 = 0;
+            if constexpr (kTree) {
+                n_drafts = sh.n[k % kPartRing];
+                row0 = sh.row0[k % kPartRing];
+            }
+            auto row_out = [&](int r) -> long long { return !kTree || sh.row_i[r] < n_drafts ? sh.row_o[r] : -1; };
+            __nv_bfloat16* const out = p.O + (kTree ? row0 * p.o_st : e.b * p.o_sb) + hq0 * p.o_sh;
             const float vs = kE4m3 && p.v_scale ? p.v_scale[e.kvh] : 1.f;
             float* const slot_o = p.part + static_cast<long long>(whole ? 0 : e.slot) * kStates * (DV + 2);
             float* const slot_ml = slot_o + kStates * DV;
@@ -1033,8 +1092,9 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             if (known) load_other();
             // log-sum-exp of a row (natural units) from its maximum (log2 units) and sum
             auto store_lse = [&](int r, float m, float sum) {
-                if (kDiff || !p.lse || sh.row_o[r] < 0) return;
-                p.lse[static_cast<long long>(hq0 + sh.row_h[r]) * p.B * p.Sq + static_cast<long long>(e.b) * p.Sq + sh.row_i[r]] =
+                if (kDiff || !p.lse || row_out(r) < 0) return;
+                const long long tokens = kTree ? p.total : static_cast<long long>(p.B) * p.Sq, first = kTree ? row0 : static_cast<long long>(e.b) * p.Sq;
+                p.lse[(hq0 + sh.row_h[r]) * tokens + first + sh.row_i[r]] =
                     sum > 0.f || sum != sum ? (m - Cfg::kBias + log2f(sum)) * 0.6931471805599453f : -INFINITY;
             };
             // (uniform) whether a group had a tile of this part
@@ -1126,7 +1186,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                 if (key < DV) {
 #pragma unroll
                     for (int r = 0; r < kRows; ++r) {
-                        const long long at = sh.row_o[r];
+                        const long long at = row_out(r);
                         if (at >= 0) out[at + key] = __float2bfloat16(y[r]);
                     }
                 }
@@ -1269,7 +1329,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                         }
                         o.x *= f * w.x; o.y *= f * w.y; o.z *= f * w.z; o.w *= f * w.w;
                     }
-                    const long long at = sh.row_o[r];
+                    const long long at = row_out(r);
                     if (at >= 0)
                         *reinterpret_cast<uint2*>(out + at + col) = make_uint2(pack_bf16x2(o.x, o.y), pack_bf16x2(o.z, o.w));
                 }

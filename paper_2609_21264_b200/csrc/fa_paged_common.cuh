@@ -44,6 +44,11 @@ struct PagedParams {
     uint32_t* status;
     unsigned long long wait_limit_ns;
     int debug_drop_v_load;
+    // drafted tokens: token i of sequence b is row cu_seqlens[b] + i of Q, O and lse, Sq the largest number of them
+    const int* cu_seqlens;        // nullptr: total / B tokens each
+    const uint32_t* mask;         // as in TreeParams
+    long long mask_stride;
+    int total;
 };
 
 // The place is the report (one store, so that reports of several CTAs cannot mix), in a word of its own behind the code and place of a
@@ -82,6 +87,24 @@ __host__ __device__ inline DraftRows draft_rows(const int* cu_seqlens, int b, in
         r.first = r.count = 0;
     }
     return r;
+}
+
+// What the kernels on drafted tokens take beside PagedParams (whose Sq, q_sb and o_sb they do not use).
+struct TreeParams {
+    const int* cu_seqlens;        // nullptr: total / B tokens each
+    int total, max_tokens;
+    const uint32_t* mask;         // nullptr: causal among the drafts
+    long long mask_stride;
+};
+
+// Word w of what token i of n sees among the drafts: bits 32 w .. 32 w + 31 (none from n on).
+FA_DEVI uint32_t draft_word(const TreeParams& tp, int row, int i, int n, int w) {
+    if (w < 0 || 32 * w >= n) return 0u;
+    const int here = n - 32 * w;                                  // drafts from this word on
+    const uint32_t in_range = here >= 32 ? 0xffffffffu : (1u << here) - 1u;
+    if (tp.mask) return tp.mask[row * tp.mask_stride + w] & in_range;
+    const int upto = i - 32 * w;
+    return upto < 0 ? 0u : upto >= 31 ? in_range : in_range & ((2u << upto) - 1u);
 }
 
 FA_DEVI float e4m3_to_float(uint8_t code) {

@@ -5,6 +5,10 @@
 #include <stdint.h>
 #include <string.h>
 
+#include <algorithm>
+#include <memory>
+#include <new>
+
 #include "../../include/fa.h"
 #include "fa_handle.h"
 #include "fa_paged_common.cuh"
@@ -12,9 +16,23 @@
 #include "fa_tree.cuh"
 #include "fa_tree_simple.cuh"
 
+namespace fa_host {      // (fa_tree_few.cu)
+
+fa_status launch_tree_few(fa_handle* h, int dqk, int dv, bool e4m3, const CUtensorMap& mk, const CUtensorMap& mv, fa::PagedParams& p, cudaStream_t st);
+fa_status plan_tree_few(int num_sms, size_t scratch, fa::PagedParams& p, int dqk, int dv, bool e4m3, fa_paged_plan_info* out, fa_paged_piece* pieces,
+                        int max_pieces);
+
+}  // namespace fa_host
+
 namespace {
 
 using namespace fa_host;
+
+// Few rows are columns of turned products, many are lanes: a pass over the keys costs the streaming kernel's softmax warps what the rows
+// are, and this one 128 rows whatever they are.  64 sequences of 300 keys, 64/8 heads of 128: 8 rows 17.8 us against 40.5, 32 rows 24.7
+// against 38.0, 64 rows 51.2 against 38.0; 48 of 4200 keys over e4m3 69.5 against 117.9, 78.1 against 126.2, 145.4 against 137.1.  (The
+// largest loss: one sequence of 8000 keys, 32/8 heads, 32 rows, 19.4 against 18.6.)
+bool few_rows(int group, int max_tokens) { return static_cast<long long>(group) * max_tokens <= 32; }
 
 template <bool kE4m3>
 fa_status launch_simple(fa_handle* h, int dqk, const fa::PagedParams& p, const fa::TreeParams& tp, cudaStream_t st) {
@@ -131,15 +149,24 @@ fa_status fa_forward_paged_tree(fa_handle* h, const fa_paged_cache* cache, const
     while (p.box_rows < 128 && cache->page_size % (2 * p.box_rows) == 0) p.box_rows *= 2;
     const int eb = e4m3 ? 1 : 2;
     const CUtensorMap* m = nullptr;
+    const bool few = few_rows(a.group, tree->max_tokens);
+    CUtensorMap mq = {};
     // (queries: heads in the place of rows, tokens in that of heads; one head may have any stride)
-    if ((s = get_map(h, Q, cache->dqk, Hq, total, 1, q_strides[0], q_strides[0], q_strides[1], a.list.row_heads, &m, 2, a.list.row_tokens)) != FA_OK) return s;
-    const CUtensorMap mq = *m;       // copies: a later insertion may move the cache's entries
+    if (!few) {
+        if ((s = get_map(h, Q, cache->dqk, Hq, total, 1, q_strides[0], q_strides[0], q_strides[1], a.list.row_heads, &m, 2, a.list.row_tokens)) != FA_OK) return s;
+        mq = *m;                     // copies: a later insertion may move the cache's entries
+    }
     if ((s = get_map(h, cache->k, cache->dqk, cache->page_size, cache->Hkv, cache->num_pages, cache->k_strides[0], cache->k_strides[1],
                      cache->k_strides[2], p.box_rows, &m, eb, 1, 128, map_promotion(cache->dqk, eb, cache->k_strides))) != FA_OK) return s;
     const CUtensorMap mk = *m;
     if ((s = get_map(h, cache->v, cache->dv, cache->page_size, cache->Hkv, cache->num_pages, cache->v_strides[0], cache->v_strides[1],
                      cache->v_strides[2], p.box_rows, &m, eb, 1, 128, map_promotion(cache->dv, eb, cache->v_strides))) != FA_OK) return s;
     const CUtensorMap mv = *m;
+    if (few) {
+        p.Sq = tree->max_tokens;
+        p.cu_seqlens = tree->cu_seqlens; p.mask = tree->mask; p.mask_stride = tree->mask_stride; p.total = total;
+        return launch_tree_few(h, cache->dqk, cache->dv, e4m3, mk, mv, p, st);
+    }
     h->last_kernel = e4m3 ? "fa_tree_e4m3" : "fa_tree";
     h->last_splits = 1;
     if (cache->dqk == 64) return e4m3 ? launch_tree<64, 64, true>(h, mq, mk, mv, p, a, st) : launch_tree<64, 64, false>(h, mq, mk, mv, p, a, st);
@@ -163,9 +190,26 @@ fa_status fa_plan_paged_tree(int num_sms, const fa_config* cfg, const fa_paged_c
     }
     fa::TreeList li = make_list(Hq / cache->Hkv, tree->max_tokens, cache->dqk, cache->type == FA_CACHE_E4M3);
     if (too_long(li, seqs->B, cache->Hkv, tree->max_tokens, static_cast<long long>(seqs->max_pages) * cache->page_size)) return FA_ERR_UNSUPPORTED;
-    const int ctas = tree_ctas(num_sms, scratch, cache->dv, li.two != 0), B = seqs->B;
-    if (ctas < 1) return FA_ERR_UNSUPPORTED;
+    const int B = seqs->B;
     const fa::TreeSeqs seq_of{tree->cu_seqlens, seqs->seq_lens, B, total, tree->max_tokens, seqs->max_pages, cache->page_size};
+    if (few_rows(Hq / cache->Hkv, tree->max_tokens)) {
+        // (a sequence without drafts counts as one without keys)
+        std::unique_ptr<int32_t[]> lens(new (std::nothrow) int32_t[B]);
+        if (!lens) return FA_ERR_CUDA;
+        for (int b = 0; b < B; ++b) {
+            int n, row0, len;
+            seq_of(b, n, row0, len);
+            lens[b] = n > 0 ? len : 0;
+        }
+        fa::PagedParams p;
+        memset(&p, 0, sizeof p);
+        p.seq_lens = lens.get();
+        p.B = B; p.max_pages = seqs->max_pages; p.page_size = cache->page_size; p.Hkv = cache->Hkv; p.Hq = Hq; p.Sq = tree->max_tokens;
+        return plan_tree_few(num_sms, std::min(scratch, static_cast<uint64_t>(32) << 20), p, cache->dqk, cache->dv, cache->type == FA_CACHE_E4M3, out,
+                             pieces, max_pieces);
+    }
+    const int ctas = tree_ctas(num_sms, scratch, cache->dv, li.two != 0);
+    if (ctas < 1) return FA_ERR_UNSUPPORTED;
     auto units_of = [&](int b) {
         int n, row0, len;
         seq_of(b, n, row0, len);

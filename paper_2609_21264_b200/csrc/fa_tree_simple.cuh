@@ -10,24 +10,6 @@
 
 namespace fa {
 
-// What the kernels on drafted tokens take beside PagedParams (whose Sq, q_sb and o_sb they do not use).
-struct TreeParams {
-    const int* cu_seqlens;        // nullptr: total / B tokens each
-    int total, max_tokens;
-    const uint32_t* mask;         // nullptr: causal among the drafts
-    long long mask_stride;
-};
-
-// Word w of what token i of n sees among the drafts: bits 32 w .. 32 w + 31 (none from n on).
-FA_DEVI uint32_t draft_word(const TreeParams& tp, int row, int i, int n, int w) {
-    if (w < 0 || 32 * w >= n) return 0u;
-    const int here = n - 32 * w;                                  // drafts from this word on
-    const uint32_t in_range = here >= 32 ? 0xffffffffu : (1u << here) - 1u;
-    if (tp.mask) return tp.mask[row * tp.mask_stride + w] & in_range;
-    const int upto = i - 32 * w;
-    return upto < 0 ? 0u : upto >= 31 ? in_range : in_range & ((2u << upto) - 1u);
-}
-
 template <int DQK, int DV, bool kE4m3>
 __global__ void __launch_bounds__(128)
 fa_tree_simple_kernel(const PagedParams p, const TreeParams tp) {
