@@ -504,3 +504,96 @@ def test_launches_without_overlap_and_two_handles_at_once():
     finally:
         for h in handles:
             b.fa_destroy(h)
+
+
+# (drafts, query heads, K/V heads) up to 32 rows, the last of each group just above
+FEW = [(1, 1, 1), (16, 2, 2), (32, 1, 1), (33, 1, 1), (8, 4, 2), (16, 4, 2), (17, 4, 2), (5, 9, 3), (8, 8, 2), (4, 14, 2), (5, 14, 2), (4, 8, 1), (2, 16, 1),
+       (1, 31, 1), (1, 32, 1), (1, 33, 1), (3, 10, 1), (4, 10, 1)]
+
+
+@pytest.mark.parametrize("most,Hq,Hkv", FEW)
+@pytest.mark.parametrize("dqk,dv", [(64, 64), (128, 128), (192, 128)])
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+def test_few_rows(handle, most, Hq, Hkv, dqk, dv, e4m3):
+    """Up to 32 rows and the first number above: ragged trees around the borders of a tile, sequences without drafts or without keys."""
+    n = [min(most, x) for x in (3, 0, 1, 32, 2, 5, 0, 17, 33, 4)]
+    lens = [700, 300, 1, 129, 128, 5, 0, 257, 33, 127]
+    assert all(a <= x for a, x in zip(n, lens))
+    run(handle, lens, n, Hq, Hkv, dqk, dv, 16, e4m3, heads_first=e4m3, seed=most + Hq, most=most, pad=2)
+
+
+@pytest.mark.parametrize("masks", ["tree", "chain", "random", "none"])
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("Hq,Hkv,most", [(2, 2, 32), (2, 2, 16), (8, 2, 8), (24, 1, 1)])
+def test_masks_of_few_rows(handle, masks, e4m3, Hq, Hkv, most):
+    """Rows that see nothing, in sequences that have nothing but drafts, or fewer keys than drafts; bits of n and more are not looked at."""
+    n = [most, 1, min(most, 9), most, 0, 1, most, most]
+    run(handle, [most, 1, 3, 300, 40, 0, 129, 128 + most // 2], n, Hq, Hkv, 128, 128, 32, e4m3, seed=9, masks=masks, most=most, pad=1)
+    run(handle, [300, 0, 17], [most] * 3, Hq, Hkv, 64, 64, 16, e4m3, seed=10, masks=masks, cu=False)
+    run(handle, [0, 0], [most] * 2, Hq, Hkv, 192, 128, 16, e4m3, seed=11, masks=masks, cu=False)
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+def test_few_rows_long_and_many(handle, e4m3):
+    run(handle, [20000], [4], 8, 1, 128, 128, 64, e4m3, seed=5)
+    run(handle, [9000, 20, 9100], [30, 2, 32], 2, 2, 64, 64, 48, e4m3, seed=5, most=32)
+    run(handle, [(i * 53) % 260 for i in range(200)], [min((i * 53) % 260, i % 9) for i in range(200)], 4, 2, 192, 128, 16, e4m3, seed=6)
+    run(handle, [3000] + [3] * 40 + [9000], [8] + [3] * 40 + [7], 8, 2, 128, 128, 16, e4m3, seed=7, q_mult=3.0)
+
+
+def test_a_chain_of_few_drafts_is_the_paged_call():
+    """Equally many drafts in a chain: the kernel, and the bits, of fa_forward_paged."""
+    from paper_2609_21264_b200 import binding as b
+    h = b.fa_create()
+    try:
+        for e4m3, dqk, dv, Hq, Hkv, n in ((False, 128, 128, 8, 2, 4), (True, 128, 128, 8, 2, 8), (False, 64, 64, 4, 4, 16), (True, 192, 128, 6, 1, 5)):
+            k, v, table, lens_t, ks, vs = pool([900, 40, 3000], 16, Hkv, dqk, dv, e4m3, False, 31)
+            q = torch.randn(3 * n, Hq, dqk, generator=torch.Generator().manual_seed(3)).to(torch.bfloat16).cuda()
+            cache = b.PagedCache(k, v, ks, vs)
+            want = b.forward_paged(h, q, cache, table, lens_t)
+            got = b.forward_paged_tree(h, q, cache, table, lens_t, None)
+            ok(h)
+            assert b.fa_last_kernel_name(h) == ("fa_tree_few_e4m3" if e4m3 else "fa_tree_few")
+            assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+    finally:
+        b.fa_destroy(h)
+
+
+def test_few_rows_captured_with_other_contents(handle):
+    """A captured call of few rows follows what lengths, offsets, masks and the table hold when it is replayed."""
+    from paper_2609_21264_b200 import binding as b
+    g = torch.Generator().manual_seed(41)
+    first, then = ([500, 130, 0], [4, 7, 0]), ([260, 505, 9], [8, 1, 2])
+    k, v, table, lens_t, _, _ = pool([520, 520, 520], 16, 2, 128, 128, False, False, 17)
+    q = torch.randn(13, 8, 128, generator=g).to(torch.bfloat16).cuda()
+    cu, mask, lens = torch.zeros(4, dtype=torch.int32, device="cuda"), torch.zeros(13, 1, dtype=torch.int32, device="cuda"), torch.zeros_like(lens_t)
+    out = torch.zeros(13, 8, 128, dtype=torch.bfloat16, device="cuda")
+    cache = b.PagedCache(k, v)
+
+    def fill(lengths, counts):
+        seens, offsets = [torch.rand(n, n, generator=g) < 0.5 for n in counts], [0]
+        for n in counts:
+            offsets.append(offsets[-1] + n)
+        rows = torch.full((13, 1), -1, dtype=torch.int32)
+        for s, a, n in zip(seens, offsets, counts):
+            rows[a:a + n] = pack(s, 1)
+        lens.copy_(torch.tensor(lengths, dtype=torch.int32))
+        cu.copy_(torch.tensor(offsets, dtype=torch.int32))
+        mask.copy_(rows)
+        out.fill_(7.0)
+        return tree_reference(q[:offsets[-1]], k, v, None, None, table, lengths, offsets, seens, 128 ** -0.5), offsets[-1]
+
+    call = lambda: b.forward_paged_tree(handle, q, cache, table, lens, mask, cu_seqlens=cu, max_tokens=8, out=out)  # noqa: E731
+    ref, n = fill(*first)
+    call()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        _, lse = call()
+    for what in (first, then, first):
+        ref, n = fill(*what)
+        graph.replay()
+        torch.cuda.synchronize()
+        ok(handle)
+        assert_attention(out[:n], lse[:, :n], *ref)
+        assert (out[n:] == 7).all()
