@@ -597,3 +597,126 @@ def test_few_rows_captured_with_other_contents(handle):
         ok(handle)
         assert_attention(out[:n], lse[:, :n], *ref)
         assert (out[n:] == 7).all()
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("Hq,n", [(1, 20), (2, 8)], ids=["32rows", "16rows"])
+def test_numbers_that_are_none_in_few_rows(handle, e4m3, Hq, n):
+    """A draft's key of NaN or infinities and a query of NaN concern the rows that see the one and are the other; a masked value of 2^120 (bf16)
+    weighs nothing."""
+    from paper_2609_21264_b200 import binding as b
+    k, v, table, lens_t, ks, vs = pool([150], 16, 1, 128, 128, e4m3, False, 12)
+    seen, _ = seen_by(random_parents(n, torch.Generator().manual_seed(4)))
+    q = torch.randn(n, Hq, 128, generator=torch.Generator().manual_seed(5)).to(torch.bfloat16).cuda()
+    mask, cache, draft = pack(seen, 1).cuda(), b.PagedCache(k, v, ks, vs), int(seen[:, :n - 1].sum(0).float().add(torch.arange(n - 1) * 1e-3).argmax())
+    o0, lse0 = b.forward_paged_tree(handle, q, cache, table, lens_t, mask)
+    ok(handle)
+    hit = seen[:, draft].cuda()
+    assert hit.any() and not hit.all()
+    at = 150 - n + draft
+    page, slot = int(table[0, at // 16]), at % 16
+    if not e4m3:
+        kept = v[page, :, slot].clone()
+        v[page, :, slot] = 2.0 ** 120
+        o1, _ = b.forward_paged_tree(handle, q, cache, table, lens_t, mask)
+        ok(handle)
+        assert torch.equal(o1[~hit], o0[~hit]) and not torch.equal(o1[hit], o0[hit])
+        v[page, :, slot] = kept
+    if e4m3:
+        k.view(torch.uint8)[page, :, slot] = 0x7F
+    else:
+        k[page, :, slot] = float("nan")
+        k[page, :, slot, ::3] = float("inf")
+    o1, lse1 = b.forward_paged_tree(handle, q, cache, table, lens_t, mask)
+    ok(handle)
+    assert torch.equal(o1[~hit], o0[~hit]) and torch.equal(lse1[:, ~hit], lse0[:, ~hit])
+    assert torch.isnan(o1[hit]).all() and torch.isnan(lse1[:, hit]).all()
+    row = int((~hit).nonzero()[0])
+    q[row, 0, 5] = float("nan")
+    o2, lse2 = b.forward_paged_tree(handle, q, cache, table, lens_t, mask)
+    ok(handle)
+    rest = ~hit
+    rest[row] = False
+    assert torch.isnan(o2[row, 0]).all() and torch.isnan(lse2[0, row]) and torch.equal(o2[rest], o0[rest])
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+def test_scores_of_few_rows(handle, e4m3):
+    """Scores in the hundreds, rising maxima, one key far above thousands, scales near zero: as above, in few rows."""
+    from paper_2609_21264_b200 import binding
+    run(handle, [1000, 77], [7, 6], 8, 2, 128, 128, 16, e4m3, seed=8, q_mult=8.0)
+    run(handle, [300, 90], [8, 3], 8, 2, 64, 64, 16, e4m3, seed=8, scale=1e-30)
+    k, v, table, lens_t, ks, vs = pool([2000], 32, 2, 128, 128, e4m3, False, 9, poison=False)
+    flat = torch.arange(2000, device="cuda")
+    ramp = (flat.float() / 2000 * 4 - 2)
+    kk = torch.zeros(k.shape, device="cuda")
+    kk[table[0, flat // 32].long(), :, flat % 32] = ramp[:, None, None].expand(2000, 2, 128)
+    k.copy_((kk * 20).to(k.dtype) if e4m3 else kk.to(k.dtype))
+    q = torch.ones(8, 8, 128, device="cuda").bfloat16()
+    q[:, ::2] *= -1
+    o, lse = binding.forward_paged_tree(handle, q, binding.PagedCache(k, v, ks, vs), table, lens_t, None)
+    ok(handle)
+    assert_attention(o, lse, *tree_reference(q, k, v, ks, vs, table, [2000], [0, 8], [torch.ones(8, 8).tril() > 0], 128 ** -0.5))
+    n = 16000
+    k, v, table, lens_t, ks, vs = pool([n], 64, 1, 128, 128, e4m3, False, 10, poison=False, shift=0.5)
+    kf = torch.zeros(k.shape, device="cuda")
+    kf[int(table[0, 3]), 0, 5, :] = 20.0 if e4m3 else 1.0
+    k.copy_(kf.to(k.dtype))
+    q = torch.full((6, 4, 128), 9.7 * 128 ** 0.5 / 128, device="cuda").bfloat16()
+    o, lse = binding.forward_paged_tree(handle, q, binding.PagedCache(k, v, ks, vs), table, lens_t, None)
+    ok(handle)
+    assert_attention(o, lse, *tree_reference(q, k, v, ks, vs, table, [n], [0, 6], [torch.ones(6, 6).tril() > 0], 128 ** -0.5))
+
+
+def test_strides_of_few_rows(handle):
+    from paper_2609_21264_b200 import binding as b
+    for dqk, dv, e4m3 in ((128, 128, False), (64, 64, True), (192, 128, False)):
+        k, v, table, lens_t, ks, vs = pool([300, 40], 16, 2, dqk, dv, e4m3, False, 13)
+        wide = torch.randn(2 * 5, 14, dqk, generator=torch.Generator().manual_seed(6)).to(torch.bfloat16).cuda()
+        q = wide[:, 2:10]
+        out = torch.full((10, 11, dv + 8), 7.0, dtype=torch.bfloat16, device="cuda")
+        cache = b.PagedCache(k, v, ks, vs)
+        mask = torch.full((10, 3), 9, dtype=torch.int32, device="cuda")[:, :2]
+        o, lse = b.forward_paged_tree(handle, q, cache, table, lens_t, mask, out=out[:, 3:, :dv])
+        o2, lse2 = b.forward_paged_tree(handle, q.contiguous(), cache, table, lens_t, mask.contiguous())
+        ok(handle)
+        assert torch.equal(o, o2) and torch.equal(lse, lse2)
+        assert (out[:, :3] == 7).all() and (out[:, :, dv:] == 7).all()
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+def test_few_rows_refuse_contents_and_give_up(e4m3):
+    """Lengths, offsets and pages that cannot be are reported and their sequences left out; a load that never comes ends the call."""
+    from paper_2609_21264_b200 import binding as b
+    k, v, table, lens_t, ks, vs = pool([300, 140], 16, 2, 128, 128, e4m3, False, 14)
+    q = torch.randn(12, 8, 128, generator=torch.Generator().manual_seed(7)).to(torch.bfloat16).cuda()
+    cache = b.PagedCache(k, v, ks, vs)
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    h = b.fa_create()
+    try:
+        good = b.forward_paged_tree(h, q, cache, table, lens_t, None, cu_seqlens=ints(0, 6, 12), max_tokens=8)[0]
+        ok(h)
+        for cu in (ints(0, 20, 12), ints(-1, 6, 12), ints(6, 3, 12)):
+            out = torch.full_like(q, 7.0)
+            b.forward_paged_tree(h, q, cache, table, lens_t, None, cu_seqlens=cu, max_tokens=8, out=out)
+            torch.cuda.synchronize()
+            assert b.fa_last_status(h) == (b.FA_ERR_INVALID_ARG, 0x0904)
+        for n in (-1, 10 ** 6):
+            o = b.forward_paged_tree(h, q, cache, table.clamp(0, k.shape[0] - 1), ints(n, 140), None, cu_seqlens=ints(0, 6, 12), max_tokens=8)[0]
+            torch.cuda.synchronize()
+            assert b.fa_last_status(h) == (b.FA_ERR_INVALID_ARG, 0x0901) and torch.equal(o[6:], good[6:])
+        bad = table.clone()
+        bad[0, 2] = k.shape[0]
+        o = b.forward_paged_tree(h, q, cache, bad, lens_t, None, cu_seqlens=ints(0, 6, 12), max_tokens=8)[0]
+        torch.cuda.synchronize()
+        assert b.fa_last_status(h) == (b.FA_ERR_INVALID_ARG, 0x0902) and torch.equal(o[6:], good[6:])
+    finally:
+        b.fa_destroy(h)
+    h = b.fa_create(flags=b.FA_FLAG_DEBUG_DROP_V_LOAD, wait_limit_ms=20)
+    try:
+        b.forward_paged_tree(h, q, cache, table, lens_t, None, cu_seqlens=ints(0, 6, 12), max_tokens=8)
+        torch.cuda.synchronize()
+        st, site = b.fa_last_status(h)
+        assert st == b.FA_ERR_DEVICE_TIMEOUT and site != 0 and b.fa_last_kernel_name(h).startswith("fa_tree_few")
+    finally:
+        b.fa_destroy(h)
