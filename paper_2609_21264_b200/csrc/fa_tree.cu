@@ -29,9 +29,9 @@ namespace {
 using namespace fa_host;
 
 // Few rows are columns of turned products, many are lanes: a pass over the keys costs the streaming kernel's softmax warps what the rows
-// are, and this one 128 rows whatever they are.  64 sequences of 300 keys, 64/8 heads of 128: 8 rows 17.8 us against 40.5, 32 rows 24.7
-// against 38.0, 64 rows 51.2 against 38.0; 48 of 4200 keys over e4m3 69.5 against 117.9, 78.1 against 126.2, 145.4 against 137.1.  (The
-// largest loss: one sequence of 8000 keys, 32/8 heads, 32 rows, 19.4 against 18.6.)
+// are, and this one 128 rows whatever they are.  64 sequences of 300 keys, 64/8 heads of 128: 8 rows 17.2 us against 40.5, 32 rows 24.3
+// against 38.0, 64 rows (forward_paged's time) 49.5 against 36.8; 48 of 4200 keys over e4m3 71.8 against 117.9, 79.8 against 126.2, 64 rows
+// 140 against 125.  (The largest loss: one sequence of 8000 keys, 32/8 heads, 32 rows, 20.0 against 18.6.)
 bool few_rows(int group, int max_tokens) { return static_cast<long long>(group) * max_tokens <= 32; }
 
 template <bool kE4m3>

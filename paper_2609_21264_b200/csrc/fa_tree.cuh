@@ -1,7 +1,7 @@
 // Attention of drafted tokens over a paged key/value cache, for sm_100a.
 //
-// A tree of n drafts gives R = n * (Hq / Hkv) query rows per (sequence, K/V head), a handful to some hundred, against thousands of keys that
-// all of them see and n that a mask of bits decides about.  2 R (dqk + dv) flops stand against (dqk + dv) * bytes a key: up to 256
+// A tree of n drafts gives R = n * (Hq / Hkv) query rows per (sequence, K/V head), more than 32 here (fewer are the work of fa_paged.cuh),
+// against thousands of keys that all of them see and n that a mask of bits decides about.  2 R (dqk + dv) flops stand against (dqk + dv) * bytes a key: up to 256
 // rows over a 16-bit cache HBM is the bound, behind that the tensor cores and, as in every kernel here, the exponentials.  So a CTA
 // takes up to 256 rows in one pass over the keys, as two tiles of 128 rows on the accumulator's lanes:
 //
@@ -21,8 +21,7 @@
 // What bounds it.  16 sequences of 129 to 8192 keys, trees of 16 to 64 drafts, 32/8 heads of 128, bf16: 67.6 us, where 248 MB take 38 at the
 // copy rate.  With 256 rows a tile of keys takes a CTA 3000 cycles, the chain softmax (2000) -> P V and next scores (1024 cycles of MMAs) of each
 // stream; 28 tiles a CTA.  Beside them: 9000 cycles from the launch to the first scores (list, block table, first loads), 6000 from
-// one block's last tile to the next one's first (result, barrier, first pass), 5 us for the join.  2 x 20000 keys of 192/128 heads, 31 drafts:
-// HBM, 91 % of the copy rate.  48 sequences of 300 to 8192 keys over e4m3, 13 drafts, 64/8 heads: 154 us, where 521 MB take 80: two tiles
+// one block's last tile to the next one's first (result, barrier, first pass), 5 us for the join.  48 sequences of 300 to 8192 keys over e4m3, 13 drafts, 64/8 heads: 152 us, where 521 MB take 80: two tiles
 // take 3600 cycles, of which MMAs 2630 (8-bit scores in three terms, fp16 products), and each CTA has four blocks.
 //
 // Over an e4m3 cache K is multiplied as it is (kind::f8f6f4), the queries as three e5m2 terms like in fa_paged.cuh, added up in one
@@ -88,7 +87,7 @@ struct TreeBatch { int blocks, units, longest, shortest, kinds; };
 constexpr int kTreeSplitCost = 3;
 // Small batches.  Where there is a CTA for every block, the longest block, unsplit, is what the call takes; split, it takes an equal share and
 // what the join of the pieces costs, about three tiles' time.  Where that is not less, all blocks count the same and nothing is split (16
-// sequences of 1003 keys, 8 K/V heads, 8 drafts: 18.3 us, against 21.0 split; one of 500 keys, 26 drafts: 12.2 split, against 13.7).  Where
+// sequences of 1003 keys, 8 K/V heads, 32 rows: 18.3 us, against 21.0 split; one of 500 keys, 26 drafts: 12.2 split, against 13.7).  Where
 // there are two CTAs for every block at least and all are equally long, their pieces are equally long too, and a CTA has one.
 // Returns the share (0: what the total gives).
 __host__ __device__ inline int tree_rules(TreeList& li, const TreeBatch& b, int ctas) {
