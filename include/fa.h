@@ -626,7 +626,7 @@ fa_status fa_tree_layout(fa_handle* h, const int32_t* parents, const int32_t* cu
  * lse = -inf.  Q [total, Hq, dqk], O [total, Hq, dv], lse [Hq, total] and everything else as for fa_forward_paged; the values (V) of the
  * drafts have to be finite, their keys where no token sees them need not be.  A key that is no number makes the rows that see it NaN.
  * Up to 32 rows, max_tokens * (Hq / Hkv), are the work of fa_forward_paged's kernel with its precision, its single launch, its needs of
- * scratch and its limits (a causal chain of equally many drafts gives the bits that it gives).  With more:
+ * scratch and its limits.  With more:
  * Scores, softmax state and accumulators are fp32.  Over a bf16 cache the probabilities enter the second product as bf16, over an e4m3
  * cache as fp16 (11 significant bits down to 2^-21 of the row's reference), and the queries as a sum of three 8-bit terms (exact for
  * entries of 2^-23 of their row's largest and more, to 2^-30 of it below).
@@ -654,8 +654,8 @@ fa_status fa_forward_paged_tree(fa_handle* h, const fa_paged_cache* cache, const
  * tree->cu_seqlens are HOST arrays here (no other pointer is looked at).  out->rows_per_block is a row tile's rows (tokens times heads of the
  * group, 128 at most), out->row_blocks the row tiles of a sequence of max_tokens, part_cost the units that a row block counts beside its
  * tiles of 128 keys.  A piece's row_block is the first row tile of its block (blocks have two where a head size has room for them and the
- * sequence has them); slot 2 * cta + 1 holds the first piece of a block, 2 * cta any other.  Up to 32 rows: the plan of fa_plan_paged for
- * one block of 16 or 32 rows, in which a sequence without drafts counts as one without keys.
+ * sequence has them); slot 2 * cta + 1 holds the first piece of a block, 2 * cta any other.  Up to 32 rows: as fa_plan_paged, one
+ * block of 16 or 32 rows, in fewer pieces where a sequence is long; a sequence without drafts counts as one without keys.
  */
 fa_status fa_plan_paged_tree(int num_sms, const fa_config* cfg, const fa_paged_cache* cache, const fa_paged_seqs* seqs, const fa_tree* tree,
                              int total, int Hq, fa_paged_plan_info* out, fa_paged_piece* pieces, int max_pieces);

@@ -331,7 +331,7 @@ fa_status fa_plan_paged(int num_sms, const fa_config* cfg, const fa_paged_cache*
     memset(&p, 0, sizeof p);
     p.seq_lens = seqs->seq_lens;
     p.B = seqs->B; p.max_pages = seqs->max_pages; p.page_size = cache->page_size; p.Hkv = cache->Hkv; p.Hq = Hq; p.Sq = Sq;
-    return plan_paged(num_sms, static_cast<size_t>(scratch), p, cache->dqk, cache->dv, cache->type == FA_CACHE_E4M3, diff != 0, out, pieces, max_pieces);
+    return plan_paged(num_sms, static_cast<size_t>(scratch), p, cache->dqk, cache->dv, cache->type == FA_CACHE_E4M3, diff != 0, false, out, pieces, max_pieces);
 }
 
 }  // extern "C"

@@ -129,7 +129,15 @@ __host__ __device__ inline int paged_len(const PagedParams& p, int b, uint32_t* 
 // How a call's units are counted: tiles that every row block has at least (0: its own), units beside them, a CTA's share (0: what
 // the total gives).
 struct PagedCount { int pad, cost, share; };
-__host__ __device__ inline PagedCount paged_count(const PagedParams& p, int ctas, int most_tiles, int all_tiles) {
+// Units that a CTA takes at least.  Drafted tokens: a long sequence in few row blocks has a CTA's tiles (0.6 us each) on one side and its
+// pieces, which one CTA joins (some 0.4 us each), on the other; tiles / s + s is least where s is their root.  One K/V head, 32 rows, one
+// sequence of 17353 keys: 29.7 us in pieces of two tiles, 17.7 in 14 pieces; 2 of 100000 57 in 74 pieces each, 43 in 34; 8 heads, 8000 keys
+// 20.0 in 18 pieces, 18.1 in 9.  (Other calls keep the shares, and so the bits, that they have.)
+__host__ __device__ inline int paged_least(const PagedParams& p, bool tree, int most_tiles) {
+    const int root = tree ? static_cast<int>(ceilf(sqrtf(static_cast<float>(most_tiles) * (2.f / 3.f)))) : 0;
+    return root > p.least_units ? root : p.least_units;
+}
+__host__ __device__ inline PagedCount paged_count(const PagedParams& p, int least, int ctas, int most_tiles, int all_tiles) {
     const long long blocks = static_cast<long long>(p.B) * p.Hkv * p.row_blocks;
     PagedCount c{0, 0, 0};
     if (most_tiles <= kWholeTiles && blocks <= ctas) {
@@ -137,7 +145,7 @@ __host__ __device__ inline PagedCount paged_count(const PagedParams& p, int ctas
     } else if (p.B == 1 && 2 * blocks <= ctas) {
         // (a block has less than one share more than its tiles fill: the shares do not outnumber the CTAs)
         const int spare = ctas - static_cast<int>(blocks), per = (all_tiles + spare - 1) / spare;
-        c.share = per < p.least_units ? p.least_units : per;
+        c.share = per < least ? least : per;
         c.pad = (most_tiles + c.share - 1) / c.share * c.share;
     } else if (blocks >= ctas && all_tiles < p.long_tiles * blocks) {
         c.cost = p.part_cost;
@@ -150,10 +158,10 @@ __host__ __device__ inline int paged_block_units(int len, PagedCount c) {
     return (nt < c.pad ? c.pad : nt) + c.cost;
 }
 __host__ __device__ inline int paged_units(const PagedParams& p, int len, PagedCount c) { return paged_block_units(len, c) * p.Hkv * p.row_blocks; }
-__host__ __device__ inline int paged_share(const PagedParams& p, int units, int ctas, PagedCount c) {
+__host__ __device__ inline int paged_share(int least, int units, int ctas, PagedCount c) {
     if (c.share > 0) return c.share;
     const int per = static_cast<int>((static_cast<unsigned>(units) + ctas - 1) / ctas);
-    return per < p.least_units ? p.least_units : per;
+    return per < least ? least : per;
 }
 
 // A part of the list as the roles of a CTA see it: tiles [t0, t1) of one (sequence, K/V head, row block).
@@ -857,7 +865,8 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             total += n;
         }
         longest = max(max(sh.warp_longest[0], sh.warp_longest[1]), max(sh.warp_longest[2], sh.warp_longest[3]));
-        const PagedCount cnt = paged_count(p, gridDim.x, paged_tiles(longest), total);
+        const int least = paged_least(p, kTree, paged_tiles(longest));
+        const PagedCount cnt = paged_count(p, least, gridDim.x, paged_tiles(longest), total);
         const int b_mine = max(0, b_last - b_first), b_before = min(b_first, p.B);
         if (cnt.pad > 0) {           // all sequences count the same
             const int units = paged_units(p, longest, cnt);
@@ -870,7 +879,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
             mine += more * b_mine;
             before += more * b_before;
         }
-        const int share = paged_share(p, total, gridDim.x, cnt);
+        const int share = paged_share(least, total, gridDim.x, cnt);
         const int u0 = min(total, static_cast<int>(blockIdx.x) * share), u1 = min(total, u0 + share);
         if (before <= u0 && u0 < before + mine) {
             int b = b_first, base = before;

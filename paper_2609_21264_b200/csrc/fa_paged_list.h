@@ -64,8 +64,8 @@ fa_status launch_paged(fa_handle* h, const CUtensorMap& mk, const CUtensorMap& m
 }
 
 // How a batch is dealt out (p: its lengths on the host, B, max_pages, page_size, Hq, Hkv, Sq).
-inline fa_status plan_paged(int num_sms, size_t scratch, fa::PagedParams& p, int dqk, int dv, bool e4m3, bool diff, fa_paged_plan_info* out,
-                            fa_paged_piece* pieces, int max_pieces) {
+inline fa_status plan_paged(int num_sms, size_t scratch, fa::PagedParams& p, int dqk, int dv, bool e4m3, bool diff, bool tree,
+                            fa_paged_plan_info* out, fa_paged_piece* pieces, int max_pieces) {
     const int rows = p.Hq / p.Hkv * p.Sq, block = rows_per_block(rows, dqk, e4m3, diff);
     p.row_blocks = (rows + block - 1) / block;
     set_list(p, dqk, dv, e4m3);
@@ -78,11 +78,12 @@ inline fa_status plan_paged(int num_sms, size_t scratch, fa::PagedParams& p, int
         longest = n > longest ? n : longest;
         total += fa::paged_units(p, n, fa::PagedCount{0, 0, 0});
     }
-    const fa::PagedCount cnt = fa::paged_count(p, ctas, fa::paged_tiles(longest), total);
+    const int least = fa::paged_least(p, tree, fa::paged_tiles(longest));
+    const fa::PagedCount cnt = fa::paged_count(p, least, ctas, fa::paged_tiles(longest), total);
     auto units_of = [&](int b) { return fa::paged_units(p, fa::paged_len(p, b, nullptr), cnt); };
     total = 0;
     for (int b = 0; b < p.B; ++b) total += units_of(b);
-    const int share = fa::paged_share(p, total, ctas, cnt);
+    const int share = fa::paged_share(least, total, ctas, cnt);
     out->rows_per_block = block;
     out->row_blocks = p.row_blocks;
     out->ctas = ctas;

@@ -26,7 +26,7 @@ fa_status launch_tree_few(fa_handle* h, int dqk, int dv, bool e4m3, const CUtens
 
 fa_status plan_tree_few(int num_sms, size_t scratch, fa::PagedParams& p, int dqk, int dv, bool e4m3, fa_paged_plan_info* out, fa_paged_piece* pieces,
                         int max_pieces) {
-    return plan_paged(num_sms, scratch, p, dqk, dv, e4m3, false, out, pieces, max_pieces);
+    return plan_paged(num_sms, scratch, p, dqk, dv, e4m3, false, true, out, pieces, max_pieces);
 }
 
 }  // namespace fa_host
