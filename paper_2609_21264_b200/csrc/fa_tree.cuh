@@ -85,11 +85,15 @@ __host__ __device__ inline int tree_head_units(const TreeUnits& u) { return u.pa
 // two row tiles are among it.
 struct TreeBatch { int blocks, units, longest, shortest, kinds; };
 constexpr int kTreeSplitCost = 3;
+// Tiles of a piece at least: a tile takes its CTA about four times what a piece takes the joining kernel, so tiles / s + s / 4 is least where a
+// piece has s = half the root of the tiles (one sequence of 17353 keys, one K/V head, 64 drafts of 8 heads: 53.3 us in pieces as small as the
+// CTAs allow, 30.3 so; 100000 and 33333 keys, 13 drafts 66.7, 47.9).
+__host__ __device__ inline int tree_root(int tiles) { return static_cast<int>(ceilf(0.5f * sqrtf(static_cast<float>(tiles)))); }
 // Small batches.  Where there is a CTA for every block, the longest block, unsplit, is what the call takes; split, it takes an equal share and
 // what the join of the pieces costs, about three tiles' time.  Where that is not less, all blocks count the same and nothing is split (16
 // sequences of 1003 keys, 8 K/V heads, 32 rows: 18.3 us, against 21.0 split; one of 500 keys, 26 drafts: 12.2 split, against 13.7).  Where
-// there are two CTAs for every block at least and all are equally long, their pieces are equally long too, and a CTA has one.
-// Returns the share (0: what the total gives).
+// there are two CTAs for every block at least and all are equally long, their pieces are equally long too, and a CTA has one.  No share
+// is smaller than a piece of the longest sequence should be (tree_root).  Returns the share (0: what the total gives).
 __host__ __device__ inline int tree_rules(TreeList& li, const TreeBatch& b, int ctas) {
     const int w = b.kinds & 1 ? li.w2 : li.w1;
     if (b.blocks <= ctas && li.cost + w * (b.longest - kTreeSplitCost) <= b.units / ctas) {
@@ -101,10 +105,11 @@ __host__ __device__ inline int tree_rules(TreeList& li, const TreeBatch& b, int 
         const int pieces = ctas / b.blocks, per = (b.longest + pieces - 1) / pieces;
         li.cost = 0;
         li.w1 = li.w2 = 1;
-        const int share = per < 2 ? 2 : per;
+        const int root = tree_root(b.longest), least = root < 2 ? 2 : root, share = per < least ? least : per;
         li.pad = (b.longest + share - 1) / share * share;
         return share;
     }
+    if (w * tree_root(b.longest) > li.least) li.least = w * tree_root(b.longest);
     return 0;
 }
 __host__ __device__ inline int tree_share(const TreeList& li, int total, int ctas) {
