@@ -21,7 +21,7 @@
 // What bounds it.  16 sequences of 129 to 8192 keys, trees of 16 to 64 drafts, 32/8 heads of 128, bf16: 67.6 us, where 248 MB take 38 at the
 // copy rate.  With 256 rows a tile of keys takes a CTA 3000 cycles, the chain softmax (2000) -> P V and next scores (1024 cycles of MMAs) of each
 // stream; 28 tiles a CTA.  Beside them: 9000 cycles from the launch to the first scores (list, block table, first loads), 6000 from
-// one block's last tile to the next one's first (result, barrier, first pass), 5 us for the join.  48 sequences of 300 to 8192 keys over e4m3, 13 drafts, 64/8 heads: 152 us, where 521 MB take 80: two tiles
+// one block's last tile to the next one's first (result, barrier, first pass), 5 us for the join.  48 sequences of 300 to 8192 keys over e4m3, 13 drafts, 64/8 heads: 148 us, where 521 MB take 80: two tiles
 // take 3600 cycles, of which MMAs 2630 (8-bit scores in three terms, fp16 products), and each CTA has four blocks.
 //
 // Over an e4m3 cache K is multiplied as it is (kind::f8f6f4), the queries as three e5m2 terms like in fa_paged.cuh, added up in one
