@@ -35,6 +35,7 @@
 #pragma once
 
 #include <cuda_fp16.h>
+#include <float.h>
 #include <math.h>
 
 #include "fa_common.cuh"
@@ -721,6 +722,9 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 if constexpr (kE4m3) {
                     if (j == 0) {
                         c *= __uint_as_float(static_cast<uint32_t>(sh.q_shift[(n_q - 1) & 1][row]) << 23);
+                        // (hidden scores are -inf already, and -inf times a factor that has become 0 is no number; scores, 2^32 at most,
+                        // times the smallest normal number are nothing all the same)
+                        if (live && c < FLT_MIN) c = FLT_MIN;
                         tau_raw = kRescaleThresholdLog2 / c;
                     }
                 }
