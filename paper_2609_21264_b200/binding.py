@@ -811,12 +811,12 @@ def forward_paged_tree(h, q, cache: PagedCache, block_table, seq_lens, mask, *, 
     return r
 
 
-def compact_paged(h, caches, block_table, seq_lens, keep, keep_counts, *, cu_seqlens=None, total: int = 0, new_lens=None):
+def compact_paged(h, caches, block_table, seq_lens, keep, keep_counts, *, cu_seqlens=None, total: int = None, new_lens=None):
     """The accepted drafts of every sequence move up to its first drafts' slots, in one or several caches (PagedCache, PagedCaches).
 
-    seq_lens [B] int32 counts the drafts in; cu_seqlens [B+1] int32 as for forward_paged_tree (None: total / B drafts each).  keep
-    [B, most] int32 holds the accepted drafts' numbers in rising order, keep_counts [B] int32 how many.  Returns the new lengths [B]
-    int32 (a new tensor where none is given; none of the inputs).
+    seq_lens [B] int32 counts the drafts in; cu_seqlens [B+1] int32 as for forward_paged_tree (None: total / B drafts each, and total
+    has to be given: nothing else says how many there are).  keep [B, most] int32 holds the accepted drafts' numbers in rising
+    order, keep_counts [B] int32 how many.  Returns the new lengths [B] int32 (a new tensor where none is given; none of the inputs).
     """
     r = (_calls or _native()).compact(h, caches.address, caches.count, caches.index, block_table, seq_lens, keep, keep_counts, cu_seqlens, total,
                                       new_lens)

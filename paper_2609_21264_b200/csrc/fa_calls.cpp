@@ -50,6 +50,8 @@ struct Args {
         if (!p && PyErr_Occurred()) throw Refused{};
         return p;
     }
+    // whether the next argument is another one than None
+    bool given() const { return at < n && a[at] != Py_None; }
     int64_t number() {
         const long long x = PyLong_AsLongLong(next());
         if (x == -1 && PyErr_Occurred()) throw Refused{};
@@ -281,15 +283,17 @@ PyObject* paged_tree(Args& a) {
     return s == FA_OK ? both(std::move(out), std::move(lse)) : status(s);
 }
 
-// (handle, address of the caches, their number, device, block_table, seq_lens, keep, keep_counts, cu_seqlens, total, new_lens) -> new_lens
+// (handle, address of the caches, their number, device, block_table, seq_lens, keep, keep_counts, cu_seqlens, total or None, new_lens) -> new_lens
 PyObject* compact(Args& a) {
     auto* h = static_cast<fa_handle*>(a.address());
     auto* caches = static_cast<const fa_paged_cache*>(a.address());
     const int count = a.integer("caches"), device = a.integer("device");
     const at::Tensor &table = a.tensor(), &lens = a.tensor(), &keep = a.tensor(), &kept = a.tensor();
     const at::Tensor* cu = a.maybe();
-    const int total = a.integer("total is out of range");
+    const bool has_total = a.given();
+    const int total = has_total ? a.integer("total is out of range") : (a.next(), 0);
     const at::Tensor* new_in = a.maybe();
+    if (!cu && !has_total && table.dim() > 0 && table.size(0) > 0) refuse("total, the number of drafts of all sequences, is needed without cu_seqlens");
     const fa_paged_seqs seqs = sequences(h, table, lens, device);
     if (keep.scalar_type() != at::kInt || keep.dim() != 2 || !on(keep, device) || keep.size(0) != seqs.B || keep.size(1) < 1 || keep.size(1) > INT32_MAX ||
         (keep.size(1) > 1 && keep.stride(1) != 1) || (seqs.B > 1 && keep.stride(0) < keep.size(1)))
