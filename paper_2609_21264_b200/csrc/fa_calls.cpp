@@ -3,7 +3,8 @@
 // host time beside the launches' 3.5 each (tree_layout 11.0 us), here a fraction of one.
 //
 // Every function returns its results, or the entry's status code as an int where that is not FA_OK, and raises ValueError for arguments
-// that no entry should see.  The C entries are bound by address: the library is the one that binding.py has loaded.
+// that no entry should see.  The C entries are bound by address: the library is the one that binding.py has loaded.  What can wait for the
+// device, a launch into a full queue or memory that the allocator has to get, runs without the interpreter's lock.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -149,6 +150,20 @@ Rows rows(const at::Tensor& t, int64_t d, int device, const char* why) {
     return r;
 }
 
+// f() with the interpreter's lock given back meanwhile: it touches no Python object.
+template <typename F>
+auto unlocked(F&& f) {
+    struct Lock {
+        PyThreadState* state = PyEval_SaveThread();
+        ~Lock() { PyEval_RestoreThread(state); }
+    } lock;
+    return f();
+}
+
+at::Tensor fresh(at::IntArrayRef sizes, const at::TensorOptions& options) {
+    return unlocked([&] { return at::empty(sizes, options); });
+}
+
 void* stream_of(int device) { return c10::cuda::getCurrentCUDAStream(static_cast<c10::DeviceIndex>(device)).stream(); }
 
 PyObject* status(fa_status s) { return PyLong_FromLong(s); }
@@ -191,9 +206,11 @@ PyObject* tree_layout(Args& a) {
     const int64_t words = (static_cast<int64_t>(most) + 31) / 32;
     if (mask_in) check_mask(*mask_in, total, words, device);
     if (pos_in && !vector_ok(*pos_in, total, device)) refuse("positions must be a contiguous int32 tensor of one number per token");
-    at::Tensor mask = mask_in ? *mask_in : at::empty({total, words}, parents.options()), pos = pos_in ? *pos_in : at::empty({total}, parents.options());
-    const fa_status s = p_layout(h, ints(&parents), cu_ptr, static_cast<int>(total), static_cast<int>(B), ints(&lens), most,
-                                 reinterpret_cast<uint32_t*>(mask.data_ptr()), total > 1 ? mask.stride(0) : words, ints(&pos), stream_of(device));
+    at::Tensor mask = mask_in ? *mask_in : fresh({total, words}, parents.options()), pos = pos_in ? *pos_in : fresh({total}, parents.options());
+    const fa_status s = unlocked([&] {
+        return p_layout(h, ints(&parents), cu_ptr, static_cast<int>(total), static_cast<int>(B), ints(&lens), most,
+                        reinterpret_cast<uint32_t*>(mask.data_ptr()), total > 1 ? mask.stride(0) : words, ints(&pos), stream_of(device));
+    });
     return s == FA_OK ? both(std::move(mask), std::move(pos)) : status(s);
 }
 
@@ -227,7 +244,7 @@ PyObject* append_at(Args& a) {
         const char* why = "q must be a 3-D bf16 tensor of the cache's head size on its device, contiguous along a head";
         qr = rows(*q, dqk, device, why);
         if (qr.n != kr.n) refuse("q must have the tokens of k");
-        out = q_out ? *q_out : at::empty({qr.n, qr.heads, dqk}, q->options());
+        out = q_out ? *q_out : fresh({qr.n, qr.heads, dqk}, q->options());
         or_ = rows(out, dqk, device, "q_out must be a 3-D bf16 tensor like q");
         if (or_.n != qr.n || or_.heads != qr.heads) refuse("q_out must have q's shape");
     } else if (q_out) {
@@ -239,9 +256,11 @@ PyObject* append_at(Args& a) {
     p.pos = ints(&pos);
     p.stride = axes > 1 ? pos.stride(0) : kr.n;
     p.axis_of_pair = axis_of_pair;
-    const fa_status s = p_append(h, cache, &seqs, cu_ptr, static_cast<int>(kr.n), k.data_ptr(), v.data_ptr(), q ? q->data_ptr() : nullptr,
-                                 q ? out.data_ptr() : nullptr, static_cast<int>(qr.heads), kr.strides, vr.strides, qr.strides, or_.strides, rope, &p,
-                                 stream_of(device));
+    const fa_status s = unlocked([&] {
+        return p_append(h, cache, &seqs, cu_ptr, static_cast<int>(kr.n), k.data_ptr(), v.data_ptr(), q ? q->data_ptr() : nullptr,
+                        q ? out.data_ptr() : nullptr, static_cast<int>(qr.heads), kr.strides, vr.strides, qr.strides, or_.strides, rope, &p,
+                        stream_of(device));
+    });
     if (s != FA_OK) return status(s);
     return q ? THPVariable_Wrap(std::move(out)) : Py_NewRef(Py_None);
 }
@@ -272,14 +291,15 @@ PyObject* paged_tree(Args& a) {
         tree.mask = reinterpret_cast<const uint32_t*>(mask->data_ptr());
         tree.mask_stride = qr.n > 1 ? mask->stride(0) : words;
     }
-    at::Tensor out = out_in ? *out_in : at::empty({qr.n, qr.heads, dv}, q.options());
+    at::Tensor out = out_in ? *out_in : fresh({qr.n, qr.heads, dv}, q.options());
     const Rows or_ = rows(out, dv, device, "out must be a bf16 tensor of shape [tokens, heads, dv] on the cache's device, contiguous along a head");
     if (or_.n != qr.n || or_.heads != qr.heads) refuse("out must have shape [tokens, heads, dv]");
     at::Tensor lse;
-    if (want_lse) lse = at::empty({qr.heads, qr.n}, q.options().dtype(at::kFloat));
-    const fa_status s = p_tree(h, cache, &seqs, &tree, static_cast<int>(qr.n), q.data_ptr(), out.data_ptr(),
-                               want_lse ? static_cast<float*>(lse.data_ptr()) : nullptr, static_cast<int>(qr.heads), static_cast<float>(scale), qr.strides,
-                               or_.strides, stream_of(device));
+    if (want_lse) lse = fresh({qr.heads, qr.n}, q.options().dtype(at::kFloat));
+    const fa_status s = unlocked([&] {
+        return p_tree(h, cache, &seqs, &tree, static_cast<int>(qr.n), q.data_ptr(), out.data_ptr(), want_lse ? static_cast<float*>(lse.data_ptr()) : nullptr,
+                      static_cast<int>(qr.heads), static_cast<float>(scale), qr.strides, or_.strides, stream_of(device));
+    });
     return s == FA_OK ? both(std::move(out), std::move(lse)) : status(s);
 }
 
@@ -302,9 +322,11 @@ PyObject* compact(Args& a) {
     if (new_in && (!vector_ok(*new_in, seqs.B, device) || (seqs.B && new_in->data_ptr() == lens.data_ptr())))
         refuse("new_lens must be a contiguous int32 tensor of B numbers, another one than seq_lens");
     const int32_t* cu_ptr = offsets(cu, seqs.B, device);
-    at::Tensor out = new_in ? *new_in : at::empty({seqs.B}, lens.options());
-    const fa_status s = p_compact(h, caches, count, &seqs, cu_ptr, cu ? INT32_MAX : total, ints(&keep), seqs.B > 1 ? keep.stride(0) : keep.size(1),
-                                  ints(&kept), static_cast<int>(keep.size(1)), ints(&out), stream_of(device));
+    at::Tensor out = new_in ? *new_in : fresh({seqs.B}, lens.options());
+    const fa_status s = unlocked([&] {
+        return p_compact(h, caches, count, &seqs, cu_ptr, cu ? INT32_MAX : total, ints(&keep), seqs.B > 1 ? keep.stride(0) : keep.size(1), ints(&kept),
+                         static_cast<int>(keep.size(1)), ints(&out), stream_of(device));
+    });
     return s == FA_OK ? THPVariable_Wrap(std::move(out)) : status(s);
 }
 
@@ -319,7 +341,7 @@ PyObject* copy_pages(Args& a) {
     if (n < 0 || n > INT32_MAX || !vector_ok(src, n, device) || !vector_ok(dst, n, device) || (slots && !vector_ok(*slots, n, device)))
         refuse("src, dst and slots must be contiguous 1-D int32 tensors of one length on the caches' device");
     if (p_device(h) != device) refuse("the handle belongs to another device than the caches");
-    const fa_status s = p_copy(h, caches, count, ints(&src), ints(&dst), ints(slots), static_cast<int>(n), stream_of(device));
+    const fa_status s = unlocked([&] { return p_copy(h, caches, count, ints(&src), ints(&dst), ints(slots), static_cast<int>(n), stream_of(device)); });
     return s == FA_OK ? Py_NewRef(Py_None) : status(s);
 }
 
