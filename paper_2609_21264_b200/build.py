@@ -1,9 +1,12 @@
-"""Builds the CUDA library in-tree with nvcc for sm_100a (no JIT cache, no torch extension)."""
+"""Builds in-tree: the CUDA library with nvcc for sm_100a, which is all that the C ABI needs, and then, where torch is installed, the
+extension module of the Python calls on drafted tokens with the C++ compiler (no JIT cache)."""
 from __future__ import annotations
 
 import os
 import shutil
 import subprocess
+import sysconfig
+import warnings
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
@@ -35,10 +38,19 @@ def is_stale() -> bool:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile csrc/*.cu into libfa_b200.so next to this file (and the Python calls of csrc/fa_calls.cpp); returns its path."""
-    build_calls(force)
-    if not force and not is_stale():
-        return LIB_PATH
+    """Compile csrc/*.cu into libfa_b200.so next to this file, and with torch the Python calls of csrc/fa_calls.cpp; returns the library's path."""
+    if force or is_stale():
+        _build_library(verbose)
+    try:
+        import torch  # noqa: F401
+    except ImportError as e:
+        warnings.warn("torch cannot be imported (%s): the extension module of the Python calls on drafted tokens is not built" % e)
+    else:
+        build_calls(force)
+    return LIB_PATH
+
+
+def _build_library(verbose: bool) -> None:
     tmp = LIB_PATH + ".tmp.%d" % os.getpid()
     extra = os.environ.get("FA_EXTRA_NVCC_FLAGS", "").split()
     cmd = [_nvcc(), *NVCC_FLAGS, *extra, "-o", tmp, *[os.path.join(CSRC, s) for s in SOURCES]]
@@ -48,17 +60,15 @@ def build(force: bool = False, verbose: bool = False) -> str:
     os.replace(tmp, LIB_PATH)
     if verbose:
         print(res.stdout + res.stderr)
-    return LIB_PATH
 
 
 def build_calls(force: bool = False) -> str:
-    """Compile csrc/fa_calls.cpp into the extension module _fa_calls.so next to this file; returns its path."""
+    """Compile csrc/fa_calls.cpp into the extension module _fa_calls.so next to this file, where its sources are newer; returns its
+    path."""
+    import torch
     sources = max(os.path.getmtime(os.path.join(CSRC, "fa_calls.cpp")), os.path.getmtime(os.path.join(os.path.dirname(_HERE), "include", "fa.h")))
     if not force and os.path.exists(CALLS_PATH) and os.path.getmtime(CALLS_PATH) >= sources:
         return CALLS_PATH
-    import sysconfig
-
-    import torch
     root = os.path.dirname(torch.__file__)
     tmp = CALLS_PATH + ".tmp.%d" % os.getpid()
     cuda = os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include")
@@ -67,6 +77,8 @@ def build_calls(force: bool = False) -> str:
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI),
            *["-I" + i for i in includes], "-o", tmp, os.path.join(CSRC, "fa_calls.cpp"), "-L" + os.path.join(root, "lib"),
            "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+    if not shutil.which(cmd[0]):
+        raise RuntimeError("%s not found" % cmd[0])
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError("%s failed:\n" % cmd[0] + res.stdout + res.stderr)
