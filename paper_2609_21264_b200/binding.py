@@ -203,6 +203,9 @@ def _native():
     lib = load()
     if not os.path.exists(_build.CALLS_PATH):
         raise ImportError("extension module %s is missing; run `python -m paper_2609_21264_b200.build`" % _build.CALLS_PATH)
+    other = _build.calls_mismatch()
+    if other:
+        raise ImportError("extension module %s was built for %s; run `python -m paper_2609_21264_b200.build`" % (_build.CALLS_PATH, other))
     from . import _fa_calls
     _fa_calls.bind(*[ctypes.cast(f, ctypes.c_void_p).value for f in (lib.fa_device, lib.fa_tree_layout, lib.fa_append_paged_at,
                                                                      lib.fa_forward_paged_tree, lib.fa_compact_paged, lib.fa_copy_pages)])

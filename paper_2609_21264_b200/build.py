@@ -12,6 +12,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libfa_b200.so")
 CALLS_PATH = os.path.join(_HERE, "_fa_calls.so")
+CALLS_BUILT_FOR = os.path.join(_HERE, "_fa_calls.built")        # the Python and torch that the module was compiled against
 SOURCES = ("fa_api.cu", "fa_noalloc.cu", "fa_paged.cu", "fa_drafts.cu", "fa_tree.cu", "fa_tree_few.cu")
 NVCC_FLAGS = ("-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-shared", "-Xcompiler", "-fPIC", "-Xptxas", "-v", "--threads", "0")
@@ -62,12 +63,32 @@ def _build_library(verbose: bool) -> None:
         print(res.stdout + res.stderr)
 
 
+def _built_for() -> str:
+    try:
+        with open(CALLS_BUILT_FOR) as f:
+            return f.read()
+    except OSError:
+        return ""
+
+
+def _running() -> str:
+    """The Python and torch of this process, whose ABIs the extension module is linked against."""
+    import torch
+    return "%s, torch %s" % (sysconfig.get_config_var("SOABI"), torch.__version__)
+
+
+def calls_mismatch() -> str:
+    """What the extension module was built for, where that is not what runs; else an empty string (also where nothing says)."""
+    built = _built_for()
+    return built if built != _running() else ""
+
+
 def build_calls(force: bool = False) -> str:
-    """Compile csrc/fa_calls.cpp into the extension module _fa_calls.so next to this file, where its sources are newer; returns its
-    path."""
+    """Compile csrc/fa_calls.cpp into the extension module _fa_calls.so next to this file, where its sources are newer or it was built for
+    another Python or torch; returns its path."""
     import torch
     sources = max(os.path.getmtime(os.path.join(CSRC, "fa_calls.cpp")), os.path.getmtime(os.path.join(os.path.dirname(_HERE), "include", "fa.h")))
-    if not force and os.path.exists(CALLS_PATH) and os.path.getmtime(CALLS_PATH) >= sources:
+    if not force and os.path.exists(CALLS_PATH) and os.path.getmtime(CALLS_PATH) >= sources and _built_for() == _running():
         return CALLS_PATH
     root = os.path.dirname(torch.__file__)
     tmp = CALLS_PATH + ".tmp.%d" % os.getpid()
@@ -82,7 +103,11 @@ def build_calls(force: bool = False) -> str:
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError("%s failed:\n" % cmd[0] + res.stdout + res.stderr)
+    if os.path.exists(CALLS_BUILT_FOR):
+        os.remove(CALLS_BUILT_FOR)              # (never a note beside another module than its own)
     os.replace(tmp, CALLS_PATH)
+    with open(CALLS_BUILT_FOR, "w") as f:
+        f.write(_running())
     return CALLS_PATH
 
 

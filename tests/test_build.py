@@ -5,7 +5,7 @@ import sys
 
 import pytest
 
-from paper_2609_21264_b200 import build
+from paper_2609_21264_b200 import binding, build
 
 
 def script(path, text):
@@ -23,7 +23,7 @@ def files(tmp_path, monkeypatch):
     """The library, the extension module and the log of what was compiled."""
     log = tmp_path / "log"
     log.write_text("")
-    for name, file in (("LIB_PATH", "lib.so"), ("CALLS_PATH", "calls.so")):
+    for name, file in (("LIB_PATH", "lib.so"), ("CALLS_PATH", "calls.so"), ("CALLS_BUILT_FOR", "calls.built")):
         monkeypatch.setattr(build, name, str(tmp_path / file))
     nvcc = script(tmp_path / "nvcc", WRITES % ("library", log))
     monkeypatch.setattr(build, "_nvcc", lambda: nvcc)
@@ -59,3 +59,31 @@ def test_the_library_is_there_where_the_module_cannot_be_built(files, monkeypatc
             build.build(force=True)
         assert lib.exists() and not calls.exists()
     assert log() == ["library"] * 2
+
+
+def test_the_module_is_built_again_for_another_torch_or_python(files, monkeypatch):
+    import torch
+    lib, calls, log = files
+    build.build()
+    with monkeypatch.context() as m:
+        m.setattr(torch, "__version__", "0.0.1")
+        assert build.calls_mismatch()
+        build.build()
+        assert log() == ["library", "calls", "calls"] and not build.calls_mismatch()
+    soabi = build.sysconfig.get_config_var
+    with monkeypatch.context() as m:
+        m.setattr(build.sysconfig, "get_config_var", lambda name: "cpython-1" if name == "SOABI" else soabi(name))
+        build.build()
+        assert log() == ["library"] + ["calls"] * 3
+    assert "cpython-1" in build.calls_mismatch()
+    build.build()
+    assert log() == ["library"] + ["calls"] * 4 and build.calls_mismatch() == ""
+
+
+def test_a_module_of_another_torch_is_not_loaded(files, monkeypatch):
+    build.build()
+    monkeypatch.setattr(binding, "load", lambda: None)         # (the stand-in is no library)
+    with open(build.CALLS_BUILT_FOR, "w") as f:
+        f.write("cpython-1, torch 0.0.1")
+    with pytest.raises(ImportError, match="torch 0.0.1.*paper_2609_21264_b200.build"):
+        binding._native()
