@@ -634,8 +634,9 @@ fa_status fa_tree_layout(fa_handle* h, const int32_t* parents, const int32_t* cu
  * share, in a fixed order, so equal calls give equal bits.  The partial results use the handle's scratch buffer, under the rule of
  * fa_forward: launches through one handle must not overlap on the device.  With less scratch than two partials per SM (130 KB each, 65 KB
  * at 192/128 and over e4m3 caches, half of that at head size 64) fewer SMs are used; with less than two, FA_ERR_UNSUPPORTED.  The list of work
- * (with few rows too) is counted in 32 bits: B * Hkv * (row tiles of max_tokens drafts) * (twice the tiles of 128 keys in max_pages
- * pages + 4) is at most 2^30, else FA_ERR_UNSUPPORTED (a row tile: 128 / (Hq / Hkv) tokens, or 128 of a token's heads).
+ * (with few rows too) is counted in 32 bits: B * Hkv * (row tiles of max_tokens drafts) * (the tiles of 128 keys in max_pages pages, over bf16
+ * caches with heads of 64 or 128 twice, + 4) is at most 2^30, else FA_ERR_UNSUPPORTED (a row tile: 128 / (Hq / Hkv) tokens, or 128 of a
+ * token's heads).
  * FA_FLAG_SERIAL_KERNEL selects a plain kernel of one CTA per query row.
  */
 typedef struct fa_tree {

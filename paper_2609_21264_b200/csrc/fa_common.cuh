@@ -23,7 +23,6 @@ enum WaitSite : uint32_t {
     kSiteEpiOFull = 0x0601, kSiteEpiStaged = 0x0602, kSiteEpiState = 0x0603,
     kSiteSmemAlign = 0x0701,
     kSiteItem = 0x0801,
-    kSiteMmaTail = 0x0307, kSiteTailIssued = 0x0a01, kSiteTailVFull = 0x0a02,
 };
 
 struct FwdParams {

@@ -55,8 +55,6 @@ FA_DEVI void st_shared_u64(uint32_t addr, uint32_t lo, uint32_t hi) {
     asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(lo), "r"(hi) : "memory");
 }
 
-FA_DEVI void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
-
 }  // namespace ptx
 
 // Bounded waits.  The result warps wait, directly or in turn, for every other role: they alone watch the clock.  Once one of their

@@ -10,6 +10,10 @@
 
 namespace fa_host {
 
+// Units that a list of work can have at most, by either kernel's count: they are counted in 32 bits, and blocks whose tiles are rounded up to
+// a share can count twice their tiles.
+constexpr long long kMostUnits = 1ll << 30;
+
 inline bool head_sizes_ok(int dqk, int dv) {
     return (dqk == 64 && dv == 64) || (dqk == 128 && dv == 128) || (dqk == 192 && dv == 128);
 }

@@ -20,9 +20,7 @@ inline int rows_per_block(int rows, int dqk, bool e4m3, bool diff) {
     return rows > 32 && !e4m3 && dqk != 192 ? 64 : 32;
 }
 
-// Units that a call's list of work can have at most; the kernel counts them in 32 bits, and the blocks of a single sequence, rounded
-// up to a share, can count twice their tiles.
-constexpr long long kMostUnits = 1ll << 30;
+// Units that a call's list of work can have at most (kMostUnits).
 inline long long most_units(const fa::PagedParams& p) {
     return static_cast<long long>(p.B) * p.Hkv * p.row_blocks *
            (fa::paged_tiles(static_cast<int>(static_cast<long long>(p.max_pages) * p.page_size)) + fa::kMostPartCost);

@@ -62,9 +62,8 @@ fa::TreeList make_list(int group, int max_tokens, int dqk, bool e4m3) {
     return li;
 }
 
-constexpr long long kMostUnits = 1ll << 30;      // the kernel counts units in 32 bits
-
-// Units that a call's list can have at most.
+// Whether a call's list can have more units than are counted.  (With few rows too: the streaming kernel's has no more tiles, and three units
+// beside them at most.)
 bool too_long(const fa::TreeList& li, int B, int Hkv, int max_tokens, long long most_keys) {
     const long long row_tiles = fa::tree_row_tiles(li, max_tokens), most_tiles = (most_keys + fa::kTileN - 1) / fa::kTileN;
     return static_cast<long long>(B) * Hkv > kMostUnits / row_tiles / (most_tiles * li.w2 + li.cost);

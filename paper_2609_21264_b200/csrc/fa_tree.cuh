@@ -318,7 +318,6 @@ FA_DEVI bool mbar_test_wait(uint32_t bar, uint32_t parity) {
         : "memory");
     return ok != 0;
 }
-FA_DEVI void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
 // Two e4m3 codes (low byte first) -> two fp16, exactly (NaN stays NaN).
 FA_DEVI uint32_t e4m3x2_to_f16x2(uint32_t codes) {

@@ -225,6 +225,7 @@ FA_DEVI void grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "m
 
 // ------------------------------------------------------------------ TMA
 
+FA_DEVI void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 FA_DEVI void prefetch_tensormap(const CUtensorMap* map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
 }
