@@ -1,6 +1,7 @@
 // The Python calls on drafted tokens: what binding.py's functions of the same names check, allocate and hand to the C entries of
 // include/fa.h.  A call is made once per layer or step and its kernels take 2 to 15 us; checks and outputs in Python took 4 to 9 us of
-// host time beside the launches' 3.5 each (tree_layout 11.0 us), here a fraction of one.
+// host time beside the launches' 3.5 each (tree_layout 11.0 us), here a fraction of one (tree_layout 5.4 us,
+// forward_paged_tree 7.9, with what giving the interpreter's lock back costs, 0.1).
 //
 // Every function returns its results, or the entry's status code as an int where that is not FA_OK, and raises ValueError for arguments
 // that no entry should see.  The C entries are bound by address: the library is the one that binding.py has loaded.  What can wait for the

@@ -18,11 +18,15 @@
 //   * The mask concerns the last tiles alone: a thread has one row, takes its bits for 32 keys out of the row's words by a funnel shift,
 //     and hides keys past the length with the same bits.
 //
-// What bounds it.  16 sequences of 129 to 8192 keys, trees of 16 to 64 drafts, 32/8 heads of 128, bf16: 67.6 us, where 248 MB take 38 at the
+// What bounds it.  16 sequences of 129 to 8192 keys, trees of 16 to 64 drafts, 32/8 heads of 128, bf16: 67.8 us, where 248 MB take 38 at the
 // copy rate.  With 256 rows a tile of keys takes a CTA 3000 cycles, the chain softmax (2000) -> P V and next scores (1024 cycles of MMAs) of each
-// stream; 28 tiles a CTA.  Beside them: 9000 cycles from the launch to the first scores (list, block table, first loads), 6000 from
-// one block's last tile to the next one's first (result, barrier, first pass), 5 us for the join.  48 sequences of 300 to 8192 keys over e4m3, 13 drafts, 64/8 heads: 148 us, where 521 MB take 80: two tiles
-// take 3600 cycles, of which MMAs 2630 (8-bit scores in three terms, fp16 products), and each CTA has four blocks.
+// stream; the list gives most CTAs 20 to 24 such tiles in one to three parts.  That is 60 to 72 thousand of this kernel's 110 (65.2 us at
+// 1.70 GHz): the rest is 9000 from the launch to the first scores (list, block table, first loads), some 6000 from one part's last tile to
+// the next one's first (result, barrier, first pass), and what has not been taken apart.  The join takes 5 us more.
+// 48 sequences of 300 to 8192 keys over e4m3, 13 drafts, 64/8 heads: 151 us, where 521 MB take 80: two tiles take 3600 cycles, of which MMAs
+// 2630 (8-bit scores in three terms, fp16 products).  Most CTAs have 105 to 113 tiles in three or four parts, 190 to 203 thousand of 266
+// thousand cycles (158.6 us at 1.68 GHz): a quarter lies outside of the loop over the tiles, not taken apart yet.  (A part's beginning is
+// a chain here: queries loaded when the last scores of the part before are done, turned into terms, then the first values into fp16.)
 //
 // Over an e4m3 cache K is multiplied as it is (kind::f8f6f4), the queries as three e5m2 terms like in fa_paged.cuh, added up in one
 // accumulator (half as many MMAs again); P V is an fp16 product, since terms of P would be work of the softmax warps, which are the
@@ -86,13 +90,14 @@ __host__ __device__ inline int tree_head_units(const TreeUnits& u) { return u.pa
 // two row tiles are among it.
 struct TreeBatch { int blocks, units, longest, shortest, kinds; };
 constexpr int kTreeSplitCost = 3;
-// Tiles of a piece at least: a tile takes its CTA about four times what a piece takes the joining kernel, so tiles / s + s / 4 is least where a
-// piece has s = half the root of the tiles (one sequence of 17353 keys, one K/V head, 64 drafts of 8 heads: 53.3 us in pieces as small as the
+// Tiles of a piece at least: a tile takes its CTA about four times what a piece takes the joining kernel, so pieces of s tiles cost
+// s + tiles / (4 s), which is least where s is half the root of the tiles (one sequence of 17353 keys, one K/V head, 64 drafts of 8 heads: 53.3 us in pieces as small as the
 // CTAs allow, 30.3 so; 100000 and 33333 keys, 13 drafts 66.7, 47.9).
 __host__ __device__ inline int tree_root(int tiles) { return static_cast<int>(ceilf(0.5f * sqrtf(static_cast<float>(tiles)))); }
 // Small batches.  Where there is a CTA for every block, the longest block, unsplit, is what the call takes; split, it takes an equal share and
 // what the join of the pieces costs, about three tiles' time.  Where that is not less, all blocks count the same and nothing is split (16
-// sequences of 1003 keys, 8 K/V heads, 32 rows: 18.3 us, against 21.0 split; one of 500 keys, 26 drafts: 12.2 split, against 13.7).  Where
+// sequences of 1003 keys, 8 K/V heads, 9 drafts of 4 heads: 18.1 us, against 20.8 split; over e4m3, 5 drafts of 8 heads, 21.0 against 25.1; one
+// of 500 keys, 26 drafts: 12.2 split, against 13.7).  Where
 // there are two CTAs for every block at least and all are equally long, their pieces are equally long too, and a CTA has one.  No share
 // is smaller than a piece of the longest sequence should be (tree_root).  Returns the share (0: what the total gives).
 __host__ __device__ inline int tree_rules(TreeList& li, const TreeBatch& b, int ctas) {
