@@ -706,9 +706,18 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                         named_barrier_sync(1 + w, 128);
                         if (key < kStates) {
                             const float old = first ? -INFINITY : Cfg::kBias - sh.neg_m[w][key];
-                            const float mx = fmaxf(fmaxf(fmaxf(sh.red[w][0][key], sh.red[w][1][key]), fmaxf(sh.red[w][2][key], sh.red[w][3][key])), old);
-                            sh.neg_m[w][key] = Cfg::kBias - mx;
-                            sh.neg_p[w][key] = mx == -INFINITY ? 0.f : Cfg::kBias - mx;
+                            const float here = fmaxf(fmaxf(sh.red[w][0][key], sh.red[w][1][key]), fmaxf(sh.red[w][2][key], sh.red[w][3][key]));
+                            float mx = fmaxf(here, old), neg = Cfg::kBias - mx;
+                            // A score between 2^27 and 2^28 has a step of 16, to which the bias of 11 is rounded, and 2^16 is no number of
+                            // fp16's: one step higher the reference leaves that score a bias of 0 (and its own negative gives it back).
+                            if constexpr (kE4m3) {
+                                if (here + neg > 15.f) {
+                                    mx = Cfg::kBias + here;
+                                    neg = Cfg::kBias - mx;
+                                }
+                            }
+                            sh.neg_m[w][key] = neg;
+                            sh.neg_p[w][key] = mx == -INFINITY ? 0.f : neg;
                             sh.rescale[w][key] = mx == -INFINITY ? 1.f : exp2_approx(old - mx);
                         }
                         if (!first)       // the group's product before: nothing else adds to this accumulator
@@ -732,7 +741,7 @@ fa_paged_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant_
                         }
                     }
                     // The sum of score and reference is rounded apart from the score's own scaling: the score that the reference was
-                    // taken from comes out as exactly the bias, however large it is.
+                    // taken from comes out as the bias, however large it is (from 2^23 on as far as the score's step allows).
 #pragma unroll
                     for (int r = 0; r < kStates; r += 4) {
                         const float4 np = *reinterpret_cast<const float4*>(&sh.neg_p[w][r]);

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from draft_util import tree_reference
-from paged_util import BF16_HALF, FP32_SLACK, assert_attention, ok, pool
+from paged_util import BF16_HALF, FP32_SLACK, assert_attention, ok, pool, rows_of
 from test_gpu_tree import run
 
 pytestmark = pytest.mark.gpu
@@ -157,3 +157,39 @@ def test_bits_of_probabilities_over_an_8_bit_cache(handle, n, dqk, dv):
     worst = ((o.cpu().double() - O).abs() / tol).max().item()
     assert worst <= 1.0, worst
     assert ((lse.cpu().double() - L).abs() <= FP32_SLACK).all()
+
+
+def far_scores(shift, n, dqk, dv, e4m3):
+    """Queries of 2^shift, so scores far beyond what the bits of a 32-bit number behind the point hold, and what comes out: the value of each row's
+    best key, which leads by more than a score's 32-bit sum of products can be off by and e^30 has room for."""
+    lens = [1500, 140, 700]
+    k, v, table, lens_t, ks, vs = pool(lens, 16, 2, dqk, dv, e4m3, False, 50)
+    q = torch.randn(3 * n, 8, dqk, generator=torch.Generator().manual_seed(51)).to(torch.bfloat16) * 2.0 ** shift
+    for b, keys in enumerate(lens):
+        kd = rows_of(k, ks, table, b, keys)
+        for h in range(8):
+            x = q[b * n:(b + 1) * n, h].double()
+            z = (x @ kd[h // 4].T).masked_fill(torch.arange(keys)[None] > torch.arange(keys - n, keys)[:, None], -float("inf"))
+            best = z.topk(2, 1)
+            off = (x.abs() @ kd[h // 4].abs().T).gather(1, best.indices).sum(1) * dqk * 2.0 ** -24
+            assert ((best.values[:, 0] - best.values[:, 1] - off) * dqk ** -0.5 > 30).all()
+    ref = tree_reference(q, k, v, ks, vs, table, lens, [0, n, 2 * n, 3 * n], [torch.ones(n, n).tril() > 0] * 3, dqk ** -0.5)
+    return q.cuda(), (k, v, ks, vs), table, lens_t, ref
+
+
+FAR = [20, 22, 23, 24, 25, 26, 27, 28, 30, 34, 60]
+
+
+@pytest.mark.parametrize("shift", FAR)
+@pytest.mark.parametrize("dqk,dv", [(64, 64), (128, 128), (192, 128)])
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+def test_scores_of_any_size_few_rows(handle, e4m3, dqk, dv, shift):
+    from paper_2609_21264_b200 import binding as b
+    q, (k, v, ks, vs), table, lens_t, ref = far_scores(shift, 4, dqk, dv, e4m3)
+    o, lse = b.forward_paged_tree(handle, q, b.PagedCache(k, v, ks, vs), table, lens_t, None)
+    ok(handle)
+    kernel_was(handle, 16, e4m3)
+    assert_attention(o, lse, *ref)
+    o, lse = b.forward_paged(handle, q, b.PagedCache(k, v, ks, vs), table, lens_t)
+    ok(handle)
+    assert_attention(o, lse, *ref)
