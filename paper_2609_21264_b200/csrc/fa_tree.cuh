@@ -435,13 +435,18 @@ FA_DEVI void tree_hide(uint32_t tS, uint32_t seen) {
     }
 }
 
+constexpr float kTreeFar = 4194304.f;      // 2^22
+
 // The pass of fa_softmax_pass.cuh, over e4m3 caches with P as fp16 under a bias.  P = 2^(s c + off), off = bias - u c with the reference u; all
 // exponentials on the special-function unit.
+// Far scores: s c + off is one rounding of the exact sum, but off itself is a rounded number, and from 2^22 on (log2 units) what it is off by
+// moves all weights of a row by more than fp16 has room for, from 2^31 on by more than fp32.  The scores of a row whose reference lies that
+// far out are taken relative to it first, s - u, which costs them no more than their own rounding.  `far` says that the warp has such a row.
 // kPSmem: P goes to the row's bytes p_row of two swizzled chunks of 64 keys; `take` is called once the scores are in registers, and
 // says when the product before (of P's space and O) is done, `arrive_first` is not.
 template <int DV, bool kHalf, bool kPSmem, typename Take, typename ArriveFirst, typename ArriveRest>
-FA_DEVI void tree_pass(uint32_t tS, uint32_t tO, uint32_t p_row, float c, float tau_raw, float bias, bool first_tile, float& m_ref, float& l, int lane,
-                       Take&& take, ArriveFirst&& arrive_first, ArriveRest&& arrive_rest) {
+FA_DEVI void tree_pass(uint32_t tS, uint32_t tO, uint32_t p_row, float c, float tau_raw, float bias, bool first_tile, float& m_ref, float& l, bool& far,
+                       int lane, Take&& take, ArriveFirst&& arrive_first, ArriveRest&& arrive_rest) {
     using namespace ptx;
     const float2 c2 = make_float2(c, c);
     float2 off2;
@@ -480,6 +485,8 @@ FA_DEVI void tree_pass(uint32_t tS, uint32_t tO, uint32_t p_row, float c, float 
             sum_b = fadd2_ftz(sum_b, make_float2(__uint_as_float(s[q * 32 + e + 2]), __uint_as_float(s[q * 32 + e + 3])));
         }
     };
+    auto is_far = [&]() -> bool { return m_ref != -INFINITY && fabsf(m_ref * c) > kTreeFar; };
+    bool fresh = first_tile;         // no reference yet
 #pragma unroll 1
     for (;;) {
         tmem_ld_x32(tS + 0, s + 0);
@@ -487,8 +494,18 @@ FA_DEVI void tree_pass(uint32_t tS, uint32_t tO, uint32_t p_row, float c, float 
         tmem_ld_x32(tS + 64, s + 64);
         tmem_ld_x32(tS + 96, s + 96);
         tc_wait_ld();
+        float base = 0.f;            // what the scores are relative to
+        if (__builtin_expect(far, 0)) {
+            if (is_far()) base = m_ref;
+#pragma unroll
+            for (int e = 0; e < kTileN; e += 2) {
+                const float2 x = __fadd2_rn(make_float2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), make_float2(-base, -base));
+                s[e] = __float_as_uint(x.x);
+                s[e + 1] = __float_as_uint(x.y);
+            }
+        }
         auto set_off = [&]() {
-            const float off = m_ref == -INFINITY ? bias : bias - m_ref * c;
+            const float off = m_ref == -INFINITY ? bias : bias - (m_ref - base) * c;
             off2 = make_float2(off, off);
         };
         set_off();
@@ -501,21 +518,26 @@ FA_DEVI void tree_pass(uint32_t tS, uint32_t tO, uint32_t p_row, float c, float 
             for (int q = 0; q < 8; ++q)
                 a[q] = fmax3(a[q], __uint_as_float(s[e + 2 * q]), __uint_as_float(s[e + 2 * q + 1]));
         }
-        if (!first_tile) exp_chunk(0);
+        if (!fresh) exp_chunk(0);
         float mx = fmaxf(fmax3(a[0], a[1], a[2]), fmax3(a[3], a[4], a[5]));
         mx = fmax3(mx, a[6], a[7]);
-        if (first_tile) {            // (nothing to guess with: the row's first reference is this maximum)
+        if (fresh) {                 // (nothing to guess with: the row's first reference is this maximum)
             m_ref = mx;
+            fresh = false;
+            far = __any_sync(0xffffffffu, is_far());
+            if (__builtin_expect(far, 0)) continue;
             set_off();
             exp_chunk(0);
             break;
         }
-        const bool grow = mx > m_ref + tau_raw;
+        const float top = mx + base;
+        const bool grow = mx > (m_ref - base) + tau_raw && top > m_ref;       // (the second alone ends the loop: references only rise)
         if (!__any_sync(0xffffffffu, grow)) break;
         if (grow) {
-            alpha = exp2_approx((m_ref - mx) * c);    // 0 on the first tile
-            m_ref = mx;
+            alpha *= exp2_approx((m_ref - top) * c);    // 0 where no key has been seen yet (a far reference may rise twice: by what is near it, then exactly)
+            m_ref = top;
         }
+        far = __any_sync(0xffffffffu, is_far());
     }
     if constexpr (kPSmem) take();
     if (!first_tile && __any_sync(0xffffffffu, alpha != 1.f)) {
@@ -719,6 +741,7 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             if (!live) c = 0.f;
             const float bias = live ? Cfg::kBias : -INFINITY;
             float m_ref = -INFINITY, l = 0.f, tau_raw = kRescaleThresholdLog2 / c;
+            bool far = false;
             for (int j = 0; j < steps; ++j, ++n_s) {
                 ok = __all_sync(0xffffffffu, ok && tree_wait_timed(sh.s_full[t], n_s & 1, &sh.wait, kSiteSoftmaxSFull));
                 if (!ok) break;
@@ -778,7 +801,7 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                     }
                     tc_wait_st();
                 }
-                tree_pass<DV, kE4m3, Cfg::kPSmem>(tS, tO + 128 * t, sP + t * Cfg::kPBytes + row * 128, c, tau_raw, bias, j == 0, m_ref, l, lane, take,
+                tree_pass<DV, kE4m3, Cfg::kPSmem>(tS, tO + 128 * t, sP + t * Cfg::kPBytes + row * 128, c, tau_raw, bias, j == 0, m_ref, l, far, lane, take,
                                      [&]() { mbar_arrive(bar_pf); }, [&]() { mbar_arrive(bar_pr); });
             }
             // ---- the part's result: sum and reference of a row that saw a key, O of one stream or of both

@@ -159,12 +159,15 @@ def test_bits_of_probabilities_over_an_8_bit_cache(handle, n, dqk, dv):
     assert ((lse.cpu().double() - L).abs() <= FP32_SLACK).all()
 
 
-def far_scores(shift, n, dqk, dv, e4m3):
-    """Queries of 2^shift, so scores far beyond what the bits of a 32-bit number behind the point hold, and what comes out: the value of each row's
-    best key, which leads by more than a score's 32-bit sum of products can be off by and e^30 has room for."""
-    lens = [1500, 140, 700]
-    k, v, table, lens_t, ks, vs = pool(lens, 16, 2, dqk, dv, e4m3, False, 50)
-    q = torch.randn(3 * n, 8, dqk, generator=torch.Generator().manual_seed(51)).to(torch.bfloat16) * 2.0 ** shift
+def far_scores(shift, n, dqk, dv, e4m3, below=False, seed=50):
+    """Queries of 2^shift, so scores far beyond what the bits of a 32-bit number behind the point hold (below: all of them negative), and what comes
+    out: the value of each row's best key, which leads by more than a score's 32-bit sum of products can be off by and e^30 has room for."""
+    lens = [300, 40, 150] if below else [1500, 140, 700]
+    k, v, table, lens_t, ks, vs = pool(lens, 16, 2, dqk, dv, e4m3, False, seed)
+    q = torch.randn(3 * n, 8, dqk, generator=torch.Generator().manual_seed(seed + 1)).to(torch.bfloat16) * 2.0 ** shift
+    if below:
+        q = q.abs()
+        k = (k.view(torch.uint8) | 0x80).view(k.dtype) if e4m3 else -k.abs()
     for b, keys in enumerate(lens):
         kd = rows_of(k, ks, table, b, keys)
         for h in range(8):
@@ -192,4 +195,28 @@ def test_scores_of_any_size_few_rows(handle, e4m3, dqk, dv, shift):
     assert_attention(o, lse, *ref)
     o, lse = b.forward_paged(handle, q, b.PagedCache(k, v, ks, vs), table, lens_t)
     ok(handle)
+    assert_attention(o, lse, *ref)
+
+
+@pytest.mark.parametrize("shift", FAR)
+@pytest.mark.parametrize("dqk,dv", [(64, 64), (128, 128), (192, 128)])
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+def test_scores_of_any_size(handle, e4m3, dqk, dv, shift):
+    from paper_2609_21264_b200 import binding as b
+    q, (k, v, ks, vs), table, lens_t, ref = far_scores(shift, 11, dqk, dv, e4m3)
+    o, lse = b.forward_paged_tree(handle, q, b.PagedCache(k, v, ks, vs), table, lens_t, None)
+    ok(handle)
+    kernel_was(handle, 44, e4m3)
+    assert_attention(o, lse, *ref)
+
+
+@pytest.mark.parametrize("shift", FAR)
+@pytest.mark.parametrize("n", [4, 11], ids=["16rows", "44rows"])
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+def test_scores_far_below_zero(handle, e4m3, n, shift):
+    from paper_2609_21264_b200 import binding as b
+    q, (k, v, ks, vs), table, lens_t, ref = far_scores(shift, n, 128, 128, e4m3, below=True, seed=60)
+    o, lse = b.forward_paged_tree(handle, q, b.PagedCache(k, v, ks, vs), table, lens_t, None)
+    ok(handle)
+    kernel_was(handle, 4 * n, e4m3)
     assert_attention(o, lse, *ref)
