@@ -18,12 +18,12 @@
 //   * The mask concerns the last tiles alone: a thread has one row, takes its bits for 32 keys out of the row's words by a funnel shift,
 //     and hides keys past the length with the same bits.
 //
-// What bounds it.  16 sequences of 129 to 8192 keys, trees of 16 to 64 drafts, 32/8 heads of 128, bf16: 67.8 us, where 248 MB take 38 at the
+// What bounds it.  16 sequences of 129 to 8192 keys, trees of 16 to 64 drafts, 32/8 heads of 128, bf16: 68.1 us, where 248 MB take 38 at the
 // copy rate.  With 256 rows a tile of keys takes a CTA 3000 cycles, the chain softmax (2000) -> P V and next scores (1024 cycles of MMAs) of each
 // stream; the list gives most CTAs 20 to 24 such tiles in one to three parts.  That is 60 to 72 thousand of this kernel's 110 (65.2 us at
 // 1.70 GHz): the rest is 9000 from the launch to the first scores (list, block table, first loads), some 6000 from one part's last tile to
 // the next one's first (result, barrier, first pass), and what has not been taken apart.  The join takes 5 us more.
-// 48 sequences of 300 to 8192 keys over e4m3, 13 drafts, 64/8 heads: 151 us, where 521 MB take 80: two tiles take 3600 cycles, of which MMAs
+// 48 sequences of 300 to 8192 keys over e4m3, 13 drafts, 64/8 heads: 153 us, where 521 MB take 80: two tiles take 3600 cycles, of which MMAs
 // 2630 (8-bit scores in three terms, fp16 products).  Most CTAs have 105 to 113 tiles in three or four parts, 190 to 203 thousand of 266
 // thousand cycles (158.6 us at 1.68 GHz): a quarter lies outside of the loop over the tiles, not taken apart yet.  (A part's beginning is
 // a chain here: queries loaded when the last scores of the part before are done, turned into terms, then the first values into fp16.)
@@ -284,7 +284,7 @@ struct TreeShared {
     TreeWait wait;
     int v_issued;                 // V tiles whose loads have been issued
     int loads[3];                 // of K and V tiles and of queries, at the end
-    float stat_m[2][kTileM], stat_l[2][kTileM];       // (of two streams on the same rows)
+    float stat_m[2][kTileM], stat_l[2][kTileM];       // (of two streams on the same rows; before a part's end stat_l: what far scores are relative to)
     uint8_t q_shift[2][kE4m3 ? kTileM : 4];      // of even and odd parts: 127 - exponent that a row was scaled by
 };
 
@@ -435,23 +435,60 @@ FA_DEVI void tree_hide(uint32_t tS, uint32_t seen) {
     }
 }
 
+// Far scores.  s c + off is one rounding of the exact sum, but off itself is a rounded number, and from 2^22 on (log2 units) what it is off by
+// moves all weights of a row by more than fp16 has room for, from 2^31 on by more than fp32.  So where references come to lie that far out, the
+// scores of the rows' tiles from there on are taken relative to a `base` first, in TMEM, which costs them no more than their own
+// rounding, and m_ref is relative to it too.  (Functions of their own, as code that hardly ever runs: see TreeWait.)
 constexpr float kTreeFar = 4194304.f;      // 2^22
+FA_DEVI bool tree_far(float m_ref, float c) { return m_ref != -INFINITY && fabsf(m_ref * c) > kTreeFar; }
+// All scores of a tile less a number of each row's.
+static __device__ __noinline__ void tree_shift(uint32_t tS, float by) {
+#pragma unroll 1
+    for (int e = 0; e < kTileN; e += 16) {
+        uint32_t s[16];
+        ptx::tmem_ld_x16(tS + e, s);
+        ptx::tc_wait_ld();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = __float_as_uint(__uint_as_float(s[i]) - by);
+        ptx::tmem_st_x16(tS + e, s);
+    }
+    ptx::tc_wait_st();
+}
+
+// Over e4m3 caches scores are below 2^32, so a row's factor says ahead of its tiles whether they can be far: then the tile's largest score is looked
+// for before the pass.  Returns the new base; m_ref follows it.
+constexpr float kTreeFarFactor = 1.f / 1024;
+static __device__ __noinline__ float tree_rebase(uint32_t tS, float c, float base, float* m_ref) {
+    float mx = -INFINITY;
+#pragma unroll 1
+    for (int e = 0; e < kTileN; e += 16) {
+        uint32_t s[16];
+        ptx::tmem_ld_x16(tS + e, s);
+        ptx::tc_wait_ld();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, __uint_as_float(s[i]));
+    }
+    const float up = (mx - base) * c;
+    float by = 0.f;
+    if (mx != -INFINITY && (*m_ref == -INFINITY ? fabsf(up) : up) > kTreeFar) by = mx - base;
+    *m_ref -= by;
+    tree_shift(tS, base + by);
+    return base + by;
+}
 
 // The pass of fa_softmax_pass.cuh, over e4m3 caches with P as fp16 under a bias.  P = 2^(s c + off), off = bias - u c with the reference u; all
 // exponentials on the special-function unit.
-// Far scores: s c + off is one rounding of the exact sum, but off itself is a rounded number, and from 2^22 on (log2 units) what it is off by
-// moves all weights of a row by more than fp16 has room for, from 2^31 on by more than fp32.  The scores of a row whose reference lies that
-// far out are taken relative to it first, s - u, which costs them no more than their own rounding.  `far` says that the warp has such a row.
+// Over bf16 caches the pass gives up where a reference has come out far (false: nothing has been handed over yet), and is made again on the
+// moved scores, the largest of which is 0, so that no reference moves a second time.
 // kPSmem: P goes to the row's bytes p_row of two swizzled chunks of 64 keys; `take` is called once the scores are in registers, and
 // says when the product before (of P's space and O) is done, `arrive_first` is not.
 template <int DV, bool kHalf, bool kPSmem, typename Take, typename ArriveFirst, typename ArriveRest>
-FA_DEVI void tree_pass(uint32_t tS, uint32_t tO, uint32_t p_row, float c, float tau_raw, float bias, bool first_tile, float& m_ref, float& l, bool& far,
+FA_DEVI bool tree_pass(uint32_t tS, uint32_t tO, uint32_t p_row, float c, float tau_raw, float bias, bool first_tile, float& m_ref, float& l, float& alpha,
                        int lane, Take&& take, ArriveFirst&& arrive_first, ArriveRest&& arrive_rest) {
     using namespace ptx;
     const float2 c2 = make_float2(c, c);
     float2 off2;
     float2 sum_a = make_float2(0.f, 0.f), sum_b = make_float2(0.f, 0.f);
-    float alpha = 1.f;
     uint32_t s[kTileN];
     auto exp_chunk = [&](int q) {
 #pragma unroll
@@ -485,8 +522,6 @@ FA_DEVI void tree_pass(uint32_t tS, uint32_t tO, uint32_t p_row, float c, float 
             sum_b = fadd2_ftz(sum_b, make_float2(__uint_as_float(s[q * 32 + e + 2]), __uint_as_float(s[q * 32 + e + 3])));
         }
     };
-    auto is_far = [&]() -> bool { return m_ref != -INFINITY && fabsf(m_ref * c) > kTreeFar; };
-    bool fresh = first_tile;         // no reference yet
 #pragma unroll 1
     for (;;) {
         tmem_ld_x32(tS + 0, s + 0);
@@ -494,18 +529,8 @@ FA_DEVI void tree_pass(uint32_t tS, uint32_t tO, uint32_t p_row, float c, float 
         tmem_ld_x32(tS + 64, s + 64);
         tmem_ld_x32(tS + 96, s + 96);
         tc_wait_ld();
-        float base = 0.f;            // what the scores are relative to
-        if (__builtin_expect(far, 0)) {
-            if (is_far()) base = m_ref;
-#pragma unroll
-            for (int e = 0; e < kTileN; e += 2) {
-                const float2 x = __fadd2_rn(make_float2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), make_float2(-base, -base));
-                s[e] = __float_as_uint(x.x);
-                s[e + 1] = __float_as_uint(x.y);
-            }
-        }
         auto set_off = [&]() {
-            const float off = m_ref == -INFINITY ? bias : bias - (m_ref - base) * c;
+            const float off = m_ref == -INFINITY ? bias : bias - m_ref * c;
             off2 = make_float2(off, off);
         };
         set_off();
@@ -518,26 +543,27 @@ FA_DEVI void tree_pass(uint32_t tS, uint32_t tO, uint32_t p_row, float c, float 
             for (int q = 0; q < 8; ++q)
                 a[q] = fmax3(a[q], __uint_as_float(s[e + 2 * q]), __uint_as_float(s[e + 2 * q + 1]));
         }
-        if (!fresh) exp_chunk(0);
+        if (!first_tile) exp_chunk(0);
         float mx = fmaxf(fmax3(a[0], a[1], a[2]), fmax3(a[3], a[4], a[5]));
         mx = fmax3(mx, a[6], a[7]);
-        if (fresh) {                 // (nothing to guess with: the row's first reference is this maximum)
+        if (first_tile) {            // (nothing to guess with: the row's first reference is this maximum)
             m_ref = mx;
-            fresh = false;
-            far = __any_sync(0xffffffffu, is_far());
-            if (__builtin_expect(far, 0)) continue;
+            if constexpr (!kHalf) {
+                if (__any_sync(0xffffffffu, tree_far(m_ref, c))) return false;
+            }
             set_off();
             exp_chunk(0);
             break;
         }
-        const float top = mx + base;
-        const bool grow = mx > (m_ref - base) + tau_raw && top > m_ref;       // (the second alone ends the loop: references only rise)
+        const bool grow = mx > m_ref + tau_raw;
         if (!__any_sync(0xffffffffu, grow)) break;
         if (grow) {
-            alpha *= exp2_approx((m_ref - top) * c);    // 0 where no key has been seen yet (a far reference may rise twice: by what is near it, then exactly)
-            m_ref = top;
+            alpha = exp2_approx((m_ref - mx) * c);    // 0 where no key has been seen yet
+            m_ref = mx;
         }
-        far = __any_sync(0xffffffffu, is_far());
+        if constexpr (!kHalf) {
+            if (__any_sync(0xffffffffu, tree_far(m_ref, c))) return false;
+        }
     }
     if constexpr (kPSmem) take();
     if (!first_tile && __any_sync(0xffffffffu, alpha != 1.f)) {
@@ -586,6 +612,7 @@ FA_DEVI void tree_pass(uint32_t tS, uint32_t tO, uint32_t p_row, float c, float 
     }
     sum_chunk(3);
     l = l * alpha + ((sum_a.x + sum_a.y) + (sum_b.x + sum_b.y));
+    return true;
 }
 
 // ------------------------------------------------------------------ kernel
@@ -741,7 +768,9 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             if (!live) c = 0.f;
             const float bias = live ? Cfg::kBias : -INFINITY;
             float m_ref = -INFINITY, l = 0.f, tau_raw = kRescaleThresholdLog2 / c;
-            bool far = false;
+            bool far = false;            // scores of the warp's rows are relative to base (over e4m3 caches, which leave no register, where stat_l is free)
+            float base_reg = 0.f;
+            float& base = kE4m3 ? sh.stat_l[t][row] : base_reg;
             for (int j = 0; j < steps; ++j, ++n_s) {
                 ok = __all_sync(0xffffffffu, ok && tree_wait_timed(sh.s_full[t], n_s & 1, &sh.wait, kSiteSoftmaxSFull));
                 if (!ok) break;
@@ -753,6 +782,8 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                         // times the smallest normal number are nothing all the same)
                         if (live && c < FLT_MIN) c = FLT_MIN;
                         tau_raw = kRescaleThresholdLog2 / c;
+                        far = __any_sync(0xffffffffu, c > kTreeFarFactor);
+                        if (far) base = 0.f;
                     }
                 }
                 // (P in shared memory: the scores are in registers; before P is written, the product of the step before has to be done)
@@ -801,12 +832,31 @@ fa_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                     }
                     tc_wait_st();
                 }
-                tree_pass<DV, kE4m3, Cfg::kPSmem>(tS, tO + 128 * t, sP + t * Cfg::kPBytes + row * 128, c, tau_raw, bias, j == 0, m_ref, l, far, lane, take,
-                                     [&]() { mbar_arrive(bar_pf); }, [&]() { mbar_arrive(bar_pr); });
+                float alpha = 1.f;
+                if (far) {
+                    if constexpr (kE4m3) {
+                        float ref = m_ref;
+                        base = tree_rebase(tS, c, base, &ref);
+                        m_ref = ref;
+                    } else {
+                        tree_shift(tS, base);
+                    }
+                }
+                for (bool again = false; !tree_pass<DV, kE4m3, Cfg::kPSmem>(tS, tO + 128 * t, sP + t * Cfg::kPBytes + row * 128, c, tau_raw, bias,
+                                                                            j == 0 && !again, m_ref, l, alpha, lane, take,
+                                                                            [&]() { mbar_arrive(bar_pf); }, [&]() { mbar_arrive(bar_pr); });
+                     again = true) {
+                    const float by = tree_far(m_ref, c) ? m_ref : 0.f;
+                    tree_shift(tS, by);
+                    m_ref -= by;
+                    base += by;
+                    far = true;
+                }
             }
             // ---- the part's result: sum and reference of a row that saw a key, O of one stream or of both
             const float off = m_ref == -INFINITY ? Cfg::kBias : Cfg::kBias - m_ref * c;
             float m = l > 0.f || l != l ? -off : -INFINITY;       // (a NaN goes through)
+            if (far) m += base * c;
             const bool whole = e.slot < 0;
             const float vs = kE4m3 && p.v_scale ? p.v_scale[e.kvh] : 1.f;
             float f0 = 1.f, f1 = 0.f;

@@ -3,7 +3,7 @@ at the name of the kernel that ran."""
 import pytest
 import torch
 
-from draft_util import tree_reference
+from draft_util import pack, tree_reference
 from paged_util import BF16_HALF, FP32_SLACK, assert_attention, ok, pool, rows_of
 from test_gpu_tree import run
 
@@ -220,3 +220,22 @@ def test_scores_far_below_zero(handle, e4m3, n, shift):
     ok(handle)
     kernel_was(handle, 4 * n, e4m3)
     assert_attention(o, lse, *ref)
+
+
+@pytest.mark.parametrize("shift", [10, 24, 28, 34])
+@pytest.mark.parametrize("dqk,dv", [(64, 64), (128, 128), (192, 128)])
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+def test_far_scores_of_rows_that_see_one_key(handle, e4m3, dqk, dv, shift):
+    """Every token sees itself alone, so most rows see nothing of their first tile of keys: the only score is the reference, however far out it is
+    (q = +-k, so half of them are far above zero and half far below)."""
+    from paper_2609_21264_b200 import binding as b
+    n = 200
+    k, v, table, lens_t, ks, vs = pool([n], 16, 1, dqk, dv, e4m3, False, 70)
+    keys = rows_of(k, None, table, 0, n)[0]
+    sign = torch.where(torch.arange(n) % 3 == 0, -1.0, 1.0)
+    q = ((keys * sign[:, None])[:, None].expand(n, 2, dqk) * 2.0 ** shift).to(torch.bfloat16).cuda()
+    seen = torch.eye(n) > 0
+    o, lse = b.forward_paged_tree(handle, q, b.PagedCache(k, v, ks, vs), table, lens_t, pack(seen, 7).cuda())
+    ok(handle)
+    kernel_was(handle, 400, e4m3)
+    assert_attention(o, lse, *tree_reference(q, k, v, ks, vs, table, [n], [0, n], [seen], dqk ** -0.5))
